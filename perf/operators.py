@@ -113,7 +113,7 @@ def draw(rng):
     half, scaling = rng.random() < 0.5, rng.choice(["none", "linear", "yarn"])
     context = _log(rng, 500, 131072) | 1
     if kind == "rope":
-        heads = rng.choice([8, 16, 28, 32, 32, 64])
+        heads = rng.choice([8, 20, 28, 32, 32, 64])
         d_nope, d_rope = rng.choice([(128, 64), (128, 64), (64, 32), (0, 128), (96, 40)])
         io = rng.choice(["bf16", "bf16", "f32"])
         tokens = _count(rng, 1, 32000)
