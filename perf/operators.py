@@ -262,7 +262,9 @@ def _run_own(s):
         layer.quantize_rows(s["x"], codes=s["codes"], scales=s["scales"])
         return {"codes": s["codes"], "scales": s["scales"]}
     if kind == "gemm":
-        layer.gemm_fp8(s["a"], s["a_scales"], s["w"], s["w_scales"], out=s["out"], workspace=s["ws"])
+        # a bf16 output is rounded a hundred times more coarsely than the matrix cores add 8-bit products
+        layer.gemm_fp8(s["a"], s["a_scales"], s["w"], s["w_scales"], out=s["out"], workspace=s["ws"],
+                       flags=layer.GEMM_FAST_SUMS if c["out"] == "bf16" else 0)
         return {"out": s["out"]}
     layout = layer.ROPE_HALF if c["half"] else layer.ROPE_INTERLEAVED
     if kind == "rope":
