@@ -1,0 +1,157 @@
+// Parameters and launchers of the operators around the attention (mla_layer_gfx950.h).
+#pragma once
+#include "mla_internal.h"
+#include "mla_layer_gfx950.h"
+
+namespace mla {
+
+constexpr int QBLOCK = 128;        // columns (and weight rows) per scale
+constexpr float E4M3_MAX = 448.f;
+
+struct NormParams {
+    const void* x;
+    const void* residual;      // or nullptr
+    const void* weight;        // or nullptr
+    void* residual_out;
+    void* y;                   // or nullptr
+    uint8_t* codes;            // or nullptr
+    float* scales;
+    int T, D;
+    int64_t x_pitch;
+    float eps;
+};
+
+struct GemmFp8Params {
+    const uint8_t* a;          // [M, K]
+    const float* a_scales;     // [ceil(K/128), M]
+    const uint8_t* w;          // [N, K]
+    const float* w_scales;     // [ceil(N/128), ceil(K/128)]
+    void* out;                 // [M, N]
+    float* part;               // workspace
+    int M, N, K;
+};
+
+struct RopeParams {
+    const void* q;
+    const int32_t* positions;
+    const double* freq;
+    void* q_nope;
+    void* q_rope;
+    int T, H, d_nope, d_rope;
+    int64_t pitch;
+    float gain;
+};
+
+struct StoreParams {
+    const void* rows;
+    const int32_t* positions;
+    const double* freq;
+    const void* norm_weight;   // or nullptr
+    void* kv;
+    float* kv_scale;
+    const int32_t* page_table;
+    int rows_total, new_tokens, d_c, d_rope, page_size, num_pages, max_pages;
+    int64_t pitch;
+    float gain, eps;
+};
+
+// the norm (norm = true) or the codes of x as it is
+hipError_t launch_rms_norm(const NormParams& p, bool norm, mla_dtype io, hipStream_t s);
+hipError_t launch_quantize_weights(const void* w, uint8_t* codes, float* scales, int N, int K, mla_dtype io, hipStream_t s);
+size_t     gemm_fp8_workspace(int M, int N, int K);
+hipError_t launch_gemm_fp8(const GemmFp8Params& p, mla_dtype out, bool fast_sums, hipStream_t s);
+hipError_t launch_rope_queries(const RopeParams& p, int layout, mla_dtype io, hipStream_t s);
+hipError_t launch_cache_store(const StoreParams& p, int layout, mla_dtype io, mla_dtype cache, hipStream_t s);
+
+// ---- device helpers
+
+// Eight consecutive values.  VEC: 16-byte accesses (the address allows them and all eight are there); otherwise one
+// by one, those at and past `left` read as zero and are not written.
+template <bool F32, bool VEC> __device__ __forceinline__ void load8(const void* base, int64_t at, int left, float (&v)[8])
+{
+    if constexpr (VEC && F32) {
+        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
+        const float4 a = src[0], b = src[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else if constexpr (VEC) {
+        const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = 0.f;
+            if (i < left) v[i] = F32 ? static_cast<const float*>(base)[at + i] : bf16_bits_to_f32(static_cast<const uint16_t*>(base)[at + i]);
+        }
+    }
+}
+
+// two values as bf16, each rounded to nearest even (v_cvt_pk_bf16_f32)
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
+{
+    typedef __attribute__((ext_vector_type(2))) float f2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 b2;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){lo, hi}, b2));
+}
+
+template <bool F32, bool VEC> __device__ __forceinline__ void store8(void* base, int64_t at, int left, const float (&v)[8])
+{
+    if constexpr (VEC && F32) {
+        float4* dst = reinterpret_cast<float4*>(static_cast<float*>(base) + at);
+        dst[0] = make_float4(v[0], v[1], v[2], v[3]);
+        dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else if constexpr (VEC) {
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + at) =
+            make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) {
+                if (F32) static_cast<float*>(base)[at + i] = v[i];
+                else     static_cast<uint16_t*>(base)[at + i] = (uint16_t)f32_to_bf16_bits(v[i]);
+            }
+    }
+}
+
+// four values as e4m3 codes, rounded to nearest even; magnitudes up to 464 (exclusive) give at most 448
+__device__ __forceinline__ uint32_t e4m3_quad(float a, float b, float c, float d)
+{
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+}
+
+// bits of |v|: as integers they order as the magnitudes do, with NaN above infinity, so that a maximum keeps a NaN
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// maximum over the 16 lanes of a row, on every lane of it
+__device__ __forceinline__ uint32_t row_max(uint32_t v)
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, false));   // row_ror:8, 4, 2, 1
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, false));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, false));
+}
+
+// Scale of a block whose largest magnitude has these bits.  At least 2^-126, so that the scale and its reciprocal are
+// normal numbers: value * (1 / scale) is then value / scale within two roundings of 2^-24 before the code's own of 2^-4.
+__device__ __forceinline__ float block_scale(uint32_t top)
+{
+    const float m = __uint_as_float(top);
+    if (top == 0) return 1.f;
+    const float s = m / E4M3_MAX;
+    return s < 1.17549435e-38f ? 1.17549435e-38f : s;      // (a NaN stays)
+}
+
+// Cosine and sine of position * freq, times gain.  The number of turns is formed and reduced in fp64 (positions reach
+// 10^5 radians, where fp32 has no digits left); what is left, in [-1/2, 1/2], loses 2^-25 of a turn as fp32.
+__device__ __forceinline__ void turn_of(int position, double freq, float gain, float& cs, float& sn)
+{
+    const double turns = (double)position * (freq * 0.15915494309189533577);
+    const float r = (float)(turns - rint(turns));
+    sincospif(2.f * r, &sn, &cs);
+    cs *= gain;
+    sn *= gain;
+}
+
+}  // namespace mla

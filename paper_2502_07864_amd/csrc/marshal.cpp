@@ -1,4 +1,4 @@
-// Argument marshalling of the serving calls (mla.py) in native code.
+// Argument marshalling of the serving calls (mla.py, layer.py) in native code.
 //
 // A decode step is three calls whose kernels together take 14 to 20 us at small sizes; checking the tensors,
 // asking for the stream and converting some twenty arguments each in Python took 6 to 8 us per call, so that
@@ -13,6 +13,7 @@
 #include <c10/hip/HIPStream.h>
 
 #include "mla_gfx950.h"
+#include "mla_layer_gfx950.h"
 
 namespace {
 
@@ -22,6 +23,11 @@ decltype(&mla_decode_paged_multi) p_decode;
 decltype(&mla_merge_out_proj_multi) p_merge_out_proj;
 decltype(&mla_merge_partials) p_merge_partials;
 decltype(&mla_cache_append) p_append;
+decltype(&mla_rms_norm) p_rms_norm;
+decltype(&mla_quantize_rows) p_quantize;
+decltype(&mla_gemm_fp8) p_gemm_fp8;
+decltype(&mla_rope_queries) p_rope;
+decltype(&mla_cache_store) p_store;
 
 struct No {};   // the arguments are not of the plain kind
 
@@ -224,22 +230,174 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
-// (addresses of the six entry points, in the order above)
+// ---- the operators around the attention (layer.py)
+
+// a tensor on the GPU whose last axis is dense
+const at::Tensor& dense_rows(PyObject* o)
+{
+    if (!THPVariable_CheckExact(o)) throw No();
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.dim() < 1 || (t.stride(-1) != 1 && t.size(-1) != 1)) throw No();
+    return t;
+}
+bool is_codes(const at::Tensor& t) { return t.scalar_type() == at::kFloat8_e4m3fn || t.scalar_type() == at::kByte; }
+int64_t scale_blocks(int64_t n) { return (n + 127) / 128; }
+
+// distance of the rows of x [T, D]
+int64_t row_pitch(const at::Tensor& x) { return x.size(0) > 1 ? x.stride(0) : x.size(1); }
+
+// (x [T, D], weight | None, eps, residual | None, residual_out | None, out | None, codes | None, scales | None)
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        require(n == 8);
+        const at::Tensor& x = dense_rows(a[0]);
+        require(x.dim() == 2 && (a[3] == Py_None) == (a[4] == Py_None) && (a[6] == Py_None) == (a[7] == Py_None));
+        const int64_t T = x.size(0), D = x.size(1);
+        const mla_dtype io = io_type(x);
+        const void *pw = nullptr, *pr = nullptr;
+        if (a[1] != Py_None) {
+            const at::Tensor& w = tensor(a[1]);
+            require(w.dim() == 1 && w.size(0) == D && w.scalar_type() == x.scalar_type());
+            pw = w.data_ptr();
+        }
+        if (a[3] != Py_None) {
+            const at::Tensor& r = tensor(a[3]);
+            require(r.dim() == 2 && r.size(0) == T && r.size(1) == D && r.scalar_type() == x.scalar_type());
+            pr = r.data_ptr();
+        }
+        void *pro = room_or_null(a[4], T * D, size_of(io)), *py = room_or_null(a[5], T * D, size_of(io)), *pc = room_or_null(a[6], T * D, 1),
+             *ps = room_or_null(a[7], T * scale_blocks(D), 4), *px = x.data_ptr(), *s = stream_of(x);
+        const int t = dim(T), d = dim(D);
+        const int64_t pitch = row_pitch(x);
+        const float eps = real(a[2]);
+        return unlocked([&] { return p_rms_norm(px, pr, pw, pro, py, static_cast<uint8_t*>(pc), static_cast<float*>(ps), t, d, pitch, eps, io, s); });
+    });
+}
+
+// (x [T, D], codes, scales)
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        require(n == 3);
+        const at::Tensor& x = dense_rows(a[0]);
+        require(x.dim() == 2);
+        const int64_t T = x.size(0), D = x.size(1);
+        const mla_dtype io = io_type(x);
+        void *px = x.data_ptr(), *pc = room(a[1], T * D, 1), *ps = room(a[2], T * scale_blocks(D), 4), *s = stream_of(x);
+        const int t = dim(T), d = dim(D);
+        const int64_t pitch = row_pitch(x);
+        return unlocked([&] { return p_quantize(px, static_cast<uint8_t*>(pc), static_cast<float*>(ps), t, d, pitch, io, s); });
+    });
+}
+
+// (a [M, K], a_scales, w [N, K], w_scales, out, workspace | None, flags)
+PyObject* gemm_fp8(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        require(n == 7);
+        const at::Tensor &x = tensor(a[0]), &xs = tensor(a[1]), &w = tensor(a[2]), &ws = tensor(a[3]), &out = tensor(a[4]);
+        require(x.dim() == 2 && w.dim() == 2 && is_codes(x) && is_codes(w) && x.size(1) == w.size(1));
+        const int M = dim(x.size(0)), N = dim(w.size(0)), K = dim(x.size(1));
+        require(xs.scalar_type() == at::kFloat && xs.dim() == 2 && xs.size(0) == scale_blocks(K) && xs.size(1) == M);
+        require(ws.scalar_type() == at::kFloat && ws.dim() == 2 && ws.size(0) == scale_blocks(N) && ws.size(1) == scale_blocks(K));
+        const mla_dtype io = io_type(out);
+        require(out.numel() >= (int64_t)M * N);
+        void *px = x.data_ptr(), *pxs = xs.data_ptr(), *pw = w.data_ptr(), *pws = ws.data_ptr(), *po = out.data_ptr(), *pk = nullptr, *s = stream_of(x);
+        size_t bytes = 0;
+        const int flags = (int)integer(a[6]);
+        if (a[5] != Py_None) {
+            const at::Tensor& k = tensor(a[5]);
+            pk = k.data_ptr();
+            bytes = k.nbytes();
+        }
+        return unlocked([&] {
+            return p_gemm_fp8(static_cast<uint8_t*>(px), static_cast<float*>(pxs), static_cast<uint8_t*>(pw), static_cast<float*>(pws), po, pk, bytes, M,
+                              N, K, io, (unsigned)flags, s);
+        });
+    });
+}
+
+// (q [T, H, d_nope + d_rope], positions, freq, gain, layout, q_nope | None, q_rope)
+PyObject* rope_queries(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        require(n == 7);
+        const at::Tensor &q = dense_rows(a[0]), &pos = tensor(a[1]), &freq = tensor(a[2]);
+        require(q.dim() == 3 && pos.scalar_type() == at::kInt && freq.scalar_type() == at::kDouble && freq.dim() == 1);
+        const int64_t T = q.size(0), H = q.size(1), width = q.size(2), d_rope = 2 * freq.size(0), d_nope = width - d_rope;
+        require(d_nope >= 0 && (H == 1 || q.stride(1) == width) && pos.dim() == 1 && pos.size(0) == T);
+        const mla_dtype io = io_type(q);
+        void *pn = room_or_null(a[5], T * H * d_nope, size_of(io)), *pr = room(a[6], T * H * d_rope, size_of(io));
+        require(pn || d_nope == 0);
+        void *pq = q.data_ptr(), *s = stream_of(q);
+        const auto* pp = static_cast<const int32_t*>(pos.data_ptr());
+        const auto* pf = static_cast<const double*>(freq.data_ptr());
+        const int t = dim(T), h = dim(H), dn = dim(d_nope), dr = dim(d_rope), layout = (int)integer(a[4]);
+        const int64_t pitch = T > 1 ? q.stride(0) : H * width;
+        const float gain = real(a[3]);
+        return unlocked([&] { return p_rope(pq, pp, pf, pn, pr, t, h, dn, dr, pitch, gain, layout, io, s); });
+    });
+}
+
+// (rows [B, new, d_c + d_rope], positions, freq, kv_cache, page_table, d_c, gain, layout, norm_weight | None, eps, kv_scale | None)
+PyObject* cache_store(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        require(n == 11);
+        const at::Tensor &x = dense_rows(a[0]), &pos = tensor(a[1]), &freq = tensor(a[2]), &kv = tensor(a[3]), &table = tensor(a[4]);
+        require(x.dim() == 3 && kv.dim() == 3 && table.dim() == 2 && x.size(2) == kv.size(2));
+        const int64_t B = x.size(0), T = x.size(1), row = x.size(2), d_c = integer(a[5]), d_rope = row - d_c;
+        require(d_c > 0 && d_rope >= 0 && pos.scalar_type() == at::kInt && pos.dim() == 2 && pos.size(0) == B && pos.size(1) == T);
+        require(freq.scalar_type() == at::kDouble && freq.dim() == 1 && 2 * freq.size(0) == d_rope && table.scalar_type() == at::kInt && table.size(0) == B);
+        const int64_t pitch = T > 1 ? x.stride(1) : B > 1 ? x.stride(0) : row;
+        require(B == 1 || T == 1 || x.stride(0) == T * pitch);
+        const mla_dtype io = io_type(x), cache = cache_type(kv);
+        const void* pw = nullptr;
+        if (a[8] != Py_None) {
+            const at::Tensor& w = tensor(a[8]);
+            require(w.dim() == 1 && w.size(0) == d_c && w.scalar_type() == x.scalar_type());
+            pw = w.data_ptr();
+        }
+        float* ps = nullptr;
+        if (a[10] != Py_None) {
+            const at::Tensor& s = tensor(a[10]);
+            require(s.scalar_type() == at::kFloat && s.dim() == 2 && s.size(0) == kv.size(0) && s.size(1) == kv.size(1));
+            ps = static_cast<float*>(s.data_ptr());
+        }
+        void *px = x.data_ptr(), *pkv = kv.data_ptr(), *s = stream_of(x);
+        const auto* pp = static_cast<const int32_t*>(pos.data_ptr());
+        const auto* pf = static_cast<const double*>(freq.data_ptr());
+        const auto* pt = static_cast<const int32_t*>(table.data_ptr());
+        const int b = dim(B), t = dim(T), dc = dim(d_c), dr = dim(d_rope), page = dim(kv.size(1)), pages = dim(kv.size(0)), mp = dim(table.size(1)),
+                  layout = (int)integer(a[7]);
+        const float gain = real(a[6]), eps = real(a[9]);
+        return unlocked([&] { return p_store(px, pp, pf, pw, pkv, ps, pt, b, t, dc, dr, pitch, page, pages, mp, gain, layout, eps, io, cache, s); });
+    });
+}
+
+// (addresses of the eleven entry points, in the order above)
 PyObject* bind(PyObject*, PyObject* args)
 {
-    unsigned long long p[6];
-    if (!PyArg_ParseTuple(args, "KKKKKK", p, p + 1, p + 2, p + 3, p + 4, p + 5)) return nullptr;
+    unsigned long long p[11];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKK", p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6, p + 7, p + 8, p + 9, p + 10)) return nullptr;
     p_absorb_q = reinterpret_cast<decltype(p_absorb_q)>(p[0]);
     p_out_proj = reinterpret_cast<decltype(p_out_proj)>(p[1]);
     p_decode = reinterpret_cast<decltype(p_decode)>(p[2]);
     p_merge_out_proj = reinterpret_cast<decltype(p_merge_out_proj)>(p[3]);
     p_merge_partials = reinterpret_cast<decltype(p_merge_partials)>(p[4]);
     p_append = reinterpret_cast<decltype(p_append)>(p[5]);
+    p_rms_norm = reinterpret_cast<decltype(p_rms_norm)>(p[6]);
+    p_quantize = reinterpret_cast<decltype(p_quantize)>(p[7]);
+    p_gemm_fp8 = reinterpret_cast<decltype(p_gemm_fp8)>(p[8]);
+    p_rope = reinterpret_cast<decltype(p_rope)>(p[9]);
+    p_store = reinterpret_cast<decltype(p_store)>(p[10]);
     Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(absorb_q), FAST(out_proj), FAST(decode), FAST(merge_out_proj), FAST(merge_partials), FAST(cache_append),
+                         FAST(rms_norm), FAST(quantize_rows), FAST(gemm_fp8), FAST(rope_queries), FAST(cache_store),
                          {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 

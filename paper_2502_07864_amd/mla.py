@@ -28,7 +28,10 @@ EXPORTS = ("mla_status_string", "mla_version", "mla_absorb_q", "mla_out_proj",
            "mla_decode_workspace_bytes", "mla_decode_paged", "mla_merge_partials",
            "mla_merge_out_proj", "mla_gather_paged", "mla_append_workspace_bytes", "mla_cache_append",
            "mla_decode_paged_multi", "mla_merge_out_proj_multi", "mla_prefill_workspace_bytes", "mla_prefill_mha",
-           "mla_static_scratch_bytes", "mla_decode_paged_static", "mla_diag_stream_tiles")
+           "mla_static_scratch_bytes", "mla_decode_paged_static", "mla_diag_stream_tiles",
+           # the operators around the attention (include/mla_layer_gfx950.h), called from layer.py
+           "mla_rms_norm", "mla_quantize_rows", "mla_quantize_weights", "mla_gemm_fp8_workspace_bytes", "mla_gemm_fp8",
+           "mla_rope_frequencies", "mla_rope_queries", "mla_cache_store")
 
 
 class MlaError(RuntimeError):
@@ -47,7 +50,8 @@ def _load_marshal(L: ctypes.CDLL):
         return None
     _marshal.bind(*(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in
                     ("mla_absorb_q", "mla_out_proj", "mla_decode_paged_multi", "mla_merge_out_proj_multi",
-                     "mla_merge_partials", "mla_cache_append")))
+                     "mla_merge_partials", "mla_cache_append", "mla_rms_norm", "mla_quantize_rows", "mla_gemm_fp8",
+                     "mla_rope_queries", "mla_cache_store")))
     return _marshal
 
 
@@ -100,6 +104,23 @@ def lib() -> ctypes.CDLL:
         L.mla_cache_append.restype = i
         L.mla_cache_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t,
                                        i, i, i, i, i, i, i, f, i, i, vp]
+        i64, d = ctypes.c_int64, ctypes.c_double
+        L.mla_rms_norm.restype = i
+        L.mla_rms_norm.argtypes = [vp] * 7 + [i, i, i64, f, i, vp]
+        L.mla_quantize_rows.restype = i
+        L.mla_quantize_rows.argtypes = [vp, vp, vp, i, i, i64, i, vp]
+        L.mla_quantize_weights.restype = i
+        L.mla_quantize_weights.argtypes = [vp, vp, vp, i, i, i, vp]
+        L.mla_gemm_fp8_workspace_bytes.restype = ctypes.c_size_t
+        L.mla_gemm_fp8_workspace_bytes.argtypes = [i, i, i]
+        L.mla_gemm_fp8.restype = i
+        L.mla_gemm_fp8.argtypes = [vp] * 6 + [ctypes.c_size_t, i, i, i, i, u, vp]
+        L.mla_rope_frequencies.restype = i
+        L.mla_rope_frequencies.argtypes = [vp, vp, i, d, i, d, i, d, d]
+        L.mla_rope_queries.restype = i
+        L.mla_rope_queries.argtypes = [vp] * 5 + [i, i, i, i, i64, f, i, i, vp]
+        L.mla_cache_store.restype = i
+        L.mla_cache_store.argtypes = [vp] * 7 + [i, i, i, i, i64, i, i, i, f, i, f, i, i, vp]
         _lib, _fast = L, _load_marshal(L)
     return _lib
 

@@ -1,0 +1,634 @@
+"""Operators around the attention on the GPU, against plain implementations in 64 bits.
+
+Tolerances follow from the arithmetic: one rounding to bf16 is at most 2^-8 of the value, one to e4m3 2^-4 of it (2^-10
+of the scale below the smallest normal code), and sums of n terms in fp32 are within n 2^-24 of the sum of magnitudes.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2502_07864_amd import layer, mla
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+BF, F32, FP8 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+ROUND = {BF: 2.0 ** -8, F32: 2.0 ** -24}
+SUM = 1e-5            # the norm: a sum of squares in fp32 (at most 128 in a row per thread, then a tree), one root, three products
+
+
+def rnd(*shape, dtype=F32, seed=0, loud=False):
+    g = torch.Generator().manual_seed(seed + 17 * sum(shape))
+    x = torch.randn(shape, generator=g)
+    if loud and shape[-1] > 4:
+        x[..., :3] *= 15.0
+    return x.to(dtype).to(DEV)
+
+
+def near(got, want, rel, floor=0.0):
+    """|got - want| <= rel |want| + floor everywhere (floor: a number or a tensor)."""
+    got, want = got.double(), want.double()
+    bad = (got - want).abs() > rel * want.abs() + floor
+    assert not bad.any(), (int(bad.sum()), float(((got - want).abs() - rel * want.abs()).max()))
+
+
+def ref_norm(x, weight, eps, residual=None):
+    s = x.double() + (residual.double() if residual is not None else 0.0)
+    y = s / (s.square().mean(-1, keepdim=True) + eps).sqrt()
+    return s, y * weight.double() if weight is not None else y
+
+
+def blocks(n):
+    return -(-n // 128)
+
+
+def spread(scales, D):
+    """scales [blocks, T] -> [T, D]"""
+    return scales.double().repeat_interleave(128, 0)[:D].t()
+
+
+def check_codes(codes, scales, y, rel):
+    """Codes and scales of y (fp64), of which the kernel knows every value within rel."""
+    T, D = y.shape
+    assert tuple(scales.shape) == (blocks(D), T)
+    pad = torch.nn.functional.pad(y, (0, blocks(D) * 128 - D)).view(T, -1, 128)
+    top = pad.abs().amax(-1).t()
+    want = torch.where(top > 0, top / 448.0, torch.ones_like(top))
+    near(scales, want, rel + 2.0 ** -23)
+    unit = spread(scales, D)
+    v = y / unit
+    q = codes.view(FP8).double()
+    off = (q - v).abs()
+    assert (off <= torch.maximum(v.abs() * 2.0 ** -4, torch.full_like(v, 2.0 ** -10)) * (1 + 1e-3) + v.abs() * 2 * rel).all(), float(off.max())
+    assert (q.abs() <= 448.0).all()
+
+
+# ------------------------------------------------------------------ norm
+
+@pytest.mark.parametrize("io", [BF, F32])
+@pytest.mark.parametrize("T, D", [(1, 4096), (3, 1), (5, 7), (2, 65), (7, 128), (4, 129), (33, 1000), (61, 3584), (2, 5120), (3, 8192),
+                                  (2, 12296), (2, 16384), (1, 32768), (1500, 2048), (2049, 4096), (1030, 300), (1100, 8200), (1027, 1003)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_norm(T, D, io, residual):
+    x, w = rnd(T, D, dtype=io, loud=True), (1 + 0.3 * rnd(D, seed=1)).to(io)
+    r = rnd(T, D, dtype=io, seed=2) if residual else None
+    s, y = ref_norm(x, w, 1e-5, r)
+    got, got_s = layer.rms_norm(x, w, 1e-5, residual=r)
+    near(got, y, ROUND[io] + SUM)
+    if residual:
+        near(got_s, s, ROUND[io], 2.0 ** -24 * (x.double().abs() + r.double().abs()))
+    else:
+        assert got_s is None
+    codes, scales, s8, y8 = layer.rms_norm_fp8(x, w, 1e-5, residual=r, out=torch.empty_like(x))
+    assert torch.equal(y8, got) and (not residual or torch.equal(s8, got_s))       # the same numbers, codes beside them
+    check_codes(codes, scales, y, SUM)
+    codes2, scales2, _, y2 = layer.rms_norm_fp8(x, w, 1e-5, residual=r)
+    assert y2 is None and torch.equal(codes2.view(torch.uint8), codes.view(torch.uint8)) and torch.equal(scales2, scales)
+
+
+@pytest.mark.parametrize("io", [BF, F32])
+@pytest.mark.parametrize("T, D", [(1, 4096), (16, 3584), (5, 7), (2, 129), (1300, 2048), (1100, 4104)])
+def test_quantize_rows(T, D, io):
+    x = rnd(T, D, dtype=io, loud=True)
+    codes, scales = layer.quantize_rows(x)
+    check_codes(codes, scales, x.double(), 0.0)
+
+
+def test_norm_without_weight_and_strided_rows():
+    wide = rnd(40, 3 * 1000, dtype=BF)[:, 512:512 + 1000]
+    y, _ = layer.rms_norm(wide)
+    near(y, ref_norm(wide, None, 1e-6)[1], ROUND[BF] + SUM)
+    odd = rnd(40, 1029, dtype=F32)[:, 3:1003]            # neither the rows nor their distance on 16 bytes
+    codes, scales = layer.quantize_rows(odd)
+    check_codes(codes, scales, odd.double(), 0.0)
+
+
+def test_norm_in_place():
+    x, r, w = rnd(70, 4096, dtype=BF), rnd(70, 4096, dtype=BF, seed=3), rnd(4096, dtype=BF, seed=4)
+    want, want_s = layer.rms_norm(x, w, residual=r)
+    y, s = layer.rms_norm(x, w, residual=r, residual_out=r, out=x)
+    assert y is x and s is r and torch.equal(x, want) and torch.equal(r, want_s)
+
+
+def test_norm_values_that_can_go_wrong():
+    """Zeros, tiny and huge values, infinities and NaN stay inside their row and block."""
+    x = rnd(8, 512, dtype=F32)
+    x[0] = 0.0
+    x[1, :128] = 0.0
+    x[2] *= 1e-41                     # every value and every scale below the smallest normal number
+    x[3] *= 1e37
+    x[4, 5] = math.inf
+    x[5, 300] = math.nan
+    codes, scales = layer.quantize_rows(x)
+    q = codes.double() * spread(scales, 512)
+    ok = [0, 1, 3, 6, 7]
+    check_codes(codes[ok], scales[:, ok].contiguous(), x[ok].double(), 0.0)
+    assert (scales[:, 0] == 1).all() and scales[0, 1] == 1 and not codes[0].double().any()
+    assert (scales[:, 2] > 0).all() and (q[2] - x[2].double()).abs().max() <= 2.0 ** -126 * 2.0 ** -10
+    assert not torch.isfinite(scales[0, 4]) and torch.isfinite(scales[1:, 4]).all()
+    assert torch.isnan(scales[2, 5]) and torch.isfinite(scales[[0, 1, 3], 5]).all()
+    assert not torch.isfinite(q[4, :128]).any() or torch.isnan(q[4, :128]).any()
+    y, _ = layer.rms_norm(x, eps=1e-6)
+    assert (y[0] == 0).all() and torch.isnan(y[5]).all() and torch.isfinite(y[[0, 1, 6, 7]]).all()
+
+
+def test_norm_rows_past_32_bits():
+    """Elements whose index passes 2^31 (bf16: their offset passes 2^32 bytes)."""
+    T, D = (1 << 31) // 4096 + 300, 4096
+    x = torch.zeros((T, D), dtype=BF, device=DEV)
+    tail = rnd(300, D, dtype=BF)
+    x[-300:] = tail
+    codes, scales = layer.quantize_rows(x)
+    want_c, want_s = layer.quantize_rows(tail)
+    assert torch.equal(codes[-300:].view(torch.uint8), want_c.view(torch.uint8)) and torch.equal(scales[:, -300:], want_s)
+    y, _ = layer.rms_norm(x, out=x)
+    near(y[-300:], ref_norm(tail, None, 1e-6)[1], ROUND[BF] + SUM)
+
+
+@pytest.mark.parametrize("io", [BF, F32])
+@pytest.mark.parametrize("N, K", [(128, 128), (1, 16), (130, 300), (576, 4096), (257, 1000)])
+def test_quantize_weights(N, K, io):
+    w = rnd(N, K, dtype=io)
+    w[: min(N, 128), : min(K, 128)] = 0.0
+    codes, scales = layer.quantize_weights(w)
+    p = torch.nn.functional.pad(w.double(), (0, blocks(K) * 128 - K, 0, blocks(N) * 128 - N)).view(blocks(N), 128, blocks(K), 128)
+    top = p.abs().amax((1, 3))
+    near(scales, torch.where(top > 0, top / 448, torch.ones_like(top)), 2.0 ** -23)
+    unit = scales.double().repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K]
+    v = w.double() / unit
+    assert ((codes.double() - v).abs() <= torch.maximum(v.abs() * 2.0 ** -4, torch.full_like(v, 2.0 ** -10)) * (1 + 1e-3)).all()
+
+
+# ------------------------------------------------------------------ product
+
+def operands(M, N, K, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed + M + N + K)
+    a = torch.randn((M, K), generator=g, device=DEV).mul_(40).clamp_(-448, 448).to(FP8)
+    w = torch.randn((N, K), generator=g, device=DEV).mul_(40).clamp_(-448, 448).to(FP8)
+    sa = torch.rand((blocks(K), M), generator=g, device=DEV) * 0.02 + 1e-3
+    sw = torch.rand((blocks(N), blocks(K)), generator=g, device=DEV) * 0.02 + 1e-3
+    return a, sa, w, sw
+
+
+def dequantised(a, sa, w, sw):
+    K, N = a.shape[1], w.shape[0]
+    return (a.double() * spread(sa, K),
+            w.double() * sw.double().repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K])
+
+
+def check_gemm(M, N, K, dtype, seed=0, out=None):
+    a, sa, w, sw = operands(M, N, K, seed)
+    got = layer.gemm_fp8(a, sa, w, sw, dtype=dtype, out=out)
+    assert got.dtype == dtype and tuple(got.shape) == (M, N)
+    A, W = dequantised(a, sa, w, sw)
+    size = torch.mm(A.abs(), W.abs().t().contiguous())
+    near(got, torch.mm(A, W.t().contiguous()), ROUND[dtype], (140 + blocks(K)) * 2.0 ** -24 * size)
+    return a, sa, w, sw, got
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("M, N, K", [
+    (1, 1, 16), (1, 6144, 4096), (2, 576, 4096), (3, 33, 48), (7, 320, 1008), (16, 576, 4096), (17, 129, 128), (31, 4096, 1024), (33, 2049, 2064),
+    (61, 3584, 3584), (64, 128, 5120), (65, 127, 144), (100, 5376, 3584), (128, 576, 256), (129, 1000, 1616), (200, 320, 7168), (255, 257, 384),
+    (256, 256, 128), (257, 6144, 512), (500, 5376, 1040), (1000, 1536, 4096), (1025, 2561, 640), (4000, 576, 3584), (4097, 1280, 2048)])
+def test_gemm(M, N, K, dtype):
+    check_gemm(M, N, K, dtype)
+
+
+@pytest.mark.parametrize("K", [16, 32, 112, 128, 144, 240, 256, 272, 384, 400, 496, 512, 528, 1024, 1040, 2032, 2048, 4080])
+@pytest.mark.parametrize("M, N", [(5, 70), (40, 200), (300, 300)])
+def test_gemm_depths(M, N, K):
+    """Every position of the end of K against the blocks and the steps."""
+    check_gemm(M, N, K, F32)
+
+
+@pytest.mark.parametrize("M", [1, 8, 15, 16, 17, 32, 47, 48, 49, 63, 64, 65, 80, 96, 97, 127, 128, 129, 160, 192, 193, 256, 300, 384, 511, 512, 513])
+def test_gemm_rows(M):
+    check_gemm(M, 576, 1152, BF)
+
+
+@pytest.mark.parametrize("M, N, K", [(1, 2048, 1024), (20, 640, 2048), (300, 512, 1024), (2000, 1024, 512)])
+def test_gemm_exact(M, N, K):
+    """Small whole numbers and scales that are powers of two: every sum is exact in fp32, whatever its order."""
+    g = torch.Generator(device=DEV).manual_seed(M)
+    a = torch.randint(-3, 4, (M, K), generator=g, device=DEV).float()
+    w = torch.randint(-3, 4, (N, K), generator=g, device=DEV).float()
+    sa = torch.exp2(torch.randint(-2, 3, (blocks(K), M), generator=g, device=DEV).float())
+    sw = torch.exp2(torch.randint(-2, 3, (blocks(N), blocks(K)), generator=g, device=DEV).float())
+    got = layer.gemm_fp8(a.to(FP8), sa, w.to(FP8), sw, dtype=F32)
+    A, W = dequantised(a, sa, w, sw)
+    assert torch.equal(got.double(), torch.mm(A, W.t().contiguous()))
+
+
+def test_gemm_each_code_and_place():
+    """Every finite code as either operand, and a unit at each k: which column goes with which."""
+    codes = torch.arange(256, dtype=torch.uint8, device=DEV)
+    codes[0x7F], codes[0xFF] = 0, 0
+    a = torch.zeros((256, 256), dtype=torch.uint8, device=DEV)
+    a[:, 37] = codes
+    eye = torch.eye(256, device=DEV).to(FP8)
+    one = torch.ones((2, 256), device=DEV)
+    got = layer.gemm_fp8(a, one, eye, one[:, :2].contiguous(), dtype=F32)
+    want = torch.zeros((256, 256), dtype=torch.float64, device=DEV)
+    want[:, 37] = codes.view(FP8).double()
+    assert torch.equal(got.double(), want)
+    full = torch.randint(0, 120, (256, 256), dtype=torch.uint8, device=DEV)
+    assert torch.equal(layer.gemm_fp8(full, one, eye, one[:, :2].contiguous(), dtype=F32).double(), full.view(FP8).double())
+    assert torch.equal(layer.gemm_fp8(eye, one, full, one[:, :2].contiguous(), dtype=F32).double(), full.view(FP8).double().t())
+
+
+@pytest.mark.parametrize("M, N, K", [(4, 576, 1024), (70, 320, 640), (600, 512, 512)])
+def test_gemm_values_that_can_go_wrong(M, N, K):
+    """A scale that is not finite reaches its own token or output block and nothing else; tiny and huge scales keep
+    their digits; zero blocks are zeros."""
+    a, sa, w, sw = operands(M, N, K)
+    sa[1, 2] = math.inf
+    sa[0, 3] = math.nan
+    sw[1, 0] = math.nan
+    got = layer.gemm_fp8(a, sa, w, sw, dtype=F32)
+    bad = torch.zeros((M, N), dtype=torch.bool, device=DEV)
+    bad[2], bad[3], bad[:, 128:256] = True, True, True
+    assert (torch.isfinite(got) == ~bad).all()
+    a, sa, w, sw = operands(M, N, K)
+    sa[0] *= 1e-12
+    sa[1] *= 1e12
+    sw[:, 1] *= 1e-12
+    A, W = dequantised(a, sa, w, sw)
+    near(layer.gemm_fp8(a, sa, w, sw, dtype=F32), torch.mm(A, W.t().contiguous()), 0.0,
+         (140 + blocks(K)) * 2.0 ** -24 * torch.mm(A.abs(), W.abs().t().contiguous()))
+    zero = torch.zeros_like(a)
+    assert not layer.gemm_fp8(zero, sa, w, sw, dtype=F32).any()
+
+
+@pytest.mark.parametrize("M, N, K", [(3, 600, 2048), (61, 576, 4096), (100, 320, 1040), (1000, 700, 528)])
+def test_gemm_writes_its_outputs_and_nothing_else(M, N, K):
+    a, sa, w, sw = operands(M, N, K)
+    need = layer.gemm_fp8_workspace_bytes(M, N, K)
+    room = torch.full((M * N + 512,), 7.0, dtype=BF, device=DEV)
+    out = room[256:256 + M * N].view(M, N)
+    scratch = torch.full((need + 512,), 0xAB, dtype=torch.uint8, device=DEV)
+    layer.gemm_fp8(a, sa, w, sw, out=out, workspace=scratch[256:256 + need] if need else scratch[:0])
+    assert (room[:256] == 7).all() and (room[256 + M * N:] == 7).all()
+    assert (scratch[:256] == 0xAB).all() and (scratch[256 + need:] == 0xAB).all()
+    again = layer.gemm_fp8(a, sa, w, sw)                   # and whatever the scratch held before
+    assert torch.equal(out, again)
+
+
+def test_gemm_odd_output_address():
+    """Rows of N odd bf16 values start on any even byte."""
+    M, N, K = 300, 577, 512
+    room = torch.empty(M * N + 1, dtype=BF, device=DEV)
+    check_gemm(M, N, K, BF, out=room[1:].view(M, N))
+
+
+@pytest.mark.parametrize("M, N, K", [(350208, 6160, 128), (66000, 32768, 16)])
+def test_gemm_outputs_past_32_bits(M, N, K):
+    a, sa, w, sw = operands(M, N, K)
+    got = layer.gemm_fp8(a, sa, w, sw)
+    for rows in (slice(0, 300), slice(M - 300, M)):
+        A, W = dequantised(a[rows], sa[:, rows].contiguous(), w, sw)
+        near(got[rows], torch.mm(A, W.t().contiguous()), ROUND[BF], (140 + blocks(K)) * 2.0 ** -24 * torch.mm(A.abs(), W.abs().t().contiguous()))
+
+
+def test_gemm_operands_past_32_bits():
+    M, N, K = 530000, 64, 4096 + 16
+    a = torch.zeros((M, K), dtype=torch.uint8, device=DEV)
+    tail, sa, w, sw = operands(200, N, K)
+    a[-200:] = tail.view(torch.uint8)
+    scales = torch.ones((blocks(K), M), device=DEV)
+    scales[:, -200:] = sa
+    got = layer.gemm_fp8(a, scales, w, sw, dtype=F32)
+    A, W = dequantised(tail, sa, w, sw)
+    near(got[-200:], torch.mm(A, W.t().contiguous()), 0.0, (140 + blocks(K)) * 2.0 ** -24 * torch.mm(A.abs(), W.abs().t().contiguous()))
+    assert not got[:-200].any()
+
+
+# ------------------------------------------------------------------ rotation
+
+def turned(x, positions, freq, gain, layout):
+    """x [..., d] with positions broadcastable to x's leading axes."""
+    a = positions.double()[..., None] * freq
+    d = x.shape[-1]
+    x = x.double()
+    re, im = (x[..., :d // 2], x[..., d // 2:]) if layout == layer.ROPE_HALF else (x[..., 0::2], x[..., 1::2])
+    p = ((re * a.cos() - im * a.sin()) * gain, (re * a.sin() + im * a.cos()) * gain)
+    m = ((re.abs() + im.abs()) * gain,) * 2
+    join = (lambda q: torch.cat(q, -1)) if layout == layer.ROPE_HALF else (lambda q: torch.stack(q, -1).flatten(-2))
+    return join(p), join(m)
+
+
+TURN = 2e-6    # an angle known to 2^-25 of a turn (1.9e-7), its sine and cosine in fp32, gain, two products and a sum; of |re| + |im|
+
+
+@pytest.mark.parametrize("io", [BF, F32])
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("T, H, dn, dr", [(1, 32, 128, 64), (16, 28, 128, 64), (5, 1, 128, 64), (3, 8, 0, 128), (7, 3, 96, 40), (9, 5, 33, 6),
+                                          (2, 2, 1, 2), (300, 16, 64, 32), (1100, 4, 128, 64), (2, 3, 7, 256), (513, 40, 128, 64)])
+def test_rope_queries(T, H, dn, dr, layout, io):
+    q = rnd(T, H, dn + dr, dtype=io)
+    pos = torch.randint(0, 131072, (T,), generator=torch.Generator().manual_seed(T)).to(torch.int32).to(DEV)
+    pos[0] = 131071
+    freq, gain = layer.rope_frequencies(dr, scaling="yarn", factor=32.0)
+    qn, qr = layer.rope_queries(q, pos, freq, gain, layout)
+    assert torch.equal(qn, q[..., :dn])
+    want, size = turned(q[..., dn:], pos[:, None].expand(T, H), freq, gain, layout)
+    near(qr, want, ROUND[io], TURN * size)
+
+
+def test_rope_positions():
+    """Position 0 turns nothing, opposite positions undo each other, the far ends of int32 work."""
+    q = rnd(4, 3, 192, dtype=F32)
+    freq, _ = layer.rope_frequencies(64)
+    at = lambda *p: torch.tensor(p, dtype=torch.int32, device=DEV)
+    _, qr = layer.rope_queries(q, at(0, 0, 0, 0), freq)
+    assert torch.equal(qr, q[..., 128:])
+    pos = at(1, 77, 131071, 2147483647)
+    _, qr = layer.rope_queries(q, pos, freq)
+    want, size = turned(q[..., 128:], pos[:, None].expand(4, 3), freq, 1.0, 0)
+    # the turns themselves are an fp64 product: 2^-52 of up to 3.5e8 turns
+    near(qr, want, 0.0, (TURN + 2 * math.pi * 3.5e8 * 2.0 ** -51) * size)
+    back = torch.cat((q[..., :128], qr), -1)
+    _, again = layer.rope_queries(back, -pos, freq)
+    near(again, q[..., 128:], 0.0, 4 * TURN * (size + qr.double().abs()))
+
+
+def test_rope_strided_queries():
+    """Queries as columns of a wider projection, on and off 16 bytes."""
+    freq, _ = layer.rope_frequencies(64)
+    for first, io in ((64, BF), (3, BF), (5, F32)):
+        wide = rnd(50, 6 * 192 + 71, dtype=io)
+        q = wide[:, first:first + 6 * 192].unflatten(1, (6, 192))
+        pos = torch.arange(50, dtype=torch.int32, device=DEV)
+        qn, qr = layer.rope_queries(q, pos, freq)
+        en, er = layer.rope_queries(q.contiguous(), pos, freq)
+        assert torch.equal(qn, en) and torch.equal(qr, er)
+
+
+# ------------------------------------------------------------------ cache rows
+
+def paged(B, width, page, pages, seed=0):
+    order = torch.randperm(pages, generator=torch.Generator().manual_seed(seed))[:B * width]
+    return order.view(B, width).to(torch.int32).to(DEV)
+
+
+def ref_rows(rows, pos, freq, gain, layout, d_c, weight, eps):
+    x = rows.double()
+    c = x[..., :d_c]
+    if weight is not None:
+        c = c / (c.square().mean(-1, keepdim=True) + eps).sqrt() * weight.double()
+    if x.shape[-1] == d_c:
+        return c, c.abs() * SUM
+    k, size = turned(x[..., d_c:], pos, freq, gain, layout)
+    return torch.cat((c, k), -1), torch.cat((c.abs() * SUM, size * TURN), -1)
+
+
+@pytest.mark.parametrize("io, cache", [(BF, BF), (F32, BF), (F32, F32), (BF, F32), (BF, FP8), (F32, FP8)])
+@pytest.mark.parametrize("layout, normed", [(0, False), (1, True)])
+@pytest.mark.parametrize("B, new, d_c, d_rope, page", [(1, 1, 512, 64, 64), (16, 1, 512, 64, 64), (3, 5, 256, 64, 16), (2, 130, 512, 64, 64), (5, 2, 440, 64, 33),
+                                                       (2, 3, 7, 2, 5), (3, 4, 960, 64, 64), (2, 3, 33, 0, 64), (1, 700, 512, 64, 64), (2, 3, 768, 256, 8)])
+def test_cache_store(B, new, d_c, d_rope, page, layout, normed, io, cache):
+    row = d_c + d_rope
+    width = -(-(new + 2 * page) // page)
+    pages = B * width + 3
+    table = paged(B, width, page, pages)
+    first = torch.randint(0, width * page - new + 1, (B,), generator=torch.Generator().manual_seed(5)).to(DEV)
+    pos = (first[:, None] + torch.arange(new, device=DEV)).to(torch.int32)
+    rows = rnd(B, new, row, dtype=io, loud=True)
+    weight = (1 + 0.3 * rnd(d_c, seed=1)).to(io) if normed else None
+    freq, gain = layer.rope_frequencies(d_rope, scaling="yarn", factor=8.0) if d_rope else (torch.empty(0, dtype=torch.float64, device=DEV), 1.0)
+    kv = torch.full((pages, page, row), 3, dtype=torch.uint8, device=DEV).view(FP8) if cache == FP8 else torch.full((pages, page, row), 3.0, dtype=cache, device=DEV)
+    scale = torch.full((pages, page), -1.0, device=DEV) if cache == FP8 else None
+    before = kv.clone()
+    layer.cache_store(rows, pos, freq, kv, table, d_c, gain, layout, weight, 1e-6, scale)
+    want, floor = ref_rows(rows, pos, freq, gain, layout, d_c, weight, 1e-6)
+    at = (table.long().gather(1, pos.long() // page) * page + pos.long() % page).view(-1)
+    flat, was = kv.view(torch.uint8).view(pages * page, -1), before.view(torch.uint8).view(pages * page, -1)
+    got = kv.view(torch.uint8).view(pages * page, -1)[at].view(cache).view(B, new, row)
+    if cache == FP8:
+        s = scale.view(-1)[at].view(B, new, 1).double()
+        top = want.abs().amax(-1, keepdim=True)
+        near(s, top / 448, 2 * SUM)
+        v = want / s
+        off = (got.double() - v).abs()
+        assert (off <= torch.maximum(v.abs() * 2.0 ** -4, torch.full_like(v, 2.0 ** -10)) * (1 + 1e-3) + 2 * floor / s).all()
+    else:
+        near(got, want, ROUND[cache], floor)
+    rest = torch.ones(pages * page, dtype=torch.bool, device=DEV)
+    rest[at] = False
+    assert torch.equal(flat[rest], was[rest])
+    if cache == FP8:
+        assert (scale.view(-1)[rest] == -1).all()
+
+
+@pytest.mark.parametrize("cache", [BF, FP8])
+def test_cache_store_skips_what_has_no_place(cache):
+    """Positions before and past the table, pages that are not in the pool: those rows only."""
+    page, pages, row = 16, 8, 576
+    table = torch.tensor([[0, 1, -1], [2, 99, 3], [4, 5, 6]], dtype=torch.int32, device=DEV)
+    pos = torch.tensor([[-1, 3, 33, 48], [16, 31, 32, 2147483647], [-2147483648, 0, 47, 15]], dtype=torch.int32, device=DEV)
+    rows = rnd(3, 4, row, dtype=BF)
+    freq, _ = layer.rope_frequencies(64)
+    kv = torch.zeros((pages, page, row), dtype=torch.uint8 if cache == FP8 else BF, device=DEV)
+    scale = torch.zeros((pages, page), device=DEV) if cache == FP8 else None
+    layer.cache_store(rows, pos, freq, kv, table, 512, kv_scale=scale)
+    written = {(0, 3): (0, 1), (3, 0): (1, 2), (4, 0): (2, 1), (6, 15): (2, 2), (4, 15): (2, 3)}
+    touched = (kv.view(torch.uint8) != 0).any(-1)
+    assert {tuple(i) for i in touched.nonzero().tolist()} == set(written)
+    for (pg, slot), (b, i) in written.items():
+        want, floor = ref_rows(rows[b, i], pos[b, i], freq, 1.0, 0, 512, None, 0.0)
+        if cache == BF:
+            near(kv[pg, slot], want, ROUND[BF], floor)
+        else:
+            assert scale[pg, slot] > 0
+
+
+def test_cache_store_strided_rows_and_agreement_with_append():
+    """Rows as columns of a wider projection; on the same row the call that multiplies the projection itself leaves the
+    same values (its angles are formed in another way: one rounding apart)."""
+    B, D, row = 6, 128, 576
+    x = rnd(B, D, dtype=F32)
+    W = torch.zeros((D, row), device=DEV)
+    W[torch.arange(row, device=DEV) % D, torch.arange(row, device=DEV)] = 1.0       # a projection that is exact
+    wide = torch.zeros((B, row + 40), device=DEV)
+    wide[:, 8:8 + row] = x[:, torch.arange(row, device=DEV) % D]
+    pos = torch.tensor([0, 1, 63, 64, 100, 127], dtype=torch.int32, device=DEV)
+    table = paged(B, 2, 64, 2 * B)
+    kv_a, kv_b = (torch.zeros((2 * B, 64, row), device=DEV) for _ in range(2))
+    mla.cache_append(x, W, kv_a, table, pos, 512)
+    freq, _ = layer.rope_frequencies(64)
+    layer.cache_store(wide[:, 8:8 + row].unsqueeze(1), pos.view(B, 1), freq, kv_b, table, 512)
+    near(kv_b, kv_a, 0.0, 1e-5)
+    assert torch.equal(kv_b[..., :512], kv_a[..., :512])
+    layer.cache_store(wide[:, 8:8 + row].unsqueeze(0), pos.view(1, B), freq, kv_b, torch.arange(2, dtype=torch.int32, device=DEV).view(1, 2), 512)
+
+
+def test_cache_store_zero_rows_and_nan():
+    freq, _ = layer.rope_frequencies(64)
+    kv = torch.full((2, 64, 576), 5, dtype=torch.uint8, device=DEV)
+    scale = torch.full((2, 64), -1.0, device=DEV)
+    rows = torch.zeros((1, 2, 576), device=DEV)
+    rows[0, 1, 17] = math.nan
+    layer.cache_store(rows, torch.tensor([[4, 5]], dtype=torch.int32, device=DEV), freq, kv, torch.tensor([[1]], dtype=torch.int32, device=DEV), 512,
+                      kv_scale=scale, norm_weight=torch.ones(512, device=DEV), eps=0.0)
+    # eps 0 on a row of zeros divides by nothing: not a number, and it says so
+    assert torch.isnan(scale[1, 5])
+    layer.cache_store(rows[:, :1], torch.tensor([[4]], dtype=torch.int32, device=DEV), freq, kv, torch.tensor([[1]], dtype=torch.int32, device=DEV), 512,
+                      kv_scale=scale)
+    assert scale[1, 4] == 1.0 and not kv.view(FP8)[1, 4].double().any()          # (a turned zero may be a negative zero)
+
+
+def test_cache_store_pool_past_32_bits():
+    """A pool of more than 2^31 elements: rows at its end."""
+    page, row = 64, 576
+    pages = (1 << 31) // (page * row) + 10
+    kv = torch.zeros((pages, page, row), dtype=BF, device=DEV)
+    rows = rnd(1, 4, row, dtype=BF)
+    table = torch.tensor([[pages - 1]], dtype=torch.int32, device=DEV)
+    freq, _ = layer.rope_frequencies(64)
+    layer.cache_store(rows, torch.tensor([[60, 61, 62, 63]], dtype=torch.int32, device=DEV), freq, kv, table, 512)
+    assert torch.equal(kv[-1, 60:, :512], rows[0, :, :512]) and not kv[-1, :60].any() and not kv[:10].any()
+
+
+# ------------------------------------------------------------------ calls as a program makes them
+
+def the_calls():
+    x, w, r = rnd(37, 1024, dtype=BF), rnd(1024, dtype=BF, seed=1), rnd(37, 1024, dtype=BF, seed=2)
+    a, sa, W, sW = operands(37, 640, 1024)
+    q, pos = rnd(37, 4, 192, dtype=BF), torch.arange(37, dtype=torch.int32, device=DEV)
+    freq, gain = layer.rope_frequencies(64, scaling="linear", factor=2.0)
+    rows, table = rnd(1, 37, 576, dtype=F32), torch.tensor([[1, 0]], dtype=torch.int32, device=DEV)
+    new = lambda *s, dtype=BF: torch.zeros(s, dtype=dtype, device=DEV)
+    ws = new(max(16, layer.gemm_fp8_workspace_bytes(37, 640, 1024)), dtype=torch.uint8)
+    return {
+        "norm": (layer.rms_norm_fp8, dict(x=x, weight=w, eps=1e-5, residual=r, codes=new(37, 1024, dtype=FP8), scales=new(8, 37, dtype=F32),
+                                          residual_out=new(37, 1024), out=new(37, 1024)), ("codes", "scales", "residual_out", "out")),
+        "quantize": (layer.quantize_rows, dict(x=x, codes=new(37, 1024, dtype=FP8), scales=new(8, 37, dtype=F32)), ("codes", "scales")),
+        "gemm": (layer.gemm_fp8, dict(a=a, a_scales=sa, w=W, w_scales=sW, out=new(37, 640), workspace=ws), ("out",)),
+        "rope": (layer.rope_queries, dict(q=q, positions=pos, freq=freq, gain=gain, layout=1, q_nope=new(37, 4, 128), q_rope=new(37, 4, 64)), ("q_nope", "q_rope")),
+        "store": (layer.cache_store, dict(rows=rows, positions=pos.view(1, 37), freq=freq, kv_cache=new(2, 64, 576, dtype=FP8), page_table=table, d_c=512,
+                                          gain=gain, layout=0, norm_weight=rnd(512, dtype=F32), eps=1e-6, kv_scale=new(2, 64, dtype=F32)), ("kv_cache", "kv_scale")),
+    }
+
+
+@pytest.mark.parametrize("name", ["norm", "quantize", "gemm", "rope", "store"])
+def test_native_path_gives_the_bits_of_the_binding(name, monkeypatch):
+    mla.lib()
+    f, args, outputs = the_calls()[name]
+    fast, got = mla._fast, {}
+    asked = []
+
+    class Asked:
+        def __getattr__(self, n):
+            return lambda *a: asked.append(getattr(fast, n)(*a)) or asked[-1]
+    for native in (True, False):
+        a = {k: v.clone() if k in outputs else v for k, v in args.items()}
+        monkeypatch.setattr(mla, "_fast", Asked() if native else None)
+        f(**a)
+        torch.cuda.synchronize()
+        got[native] = {k: a[k].view(torch.uint8) for k in outputs}
+    assert asked == [0]
+    for k in outputs:
+        assert torch.equal(got[True][k], got[False][k]) and not torch.equal(got[True][k], args[k].view(torch.uint8)), k
+
+
+WRONG = {
+    "norm": [dict(weight=lambda t: t.float()), dict(weight=lambda t: t[:-1].clone()), dict(residual=lambda t: t[:-1].clone()), dict(residual=lambda t: t.float()),
+             dict(out=lambda t: t[:-1].clone()), dict(out=lambda t: t.float()), dict(codes=lambda t: t.float()), dict(scales=lambda t: t[:-1].clone()),
+             dict(scales=lambda t: t.double()), dict(residual_out=lambda t: t[:-1].clone()), dict(x=lambda t: t.half()), dict(x=lambda t: t.t()),
+             dict(x=lambda t: t[:1].expand(37, 1024)), dict(x=lambda t: t[0])],
+    "quantize": [dict(codes=lambda t: t[:-1].clone()), dict(scales=lambda t: t[:, :-1].clone()), dict(x=lambda t: t.double()), dict(x=lambda t: t[0])],
+    "gemm": [dict(a=lambda t: t.float()), dict(w=lambda t: t[:, :-16].clone()), dict(a_scales=lambda t: t.t().contiguous()), dict(w_scales=lambda t: t[:-1].clone()),
+             dict(w_scales=lambda t: t.double()), dict(out=lambda t: t[:-1].clone()), dict(out=lambda t: t.half()),
+             dict(a=lambda t: t[:, :1000].clone(), w=lambda t: t[:, :1000].clone())],
+    "rope": [dict(positions=lambda t: t.long()), dict(positions=lambda t: t[:-1].clone()), dict(freq=lambda t: t.float()), dict(q_nope=lambda t: t[:-1].clone()),
+             dict(q_rope=lambda t: t.float()), dict(q=lambda t: t.transpose(0, 1)), dict(q=lambda t: t[0]), dict(layout=lambda t: 5), dict(gain=lambda t: math.nan),
+             dict(freq=lambda t: t.repeat(5))],
+    "store": [dict(positions=lambda t: t.long()), dict(positions=lambda t: t[:, :-1].clone()), dict(freq=lambda t: t[:-1].clone()), dict(freq=lambda t: t.float()),
+              dict(kv_scale=lambda t: None), dict(kv_scale=lambda t: t[:-1].clone()), dict(norm_weight=lambda t: t.bfloat16()), dict(norm_weight=lambda t: t[:-1].clone()),
+              dict(page_table=lambda t: t.long()), dict(page_table=lambda t: t.repeat(2, 1)), dict(rows=lambda t: t[..., :-1]), dict(rows=lambda t: t.half()),
+              dict(layout=lambda t: 2), dict(d_c=lambda t: 511), dict(kv_cache=lambda t: t[..., :-1].clone())],
+}
+
+
+@pytest.mark.parametrize("name", list(WRONG))
+def test_what_is_refused(name, monkeypatch):
+    """One wrong argument at a time, with the native path and without: nothing is written."""
+    mla.lib()
+    f, args, outputs = the_calls()[name]
+    fast = mla._fast
+    for case in WRONG[name]:
+        for native in (True, False):
+            a = {**args, **{k: change(args[k]) for k, change in case.items()}}
+            monkeypatch.setattr(mla, "_fast", fast if native else None)
+            with pytest.raises((ValueError, TypeError, mla.MlaError)):
+                f(**a)
+    torch.cuda.synchronize()
+    for k in outputs:
+        assert not args[k].view(torch.uint8).any(), k
+
+
+def test_workspace_that_is_too_small_is_refused():
+    for M, N, K in ((1, 576, 4096), (64, 576, 4096), (61, 320, 7168), (300, 576, 4096)):
+        need = layer.gemm_fp8_workspace_bytes(M, N, K)
+        if need:
+            a, sa, w, sw = operands(M, N, K)
+            out = torch.zeros((M, N), dtype=BF, device=DEV)
+            with pytest.raises(mla.MlaError) as e:
+                layer.gemm_fp8(a, sa, w, sw, out=out, workspace=torch.empty(need - 1, dtype=torch.uint8, device=DEV))
+            assert e.value.status == -4
+            torch.cuda.synchronize()
+            assert not out.any()
+
+
+def test_another_stream_and_graphs():
+    """The calls follow torch's current stream, and a captured graph of them gives the eager bits on every replay, with
+    new inputs in the same buffers."""
+    calls = the_calls()
+    eager = {}
+    for name, (f, args, outputs) in calls.items():
+        f(**args)
+        eager[name] = {k: args[k].clone() for k in outputs}
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    for name, (f, args, outputs) in calls.items():
+        for k in outputs:
+            args[k].view(torch.uint8).zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        for f, args, _ in calls.values():
+            f(**args)
+    stream.synchronize()
+    for name, (f, args, outputs) in calls.items():
+        for k in outputs:
+            assert torch.equal(args[k].view(torch.uint8), eager[name][k].view(torch.uint8)), (name, k)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for f, args, _ in calls.values():
+            f(**args)
+    for turn in range(3):
+        for name in ("norm", "quantize"):
+            calls[name][1]["x"].copy_(rnd(37, 1024, dtype=BF, seed=20 + turn))
+        calls["rope"][1]["q"].copy_(rnd(37, 4, 192, dtype=BF, seed=30 + turn))
+        calls["store"][1]["rows"].copy_(rnd(1, 37, 576, dtype=F32, seed=40 + turn))
+        calls["gemm"][1]["a_scales"].mul_(1.5)
+        want = {}
+        for name, (f, args, outputs) in calls.items():
+            f(**args)
+            want[name] = {k: args[k].clone() for k in outputs}
+            for k in outputs:
+                args[k].view(torch.uint8).zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, (f, args, outputs) in calls.items():
+            for k in outputs:
+                assert torch.equal(args[k].view(torch.uint8), want[name][k].view(torch.uint8)), (turn, name, k)
+
+
+@pytest.mark.parametrize("M, N, K", [(1, 576, 4096), (61, 576, 4096), (300, 576, 4096), (2000, 2048, 2048)])
+def test_gemm_same_bits_every_time(M, N, K):
+    a, sa, w, sw = operands(M, N, K)
+    first = layer.gemm_fp8(a, sa, w, sw, dtype=F32)
+    for _ in range(5):
+        assert torch.equal(layer.gemm_fp8(a, sa, w, sw, dtype=F32), first)
