@@ -115,7 +115,7 @@ size_t mla_gemm_fp8_workspace_bytes(int M, int N, int K);
  *   out  [M, N] out dtype (MLA_F32 or MLA_BF16)
  *   workspace  mla_gemm_fp8_workspace_bytes(M, N, K) bytes, 16-byte aligned (may
  *              be NULL where that is 0); scratch
- * K a multiple of 16, a and w on 16 bytes (otherwise MLA_ERR_UNSUPPORTED), any M
+ * K a multiple of 16 up to 2^23, a and w on 16 bytes (otherwise MLA_ERR_UNSUPPORTED), any M
  * and N.  Products are exact and summed in fp32 (but see MLA_GEMM_FAST_SUMS), the
  * blocks with their scales in fp32 beside them; the order of the sums depends on
  * the sizes alone, so that a call's bits do not change from run to run.

@@ -3,20 +3,28 @@
 // The inner sum runs on the matrix cores, starts from zero and is added to the running sum with the two scales.  The
 // weights are the instruction's row operand, so that a lane's outputs belong to one token and take one scale.
 //
-// Which instruction: v_mfma_f32_16x16x128_f8f6f4 takes the codes as they are, but its adders align the products of eight
+// Which instruction: the f8f6f4 ones take the codes as they are, but their adders align the products of eight
 // neighbouring k to the largest of them and keep 13 bits below it (measured: 2^16 + 2^2 in one group gives 2^16; across
 // groups, and to the accumulator, nothing is lost).  A result of 128 random products is 1.4e-5 off.  Every e4m3
-// value is an f16 value, and v_mfma_f32_16x16x32_f16 adds such products without loss, at half the rate.
+// value is an f16 value, and the f16 instructions add such products without loss, at half the rate.  So: f16 wherever
+// the matrix cores wait for memory anyway (few tokens), and at many tokens unless the caller allows the other
+// (MLA_GEMM_FAST_SUMS).
+//
+// The columns of a block may go into the operands in any order that is the same for both: a lane takes 16-byte pieces
+// that suit the loads.
 #include "layer_internal.h"
 #include "mfma_tile.h"
+
+#include <algorithm>
 
 namespace mla {
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
-
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 // eight codes as f16 (exact)
 __device__ __forceinline__ f16x8 widen8(int lo, int hi)
@@ -26,72 +34,419 @@ __device__ __forceinline__ f16x8 widen8(int lo, int hi)
     return (f16x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// rows of 128 codes -> 16 x 16 sums: lane (g, n) supplies the same 32 columns of row n of either operand, in the same
-// order (which 32 does not matter), and holds results (row 4 g + i of w, row n of a)
-__device__ __forceinline__ f32x4 block_products(const i32x8& w, const i32x8& a)
+// workgroup barrier over which the compiler moves no access to memory (waits are placed by hand)
+__device__ __forceinline__ void barrier()
 {
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(w[2 * i], w[2 * i + 1]), widen8(a[2 * i], a[2 * i + 1]), s, 0, 0, 0);
-    return s;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
-// 32 codes of a row; columns at and past K (a multiple of 16) are zeros
-__device__ __forceinline__ i32x8 codes32(const uint8_t* row, int k, int K)
+template <bool F32> __device__ __forceinline__ void put(void* out, int64_t at, float v)
 {
-    u32x4 lo = {0u, 0u, 0u, 0u}, hi = lo;
-    if (k < K) lo = *reinterpret_cast<const u32x4*>(row + k);
-    if (k + 16 < K) hi = *reinterpret_cast<const u32x4*>(row + k + 16);
-    return __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    if (F32) static_cast<float*>(out)[at] = v;
+    else     static_cast<uint16_t*>(out)[at] = (uint16_t)f32_to_bf16_bits(v);
 }
 
-// 64 tokens x 64 outputs per workgroup, 16 outputs per wavefront, operands straight from memory.
-template <bool F32>
-__global__ __launch_bounds__(256) void gemm_fp8_kernel(GemmFp8Params p)
+// ---------------------------------------------------------------- few tokens
+
+// A workgroup takes 16 outputs of up to 16 MT tokens over the whole depth, its wavefronts share out the blocks: what
+// bounds it is reading the weights once, and with every block of a wavefront on its way at once that is one round trip.
+// The partial sums meet in LDS and are added in the wavefronts' order.
+template <int MT, int WAVES, bool F32>
+__global__ __launch_bounds__(WAVES * 64) void gemm_rows_kernel(GemmFp8Params p)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
-    const int m0 = blockIdx.x * 64, n0 = blockIdx.y * 64 + wave * 16;
-    if (n0 >= p.N) return;
+    constexpr int U = MT <= 1 ? 4 : 2;                 // blocks of a wavefront in flight
+    __shared__ __attribute__((aligned(16))) float red[WAVES][MT][256];
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
     const int blocks = (p.K + QBLOCK - 1) / QBLOCK;
-    const uint8_t* w = p.w + (int64_t)min(n0 + n, p.N - 1) * p.K;
+    const uint8_t* w = p.w + (int64_t)min(n0 + n, p.N - 1) * p.K + 16 * g;
     const float* ws = p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
-    f32x4 acc[4] = {};
-    for (int b = 0; b < blocks; ++b) {
-        const int k = b * QBLOCK + g * 32;
-        const i32x8 wv = codes32(w, k, p.K);
+    const uint8_t* a[MT];
+    const float* as[MT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int m = min(m0 + i * 16 + n, p.M - 1);
-            const f32x4 s = block_products(wv, codes32(p.a + (int64_t)m * p.K, k, p.K));
-            const float scale = p.a_scales[(int64_t)b * p.M + m] * ws[b];
+    for (int t = 0; t < MT; ++t) {
+        const int m = min(m0 + t * 16 + n, p.M - 1);
+        a[t] = p.a + (int64_t)m * p.K + 16 * g;
+        as[t] = p.a_scales + m;
+    }
+    f32x4 acc[MT] = {};
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    for (int b0 = wave; b0 < blocks; b0 += WAVES * U) {
+        u32x4 wv[U][2], av[U][MT][2];
+        float sa[U][MT], sw[U];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] += s[j] * scale;
+        for (int u = 0; u < U; ++u) {
+            const int b = b0 + u * WAVES, k = b * QBLOCK;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {              // the pieces at columns 16 g and 64 + 16 g
+                const bool in = k + 64 * i + 16 * g < p.K;
+                wv[u][i] = zero;
+                if (in) wv[u][i] = *reinterpret_cast<const u32x4*>(w + k + 64 * i);
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    av[u][t][i] = zero;
+                    if (in) av[u][t][i] = *reinterpret_cast<const u32x4*>(a[t] + k + 64 * i);
+                }
+            }
+            sw[u] = ws[min(b, blocks - 1)];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) sa[u][t] = as[t][(int64_t)min(b, blocks - 1) * p.M];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (b0 + u * WAVES >= blocks) break;       // (a scale that is not finite must not meet a block's zeros twice)
+            f16x8 wh[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) wh[q] = widen8((int)wv[u][q >> 1][2 * (q & 1)], (int)wv[u][q >> 1][2 * (q & 1) + 1]);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    s = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[q], widen8((int)av[u][t][q >> 1][2 * (q & 1)], (int)av[u][t][q >> 1][2 * (q & 1) + 1]), s, 0, 0, 0);
+                const float f = sa[u][t] * sw[u];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[t][j] += s[j] * f;
+            }
         }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = m0 + i * 16 + n;
-        if (m >= p.M) continue;
+    for (int t = 0; t < MT; ++t) *reinterpret_cast<f32x4*>(&red[wave][t][n * 16 + 4 * g]) = acc[t];
+    __syncthreads();
+    for (int i = tid; i < MT * 256; i += WAVES * 64) {
+        const int m = m0 + (i >> 4), c = n0 + (i & 15);
+        float v = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = n0 + 4 * g + j;
-            if (c >= p.N) continue;
-            if (F32) static_cast<float*>(p.out)[(int64_t)m * p.N + c] = acc[i][j];
-            else     static_cast<uint16_t*>(p.out)[(int64_t)m * p.N + c] = (uint16_t)f32_to_bf16_bits(acc[i][j]);
+        for (int q = 0; q < WAVES; ++q) v += red[q][i >> 8][i & 255];
+        if (m < p.M && c < p.N) put<F32>(p.out, (int64_t)m * p.N + c, v);
+    }
+}
+
+// ---------------------------------------------------------------- many tokens
+
+__device__ __attribute__((aligned(16))) const uint32_t zeros16[4] = {0u, 0u, 0u, 0u};
+
+// A workgroup of eight wavefronts computes 256 outputs of 128 MT tokens (a wavefront 128 outputs of 32 MT).  The codes of
+// a block travel by direct-to-LDS loads, `STAGES` blocks deep; 16-byte piece c of a row lies at position c ^ (row >> 1 & 7)
+// of its 128 bytes, so that the operand reads (32 rows, one piece each half) are free of bank conflicts.
+//
+// A step is one block: 4 MT units of 32 outputs x 32 tokens, each one chain of instructions whose result is scaled and
+// added while the next chain runs (32 x 32 x 64 and not 16 x 16 x 128 instructions: beside the latter vector
+// instructions hardly issue, 33.5 against 45 cycles per 16 x 16 x 128 with its four additions).  Operands are
+// read a unit ahead.  One barrier per step, before its last outputs: by then everybody has read the block, and the next
+// one has arrived; the loads of the block after take its place and are spread over the units, because a wavefront stands
+// still while a load is accepted.
+//
+// What bounds it: power.  At 32768 x 6144 x 4096 the matrix cores are busy 55 - 65 % of the cycles at 1.65 - 1.7 GHz of the
+// card's 2.4.
+template <int MT, int STAGES, bool FAST, bool F32, bool SPLIT>
+__global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int tiles_m, int tiles_n, int splits, bool stream_out)
+{
+    constexpr int W_B = 256 * QBLOCK, A_B = 128 * MT * QBLOCK, STAGE = W_B + A_B + 2048;   // weights | tokens | scales
+    constexpr int WLOADS = 4, ALOADS = 2 * MT, LOADS = WLOADS + ALOADS + 1;                // per wavefront and block
+    constexpr int UNITS = 4 * MT;
+    constexpr int PITCH = 272;                                                             // epilogue: a token's 256 bytes and 16 more
+    static_assert(8 * 32 * PITCH <= STAGES * STAGE && STAGES * STAGE <= 160 * 1024);
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[STAGES * STAGE];
+    LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // Workgroup -> tile: consecutive tiles on one XCD (ids equal mod 8), in bands of four tiles of tokens, so that what
+    // an XCD runs at once shares its operands in its L2
+    const int total = tiles_m * tiles_n * splits, per = (total + 7) / 8;
+    int lin = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if (lin >= total || (int)(blockIdx.x >> 3) >= per) return;
+    const int split = lin % splits;
+    lin /= splits;
+    constexpr int BAND = 4;
+    const int band = lin / (BAND * tiles_n), rows_in = min(BAND, tiles_m - band * BAND), in = lin - band * BAND * tiles_n;
+    const int m0 = (band * BAND + in % rows_in) * 128 * MT, n0 = in / rows_in * 256;
+    const int blocks = (p.K + QBLOCK - 1) / QBLOCK, whole = p.K / QBLOCK;
+    const int first = (int)((int64_t)whole * split / splits), last = (int)((int64_t)whole * (split + 1) / splits);
+
+    // Loads: load i of a wavefront brings rows 8 (8 i + wave) .. + 7; rows past the end repeat the last (their outputs
+    // are not stored)
+    const int piece = (lane & 7) ^ ((lane >> 4) | ((wave & 1) << 2));
+    uint32_t off_w[WLOADS], off_a[ALOADS];
+#pragma unroll
+    for (int i = 0; i < WLOADS; ++i) off_w[i] = (uint32_t)min((i * 8 + wave) * 8 + (lane >> 3), p.N - 1 - n0) * (uint32_t)p.K + piece * 16;
+#pragma unroll
+    for (int i = 0; i < ALOADS; ++i) off_a[i] = (uint32_t)min((i * 8 + wave) * 8 + (lane >> 3), p.M - 1 - m0) * (uint32_t)p.K + piece * 16;
+    const uint8_t* a0 = p.a + (int64_t)m0 * p.K;
+    const uint8_t* w0 = p.w + (int64_t)n0 * p.K;
+    // scales: wavefronts 0 .. 2 MT - 1 bring the tokens', the others the weights' two (only those of wavefront 2 MT are read)
+    const bool tokens = wave < 2 * MT;
+    const float* scale0 = tokens ? p.a_scales + m0 : p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
+    const int64_t scale_step = tokens ? p.M : 1;
+    const uint32_t off_s = 4u * (tokens ? (uint32_t)min(wave * 64 + lane, p.M - 1 - m0) : (uint32_t)min(lane & 1, (p.N - 1 - n0) / QBLOCK) * (uint32_t)blocks);
+    auto load = [&](int kb, uint32_t stage, int k) {
+        if (k < WLOADS + ALOADS) {
+            const bool W = k < WLOADS;
+            const int i = W ? k : k - WLOADS;
+            const uint8_t* src = (W ? w0 : a0) + (int64_t)kb * QBLOCK;
+            const uint32_t dst = lds0 + stage + (W ? 0 : W_B) + i * 8192 + wave * 1024;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(W ? off_w[i] : off_a[i]), "s"(src) : "memory");
+        } else {
+            const float* src = scale0 + kb * scale_step;
+            const uint32_t dst = lds0 + stage + W_B + A_B + wave * 256;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(dst), "v"(off_s), "s"(src) : "memory");
         }
+    };
+
+    // Operands: lane (h, n) takes pieces h, 2 + h, 4 + h, 6 + h of row n
+    const int wn = wave & 1, wm = wave >> 1, key = (n >> 1) & 7;
+    const uint32_t w_row = (wn * 128 + n) * QBLOCK, a_row = W_B + (wm * 32 * MT + n) * QBLOCK;
+    uint32_t at[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) at[r] = ((2 * r + h) ^ key) * 16;
+    auto half = [&](uint32_t stage, uint32_t row, int q) -> i32x8 {
+        LDS_AS unsigned char* st = lds + stage + row;
+        const i32x4 lo = *(LDS_AS i32x4*)(st + at[2 * q]), hi = *(LDS_AS i32x4*)(st + at[2 * q + 1]);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    struct Raw { float a[MT], w; } raw;
+    auto scales = [&](uint32_t stage) {
+        LDS_AS unsigned char* st = lds + stage + W_B + A_B;
+#pragma unroll
+        for (int j = 0; j < MT; ++j) raw.a[j] = *(LDS_AS float*)(st + (wm * 32 * MT + j * 32 + n) * 4);
+        raw.w = *(LDS_AS float*)(st + 2 * MT * 256 + wn * 4);
+    };
+    // half q of a chain: 64 columns, on the codes or on their f16 values
+    auto chain = [&](const i32x8& wv, const i32x8& av, const f32x16& c) {
+        if constexpr (FAST) {
+            return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv, av, c, 0, 0, 0, 0, 0, 0);
+        } else {
+            f32x16 s = c;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                s = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(wv[2 * i], wv[2 * i + 1]), widen8(av[2 * i], av[2 * i + 1]), s, 0, 0, 0);
+            return s;
+        }
+    };
+
+    f32x16 acc[4][MT] = {}, s[2] = {};
+    float f[MT] = {};
+    i32x8 wv[2][2], av[MT][2];
+
+    // the short block at the end of K, alone and first
+    if (whole < blocks && split == splits - 1) {
+        const bool in = piece * 16 < p.K - whole * QBLOCK;
+#pragma unroll
+        for (int k = 0; k < WLOADS + ALOADS; ++k) {
+            const bool W = k < WLOADS;
+            const int i = W ? k : k - WLOADS;
+            const uint8_t* src = in ? (W ? w0 + off_w[i] : a0 + off_a[i]) + (int64_t)whole * QBLOCK : reinterpret_cast<const uint8_t*>(zeros16);
+            const uint32_t dst = lds0 + (W ? 0 : W_B) + i * 8192 + wave * 1024;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(dst), "v"(src) : "memory");
+        }
+        load(whole, 0, LOADS - 1);
+        wait_vmcnt<0>();
+        barrier();
+        scales(0);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            const i32x8 a_lo = half(0, a_row + j * 4096, 0), a_hi = half(0, a_row + j * 4096, 1);
+            const float fj = raw.a[j] * raw.w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x16 t = chain(half(0, w_row + i * 4096, 1), a_hi, chain(half(0, w_row + i * 4096, 0), a_lo, (f32x16){}));
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] += t[e] * fj;
+            }
+        }
+        __syncthreads();
+    }
+
+    if (first < last) {
+        const int steps = last - first;
+#pragma unroll
+        for (int st = 0; st < STAGES; ++st)        // (past the end: the last block again, never read)
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k) load(min(first + st, last - 1), st * STAGE, k);
+        wait_vmcnt<(STAGES - 1) * LOADS>();
+        barrier();
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+#pragma unroll
+            for (int j = 0; j < MT; ++j) av[j][q] = half(0, a_row + j * 4096, q);
+            wv[0][q] = half(0, w_row, q);
+        }
+        scales(0);
+        uint32_t cur = 0;
+        for (int kb = 0; kb < steps; ++kb) {
+            const uint32_t next = cur + STAGE == STAGES * STAGE ? 0u : cur + STAGE;
+            const int kl = first + min(kb + STAGES, steps - 1);       // the block that takes this one's place
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                const int i = u / MT, j = u % MT;
+                if (u == UNITS - MT) {
+                    // this block is read (its last weights have arrived), the next one has landed
+                    wait_vmcnt<(STAGES - 2) * LOADS>();
+                    __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0)
+                    barrier();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (j == 0) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) wv[(i + 1) & 1][q] = i < 3 ? half(cur, w_row + (i + 1) * 4096, q) : half(next, w_row, q);
+                }
+                if (u == 1 || UNITS == 1) {
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) f[t] = raw.a[t] * raw.w;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                const int pu = (u + UNITS - 1) % UNITS;               // the unit before: its sums are scaled and added now
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    s[u & 1] = chain(wv[i & 1][q], av[j][q], q ? s[u & 1] : (f32x16){});
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (i == 3) {
+                        av[j][q] = half(next, a_row + j * 4096, q);
+                        constexpr int EACH = (LOADS + 2 * MT - 1) / (2 * MT);
+#pragma unroll
+                        for (int k = 0; k < EACH; ++k)
+                            if ((j * 2 + q) * EACH + k < LOADS) load(kl, cur, (j * 2 + q) * EACH + k);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int e = 8 * q; e < 8 * q + 8; ++e) acc[pu / MT][pu % MT][e] += s[pu & 1][e] * f[pu % MT];
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (u == UNITS - 1) scales(next);
+            }
+            cur = next;
+        }
+        wait_vmcnt<0>();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[3][MT - 1][e] += s[1][e] * f[MT - 1];
+    }
+
+    // Outputs: lane (h, n) holds outputs 8 r + 4 h .. + 3 of every 32, of token n.  Through LDS they leave in whole
+    // lines: stored as they lie (8 bytes per token and lane) they took 10 % of the product of 32768 tokens.
+    __syncthreads();
+    const bool wide = p.N % (F32 || SPLIT ? 4 : 8) == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
+    LDS_AS unsigned char* mine = lds + wave * 32 * PITCH;
+    constexpr bool O32 = F32 || SPLIT;
+    constexpr int PARTS = O32 ? 2 : 1, COLS = 128 / PARTS, PER = O32 ? 4 : 8;    // outputs per pass, per 16 bytes
+    void* out = SPLIT ? static_cast<void*>(p.part + (int64_t)split * p.M * p.N) : p.out;
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+#pragma unroll
+            for (int ii = 0; ii < 4 / PARTS; ++ii)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const f32x16& v = acc[part * (4 / PARTS) + ii][j];
+                    LDS_AS unsigned char* dst = mine + n * PITCH + (ii * 32 + 8 * r + 4 * h) * (O32 ? 4 : 2);
+                    if constexpr (O32) *(LDS_AS f32x4*)dst = (f32x4){v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]};
+                    else               *(LDS_AS u32x2*)dst = (u32x2){bf16_pair(v[4 * r], v[4 * r + 1]), bf16_pair(v[4 * r + 2], v[4 * r + 3])};
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const int t = q * 4 + (lane >> 4), m = m0 + wm * 32 * MT + j * 32 + t, c = n0 + wn * 128 + part * COLS + (lane & 15) * PER;
+                const u32x4 v = *(LDS_AS u32x4*)(mine + t * PITCH + (lane & 15) * 16);
+                if (m >= p.M || c >= p.N) continue;
+                const int64_t o = (int64_t)m * p.N + c;
+                if (wide) {
+                    u32x4* dst = reinterpret_cast<u32x4*>(static_cast<unsigned char*>(out) + o * (O32 ? 4 : 2));
+                    if (stream_out) __builtin_nontemporal_store(v, dst);
+                    else            *dst = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        if (c + e < p.N) {
+                            if constexpr (O32) static_cast<float*>(out)[o + e] = __uint_as_float(v[e]);
+                            else               static_cast<uint16_t*>(out)[o + e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+                        }
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+}
+
+// partial products of the shares of K, added in their order
+template <bool F32>
+__global__ __launch_bounds__(256) void gemm_merge_kernel(GemmFp8Params p, int splits)
+{
+    const int64_t size = (int64_t)p.M * p.N;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
+        float v = p.part[i];
+        for (int s = 1; s < splits; ++s) v += p.part[s * size + i];
+        put<F32>(p.out, i, v);
+    }
+}
+
+enum Form { ROWS, TILE128, TILE256 };
+struct Plan {
+    Form form;
+    int splits;
+};
+
+Plan plan_of(int M, int N, int K, bool fast)
+{
+    if (M <= 64) return {ROWS, 1};
+    const int whole = K / QBLOCK;
+    const long t256 = (long)((M + 255) / 256) * ((N + 255) / 256), t128 = (long)((M + 127) / 128) * ((N + 255) / 256);
+    if (fast && t256 >= 200) return {TILE256, 1};
+    int splits = 1;
+    while (t128 * splits * 2 <= 256 && whole / (splits * 2) >= 4 && splits < 8) splits *= 2;
+    return {TILE128, splits};
+}
+
+template <int MT, bool F32> void launch_rows(const GemmFp8Params& p, hipStream_t s)
+{
+    const dim3 grid((unsigned)((p.N + 15) / 16), (unsigned)((p.M + 16 * MT - 1) / (16 * MT)));
+    if (MT <= 2 && p.K <= 4096) gemm_rows_kernel<MT, 8, F32><<<grid, dim3(512), 0, s>>>(p);
+    else                        gemm_rows_kernel<MT, 16, F32><<<grid, dim3(1024), 0, s>>>(p);
+}
+
+template <int MT, int STAGES, bool FAST> void launch_tiles(const GemmFp8Params& p, bool f32, int splits, hipStream_t s)
+{
+    const int tm = (p.M + 128 * MT - 1) / (128 * MT), tn = (p.N + 255) / 256;
+    const dim3 grid((unsigned)(((long)tm * tn * splits + 7) / 8 * 8)), block(512);
+    const bool stream_out = (int64_t)p.M * p.N * (f32 ? 4 : 2) > (int64_t)64 << 20;
+    if (splits > 1) gemm_tile_kernel<MT, STAGES, FAST, false, true><<<grid, block, 0, s>>>(p, tm, tn, splits, false);
+    else if (f32)   gemm_tile_kernel<MT, STAGES, FAST, true, false><<<grid, block, 0, s>>>(p, tm, tn, 1, stream_out);
+    else            gemm_tile_kernel<MT, STAGES, FAST, false, false><<<grid, block, 0, s>>>(p, tm, tn, 1, stream_out);
+    if (splits > 1) {
+        const dim3 mg((unsigned)std::min<int64_t>(((int64_t)p.M * p.N + 255) / 256, 4096));
+        if (f32) gemm_merge_kernel<true><<<mg, dim3(256), 0, s>>>(p, splits);
+        else     gemm_merge_kernel<false><<<mg, dim3(256), 0, s>>>(p, splits);
     }
 }
 
 }  // namespace
 
-size_t gemm_fp8_workspace(int, int, int) { return 0; }
-
-hipError_t launch_gemm_fp8(const GemmFp8Params& p, mla_dtype out, bool, hipStream_t s)
+size_t gemm_fp8_workspace(int M, int N, int K)
 {
-    const dim3 grid((unsigned)((p.M + 63) / 64), (unsigned)((p.N + 63) / 64)), block(256);
-    if (out == MLA_F32) gemm_fp8_kernel<true><<<grid, block, 0, s>>>(p);
-    else                gemm_fp8_kernel<false><<<grid, block, 0, s>>>(p);
+    int splits = 1;
+    for (bool fast : {false, true}) splits = std::max(splits, plan_of(M, N, K, fast).splits);
+    return splits > 1 ? (size_t)splits * M * N * sizeof(float) : 0;
+}
+
+hipError_t launch_gemm_fp8(const GemmFp8Params& p, mla_dtype out, bool fast_sums, hipStream_t s)
+{
+    const bool f32 = out == MLA_F32;
+    const Plan plan = plan_of(p.M, p.N, p.K, fast_sums);
+    if (plan.form == ROWS) {
+        const int tiles = (p.M + 15) / 16;
+        if      (tiles == 1) f32 ? launch_rows<1, true>(p, s) : launch_rows<1, false>(p, s);
+        else if (tiles == 2) f32 ? launch_rows<2, true>(p, s) : launch_rows<2, false>(p, s);
+        else                 f32 ? launch_rows<4, true>(p, s) : launch_rows<4, false>(p, s);
+    } else if (plan.form == TILE256) {
+        launch_tiles<2, 2, true>(p, f32, plan.splits, s);
+    } else if (fast_sums) {
+        launch_tiles<1, 3, true>(p, f32, plan.splits, s);
+    } else {
+        launch_tiles<1, 3, false>(p, f32, plan.splits, s);
+    }
     return hipGetLastError();
 }
 

@@ -58,7 +58,7 @@ extern "C" int mla_gemm_fp8(const uint8_t* a, const float* a_scales, const uint8
     if (!a || !a_scales || !w || !w_scales || !out) return MLA_ERR_NULL;
     if (M <= 0 || N <= 0 || K <= 0) return MLA_ERR_SHAPE;
     if (!io_ok(out_dtype) || K % 16 || reinterpret_cast<uintptr_t>(a) % 16 || reinterpret_cast<uintptr_t>(w) % 16 ||
-        N > 65535 * 64 || (flags & ~(unsigned)MLA_GEMM_FAST_SUMS))
+        K > 1 << 23 || (flags & ~(unsigned)MLA_GEMM_FAST_SUMS))
         return MLA_ERR_UNSUPPORTED;
     const size_t need = gemm_fp8_workspace(M, N, K);
     if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16)) return MLA_ERR_WORKSPACE;

@@ -49,7 +49,7 @@ def gemm(L, a=P, sa=P, w=P, sw=P, out=P, ws=P, ws_bytes=1 << 40, M=4, N=64, K=25
 @pytest.mark.parametrize("kw, want", [
     (dict(a=None), E_NULL), (dict(sa=None), E_NULL), (dict(w=None), E_NULL), (dict(sw=None), E_NULL), (dict(out=None), E_NULL),
     (dict(M=0), E_SHAPE), (dict(N=-1), E_SHAPE), (dict(K=0), E_SHAPE),
-    (dict(K=24), E_UNSUP), (dict(dt=FP8), E_UNSUP), (dict(a=P + 8), E_UNSUP), (dict(w=P + 1), E_UNSUP), (dict(flags=2), E_UNSUP)])
+    (dict(K=24), E_UNSUP), (dict(dt=FP8), E_UNSUP), (dict(a=P + 8), E_UNSUP), (dict(w=P + 1), E_UNSUP), (dict(flags=2), E_UNSUP), (dict(K=(1 << 23) + 16), E_UNSUP)])
 def test_gemm_refusals(L, kw, want):
     assert gemm(L, **kw) == want
 
