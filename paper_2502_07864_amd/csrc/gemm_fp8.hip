@@ -34,6 +34,21 @@ __device__ __forceinline__ f16x8 widen8(int lo, int hi)
     return (f16x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// c + 32 x 32 sums over 64 columns: lane (h, n) supplies 32 columns of row n of either operand and holds results (row
+// 8 r + 4 h + i of w, row n of a); on the codes (FAST) or on their f16 values
+template <bool FAST> __device__ __forceinline__ f32x16 products(const i32x8& w, const i32x8& a, const f32x16& c)
+{
+    if constexpr (FAST) {
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, a, c, 0, 0, 0, 0, 0, 0);
+    } else {
+        f32x16 s = c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2 * i], w[2 * i + 1]), widen8(a[2 * i], a[2 * i + 1]), s, 0, 0, 0);
+        return s;
+    }
+}
+
 // workgroup barrier over which the compiler moves no access to memory (waits are placed by hand)
 __device__ __forceinline__ void barrier()
 {
@@ -50,74 +65,66 @@ template <bool F32> __device__ __forceinline__ void put(void* out, int64_t at, f
 
 // ---------------------------------------------------------------- few tokens
 
-// A workgroup takes 16 outputs of up to 16 MT tokens over the whole depth, its wavefronts share out the blocks: what
+// A workgroup takes 16 NT outputs of up to 16 tokens over the whole depth, its wavefronts share out the blocks: what
 // bounds it is reading the weights once, and with every block of a wavefront on its way at once that is one round trip.
 // The partial sums meet in LDS and are added in the wavefronts' order.
-template <int MT, int WAVES, bool F32>
+template <int NT, int WAVES, int U, bool F32>
 __global__ __launch_bounds__(WAVES * 64) void gemm_rows_kernel(GemmFp8Params p)
 {
-    constexpr int U = MT <= 1 ? 4 : 2;                 // blocks of a wavefront in flight
-    __shared__ __attribute__((aligned(16))) float red[WAVES][MT][256];
+    __shared__ __attribute__((aligned(16))) float red[WAVES][NT][256];
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
+    const int n0 = blockIdx.x * 16 * NT;
     const int blocks = (p.K + QBLOCK - 1) / QBLOCK;
-    const uint8_t* w = p.w + (int64_t)min(n0 + n, p.N - 1) * p.K + 16 * g;
-    const float* ws = p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
-    const uint8_t* a[MT];
-    const float* as[MT];
+    const uint8_t* w[NT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int m = min(m0 + t * 16 + n, p.M - 1);
-        a[t] = p.a + (int64_t)m * p.K + 16 * g;
-        as[t] = p.a_scales + m;
-    }
-    f32x4 acc[MT] = {};
+    for (int t = 0; t < NT; ++t) w[t] = p.w + (int64_t)min(n0 + t * 16 + n, p.N - 1) * p.K + 16 * g;
+    const float* ws = p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
+    const uint8_t* a = p.a + (int64_t)min(n, p.M - 1) * p.K + 16 * g;
+    const float* as = p.a_scales + min(n, p.M - 1);
+    f32x4 acc[NT] = {};
     const u32x4 zero = {0u, 0u, 0u, 0u};
     for (int b0 = wave; b0 < blocks; b0 += WAVES * U) {
-        u32x4 wv[U][2], av[U][MT][2];
-        float sa[U][MT], sw[U];
+        u32x4 wv[U][NT][2], av[U][2];
+        float f[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int b = b0 + u * WAVES, k = b * QBLOCK;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {              // the pieces at columns 16 g and 64 + 16 g
                 const bool in = k + 64 * i + 16 * g < p.K;
-                wv[u][i] = zero;
-                if (in) wv[u][i] = *reinterpret_cast<const u32x4*>(w + k + 64 * i);
 #pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    av[u][t][i] = zero;
-                    if (in) av[u][t][i] = *reinterpret_cast<const u32x4*>(a[t] + k + 64 * i);
+                for (int t = 0; t < NT; ++t) {
+                    wv[u][t][i] = zero;
+                    if (in) wv[u][t][i] = *reinterpret_cast<const u32x4*>(w[t] + k + 64 * i);
                 }
+                av[u][i] = zero;
+                if (in) av[u][i] = *reinterpret_cast<const u32x4*>(a + k + 64 * i);
             }
-            sw[u] = ws[min(b, blocks - 1)];
-#pragma unroll
-            for (int t = 0; t < MT; ++t) sa[u][t] = as[t][(int64_t)min(b, blocks - 1) * p.M];
+            // (a block past the end is zeros, but its scale need not be finite)
+            f[u] = b < blocks ? ws[b] * as[(int64_t)b * p.M] : 0.f;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (b0 + u * WAVES >= blocks) break;       // (a scale that is not finite must not meet a block's zeros twice)
-            f16x8 wh[4];
+            f16x8 ah[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) wh[q] = widen8((int)wv[u][q >> 1][2 * (q & 1)], (int)wv[u][q >> 1][2 * (q & 1) + 1]);
+            for (int q = 0; q < 4; ++q) ah[q] = widen8((int)av[u][q >> 1][2 * (q & 1)], (int)av[u][q >> 1][2 * (q & 1) + 1]);
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
+            for (int t = 0; t < NT; ++t) {
                 f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    s = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[q], widen8((int)av[u][t][q >> 1][2 * (q & 1)], (int)av[u][t][q >> 1][2 * (q & 1) + 1]), s, 0, 0, 0);
-                const float f = sa[u][t] * sw[u];
+                    s = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8((int)wv[u][t][q >> 1][2 * (q & 1)], (int)wv[u][t][q >> 1][2 * (q & 1) + 1]), ah[q], s, 0, 0, 0);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[t][j] += s[j] * f;
+                for (int j = 0; j < 4; ++j) acc[t][j] += s[j] * f[u];
             }
         }
     }
 #pragma unroll
-    for (int t = 0; t < MT; ++t) *reinterpret_cast<f32x4*>(&red[wave][t][n * 16 + 4 * g]) = acc[t];
+    for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(&red[wave][t][n * 16 + 4 * g]) = acc[t];
     __syncthreads();
-    for (int i = tid; i < MT * 256; i += WAVES * 64) {
-        const int m = m0 + (i >> 4), c = n0 + (i & 15);
+    for (int i = tid; i < NT * 256; i += WAVES * 64) {
+        const int m = (i & 255) >> 4, c = n0 + (i >> 8) * 16 + (i & 15);
         float v = 0.f;
 #pragma unroll
         for (int q = 0; q < WAVES; ++q) v += red[q][i >> 8][i & 255];
@@ -216,19 +223,6 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
         for (int j = 0; j < MT; ++j) raw.a[j] = *(LDS_AS float*)(st + (wm * 32 * MT + j * 32 + n) * 4);
         raw.w = *(LDS_AS float*)(st + 2 * MT * 256 + wn * 4);
     };
-    // half q of a chain: 64 columns, on the codes or on their f16 values
-    auto chain = [&](const i32x8& wv, const i32x8& av, const f32x16& c) {
-        if constexpr (FAST) {
-            return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv, av, c, 0, 0, 0, 0, 0, 0);
-        } else {
-            f32x16 s = c;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(wv[2 * i], wv[2 * i + 1]), widen8(av[2 * i], av[2 * i + 1]), s, 0, 0, 0);
-            return s;
-        }
-    };
-
     f32x16 acc[4][MT] = {}, s[2] = {};
     float f[MT] = {};
     i32x8 wv[2][2], av[MT][2];
@@ -254,7 +248,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
             const float fj = raw.a[j] * raw.w;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const f32x16 t = chain(half(0, w_row + i * 4096, 1), a_hi, chain(half(0, w_row + i * 4096, 0), a_lo, (f32x16){}));
+                const f32x16 t = products<FAST>(half(0, w_row + i * 4096, 1), a_hi, products<FAST>(half(0, w_row + i * 4096, 0), a_lo, (f32x16){}));
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] += t[e] * fj;
             }
@@ -264,11 +258,13 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
 
     if (first < last) {
         const int steps = last - first;
+        // loads of the last stage beyond the first 2 MT are left to the first step (past the end: the last block
+        // again, never read)
 #pragma unroll
-        for (int st = 0; st < STAGES; ++st)        // (past the end: the last block again, never read)
+        for (int st = 0; st < STAGES; ++st)
 #pragma unroll
-            for (int k = 0; k < LOADS; ++k) load(min(first + st, last - 1), st * STAGE, k);
-        wait_vmcnt<(STAGES - 1) * LOADS>();
+            for (int k = 0; k < (st < STAGES - 1 ? LOADS : 2 * MT); ++k) load(min(first + st, last - 1), st * STAGE, k);
+        wait_vmcnt<(STAGES - 2) * LOADS + 2 * MT>();
         barrier();
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
@@ -277,10 +273,11 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
             wv[0][q] = half(0, w_row, q);
         }
         scales(0);
-        uint32_t cur = 0;
+        uint32_t prev = (STAGES - 1) * STAGE, cur = 0;
         for (int kb = 0; kb < steps; ++kb) {
             const uint32_t next = cur + STAGE == STAGES * STAGE ? 0u : cur + STAGE;
-            const int kl = first + min(kb + STAGES, steps - 1);       // the block that takes this one's place
+            // the blocks that take the place of the one before this and of this one
+            const int kp = first + min(kb + STAGES - 1, steps - 1), kl = first + min(kb + STAGES, steps - 1);
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
                 const int i = u / MT, j = u % MT;
@@ -303,15 +300,12 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
                 const int pu = (u + UNITS - 1) % UNITS;               // the unit before: its sums are scaled and added now
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    s[u & 1] = chain(wv[i & 1][q], av[j][q], q ? s[u & 1] : (f32x16){});
+                    s[u & 1] = products<FAST>(wv[i & 1][q], av[j][q], q ? s[u & 1] : (f32x16){});
                     __builtin_amdgcn_sched_barrier(0);
-                    if (i == 3) {
-                        av[j][q] = half(next, a_row + j * 4096, q);
-                        constexpr int EACH = (LOADS + 2 * MT - 1) / (2 * MT);
-#pragma unroll
-                        for (int k = 0; k < EACH; ++k)
-                            if ((j * 2 + q) * EACH + k < LOADS) load(kl, cur, (j * 2 + q) * EACH + k);
-                    }
+                    if (i == 3) av[j][q] = half(next, a_row + j * 4096, q);
+                    // a load per half chain from the barrier on
+                    if (i == 3) load(kl, cur, j * 2 + q);
+                    else if (2 * MT + u * 2 + q < LOADS) load(kp, prev, 2 * MT + u * 2 + q);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int e = 8 * q; e < 8 * q + 8; ++e) acc[pu / MT][pu % MT][e] += s[pu & 1][e] * f[pu % MT];
@@ -319,6 +313,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
                 }
                 if (u == UNITS - 1) scales(next);
             }
+            prev = cur;
             cur = next;
         }
         wait_vmcnt<0>();
@@ -371,6 +366,150 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
         }
 }
 
+// ---------------------------------------------------------------- in between
+
+// A workgroup of eight wavefronts computes 32 WN outputs of 32 WM tokens; a wavefront 32 x 32 of them over every KS-th
+// block, so that small tiles still keep eight wavefronts.  Up to a few hundred tokens, and for few outputs, small tiles over
+// the whole depth beat large ones over shares of it, whose partial sums go through memory.  Blocks travel as in the tile
+// kernel, KS at a time.  What bounds it: 64 bytes a cycle into a CU.
+template <int WN, int WM, int KS, int STAGES, bool FAST, bool F32>
+__global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p, int tiles_m)
+{
+    static_assert(WN * WM * KS == 8);
+    constexpr int W_ROWS = 32 * WN, A_ROWS = 32 * WM, GROUPS = (W_ROWS + A_ROWS) / 8;      // groups of 8 rows of a block
+    constexpr int CODES = KS * GROUPS, LOADS = CODES / 8 + 1;                              // loads of a stage, per wavefront
+    constexpr int BLOCK_B = (W_ROWS + A_ROWS) * QBLOCK, STAGE = KS * BLOCK_B + 2048;
+    constexpr int PITCH = 36;                                                              // floats per token of 32 outputs
+    static_assert(CODES % 8 == 0 && KS * A_ROWS <= 256 && STAGES * STAGE <= 160 * 1024 && 8 * 32 * PITCH * 4 <= STAGES * STAGE);
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[STAGES * STAGE];
+    LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int total = tiles_m * ((p.N + W_ROWS - 1) / W_ROWS), per = (total + 7) / 8;
+    const int lin = (blockIdx.x & 7) * per + (blockIdx.x >> 3);                            // consecutive tiles on one XCD
+    if (lin >= total) return;
+    const int m0 = lin % tiles_m * A_ROWS, n0 = lin / tiles_m * W_ROWS;
+    const int blocks = (p.K + QBLOCK - 1) / QBLOCK, steps = (blocks + KS - 1) / KS;
+
+    // Group G = 8 i + wave of a stage: block G / GROUPS of it, rows of w, then rows of a.  Rows past the end repeat the last
+    const uint8_t* src[LOADS - 1];
+    uint32_t off[LOADS - 1];
+    int block_of[LOADS - 1];
+#pragma unroll
+    for (int i = 0; i < LOADS - 1; ++i) {
+        const int G = i * 8 + wave, ks = G / GROUPS, r = (G % GROUPS) * 8;
+        const bool W = r < W_ROWS;
+        const int row = (W ? r : r - W_ROWS) + (lane >> 3);
+        const int piece = (lane & 7) ^ ((row >> 1) & 7);
+        src[i] = W ? p.w + (int64_t)n0 * p.K : p.a + (int64_t)m0 * p.K;
+        off[i] = (uint32_t)min(row, W ? p.N - 1 - n0 : p.M - 1 - m0) * (uint32_t)p.K + piece * 16;
+        block_of[i] = ks;
+    }
+    const int si = wave * 64 + lane;                   // wavefronts below 4 bring the tokens' scales, the others the weights'
+    const bool tokens = si < KS * A_ROWS;
+    const int s_block = tokens ? si / A_ROWS : lane % KS;
+    const float* s_src = tokens ? p.a_scales + min(m0 + si % A_ROWS, p.M - 1) : p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
+    const int64_t s_step = tokens ? p.M : 1;
+    auto request = [&](int step, uint32_t stage) {
+        const int b0 = step * KS;
+        if ((b0 + KS) * QBLOCK <= p.K) {
+#pragma unroll
+            for (int i = 0; i < LOADS - 1; ++i) {
+                const uint32_t dst = lds0 + stage + (i * 8 + wave) * 1024;
+                const uint8_t* from = src[i] + (int64_t)(b0 + block_of[i]) * QBLOCK;
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off[i]), "s"(from) : "memory");
+            }
+        } else {                                       // columns at and past K are zeros
+#pragma unroll
+            for (int i = 0; i < LOADS - 1; ++i) {
+                const uint32_t dst = lds0 + stage + (i * 8 + wave) * 1024;
+                const int piece = (lane & 7) ^ (((lane >> 3) + ((i * 8 + wave) % GROUPS) * 8 - (((i * 8 + wave) % GROUPS) * 8 < W_ROWS ? 0 : W_ROWS)) >> 1 & 7);
+                const int64_t k = (int64_t)(b0 + block_of[i]) * QBLOCK;
+                const uint8_t* from = k + piece * 16 < p.K ? src[i] + k + off[i] : reinterpret_cast<const uint8_t*>(zeros16);
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(dst), "v"(from) : "memory");
+            }
+        }
+        const float* from = s_src + (int64_t)min(b0 + s_block, blocks - 1) * s_step;
+        const uint32_t dst = lds0 + stage + KS * BLOCK_B + wave * 256;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(dst), "v"(from) : "memory");
+    };
+
+    const int wn = wave % WN, wm = wave / WN % WM, ks = wave / (WN * WM), key = (n >> 1) & 7;
+    const uint32_t w_row = ks * BLOCK_B + (wn * 32 + n) * QBLOCK, a_row = ks * BLOCK_B + (W_ROWS + wm * 32 + n) * QBLOCK;
+    struct Operands { i32x8 w[2], a[2]; float sa, sw; };
+    auto read = [&](uint32_t stage) {
+        LDS_AS unsigned char* st = lds + stage;
+        Operands o;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const uint32_t lo = ((4 * q + h) ^ key) * 16, hi = ((4 * q + 2 + h) ^ key) * 16;
+            o.w[q] = __builtin_shufflevector(*(LDS_AS i32x4*)(st + w_row + lo), *(LDS_AS i32x4*)(st + w_row + hi), 0, 1, 2, 3, 4, 5, 6, 7);
+            o.a[q] = __builtin_shufflevector(*(LDS_AS i32x4*)(st + a_row + lo), *(LDS_AS i32x4*)(st + a_row + hi), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        o.sa = *(LDS_AS float*)(st + KS * BLOCK_B + (ks * A_ROWS + wm * 32 + n) * 4);
+        o.sw = *(LDS_AS float*)(st + KS * BLOCK_B + (KS * A_ROWS + 63) / 64 * 256 + ks * 4);
+        return o;
+    };
+
+    f32x16 acc = {};
+#pragma unroll
+    for (int st = 0; st < STAGES; ++st) request(min(st, steps - 1), st * STAGE);           // (past the end: never read)
+    wait_vmcnt<(STAGES - 1) * LOADS>();
+    barrier();
+    Operands now = read(0);
+    uint32_t cur = 0;
+    for (int st = 0; st < steps; ++st) {
+        const uint32_t next = cur + STAGE == STAGES * STAGE ? 0u : cur + STAGE;
+        // this stage is in everybody's registers, the next one has landed
+        wait_vmcnt<(STAGES - 2) * LOADS>();
+        __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0)
+        barrier();
+        // the products first: while they run the wavefront asks for what comes next, and stands while that is accepted
+        f32x16 s = products<FAST>(now.w[0], now.a[0], (f32x16){});
+        __builtin_amdgcn_sched_barrier(0);
+        const Operands then = read(next);
+        __builtin_amdgcn_sched_barrier(0);
+        s = products<FAST>(now.w[1], now.a[1], s);
+        __builtin_amdgcn_sched_barrier(0);
+        request(min(st + STAGES, steps - 1), cur);
+        __builtin_amdgcn_sched_barrier(0);
+        // (a block past the end is zeros, but its scale need not be finite)
+        const float f = st * KS + ks < blocks ? now.sa * now.sw : 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] += s[e] * f;
+        now = then;
+        cur = next;
+    }
+    wait_vmcnt<0>();
+    barrier();
+    // sums of the wavefronts' blocks, in their order; [wave][token][output]
+    LDS_AS float* red = (LDS_AS float*)lds;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        *(LDS_AS f32x4*)(red + (wave * 32 + n) * PITCH + 8 * r + 4 * h) = (f32x4){acc[4 * r], acc[4 * r + 1], acc[4 * r + 2], acc[4 * r + 3]};
+    __syncthreads();
+    const bool wide = p.N % 4 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
+    for (int i = tid; i < W_ROWS * A_ROWS / 4; i += 512) {
+        const int c = i % (W_ROWS / 4) * 4, t = i / (W_ROWS / 4);                          // four outputs of a token
+        const LDS_AS float* at = red + ((t / 32 * WN + c / 32) * 32 + t % 32) * PITCH + c % 32;
+        f32x4 v = *(const LDS_AS f32x4*)at;
+#pragma unroll
+        for (int k = 1; k < KS; ++k) v += *(const LDS_AS f32x4*)(at + k * WN * WM * 32 * PITCH);
+        const int m = m0 + t, col = n0 + c;
+        if (m >= p.M || col >= p.N) continue;
+        const int64_t o = (int64_t)m * p.N + col;
+        if (wide) {
+            if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + o) = v;
+            else               *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + o) = (u32x2){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < p.N) put<F32>(p.out, o + e, v[e]);
+        }
+    }
+}
+
 // partial products of the shares of K, added in their order
 template <bool F32>
 __global__ __launch_bounds__(256) void gemm_merge_kernel(GemmFp8Params p, int splits)
@@ -383,28 +522,65 @@ __global__ __launch_bounds__(256) void gemm_merge_kernel(GemmFp8Params p, int sp
     }
 }
 
-enum Form { ROWS, TILE128, TILE256 };
+// ---------------------------------------------------------------- choice
+
+enum Form { ROWS16, ROWS32, SMALL_1x1, SMALL_1x2, SMALL_2x2, SMALL_2x4, TILE128, TILE256 };
 struct Plan {
     Form form;
     int splits;
 };
 
+// The form that a model of the times finds fastest: a launch, and per round of 256 workgroups (each fills its CU) the steps
+// over K, or the time that the operands take from memory.  us per step measured with few workgroups, on codes (fast) and on
+// f16; the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  On 115
+// sizes of 1 to 32768 tokens and five (N, K) the choice takes up to 17 % longer than the best form, at most 7 % on nine in ten.
 Plan plan_of(int M, int N, int K, bool fast)
 {
-    if (M <= 64) return {ROWS, 1};
-    const int whole = K / QBLOCK;
-    const long t256 = (long)((M + 255) / 256) * ((N + 255) / 256), t128 = (long)((M + 127) / 128) * ((N + 255) / 256);
-    if (fast && t256 >= 200) return {TILE256, 1};
-    int splits = 1;
-    while (t128 * splits * 2 <= 256 && whole / (splits * 2) >= 4 && splits < 8) splits *= 2;
-    return {TILE128, splits};
+    const int blocks = (K + QBLOCK - 1) / QBLOCK;
+    if (M <= 16) return {(N + 15) / 16 <= 256 ? ROWS16 : ROWS32, 1};     // 6144 x 4096, one token: 7.3 / 7.0 us; 3584 x 3584: 4.5 / 6.0
+    struct Shape { Form form; int tokens, outputs, blocks; float launch, step_fast, step_f16, crowded_fast, crowded_f16; };
+    static const Shape shapes[] = {
+        {SMALL_1x1, 32, 32, 8, 3.3f, 0.67f, 0.83f, 1.9f, 1.9f}, {SMALL_1x2, 64, 32, 4, 3.8f, 0.50f, 0.70f, 1.65f, 1.65f},
+        {SMALL_2x2, 64, 64, 2, 3.7f, 0.41f, 0.62f, 1.35f, 1.43f}, {SMALL_2x4, 128, 64, 1, 3.9f, 0.34f, 0.63f, 1.3f, 1.3f},
+        {TILE128, 128, 256, 1, 4.2f, 0.59f, 1.30f, 1.6f, 1.3f}, {TILE256, 256, 256, 1, 4.8f, 1.00f, 0.f, 1.75f, 0.f}};
+    Plan best = {TILE128, 1};
+    float least = 3e38f;
+    for (const Shape& f : shapes) {
+        if (f.form == TILE256 && !fast) continue;                        // (its registers are taken on f16)
+        const long tiles_m = (M + f.tokens - 1) / f.tokens, tiles = tiles_m * ((N + f.outputs - 1) / f.outputs);
+        const int steps = (blocks + f.blocks - 1) / f.blocks;
+        // shares of K, merged by a second launch
+        for (int s = 1; s == 1 || (f.form == TILE128 && s <= 8 && steps / s >= 4 && tiles * s <= 256); s *= 2) {
+            const long rounds = (tiles * s + 255) / 256;
+            const float fill = (float)(tiles * s) / (float)(rounds * 256), crowded = fast ? f.crowded_fast : f.crowded_f16;
+            const float step = (fast ? f.step_fast : f.step_f16) * (1.f + (crowded - 1.f) * fill * fill);
+            const float memory = ((float)N + (float)M) * (float)K / 5.5e6f;
+            float t = f.launch + std::max(memory, (float)rounds * (float)((steps + s - 1) / s) * step);
+            if (s > 1) t += 2.5f + (float)s * (float)M * (float)N * 8.f / 8e6f;      // (the partial sums, in the caches)
+            if (t < least) { least = t; best = {f.form, s}; }
+        }
+    }
+    return best;
 }
 
-template <int MT, bool F32> void launch_rows(const GemmFp8Params& p, hipStream_t s)
+template <int NT, int WAVES, int U> void launch_rows(const GemmFp8Params& p, bool f32, hipStream_t s)
 {
-    const dim3 grid((unsigned)((p.N + 15) / 16), (unsigned)((p.M + 16 * MT - 1) / (16 * MT)));
-    if (MT <= 2 && p.K <= 4096) gemm_rows_kernel<MT, 8, F32><<<grid, dim3(512), 0, s>>>(p);
-    else                        gemm_rows_kernel<MT, 16, F32><<<grid, dim3(1024), 0, s>>>(p);
+    const dim3 grid((unsigned)((p.N + 16 * NT - 1) / (16 * NT))), block(WAVES * 64);
+    if (f32) gemm_rows_kernel<NT, WAVES, U, true><<<grid, block, 0, s>>>(p);
+    else     gemm_rows_kernel<NT, WAVES, U, false><<<grid, block, 0, s>>>(p);
+}
+
+template <int WN, int WM, int KS, int STAGES> void launch_small_tiles(const GemmFp8Params& p, bool f32, bool fast, hipStream_t s)
+{
+    const int tm = (p.M + 32 * WM - 1) / (32 * WM), tn = (p.N + 32 * WN - 1) / (32 * WN);
+    const dim3 grid((unsigned)(((long)tm * tn + 7) / 8 * 8)), block(512);
+    if (fast) {
+        if (f32) gemm_small_tile_kernel<WN, WM, KS, STAGES, true, true><<<grid, block, 0, s>>>(p, tm);
+        else     gemm_small_tile_kernel<WN, WM, KS, STAGES, true, false><<<grid, block, 0, s>>>(p, tm);
+    } else {
+        if (f32) gemm_small_tile_kernel<WN, WM, KS, STAGES, false, true><<<grid, block, 0, s>>>(p, tm);
+        else     gemm_small_tile_kernel<WN, WM, KS, STAGES, false, false><<<grid, block, 0, s>>>(p, tm);
+    }
 }
 
 template <int MT, int STAGES, bool FAST> void launch_tiles(const GemmFp8Params& p, bool f32, int splits, hipStream_t s)
@@ -412,7 +588,7 @@ template <int MT, int STAGES, bool FAST> void launch_tiles(const GemmFp8Params& 
     const int tm = (p.M + 128 * MT - 1) / (128 * MT), tn = (p.N + 255) / 256;
     const dim3 grid((unsigned)(((long)tm * tn * splits + 7) / 8 * 8)), block(512);
     const bool stream_out = (int64_t)p.M * p.N * (f32 ? 4 : 2) > (int64_t)64 << 20;
-    if (splits > 1) gemm_tile_kernel<MT, STAGES, FAST, false, true><<<grid, block, 0, s>>>(p, tm, tn, splits, false);
+    if (MT == 1 && splits > 1) gemm_tile_kernel<1, STAGES, FAST, false, true><<<grid, block, 0, s>>>(p, tm, tn, splits, false);
     else if (f32)   gemm_tile_kernel<MT, STAGES, FAST, true, false><<<grid, block, 0, s>>>(p, tm, tn, 1, stream_out);
     else            gemm_tile_kernel<MT, STAGES, FAST, false, false><<<grid, block, 0, s>>>(p, tm, tn, 1, stream_out);
     if (splits > 1) {
@@ -435,17 +611,18 @@ hipError_t launch_gemm_fp8(const GemmFp8Params& p, mla_dtype out, bool fast_sums
 {
     const bool f32 = out == MLA_F32;
     const Plan plan = plan_of(p.M, p.N, p.K, fast_sums);
-    if (plan.form == ROWS) {
-        const int tiles = (p.M + 15) / 16;
-        if      (tiles == 1) f32 ? launch_rows<1, true>(p, s) : launch_rows<1, false>(p, s);
-        else if (tiles == 2) f32 ? launch_rows<2, true>(p, s) : launch_rows<2, false>(p, s);
-        else                 f32 ? launch_rows<4, true>(p, s) : launch_rows<4, false>(p, s);
-    } else if (plan.form == TILE256) {
-        launch_tiles<2, 2, true>(p, f32, plan.splits, s);
-    } else if (fast_sums) {
-        launch_tiles<1, 3, true>(p, f32, plan.splits, s);
-    } else {
-        launch_tiles<1, 3, false>(p, f32, plan.splits, s);
+    switch (plan.form) {
+        case ROWS16:    launch_rows<1, 16, 2>(p, f32, s); break;
+        case ROWS32:    launch_rows<2, 16, 2>(p, f32, s); break;
+        case SMALL_1x1: launch_small_tiles<1, 1, 8, 2>(p, f32, fast_sums, s); break;
+        case SMALL_1x2: launch_small_tiles<1, 2, 4, 3>(p, f32, fast_sums, s); break;
+        case SMALL_2x2: launch_small_tiles<2, 2, 2, 4>(p, f32, fast_sums, s); break;
+        case SMALL_2x4: launch_small_tiles<2, 4, 1, 6>(p, f32, fast_sums, s); break;
+        case TILE128:
+            if (fast_sums) launch_tiles<1, 3, true>(p, f32, plan.splits, s);
+            else           launch_tiles<1, 3, false>(p, f32, plan.splits, s);
+            break;
+        case TILE256: launch_tiles<2, 2, true>(p, f32, 1, s); break;
     }
     return hipGetLastError();
 }
