@@ -65,25 +65,26 @@ hipError_t launch_cache_store(const StoreParams& p, int layout, mla_dtype io, ml
 
 // ---- device helpers
 
-// Eight consecutive values.  VEC: 16-byte accesses (the address allows them and all eight are there); otherwise one
-// by one, those at and past `left` read as zero and are not written.
-template <bool F32, bool VEC> __device__ __forceinline__ void load8(const void* base, int64_t at, int left, float (&v)[8])
+// V (8 or 4) consecutive values in accesses of up to 16 bytes, which the address has to allow
+template <bool F32, int V> __device__ __forceinline__ void load_vec(const void* base, int64_t at, float (&v)[V])
 {
-    if constexpr (VEC && F32) {
-        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
-        const float4 a = src[0], b = src[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else if constexpr (VEC) {
-        const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    if constexpr (F32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = 0.f;
-            if (i < left) v[i] = F32 ? static_cast<const float*>(base)[at + i] : bf16_bits_to_f32(static_cast<const uint16_t*>(base)[at + i]);
+        for (int i = 0; i < V; i += 4) {
+            const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(base) + at + i);
+            v[i] = a.x; v[i + 1] = a.y; v[i + 2] = a.z; v[i + 3] = a.w;
         }
+    } else {
+        uint32_t w[V / 2];
+        if constexpr (V == 8) {
+            const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at);
+            w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+        } else {
+            const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + at);
+            w[0] = u.x; w[1] = u.y;
+        }
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
     }
 }
 
@@ -95,15 +96,39 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){lo, hi}, b2));
 }
 
-template <bool F32, bool VEC> __device__ __forceinline__ void store8(void* base, int64_t at, int left, const float (&v)[8])
+template <bool F32, int V> __device__ __forceinline__ void store_vec(void* base, int64_t at, const float (&v)[V])
 {
-    if constexpr (VEC && F32) {
-        float4* dst = reinterpret_cast<float4*>(static_cast<float*>(base) + at);
-        dst[0] = make_float4(v[0], v[1], v[2], v[3]);
-        dst[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else if constexpr (VEC) {
+    if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4)
+            *reinterpret_cast<float4*>(static_cast<float*>(base) + at + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    } else if constexpr (V == 8) {
         *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + at) =
             make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+    } else {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + at) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+    }
+}
+
+// Eight consecutive values.  VEC: whole vectors, as above; otherwise one by one, those at and past `left` read as zero and
+// are not written.
+template <bool F32, bool VEC> __device__ __forceinline__ void load8(const void* base, int64_t at, int left, float (&v)[8])
+{
+    if constexpr (VEC) {
+        load_vec<F32, 8>(base, at, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = 0.f;
+            if (i < left) v[i] = F32 ? static_cast<const float*>(base)[at + i] : bf16_bits_to_f32(static_cast<const uint16_t*>(base)[at + i]);
+        }
+    }
+}
+
+template <bool F32, bool VEC> __device__ __forceinline__ void store8(void* base, int64_t at, int left, const float (&v)[8])
+{
+    if constexpr (VEC) {
+        store_vec<F32, 8>(base, at, v);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)

@@ -4,14 +4,132 @@
 // Both move every value once; the angles are worked out once per token, not per head.
 #include "layer_internal.h"
 
+#include <algorithm>
+#include <type_traits>
+
 namespace mla {
 namespace {
 
 constexpr int MAX_PAIRS = 128;
 
-// One workgroup per token and group of heads: the token's turns go to LDS, then its values stream past.
+// (re + i im) (cs + i sn); which product is rounded first is fixed, so that every kernel gives the same bits
+__device__ __forceinline__ float2 rotate(float re, float im, float cs, float sn)
+{
+    return make_float2(__builtin_fmaf(re, cs, -(im * sn)), __builtin_fmaf(re, sn, im * cs));
+}
+
+// ---------------------------------------------------------------- queries
+
+// V values at a time.  A workgroup takes `tokens` tokens of `heads` heads: every thread asks for its values first, the
+// turns of the tokens are worked out while they travel and go to LDS, the nope values leave as they came.  HALF: a thread
+// holds the vector of real parts and that of imaginary parts; otherwise V / 2 whole pairs.
+// Memory bound: 32768 tokens x 32 heads x (128 + 64) bf16, 805 MB moved.
+constexpr int ROPE_TOKENS = 16, ROPE_UNITS = 4;
+
+// j / d for small numbers (j < 2^16: the quotient's error stays below the half that is added)
+__device__ __forceinline__ int divide(int j, float inv_d) { return (int)(((float)j + 0.5f) * inv_d); }
+
+template <bool F32, bool HALF, int V>
+__global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p, int tokens, int heads, int groups)
+{
+    __shared__ float2 turns[ROPE_TOKENS * MAX_PAIRS];
+    const int tid = threadIdx.x, pairs = p.d_rope / 2, width = p.d_nope + p.d_rope;
+    const int t0 = (int)(blockIdx.x / groups) * tokens, h0 = (int)(blockIdx.x % groups) * heads;
+    const int nt = min(tokens, p.T - t0), nh = min(heads, p.H - h0), rows = nt * nh;
+    const int nv = p.d_nope / V, rv = (HALF ? pairs : p.d_rope) / V;       // vectors of a head's row
+    const int n_nope = rows * nv, n_rope = rows * rv;
+    const float inv_nv = 1.f / (float)max(nv, 1), inv_rv = 1.f / (float)rv, inv_nh = 1.f / (float)nh;
+    using vec = std::conditional_t<V == 8 && !F32, uint4, std::conditional_t<F32, uint4, uint2>>;
+    constexpr int PARTS = F32 && V == 8 ? 2 : 1;                           // 16-byte accesses of a vector
+
+    auto row_of = [&](int r, int& t, int& h) { t = divide(r, inv_nh); h = h0 + r - t * nh; t += t0; };
+    // nope: copied as it lies, ROPE_UNITS vectors of a thread on their way at once
+    auto nope = [&](int j0, auto store) {
+        vec buf[ROPE_UNITS][PARTS];
+        const int size = F32 ? 4 : 2;
+#pragma unroll
+        for (int i = 0; i < ROPE_UNITS; ++i) {
+            const int j = j0 + i * 256 + tid;
+            if (j >= n_nope) continue;
+            const int r = divide(j, inv_nv);
+            int t, h;
+            row_of(r, t, h);
+            const char* src = static_cast<const char*>(p.q) + ((int64_t)t * p.pitch + (int64_t)h * width + (j - r * nv) * V) * size;
+#pragma unroll
+            for (int k = 0; k < PARTS; ++k) buf[i][k] = reinterpret_cast<const vec*>(src)[k];
+        }
+        store();
+#pragma unroll
+        for (int i = 0; i < ROPE_UNITS; ++i) {
+            const int j = j0 + i * 256 + tid;
+            if (j >= n_nope) continue;
+            const int r = divide(j, inv_nv);
+            int t, h;
+            row_of(r, t, h);
+            char* dst = static_cast<char*>(p.q_nope) + (((int64_t)t * p.H + h) * p.d_nope + (j - r * nv) * V) * size;
+#pragma unroll
+            for (int k = 0; k < PARTS; ++k) reinterpret_cast<vec*>(dst)[k] = buf[i][k];
+        }
+    };
+    auto load = [&](int j, float (&a)[V], float (&b)[V], int64_t& to, int& at) {
+        const int r = divide(j, inv_rv), c = (j - r * rv) * V;
+        int t, h;
+        row_of(r, t, h);
+        const int64_t from = (int64_t)t * p.pitch + (int64_t)h * width + p.d_nope + c;
+        load_vec<F32, V>(p.q, from, a);
+        if (HALF) load_vec<F32, V>(p.q, from + pairs, b);
+        to = ((int64_t)t * p.H + h) * p.d_rope + c;
+        at = (t - t0) * pairs + (HALF ? c : c / 2);
+    };
+    auto turn = [&](float (&a)[V], float (&b)[V], int64_t to, int at) {
+        if constexpr (HALF) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float2 w = turns[at + k], z = rotate(a[k], b[k], w.x, w.y);
+                a[k] = z.x;
+                b[k] = z.y;
+            }
+            store_vec<F32, V>(p.q_rope, to, a);
+            store_vec<F32, V>(p.q_rope, to + pairs, b);
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; k += 2) {
+                const float2 w = turns[at + k / 2], z = rotate(a[k], a[k + 1], w.x, w.y);
+                a[k] = z.x;
+                a[k + 1] = z.y;
+            }
+            store_vec<F32, V>(p.q_rope, to, a);
+        }
+    };
+
+    float a[2][V], b[2][V];
+    int64_t to[2];
+    int at[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (i * 256 + tid < n_rope) load(i * 256 + tid, a[i], b[i], to[i], at[i]);
+    nope(0, [&] {
+        for (int i = tid; i < nt * pairs; i += 256) {
+            const int t = i / pairs;
+            float cs, sn;
+            turn_of(p.positions[t0 + t], p.freq[i - t * pairs], p.gain, cs, sn);
+            turns[i] = make_float2(cs, sn);
+        }
+    });
+    for (int j0 = ROPE_UNITS * 256; j0 < n_nope; j0 += ROPE_UNITS * 256) nope(j0, [] {});
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (i * 256 + tid < n_rope) turn(a[i], b[i], to[i], at[i]);
+    for (int j = 512 + tid; j < n_rope; j += 256) {
+        load(j, a[0], b[0], to[0], at[0]);
+        turn(a[0], b[0], to[0], at[0]);
+    }
+}
+
+// any widths and addresses, value by value; one workgroup per token
 template <bool F32, bool HALF>
-__global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p)
+__global__ __launch_bounds__(256) void rope_queries_any_kernel(RopeParams p)
 {
     __shared__ float cs[MAX_PAIRS], sn[MAX_PAIRS];
     const int64_t t = blockIdx.x;
@@ -33,27 +151,143 @@ __global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p)
         const int h = j / pairs, i = j - h * pairs;
         const int re = HALF ? i : 2 * i, im = HALF ? i + pairs : 2 * i + 1;
         const int64_t from = src + (int64_t)h * width + p.d_nope, to = (t * p.H + h) * (int64_t)p.d_rope;
-        const float a = get(from + re), b = get(from + im);
-        put(p.q_rope, to + re, a * cs[i] - b * sn[i]);
-        put(p.q_rope, to + im, a * sn[i] + b * cs[i]);
+        const float2 z = rotate(get(from + re), get(from + im), cs[i], sn[i]);
+        put(p.q_rope, to + re, z.x);
+        put(p.q_rope, to + im, z.y);
     }
 }
 
-// One workgroup per row: the row in LDS as fp32, its rope part turned there, then rounded and stored.
+// ---------------------------------------------------------------- cache rows
+
 constexpr int MAX_ROW = 1024;
+
+// where row r goes: its row of the pool, or -1 where it has no place
+__device__ __forceinline__ int64_t place_of(const StoreParams& p, int r, int& pos)
+{
+    pos = p.positions[r];
+    if (pos < 0 || pos >= p.max_pages * p.page_size) return -1;                    // outside the table
+    const int page = p.page_table[(int64_t)(r / p.new_tokens) * p.max_pages + pos / p.page_size];
+    if (page < 0 || page >= p.num_pages) return -1;                                // outside the pool
+    return (int64_t)page * p.page_size + pos % p.page_size;
+}
+
+// A wavefront per row, four rows per workgroup: the row in registers, eight values at a time, turns (and for HALF the
+// rope part) in the wavefront's own LDS.
 template <bool F32, bool HALF, int CACHE>
 __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
+{
+    __shared__ float2 turns_lds[4][MAX_PAIRS];
+    __shared__ __attribute__((aligned(16))) float part_lds[HALF ? 4 : 1][HALF ? 2 * MAX_PAIRS : 4];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = blockIdx.x * 4 + wave;
+    if (r >= p.rows_total) return;
+    const int n = p.d_c + p.d_rope, pairs = p.d_rope / 2, vecs = n / 8, cv = p.d_c / 8;
+    constexpr int NV = MAX_ROW / 512;
+    float v[NV][8], w[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = lane + i * 64;
+        if (c < vecs) load_vec<F32, 8>(p.rows, (int64_t)r * p.pitch + c * 8, v[i]);
+        if (p.norm_weight && c < cv) load_vec<F32, 8>(p.norm_weight, c * 8, w[i]);
+    }
+    int pos;
+    const int64_t at = place_of(p, r, pos);
+    if (at < 0) return;
+    for (int i = lane; i < pairs; i += 64) {
+        float cs, sn;
+        turn_of(pos, p.freq[i], p.gain, cs, sn);
+        turns_lds[wave][i] = make_float2(cs, sn);
+    }
+    if (p.norm_weight) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (lane + i * 64 < cv) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum += v[i][k] * v[i][k];
+            }
+        const float inv = 1.f / sqrtf(wave_sum(sum) / (float)p.d_c + p.eps);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (lane + i * 64 < cv) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * inv * w[i][k];
+            }
+    }
+    if (HALF) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = lane + i * 64;
+            if (c < cv || c >= vecs) continue;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) part_lds[HALF ? wave : 0][(c - cv) * 8 + k] = v[i][k];
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");                         // (accesses of a wavefront complete in order)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = lane + i * 64;
+        if (c < cv || c >= vecs) continue;
+        const int first = (c - cv) * 8;
+        if (HALF) {
+            const bool im = first >= pairs;
+            const int pair = im ? first - pairs : first;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float2 t = turns_lds[wave][pair + k];
+                const float other = part_lds[HALF ? wave : 0][im ? pair + k : first + pairs + k];
+                v[i][k] = im ? rotate(other, v[i][k], t.x, t.y).y : rotate(v[i][k], other, t.x, t.y).x;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                const float2 t = turns_lds[wave][first / 2 + k / 2], z = rotate(v[i][k], v[i][k + 1], t.x, t.y);
+                v[i][k] = z.x;
+                v[i][k + 1] = z.y;
+            }
+        }
+    }
+    float scale = 1.f;
+    if (CACHE == MLA_FP8_E4M3) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (lane + i * 64 < vecs) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) top = max(top, magnitude(v[i][k]));
+            }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+        scale = block_scale(top);
+        if (lane == 0) p.kv_scale[at] = scale;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = lane + i * 64;
+        if (c >= vecs) continue;
+        const int64_t o = at * n + c * 8;
+        if constexpr (CACHE == MLA_FP8_E4M3)
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.kv) + o) =
+                make_uint2(e4m3_quad(v[i][0] / scale, v[i][1] / scale, v[i][2] / scale, v[i][3] / scale),
+                           e4m3_quad(v[i][4] / scale, v[i][5] / scale, v[i][6] / scale, v[i][7] / scale));
+        else
+            store_vec<CACHE == MLA_F32, 8>(p.kv, o, v[i]);
+    }
+}
+
+// any widths and addresses; one workgroup per row, the row in LDS as fp32
+template <bool F32, bool HALF, int CACHE>
+__global__ __launch_bounds__(256) void cache_store_any_kernel(StoreParams p)
 {
     __shared__ float row[MAX_ROW];
     __shared__ float part[4];
     __shared__ uint32_t tops[4];
-    const int r = blockIdx.x, b = r / p.new_tokens, tid = threadIdx.x;
+    const int r = blockIdx.x, tid = threadIdx.x;
     const int n = p.d_c + p.d_rope, pairs = p.d_rope / 2;
-    const int pos = p.positions[r];
-    if (pos < 0 || pos >= p.max_pages * p.page_size) return;                       // outside the table
-    const int page = p.page_table[(int64_t)b * p.max_pages + pos / p.page_size];
-    if (page < 0 || page >= p.num_pages) return;                                   // outside the pool
-    const int64_t at = (int64_t)page * p.page_size + pos % p.page_size;
+    int pos;
+    const int64_t at = place_of(p, r, pos);
+    if (at < 0) return;
     auto load = [&](const void* base, int64_t i) {
         return F32 ? static_cast<const float*>(base)[i] : bf16_bits_to_f32(static_cast<const uint16_t*>(base)[i]);
     };
@@ -74,9 +308,9 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
     }
     if (tid < pairs) {
         const int re = p.d_c + (HALF ? tid : 2 * tid), im = p.d_c + (HALF ? tid + pairs : 2 * tid + 1);
-        const float x = row[re], y = row[im];
-        row[re] = x * cs - y * sn;
-        row[im] = x * sn + y * cs;
+        const float2 z = rotate(row[re], row[im], cs, sn);
+        row[re] = z.x;
+        row[im] = z.y;
     }
     __syncthreads();
     if (CACHE == MLA_F32) {
@@ -96,35 +330,62 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
     }
 }
 
+bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+template <bool F32, bool HALF> void rope(const RopeParams& p, hipStream_t s)
+{
+    // vectors of 8 or 4 values: they have to fit the parts of a head's row, and every row to lie on their bytes
+    const int unit = HALF ? p.d_rope / 2 : p.d_rope;
+    auto fits = [&](int v) {
+        const int bytes = F32 ? 16 : 2 * v, per = bytes / (F32 ? 4 : 2);
+        return p.d_nope % v == 0 && unit % v == 0 && p.pitch % per == 0 && on(p.q, bytes) && on(p.q_nope, bytes) && on(p.q_rope, bytes) &&
+               p.d_nope <= 4096;
+    };
+    const int v = fits(8) ? 8 : fits(4) ? 4 : 0;
+    if (!v) {
+        rope_queries_any_kernel<F32, HALF><<<dim3((unsigned)p.T), dim3(256), 0, s>>>(p);
+        return;
+    }
+    // 64 heads' rows per workgroup, fewer while that leaves CUs without one
+    int heads = std::min(p.H, 64), tokens = std::max(1, std::min(64 / heads, ROPE_TOKENS));
+    auto grid_of = [&] { return (int64_t)((p.T + tokens - 1) / tokens) * ((p.H + heads - 1) / heads); };
+    while (grid_of() < 512 && tokens > 1) tokens = (tokens + 1) / 2;
+    while (grid_of() < 512 && heads > 4) heads = (heads + 1) / 2;
+    const int groups = (p.H + heads - 1) / heads;
+    const dim3 grid((unsigned)grid_of()), block(256);
+    if (v == 8) rope_queries_kernel<F32, HALF, 8><<<grid, block, 0, s>>>(p, tokens, heads, groups);
+    else        rope_queries_kernel<F32, HALF, 4><<<grid, block, 0, s>>>(p, tokens, heads, groups);
+}
+
+template <bool F32, bool HALF, int CACHE> void store_rows(const StoreParams& p, hipStream_t s)
+{
+    const int n = p.d_c + p.d_rope;
+    const bool vec = p.d_c % 8 == 0 && p.d_rope % (HALF ? 16 : 8) == 0 && p.pitch % (F32 ? 4 : 8) == 0 && on(p.rows, 16) &&
+                     on(p.norm_weight, 16) && on(p.kv, 16) && n <= MAX_ROW;
+    if (vec) cache_store_kernel<F32, HALF, CACHE><<<dim3((unsigned)((p.rows_total + 3) / 4)), dim3(256), 0, s>>>(p);
+    else     cache_store_any_kernel<F32, HALF, CACHE><<<dim3((unsigned)p.rows_total), dim3(256), 0, s>>>(p);
+}
+
+template <bool F32, bool HALF> void store(const StoreParams& p, mla_dtype cache, hipStream_t s)
+{
+    if (cache == MLA_F32)       store_rows<F32, HALF, MLA_F32>(p, s);
+    else if (cache == MLA_BF16) store_rows<F32, HALF, MLA_BF16>(p, s);
+    else                        store_rows<F32, HALF, MLA_FP8_E4M3>(p, s);
+}
+
 }  // namespace
 
 hipError_t launch_rope_queries(const RopeParams& p, int layout, mla_dtype io, hipStream_t s)
 {
-    const dim3 grid((unsigned)p.T), block(256);
-    if (io == MLA_F32) {
-        if (layout == MLA_ROPE_HALF) rope_queries_kernel<true, true><<<grid, block, 0, s>>>(p);
-        else                         rope_queries_kernel<true, false><<<grid, block, 0, s>>>(p);
-    } else {
-        if (layout == MLA_ROPE_HALF) rope_queries_kernel<false, true><<<grid, block, 0, s>>>(p);
-        else                         rope_queries_kernel<false, false><<<grid, block, 0, s>>>(p);
-    }
+    if (io == MLA_F32) layout == MLA_ROPE_HALF ? rope<true, true>(p, s) : rope<true, false>(p, s);
+    else               layout == MLA_ROPE_HALF ? rope<false, true>(p, s) : rope<false, false>(p, s);
     return hipGetLastError();
 }
 
-namespace {
-template <bool F32, bool HALF> void store_rows(const StoreParams& p, mla_dtype cache, hipStream_t s)
-{
-    const dim3 grid((unsigned)p.rows_total), block(256);
-    if (cache == MLA_F32)       cache_store_kernel<F32, HALF, MLA_F32><<<grid, block, 0, s>>>(p);
-    else if (cache == MLA_BF16) cache_store_kernel<F32, HALF, MLA_BF16><<<grid, block, 0, s>>>(p);
-    else                        cache_store_kernel<F32, HALF, MLA_FP8_E4M3><<<grid, block, 0, s>>>(p);
-}
-}  // namespace
-
 hipError_t launch_cache_store(const StoreParams& p, int layout, mla_dtype io, mla_dtype cache, hipStream_t s)
 {
-    if (io == MLA_F32) layout == MLA_ROPE_HALF ? store_rows<true, true>(p, cache, s) : store_rows<true, false>(p, cache, s);
-    else               layout == MLA_ROPE_HALF ? store_rows<false, true>(p, cache, s) : store_rows<false, false>(p, cache, s);
+    if (io == MLA_F32) layout == MLA_ROPE_HALF ? store<true, true>(p, cache, s) : store<true, false>(p, cache, s);
+    else               layout == MLA_ROPE_HALF ? store<false, true>(p, cache, s) : store<false, false>(p, cache, s);
     return hipGetLastError();
 }
 
