@@ -16,6 +16,7 @@
 #include "mfma_tile.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace mla {
 namespace {
@@ -149,8 +150,8 @@ __device__ __attribute__((aligned(16))) const uint32_t zeros16[4] = {0u, 0u, 0u,
 //
 // What bounds it: power.  At 32768 x 6144 x 4096 the matrix cores are busy 55 - 65 % of the cycles at 1.65 - 1.7 GHz of the
 // card's 2.4.
-template <int MT, int STAGES, bool FAST, bool F32, bool SPLIT>
-__global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int tiles_m, int tiles_n, int splits, bool stream_out)
+template <int MT, int STAGES, bool FAST, bool F32, bool SPLIT, bool STREAM>
+__global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int tiles_m, int tiles_n, int splits)
 {
     constexpr int W_B = 256 * QBLOCK, A_B = 128 * MT * QBLOCK, STAGE = W_B + A_B + 2048;   // weights | tokens | scales
     constexpr int WLOADS = 4, ALOADS = 2 * MT, LOADS = WLOADS + ALOADS + 1;                // per wavefront and block
@@ -350,9 +351,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
                 if (m >= p.M || c >= p.N) continue;
                 const int64_t o = (int64_t)m * p.N + c;
                 if (wide) {
-                    u32x4* dst = reinterpret_cast<u32x4*>(static_cast<unsigned char*>(out) + o * (O32 ? 4 : 2));
-                    if (stream_out) __builtin_nontemporal_store(v, dst);
-                    else            *dst = v;
+                    put_words<STREAM>(static_cast<unsigned char*>(out) + o * (O32 ? 4 : 2), v);
                 } else {
 #pragma unroll
                     for (int e = 0; e < PER; ++e)
@@ -587,10 +586,13 @@ template <int MT, int STAGES, bool FAST> void launch_tiles(const GemmFp8Params& 
 {
     const int tm = (p.M + 128 * MT - 1) / (128 * MT), tn = (p.N + 255) / 256;
     const dim3 grid((unsigned)(((long)tm * tn * splits + 7) / 8 * 8)), block(512);
-    const bool stream_out = (int64_t)p.M * p.N * (f32 ? 4 : 2) > (int64_t)64 << 20;
-    if (MT == 1 && splits > 1) gemm_tile_kernel<1, STAGES, FAST, false, true><<<grid, block, 0, s>>>(p, tm, tn, splits, false);
-    else if (f32)   gemm_tile_kernel<MT, STAGES, FAST, true, false><<<grid, block, 0, s>>>(p, tm, tn, 1, stream_out);
-    else            gemm_tile_kernel<MT, STAGES, FAST, false, false><<<grid, block, 0, s>>>(p, tm, tn, 1, stream_out);
+    const bool stream = (int64_t)p.M * p.N * (f32 ? 4 : 2) > STREAM_BYTES;
+    auto run = [&](auto is_f32, auto is_stream) {
+        gemm_tile_kernel<MT, STAGES, FAST, decltype(is_f32)::value, false, decltype(is_stream)::value><<<grid, block, 0, s>>>(p, tm, tn, 1);
+    };
+    if (MT == 1 && splits > 1) gemm_tile_kernel<1, STAGES, FAST, false, true, false><<<grid, block, 0, s>>>(p, tm, tn, splits);
+    else if (f32)              stream ? run(std::true_type{}, std::true_type{}) : run(std::true_type{}, std::false_type{});
+    else                       stream ? run(std::false_type{}, std::true_type{}) : run(std::false_type{}, std::false_type{});
     if (splits > 1) {
         const dim3 mg((unsigned)std::min<int64_t>(((int64_t)p.M * p.N + 255) / 256, 4096));
         if (f32) gemm_merge_kernel<true><<<mg, dim3(256), 0, s>>>(p, splits);

@@ -74,7 +74,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormPar
         const uint32_t hi = e4m3_quad(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
         uint8_t* dst = p.codes + (int64_t)row * p.D + c;
         if constexpr (VEC) {
-            *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
+            *reinterpret_cast<words2*>(dst) = (words2){lo, hi};
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k)

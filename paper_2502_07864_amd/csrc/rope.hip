@@ -29,7 +29,7 @@ constexpr int ROPE_TOKENS = 16, ROPE_UNITS = 4;
 // j / d for small numbers (j < 2^16: the quotient's error stays below the half that is added)
 __device__ __forceinline__ int divide(int j, float inv_d) { return (int)(((float)j + 0.5f) * inv_d); }
 
-template <bool F32, bool HALF, int V>
+template <bool F32, bool HALF, int V, bool STREAM>
 __global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p, int tokens, int heads, int groups)
 {
     __shared__ float2 turns[ROPE_TOKENS * MAX_PAIRS];
@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p, int tok
     const int nv = p.d_nope / V, rv = (HALF ? pairs : p.d_rope) / V;       // vectors of a head's row
     const int n_nope = rows * nv, n_rope = rows * rv;
     const float inv_nv = 1.f / (float)max(nv, 1), inv_rv = 1.f / (float)rv, inv_nh = 1.f / (float)nh;
-    using vec = std::conditional_t<V == 8 && !F32, uint4, std::conditional_t<F32, uint4, uint2>>;
+    using vec = std::conditional_t<V == 8 || F32, words4, words2>;
     constexpr int PARTS = F32 && V == 8 ? 2 : 1;                           // 16-byte accesses of a vector
 
     auto row_of = [&](int r, int& t, int& h) { t = divide(r, inv_nh); h = h0 + r - t * nh; t += t0; };
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p, int tok
             row_of(r, t, h);
             char* dst = static_cast<char*>(p.q_nope) + (((int64_t)t * p.H + h) * p.d_nope + (j - r * nv) * V) * size;
 #pragma unroll
-            for (int k = 0; k < PARTS; ++k) reinterpret_cast<vec*>(dst)[k] = buf[i][k];
+            for (int k = 0; k < PARTS; ++k) put_words<STREAM>(reinterpret_cast<vec*>(dst) + k, buf[i][k]);
         }
     };
     auto load = [&](int j, float (&a)[V], float (&b)[V], int64_t& to, int& at) {
@@ -89,8 +89,8 @@ __global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p, int tok
                 a[k] = z.x;
                 b[k] = z.y;
             }
-            store_vec<F32, V>(p.q_rope, to, a);
-            store_vec<F32, V>(p.q_rope, to + pairs, b);
+            store_vec<F32, V, STREAM>(p.q_rope, to, a);
+            store_vec<F32, V, STREAM>(p.q_rope, to + pairs, b);
         } else {
 #pragma unroll
             for (int k = 0; k < V; k += 2) {
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p, int tok
                 a[k] = z.x;
                 a[k + 1] = z.y;
             }
-            store_vec<F32, V>(p.q_rope, to, a);
+            store_vec<F32, V, STREAM>(p.q_rope, to, a);
         }
     };
 
@@ -346,15 +346,23 @@ template <bool F32, bool HALF> void rope(const RopeParams& p, hipStream_t s)
         rope_queries_any_kernel<F32, HALF><<<dim3((unsigned)p.T), dim3(256), 0, s>>>(p);
         return;
     }
-    // 64 heads' rows per workgroup, fewer while that leaves CUs without one
-    int heads = std::min(p.H, 64), tokens = std::max(1, std::min(64 / heads, ROPE_TOKENS));
+    // As many heads' rows per workgroup as give half of its threads a vector to turn (32768 tokens x 32 heads, 16 / 32 / 64 rows:
+    // pairs 131 / 141 / 146 us, halves 157 / 138 / 147), fewer while that leaves CUs without one
+    const int rows = std::max(1, 128 / (unit / v));
+    int heads = std::min(p.H, rows), tokens = std::max(1, std::min(rows / heads, ROPE_TOKENS));
     auto grid_of = [&] { return (int64_t)((p.T + tokens - 1) / tokens) * ((p.H + heads - 1) / heads); };
     while (grid_of() < 512 && tokens > 1) tokens = (tokens + 1) / 2;
     while (grid_of() < 512 && heads > 4) heads = (heads + 1) / 2;
     const int groups = (p.H + heads - 1) / heads;
     const dim3 grid((unsigned)grid_of()), block(256);
-    if (v == 8) rope_queries_kernel<F32, HALF, 8><<<grid, block, 0, s>>>(p, tokens, heads, groups);
-    else        rope_queries_kernel<F32, HALF, 4><<<grid, block, 0, s>>>(p, tokens, heads, groups);
+    const bool stream = (int64_t)p.T * p.H * (p.d_nope + p.d_rope) * (F32 ? 4 : 2) > STREAM_BYTES;
+    auto run = [&](auto vec) {
+        constexpr int V = decltype(vec)::value;
+        if (stream) rope_queries_kernel<F32, HALF, V, true><<<grid, block, 0, s>>>(p, tokens, heads, groups);
+        else        rope_queries_kernel<F32, HALF, V, false><<<grid, block, 0, s>>>(p, tokens, heads, groups);
+    };
+    if (v == 8) run(std::integral_constant<int, 8>{});
+    else        run(std::integral_constant<int, 4>{});
 }
 
 template <bool F32, bool HALF, int CACHE> void store_rows(const StoreParams& p, hipStream_t s)
