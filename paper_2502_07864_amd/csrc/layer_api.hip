@@ -11,8 +11,8 @@ bool io_ok(mla_dtype t) { return t == MLA_F32 || t == MLA_BF16; }
 int status_of(hipError_t e) { return e == hipSuccess ? MLA_OK : MLA_ERR_HIP; }
 bool layout_ok(int l) { return l == MLA_ROPE_INTERLEAVED || l == MLA_ROPE_HALF; }
 
-// A workgroup of 256 threads per row at most: the grid's threads are counted in 32 bits
-constexpr int MAX_ROWS = (1 << 24) - 1;
+// A workgroup of up to 512 threads per row: the grid's threads are counted in 32 bits
+constexpr int MAX_ROWS = (1 << 23) - 1;
 
 int rows_call(const NormParams& p, bool norm, mla_dtype io, void* stream)
 {

@@ -8,7 +8,8 @@ namespace mla {
 constexpr int QBLOCK = 128;        // columns (and weight rows) per scale
 constexpr float E4M3_MAX = 448.f;
 // Outputs beyond this many bytes go past the caches: they are read again from memory anyway, and what they would displace is
-// not (32768 tokens x 32 heads of queries 167 us kept, 131 streamed; norms and cache rows show no difference)
+// not (us, kept / streamed: queries of 32768 tokens x 32 heads 167 / 131, norm of 32768 x 4096 161 / 155, product of
+// 32768 x 6144 803 / 771; at 8192 tokens and below no difference)
 constexpr int64_t STREAM_BYTES = (int64_t)64 << 20;
 
 struct NormParams {
@@ -137,10 +138,10 @@ template <bool F32, bool VEC> __device__ __forceinline__ void load8(const void* 
     }
 }
 
-template <bool F32, bool VEC> __device__ __forceinline__ void store8(void* base, int64_t at, int left, const float (&v)[8])
+template <bool F32, bool VEC, bool STREAM = false> __device__ __forceinline__ void store8(void* base, int64_t at, int left, const float (&v)[8])
 {
     if constexpr (VEC) {
-        store_vec<F32, 8>(base, at, v);
+        store_vec<F32, 8, STREAM>(base, at, v);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)

@@ -9,30 +9,35 @@ namespace mla {
 namespace {
 
 // TPR threads per row, NV vectors of eight columns per thread (8 TPR NV >= D).
-template <bool F32, int TPR, int NV, bool VEC, bool NORM>
+// Memory bound: 32768 x 4096 bf16 with residual and codes moves 940 MB in 155 us (6.1 TB/s).  Wide rows take 512 threads
+// with one vector each: with 256, 128, 64 threads and 2, 4, 8 vectors it was 162, 169, 193 us, and 3.6, 5.4, 8.5 against
+// 3.1 us for 64 tokens.
+template <bool F32, int TPR, int NV, bool VEC, bool NORM, bool STREAM>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormParams p)
 {
-    constexpr int THREADS = TPR < 256 ? 256 : TPR;
+    constexpr int THREADS = TPR < 256 ? 256 : TPR, WAVES = TPR / 64;       // wavefronts per row
+    __shared__ float part[THREADS / 64];
     const int tid = threadIdx.x, t = tid % TPR;
-    const int row = blockIdx.x * (THREADS / TPR) + tid / TPR;
-    if (TPR <= 64 && row >= p.T) return;                 // (wider rows are a workgroup each: the grid is T)
+    const int64_t mine = (int64_t)blockIdx.x * (THREADS / TPR) + tid / TPR;
+    const bool live = mine < p.T;                                          // (the others repeat the last row and store nothing)
+    const int64_t row = live ? mine : p.T - 1;
 
-    float v[NV][8];
+    float v[NV][8], w[NV][8];
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + t) * 8;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
+        for (int k = 0; k < 8; ++k) { v[i][k] = 0.f; w[i][k] = 1.f; }
         if (c < p.D) {
-            load8<F32, VEC>(p.x, (int64_t)row * p.x_pitch + c, p.D - c, v[i]);
+            load8<F32, VEC>(p.x, row * p.x_pitch + c, p.D - c, v[i]);
             if (NORM && p.residual) {
                 float r[8];
-                load8<F32, VEC>(p.residual, (int64_t)row * p.D + c, p.D - c, r);
+                load8<F32, VEC>(p.residual, row * p.D + c, p.D - c, r);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[i][k] += r[k];
-                store8<F32, VEC>(p.residual_out, (int64_t)row * p.D + c, p.D - c, v[i]);
             }
+            if (NORM && p.weight) load8<F32, VEC>(p.weight, c, p.D - c, w[i]);
         }
         if (NORM) {
 #pragma unroll
@@ -40,24 +45,28 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormPar
         }
     }
     if (NORM) {
+        if (p.residual_out && live) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * TPR + t) * 8;
+                if (c < p.D) store8<F32, VEC, STREAM>(p.residual_out, row * p.D + c, p.D - c, v[i]);
+            }
+        }
         sum = wave_sum(sum);
-        if constexpr (TPR > 64) {
-            __shared__ float part[TPR / 64];
-            if (t % 64 == 0) part[t / 64] = sum;
+        if constexpr (WAVES > 1) {
+            if (tid % 64 == 0) part[tid / 64] = sum;
             __syncthreads();
             sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < TPR / 64; ++i) sum += part[i];
+            for (int i = 0; i < WAVES; ++i) sum += part[tid / TPR * WAVES + i];
         }
         const float inv = 1.f / sqrtf(sum / (float)p.D + p.eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * TPR + t) * 8;
-            float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-            if (p.weight && c < p.D) load8<F32, VEC>(p.weight, c, p.D - c, w);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * inv * w[k];
-            if (p.y && c < p.D) store8<F32, VEC>(p.y, (int64_t)row * p.D + c, p.D - c, v[i]);
+            for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * inv * w[i][k];
+            if (p.y && c < p.D && live) store8<F32, VEC, STREAM>(p.y, row * p.D + c, p.D - c, v[i]);
         }
     }
     if (!p.codes) return;
@@ -66,15 +75,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormPar
         const int c = (i * TPR + t) * 8;
         uint32_t top = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) top = max(top, magnitude(v[i][k]));
-        const float scale = block_scale(row_max(top)), inv = 1.f / scale;      // (columns past D are zeros)
-        if (c >= p.D) continue;
+        for (int k = 0; k < 8; ++k) top = max(top, c + k < p.D ? magnitude(v[i][k]) : 0u);
+        const float scale = block_scale(row_max(top)), inv = 1.f / scale;
+        if (c >= p.D || !live) continue;
         if (c % QBLOCK == 0) p.scales[(int64_t)(c / QBLOCK) * p.T + row] = scale;
         const uint32_t lo = e4m3_quad(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
         const uint32_t hi = e4m3_quad(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
-        uint8_t* dst = p.codes + (int64_t)row * p.D + c;
+        uint8_t* dst = p.codes + row * p.D + c;
         if constexpr (VEC) {
-            *reinterpret_cast<words2*>(dst) = (words2){lo, hi};
+            put_words<STREAM>(dst, (words2){lo, hi});
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -109,21 +118,24 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(const void* w, ui
             codes[(int64_t)(n0 + r) * K + k0 + c] = (uint8_t)e4m3_quad(at(r, c) * inv, 0.f, 0.f, 0.f);
 }
 
-template <bool F32, int TPR, int NV, bool NORM> void launch_rows(const NormParams& p, bool vec, hipStream_t s)
+template <bool F32, int TPR, int NV, bool NORM> void launch_rows(const NormParams& p, bool vec, bool stream, hipStream_t s)
 {
     constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
     const dim3 grid((unsigned)((p.T + ROWS - 1) / ROWS)), block(THREADS);
-    if (vec) rms_norm_kernel<F32, TPR, NV, true, NORM><<<grid, block, 0, s>>>(p);
-    else     rms_norm_kernel<F32, TPR, NV, false, NORM><<<grid, block, 0, s>>>(p);
+    if (!vec)        rms_norm_kernel<F32, TPR, NV, false, NORM, false><<<grid, block, 0, s>>>(p);
+    else if (stream) rms_norm_kernel<F32, TPR, NV, true, NORM, true><<<grid, block, 0, s>>>(p);
+    else             rms_norm_kernel<F32, TPR, NV, true, NORM, false><<<grid, block, 0, s>>>(p);
 }
 
-template <bool F32, bool NORM> void launch_dim(const NormParams& p, bool vec, hipStream_t s)
+template <bool F32, bool NORM> void launch_dim(const NormParams& p, bool vec, bool stream, hipStream_t s)
 {
-    if      (p.D <= 2048)  launch_rows<F32, 256, 1, NORM>(p, vec, s);
-    else if (p.D <= 4096)  launch_rows<F32, 256, 2, NORM>(p, vec, s);
-    else if (p.D <= 8192)  launch_rows<F32, 256, 4, NORM>(p, vec, s);
-    else if (p.D <= 16384) launch_rows<F32, 256, 8, NORM>(p, vec, s);
-    else                   launch_rows<F32, 256, 16, NORM>(p, vec, s);
+    if      (p.D <= 512)   launch_rows<F32, 64, 1, NORM>(p, vec, stream, s);
+    else if (p.D <= 1024)  launch_rows<F32, 128, 1, NORM>(p, vec, stream, s);
+    else if (p.D <= 2048)  launch_rows<F32, 256, 1, NORM>(p, vec, stream, s);
+    else if (p.D <= 4096)  launch_rows<F32, 512, 1, NORM>(p, vec, stream, s);
+    else if (p.D <= 8192)  launch_rows<F32, 512, 2, NORM>(p, vec, stream, s);
+    else if (p.D <= 16384) launch_rows<F32, 512, 4, NORM>(p, vec, stream, s);
+    else                   launch_rows<F32, 512, 8, NORM>(p, vec, stream, s);
 }
 
 bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
@@ -136,8 +148,10 @@ hipError_t launch_rms_norm(const NormParams& p, bool norm, mla_dtype io, hipStre
     const int per16 = io == MLA_F32 ? 4 : 8;
     const bool vec = p.D % 8 == 0 && p.x_pitch % per16 == 0 && on(p.x, 16) && on(p.residual, 16) && on(p.residual_out, 16) &&
                      on(p.weight, 16) && on(p.y, 16) && on(p.codes, 8);
-    if (io == MLA_F32) norm ? launch_dim<true, true>(p, vec, s) : launch_dim<true, false>(p, vec, s);
-    else               norm ? launch_dim<false, true>(p, vec, s) : launch_dim<false, false>(p, vec, s);
+    const int wide = (p.residual_out ? 1 : 0) + (p.y ? 1 : 0);
+    const bool stream = (int64_t)p.T * p.D * (wide * (io == MLA_F32 ? 4 : 2) + (p.codes ? 1 : 0)) > STREAM_BYTES;
+    if (io == MLA_F32) norm ? launch_dim<true, true>(p, vec, stream, s) : launch_dim<true, false>(p, vec, stream, s);
+    else               norm ? launch_dim<false, true>(p, vec, stream, s) : launch_dim<false, false>(p, vec, stream, s);
     return hipGetLastError();
 }
 
