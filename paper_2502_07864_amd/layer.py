@@ -54,11 +54,20 @@ def _new_codes(T: int, D: int, device, codes, scales):
     return codes, scales
 
 
+# As in mla.py the native path is asked first, and what it does not take (None) the checks below decide.
+
 def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
              residual: Optional[torch.Tensor] = None, residual_out: Optional[torch.Tensor] = None,
              out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """y = s / sqrt(mean(s^2) + eps) * weight with s = x + residual;  x [T, D] (rows may be apart), residual [T, D],
     weight [D].  Returns (y, s), s None without a residual."""
+    fast = mla._fast
+    if fast is not None and out is not None:
+        status = fast.rms_norm(x, weight, eps, residual, residual_out, out, None, None)
+        if status == 0:
+            return out, residual_out
+        if status is not None:
+            _check(status, "mla_rms_norm")
     if out is None:
         if x.dim() != 2:
             raise ValueError("x must be [T, D]")
@@ -72,6 +81,13 @@ def rms_norm_fp8(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: fl
                  out: Optional[torch.Tensor] = None):
     """rms_norm whose y comes as e4m3 codes [T, D] and scales [ceil(D/128), T], for gemm_fp8.
     Returns (codes, scales, s, y): s None without a residual, y None unless `out` is passed (it is then written too)."""
+    fast = mla._fast
+    if fast is not None and codes is not None:
+        status = fast.rms_norm(x, weight, eps, residual, residual_out, out, codes, scales)
+        if status == 0:
+            return codes, scales, residual_out, out
+        if status is not None:
+            _check(status, "mla_rms_norm")
     if codes is None or scales is None:
         if x.dim() != 2:
             raise ValueError("x must be [T, D]")
@@ -80,17 +96,12 @@ def rms_norm_fp8(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: fl
 
 
 def _norm(x, weight, eps, residual, residual_out, out, codes, scales):
-    if residual is not None and residual_out is None:
-        residual_out = torch.empty_like(residual, memory_format=torch.contiguous_format)
-    if mla._fast is not None:
-        status = mla._fast.rms_norm(x, weight, eps, residual, residual_out, out, codes, scales)
-        if status is not None:
-            _check(status, "mla_rms_norm")
-            return codes, scales, residual_out, out
     if x.dim() != 2:
         raise ValueError("x must be [T, D]")
     if residual is None and residual_out is not None:
         raise ValueError("residual_out without a residual")
+    if residual is not None and residual_out is None:
+        residual_out = torch.empty_like(residual, memory_format=torch.contiguous_format)
     T, D = x.shape
     px, pitch = _rows(x, "x", T, D)
     if codes is not None:
@@ -107,11 +118,13 @@ def _norm(x, weight, eps, residual, residual_out, out, codes, scales):
 
 def quantize_rows(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None):
     """e4m3 codes [T, D] and scales [ceil(D/128), T] of x [T, D] (rows may be apart).  Returns (codes, scales)."""
-    if codes is not None and scales is not None and mla._fast is not None:
-        status = mla._fast.quantize_rows(x, codes, scales)
+    fast = mla._fast
+    if fast is not None and codes is not None:
+        status = fast.quantize_rows(x, codes, scales)
+        if status == 0:
+            return codes, scales
         if status is not None:
             _check(status, "mla_quantize_rows")
-            return codes, scales
     if x.dim() != 2:
         raise ValueError("x must be [T, D]")
     T, D = x.shape
@@ -153,13 +166,13 @@ def gemm_fp8(a: torch.Tensor, a_scales: torch.Tensor, w: torch.Tensor, w_scales:
     w_scales [ceil(N/128), ceil(K/128)].  out float32 or bfloat16 (`dtype` where it is allocated here).
     flags GEMM_FAST_SUMS: the matrix cores may add the 8-bit products as they are (twice the rate at many tokens,
     results 1.5e-5 off)."""
-    if out is not None and mla._fast is not None:
-        status = mla._fast.gemm_fp8(a, a_scales, w, w_scales, out, workspace, flags)
-        if status == -4 and workspace is None:      # sizes that want scratch: allocated below
-            status = None
-        if status is not None:
-            _check(status, "mla_gemm_fp8")
+    fast = mla._fast
+    if fast is not None and out is not None:
+        status = fast.gemm_fp8(a, a_scales, w, w_scales, out, workspace, flags)
+        if status == 0:
             return out
+        if status is not None and not (status == -4 and workspace is None):      # (sizes that want scratch: allocated below)
+            _check(status, "mla_gemm_fp8")
     if a.dim() != 2 or w.dim() != 2 or a.shape[1] != w.shape[1]:
         raise ValueError("a must be [M, K] and w [N, K]")
     if a.dtype not in _CODES or w.dtype not in _CODES:
@@ -200,11 +213,13 @@ def rope_queries(q: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, g
                  q_rope: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """q [T, H, d_nope + d_rope] (tokens may be apart) -> (q_nope [T, H, d_nope], q_rope [T, H, d_rope]), the rope part
     turned by positions[t] * freq;  positions [T] int32, freq [d_rope / 2] float64 (rope_frequencies)."""
-    if q_nope is not None and q_rope is not None and mla._fast is not None:
-        status = mla._fast.rope_queries(q, positions, freq, gain, layout, q_nope, q_rope)
+    fast = mla._fast
+    if fast is not None and q_rope is not None:
+        status = fast.rope_queries(q, positions, freq, gain, layout, q_nope, q_rope)
+        if status == 0:
+            return q_nope, q_rope
         if status is not None:
             _check(status, "mla_rope_queries")
-            return q_nope, q_rope
     if q.dim() != 3:
         raise ValueError("q must be [T, H, d_nope + d_rope]")
     T, H, width = q.shape
@@ -235,11 +250,13 @@ def cache_store(rows: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor,
                 kv_scale: Optional[torch.Tensor] = None) -> None:
     """Writes rows [B, new, d_c + d_rope] (may be apart) into kv_cache at logical positions [B, new]: the latent part
     as it is or RMS-normed with norm_weight [d_c], the rope part turned by positions * freq."""
-    if mla._fast is not None:
-        status = mla._fast.cache_store(rows, positions, freq, kv_cache, page_table, d_c, gain, layout, norm_weight, eps, kv_scale)
+    fast = mla._fast
+    if fast is not None:
+        status = fast.cache_store(rows, positions, freq, kv_cache, page_table, d_c, gain, layout, norm_weight, eps, kv_scale)
+        if status == 0:
+            return
         if status is not None:
             _check(status, "mla_cache_store")
-            return
     if rows.dim() != 3 or kv_cache.dim() != 3:
         raise ValueError("rows must be [B, new, d_c + d_rope], kv_cache [num_pages, page_size, d_c + d_rope]")
     B, T, row = rows.shape
