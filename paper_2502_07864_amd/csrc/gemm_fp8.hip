@@ -103,7 +103,7 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_rows_kernel(GemmFp8Params p)
                 if (in) av[u][i] = *reinterpret_cast<const u32x4*>(a + k + 64 * i);
             }
             // (a block past the end is zeros, but its scale need not be finite)
-            f[u] = b < blocks ? ws[b] * as[(int64_t)b * p.M] : 0.f;
+            f[u] = b < blocks ? ws[b] * as[(int64_t)b * p.scale_pitch] : 0.f;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
     // scales: wavefronts 0 .. 2 MT - 1 bring the tokens', the others the weights' two (only those of wavefront 2 MT are read)
     const bool tokens = wave < 2 * MT;
     const float* scale0 = tokens ? p.a_scales + m0 : p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
-    const int64_t scale_step = tokens ? p.M : 1;
+    const int64_t scale_step = tokens ? p.scale_pitch : 1;
     const uint32_t off_s = 4u * (tokens ? (uint32_t)min(wave * 64 + lane, p.M - 1 - m0) : (uint32_t)min(lane & 1, (p.N - 1 - n0) / QBLOCK) * (uint32_t)blocks);
     auto load = [&](int kb, uint32_t stage, int k) {
         if (k < WLOADS + ALOADS) {
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
     const bool tokens = si < KS * A_ROWS;
     const int s_block = tokens ? si / A_ROWS : lane % KS;
     const float* s_src = tokens ? p.a_scales + min(m0 + si % A_ROWS, p.M - 1) : p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
-    const int64_t s_step = tokens ? p.M : 1;
+    const int64_t s_step = tokens ? p.scale_pitch : 1;
     auto request = [&](int step, uint32_t stage) {
         const int b0 = step * KS;
         if ((b0 + KS) * QBLOCK <= p.K) {
@@ -526,24 +526,25 @@ __global__ __launch_bounds__(256) void gemm_merge_kernel(GemmFp8Params p, int sp
 enum Form { ROWS16, ROWS32, SMALL_1x1, SMALL_1x2, SMALL_2x2, SMALL_2x4, TILE128, TILE256 };
 struct Plan {
     Form form;
-    int splits;
+    int splits;      // shares of K
+    int tokens;      // of this launch; those beyond go to another
+    float us;
 };
 
 // The form that a model of the times finds fastest: a launch, and per round of 256 workgroups (each fills its CU) the steps
 // over K, or the time that the operands take from memory.  us per step measured with few workgroups, on codes (fast) and on
-// f16; the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  On 115
-// sizes of 1 to 32768 tokens and five (N, K) the choice takes up to 17 % longer than the best form, at most 7 % on nine in ten.
-Plan plan_of(int M, int N, int K, bool fast)
+// f16; the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  On 186
+// sizes of 1 to 32768 tokens and six (N, K) the choice takes up to 17 % longer than the best form, at most 7 % on most.
+Plan one_launch(int M, int N, int K, bool fast)
 {
     const int blocks = (K + QBLOCK - 1) / QBLOCK;
-    if (M <= 16) return {(N + 15) / 16 <= 256 ? ROWS16 : ROWS32, 1};     // 6144 x 4096, one token: 7.3 / 7.0 us; 3584 x 3584: 4.5 / 6.0
+    if (M <= 16) return {(N + 15) / 16 <= 256 ? ROWS16 : ROWS32, 1, M, 4.f + (float)N * (float)K / 5.5e6f};     // 6144 x 4096, one token: 7.3 / 7.0 us; 3584 x 3584: 4.5 / 6.0
     struct Shape { Form form; int tokens, outputs, blocks; float launch, step_fast, step_f16, crowded_fast, crowded_f16; };
     static const Shape shapes[] = {
         {SMALL_1x1, 32, 32, 8, 3.3f, 0.67f, 0.83f, 1.9f, 1.9f}, {SMALL_1x2, 64, 32, 4, 3.8f, 0.50f, 0.70f, 1.65f, 1.65f},
-        {SMALL_2x2, 64, 64, 2, 3.7f, 0.41f, 0.62f, 1.35f, 1.43f}, {SMALL_2x4, 128, 64, 1, 3.9f, 0.34f, 0.63f, 1.3f, 1.3f},
-        {TILE128, 128, 256, 1, 4.2f, 0.59f, 1.30f, 1.6f, 1.3f}, {TILE256, 256, 256, 1, 4.8f, 1.00f, 0.f, 1.75f, 0.f}};
-    Plan best = {TILE128, 1};
-    float least = 3e38f;
+        {SMALL_2x2, 64, 64, 2, 3.7f, 0.41f, 0.62f, 1.35f, 1.43f}, {SMALL_2x4, 128, 64, 1, 3.9f, 0.34f, 0.63f, 1.5f, 1.4f},
+        {TILE128, 128, 256, 1, 4.2f, 0.59f, 1.30f, 1.8f, 1.5f}, {TILE256, 256, 256, 1, 4.8f, 1.00f, 0.f, 1.85f, 0.f}};
+    Plan best = {TILE128, 1, M, 3e38f};
     for (const Shape& f : shapes) {
         if (f.form == TILE256 && !fast) continue;                        // (its registers are taken on f16)
         const long tiles_m = (M + f.tokens - 1) / f.tokens, tiles = tiles_m * ((N + f.outputs - 1) / f.outputs);
@@ -556,10 +557,33 @@ Plan plan_of(int M, int N, int K, bool fast)
             const float memory = ((float)N + (float)M) * (float)K / 5.5e6f;
             float t = f.launch + std::max(memory, (float)rounds * (float)((steps + s - 1) / s) * step);
             if (s > 1) t += 2.5f + (float)s * (float)M * (float)N * 8.f / 8e6f;      // (the partial sums, in the caches)
-            if (t < least) { least = t; best = {f.form, s}; }
+            if (t < best.us) best = {f.form, s, M, t};
         }
     }
     return best;
+}
+
+// One launch, or one whose tiles fill whole rounds and another for the tokens that are left: the last round of large tiles
+// is rarely full (4000 x 5376 x 3584: 336 tiles, 86 us; 252 and the rest in smaller ones 83 us).
+Plan plan_of(int M, int N, int K, bool fast)
+{
+    Plan best = one_launch(M, N, K, fast);
+    const int rows = best.form == TILE256 ? 256 : best.form == TILE128 && best.splits == 1 ? 128 : 0;
+    if (!rows) return best;
+    const long across = (N + 255) / 256, down = (M + rows - 1) / rows, rounds = (down * across) / 256;
+    const long whole = rounds * 256 / across;                            // rows of tiles in so many rounds
+    if (whole < 1 || whole >= down) return best;
+    const int tokens = (int)whole * rows;
+    const Plan main = one_launch(tokens, N, K, fast), rest = one_launch(M - tokens, N, K, fast);
+    const float us = main.us + rest.us - 2.f;                            // (the second launch is in place when the first ends)
+    return us < best.us ? Plan{main.form, main.splits, tokens, us} : best;
+}
+
+long workgroups(const Plan& plan, int N)
+{
+    static const int tile[][2] = {{16, 16}, {16, 32}, {32, 32}, {64, 32}, {64, 64}, {128, 64}, {128, 256}, {256, 256}};
+    const int* t = tile[plan.form];
+    return (long)((plan.tokens + t[0] - 1) / t[0]) * ((N + t[1] - 1) / t[1]) * plan.splits;
 }
 
 template <int NT, int WAVES, int U> void launch_rows(const GemmFp8Params& p, bool f32, hipStream_t s)
@@ -602,30 +626,54 @@ template <int MT, int STAGES, bool FAST> void launch_tiles(const GemmFp8Params& 
 
 }  // namespace
 
-size_t gemm_fp8_workspace(int M, int N, int K)
+// f(plan, tokens before it) for every launch of a product
+template <typename F> static void each_launch(int M, int N, int K, bool fast, F f)
 {
-    int splits = 1;
-    for (bool fast : {false, true}) splits = std::max(splits, plan_of(M, N, K, fast).splits);
-    return splits > 1 ? (size_t)splits * M * N * sizeof(float) : 0;
+    const Plan first = plan_of(M, N, K, fast);
+    f(first, 0);
+    if (first.tokens < M) f(one_launch(M - first.tokens, N, K, fast), first.tokens);
 }
 
-hipError_t launch_gemm_fp8(const GemmFp8Params& p, mla_dtype out, bool fast_sums, hipStream_t s)
+size_t gemm_fp8_workspace(int M, int N, int K)
+{
+    size_t most = 0;
+    for (bool fast : {false, true})
+        each_launch(M, N, K, fast, [&](const Plan& plan, int) {
+            if (plan.splits > 1) most = std::max(most, (size_t)plan.splits * plan.tokens * N * sizeof(float));
+        });
+    return most;
+}
+
+bool gemm_fp8_supported(int M, int N, int K)
+{
+    long most = 0;
+    for (bool fast : {false, true}) each_launch(M, N, K, fast, [&](const Plan& plan, int) { most = std::max(most, workgroups(plan, N)); });
+    return most < 1l << 22;              // (1024 threads each at most)
+}
+
+hipError_t launch_gemm_fp8(const GemmFp8Params& all, mla_dtype out, bool fast_sums, hipStream_t s)
 {
     const bool f32 = out == MLA_F32;
-    const Plan plan = plan_of(p.M, p.N, p.K, fast_sums);
-    switch (plan.form) {
-        case ROWS16:    launch_rows<1, 16, 2>(p, f32, s); break;
-        case ROWS32:    launch_rows<2, 16, 2>(p, f32, s); break;
-        case SMALL_1x1: launch_small_tiles<1, 1, 8, 2>(p, f32, fast_sums, s); break;
-        case SMALL_1x2: launch_small_tiles<1, 2, 4, 3>(p, f32, fast_sums, s); break;
-        case SMALL_2x2: launch_small_tiles<2, 2, 2, 4>(p, f32, fast_sums, s); break;
-        case SMALL_2x4: launch_small_tiles<2, 4, 1, 6>(p, f32, fast_sums, s); break;
-        case TILE128:
-            if (fast_sums) launch_tiles<1, 3, true>(p, f32, plan.splits, s);
-            else           launch_tiles<1, 3, false>(p, f32, plan.splits, s);
-            break;
-        case TILE256: launch_tiles<2, 2, true>(p, f32, 1, s); break;
-    }
+    each_launch(all.M, all.N, all.K, fast_sums, [&](const Plan& plan, int before) {
+        GemmFp8Params p = all;
+        p.M = plan.tokens;
+        p.a += (int64_t)before * all.K;
+        p.a_scales += before;
+        p.out = static_cast<char*>(all.out) + (int64_t)before * all.N * (f32 ? 4 : 2);
+        switch (plan.form) {
+            case ROWS16:    launch_rows<1, 16, 2>(p, f32, s); break;
+            case ROWS32:    launch_rows<2, 16, 2>(p, f32, s); break;
+            case SMALL_1x1: launch_small_tiles<1, 1, 8, 2>(p, f32, fast_sums, s); break;
+            case SMALL_1x2: launch_small_tiles<1, 2, 4, 3>(p, f32, fast_sums, s); break;
+            case SMALL_2x2: launch_small_tiles<2, 2, 2, 4>(p, f32, fast_sums, s); break;
+            case SMALL_2x4: launch_small_tiles<2, 4, 1, 6>(p, f32, fast_sums, s); break;
+            case TILE128:
+                if (fast_sums) launch_tiles<1, 3, true>(p, f32, plan.splits, s);
+                else           launch_tiles<1, 3, false>(p, f32, plan.splits, s);
+                break;
+            case TILE256: launch_tiles<2, 2, true>(p, f32, 1, s); break;
+        }
+    });
     return hipGetLastError();
 }
 

@@ -58,11 +58,11 @@ extern "C" int mla_gemm_fp8(const uint8_t* a, const float* a_scales, const uint8
     if (!a || !a_scales || !w || !w_scales || !out) return MLA_ERR_NULL;
     if (M <= 0 || N <= 0 || K <= 0) return MLA_ERR_SHAPE;
     if (!io_ok(out_dtype) || K % 16 || reinterpret_cast<uintptr_t>(a) % 16 || reinterpret_cast<uintptr_t>(w) % 16 ||
-        K > 1 << 23 || (flags & ~(unsigned)MLA_GEMM_FAST_SUMS))
+        K > 1 << 23 || (flags & ~(unsigned)MLA_GEMM_FAST_SUMS) || !gemm_fp8_supported(M, N, K))
         return MLA_ERR_UNSUPPORTED;
     const size_t need = gemm_fp8_workspace(M, N, K);
     if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16)) return MLA_ERR_WORKSPACE;
-    const GemmFp8Params p{a, a_scales, w, w_scales, out, static_cast<float*>(workspace), M, N, K};
+    const GemmFp8Params p{a, a_scales, w, w_scales, out, static_cast<float*>(workspace), M, N, K, M};
     return status_of(launch_gemm_fp8(p, out_dtype, (flags & MLA_GEMM_FAST_SUMS) != 0, static_cast<hipStream_t>(hip_stream)));
 }
 
