@@ -259,13 +259,14 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
 
     if (first < last) {
         const int steps = last - first;
-        // loads of the last stage beyond the first 2 MT are left to the first step (past the end: the last block
-        // again, never read)
+        // loads of the last stage beyond the first 2 MT are left to the first step
 #pragma unroll
         for (int st = 0; st < STAGES; ++st)
+            if (st < steps)
 #pragma unroll
-            for (int k = 0; k < (st < STAGES - 1 ? LOADS : 2 * MT); ++k) load(min(first + st, last - 1), st * STAGE, k);
-        wait_vmcnt<(STAGES - 2) * LOADS + 2 * MT>();
+                for (int k = 0; k < (st < STAGES - 1 ? LOADS : 2 * MT); ++k) load(first + st, st * STAGE, k);
+        if (STAGES <= steps) wait_vmcnt<(STAGES - 2) * LOADS + 2 * MT>();
+        else                 wait_vmcnt<0>();
         barrier();
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
@@ -275,16 +276,18 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
         }
         scales(0);
         uint32_t prev = (STAGES - 1) * STAGE, cur = 0;
-        for (int kb = 0; kb < steps; ++kb) {
+        // A step.  LOAD: of the blocks that take the place of the one before this and of this one the loads are still to be
+        // sent (2), only of the former (1), of neither (0)
+        auto step = [&](int kb, auto load_constant) {
+            constexpr int LOAD = decltype(load_constant)::value;
             const uint32_t next = cur + STAGE == STAGES * STAGE ? 0u : cur + STAGE;
-            // the blocks that take the place of the one before this and of this one
-            const int kp = first + min(kb + STAGES - 1, steps - 1), kl = first + min(kb + STAGES, steps - 1);
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
                 const int i = u / MT, j = u % MT;
                 if (u == UNITS - MT) {
                     // this block is read (its last weights have arrived), the next one has landed
-                    wait_vmcnt<(STAGES - 2) * LOADS>();
+                    if constexpr (LOAD) wait_vmcnt<(STAGES - 2) * LOADS>();
+                    else                wait_vmcnt<0>();
                     __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0)
                     barrier();
                 }
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
 #pragma unroll
                     for (int q = 0; q < 2; ++q) wv[(i + 1) & 1][q] = i < 3 ? half(cur, w_row + (i + 1) * 4096, q) : half(next, w_row, q);
                 }
-                if (u == 1 || UNITS == 1) {
+                if (u == 1) {
 #pragma unroll
                     for (int t = 0; t < MT; ++t) f[t] = raw.a[t] * raw.w;
                 }
@@ -305,8 +308,8 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
                     __builtin_amdgcn_sched_barrier(0);
                     if (i == 3) av[j][q] = half(next, a_row + j * 4096, q);
                     // a load per half chain from the barrier on
-                    if (i == 3) load(kl, cur, j * 2 + q);
-                    else if (2 * MT + u * 2 + q < LOADS) load(kp, prev, 2 * MT + u * 2 + q);
+                    if (i == 3) { if (LOAD == 2) load(first + kb + STAGES, cur, j * 2 + q); }
+                    else if (LOAD && 2 * MT + u * 2 + q < LOADS) load(first + kb + STAGES - 1, prev, 2 * MT + u * 2 + q);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int e = 8 * q; e < 8 * q + 8; ++e) acc[pu / MT][pu % MT][e] += s[pu & 1][e] * f[pu % MT];
@@ -316,7 +319,11 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
             }
             prev = cur;
             cur = next;
-        }
+        };
+        int kb = 0;
+        for (; kb + STAGES < steps; ++kb) step(kb, std::integral_constant<int, 2>{});
+        if (kb + STAGES == steps) step(kb++, std::integral_constant<int, 1>{});
+        for (; kb < steps; ++kb) step(kb, std::integral_constant<int, 0>{});
         wait_vmcnt<0>();
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[3][MT - 1][e] += s[1][e] * f[MT - 1];
@@ -453,15 +460,19 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
 
     f32x16 acc = {};
 #pragma unroll
-    for (int st = 0; st < STAGES; ++st) request(min(st, steps - 1), st * STAGE);           // (past the end: never read)
-    wait_vmcnt<(STAGES - 1) * LOADS>();
+    for (int st = 0; st < STAGES; ++st)
+        if (st < steps) request(st, st * STAGE);
+    if (STAGES <= steps) wait_vmcnt<(STAGES - 1) * LOADS>();
+    else                 wait_vmcnt<0>();
     barrier();
     Operands now = read(0);
     uint32_t cur = 0;
-    for (int st = 0; st < steps; ++st) {
+    auto step = [&](int st, auto more_constant) {      // more: the stage that takes this one's place is asked for
+        constexpr bool MORE = decltype(more_constant)::value;
         const uint32_t next = cur + STAGE == STAGES * STAGE ? 0u : cur + STAGE;
         // this stage is in everybody's registers, the next one has landed
-        wait_vmcnt<(STAGES - 2) * LOADS>();
+        if (MORE || st + STAGES == steps) wait_vmcnt<(STAGES - 2) * LOADS>();
+        else                              wait_vmcnt<0>();
         __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0)
         barrier();
         // the products first: while they run the wavefront asks for what comes next, and stands while that is accepted
@@ -471,7 +482,7 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
         __builtin_amdgcn_sched_barrier(0);
         s = products<FAST>(now.w[1], now.a[1], s);
         __builtin_amdgcn_sched_barrier(0);
-        request(min(st + STAGES, steps - 1), cur);
+        if constexpr (MORE) request(st + STAGES, cur);
         __builtin_amdgcn_sched_barrier(0);
         // (a block past the end is zeros, but its scale need not be finite)
         const float f = st * KS + ks < blocks ? now.sa * now.sw : 0.f;
@@ -479,7 +490,10 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
         for (int e = 0; e < 16; ++e) acc[e] += s[e] * f;
         now = then;
         cur = next;
-    }
+    };
+    int st = 0;
+    for (; st + STAGES < steps; ++st) step(st, std::true_type{});
+    for (; st < steps; ++st) step(st, std::false_type{});
     wait_vmcnt<0>();
     barrier();
     // sums of the wavefronts' blocks, in their order; [wave][token][output]
@@ -541,9 +555,9 @@ Plan one_launch(int M, int N, int K, bool fast)
     if (M <= 16) return {(N + 15) / 16 <= 256 ? ROWS16 : ROWS32, 1, M, 4.f + (float)N * (float)K / 5.5e6f};     // 6144 x 4096, one token: 7.3 / 7.0 us; 3584 x 3584: 4.5 / 6.0
     struct Shape { Form form; int tokens, outputs, blocks; float launch, step_fast, step_f16, crowded_fast, crowded_f16; };
     static const Shape shapes[] = {
-        {SMALL_1x1, 32, 32, 8, 3.3f, 0.67f, 0.83f, 1.9f, 1.9f}, {SMALL_1x2, 64, 32, 4, 3.8f, 0.50f, 0.70f, 1.65f, 1.65f},
-        {SMALL_2x2, 64, 64, 2, 3.7f, 0.41f, 0.62f, 1.35f, 1.43f}, {SMALL_2x4, 128, 64, 1, 3.9f, 0.34f, 0.63f, 1.5f, 1.4f},
-        {TILE128, 128, 256, 1, 4.2f, 0.59f, 1.30f, 1.8f, 1.5f}, {TILE256, 256, 256, 1, 4.8f, 1.00f, 0.f, 1.85f, 0.f}};
+        {SMALL_1x1, 32, 32, 8, 2.8f, 0.67f, 0.83f, 1.9f, 1.9f}, {SMALL_1x2, 64, 32, 4, 3.5f, 0.50f, 0.72f, 1.65f, 1.65f},
+        {SMALL_2x2, 64, 64, 2, 3.4f, 0.40f, 0.61f, 1.35f, 1.43f}, {SMALL_2x4, 128, 64, 1, 3.9f, 0.35f, 0.61f, 1.5f, 1.4f},
+        {TILE128, 128, 256, 1, 3.4f, 0.59f, 1.30f, 1.8f, 1.5f}, {TILE256, 256, 256, 1, 4.4f, 1.00f, 0.f, 1.85f, 0.f}};
     Plan best = {TILE128, 1, M, 3e38f};
     for (const Shape& f : shapes) {
         if (f.form == TILE256 && !fast) continue;                        // (its registers are taken on f16)
@@ -556,7 +570,7 @@ Plan one_launch(int M, int N, int K, bool fast)
             const float step = (fast ? f.step_fast : f.step_f16) * (1.f + (crowded - 1.f) * fill * fill);
             const float memory = ((float)N + (float)M) * (float)K / 5.5e6f;
             float t = f.launch + std::max(memory, (float)rounds * (float)((steps + s - 1) / s) * step);
-            if (s > 1) t += 2.5f + (float)s * (float)M * (float)N * 8.f / 8e6f;      // (the partial sums, in the caches)
+            if (s > 1) t += 4.0f + (float)s * (float)M * (float)N * 8.f / 8e6f;      // (the partial sums, in the caches)
             if (t < best.us) best = {f.form, s, M, t};
         }
     }
@@ -564,7 +578,7 @@ Plan one_launch(int M, int N, int K, bool fast)
 }
 
 // One launch, or one whose tiles fill whole rounds and another for the tokens that are left: the last round of large tiles
-// is rarely full (4000 x 5376 x 3584: 336 tiles, 86 us; 252 and the rest in smaller ones 83 us).
+// is rarely full (4000 x 5376 x 3584: 336 tiles, 86 us; 252 and the rest in smaller ones 79 us).
 Plan plan_of(int M, int N, int K, bool fast)
 {
     Plan best = one_launch(M, N, K, fast);
