@@ -50,6 +50,20 @@ template <bool FAST> __device__ __forceinline__ f32x16 products(const i32x8& w, 
     }
 }
 
+// the same with the f16 values at hand (32 columns a lane)
+struct Wide { f16x8 h[4]; };
+__device__ __forceinline__ Wide widen32(const i32x8& a)
+{
+    return Wide{{widen8(a[0], a[1]), widen8(a[2], a[3]), widen8(a[4], a[5]), widen8(a[6], a[7])}};
+}
+__device__ __forceinline__ f32x16 products(const Wide& w, const Wide& a, const f32x16& c)
+{
+    f32x16 s = c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(w.h[i], a.h[i], s, 0, 0, 0);
+    return s;
+}
+
 // workgroup barrier over which the compiler moves no access to memory (waits are placed by hand)
 __device__ __forceinline__ void barrier()
 {
@@ -137,11 +151,12 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_rows_kernel(GemmFp8Params p)
 
 __device__ __attribute__((aligned(16))) const uint32_t zeros16[4] = {0u, 0u, 0u, 0u};
 
-// A workgroup of eight wavefronts computes 256 outputs of 128 MT tokens (a wavefront 128 outputs of 32 MT).  The codes of
+// A workgroup of eight wavefronts, WN of them abreast, computes 256 outputs of 32 MT (8 / WN) tokens, a wavefront 32 NI
+// outputs of 32 MT tokens: 256 tokens by 128 x 64 each, 128 tokens by 64 x 64.  The codes of
 // a block travel by direct-to-LDS loads, `STAGES` blocks deep; 16-byte piece c of a row lies at position c ^ (row >> 1 & 7)
 // of its 128 bytes, so that the operand reads (32 rows, one piece each half) are free of bank conflicts.
 //
-// A step is one block: 4 MT units of 32 outputs x 32 tokens, each one chain of instructions whose result is scaled and
+// A step is one block: NI MT units of 32 outputs x 32 tokens, each one chain of instructions whose result is scaled and
 // added while the next chain runs (32 x 32 x 64 and not 16 x 16 x 128 instructions: beside the latter vector
 // instructions hardly issue, 33.5 against 45 cycles per 16 x 16 x 128 with its four additions).  Operands are
 // read a unit ahead.  One barrier per step, before its last outputs: by then everybody has read the block, and the next
@@ -150,13 +165,15 @@ __device__ __attribute__((aligned(16))) const uint32_t zeros16[4] = {0u, 0u, 0u,
 //
 // What bounds it: power.  At 32768 x 6144 x 4096 the matrix cores are busy 55 - 65 % of the cycles at 1.65 - 1.7 GHz of the
 // card's 2.4.
-template <int MT, int STAGES, bool FAST, bool F32, bool SPLIT, bool STREAM>
+template <int NI, int MT, int WN, int STAGES, bool FAST, bool F32, bool SPLIT, bool STREAM>
 __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int tiles_m, int tiles_n, int splits)
 {
-    constexpr int W_B = 256 * QBLOCK, A_B = 128 * MT * QBLOCK, STAGE = W_B + A_B + 2048;   // weights | tokens | scales
-    constexpr int WLOADS = 4, ALOADS = 2 * MT, LOADS = WLOADS + ALOADS + 1;                // per wavefront and block
-    constexpr int UNITS = 4 * MT;
+    constexpr int TOKENS = 32 * MT * (8 / WN), SWAVES = TOKENS / 64;                       // (a wavefront brings 64 scales)
+    constexpr int W_B = 256 * QBLOCK, A_B = TOKENS * QBLOCK, STAGE = W_B + A_B + 2048;     // weights | tokens | scales
+    constexpr int WLOADS = 4, ALOADS = TOKENS / 64, LOADS = WLOADS + ALOADS + 1;                // per wavefront and block
+    constexpr int UNITS = NI * MT;
     constexpr int PITCH = 272;                                                             // epilogue: a token's 256 bytes and 16 more
+    static_assert(32 * NI * WN == 256 && UNITS % 2 == 0 && NI % 2 == 0 && LOADS <= 2 * UNITS && SWAVES < 8);
     static_assert(8 * 32 * PITCH <= STAGES * STAGE && STAGES * STAGE <= 160 * 1024);
     __shared__ __attribute__((aligned(1024))) unsigned char smem[STAGES * STAGE];
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
@@ -173,7 +190,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
     lin /= splits;
     constexpr int BAND = 4;
     const int band = lin / (BAND * tiles_n), rows_in = min(BAND, tiles_m - band * BAND), in = lin - band * BAND * tiles_n;
-    const int m0 = (band * BAND + in % rows_in) * 128 * MT, n0 = in / rows_in * 256;
+    const int m0 = (band * BAND + in % rows_in) * TOKENS, n0 = in / rows_in * 256;
     const int blocks = (p.K + QBLOCK - 1) / QBLOCK, whole = p.K / QBLOCK;
     const int first = (int)((int64_t)whole * split / splits), last = (int)((int64_t)whole * (split + 1) / splits);
 
@@ -187,8 +204,8 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
     for (int i = 0; i < ALOADS; ++i) off_a[i] = (uint32_t)min((i * 8 + wave) * 8 + (lane >> 3), p.M - 1 - m0) * (uint32_t)p.K + piece * 16;
     const uint8_t* a0 = p.a + (int64_t)m0 * p.K;
     const uint8_t* w0 = p.w + (int64_t)n0 * p.K;
-    // scales: wavefronts 0 .. 2 MT - 1 bring the tokens', the others the weights' two (only those of wavefront 2 MT are read)
-    const bool tokens = wave < 2 * MT;
+    // scales: the first SWAVES wavefronts bring the tokens', the others the weights' two (only those of the next are read)
+    const bool tokens = wave < SWAVES;
     const float* scale0 = tokens ? p.a_scales + m0 : p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
     const int64_t scale_step = tokens ? p.scale_pitch : 1;
     const uint32_t off_s = 4u * (tokens ? (uint32_t)min(wave * 64 + lane, p.M - 1 - m0) : (uint32_t)min(lane & 1, (p.N - 1 - n0) / QBLOCK) * (uint32_t)blocks);
@@ -207,8 +224,8 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
     };
 
     // Operands: lane (h, n) takes pieces h, 2 + h, 4 + h, 6 + h of row n
-    const int wn = wave & 1, wm = wave >> 1, key = (n >> 1) & 7;
-    const uint32_t w_row = (wn * 128 + n) * QBLOCK, a_row = W_B + (wm * 32 * MT + n) * QBLOCK;
+    const int wn = wave % WN, wm = wave / WN, key = (n >> 1) & 7;
+    const uint32_t w_row = (wn * 32 * NI + n) * QBLOCK, a_row = W_B + (wm * 32 * MT + n) * QBLOCK;
     uint32_t at[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) at[r] = ((2 * r + h) ^ key) * 16;
@@ -222,9 +239,9 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
         LDS_AS unsigned char* st = lds + stage + W_B + A_B;
 #pragma unroll
         for (int j = 0; j < MT; ++j) raw.a[j] = *(LDS_AS float*)(st + (wm * 32 * MT + j * 32 + n) * 4);
-        raw.w = *(LDS_AS float*)(st + 2 * MT * 256 + wn * 4);
+        raw.w = *(LDS_AS float*)(st + SWAVES * 256 + wn * 32 * NI / QBLOCK * 4);
     };
-    f32x16 acc[4][MT] = {}, s[2] = {};
+    f32x16 acc[NI][MT] = {}, s[2] = {};
     float f[MT] = {};
     i32x8 wv[2][2], av[MT][2];
 
@@ -248,7 +265,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
             const i32x8 a_lo = half(0, a_row + j * 4096, 0), a_hi = half(0, a_row + j * 4096, 1);
             const float fj = raw.a[j] * raw.w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < NI; ++i) {
                 const f32x16 t = products<FAST>(half(0, w_row + i * 4096, 1), a_hi, products<FAST>(half(0, w_row + i * 4096, 0), a_lo, (f32x16){}));
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] += t[e] * fj;
@@ -276,6 +293,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
         }
         scales(0);
         uint32_t prev = (STAGES - 1) * STAGE, cur = 0;
+        Wide wide_a[MT][2], wide_w[2];                 // (on f16: each operand is widened once)
         // A step.  LOAD: of the blocks that take the place of the one before this and of this one the loads are still to be
         // sent (2), only of the former (1), of neither (0)
         auto step = [&](int kb, auto load_constant) {
@@ -294,7 +312,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
                 __builtin_amdgcn_sched_barrier(0);
                 if (j == 0) {
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) wv[(i + 1) & 1][q] = i < 3 ? half(cur, w_row + (i + 1) * 4096, q) : half(next, w_row, q);
+                    for (int q = 0; q < 2; ++q) wv[(i + 1) & 1][q] = i < NI - 1 ? half(cur, w_row + (i + 1) * 4096, q) : half(next, w_row, q);
                 }
                 if (u == 1) {
 #pragma unroll
@@ -304,11 +322,18 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
                 const int pu = (u + UNITS - 1) % UNITS;               // the unit before: its sums are scaled and added now
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    s[u & 1] = products<FAST>(wv[i & 1][q], av[j][q], q ? s[u & 1] : (f32x16){});
+                    const f32x16 c = q ? s[u & 1] : (f32x16){};
+                    if constexpr (FAST) {
+                        s[u & 1] = products<true>(wv[i & 1][q], av[j][q], c);
+                    } else {
+                        if (i == 0) wide_a[j][q] = widen32(av[j][q]);
+                        if (j == 0) wide_w[q] = widen32(wv[i & 1][q]);
+                        s[u & 1] = products(wide_w[q], wide_a[j][q], c);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
-                    if (i == 3) av[j][q] = half(next, a_row + j * 4096, q);
+                    if (i == NI - 1) av[j][q] = half(next, a_row + j * 4096, q);
                     // a load per half chain from the barrier on
-                    if (i == 3) { if (LOAD == 2) load(first + kb + STAGES, cur, j * 2 + q); }
+                    if (i == NI - 1) { if (LOAD == 2) load(first + kb + STAGES, cur, j * 2 + q); }
                     else if (LOAD && 2 * MT + u * 2 + q < LOADS) load(first + kb + STAGES - 1, prev, 2 * MT + u * 2 + q);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -326,7 +351,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
         for (; kb < steps; ++kb) step(kb, std::integral_constant<int, 0>{});
         wait_vmcnt<0>();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[3][MT - 1][e] += s[1][e] * f[MT - 1];
+        for (int e = 0; e < 16; ++e) acc[NI - 1][MT - 1][e] += s[1][e] * f[MT - 1];
     }
 
     // Outputs: lane (h, n) holds outputs 8 r + 4 h .. + 3 of every 32, of token n.  Through LDS they leave in whole
@@ -335,26 +360,27 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
     const bool wide = p.N % (F32 || SPLIT ? 4 : 8) == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
     LDS_AS unsigned char* mine = lds + wave * 32 * PITCH;
     constexpr bool O32 = F32 || SPLIT;
-    constexpr int PARTS = O32 ? 2 : 1, COLS = 128 / PARTS, PER = O32 ? 4 : 8;    // outputs per pass, per 16 bytes
+    constexpr int COLS = O32 ? 64 : 32 * NI, PARTS = 32 * NI / COLS;             // outputs per pass
+    constexpr int PER = O32 ? 4 : 8, LANES = COLS / PER;                         // per 16 bytes; lanes per token
     void* out = SPLIT ? static_cast<void*>(p.part + (int64_t)split * p.M * p.N) : p.out;
 #pragma unroll
     for (int j = 0; j < MT; ++j)
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) {
 #pragma unroll
-            for (int ii = 0; ii < 4 / PARTS; ++ii)
+            for (int ii = 0; ii < COLS / 32; ++ii)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const f32x16& v = acc[part * (4 / PARTS) + ii][j];
+                    const f32x16& v = acc[part * (COLS / 32) + ii][j];
                     LDS_AS unsigned char* dst = mine + n * PITCH + (ii * 32 + 8 * r + 4 * h) * (O32 ? 4 : 2);
                     if constexpr (O32) *(LDS_AS f32x4*)dst = (f32x4){v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]};
                     else               *(LDS_AS u32x2*)dst = (u32x2){bf16_pair(v[4 * r], v[4 * r + 1]), bf16_pair(v[4 * r + 2], v[4 * r + 3])};
                 }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const int t = q * 4 + (lane >> 4), m = m0 + wm * 32 * MT + j * 32 + t, c = n0 + wn * 128 + part * COLS + (lane & 15) * PER;
-                const u32x4 v = *(LDS_AS u32x4*)(mine + t * PITCH + (lane & 15) * 16);
+            for (int q = 0; q < LANES / 2; ++q) {
+                const int t = q * (64 / LANES) + lane / LANES, m = m0 + wm * 32 * MT + j * 32 + t, c = n0 + wn * 32 * NI + part * COLS + lane % LANES * PER;
+                const u32x4 v = *(LDS_AS u32x4*)(mine + t * PITCH + lane % LANES * 16);
                 if (m >= p.M || c >= p.N) continue;
                 const int64_t o = (int64_t)m * p.N + c;
                 if (wide) {
@@ -556,8 +582,8 @@ Plan one_launch(int M, int N, int K, bool fast)
     struct Shape { Form form; int tokens, outputs, blocks; float launch, step_fast, step_f16, crowded_fast, crowded_f16; };
     static const Shape shapes[] = {
         {SMALL_1x1, 32, 32, 8, 2.8f, 0.67f, 0.83f, 1.9f, 1.9f}, {SMALL_1x2, 64, 32, 4, 3.5f, 0.50f, 0.72f, 1.65f, 1.65f},
-        {SMALL_2x2, 64, 64, 2, 3.4f, 0.40f, 0.61f, 1.35f, 1.43f}, {SMALL_2x4, 128, 64, 1, 3.9f, 0.35f, 0.61f, 1.5f, 1.4f},
-        {TILE128, 128, 256, 1, 3.4f, 0.59f, 1.30f, 1.8f, 1.5f}, {TILE256, 256, 256, 1, 4.4f, 1.00f, 0.f, 1.85f, 0.f}};
+        {SMALL_2x2, 64, 64, 2, 3.4f, 0.40f, 0.61f, 1.5f, 1.5f}, {SMALL_2x4, 128, 64, 1, 3.9f, 0.35f, 0.61f, 1.35f, 1.35f},
+        {TILE128, 128, 256, 1, 3.4f, 0.58f, 1.25f, 1.75f, 1.45f}, {TILE256, 256, 256, 1, 4.4f, 1.00f, 0.f, 1.85f, 0.f}};
     Plan best = {TILE128, 1, M, 3e38f};
     for (const Shape& f : shapes) {
         if (f.form == TILE256 && !fast) continue;                        // (its registers are taken on f16)
@@ -620,17 +646,21 @@ template <int WN, int WM, int KS, int STAGES> void launch_small_tiles(const Gemm
     }
 }
 
-template <int MT, int STAGES, bool FAST> void launch_tiles(const GemmFp8Params& p, bool f32, int splits, hipStream_t s)
+template <int NI, int MT, int WN, int STAGES, bool FAST> void launch_tiles(const GemmFp8Params& p, bool f32, int splits, hipStream_t s)
 {
-    const int tm = (p.M + 128 * MT - 1) / (128 * MT), tn = (p.N + 255) / 256;
+    constexpr int TOKENS = 32 * MT * (8 / WN);
+    const int tm = (p.M + TOKENS - 1) / TOKENS, tn = (p.N + 255) / 256;
     const dim3 grid((unsigned)(((long)tm * tn * splits + 7) / 8 * 8)), block(512);
     const bool stream = (int64_t)p.M * p.N * (f32 ? 4 : 2) > STREAM_BYTES;
-    auto run = [&](auto is_f32, auto is_stream) {
-        gemm_tile_kernel<MT, STAGES, FAST, decltype(is_f32)::value, false, decltype(is_stream)::value><<<grid, block, 0, s>>>(p, tm, tn, 1);
+    auto run = [&](auto is_f32, auto is_split, auto is_stream) {
+        gemm_tile_kernel<NI, MT, WN, STAGES, FAST, decltype(is_f32)::value, decltype(is_split)::value, decltype(is_stream)::value>
+            <<<grid, block, 0, s>>>(p, tm, tn, splits);
     };
-    if (MT == 1 && splits > 1) gemm_tile_kernel<1, STAGES, FAST, false, true, false><<<grid, block, 0, s>>>(p, tm, tn, splits);
-    else if (f32)              stream ? run(std::true_type{}, std::true_type{}) : run(std::true_type{}, std::false_type{});
-    else                       stream ? run(std::false_type{}, std::true_type{}) : run(std::false_type{}, std::false_type{});
+    using std::true_type;
+    using std::false_type;
+    if (TOKENS == 128 && splits > 1) { if constexpr (TOKENS == 128) run(false_type{}, true_type{}, false_type{}); }
+    else if (f32)                    stream ? run(true_type{}, false_type{}, true_type{}) : run(true_type{}, false_type{}, false_type{});
+    else                             stream ? run(false_type{}, false_type{}, true_type{}) : run(false_type{}, false_type{}, false_type{});
     if (splits > 1) {
         const dim3 mg((unsigned)std::min<int64_t>(((int64_t)p.M * p.N + 255) / 256, 4096));
         if (f32) gemm_merge_kernel<true><<<mg, dim3(256), 0, s>>>(p, splits);
@@ -682,10 +712,10 @@ hipError_t launch_gemm_fp8(const GemmFp8Params& all, mla_dtype out, bool fast_su
             case SMALL_2x2: launch_small_tiles<2, 2, 2, 4>(p, f32, fast_sums, s); break;
             case SMALL_2x4: launch_small_tiles<2, 4, 1, 6>(p, f32, fast_sums, s); break;
             case TILE128:
-                if (fast_sums) launch_tiles<1, 3, true>(p, f32, plan.splits, s);
-                else           launch_tiles<1, 3, false>(p, f32, plan.splits, s);
+                if (fast_sums) launch_tiles<2, 2, 4, 3, true>(p, f32, plan.splits, s);
+                else           launch_tiles<2, 2, 4, 3, false>(p, f32, plan.splits, s);
                 break;
-            case TILE256: launch_tiles<2, 2, true>(p, f32, 1, s); break;
+            case TILE256: launch_tiles<4, 2, 2, 2, true>(p, f32, 1, s); break;
         }
     });
     return hipGetLastError();
