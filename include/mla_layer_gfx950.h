@@ -115,10 +115,11 @@ size_t mla_gemm_fp8_workspace_bytes(int M, int N, int K);
  *   out  [M, N] out dtype (MLA_F32 or MLA_BF16)
  *   workspace  mla_gemm_fp8_workspace_bytes(M, N, K) bytes, 16-byte aligned (may
  *              be NULL where that is 0); scratch
- * K a multiple of 16 up to 2^23, a and w on 16 bytes (otherwise MLA_ERR_UNSUPPORTED), any M
- * and N.  Products are exact and summed in fp32 (but see MLA_GEMM_FAST_SUMS), the
- * blocks with their scales in fp32 beside them; the order of the sums depends on
- * the sizes alone, so that a call's bits do not change from run to run.
+ * K a multiple of 16 up to 2^23, a and w on 16 bytes, M and N up to 2^30 and no
+ * more tiles than a grid holds (otherwise MLA_ERR_UNSUPPORTED).  Products are
+ * exact and summed in fp32 (but see MLA_GEMM_FAST_SUMS), the blocks with their
+ * scales in fp32 beside them; the order of the sums depends on the sizes alone,
+ * so that a call's bits do not change from run to run.
  */
 int mla_gemm_fp8(const uint8_t* a, const float* a_scales, const uint8_t* w, const float* w_scales, void* out,
                  void* workspace, size_t workspace_bytes, int M, int N, int K, mla_dtype out_dtype, unsigned flags,
@@ -153,7 +154,8 @@ int mla_rope_frequencies(double* freq, float* gain, int d_rope, double base, int
  *   q_nope     [T, H, d_nope] (output; NULL iff d_nope is 0)
  *   q_rope     [T, H, d_rope] (output)
  * Pair i of the rotated part turns by positions[t] freq[i] (formed in fp64; the
- * turn itself is fp32).  d_rope even, 2 to 256; d_nope >= 0.
+ * turn itself is fp32).  d_rope even, 2 to 256; d_nope >= 0, H (d_nope + d_rope)
+ * up to 2^30.
  */
 int mla_rope_queries(const void* q, const int32_t* positions, const double* freq, void* q_nope, void* q_rope,
                      int T, int H, int d_nope, int d_rope, int64_t q_pitch, float gain, int layout,

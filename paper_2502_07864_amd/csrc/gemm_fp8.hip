@@ -185,7 +185,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
     // an XCD runs at once shares its operands in its L2
     const int total = tiles_m * tiles_n * splits, per = (total + 7) / 8;
     int lin = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if (lin >= total || (int)(blockIdx.x >> 3) >= per) return;
+    if (lin >= total) return;
     const int split = lin % splits;
     lin /= splits;
     constexpr int BAND = 4;
@@ -426,16 +426,16 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
 
     // Group G = 8 i + wave of a stage: block G / GROUPS of it, rows of w, then rows of a.  Rows past the end repeat the last
     const uint8_t* src[LOADS - 1];
-    uint32_t off[LOADS - 1];
+    uint32_t off[LOADS - 1], column[LOADS - 1];
     int block_of[LOADS - 1];
 #pragma unroll
     for (int i = 0; i < LOADS - 1; ++i) {
         const int G = i * 8 + wave, ks = G / GROUPS, r = (G % GROUPS) * 8;
         const bool W = r < W_ROWS;
         const int row = (W ? r : r - W_ROWS) + (lane >> 3);
-        const int piece = (lane & 7) ^ ((row >> 1) & 7);
+        column[i] = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
         src[i] = W ? p.w + (int64_t)n0 * p.K : p.a + (int64_t)m0 * p.K;
-        off[i] = (uint32_t)min(row, W ? p.N - 1 - n0 : p.M - 1 - m0) * (uint32_t)p.K + piece * 16;
+        off[i] = (uint32_t)min(row, W ? p.N - 1 - n0 : p.M - 1 - m0) * (uint32_t)p.K + column[i];
         block_of[i] = ks;
     }
     const int si = wave * 64 + lane;                   // wavefronts below 4 bring the tokens' scales, the others the weights'
@@ -456,9 +456,8 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
 #pragma unroll
             for (int i = 0; i < LOADS - 1; ++i) {
                 const uint32_t dst = lds0 + stage + (i * 8 + wave) * 1024;
-                const int piece = (lane & 7) ^ (((lane >> 3) + ((i * 8 + wave) % GROUPS) * 8 - (((i * 8 + wave) % GROUPS) * 8 < W_ROWS ? 0 : W_ROWS)) >> 1 & 7);
                 const int64_t k = (int64_t)(b0 + block_of[i]) * QBLOCK;
-                const uint8_t* from = k + piece * 16 < p.K ? src[i] + k + off[i] : reinterpret_cast<const uint8_t*>(zeros16);
+                const uint8_t* from = k + column[i] < p.K ? src[i] + k + off[i] : reinterpret_cast<const uint8_t*>(zeros16);
                 asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(dst), "v"(from) : "memory");
             }
         }
@@ -678,8 +677,11 @@ template <typename F> static void each_launch(int M, int N, int K, bool fast, F 
     if (first.tokens < M) f(one_launch(M - first.tokens, N, K, fast), first.tokens);
 }
 
+constexpr int MOST = 1 << 30;        // tokens, outputs: sums with a tile's size stay in 32 bits
+
 size_t gemm_fp8_workspace(int M, int N, int K)
 {
+    if (M > MOST || N > MOST) return 0;
     size_t most = 0;
     for (bool fast : {false, true})
         each_launch(M, N, K, fast, [&](const Plan& plan, int) {
@@ -690,6 +692,7 @@ size_t gemm_fp8_workspace(int M, int N, int K)
 
 bool gemm_fp8_supported(int M, int N, int K)
 {
+    if (M > MOST || N > MOST) return false;
     long most = 0;
     for (bool fast : {false, true}) each_launch(M, N, K, fast, [&](const Plan& plan, int) { most = std::max(most, workgroups(plan, N)); });
     return most < 1l << 22;              // (1024 threads each at most)

@@ -26,7 +26,7 @@ __device__ __forceinline__ float2 rotate(float re, float im, float cs, float sn)
 // Memory bound: 32768 tokens x 32 heads x (128 + 64) bf16, 805 MB moved.
 constexpr int ROPE_TOKENS = 16, ROPE_UNITS = 4;
 
-// j / d for small numbers (j < 2^16: the quotient's error stays below the half that is added)
+// j / d for j < 2^21: the quotient's error, j / d 2^-22, stays below the half of 1 / d that separates it from the next whole number
 __device__ __forceinline__ int divide(int j, float inv_d) { return (int)(((float)j + 0.5f) * inv_d); }
 
 template <bool F32, bool HALF, int V, bool STREAM>

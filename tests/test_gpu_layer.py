@@ -162,6 +162,11 @@ def test_quantize_weights(N, K, io):
 
 # ------------------------------------------------------------------ product
 
+# GEMM_FAST_SUMS: within eight neighbouring products the adders drop what lies 2^-13 below the largest, so each of the seven
+# others is off by less than 2^-13 of it; random operands are 1.4e-5 off in the 2-norm
+FAST_DROP, FAST_NORM = 7 * 2.0 ** -13, 3e-5
+
+
 def operands(M, N, K, seed=0):
     g = torch.Generator(device=DEV).manual_seed(seed + M + N + K)
     a = torch.randn((M, K), generator=g, device=DEV).mul_(40).clamp_(-448, 448).to(FP8)
@@ -196,6 +201,29 @@ def test_gemm(M, N, K, dtype):
     check_gemm(M, N, K, dtype)
 
 
+@pytest.mark.parametrize("fast", [False, True])
+@pytest.mark.parametrize("M, N, K", [(33, 6144, 4112), (61, 6145, 4112), (90, 3585, 2064), (260, 6145, 4112), (450, 3585, 3600), (1000, 1537, 4112),
+                                     (2500, 577, 4112), (4000, 577, 4112), (4701, 5381, 2064), (5000, 5376, 3600), (5000, 6100, 400), (4000, 5376, 3600),
+                                     (10001, 4097, 336), (20000, 1281, 1040)])
+def test_gemm_forms(M, N, K, fast):
+    """Sizes at which the forms of the product change hands, a short block at the end of each: tiles of every size, shares
+    of K, a second launch for the last tokens.  Whatever lies around the output and the scratch stays."""
+    a, sa, w, sw = operands(M, N, K)
+    dtype = BF if (M + N) % 2 else F32
+    need = layer.gemm_fp8_workspace_bytes(M, N, K)
+    room = torch.full((M * N + 512,), 7.0, dtype=dtype, device=DEV)
+    scratch = torch.full((need + 512,), 0xAB, dtype=torch.uint8, device=DEV)
+    got = layer.gemm_fp8(a, sa, w, sw, out=room[256:256 + M * N].view(M, N), workspace=scratch[256:256 + need] if need else None,
+                         flags=layer.GEMM_FAST_SUMS if fast else 0)
+    A, W = dequantised(a, sa, w, sw)
+    want, size = torch.mm(A, W.t().contiguous()), torch.mm(A.abs(), W.abs().t().contiguous())
+    near(got, want, ROUND[dtype], ((FAST_DROP if fast else 0.0) + (140 + blocks(K)) * 2.0 ** -24) * size)
+    if fast:
+        assert (got.double() - want).norm() <= (FAST_NORM + (2.0 ** -9 if dtype == BF else 0.0)) * want.norm()
+    assert (room[:256] == 7).all() and (room[256 + M * N:] == 7).all()
+    assert (scratch[:256] == 0xAB).all() and (scratch[256 + need:] == 0xAB).all()
+
+
 @pytest.mark.parametrize("K", [16, 32, 112, 128, 144, 240, 256, 272, 384, 400, 496, 512, 528, 1024, 1040, 2032, 2048, 4080])
 @pytest.mark.parametrize("M, N", [(5, 70), (40, 200), (300, 300)])
 def test_gemm_depths(M, N, K):
@@ -219,11 +247,6 @@ def test_gemm_exact(M, N, K):
     got = layer.gemm_fp8(a.to(FP8), sa, w.to(FP8), sw, dtype=F32)
     A, W = dequantised(a, sa, w, sw)
     assert torch.equal(got.double(), torch.mm(A, W.t().contiguous()))
-
-
-# GEMM_FAST_SUMS: within eight neighbouring products the adders drop what lies 2^-13 below the largest, so each of the seven
-# others is off by less than 2^-13 of it; random operands are 1.4e-5 off in the 2-norm
-FAST_DROP, FAST_NORM = 7 * 2.0 ** -13, 3e-5
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])

@@ -49,13 +49,14 @@ def gemm(L, a=P, sa=P, w=P, sw=P, out=P, ws=P, ws_bytes=1 << 40, M=4, N=64, K=25
 @pytest.mark.parametrize("kw, want", [
     (dict(a=None), E_NULL), (dict(sa=None), E_NULL), (dict(w=None), E_NULL), (dict(sw=None), E_NULL), (dict(out=None), E_NULL),
     (dict(M=0), E_SHAPE), (dict(N=-1), E_SHAPE), (dict(K=0), E_SHAPE),
-    (dict(K=24), E_UNSUP), (dict(dt=FP8), E_UNSUP), (dict(a=P + 8), E_UNSUP), (dict(w=P + 1), E_UNSUP), (dict(flags=2), E_UNSUP), (dict(K=(1 << 23) + 16), E_UNSUP)])
+    (dict(K=24), E_UNSUP), (dict(dt=FP8), E_UNSUP), (dict(a=P + 8), E_UNSUP), (dict(w=P + 1), E_UNSUP), (dict(flags=2), E_UNSUP), (dict(K=(1 << 23) + 16), E_UNSUP),
+    (dict(M=(1 << 30) + 1), E_UNSUP), (dict(N=0x7FFFFFFF), E_UNSUP), (dict(M=1 << 30, N=1 << 30, K=16), E_UNSUP)])
 def test_gemm_refusals(L, kw, want):
     assert gemm(L, **kw) == want
 
 
 def test_gemm_workspace(L):
-    assert L.mla_gemm_fp8_workspace_bytes(0, 64, 64) == 0 and L.mla_gemm_fp8_workspace_bytes(4, 64, -1) == 0
+    assert L.mla_gemm_fp8_workspace_bytes(0x7FFFFFFF, 64, 64) == 0 and L.mla_gemm_fp8_workspace_bytes(0, 64, 64) == 0 and L.mla_gemm_fp8_workspace_bytes(4, 64, -1) == 0
     for M in (1, 16, 61, 500, 4000):
         for N in (320, 576, 3584):
             for K in (256, 4096):
@@ -74,7 +75,8 @@ def rope(L, q=P, pos=P, freq=P, qn=P, qr=P, T=4, H=2, dn=128, dr=64, pitch=384, 
     (dict(q=None), E_NULL), (dict(pos=None), E_NULL), (dict(freq=None), E_NULL), (dict(qn=None), E_NULL), (dict(qr=None), E_NULL),
     (dict(T=0), E_SHAPE), (dict(H=0), E_SHAPE), (dict(dn=-1), E_SHAPE), (dict(dr=0), E_SHAPE), (dict(dr=63), E_SHAPE),
     (dict(pitch=383), E_SHAPE), (dict(gain=math.nan), E_SHAPE),
-    (dict(layout=2), E_UNSUP), (dict(io=FP8), E_UNSUP), (dict(dr=258, pitch=4096), E_UNSUP), (dict(T=1 << 24), E_UNSUP)])
+    (dict(layout=2), E_UNSUP), (dict(io=FP8), E_UNSUP), (dict(dr=258, pitch=4096), E_UNSUP), (dict(T=1 << 24), E_UNSUP),
+    (dict(H=1 << 23, pitch=1 << 40), E_UNSUP)])
 def test_rope_refusals(L, kw, want):
     assert rope(L, **kw) == want
 
