@@ -82,7 +82,8 @@ template <bool F32> __device__ __forceinline__ void put(void* out, int64_t at, f
 
 // A workgroup takes 16 NT outputs of up to 16 tokens over the whole depth, its wavefronts share out the blocks: what
 // bounds it is reading the weights once, and with every block of a wavefront on its way at once that is one round trip.
-// The partial sums meet in LDS and are added in the wavefronts' order.
+// The partial sums meet in LDS and are added in the wavefronts' order.  One token by 6144 x 4096: 7.0 us, 3.6 TB/s (25 MB; a
+// launch of nothing takes 1.6).
 template <int NT, int WAVES, int U, bool F32>
 __global__ __launch_bounds__(WAVES * 64) void gemm_rows_kernel(GemmFp8Params p)
 {
@@ -151,9 +152,9 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_rows_kernel(GemmFp8Params p)
 
 __device__ __attribute__((aligned(16))) const uint32_t zeros16[4] = {0u, 0u, 0u, 0u};
 
-// A workgroup of eight wavefronts, WN of them abreast, computes 256 outputs of 32 MT (8 / WN) tokens, a wavefront 32 NI
-// outputs of 32 MT tokens: 256 tokens by 128 x 64 each, 128 tokens by 64 x 64.  The codes of
-// a block travel by direct-to-LDS loads, `STAGES` blocks deep; 16-byte piece c of a row lies at position c ^ (row >> 1 & 7)
+// A workgroup of eight wavefronts, WN of them abreast, computes 32 NI WN outputs of 32 MT (8 / WN) tokens, a wavefront 32 NI
+// outputs of 32 MT tokens: 256 tokens by 256 outputs, 64 x 128 each, or by 128, 64 x 64 each (128 tokens by 256 outputs take
+// as long at 6144 outputs, and at few 5 - 40 % longer: 25000 x 576 x 4096 80 us, these 61).  The codes of a block travel by direct-to-LDS loads, `STAGES` blocks deep; 16-byte piece c of a row lies at position c ^ (row >> 1 & 7)
 // of its 128 bytes, so that the operand reads (32 rows, one piece each half) are free of bank conflicts.
 //
 // A step is one block: NI MT units of 32 outputs x 32 tokens, each one chain of instructions whose result is scaled and
@@ -163,17 +164,17 @@ __device__ __attribute__((aligned(16))) const uint32_t zeros16[4] = {0u, 0u, 0u,
 // one has arrived; the loads of the block after take its place and are spread over the units, because a wavefront stands
 // still while a load is accepted.
 //
-// What bounds it: power.  At 32768 x 6144 x 4096 the matrix cores are busy 55 - 65 % of the cycles at 1.65 - 1.7 GHz of the
-// card's 2.4.
+// What bounds it: power.  At 32768 x 6144 x 4096 on codes (690 us, 2390 Tflop/s) the matrix cores are busy 70 % of the
+// cycles at 1.51 GHz of the card's 2.4.  On f16, whose instructions do half the work a cycle, 1365 us.
 template <int NI, int MT, int WN, int STAGES, bool FAST, bool F32, bool SPLIT, bool STREAM>
 __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int tiles_m, int tiles_n, int splits)
 {
     constexpr int TOKENS = 32 * MT * (8 / WN), SWAVES = TOKENS / 64;                       // (a wavefront brings 64 scales)
-    constexpr int W_B = 256 * QBLOCK, A_B = TOKENS * QBLOCK, STAGE = W_B + A_B + 2048;     // weights | tokens | scales
-    constexpr int WLOADS = 4, ALOADS = TOKENS / 64, LOADS = WLOADS + ALOADS + 1;                // per wavefront and block
+    constexpr int OUTPUTS = 32 * NI * WN, W_B = OUTPUTS * QBLOCK, A_B = TOKENS * QBLOCK, STAGE = W_B + A_B + 2048;     // weights | tokens | scales
+    constexpr int WLOADS = OUTPUTS / 64, ALOADS = TOKENS / 64, LOADS = WLOADS + ALOADS + 1;                // per wavefront and block
     constexpr int UNITS = NI * MT;
     constexpr int PITCH = 272;                                                             // epilogue: a token's 256 bytes and 16 more
-    static_assert(32 * NI * WN == 256 && UNITS % 2 == 0 && NI % 2 == 0 && LOADS <= 2 * UNITS && SWAVES < 8);
+    static_assert(OUTPUTS % QBLOCK == 0 && UNITS % 2 == 0 && NI % 2 == 0 && LOADS <= 2 * UNITS && SWAVES < 8);
     static_assert(8 * 32 * PITCH <= STAGES * STAGE && STAGES * STAGE <= 160 * 1024);
     __shared__ __attribute__((aligned(1024))) unsigned char smem[STAGES * STAGE];
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
     lin /= splits;
     constexpr int BAND = 4;
     const int band = lin / (BAND * tiles_n), rows_in = min(BAND, tiles_m - band * BAND), in = lin - band * BAND * tiles_n;
-    const int m0 = (band * BAND + in % rows_in) * TOKENS, n0 = in / rows_in * 256;
+    const int m0 = (band * BAND + in % rows_in) * TOKENS, n0 = in / rows_in * OUTPUTS;
     const int blocks = (p.K + QBLOCK - 1) / QBLOCK, whole = p.K / QBLOCK;
     const int first = (int)((int64_t)whole * split / splits), last = (int)((int64_t)whole * (split + 1) / splits);
 
@@ -204,11 +205,11 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
     for (int i = 0; i < ALOADS; ++i) off_a[i] = (uint32_t)min((i * 8 + wave) * 8 + (lane >> 3), p.M - 1 - m0) * (uint32_t)p.K + piece * 16;
     const uint8_t* a0 = p.a + (int64_t)m0 * p.K;
     const uint8_t* w0 = p.w + (int64_t)n0 * p.K;
-    // scales: the first SWAVES wavefronts bring the tokens', the others the weights' two (only those of the next are read)
+    // scales: the first SWAVES wavefronts bring the tokens', the others the weights' (only those of the next are read)
     const bool tokens = wave < SWAVES;
     const float* scale0 = tokens ? p.a_scales + m0 : p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
     const int64_t scale_step = tokens ? p.scale_pitch : 1;
-    const uint32_t off_s = 4u * (tokens ? (uint32_t)min(wave * 64 + lane, p.M - 1 - m0) : (uint32_t)min(lane & 1, (p.N - 1 - n0) / QBLOCK) * (uint32_t)blocks);
+    const uint32_t off_s = 4u * (tokens ? (uint32_t)min(wave * 64 + lane, p.M - 1 - m0) : (uint32_t)min(lane % (OUTPUTS / QBLOCK), (p.N - 1 - n0) / QBLOCK) * (uint32_t)blocks);
     auto load = [&](int kb, uint32_t stage, int k) {
         if (k < WLOADS + ALOADS) {
             const bool W = k < WLOADS;
@@ -403,7 +404,8 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
 // A workgroup of eight wavefronts computes 32 WN outputs of 32 WM tokens; a wavefront 32 x 32 of them over every KS-th
 // block, so that small tiles still keep eight wavefronts.  Up to a few hundred tokens, and for few outputs, small tiles over
 // the whole depth beat large ones over shares of it, whose partial sums go through memory.  Blocks travel as in the tile
-// kernel, KS at a time.  What bounds it: 64 bytes a cycle into a CU.
+// kernel, KS at a time.  What bounds it: 64 bytes a cycle into a CU, the launch and one round trip to memory where a
+// wavefront has few blocks (61 x 3584 x 3584: 6.9 us; 1024 x 576 x 4096 on codes: 10.6).
 template <int WN, int WM, int KS, int STAGES, bool FAST, bool F32>
 __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p, int tiles_m)
 {
@@ -572,8 +574,9 @@ struct Plan {
 
 // The form that a model of the times finds fastest: a launch, and per round of 256 workgroups (each fills its CU) the steps
 // over K, or the time that the operands take from memory.  us per step measured with few workgroups, on codes (fast) and on
-// f16; the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  On 186
-// sizes of 1 to 32768 tokens and six (N, K) the choice takes up to 17 % longer than the best form, at most 7 % on most.
+// f16; the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  On 140
+// sizes of 400 to 32768 tokens and seven (N, K), with each kind of sums, the choice takes 0.5 % longer than the best form on
+// average, 19 % at the most.
 Plan one_launch(int M, int N, int K, bool fast)
 {
     const int blocks = (K + QBLOCK - 1) / QBLOCK;
@@ -582,7 +585,7 @@ Plan one_launch(int M, int N, int K, bool fast)
     static const Shape shapes[] = {
         {SMALL_1x1, 32, 32, 8, 2.8f, 0.67f, 0.83f, 1.9f, 1.9f}, {SMALL_1x2, 64, 32, 4, 3.5f, 0.50f, 0.72f, 1.65f, 1.65f},
         {SMALL_2x2, 64, 64, 2, 3.4f, 0.40f, 0.61f, 1.5f, 1.5f}, {SMALL_2x4, 128, 64, 1, 3.9f, 0.35f, 0.61f, 1.35f, 1.35f},
-        {TILE128, 128, 256, 1, 3.4f, 0.58f, 1.25f, 1.75f, 1.45f}, {TILE256, 256, 256, 1, 4.4f, 1.00f, 0.f, 1.85f, 0.f}};
+        {TILE128, 256, 128, 1, 3.4f, 0.58f, 1.25f, 1.75f, 1.45f}, {TILE256, 256, 256, 1, 4.4f, 1.00f, 0.f, 1.85f, 0.f}};
     Plan best = {TILE128, 1, M, 3e38f};
     for (const Shape& f : shapes) {
         if (f.form == TILE256 && !fast) continue;                        // (its registers are taken on f16)
@@ -595,7 +598,7 @@ Plan one_launch(int M, int N, int K, bool fast)
             const float step = (fast ? f.step_fast : f.step_f16) * (1.f + (crowded - 1.f) * fill * fill);
             const float memory = ((float)N + (float)M) * (float)K / 5.5e6f;
             float t = f.launch + std::max(memory, (float)rounds * (float)((steps + s - 1) / s) * step);
-            if (s > 1) t += 4.0f + (float)s * (float)M * (float)N * 8.f / 8e6f;      // (the partial sums, in the caches)
+            if (s > 1) t += 4.0f + (float)s * (float)M * (float)N * 8.f / 6e6f;      // (the partial sums, in the caches)
             if (t < best.us) best = {f.form, s, M, t};
         }
     }
@@ -607,9 +610,9 @@ Plan one_launch(int M, int N, int K, bool fast)
 Plan plan_of(int M, int N, int K, bool fast)
 {
     Plan best = one_launch(M, N, K, fast);
-    const int rows = best.form == TILE256 ? 256 : best.form == TILE128 && best.splits == 1 ? 128 : 0;
-    if (!rows) return best;
-    const long across = (N + 255) / 256, down = (M + rows - 1) / rows, rounds = (down * across) / 256;
+    if (best.form < TILE128 || best.splits > 1) return best;
+    const int rows = 256, wide = best.form == TILE256 ? 256 : 128;
+    const long across = (N + wide - 1) / wide, down = (M + rows - 1) / rows, rounds = (down * across) / 256;
     const long whole = rounds * 256 / across;                            // rows of tiles in so many rounds
     if (whole < 1 || whole >= down) return best;
     const int tokens = (int)whole * rows;
@@ -620,7 +623,7 @@ Plan plan_of(int M, int N, int K, bool fast)
 
 long workgroups(const Plan& plan, int N)
 {
-    static const int tile[][2] = {{16, 16}, {16, 32}, {32, 32}, {64, 32}, {64, 64}, {128, 64}, {128, 256}, {256, 256}};
+    static const int tile[][2] = {{16, 16}, {16, 32}, {32, 32}, {64, 32}, {64, 64}, {128, 64}, {256, 128}, {256, 256}};
     const int* t = tile[plan.form];
     return (long)((plan.tokens + t[0] - 1) / t[0]) * ((N + t[1] - 1) / t[1]) * plan.splits;
 }
@@ -647,8 +650,8 @@ template <int WN, int WM, int KS, int STAGES> void launch_small_tiles(const Gemm
 
 template <int NI, int MT, int WN, int STAGES, bool FAST> void launch_tiles(const GemmFp8Params& p, bool f32, int splits, hipStream_t s)
 {
-    constexpr int TOKENS = 32 * MT * (8 / WN);
-    const int tm = (p.M + TOKENS - 1) / TOKENS, tn = (p.N + 255) / 256;
+    constexpr int TOKENS = 32 * MT * (8 / WN), OUTPUTS = 32 * NI * WN;
+    const int tm = (p.M + TOKENS - 1) / TOKENS, tn = (p.N + OUTPUTS - 1) / OUTPUTS;
     const dim3 grid((unsigned)(((long)tm * tn * splits + 7) / 8 * 8)), block(512);
     const bool stream = (int64_t)p.M * p.N * (f32 ? 4 : 2) > STREAM_BYTES;
     auto run = [&](auto is_f32, auto is_split, auto is_stream) {
@@ -657,7 +660,7 @@ template <int NI, int MT, int WN, int STAGES, bool FAST> void launch_tiles(const
     };
     using std::true_type;
     using std::false_type;
-    if (TOKENS == 128 && splits > 1) { if constexpr (TOKENS == 128) run(false_type{}, true_type{}, false_type{}); }
+    if (splits > 1) { if constexpr (OUTPUTS == 128) run(false_type{}, true_type{}, false_type{}); }
     else if (f32)                    stream ? run(true_type{}, false_type{}, true_type{}) : run(true_type{}, false_type{}, false_type{});
     else                             stream ? run(false_type{}, false_type{}, true_type{}) : run(false_type{}, false_type{}, false_type{});
     if (splits > 1) {
@@ -715,8 +718,8 @@ hipError_t launch_gemm_fp8(const GemmFp8Params& all, mla_dtype out, bool fast_su
             case SMALL_2x2: launch_small_tiles<2, 2, 2, 4>(p, f32, fast_sums, s); break;
             case SMALL_2x4: launch_small_tiles<2, 4, 1, 6>(p, f32, fast_sums, s); break;
             case TILE128:
-                if (fast_sums) launch_tiles<2, 2, 4, 3, true>(p, f32, plan.splits, s);
-                else           launch_tiles<2, 2, 4, 3, false>(p, f32, plan.splits, s);
+                if (fast_sums) launch_tiles<2, 2, 2, 3, true>(p, f32, plan.splits, s);
+                else           launch_tiles<2, 2, 2, 3, false>(p, f32, plan.splits, s);
                 break;
             case TILE256: launch_tiles<4, 2, 2, 2, true>(p, f32, 1, s); break;
         }

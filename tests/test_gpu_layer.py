@@ -224,6 +224,13 @@ def test_gemm_forms(M, N, K, fast):
     assert (scratch[:256] == 0xAB).all() and (scratch[256 + need:] == 0xAB).all()
 
 
+@pytest.mark.parametrize("fast", [False, True])
+@pytest.mark.parametrize("M, N, K", [(24577, 577, 400), (12000, 577, 1040), (20003, 321, 2064), (9001, 321, 7184), (5000, 321, 7184)])
+def test_gemm_few_outputs_of_many_tokens(M, N, K, fast):
+    """Large tiles of 128 outputs, in one launch and in two, and shares of K."""
+    test_gemm_forms(M, N, K, fast)
+
+
 @pytest.mark.parametrize("K", [16, 32, 112, 128, 144, 240, 256, 272, 384, 400, 496, 512, 528, 1024, 1040, 2032, 2048, 4080])
 @pytest.mark.parametrize("M, N", [(5, 70), (40, 200), (300, 300)])
 def test_gemm_depths(M, N, K):
