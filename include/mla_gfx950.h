@@ -11,11 +11,12 @@
  *   o_i     = W^{UV}_i o_hat_i                                  mla_out_proj
  *
  * Notation: H query heads (paper: h), d_head (d), latent rank d_c (r_kv),
- * decoupled-RoPE width d_rope (d^R).  The final W^O projection and the
- * projections that produce q^C and q^R are outside this library.
- * q_rope and the k_rope part of the cache are passed ALREADY rotated by RoPE
- * to the three calls above; mla_cache_append is the one call that produces a
- * cache row (c^{KV} and the rotated k^R of a new token) and applies RoPE.
+ * decoupled-RoPE width d_rope (d^R).  The final W^O projection, the
+ * projections that produce q^C and q^R and the rotation of q^R are calls of
+ * mla_layer_gfx950.h.  q_rope and the k_rope part of the cache are passed
+ * ALREADY rotated by RoPE to the three calls above; of the calls here only
+ * mla_cache_append produces a cache row (c^{KV} and the rotated k^R of a new
+ * token) and applies RoPE.
  *
  * General conventions
  *  - Every pointer is a DEVICE pointer unless the comment says "host".

@@ -164,7 +164,7 @@ __device__ __attribute__((aligned(16))) const uint32_t zeros16[4] = {0u, 0u, 0u,
 // one has arrived; the loads of the block after take its place and are spread over the units, because a wavefront stands
 // still while a load is accepted.
 //
-// What bounds it: power.  At 32768 x 6144 x 4096 on codes (690 us, 2390 Tflop/s) the matrix cores are busy 70 % of the
+// What bounds it: power.  At 32768 x 6144 x 4096 on codes (660 - 690 us, 2390 - 2500 Tflop/s) the matrix cores are busy 70 % of the
 // cycles at 1.51 GHz of the card's 2.4.  On f16, whose instructions do half the work a cycle, 1365 us.
 template <int NI, int MT, int WN, int STAGES, bool FAST, bool F32, bool SPLIT, bool STREAM>
 __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int tiles_m, int tiles_n, int splits)
@@ -606,7 +606,7 @@ Plan one_launch(int M, int N, int K, bool fast)
 }
 
 // One launch, or one whose tiles fill whole rounds and another for the tokens that are left: the last round of large tiles
-// is rarely full (4000 x 5376 x 3584: 336 tiles, 86 us; 252 and the rest in smaller ones 79 us).
+// is rarely full (4000 x 5376 x 3584: 336 tiles, 82.8 us; 252 and the rest in smaller ones 74.5).
 Plan plan_of(int M, int N, int K, bool fast)
 {
     Plan best = one_launch(M, N, K, fast);

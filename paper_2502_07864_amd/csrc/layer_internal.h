@@ -8,8 +8,8 @@ namespace mla {
 constexpr int QBLOCK = 128;        // columns (and weight rows) per scale
 constexpr float E4M3_MAX = 448.f;
 // Outputs beyond this many bytes go past the caches: they are read again from memory anyway, and what they would displace is
-// not (us, kept / streamed: queries of 32768 tokens x 32 heads 167 / 131, norm of 32768 x 4096 161 / 155, product of
-// 32768 x 6144 803 / 771; at 8192 tokens and below no difference)
+// not (us, kept / streamed: queries of 32768 tokens x 32 heads 167 / 131, norm of 32768 x 4096 165 / 159, product of
+// 32768 x 6144 697 / 659; at 8192 tokens and below no difference)
 constexpr int64_t STREAM_BYTES = (int64_t)64 << 20;
 
 struct NormParams {

@@ -9,9 +9,9 @@ namespace mla {
 namespace {
 
 // TPR threads per row, NV vectors of eight columns per thread (8 TPR NV >= D).
-// Memory bound: 32768 x 4096 bf16 with residual and codes moves 940 MB in 155 us (6.1 TB/s).  Wide rows take 512 threads
-// with one vector each: with 256, 128, 64 threads and 2, 4, 8 vectors it was 162, 169, 193 us, and 3.6, 5.4, 8.5 against
-// 3.1 us for 64 tokens.
+// Memory bound: 32768 x 4096 bf16 with residual and codes moves 940 MB in 159 us (5.9 TB/s).  Wide rows take 512 threads
+// with one vector each: with 256, 128, 64 threads and 2, 4, 8 vectors it was 4, 9, 25 % slower, and 3.6, 5.4, 8.5 us
+// against 3.1 for 64 tokens, whose time is the launch and two dependent steps (load, sum).
 template <bool F32, int TPR, int NV, bool VEC, bool NORM, bool STREAM>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormParams p)
 {
