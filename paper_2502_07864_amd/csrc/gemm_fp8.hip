@@ -153,9 +153,11 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_rows_kernel(GemmFp8Params p)
 __device__ __attribute__((aligned(16))) const uint32_t zeros16[4] = {0u, 0u, 0u, 0u};
 
 // A workgroup of eight wavefronts, WN of them abreast, computes 32 NI WN outputs of 32 MT (8 / WN) tokens, a wavefront 32 NI
-// outputs of 32 MT tokens: 256 tokens by 256 outputs, 64 x 128 each, or by 128, 64 x 64 each (128 tokens by 256 outputs take
-// as long at 6144 outputs, and at few 5 - 40 % longer: 25000 x 576 x 4096 80 us, these 61).  The codes of a block travel by direct-to-LDS loads, `STAGES` blocks deep; 16-byte piece c of a row lies at position c ^ (row >> 1 & 7)
-// of its 128 bytes, so that the operand reads (32 rows, one piece each half) are free of bank conflicts.
+// outputs of 32 MT tokens: 256 tokens by 256 outputs, 64 x 128 a wavefront, 256 by 128 (64 x 64) or 128 by 128 (32 x 64).
+// 128 tokens by 256 outputs take as long as 256 by 128 at 6144 outputs, and at few 5 - 40 % longer: 25000 x 576 x 4096 80 us,
+// these 61.  128 by 128 fill the CUs sooner: 512 x 6144 x 4096 22.7 us with 256 x 128, 18.0 with these; 1024 x 3584 x 3584 21.0
+// and 17.5.  The codes of a block travel by direct-to-LDS loads, `STAGES` blocks deep; 16-byte piece c of a row lies at position
+// c ^ (row >> 1 & 7) of its 128 bytes, so that the operand reads (32 rows, one piece each half) are free of bank conflicts.
 //
 // A step is one block: NI MT units of 32 outputs x 32 tokens, each one chain of instructions whose result is scaled and
 // added while the next chain runs (32 x 32 x 64 and not 16 x 16 x 128 instructions: beside the latter vector
@@ -174,7 +176,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
     constexpr int WLOADS = OUTPUTS / 64, ALOADS = TOKENS / 64, LOADS = WLOADS + ALOADS + 1;                // per wavefront and block
     constexpr int UNITS = NI * MT;
     constexpr int PITCH = 272;                                                             // epilogue: a token's 256 bytes and 16 more
-    static_assert(OUTPUTS % QBLOCK == 0 && UNITS % 2 == 0 && NI % 2 == 0 && LOADS <= 2 * UNITS && SWAVES < 8);
+    static_assert(OUTPUTS % QBLOCK == 0 && UNITS % 2 == 0 && NI % 2 == 0 && LOADS <= 2 * UNITS + 1 && SWAVES < 8);
     static_assert(8 * 32 * PITCH <= STAGES * STAGE && STAGES * STAGE <= 160 * 1024);
     __shared__ __attribute__((aligned(1024))) unsigned char smem[STAGES * STAGE];
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
@@ -336,6 +338,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
                     // a load per half chain from the barrier on
                     if (i == NI - 1) { if (LOAD == 2) load(first + kb + STAGES, cur, j * 2 + q); }
                     else if (LOAD && 2 * MT + u * 2 + q < LOADS) load(first + kb + STAGES - 1, prev, 2 * MT + u * 2 + q);
+                    if (LOAD && LOADS > 2 * UNITS && u == 0 && q == 1) load(first + kb + STAGES - 1, prev, 2 * UNITS);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int e = 8 * q; e < 8 * q + 8; ++e) acc[pu / MT][pu % MT][e] += s[pu & 1][e] * f[pu % MT];
@@ -564,7 +567,8 @@ __global__ __launch_bounds__(256) void gemm_merge_kernel(GemmFp8Params p, int sp
 
 // ---------------------------------------------------------------- choice
 
-enum Form { ROWS16, ROWS32, SMALL_1x1, SMALL_1x2, SMALL_2x2, SMALL_2x4, TILE128, TILE256 };
+enum Form { ROWS16, ROWS32, SMALL_1x1, SMALL_1x2, SMALL_2x2, SMALL_2x4, TILE_128x128, TILE_256x128, TILE_256x256 };
+constexpr int TILE[][2] = {{16, 16}, {16, 32}, {32, 32}, {64, 32}, {64, 64}, {128, 64}, {128, 128}, {256, 128}, {256, 256}};      // tokens, outputs
 struct Plan {
     Form form;
     int splits;      // shares of K
@@ -574,25 +578,25 @@ struct Plan {
 
 // The form that a model of the times finds fastest: a launch, and per round of 256 workgroups (each fills its CU) the steps
 // over K, or the time that the operands take from memory.  us per step measured with few workgroups, on codes (fast) and on
-// f16; the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  On 140
-// sizes of 400 to 32768 tokens and seven (N, K), with each kind of sums, the choice takes 0.5 % longer than the best form on
-// average, 19 % at the most.
+// f16; the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  On 196
+// sizes of 17 to 32768 tokens and seven (N, K), with each kind of sums, the choice takes 0.3 % longer than the best form on
+// average, 16 % at the most.
 Plan one_launch(int M, int N, int K, bool fast)
 {
     const int blocks = (K + QBLOCK - 1) / QBLOCK;
     if (M <= 16) return {(N + 15) / 16 <= 256 ? ROWS16 : ROWS32, 1, M, 4.f + (float)N * (float)K / 5.5e6f};     // 6144 x 4096, one token: 7.3 / 7.0 us; 3584 x 3584: 4.5 / 6.0
-    struct Shape { Form form; int tokens, outputs, blocks; float launch, step_fast, step_f16, crowded_fast, crowded_f16; };
+    struct Shape { Form form; int blocks; float launch, step_fast, step_f16, crowded_fast, crowded_f16; };
     static const Shape shapes[] = {
-        {SMALL_1x1, 32, 32, 8, 2.8f, 0.67f, 0.83f, 1.9f, 1.9f}, {SMALL_1x2, 64, 32, 4, 3.5f, 0.50f, 0.72f, 1.65f, 1.65f},
-        {SMALL_2x2, 64, 64, 2, 3.4f, 0.40f, 0.61f, 1.5f, 1.5f}, {SMALL_2x4, 128, 64, 1, 3.9f, 0.35f, 0.61f, 1.35f, 1.35f},
-        {TILE128, 256, 128, 1, 3.4f, 0.58f, 1.25f, 1.75f, 1.45f}, {TILE256, 256, 256, 1, 4.4f, 1.00f, 0.f, 1.85f, 0.f}};
-    Plan best = {TILE128, 1, M, 3e38f};
+        {SMALL_1x1, 8, 2.8f, 0.67f, 0.83f, 1.9f, 1.9f}, {SMALL_1x2, 4, 3.5f, 0.50f, 0.72f, 1.65f, 1.65f}, {SMALL_2x2, 2, 3.4f, 0.40f, 0.61f, 1.5f, 1.5f},
+        {SMALL_2x4, 1, 3.9f, 0.35f, 0.61f, 1.35f, 1.35f}, {TILE_128x128, 1, 3.4f, 0.37f, 0.75f, 1.5f, 1.4f},
+        {TILE_256x128, 1, 3.4f, 0.58f, 1.25f, 1.75f, 1.45f}, {TILE_256x256, 1, 4.4f, 1.00f, 0.f, 1.85f, 0.f}};
+    Plan best = {TILE_256x128, 1, M, 3e38f};
     for (const Shape& f : shapes) {
-        if (f.form == TILE256 && !fast) continue;                        // (its registers are taken on f16)
-        const long tiles_m = (M + f.tokens - 1) / f.tokens, tiles = tiles_m * ((N + f.outputs - 1) / f.outputs);
+        if (f.form == TILE_256x256 && !fast) continue;                   // (its registers are taken on f16)
+        const long tokens = TILE[f.form][0], outputs = TILE[f.form][1], tiles = ((M + tokens - 1) / tokens) * ((N + outputs - 1) / outputs);
         const int steps = (blocks + f.blocks - 1) / f.blocks;
         // shares of K, merged by a second launch
-        for (int s = 1; s == 1 || (f.form == TILE128 && s <= 8 && steps / s >= 4 && tiles * s <= 256); s *= 2) {
+        for (int s = 1; s == 1 || (f.form == TILE_256x128 && s <= 8 && steps / s >= 4 && tiles * s <= 256); s *= 2) {
             const long rounds = (tiles * s + 255) / 256;
             const float fill = (float)(tiles * s) / (float)(rounds * 256), crowded = fast ? f.crowded_fast : f.crowded_f16;
             const float step = (fast ? f.step_fast : f.step_f16) * (1.f + (crowded - 1.f) * fill * fill);
@@ -610,8 +614,8 @@ Plan one_launch(int M, int N, int K, bool fast)
 Plan plan_of(int M, int N, int K, bool fast)
 {
     Plan best = one_launch(M, N, K, fast);
-    if (best.form < TILE128 || best.splits > 1) return best;
-    const int rows = 256, wide = best.form == TILE256 ? 256 : 128;
+    if (best.form < TILE_128x128 || best.splits > 1) return best;
+    const int rows = TILE[best.form][0], wide = TILE[best.form][1];
     const long across = (N + wide - 1) / wide, down = (M + rows - 1) / rows, rounds = (down * across) / 256;
     const long whole = rounds * 256 / across;                            // rows of tiles in so many rounds
     if (whole < 1 || whole >= down) return best;
@@ -623,8 +627,7 @@ Plan plan_of(int M, int N, int K, bool fast)
 
 long workgroups(const Plan& plan, int N)
 {
-    static const int tile[][2] = {{16, 16}, {16, 32}, {32, 32}, {64, 32}, {64, 64}, {128, 64}, {256, 128}, {256, 256}};
-    const int* t = tile[plan.form];
+    const int* t = TILE[plan.form];
     return (long)((plan.tokens + t[0] - 1) / t[0]) * ((N + t[1] - 1) / t[1]) * plan.splits;
 }
 
@@ -660,7 +663,7 @@ template <int NI, int MT, int WN, int STAGES, bool FAST> void launch_tiles(const
     };
     using std::true_type;
     using std::false_type;
-    if (splits > 1) { if constexpr (OUTPUTS == 128) run(false_type{}, true_type{}, false_type{}); }
+    if (splits > 1) { if constexpr (OUTPUTS == 128 && TOKENS == 256) run(false_type{}, true_type{}, false_type{}); }
     else if (f32)                    stream ? run(true_type{}, false_type{}, true_type{}) : run(true_type{}, false_type{}, false_type{});
     else                             stream ? run(false_type{}, false_type{}, true_type{}) : run(false_type{}, false_type{}, false_type{});
     if (splits > 1) {
@@ -717,11 +720,15 @@ hipError_t launch_gemm_fp8(const GemmFp8Params& all, mla_dtype out, bool fast_su
             case SMALL_1x2: launch_small_tiles<1, 2, 4, 3>(p, f32, fast_sums, s); break;
             case SMALL_2x2: launch_small_tiles<2, 2, 2, 4>(p, f32, fast_sums, s); break;
             case SMALL_2x4: launch_small_tiles<2, 4, 1, 6>(p, f32, fast_sums, s); break;
-            case TILE128:
+            case TILE_128x128:
+                if (fast_sums) launch_tiles<2, 1, 2, 3, true>(p, f32, 1, s);
+                else           launch_tiles<2, 1, 2, 3, false>(p, f32, 1, s);
+                break;
+            case TILE_256x128:
                 if (fast_sums) launch_tiles<2, 2, 2, 3, true>(p, f32, plan.splits, s);
                 else           launch_tiles<2, 2, 2, 3, false>(p, f32, plan.splits, s);
                 break;
-            case TILE256: launch_tiles<4, 2, 2, 2, true>(p, f32, 1, s); break;
+            case TILE_256x256: launch_tiles<4, 2, 2, 2, true>(p, f32, 1, s); break;
         }
     });
     return hipGetLastError();

@@ -231,6 +231,13 @@ def test_gemm_few_outputs_of_many_tokens(M, N, K, fast):
     test_gemm_forms(M, N, K, fast)
 
 
+@pytest.mark.parametrize("fast", [False, True])
+@pytest.mark.parametrize("M, N, K", [(513, 6145, 128), (400, 6100, 4112), (1025, 3585, 272), (3000, 577, 1040), (3001, 640, 16), (2049, 1281, 2064), (5000, 321, 400)])
+def test_gemm_tiles_of_128(M, N, K, fast):
+    """Tiles of 128 tokens and outputs: a few blocks, one, and less than one."""
+    test_gemm_forms(M, N, K, fast)
+
+
 @pytest.mark.parametrize("K", [16, 32, 112, 128, 144, 240, 256, 272, 384, 400, 496, 512, 528, 1024, 1040, 2032, 2048, 4080])
 @pytest.mark.parametrize("M, N", [(5, 70), (40, 200), (300, 300)])
 def test_gemm_depths(M, N, K):
