@@ -84,6 +84,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormPar
         uint8_t* dst = p.codes + row * p.D + c;
         if constexpr (VEC) {
             put_words<STREAM>(dst, (words2){lo, hi});
+        } else if (p.D - c >= 8) {
+            *reinterpret_cast<words2_any*>(dst) = (words2){lo, hi};
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
