@@ -172,110 +172,136 @@ __device__ __forceinline__ int64_t place_of(const StoreParams& p, int r, int& po
     return (int64_t)page * p.page_size + pos % p.page_size;
 }
 
-// A wavefront per row, four rows per workgroup, so that a workgroup needs no barrier and its rows no order: 32768 rows of 576
-// in bf16, the latents normed, are 75 MB in 18 us (4.2 TB/s: the launch and three dependent loads, position, page, row, count
-// at this size); one row each of four sequences 2.8 us.  The row in registers, eight values at a time, turns (and for HALF the
-// rope part) in the wavefront's own LDS.
-template <bool F32, bool HALF, int CACHE>
+// v / d, correctly rounded where nothing underflows: one step from the quotient by the rounded reciprocal.  (Eighteen divisions
+// a lane, ten instructions each, took as long as the memory.)
+__device__ __forceinline__ float quotient(float v, float d, float reciprocal)
+{
+    const float q = v * reciprocal;
+    return __builtin_fmaf(__builtin_fmaf(-q, d, v), reciprocal, q);
+}
+
+// A wavefront per row, four rows per workgroup, so that a workgroup needs no barrier and its rows no order.  A lane holds eight
+// values of c (CV times, CV 512 >= d_c) and pair `lane` of k (and lane + 64), whose turn it works out itself.
+template <bool F32, bool HALF, int CACHE, int CV>
 __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
 {
-    __shared__ float2 turns_lds[4][MAX_PAIRS];
-    __shared__ __attribute__((aligned(16))) float part_lds[HALF ? 4 : 1][HALF ? 2 * MAX_PAIRS : 4];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = blockIdx.x * 4 + wave;
     if (r >= p.rows_total) return;
-    const int n = p.d_c + p.d_rope, pairs = p.d_rope / 2, vecs = n / 8, cv = p.d_c / 8;
-    constexpr int NV = MAX_ROW / 512;
-    float v[NV][8], w[NV][8];
+    const int n = p.d_c + p.d_rope, pairs = p.d_rope / 2, cv = p.d_c / 8;
+    constexpr int KV = MAX_PAIRS / 64;
+    float v[CV][8], w[CV][8], re[KV], im[KV];
+    const int64_t row = (int64_t)r * p.pitch;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
+    for (int i = 0; i < CV; ++i) {
         const int c = lane + i * 64;
-        if (c < vecs) load_vec<F32, 8>(p.rows, (int64_t)r * p.pitch + c * 8, v[i]);
+        if (c < cv) load_vec<F32, 8>(p.rows, row + c * 8, v[i]);
         if (p.norm_weight && c < cv) load_vec<F32, 8>(p.norm_weight, c * 8, w[i]);
+    }
+    // columns of k that make up pair i
+    auto re_at = [&](int i) { return p.d_c + (HALF ? i : 2 * i); };
+    auto im_at = [&](int i) { return p.d_c + (HALF ? i + pairs : 2 * i + 1); };
+#pragma unroll
+    for (int i = 0; i < KV; ++i) {
+        const int c = lane + i * 64;
+        if (c >= pairs) continue;
+        if (F32) {
+            const float* src = static_cast<const float*>(p.rows) + row;
+            re[i] = src[re_at(c)];
+            im[i] = src[im_at(c)];
+        } else {
+            const uint16_t* src = static_cast<const uint16_t*>(p.rows) + row;
+            re[i] = bf16_bits_to_f32(src[re_at(c)]);
+            im[i] = bf16_bits_to_f32(src[im_at(c)]);
+        }
     }
     int pos;
     const int64_t at = place_of(p, r, pos);
     if (at < 0) return;
-    for (int i = lane; i < pairs; i += 64) {
+#pragma unroll
+    for (int i = 0; i < KV; ++i) {
+        const int c = lane + i * 64;
+        if (c >= pairs) continue;
         float cs, sn;
-        turn_of(pos, p.freq[i], p.gain, cs, sn);
-        turns_lds[wave][i] = make_float2(cs, sn);
+        turn_of(pos, p.freq[c], p.gain, cs, sn);
+        const float2 z = rotate(re[i], im[i], cs, sn);
+        re[i] = z.x;
+        im[i] = z.y;
     }
     if (p.norm_weight) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < CV; ++i)
             if (lane + i * 64 < cv) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sum += v[i][k] * v[i][k];
             }
         const float inv = 1.f / sqrtf(wave_sum(sum) / (float)p.d_c + p.eps);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < CV; ++i)
             if (lane + i * 64 < cv) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * inv * w[i][k];
             }
     }
-    if (HALF) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = lane + i * 64;
-            if (c < cv || c >= vecs) continue;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) part_lds[HALF ? wave : 0][(c - cv) * 8 + k] = v[i][k];
-        }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");                         // (accesses of a wavefront complete in order)
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = lane + i * 64;
-        if (c < cv || c >= vecs) continue;
-        const int first = (c - cv) * 8;
-        if (HALF) {
-            const bool im = first >= pairs;
-            const int pair = im ? first - pairs : first;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float2 t = turns_lds[wave][pair + k];
-                const float other = part_lds[HALF ? wave : 0][im ? pair + k : first + pairs + k];
-                v[i][k] = im ? rotate(other, v[i][k], t.x, t.y).y : rotate(v[i][k], other, t.x, t.y).x;
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; k += 2) {
-                const float2 t = turns_lds[wave][first / 2 + k / 2], z = rotate(v[i][k], v[i][k + 1], t.x, t.y);
-                v[i][k] = z.x;
-                v[i][k + 1] = z.y;
-            }
-        }
-    }
-    float scale = 1.f;
+    float scale = 1.f, inv = 1.f;
     if (CACHE == MLA_FP8_E4M3) {
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (lane + i * 64 < vecs) {
+        for (int i = 0; i < CV; ++i)
+            if (lane + i * 64 < cv) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) top = max(top, magnitude(v[i][k]));
             }
 #pragma unroll
+        for (int i = 0; i < KV; ++i)
+            if (lane + i * 64 < pairs) top = max(top, max(magnitude(re[i]), magnitude(im[i])));
+#pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
         scale = block_scale(top);
+        inv = 1.f / scale;
         if (lane == 0) p.kv_scale[at] = scale;
     }
+    auto q = [&](float x) { return quotient(x, scale, inv); };
+    const int64_t o = at * n;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
+    for (int i = 0; i < CV; ++i) {
         const int c = lane + i * 64;
-        if (c >= vecs) continue;
-        const int64_t o = at * n + c * 8;
+        if (c >= cv) continue;
         if constexpr (CACHE == MLA_FP8_E4M3)
-            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.kv) + o) =
-                make_uint2(e4m3_quad(v[i][0] / scale, v[i][1] / scale, v[i][2] / scale, v[i][3] / scale),
-                           e4m3_quad(v[i][4] / scale, v[i][5] / scale, v[i][6] / scale, v[i][7] / scale));
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.kv) + o + c * 8) =
+                make_uint2(e4m3_quad(q(v[i][0]), q(v[i][1]), q(v[i][2]), q(v[i][3])), e4m3_quad(q(v[i][4]), q(v[i][5]), q(v[i][6]), q(v[i][7])));
         else
-            store_vec<CACHE == MLA_F32, 8>(p.kv, o, v[i]);
+            store_vec<CACHE == MLA_F32, 8>(p.kv, o + c * 8, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < KV; ++i) {
+        const int c = lane + i * 64;
+        if (c >= pairs) continue;
+        if constexpr (CACHE == MLA_F32) {
+            float* dst = static_cast<float*>(p.kv) + o;
+            dst[re_at(c)] = re[i];
+            dst[im_at(c)] = im[i];
+        } else if constexpr (CACHE == MLA_BF16) {
+            const uint32_t two = bf16_pair(re[i], im[i]);
+            uint16_t* dst = static_cast<uint16_t*>(p.kv) + o;
+            if (HALF) {
+                dst[re_at(c)] = (uint16_t)two;
+                dst[im_at(c)] = (uint16_t)(two >> 16);
+            } else {
+                *reinterpret_cast<uint32_t*>(dst + re_at(c)) = two;
+            }
+        } else {
+            const uint32_t two = e4m3_quad(q(re[i]), q(im[i]), 0.f, 0.f);
+            uint8_t* dst = static_cast<uint8_t*>(p.kv) + o;
+            if (HALF) {
+                dst[re_at(c)] = (uint8_t)two;
+                dst[im_at(c)] = (uint8_t)(two >> 8);
+            } else {
+                *reinterpret_cast<uint16_t*>(dst + re_at(c)) = (uint16_t)two;
+            }
+        }
     }
 }
 
@@ -371,10 +397,12 @@ template <bool F32, bool HALF> void rope(const RopeParams& p, hipStream_t s)
 template <bool F32, bool HALF, int CACHE> void store_rows(const StoreParams& p, hipStream_t s)
 {
     const int n = p.d_c + p.d_rope;
-    const bool vec = p.d_c % 8 == 0 && p.d_rope % (HALF ? 16 : 8) == 0 && p.pitch % (F32 ? 4 : 8) == 0 && on(p.rows, 16) &&
-                     on(p.norm_weight, 16) && on(p.kv, 16) && n <= MAX_ROW;
-    if (vec) cache_store_kernel<F32, HALF, CACHE><<<dim3((unsigned)((p.rows_total + 3) / 4)), dim3(256), 0, s>>>(p);
-    else     cache_store_any_kernel<F32, HALF, CACHE><<<dim3((unsigned)p.rows_total), dim3(256), 0, s>>>(p);
+    const bool vec = p.d_c % 8 == 0 && p.d_rope % 8 == 0 && p.pitch % (F32 ? 4 : 8) == 0 && on(p.rows, 16) && on(p.norm_weight, 16) &&
+                     on(p.kv, 16) && n <= MAX_ROW;
+    const dim3 grid((unsigned)((p.rows_total + 3) / 4)), block(256);
+    if (vec && p.d_c <= 512) cache_store_kernel<F32, HALF, CACHE, 1><<<grid, block, 0, s>>>(p);
+    else if (vec)            cache_store_kernel<F32, HALF, CACHE, 2><<<grid, block, 0, s>>>(p);
+    else                     cache_store_any_kernel<F32, HALF, CACHE><<<dim3((unsigned)p.rows_total), dim3(256), 0, s>>>(p);
 }
 
 template <bool F32, bool HALF> void store(const StoreParams& p, mla_dtype cache, hipStream_t s)
