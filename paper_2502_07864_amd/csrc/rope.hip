@@ -162,10 +162,9 @@ __global__ __launch_bounds__(256) void rope_queries_any_kernel(RopeParams p)
 
 constexpr int MAX_ROW = 1024;
 
-// where row r goes: its row of the pool, or -1 where it has no place
-__device__ __forceinline__ int64_t place_of(const StoreParams& p, int r, int& pos)
+// where row r, of position pos, goes: its row of the pool, or -1 where it has no place
+__device__ __forceinline__ int64_t place_of(const StoreParams& p, int r, int pos)
 {
-    pos = p.positions[r];
     if (pos < 0 || pos >= p.max_pages * p.page_size) return -1;                    // outside the table
     const int page = p.page_table[(int64_t)(r / p.new_tokens) * p.max_pages + pos / p.page_size];
     if (page < 0 || page >= p.num_pages) return -1;                                // outside the pool
@@ -181,8 +180,10 @@ __device__ __forceinline__ float quotient(float v, float d, float reciprocal)
 }
 
 // A wavefront per row, four rows per workgroup, so that a workgroup needs no barrier and its rows no order.  A lane holds eight
-// values of c (CV times, CV 512 >= d_c) and pair `lane` of k (and lane + 64), whose turn it works out itself.
-template <bool F32, bool HALF, int CACHE, int CV>
+// values of c and a pair of k, whose turn it works out itself, NV times (512 NV >= d_c, 128 NV >= d_rope > 0).
+// 32768 rows of 576 in bf16, the latents normed, are 75 MB in 15.5 us (4.9 TB/s; the launch, a round trip for position and
+// page, and the stores count at this size), from fp32 to fp8 94 MB in 16.2 (5.8); one row each of 64 sequences 2.8 us.
+template <bool F32, bool HALF, int CACHE, int NV>
 __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
 {
     const int tid = threadIdx.x, lane = tid & 63;
@@ -190,41 +191,61 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
     const int r = blockIdx.x * 4 + wave;
     if (r >= p.rows_total) return;
     const int n = p.d_c + p.d_rope, pairs = p.d_rope / 2, cv = p.d_c / 8;
-    constexpr int KV = MAX_PAIRS / 64;
-    float v[CV][8], w[CV][8], re[KV], im[KV];
+    // Every load that depends on no other goes out before the first wait: lanes past the end repeat the last vector or pair
+    // (with branches around the loads, and a wait in each, 18.1 us).
     const int64_t row = (int64_t)r * p.pitch;
+    const uint16_t* halves = static_cast<const uint16_t*>(p.rows) + row;
+    const float* words = static_cast<const float*>(p.rows) + row;
+    const int pos = p.positions[r];
+    words4 v_raw[NV][F32 ? 2 : 1], w_raw[NV][F32 ? 2 : 1];
+    float re[NV], im[NV];
+    uint32_t k_raw[NV];
+    double freq[NV];
+    auto raw = [&](const void* base, int c, words4 (&to)[F32 ? 2 : 1]) {
+        const words4* src = reinterpret_cast<const words4*>(F32 ? static_cast<const void*>(static_cast<const float*>(base) + c * 8)
+                                                                : static_cast<const void*>(static_cast<const uint16_t*>(base) + c * 8));
 #pragma unroll
-    for (int i = 0; i < CV; ++i) {
-        const int c = lane + i * 64;
-        if (c < cv) load_vec<F32, 8>(p.rows, row + c * 8, v[i]);
-        if (p.norm_weight && c < cv) load_vec<F32, 8>(p.norm_weight, c * 8, w[i]);
-    }
+        for (int i = 0; i < (F32 ? 2 : 1); ++i) to[i] = src[i];
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) raw(F32 ? static_cast<const void*>(words) : static_cast<const void*>(halves), min(lane + i * 64, cv - 1), v_raw[i]);
     // columns of k that make up pair i
     auto re_at = [&](int i) { return p.d_c + (HALF ? i : 2 * i); };
     auto im_at = [&](int i) { return p.d_c + (HALF ? i + pairs : 2 * i + 1); };
 #pragma unroll
-    for (int i = 0; i < KV; ++i) {
-        const int c = lane + i * 64;
-        if (c >= pairs) continue;
+    for (int i = 0; i < NV; ++i) {
+        const int c = min(lane + i * 64, pairs - 1);
         if (F32) {
-            const float* src = static_cast<const float*>(p.rows) + row;
-            re[i] = src[re_at(c)];
-            im[i] = src[im_at(c)];
+            re[i] = words[re_at(c)];
+            im[i] = words[im_at(c)];
         } else {
-            const uint16_t* src = static_cast<const uint16_t*>(p.rows) + row;
-            re[i] = bf16_bits_to_f32(src[re_at(c)]);
-            im[i] = bf16_bits_to_f32(src[im_at(c)]);
+            k_raw[i] = HALF ? halves[re_at(c)] | (uint32_t)halves[im_at(c)] << 16 : *reinterpret_cast<const uint32_t*>(halves + re_at(c));
         }
+        freq[i] = p.freq[c];
     }
-    int pos;
+    if (p.norm_weight) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw(p.norm_weight, min(lane + i * 64, cv - 1), w_raw[i]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     const int64_t at = place_of(p, r, pos);
     if (at < 0) return;
+    auto values = [&](const words4 (&from)[F32 ? 2 : 1], float (&to)[8]) {
 #pragma unroll
-    for (int i = 0; i < KV; ++i) {
-        const int c = lane + i * 64;
-        if (c >= pairs) continue;
+        for (int k = 0; k < 8; ++k)
+            to[k] = F32 ? __uint_as_float(from[F32 ? k / 4 : 0][k % 4]) : __uint_as_float(k % 2 ? from[0][k / 2 % 4] & 0xFFFF0000u : from[0][k / 2 % 4] << 16);
+    };
+    float v[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) values(v_raw[i], v[i]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (!F32) {
+            re[i] = __uint_as_float(k_raw[i] << 16);
+            im[i] = __uint_as_float(k_raw[i] & 0xFFFF0000u);
+        }
         float cs, sn;
-        turn_of(pos, p.freq[c], p.gain, cs, sn);
+        turn_of(pos, freq[i], p.gain, cs, sn);
         const float2 z = rotate(re[i], im[i], cs, sn);
         re[i] = z.x;
         im[i] = z.y;
@@ -232,30 +253,31 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
     if (p.norm_weight) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < CV; ++i)
+        for (int i = 0; i < NV; ++i)
             if (lane + i * 64 < cv) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sum += v[i][k] * v[i][k];
             }
         const float inv = 1.f / sqrtf(wave_sum(sum) / (float)p.d_c + p.eps);
 #pragma unroll
-        for (int i = 0; i < CV; ++i)
-            if (lane + i * 64 < cv) {
+        for (int i = 0; i < NV; ++i) {
+            float w[8];
+            values(w_raw[i], w);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * inv * w[i][k];
-            }
+            for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * inv * w[k];
+        }
     }
     float scale = 1.f, inv = 1.f;
     if (CACHE == MLA_FP8_E4M3) {
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < CV; ++i)
+        for (int i = 0; i < NV; ++i)
             if (lane + i * 64 < cv) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) top = max(top, magnitude(v[i][k]));
             }
 #pragma unroll
-        for (int i = 0; i < KV; ++i)
+        for (int i = 0; i < NV; ++i)
             if (lane + i * 64 < pairs) top = max(top, max(magnitude(re[i]), magnitude(im[i])));
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
@@ -266,7 +288,7 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
     auto q = [&](float x) { return quotient(x, scale, inv); };
     const int64_t o = at * n;
 #pragma unroll
-    for (int i = 0; i < CV; ++i) {
+    for (int i = 0; i < NV; ++i) {
         const int c = lane + i * 64;
         if (c >= cv) continue;
         if constexpr (CACHE == MLA_FP8_E4M3)
@@ -276,7 +298,7 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
             store_vec<CACHE == MLA_F32, 8>(p.kv, o + c * 8, v[i]);
     }
 #pragma unroll
-    for (int i = 0; i < KV; ++i) {
+    for (int i = 0; i < NV; ++i) {
         const int c = lane + i * 64;
         if (c >= pairs) continue;
         if constexpr (CACHE == MLA_F32) {
@@ -314,7 +336,7 @@ __global__ __launch_bounds__(256) void cache_store_any_kernel(StoreParams p)
     __shared__ uint32_t tops[4];
     const int r = blockIdx.x, tid = threadIdx.x;
     const int n = p.d_c + p.d_rope, pairs = p.d_rope / 2;
-    int pos;
+    const int pos = p.positions[r];
     const int64_t at = place_of(p, r, pos);
     if (at < 0) return;
     auto load = [&](const void* base, int64_t i) {
@@ -397,12 +419,12 @@ template <bool F32, bool HALF> void rope(const RopeParams& p, hipStream_t s)
 template <bool F32, bool HALF, int CACHE> void store_rows(const StoreParams& p, hipStream_t s)
 {
     const int n = p.d_c + p.d_rope;
-    const bool vec = p.d_c % 8 == 0 && p.d_rope % 8 == 0 && p.pitch % (F32 ? 4 : 8) == 0 && on(p.rows, 16) && on(p.norm_weight, 16) &&
+    const bool vec = p.d_c % 8 == 0 && p.d_rope % 8 == 0 && p.d_rope > 0 && p.pitch % (F32 ? 4 : 8) == 0 && on(p.rows, 16) && on(p.norm_weight, 16) &&
                      on(p.kv, 16) && n <= MAX_ROW;
     const dim3 grid((unsigned)((p.rows_total + 3) / 4)), block(256);
-    if (vec && p.d_c <= 512) cache_store_kernel<F32, HALF, CACHE, 1><<<grid, block, 0, s>>>(p);
-    else if (vec)            cache_store_kernel<F32, HALF, CACHE, 2><<<grid, block, 0, s>>>(p);
-    else                     cache_store_any_kernel<F32, HALF, CACHE><<<dim3((unsigned)p.rows_total), dim3(256), 0, s>>>(p);
+    if (vec && p.d_c <= 512 && p.d_rope <= 128) cache_store_kernel<F32, HALF, CACHE, 1><<<grid, block, 0, s>>>(p);
+    else if (vec) cache_store_kernel<F32, HALF, CACHE, 2><<<grid, block, 0, s>>>(p);
+    else          cache_store_any_kernel<F32, HALF, CACHE><<<dim3((unsigned)p.rows_total), dim3(256), 0, s>>>(p);
 }
 
 template <bool F32, bool HALF> void store(const StoreParams& p, mla_dtype cache, hipStream_t s)
