@@ -3,6 +3,8 @@
 #include "mla_internal.h"
 #include "mla_layer_gfx950.h"
 
+#include <type_traits>
+
 namespace mla {
 
 constexpr int QBLOCK = 128;        // columns (and weight rows) per scale
@@ -71,27 +73,34 @@ hipError_t launch_cache_store(const StoreParams& p, int layout, mla_dtype io, ml
 
 // ---- device helpers
 
-// V (8 or 4) consecutive values in accesses of up to 16 bytes, which the address has to allow
+typedef __attribute__((ext_vector_type(4))) uint32_t words4;
+typedef __attribute__((ext_vector_type(2))) uint32_t words2;
+
+// V (8 or 4) consecutive values in accesses of up to 16 bytes, which the address has to allow.  As they come (raw_vec) and as
+// floats (values_of): kernels ask for all they can before they unpack any, or the compiler waits for each in turn.
+template <bool F32, int V> struct RawVec {
+    static constexpr int N = F32 && V == 8 ? 2 : 1;
+    std::conditional_t<F32 || V == 8, words4, words2> w[N];
+};
+template <bool F32, int V> __device__ __forceinline__ RawVec<F32, V> raw_vec(const void* base, int64_t at)
+{
+    RawVec<F32, V> r;
+    const auto* src = reinterpret_cast<const std::remove_reference_t<decltype(r.w[0])>*>(static_cast<const char*>(base) + at * (F32 ? 4 : 2));
+#pragma unroll
+    for (int i = 0; i < r.N; ++i) r.w[i] = src[i];
+    return r;
+}
+template <bool F32, int V> __device__ __forceinline__ void values_of(const RawVec<F32, V>& r, float (&v)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const uint32_t word = F32 ? r.w[i / 4 % r.N][i % 4] : r.w[0][i / 2];
+        v[i] = __uint_as_float(F32 ? word : i % 2 ? word & 0xFFFF0000u : word << 16);
+    }
+}
 template <bool F32, int V> __device__ __forceinline__ void load_vec(const void* base, int64_t at, float (&v)[V])
 {
-    if constexpr (F32) {
-#pragma unroll
-        for (int i = 0; i < V; i += 4) {
-            const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(base) + at + i);
-            v[i] = a.x; v[i + 1] = a.y; v[i + 2] = a.z; v[i + 3] = a.w;
-        }
-    } else {
-        uint32_t w[V / 2];
-        if constexpr (V == 8) {
-            const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at);
-            w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-        } else {
-            const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + at);
-            w[0] = u.x; w[1] = u.y;
-        }
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-    }
+    values_of<F32, V>(raw_vec<F32, V>(base, at), v);
 }
 
 // two values as bf16, each rounded to nearest even (v_cvt_pk_bf16_f32)
@@ -103,8 +112,6 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
 }
 
 // STREAM: past the caches
-typedef __attribute__((ext_vector_type(4))) uint32_t words4;
-typedef __attribute__((ext_vector_type(2))) uint32_t words2;
 template <bool STREAM, typename W> __device__ __forceinline__ void put_words(void* dst, W w)
 {
     if constexpr (STREAM) __builtin_nontemporal_store(w, static_cast<W*>(dst));
@@ -125,17 +132,14 @@ template <bool F32, int V, bool STREAM = false> __device__ __forceinline__ void 
     }
 }
 
-// Eight consecutive values.  VEC: whole vectors, as above.  Otherwise at any address of the type: 16-byte accesses all the
-// same (the hardware takes them apart where they cross a line), and where fewer than eight are `left` one by one; those past
-// them read as zero and are not written.  (Norm of 6517 x 3443 and 32768 x 4095, one by one / so: bf16 94 / 41 us and 574 / 335,
-// fp32 162 / 61 and 952 / 321.)
+// Eight consecutive values at any address of the type: 16-byte accesses all the same (the hardware takes them apart where they
+// cross a line), and where fewer than eight are `left` one by one; those past them read as zero and are not written.  (Norm of
+// 6517 x 3443 and 32768 x 4095, one by one / so: bf16 94 / 41 us and 574 / 335, fp32 162 / 61 and 952 / 321.)  VEC: whole vectors.
 typedef words4 __attribute__((aligned(2))) words4_any;
 typedef words2 __attribute__((aligned(1))) words2_any;
-template <bool F32, bool VEC> __device__ __forceinline__ void load8(const void* base, int64_t at, int left, float (&v)[8])
+template <bool F32> __device__ __forceinline__ void load8(const void* base, int64_t at, int left, float (&v)[8])
 {
-    if constexpr (VEC) {
-        load_vec<F32, 8>(base, at, v);
-    } else if (left >= 8) {
+    if (left >= 8) {
         if constexpr (F32) {
             const words4_any* p = reinterpret_cast<const words4_any*>(static_cast<const float*>(base) + at);
             const words4 a = p[0], b = p[1];

@@ -24,20 +24,37 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormPar
 
     float v[NV][8], w[NV][8];
     float sum = 0.f;
+    // whole vectors: everything is asked for before the first wait, threads past the end take the last vector
+    RawVec<F32, 8> x_raw[VEC ? NV : 1], r_raw[VEC ? NV : 1], w_raw[VEC ? NV : 1];
+    if constexpr (VEC) {
+        auto ask = [&](const void* base, int64_t at, auto& raw) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) raw[i] = raw_vec<F32, 8>(base, at + min((i * TPR + t) * 8, p.D - 8));
+        };
+        ask(p.x, row * p.x_pitch, x_raw);
+        if (NORM && p.residual) ask(p.residual, row * p.D, r_raw);
+        if (NORM && p.weight) ask(p.weight, 0, w_raw);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + t) * 8;
 #pragma unroll
         for (int k = 0; k < 8; ++k) { v[i][k] = 0.f; w[i][k] = 1.f; }
         if (c < p.D) {
-            load8<F32, VEC>(p.x, row * p.x_pitch + c, p.D - c, v[i]);
+            if constexpr (VEC) values_of<F32, 8>(x_raw[i], v[i]);
+            else               load8<F32>(p.x, row * p.x_pitch + c, p.D - c, v[i]);
             if (NORM && p.residual) {
                 float r[8];
-                load8<F32, VEC>(p.residual, row * p.D + c, p.D - c, r);
+                if constexpr (VEC) values_of<F32, 8>(r_raw[i], r);
+                else               load8<F32>(p.residual, row * p.D + c, p.D - c, r);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[i][k] += r[k];
             }
-            if (NORM && p.weight) load8<F32, VEC>(p.weight, c, p.D - c, w[i]);
+            if (NORM && p.weight) {
+                if constexpr (VEC) values_of<F32, 8>(w_raw[i], w[i]);
+                else               load8<F32>(p.weight, c, p.D - c, w[i]);
+            }
         }
         if (NORM) {
 #pragma unroll

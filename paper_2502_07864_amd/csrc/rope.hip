@@ -23,8 +23,8 @@ __device__ __forceinline__ float2 rotate(float re, float im, float cs, float sn)
 // V values at a time.  A workgroup takes `tokens` tokens of `heads` heads: every thread asks for its values first, the
 // turns of the tokens are worked out while they travel and go to LDS, the nope values leave as they came.  HALF: a thread
 // holds the vector of real parts and that of imaginary parts; otherwise V / 2 whole pairs.
-// Memory bound: 32768 tokens x 32 heads x (128 + 64) bf16, 805 MB moved in 132 us (6.1 TB/s); 16 tokens: 2.9 us, the launch
-// and a round trip.
+// Memory bound: 32768 tokens x 32 heads x (128 + 64) bf16, 805 MB moved in 128 - 131 us (6.2 TB/s); 16 tokens: 2.3 us from a
+// graph, the launch and a round trip.
 constexpr int ROPE_TOKENS = 16, ROPE_UNITS = 4;
 
 // j / d for j < 2^21: the quotient's error, j / d 2^-22, stays below the half of 1 / d that separates it from the next whole number
@@ -72,18 +72,22 @@ __global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p, int tok
             for (int k = 0; k < PARTS; ++k) put_words<STREAM>(reinterpret_cast<vec*>(dst) + k, buf[i][k]);
         }
     };
-    auto load = [&](int j, float (&a)[V], float (&b)[V], int64_t& to, int& at) {
+    using Raw = RawVec<F32, V>;
+    auto load = [&](int j, Raw& a, Raw& b, int64_t& to, int& at) {
         const int r = divide(j, inv_rv), c = (j - r * rv) * V;
         int t, h;
         row_of(r, t, h);
         const int64_t from = (int64_t)t * p.pitch + (int64_t)h * width + p.d_nope + c;
-        load_vec<F32, V>(p.q, from, a);
-        if (HALF) load_vec<F32, V>(p.q, from + pairs, b);
+        a = raw_vec<F32, V>(p.q, from);
+        if (HALF) b = raw_vec<F32, V>(p.q, from + pairs);
         to = ((int64_t)t * p.H + h) * p.d_rope + c;
         at = (t - t0) * pairs + (HALF ? c : c / 2);
     };
-    auto turn = [&](float (&a)[V], float (&b)[V], int64_t to, int at) {
+    auto turn = [&](const Raw& ra, const Raw& rb, int64_t to, int at) {
+        float a[V], b[V];
+        values_of<F32, V>(ra, a);
         if constexpr (HALF) {
+            values_of<F32, V>(rb, b);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const float2 w = turns[at + k], z = rotate(a[k], b[k], w.x, w.y);
@@ -103,7 +107,7 @@ __global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p, int tok
         }
     };
 
-    float a[2][V], b[2][V];
+    Raw a[2], b[2];
     int64_t to[2];
     int at[2];
 #pragma unroll
@@ -197,18 +201,12 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
     const uint16_t* halves = static_cast<const uint16_t*>(p.rows) + row;
     const float* words = static_cast<const float*>(p.rows) + row;
     const int pos = p.positions[r];
-    words4 v_raw[NV][F32 ? 2 : 1], w_raw[NV][F32 ? 2 : 1];
+    RawVec<F32, 8> v_raw[NV], w_raw[NV];
     float re[NV], im[NV];
     uint32_t k_raw[NV];
     double freq[NV];
-    auto raw = [&](const void* base, int c, words4 (&to)[F32 ? 2 : 1]) {
-        const words4* src = reinterpret_cast<const words4*>(F32 ? static_cast<const void*>(static_cast<const float*>(base) + c * 8)
-                                                                : static_cast<const void*>(static_cast<const uint16_t*>(base) + c * 8));
 #pragma unroll
-        for (int i = 0; i < (F32 ? 2 : 1); ++i) to[i] = src[i];
-    };
-#pragma unroll
-    for (int i = 0; i < NV; ++i) raw(F32 ? static_cast<const void*>(words) : static_cast<const void*>(halves), min(lane + i * 64, cv - 1), v_raw[i]);
+    for (int i = 0; i < NV; ++i) v_raw[i] = raw_vec<F32, 8>(p.rows, row + min(lane + i * 64, cv - 1) * 8);
     // columns of k that make up pair i
     auto re_at = [&](int i) { return p.d_c + (HALF ? i : 2 * i); };
     auto im_at = [&](int i) { return p.d_c + (HALF ? i + pairs : 2 * i + 1); };
@@ -225,19 +223,14 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
     }
     if (p.norm_weight) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) raw(p.norm_weight, min(lane + i * 64, cv - 1), w_raw[i]);
+        for (int i = 0; i < NV; ++i) w_raw[i] = raw_vec<F32, 8>(p.norm_weight, min(lane + i * 64, cv - 1) * 8);
     }
     __builtin_amdgcn_sched_barrier(0);
     const int64_t at = place_of(p, r, pos);
     if (at < 0) return;
-    auto values = [&](const words4 (&from)[F32 ? 2 : 1], float (&to)[8]) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            to[k] = F32 ? __uint_as_float(from[F32 ? k / 4 : 0][k % 4]) : __uint_as_float(k % 2 ? from[0][k / 2 % 4] & 0xFFFF0000u : from[0][k / 2 % 4] << 16);
-    };
     float v[NV][8];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) values(v_raw[i], v[i]);
+    for (int i = 0; i < NV; ++i) values_of<F32, 8>(v_raw[i], v[i]);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         if (!F32) {
@@ -262,7 +255,7 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float w[8];
-            values(w_raw[i], w);
+            values_of<F32, 8>(w_raw[i], w);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * inv * w[k];
         }
@@ -397,9 +390,9 @@ template <bool F32, bool HALF> void rope(const RopeParams& p, hipStream_t s)
         rope_queries_any_kernel<F32, HALF><<<dim3((unsigned)p.T), dim3(256), 0, s>>>(p);
         return;
     }
-    // As many heads' rows per workgroup as give half of its threads a vector to turn (32768 tokens x 32 heads, 16 / 32 / 64 rows:
-    // pairs 131 / 141 / 146 us, halves 157 / 138 / 147), fewer while that leaves CUs without one
-    const int rows = std::max(1, 128 / (unit / v));
+    // As many heads' rows per workgroup as have 128 vectors to turn (32768 tokens x 32 heads, 8 / 16 / 32 rows: pairs 160 / 128 /
+    // 141 us; 16 / 32 / 64: halves 131 / 142 / 148), fewer while that leaves CUs without one
+    const int rows = std::max(1, 128 / (p.d_rope / v));
     int heads = std::min(p.H, rows), tokens = std::max(1, std::min(rows / heads, ROPE_TOKENS));
     auto grid_of = [&] { return (int64_t)((p.T + tokens - 1) / tokens) * ((p.H + heads - 1) / heads); };
     while (grid_of() < 512 && tokens > 1) tokens = (tokens + 1) / 2;
