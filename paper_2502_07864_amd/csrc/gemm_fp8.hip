@@ -408,7 +408,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
 // block, so that small tiles still keep eight wavefronts.  Up to a few hundred tokens, and for few outputs, small tiles over
 // the whole depth beat large ones over shares of it, whose partial sums go through memory.  Blocks travel as in the tile
 // kernel, KS at a time.  What bounds it: 64 bytes a cycle into a CU, the launch and one round trip to memory where a
-// wavefront has few blocks (61 x 3584 x 3584: 6.9 us; 1024 x 576 x 4096 on codes: 10.6).
+// wavefront has few blocks (61 x 3584 x 3584: 6.7 us; 1024 x 576 x 4096 on codes: 10.4).
 template <int WN, int WM, int KS, int STAGES, bool FAST, bool F32>
 __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p, int tiles_m)
 {
@@ -417,6 +417,10 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
     constexpr int CODES = KS * GROUPS, LOADS = CODES / 8 + 1;                              // loads of a stage, per wavefront
     constexpr int BLOCK_B = (W_ROWS + A_ROWS) * QBLOCK, STAGE = KS * BLOCK_B + 2048;
     constexpr int PITCH = 36;                                                              // floats per token of 32 outputs
+    // One wavefront of each SIMD asks for the next blocks between its two products, the other behind them: the loads have no
+    // pause then.  3 - 8 % of the time of tiles of 32 x 32 and 64 x 32, 2 % of 64 x 64 on codes (all before the products, or half
+    // of each wavefront's: less), but 64 x 64 on f16 and 128 x 64 lose 10 %.
+    constexpr bool APART = KS >= (FAST ? 2 : 4);
     static_assert(CODES % 8 == 0 && KS * A_ROWS <= 256 && STAGES * STAGE <= 160 * 1024 && 8 * 32 * PITCH * 4 <= STAGES * STAGE);
     __shared__ __attribute__((aligned(1024))) unsigned char smem[STAGES * STAGE];
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
@@ -508,11 +512,13 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
         // the products first: while they run the wavefront asks for what comes next, and stands while that is accepted
         f32x16 s = products<FAST>(now.w[0], now.a[0], (f32x16){});
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (MORE && APART) { if (wave < 4) request(st + STAGES, cur); }
+        __builtin_amdgcn_sched_barrier(0);
         const Operands then = read(next);
         __builtin_amdgcn_sched_barrier(0);
         s = products<FAST>(now.w[1], now.a[1], s);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (MORE) request(st + STAGES, cur);
+        if constexpr (MORE) { if (!APART || wave >= 4) request(st + STAGES, cur); }
         __builtin_amdgcn_sched_barrier(0);
         // (a block past the end is zeros, but its scale need not be finite)
         const float f = st * KS + ks < blocks ? now.sa * now.sw : 0.f;
@@ -577,17 +583,17 @@ struct Plan {
 };
 
 // The form that a model of the times finds fastest: a launch, and per round of 256 workgroups (each fills its CU) the steps
-// over K, or the time that the operands take from memory.  us per step measured with few workgroups, on codes (fast) and on
-// f16; the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  On 196
-// sizes of 17 to 32768 tokens and seven (N, K), with each kind of sums, the choice takes 0.3 % longer than the best form on
-// average, 16 % at the most.
+// over K and 1 us from one to the next, or the time that the operands take from memory.  us per step measured with few workgroups, on codes (fast) and on
+// f16; the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  On 280
+// sizes of 17 to 32768 tokens and ten (N, K), with each kind of sums, the choice takes 0.3 % longer than the best form on
+// average, 11 % at the most.
 Plan one_launch(int M, int N, int K, bool fast)
 {
     const int blocks = (K + QBLOCK - 1) / QBLOCK;
     if (M <= 16) return {(N + 15) / 16 <= 256 ? ROWS16 : ROWS32, 1, M, 4.f + (float)N * (float)K / 5.5e6f};     // 6144 x 4096, one token: 7.3 / 7.0 us; 3584 x 3584: 4.5 / 6.0
     struct Shape { Form form; int blocks; float launch, step_fast, step_f16, crowded_fast, crowded_f16; };
     static const Shape shapes[] = {
-        {SMALL_1x1, 8, 2.8f, 0.67f, 0.83f, 1.9f, 1.9f}, {SMALL_1x2, 4, 3.5f, 0.50f, 0.72f, 1.65f, 1.65f}, {SMALL_2x2, 2, 3.4f, 0.40f, 0.61f, 1.5f, 1.5f},
+        {SMALL_1x1, 8, 2.8f, 0.64f, 0.79f, 1.9f, 1.9f}, {SMALL_1x2, 4, 3.5f, 0.47f, 0.70f, 1.65f, 1.65f}, {SMALL_2x2, 2, 3.4f, 0.39f, 0.61f, 1.5f, 1.5f},
         {SMALL_2x4, 1, 3.9f, 0.35f, 0.61f, 1.35f, 1.35f}, {TILE_128x128, 1, 3.4f, 0.37f, 0.75f, 1.5f, 1.4f},
         {TILE_256x128, 1, 3.4f, 0.58f, 1.25f, 1.75f, 1.45f}, {TILE_256x256, 1, 4.4f, 1.00f, 0.f, 1.85f, 0.f}};
     Plan best = {TILE_256x128, 1, M, 3e38f};
@@ -601,7 +607,7 @@ Plan one_launch(int M, int N, int K, bool fast)
             const float fill = (float)(tiles * s) / (float)(rounds * 256), crowded = fast ? f.crowded_fast : f.crowded_f16;
             const float step = (fast ? f.step_fast : f.step_f16) * (1.f + (crowded - 1.f) * fill * fill);
             const float memory = ((float)N + (float)M) * (float)K / 5.5e6f;
-            float t = f.launch + std::max(memory, (float)rounds * (float)((steps + s - 1) / s) * step);
+            float t = f.launch + std::max(memory, (float)rounds * (float)((steps + s - 1) / s) * step + (float)(rounds - 1));
             if (s > 1) t += 4.0f + (float)s * (float)M * (float)N * 8.f / 6e6f;      // (the partial sums, in the caches)
             if (t < best.us) best = {f.form, s, M, t};
         }
