@@ -104,6 +104,29 @@ def test_norm_without_weight_and_strided_rows():
     check_codes(codes, scales, odd.double(), 0.0)
 
 
+@pytest.mark.parametrize("io", [BF, F32])
+@pytest.mark.parametrize("T, D, shift", [(5, 9, 1), (7, 127, 3), (9, 1001, 1), (3, 1000, 5), (4, 4099, 7), (300, 2051, 1)])
+def test_norm_at_any_address(T, D, shift, io):
+    """Inputs and outputs that lie on no 16 bytes: the same numbers, and nothing around the outputs changes."""
+    def at(t, fill=0.0):
+        room = torch.full((t.numel() + 64,), fill, dtype=t.dtype, device=DEV)
+        view = room[shift:shift + t.numel()].view(t.shape)
+        view.copy_(t)
+        return view, room
+    x, r, w = rnd(T, D, dtype=io, loud=True), rnd(T, D, dtype=io, seed=2), (1 + 0.3 * rnd(D, seed=1)).to(io)
+    s, y = ref_norm(x, w, 1e-5, r)
+    out, out_room = at(torch.zeros_like(x), 7.0)
+    sum_out, sum_room = at(torch.zeros_like(x), 7.0)
+    codes, codes_room = at(torch.zeros((T, D), dtype=torch.uint8, device=DEV), 9)
+    scales = torch.empty((blocks(D), T), device=DEV)
+    layer.rms_norm_fp8(at(x)[0], at(w)[0], 1e-5, residual=at(r)[0], codes=codes, scales=scales, residual_out=sum_out, out=out)
+    near(out, y, ROUND[io] + SUM)
+    near(sum_out, s, ROUND[io], 2.0 ** -24 * (x.double().abs() + r.double().abs()))
+    check_codes(codes.contiguous().view(FP8), scales, y, SUM)
+    for room, fill in ((out_room, 7), (sum_room, 7), (codes_room, 9)):
+        assert (room[:shift] == fill).all() and (room[shift + T * D:] == fill).all()
+
+
 def test_norm_in_place():
     x, r, w = rnd(70, 4096, dtype=BF), rnd(70, 4096, dtype=BF, seed=3), rnd(4096, dtype=BF, seed=4)
     want, want_s = layer.rms_norm(x, w, residual=r)
@@ -486,6 +509,14 @@ def test_cache_store(B, new, d_c, d_rope, page, layout, normed, io, cache):
     assert torch.equal(flat[rest], was[rest])
     if cache == FP8:
         assert (scale.view(-1)[rest] == -1).all()
+
+
+@pytest.mark.parametrize("io, cache", [(BF, BF), (F32, F32), (F32, FP8)])
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("d_c, d_rope", [(8, 8), (512, 0), (504, 128), (520, 8), (512, 136), (8, 256), (512, 60)])
+def test_cache_store_parts(d_c, d_rope, layout, io, cache):
+    """Parts at the edges of what the lanes of a wavefront hold: 512 values of c, 64 pairs of k."""
+    test_cache_store(3, 5, d_c, d_rope, 16, layout, True, io, cache)
 
 
 @pytest.mark.parametrize("cache", [BF, FP8])
