@@ -582,11 +582,11 @@ struct Plan {
     float us;
 };
 
-// The form that a model of the times finds fastest: a launch, and per round of 256 workgroups (each fills its CU) the steps
-// over K and 1 us from one to the next, or the time that the operands take from memory.  us per step measured with few workgroups, on codes (fast) and on
-// f16; the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  On 280
-// sizes of 17 to 32768 tokens and ten (N, K), with each kind of sums, the choice takes 0.3 % longer than the best form on
-// average, 11 % at the most.
+// The form that a model of the times finds fastest: a launch, and per round of 256 workgroups (each fills its CU) the steps over
+// K, and 1 us from a round to the next, or the time that the operands take from memory.  us per step measured with few
+// workgroups, on codes (fast) and on f16; the fuller the rounds, the longer the steps, for power and the caches' rates
+// (`crowded`: all CUs).  On 280 sizes of 17 to 32768 tokens and ten (N, K), with each kind of sums, the choice takes 0.3 %
+// longer than the best form on average, 11 % at the most.
 Plan one_launch(int M, int N, int K, bool fast)
 {
     const int blocks = (K + QBLOCK - 1) / QBLOCK;
