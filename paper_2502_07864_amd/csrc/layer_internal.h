@@ -133,52 +133,78 @@ template <bool F32, int V, bool STREAM = false> __device__ __forceinline__ void 
 }
 
 // Eight consecutive values at any address of the type: 16-byte accesses all the same (the hardware takes them apart where they
-// cross a line), and where fewer than eight are `left` one by one; those past them read as zero and are not written.  (Norm of
-// 6517 x 3443 and 32768 x 4095, one by one / so: bf16 94 / 41 us and 574 / 335, fp32 162 / 61 and 952 / 321.)  VEC: whole vectors.
+// cross a line).  Fewer than eight, `left`: four, two and one of them, as its bits say.
 typedef words4 __attribute__((aligned(2))) words4_any;
 typedef words2 __attribute__((aligned(1))) words2_any;
-template <bool F32> __device__ __forceinline__ void load8(const void* base, int64_t at, int left, float (&v)[8])
+typedef uint32_t __attribute__((aligned(1))) word_any;
+typedef uint16_t __attribute__((aligned(1))) half_any;
+template <bool F32> __device__ __forceinline__ RawVec<F32, 8> raw8_any(const void* base, int64_t at)
 {
-    if (left >= 8) {
-        if constexpr (F32) {
-            const words4_any* p = reinterpret_cast<const words4_any*>(static_cast<const float*>(base) + at);
-            const words4 a = p[0], b = p[1];
+    RawVec<F32, 8> r;
+    const words4_any* src = reinterpret_cast<const words4_any*>(static_cast<const char*>(base) + at * (F32 ? 4 : 2));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(a[i]); v[4 + i] = __uint_as_float(b[i]); }
-        } else {
-            const words4 a = *reinterpret_cast<const words4_any*>(static_cast<const uint16_t*>(base) + at);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(a[i] << 16); v[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u); }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = 0.f;
-            if (i < left) v[i] = F32 ? static_cast<const float*>(base)[at + i] : bf16_bits_to_f32(static_cast<const uint16_t*>(base)[at + i]);
-        }
-    }
+    for (int i = 0; i < r.N; ++i) r.w[i] = src[i];
+    return r;
+}
+template <bool F32> __device__ __forceinline__ void load_few(const void* base, int64_t at, int left, float (&v)[8])
+{
+    const bool four = left & 4, two = left & 2, one = left & 1;
+    const char* src = static_cast<const char*>(base) + at * (F32 ? 4 : 2);
+    words4 q = {};                     // four | two | one, as they come
+    words2 h = {};
+    uint32_t s = 0;
+    constexpr int B = F32 ? 4 : 2;
+    if (four) { if (F32) q = *reinterpret_cast<const words4_any*>(src); else { const words2 t = *reinterpret_cast<const words2_any*>(src); q[0] = t[0]; q[1] = t[1]; } }
+    if (two)  { if (F32) h = *reinterpret_cast<const words2_any*>(src + (left & 4) * B); else h[0] = *reinterpret_cast<const word_any*>(src + (left & 4) * B); }
+    if (one)  { if (F32) s = *reinterpret_cast<const word_any*>(src + (left & 6) * B); else s = *reinterpret_cast<const half_any*>(src + (left & 6) * B); }
+    auto low = [](uint32_t w) { return __uint_as_float(F32 ? w : w << 16); };
+    auto high = [](uint32_t w, uint32_t next) { return __uint_as_float(F32 ? next : w & 0xFFFF0000u); };
+    const float p0 = low(h[0]), p1 = high(h[0], h[1]), s0 = low(s);
+    const float t0 = two ? p0 : s0, t1 = p1, t2 = two ? s0 : 0.f;        // what follows the four
+    v[0] = four ? low(q[0]) : t0;
+    v[1] = four ? high(q[0], q[1]) : t1;
+    v[2] = four ? low(F32 ? q[2] : q[1]) : t2;
+    v[3] = four ? high(q[1], q[3]) : 0.f;
+    v[4] = four ? t0 : 0.f;
+    v[5] = four ? t1 : 0.f;
+    v[6] = four ? t2 : 0.f;
+    v[7] = 0.f;
 }
 
+// (VEC: whole vectors on their bytes)
 template <bool F32, bool VEC, bool STREAM = false> __device__ __forceinline__ void store8(void* base, int64_t at, int left, const float (&v)[8])
 {
     if constexpr (VEC) {
         store_vec<F32, 8, STREAM>(base, at, v);
-    } else if (left >= 8) {
+        return;
+    }
+    char* dst = static_cast<char*>(base) + at * (F32 ? 4 : 2);
+    constexpr int B = F32 ? 4 : 2;
+    auto quad = [](char* to, float a, float b, float c, float d) {
+        if constexpr (F32) *reinterpret_cast<words4_any*>(to) = (words4){__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)};
+        else               *reinterpret_cast<words2_any*>(to) = (words2){bf16_pair(a, b), bf16_pair(c, d)};
+    };
+    if (left >= 8) {
         if constexpr (F32) {
-            words4_any* p = reinterpret_cast<words4_any*>(static_cast<float*>(base) + at);
-            p[0] = (words4){__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-            p[1] = (words4){__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+            quad(dst, v[0], v[1], v[2], v[3]);
+            quad(dst + 16, v[4], v[5], v[6], v[7]);
         } else {
-            *reinterpret_cast<words4_any*>(static_cast<uint16_t*>(base) + at) =
-                (words4){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+            *reinterpret_cast<words4_any*>(dst) = (words4){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < left) {
-                if (F32) static_cast<float*>(base)[at + i] = v[i];
-                else     static_cast<uint16_t*>(base)[at + i] = (uint16_t)f32_to_bf16_bits(v[i]);
-            }
+        return;
+    }
+    const bool four = left & 4, two = left & 2;
+    // (a choice between values; between elements it would be one of addresses, and the array would go to memory)
+    const float v0 = v[0], v1 = v[1], v2 = v[2], v4 = v[4], v5 = v[5], v6 = v[6];
+    const float p0 = four ? v4 : v0, p1 = four ? v5 : v1, last = four ? (two ? v6 : v4) : (two ? v2 : v0);
+    if (four) quad(dst, v[0], v[1], v[2], v[3]);
+    if (two) {
+        if constexpr (F32) *reinterpret_cast<words2_any*>(dst + (left & 4) * B) = (words2){__float_as_uint(p0), __float_as_uint(p1)};
+        else               *reinterpret_cast<word_any*>(dst + (left & 4) * B) = bf16_pair(p0, p1);
+    }
+    if (left & 1) {
+        if constexpr (F32) *reinterpret_cast<word_any*>(dst + (left & 6) * B) = __float_as_uint(last);
+        else               *reinterpret_cast<half_any*>(dst + (left & 6) * B) = (uint16_t)f32_to_bf16_bits(last);
     }
 }
 

@@ -12,6 +12,8 @@ namespace {
 // Memory bound: 32768 x 4096 bf16 with residual and codes moves 940 MB in 159 us (5.9 TB/s).  Wide rows take 512 threads
 // with one vector each: with 256, 128, 64 threads and 2, 4, 8 vectors it was 4, 9, 25 % slower, and 3.6, 5.4, 8.5 us
 // against 3.1 for 64 tokens, whose time is the launch and two dependent steps (load, sum).
+// Rows on no 16 bytes, or of a width that is no multiple of 8 (VEC = false): 32768 x 4095 in 232 us, 6517 x 3443 in 38 (with one
+// value per access 574 and 94).
 template <bool F32, int TPR, int NV, bool VEC, bool NORM, bool STREAM>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormParams p)
 {
@@ -24,12 +26,17 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormPar
 
     float v[NV][8], w[NV][8];
     float sum = 0.f;
-    // whole vectors: everything is asked for before the first wait, threads past the end take the last vector
-    RawVec<F32, 8> x_raw[VEC ? NV : 1], r_raw[VEC ? NV : 1], w_raw[VEC ? NV : 1];
-    if constexpr (VEC) {
+    // Everything is asked for before the first wait; threads past the end, and the one whose vector is cut short, take the
+    // row's last eight values (the latter gets its own below).
+    RawVec<F32, 8> x_raw[NV], r_raw[NV], w_raw[NV];
+    if (VEC || p.D >= 8) {
         auto ask = [&](const void* base, int64_t at, auto& raw) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) raw[i] = raw_vec<F32, 8>(base, at + min((i * TPR + t) * 8, p.D - 8));
+            for (int i = 0; i < NV; ++i) {
+                const int64_t from = at + min((i * TPR + t) * 8, p.D - 8);
+                if constexpr (VEC) raw[i] = raw_vec<F32, 8>(base, from);
+                else               raw[i] = raw8_any<F32>(base, from);
+            }
         };
         ask(p.x, row * p.x_pitch, x_raw);
         if (NORM && p.residual) ask(p.residual, row * p.D, r_raw);
@@ -41,20 +48,20 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormPar
         const int c = (i * TPR + t) * 8;
 #pragma unroll
         for (int k = 0; k < 8; ++k) { v[i][k] = 0.f; w[i][k] = 1.f; }
-        if (c < p.D) {
-            if constexpr (VEC) values_of<F32, 8>(x_raw[i], v[i]);
-            else               load8<F32>(p.x, row * p.x_pitch + c, p.D - c, v[i]);
-            if (NORM && p.residual) {
-                float r[8];
-                if constexpr (VEC) values_of<F32, 8>(r_raw[i], r);
-                else               load8<F32>(p.residual, row * p.D + c, p.D - c, r);
+        const bool whole = VEC ? c < p.D : c + 8 <= p.D;
+        float r[8];
+        if (whole) {
+            values_of<F32, 8>(x_raw[i], v[i]);
+            if (NORM && p.residual) values_of<F32, 8>(r_raw[i], r);
+            if (NORM && p.weight) values_of<F32, 8>(w_raw[i], w[i]);
+        } else if (!VEC && c < p.D) {
+            load_few<F32>(p.x, row * p.x_pitch + c, p.D - c, v[i]);
+            if (NORM && p.residual) load_few<F32>(p.residual, row * p.D + c, p.D - c, r);
+            if (NORM && p.weight) load_few<F32>(p.weight, c, p.D - c, w[i]);
+        }
+        if (NORM && p.residual && c < p.D) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[i][k] += r[k];
-            }
-            if (NORM && p.weight) {
-                if constexpr (VEC) values_of<F32, 8>(w_raw[i], w[i]);
-                else               load8<F32>(p.weight, c, p.D - c, w[i]);
-            }
+            for (int k = 0; k < 8; ++k) v[i][k] += r[k];
         }
         if (NORM) {
 #pragma unroll
@@ -101,12 +108,16 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormPar
         uint8_t* dst = p.codes + row * p.D + c;
         if constexpr (VEC) {
             put_words<STREAM>(dst, (words2){lo, hi});
-        } else if (p.D - c >= 8) {
-            *reinterpret_cast<words2_any*>(dst) = (words2){lo, hi};
         } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (c + k < p.D) dst[k] = (uint8_t)((k < 4 ? lo : hi) >> (8 * (k & 3)));
+            const int left = p.D - c;
+            const uint64_t all = (uint64_t)hi << 32 | lo;
+            if (left >= 8) {
+                *reinterpret_cast<words2_any*>(dst) = (words2){lo, hi};
+            } else {
+                if (left & 4) *reinterpret_cast<word_any*>(dst) = lo;
+                if (left & 2) *reinterpret_cast<half_any*>(dst + (left & 4)) = (uint16_t)(all >> 8 * (left & 4));
+                if (left & 1) dst[left & 6] = (uint8_t)(all >> 8 * (left & 6));
+            }
         }
     }
 }
