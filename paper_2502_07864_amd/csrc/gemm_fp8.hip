@@ -359,9 +359,9 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
     }
 
     // Outputs: lane (h, n) holds outputs 8 r + 4 h .. + 3 of every 32, of token n.  Through LDS they leave in whole
-    // lines: stored as they lie (8 bytes per token and lane) they took 10 % of the product of 32768 tokens.
+    // lines: stored as they lie (8 bytes per token and lane) they took 10 % of the product of 32768 tokens.  16 bytes at
+    // any address: rows of odd widths lie on two.
     __syncthreads();
-    const bool wide = p.N % (F32 || SPLIT ? 4 : 8) == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
     LDS_AS unsigned char* mine = lds + wave * 32 * PITCH;
     constexpr bool O32 = F32 || SPLIT;
     constexpr int COLS = O32 ? 64 : 32 * NI, PARTS = 32 * NI / COLS;             // outputs per pass
@@ -387,8 +387,8 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
                 const u32x4 v = *(LDS_AS u32x4*)(mine + t * PITCH + lane % LANES * 16);
                 if (m >= p.M || c >= p.N) continue;
                 const int64_t o = (int64_t)m * p.N + c;
-                if (wide) {
-                    put_words<STREAM>(static_cast<unsigned char*>(out) + o * (O32 ? 4 : 2), v);
+                if (c + PER <= p.N) {
+                    put_words_any<STREAM>(static_cast<unsigned char*>(out) + o * (O32 ? 4 : 2), v);
                 } else {
 #pragma unroll
                     for (int e = 0; e < PER; ++e)
@@ -538,7 +538,6 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
     for (int r = 0; r < 4; ++r)
         *(LDS_AS f32x4*)(red + (wave * 32 + n) * PITCH + 8 * r + 4 * h) = (f32x4){acc[4 * r], acc[4 * r + 1], acc[4 * r + 2], acc[4 * r + 3]};
     __syncthreads();
-    const bool wide = p.N % 4 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
     for (int i = tid; i < W_ROWS * A_ROWS / 4; i += 512) {
         const int c = i % (W_ROWS / 4) * 4, t = i / (W_ROWS / 4);                          // four outputs of a token
         const LDS_AS float* at = red + ((t / 32 * WN + c / 32) * 32 + t % 32) * PITCH + c % 32;
@@ -548,9 +547,9 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
         const int m = m0 + t, col = n0 + c;
         if (m >= p.M || col >= p.N) continue;
         const int64_t o = (int64_t)m * p.N + col;
-        if (wide) {
-            if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + o) = v;
-            else               *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + o) = (u32x2){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+        if (col + 4 <= p.N) {
+            if constexpr (F32) *reinterpret_cast<words4_any*>(static_cast<float*>(p.out) + o) = __builtin_bit_cast(words4, v);
+            else               *reinterpret_cast<words2_any*>(static_cast<uint16_t*>(p.out) + o) = (words2){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)

@@ -118,6 +118,17 @@ template <bool STREAM, typename W> __device__ __forceinline__ void put_words(voi
     else                  *static_cast<W*>(dst) = w;
 }
 
+// accesses at any address of a value (the hardware takes them apart where they cross a line)
+typedef words4 __attribute__((aligned(2))) words4_any;
+typedef words2 __attribute__((aligned(1))) words2_any;
+typedef uint32_t __attribute__((aligned(1))) word_any;
+typedef uint16_t __attribute__((aligned(1))) half_any;
+template <bool STREAM> __device__ __forceinline__ void put_words_any(void* dst, words4 w)
+{
+    if constexpr (STREAM) __builtin_nontemporal_store(w, static_cast<words4_any*>(dst));
+    else                  *static_cast<words4_any*>(dst) = w;
+}
+
 template <bool F32, int V, bool STREAM = false> __device__ __forceinline__ void store_vec(void* base, int64_t at, const float (&v)[V])
 {
     if constexpr (F32) {
@@ -132,12 +143,7 @@ template <bool F32, int V, bool STREAM = false> __device__ __forceinline__ void 
     }
 }
 
-// Eight consecutive values at any address of the type: 16-byte accesses all the same (the hardware takes them apart where they
-// cross a line).  Fewer than eight, `left`: four, two and one of them, as its bits say.
-typedef words4 __attribute__((aligned(2))) words4_any;
-typedef words2 __attribute__((aligned(1))) words2_any;
-typedef uint32_t __attribute__((aligned(1))) word_any;
-typedef uint16_t __attribute__((aligned(1))) half_any;
+// Eight consecutive values at any address of the type.  Fewer than eight, `left`: four, two and one of them, as its bits say.
 template <bool F32> __device__ __forceinline__ RawVec<F32, 8> raw8_any(const void* base, int64_t at)
 {
     RawVec<F32, 8> r;
