@@ -64,6 +64,32 @@ __device__ __forceinline__ f32x16 products(const Wide& w, const Wide& a, const f
     return s;
 }
 
+// Which tile a workgroup takes.  Workgroups whose ids are equal mod 8 run on one XCD, whose L2 its tiles' operands pass
+// through: the XCDs share out the tiles as `across` x 8 / `across` rectangles of rows x columns tiles, as square as they go.
+// (Tiles in a row instead, all tokens of some outputs on an XCD: 2000 x 320 x 7168 in tiles of 64 x 32 28.2 us, so 20.5;
+// 1179 x 576 x 5120 19.4 and 17.0; no difference where the tiles are few.)  Where rectangles would take one more round of an
+// XCD's 32 CUs, the tiles are in a row all the same: `columns` an XCD (log_across < 0), rows = the tiles down the tokens.
+struct Layout {
+    int log_across, rows, columns;
+    float inv_rows;
+    // false, or m and n past the tiles: nothing to do
+    __device__ __forceinline__ bool at(int id, int& m, int& n) const
+    {
+        const int x = id & 7, s = id >> 3;
+        if (log_across < 0) {
+            const int lin = x * columns + s;
+            n = lin / rows;
+            m = lin - n * rows;
+            return s < columns;
+        }
+        const int column = __builtin_amdgcn_readfirstlane((int)(((float)s + 0.5f) * inv_rows));      // s / rows (s < 2^21)
+        m = (x & ((1 << log_across) - 1)) * rows + s - column * rows;
+        n = (x >> log_across) * columns + column;
+        return column < columns;
+    }
+    int workgroups() const { return 8 * columns * (log_across < 0 ? 1 : rows); }
+};
+
 // workgroup barrier over which the compiler moves no access to memory (waits are placed by hand)
 __device__ __forceinline__ void barrier()
 {
@@ -410,7 +436,7 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
 // kernel, KS at a time.  What bounds it: 64 bytes a cycle into a CU, the launch and one round trip to memory where a
 // wavefront has few blocks (61 x 3584 x 3584: 6.7 us; 1024 x 576 x 4096 on codes: 10.4).
 template <int WN, int WM, int KS, int STAGES, bool FAST, bool F32>
-__global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p, int tiles_m)
+__global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p, Layout tiles)
 {
     static_assert(WN * WM * KS == 8);
     constexpr int W_ROWS = 32 * WN, A_ROWS = 32 * WM, GROUPS = (W_ROWS + A_ROWS) / 8;      // groups of 8 rows of a block
@@ -427,10 +453,11 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int total = tiles_m * ((p.N + W_ROWS - 1) / W_ROWS), per = (total + 7) / 8;
-    const int lin = (blockIdx.x & 7) * per + (blockIdx.x >> 3);                            // consecutive tiles on one XCD
-    if (lin >= total) return;
-    const int m0 = lin % tiles_m * A_ROWS, n0 = lin / tiles_m * W_ROWS;
+    int m0, n0;
+    const bool there = tiles.at(blockIdx.x, m0, n0);
+    m0 *= A_ROWS;
+    n0 *= W_ROWS;
+    if (!there || m0 >= p.M || n0 >= p.N) return;
     const int blocks = (p.K + QBLOCK - 1) / QBLOCK, steps = (blocks + KS - 1) / KS;
 
     // Group G = 8 i + wave of a stage: block G / GROUPS of it, rows of w, then rows of a.  Rows past the end repeat the last
@@ -584,8 +611,8 @@ struct Plan {
 // The form that a model of the times finds fastest: a launch, and per round of 256 workgroups (each fills its CU) the steps over
 // K, and 1 us from a round to the next, or the time that the operands take from memory.  us per step measured with few
 // workgroups, on codes (fast) and on f16; the fuller the rounds, the longer the steps, for power and the caches' rates
-// (`crowded`: all CUs).  On 280 sizes of 17 to 32768 tokens and ten (N, K), with each kind of sums, the choice takes 0.3 %
-// longer than the best form on average, 11 % at the most.
+// (`crowded`: all CUs).  On 280 sizes of 17 to 32768 tokens and ten (N, K), with each kind of sums, the choice takes 0.5 %
+// longer than the best form on average, 14 % at the most.
 Plan one_launch(int M, int N, int K, bool fast)
 {
     const int blocks = (K + QBLOCK - 1) / QBLOCK;
@@ -643,16 +670,32 @@ template <int NT, int WAVES, int U> void launch_rows(const GemmFp8Params& p, boo
     else     gemm_rows_kernel<NT, WAVES, U, false><<<grid, block, 0, s>>>(p);
 }
 
+// The rectangles with the fewest rows of operands, of those that take no more rounds than tiles in a row
+Layout layout_of(int tiles_m, int tiles_n, int tokens, int outputs)
+{
+    const long per = ((long)tiles_m * tiles_n + 7) / 8, rounds = (per + 31) / 32;
+    Layout best = {-1, tiles_m, (int)per, 0.f};
+    long best_rows = 0;
+    for (int l = 0; l <= 3; ++l) {
+        const int across = 1 << l, down = 8 >> l, rows = (tiles_m + across - 1) / across, columns = (tiles_n + down - 1) / down;
+        const long size = (long)rows * tokens + (long)columns * outputs;
+        if (((long)rows * columns + 31) / 32 > rounds || (best.log_across >= 0 && size >= best_rows)) continue;
+        best = {l, rows, columns, 1.f / (float)rows};
+        best_rows = size;
+    }
+    return best;
+}
+
 template <int WN, int WM, int KS, int STAGES> void launch_small_tiles(const GemmFp8Params& p, bool f32, bool fast, hipStream_t s)
 {
-    const int tm = (p.M + 32 * WM - 1) / (32 * WM), tn = (p.N + 32 * WN - 1) / (32 * WN);
-    const dim3 grid((unsigned)(((long)tm * tn + 7) / 8 * 8)), block(512);
+    const Layout tiles = layout_of((p.M + 32 * WM - 1) / (32 * WM), (p.N + 32 * WN - 1) / (32 * WN), 32 * WM, 32 * WN);
+    const dim3 grid((unsigned)tiles.workgroups()), block(512);
     if (fast) {
-        if (f32) gemm_small_tile_kernel<WN, WM, KS, STAGES, true, true><<<grid, block, 0, s>>>(p, tm);
-        else     gemm_small_tile_kernel<WN, WM, KS, STAGES, true, false><<<grid, block, 0, s>>>(p, tm);
+        if (f32) gemm_small_tile_kernel<WN, WM, KS, STAGES, true, true><<<grid, block, 0, s>>>(p, tiles);
+        else     gemm_small_tile_kernel<WN, WM, KS, STAGES, true, false><<<grid, block, 0, s>>>(p, tiles);
     } else {
-        if (f32) gemm_small_tile_kernel<WN, WM, KS, STAGES, false, true><<<grid, block, 0, s>>>(p, tm);
-        else     gemm_small_tile_kernel<WN, WM, KS, STAGES, false, false><<<grid, block, 0, s>>>(p, tm);
+        if (f32) gemm_small_tile_kernel<WN, WM, KS, STAGES, false, true><<<grid, block, 0, s>>>(p, tiles);
+        else     gemm_small_tile_kernel<WN, WM, KS, STAGES, false, false><<<grid, block, 0, s>>>(p, tiles);
     }
 }
 
