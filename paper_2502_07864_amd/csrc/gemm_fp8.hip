@@ -106,28 +106,26 @@ template <bool F32> __device__ __forceinline__ void put(void* out, int64_t at, f
 
 // ---------------------------------------------------------------- few tokens
 
-// A workgroup takes 16 NT outputs of up to 16 tokens over the whole depth, its wavefronts share out the blocks: what
+// A workgroup takes 16 outputs of up to 16 tokens over the whole depth, its wavefronts share out the blocks: what
 // bounds it is reading the weights once, and with every block of a wavefront on its way at once that is one round trip.
-// The partial sums meet in LDS and are added in the wavefronts' order.  One token by 6144 x 4096: 7.0 us, 3.6 TB/s (25 MB; a
-// launch of nothing takes 1.6).
-template <int NT, int WAVES, int U, bool F32>
+// The partial sums meet in LDS and are added in the wavefronts' order.  One token by 3584 x 3584: 4.5 us, 2.9 TB/s (13 MB; a
+// launch of nothing takes 1.6); 16 tokens by 576 x 4096: 5.6.
+template <int WAVES, int U, bool F32>
 __global__ __launch_bounds__(WAVES * 64) void gemm_rows_kernel(GemmFp8Params p)
 {
-    __shared__ __attribute__((aligned(16))) float red[WAVES][NT][256];
+    __shared__ __attribute__((aligned(16))) float red[WAVES][256];
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n0 = blockIdx.x * 16 * NT;
+    const int n0 = blockIdx.x * 16;
     const int blocks = (p.K + QBLOCK - 1) / QBLOCK;
-    const uint8_t* w[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) w[t] = p.w + (int64_t)min(n0 + t * 16 + n, p.N - 1) * p.K + 16 * g;
+    const uint8_t* w = p.w + (int64_t)min(n0 + n, p.N - 1) * p.K + 16 * g;
     const float* ws = p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
     const uint8_t* a = p.a + (int64_t)min(n, p.M - 1) * p.K + 16 * g;
     const float* as = p.a_scales + min(n, p.M - 1);
-    f32x4 acc[NT] = {};
+    f32x4 acc = {};
     const u32x4 zero = {0u, 0u, 0u, 0u};
     for (int b0 = wave; b0 < blocks; b0 += WAVES * U) {
-        u32x4 wv[U][NT][2], av[U][2];
+        u32x4 wv[U][2], av[U][2];
         float f[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -135,11 +133,8 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_rows_kernel(GemmFp8Params p)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {              // the pieces at columns 16 g and 64 + 16 g
                 const bool in = k + 64 * i + 16 * g < p.K;
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    wv[u][t][i] = zero;
-                    if (in) wv[u][t][i] = *reinterpret_cast<const u32x4*>(w[t] + k + 64 * i);
-                }
+                wv[u][i] = zero;
+                if (in) wv[u][i] = *reinterpret_cast<const u32x4*>(w + k + 64 * i);
                 av[u][i] = zero;
                 if (in) av[u][i] = *reinterpret_cast<const u32x4*>(a + k + 64 * i);
             }
@@ -151,25 +146,21 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_rows_kernel(GemmFp8Params p)
             f16x8 ah[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) ah[q] = widen8((int)av[u][q >> 1][2 * (q & 1)], (int)av[u][q >> 1][2 * (q & 1) + 1]);
+            f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                f32x4 s = {0.f, 0.f, 0.f, 0.f};
+            for (int q = 0; q < 4; ++q)
+                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8((int)wv[u][q >> 1][2 * (q & 1)], (int)wv[u][q >> 1][2 * (q & 1) + 1]), ah[q], s, 0, 0, 0);
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    s = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8((int)wv[u][t][q >> 1][2 * (q & 1)], (int)wv[u][t][q >> 1][2 * (q & 1) + 1]), ah[q], s, 0, 0, 0);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[t][j] += s[j] * f[u];
-            }
+            for (int j = 0; j < 4; ++j) acc[j] += s[j] * f[u];
         }
     }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(&red[wave][t][n * 16 + 4 * g]) = acc[t];
+    *reinterpret_cast<f32x4*>(&red[wave][n * 16 + 4 * g]) = acc;
     __syncthreads();
-    for (int i = tid; i < NT * 256; i += WAVES * 64) {
-        const int m = (i & 255) >> 4, c = n0 + (i >> 8) * 16 + (i & 15);
+    if (tid < 256) {
+        const int m = tid >> 4, c = n0 + (tid & 15);
         float v = 0.f;
 #pragma unroll
-        for (int q = 0; q < WAVES; ++q) v += red[q][i >> 8][i & 255];
+        for (int q = 0; q < WAVES; ++q) v += red[q][tid];
         if (m < p.M && c < p.N) put<F32>(p.out, (int64_t)m * p.N + c, v);
     }
 }
@@ -430,27 +421,26 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
 
 // ---------------------------------------------------------------- in between
 
-// A workgroup of eight wavefronts computes 32 WN outputs of 32 WM tokens; a wavefront 32 x 32 of them over every KS-th
-// block, so that small tiles still keep eight wavefronts.  Up to a few hundred tokens, and for few outputs, small tiles over
-// the whole depth beat large ones over shares of it, whose partial sums go through memory.  Blocks travel as in the tile
-// kernel, KS at a time.  What bounds it: 64 bytes a cycle into a CU, the launch and one round trip to memory where a
-// wavefront has few blocks (61 x 3584 x 3584: 6.7 us; 1024 x 576 x 4096 on codes: 10.4).
-template <int WN, int WM, int KS, int STAGES, bool FAST, bool F32>
-__global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p, Layout tiles)
+// A workgroup of eight wavefronts computes 32 NI outputs of 32 MT tokens, each wavefront all of them over every eighth block:
+// what a wavefront reads from LDS it has brought there itself, in buffers of its own, so that it waits for nobody until the
+// sums meet.  Up to a few hundred tokens, and for few outputs, such tiles over the whole depth beat large ones over shares
+// of it, whose partial sums go through memory.
+//
+// What bounds it: what passes through LDS, 128 bytes a cycle read and written (64 come in), then the L2s and what is behind
+// them where many CUs read; the launch and one round trip where a wavefront has few blocks.  Wavefronts of 32 x 32 that share
+// the blocks of a 64 x 64 tile read each byte twice and meet at a barrier every step: 256 x 3584 x 3584 10.3 us on codes and
+// 13.0 on f16, so 9.3 and 10.6; 61 x 3584 x 3584 6.7, so 5.7 (two buffers a wavefront, one for the larger tiles);
+// 1024 x 576 x 4096 10.2, so 9.7.
+template <int NI, int MT, int STAGES, bool FAST, bool F32>
+__global__ __launch_bounds__(512, 2) void gemm_wave_tile_kernel(GemmFp8Params p, Layout tiles)
 {
-    static_assert(WN * WM * KS == 8);
-    constexpr int W_ROWS = 32 * WN, A_ROWS = 32 * WM, GROUPS = (W_ROWS + A_ROWS) / 8;      // groups of 8 rows of a block
-    constexpr int CODES = KS * GROUPS, LOADS = CODES / 8 + 1;                              // loads of a stage, per wavefront
-    constexpr int BLOCK_B = (W_ROWS + A_ROWS) * QBLOCK, STAGE = KS * BLOCK_B + 2048;
-    constexpr int PITCH = 36;                                                              // floats per token of 32 outputs
-    // One wavefront of each SIMD asks for the next blocks between its two products, the other behind them: the loads have no
-    // pause then.  3 - 8 % of the time of tiles of 32 x 32 and 64 x 32, 2 % of 64 x 64 on codes (all before the products, or half
-    // of each wavefront's: less), but 64 x 64 on f16 and 128 x 64 lose 10 %.
-    constexpr bool APART = KS >= (FAST ? 2 : 4);
-    static_assert(CODES % 8 == 0 && KS * A_ROWS <= 256 && STAGES * STAGE <= 160 * 1024 && 8 * 32 * PITCH * 4 <= STAGES * STAGE);
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[STAGES * STAGE];
+    constexpr int W_ROWS = 32 * NI, A_ROWS = 32 * MT, GROUPS = (W_ROWS + A_ROWS) / 8, LOADS = GROUPS + 1;
+    constexpr int BLOCK_B = (W_ROWS + A_ROWS) * QBLOCK, STAGE = BLOCK_B + 256;
+    constexpr int PITCH = W_ROWS + 4;                                                      // floats per token
+    constexpr int LDS_B = std::max(8 * STAGES * STAGE, 8 * A_ROWS * PITCH * 4);
+    static_assert(STAGES <= 2 && MT <= 2 && LDS_B <= 160 * 1024);
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[LDS_B];
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int m0, n0;
@@ -458,119 +448,100 @@ __global__ __launch_bounds__(512, 2) void gemm_small_tile_kernel(GemmFp8Params p
     m0 *= A_ROWS;
     n0 *= W_ROWS;
     if (!there || m0 >= p.M || n0 >= p.N) return;
-    const int blocks = (p.K + QBLOCK - 1) / QBLOCK, steps = (blocks + KS - 1) / KS;
+    const int blocks = (p.K + QBLOCK - 1) / QBLOCK;
+    const uint32_t mine = (uint32_t)(uintptr_t)lds + wave * STAGES * STAGE;
 
-    // Group G = 8 i + wave of a stage: block G / GROUPS of it, rows of w, then rows of a.  Rows past the end repeat the last
-    const uint8_t* src[LOADS - 1];
-    uint32_t off[LOADS - 1], column[LOADS - 1];
-    int block_of[LOADS - 1];
+    // Load k of a block: rows 8 k .. + 7 of w, then of a; 16-byte piece c of a row lies at c ^ (row >> 1 & 7).  Rows past the end
+    // repeat the last
+    const uint32_t row = (uint32_t)(lane >> 3) * (uint32_t)p.K, even = ((lane & 7) ^ (lane >> 4)) * 16;
+    const uint32_t last_w = (uint32_t)min(W_ROWS - 1, p.N - 1 - n0) * (uint32_t)p.K, last_a = (uint32_t)min(A_ROWS - 1, p.M - 1 - m0) * (uint32_t)p.K;
+    const uint8_t* w0 = p.w + (int64_t)n0 * p.K;
+    const uint8_t* a0 = p.a + (int64_t)m0 * p.K;
+    const float* as = p.a_scales + min(m0 + lane, p.M - 1);
+    const float* ws = p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
+    auto request = [&](int b, uint32_t stage) {
+        const int64_t at = (int64_t)b * QBLOCK;
+        const bool whole = at + QBLOCK <= p.K;
 #pragma unroll
-    for (int i = 0; i < LOADS - 1; ++i) {
-        const int G = i * 8 + wave, ks = G / GROUPS, r = (G % GROUPS) * 8;
-        const bool W = r < W_ROWS;
-        const int row = (W ? r : r - W_ROWS) + (lane >> 3);
-        column[i] = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
-        src[i] = W ? p.w + (int64_t)n0 * p.K : p.a + (int64_t)m0 * p.K;
-        off[i] = (uint32_t)min(row, W ? p.N - 1 - n0 : p.M - 1 - m0) * (uint32_t)p.K + column[i];
-        block_of[i] = ks;
-    }
-    const int si = wave * 64 + lane;                   // wavefronts below 4 bring the tokens' scales, the others the weights'
-    const bool tokens = si < KS * A_ROWS;
-    const int s_block = tokens ? si / A_ROWS : lane % KS;
-    const float* s_src = tokens ? p.a_scales + min(m0 + si % A_ROWS, p.M - 1) : p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
-    const int64_t s_step = tokens ? p.scale_pitch : 1;
-    auto request = [&](int step, uint32_t stage) {
-        const int b0 = step * KS;
-        if ((b0 + KS) * QBLOCK <= p.K) {
-#pragma unroll
-            for (int i = 0; i < LOADS - 1; ++i) {
-                const uint32_t dst = lds0 + stage + (i * 8 + wave) * 1024;
-                const uint8_t* from = src[i] + (int64_t)(b0 + block_of[i]) * QBLOCK;
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off[i]), "s"(from) : "memory");
-            }
-        } else {                                       // columns at and past K are zeros
-#pragma unroll
-            for (int i = 0; i < LOADS - 1; ++i) {
-                const uint32_t dst = lds0 + stage + (i * 8 + wave) * 1024;
-                const int64_t k = (int64_t)(b0 + block_of[i]) * QBLOCK;
-                const uint8_t* from = k + column[i] < p.K ? src[i] + k + off[i] : reinterpret_cast<const uint8_t*>(zeros16);
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(dst), "v"(from) : "memory");
+        for (int k = 0; k < GROUPS; ++k) {
+            const bool W = k < W_ROWS / 8;
+            const uint32_t piece = even ^ (k & 1) * 64, off = min(row + (uint32_t)(W ? k : k - W_ROWS / 8) * 8 * (uint32_t)p.K, W ? last_w : last_a) + piece;
+            const uint8_t* from = (W ? w0 : a0) + at;
+            const uint32_t dst = mine + stage + k * 1024;
+            if (whole) {
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off), "s"(from) : "memory");
+            } else {                                   // columns at and past K are zeros
+                const uint8_t* src = at + piece < p.K ? from + off : reinterpret_cast<const uint8_t*>(zeros16);
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(dst), "v"(src) : "memory");
             }
         }
-        const float* from = s_src + (int64_t)min(b0 + s_block, blocks - 1) * s_step;
-        const uint32_t dst = lds0 + stage + KS * BLOCK_B + wave * 256;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(dst), "v"(from) : "memory");
+        const float* src = as + b * p.scale_pitch;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(mine + stage + BLOCK_B), "v"(src) : "memory");
     };
 
-    const int wn = wave % WN, wm = wave / WN % WM, ks = wave / (WN * WM), key = (n >> 1) & 7;
-    const uint32_t w_row = ks * BLOCK_B + (wn * 32 + n) * QBLOCK, a_row = ks * BLOCK_B + (W_ROWS + wm * 32 + n) * QBLOCK;
-    struct Operands { i32x8 w[2], a[2]; float sa, sw; };
-    auto read = [&](uint32_t stage) {
-        LDS_AS unsigned char* st = lds + stage;
-        Operands o;
+    f32x16 acc[NI][MT] = {};
+#pragma unroll
+    for (int st = 0; st < STAGES; ++st)
+        if (wave + 8 * st < blocks) request(wave + 8 * st, st * STAGE);
+    uint32_t cur = 0;
+    const int key = (n >> 1) & 7;
+    LDS_AS unsigned char* own = lds + wave * STAGES * STAGE;
+    for (int b = wave; b < blocks; b += 8) {
+        const float sw = ws[b];
+        if (STAGES == 2 && b + 8 < blocks) wait_vmcnt<LOADS>();
+        else                               wait_vmcnt<0>();
+        asm volatile("" ::: "memory");
+        i32x8 wv[NI][2], av[MT][2];
+        float sa[MT];
+        LDS_AS unsigned char* st = own + cur;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             const uint32_t lo = ((4 * q + h) ^ key) * 16, hi = ((4 * q + 2 + h) ^ key) * 16;
-            o.w[q] = __builtin_shufflevector(*(LDS_AS i32x4*)(st + w_row + lo), *(LDS_AS i32x4*)(st + w_row + hi), 0, 1, 2, 3, 4, 5, 6, 7);
-            o.a[q] = __builtin_shufflevector(*(LDS_AS i32x4*)(st + a_row + lo), *(LDS_AS i32x4*)(st + a_row + hi), 0, 1, 2, 3, 4, 5, 6, 7);
+            auto half = [&](int r) {
+                LDS_AS unsigned char* at = st + (r * 32 + n) * QBLOCK;
+                return __builtin_shufflevector(*(LDS_AS i32x4*)(at + lo), *(LDS_AS i32x4*)(at + hi), 0, 1, 2, 3, 4, 5, 6, 7);
+            };
+#pragma unroll
+            for (int i = 0; i < NI; ++i) wv[i][q] = half(i);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) av[j][q] = half(NI + j);
         }
-        o.sa = *(LDS_AS float*)(st + KS * BLOCK_B + (ks * A_ROWS + wm * 32 + n) * 4);
-        o.sw = *(LDS_AS float*)(st + KS * BLOCK_B + (KS * A_ROWS + 63) / 64 * 256 + ks * 4);
-        return o;
-    };
-
-    f32x16 acc = {};
 #pragma unroll
-    for (int st = 0; st < STAGES; ++st)
-        if (st < steps) request(st, st * STAGE);
-    if (STAGES <= steps) wait_vmcnt<(STAGES - 1) * LOADS>();
-    else                 wait_vmcnt<0>();
-    barrier();
-    Operands now = read(0);
-    uint32_t cur = 0;
-    auto step = [&](int st, auto more_constant) {      // more: the stage that takes this one's place is asked for
-        constexpr bool MORE = decltype(more_constant)::value;
-        const uint32_t next = cur + STAGE == STAGES * STAGE ? 0u : cur + STAGE;
-        // this stage is in everybody's registers, the next one has landed
-        if (MORE || st + STAGES == steps) wait_vmcnt<(STAGES - 2) * LOADS>();
-        else                              wait_vmcnt<0>();
-        __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0)
-        barrier();
-        // the products first: while they run the wavefront asks for what comes next, and stands while that is accepted
-        f32x16 s = products<FAST>(now.w[0], now.a[0], (f32x16){});
+        for (int j = 0; j < MT; ++j) sa[j] = *(LDS_AS float*)(st + BLOCK_B + (j * 32 + n) * 4);
+        __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): the block is in registers, the next may take its place
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (MORE && APART) { if (wave < 4) request(st + STAGES, cur); }
+        if (b + 8 * STAGES < blocks) request(b + 8 * STAGES, cur);
         __builtin_amdgcn_sched_barrier(0);
-        const Operands then = read(next);
-        __builtin_amdgcn_sched_barrier(0);
-        s = products<FAST>(now.w[1], now.a[1], s);
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (MORE) { if (!APART || wave >= 4) request(st + STAGES, cur); }
-        __builtin_amdgcn_sched_barrier(0);
-        // (a block past the end is zeros, but its scale need not be finite)
-        const float f = st * KS + ks < blocks ? now.sa * now.sw : 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[e] += s[e] * f;
-        now = then;
-        cur = next;
-    };
-    int st = 0;
-    for (; st + STAGES < steps; ++st) step(st, std::true_type{});
-    for (; st < steps; ++st) step(st, std::false_type{});
-    wait_vmcnt<0>();
-    barrier();
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                const f32x16 s = products<FAST>(wv[i][1], av[j][1], products<FAST>(wv[i][0], av[j][0], (f32x16){}));
+                const float f = sa[j] * sw;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] += s[e] * f;
+            }
+        if (STAGES == 2) cur ^= STAGE;
+    }
+    __syncthreads();
     // sums of the wavefronts' blocks, in their order; [wave][token][output]
     LDS_AS float* red = (LDS_AS float*)lds;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-        *(LDS_AS f32x4*)(red + (wave * 32 + n) * PITCH + 8 * r + 4 * h) = (f32x4){acc[4 * r], acc[4 * r + 1], acc[4 * r + 2], acc[4 * r + 3]};
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                *(LDS_AS f32x4*)(red + (wave * A_ROWS + j * 32 + n) * PITCH + i * 32 + 8 * r + 4 * h) =
+                    (f32x4){acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]};
     __syncthreads();
     for (int i = tid; i < W_ROWS * A_ROWS / 4; i += 512) {
         const int c = i % (W_ROWS / 4) * 4, t = i / (W_ROWS / 4);                          // four outputs of a token
-        const LDS_AS float* at = red + ((t / 32 * WN + c / 32) * 32 + t % 32) * PITCH + c % 32;
+        const LDS_AS float* at = red + t * PITCH + c;
         f32x4 v = *(const LDS_AS f32x4*)at;
 #pragma unroll
-        for (int k = 1; k < KS; ++k) v += *(const LDS_AS f32x4*)(at + k * WN * WM * 32 * PITCH);
+        for (int k = 1; k < 8; ++k) v += *(const LDS_AS f32x4*)(at + k * A_ROWS * PITCH);
         const int m = m0 + t, col = n0 + c;
         if (m >= p.M || col >= p.N) continue;
         const int64_t o = (int64_t)m * p.N + col;
@@ -599,8 +570,8 @@ __global__ __launch_bounds__(256) void gemm_merge_kernel(GemmFp8Params p, int sp
 
 // ---------------------------------------------------------------- choice
 
-enum Form { ROWS16, ROWS32, SMALL_1x1, SMALL_1x2, SMALL_2x2, SMALL_2x4, TILE_128x128, TILE_256x128, TILE_256x256 };
-constexpr int TILE[][2] = {{16, 16}, {16, 32}, {32, 32}, {64, 32}, {64, 64}, {128, 64}, {128, 128}, {256, 128}, {256, 256}};      // tokens, outputs
+enum Form { ROWS, WAVE_32x32, WAVE_64x32, WAVE_64x64, TILE_128x128, TILE_256x128, TILE_256x256 };
+constexpr int TILE[][2] = {{16, 16}, {32, 32}, {64, 32}, {64, 64}, {128, 128}, {256, 128}, {256, 256}};      // tokens, outputs
 struct Plan {
     Form form;
     int splits;      // shares of K
@@ -608,34 +579,37 @@ struct Plan {
     float us;
 };
 
-// The form that a model of the times finds fastest: a launch, and per round of 256 workgroups (each fills its CU) the steps over
-// K, and 1 us from a round to the next, or the time that the operands take from memory.  us per step measured with few
-// workgroups, on codes (fast) and on f16; the fuller the rounds, the longer the steps, for power and the caches' rates
-// (`crowded`: all CUs).  On 280 sizes of 17 to 32768 tokens and ten (N, K), with each kind of sums, the choice takes 0.5 %
-// longer than the best form on average, 14 % at the most.
+// The form that a model of the times finds fastest: a launch, per round of 256 workgroups (each fills its CU) the steps over K,
+// and something from a round to the next; or the time that the operands take from memory.  us per step with few workgroups;
+// the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  Fitted to 280 sizes of 17 to
+// 32768 tokens and ten (N, K), with each kind of sums: the choice takes 0.2 % longer than the best form on average, 9 % at
+// the most.
 Plan one_launch(int M, int N, int K, bool fast)
 {
     const int blocks = (K + QBLOCK - 1) / QBLOCK;
-    if (M <= 16) return {(N + 15) / 16 <= 256 ? ROWS16 : ROWS32, 1, M, 4.f + (float)N * (float)K / 5.5e6f};     // 6144 x 4096, one token: 7.3 / 7.0 us; 3584 x 3584: 4.5 / 6.0
-    struct Shape { Form form; int blocks; float launch, step_fast, step_f16, crowded_fast, crowded_f16; };
+    // (one token by 3584 x 3584 4.5 us, 32 x 32 tiles 5.4; by 6144 x 4096, more workgroups than CUs, 7.5 and 6.9)
+    if (M <= 16 && (N + 15) / 16 <= 256) return {ROWS, 1, M, 4.f};
+    struct Times { float launch, step, crowded, round; };
+    struct Shape { Form form; int blocks; Times fast, f16; };
     static const Shape shapes[] = {
-        {SMALL_1x1, 8, 2.8f, 0.64f, 0.79f, 1.9f, 1.9f}, {SMALL_1x2, 4, 3.5f, 0.47f, 0.70f, 1.65f, 1.65f}, {SMALL_2x2, 2, 3.4f, 0.39f, 0.61f, 1.5f, 1.5f},
-        {SMALL_2x4, 1, 3.9f, 0.35f, 0.61f, 1.35f, 1.35f}, {TILE_128x128, 1, 3.4f, 0.37f, 0.75f, 1.5f, 1.4f},
-        {TILE_256x128, 1, 3.4f, 0.58f, 1.25f, 1.75f, 1.45f}, {TILE_256x256, 1, 4.4f, 1.00f, 0.f, 1.85f, 0.f}};
+        {WAVE_32x32, 8, {2.4f, 0.70f, 1.2f, 1.f}, {2.8f, 0.73f, 1.35f, 1.f}}, {WAVE_64x32, 8, {2.4f, 1.01f, 1.35f, 1.f}, {2.8f, 1.16f, 1.2f, 1.5f}},
+        {WAVE_64x64, 8, {3.2f, 1.46f, 1.2f, 2.f}, {3.6f, 1.85f, 1.2f, 2.f}}, {TILE_128x128, 1, {4.f, 0.326f, 1.65f, 2.f}, {4.f, 0.75f, 1.35f, 2.f}},
+        {TILE_256x128, 1, {4.4f, 0.557f, 1.65f, 2.f}, {4.4f, 1.2f, 1.5f, 2.f}}, {TILE_256x256, 1, {4.4f, 1.24f, 1.35f, 2.f}, {}}};
     Plan best = {TILE_256x128, 1, M, 3e38f};
     for (const Shape& f : shapes) {
         if (f.form == TILE_256x256 && !fast) continue;                   // (its registers are taken on f16)
+        const Times& t = fast ? f.fast : f.f16;
         const long tokens = TILE[f.form][0], outputs = TILE[f.form][1], tiles = ((M + tokens - 1) / tokens) * ((N + outputs - 1) / outputs);
         const int steps = (blocks + f.blocks - 1) / f.blocks;
         // shares of K, merged by a second launch
         for (int s = 1; s == 1 || (f.form == TILE_256x128 && s <= 8 && steps / s >= 4 && tiles * s <= 256); s *= 2) {
             const long rounds = (tiles * s + 255) / 256;
-            const float fill = (float)(tiles * s) / (float)(rounds * 256), crowded = fast ? f.crowded_fast : f.crowded_f16;
-            const float step = (fast ? f.step_fast : f.step_f16) * (1.f + (crowded - 1.f) * fill * fill);
+            const float fill = (float)(tiles * s) / (float)(rounds * 256);
+            const float step = t.step * (1.f + (t.crowded - 1.f) * fill * fill);
             const float memory = ((float)N + (float)M) * (float)K / 5.5e6f;
-            float t = f.launch + std::max(memory, (float)rounds * (float)((steps + s - 1) / s) * step + (float)(rounds - 1));
-            if (s > 1) t += 4.0f + (float)s * (float)M * (float)N * 8.f / 6e6f;      // (the partial sums, in the caches)
-            if (t < best.us) best = {f.form, s, M, t};
+            float us = t.launch + std::max(memory, (float)rounds * (float)((steps + s - 1) / s) * step + (float)(rounds - 1) * t.round);
+            if (s > 1) us += 4.0f + (float)s * (float)M * (float)N * 8.f / 6e6f;      // (the partial sums, in the caches)
+            if (us < best.us) best = {f.form, s, M, us};
         }
     }
     return best;
@@ -663,11 +637,11 @@ long workgroups(const Plan& plan, int N)
     return (long)((plan.tokens + t[0] - 1) / t[0]) * ((N + t[1] - 1) / t[1]) * plan.splits;
 }
 
-template <int NT, int WAVES, int U> void launch_rows(const GemmFp8Params& p, bool f32, hipStream_t s)
+template <int WAVES, int U> void launch_rows(const GemmFp8Params& p, bool f32, hipStream_t s)
 {
-    const dim3 grid((unsigned)((p.N + 16 * NT - 1) / (16 * NT))), block(WAVES * 64);
-    if (f32) gemm_rows_kernel<NT, WAVES, U, true><<<grid, block, 0, s>>>(p);
-    else     gemm_rows_kernel<NT, WAVES, U, false><<<grid, block, 0, s>>>(p);
+    const dim3 grid((unsigned)((p.N + 15) / 16)), block(WAVES * 64);
+    if (f32) gemm_rows_kernel<WAVES, U, true><<<grid, block, 0, s>>>(p);
+    else     gemm_rows_kernel<WAVES, U, false><<<grid, block, 0, s>>>(p);
 }
 
 // The rectangles with the fewest rows of operands, of those that take no more rounds than tiles in a row
@@ -686,16 +660,16 @@ Layout layout_of(int tiles_m, int tiles_n, int tokens, int outputs)
     return best;
 }
 
-template <int WN, int WM, int KS, int STAGES> void launch_small_tiles(const GemmFp8Params& p, bool f32, bool fast, hipStream_t s)
+template <int NI, int MT, int STAGES> void launch_wave_tiles(const GemmFp8Params& p, bool f32, bool fast, hipStream_t s)
 {
-    const Layout tiles = layout_of((p.M + 32 * WM - 1) / (32 * WM), (p.N + 32 * WN - 1) / (32 * WN), 32 * WM, 32 * WN);
+    const Layout tiles = layout_of((p.M + 32 * MT - 1) / (32 * MT), (p.N + 32 * NI - 1) / (32 * NI), 32 * MT, 32 * NI);
     const dim3 grid((unsigned)tiles.workgroups()), block(512);
     if (fast) {
-        if (f32) gemm_small_tile_kernel<WN, WM, KS, STAGES, true, true><<<grid, block, 0, s>>>(p, tiles);
-        else     gemm_small_tile_kernel<WN, WM, KS, STAGES, true, false><<<grid, block, 0, s>>>(p, tiles);
+        if (f32) gemm_wave_tile_kernel<NI, MT, STAGES, true, true><<<grid, block, 0, s>>>(p, tiles);
+        else     gemm_wave_tile_kernel<NI, MT, STAGES, true, false><<<grid, block, 0, s>>>(p, tiles);
     } else {
-        if (f32) gemm_small_tile_kernel<WN, WM, KS, STAGES, false, true><<<grid, block, 0, s>>>(p, tiles);
-        else     gemm_small_tile_kernel<WN, WM, KS, STAGES, false, false><<<grid, block, 0, s>>>(p, tiles);
+        if (f32) gemm_wave_tile_kernel<NI, MT, STAGES, false, true><<<grid, block, 0, s>>>(p, tiles);
+        else     gemm_wave_tile_kernel<NI, MT, STAGES, false, false><<<grid, block, 0, s>>>(p, tiles);
     }
 }
 
@@ -762,12 +736,10 @@ hipError_t launch_gemm_fp8(const GemmFp8Params& all, mla_dtype out, bool fast_su
         p.a_scales += before;
         p.out = static_cast<char*>(all.out) + (int64_t)before * all.N * (f32 ? 4 : 2);
         switch (plan.form) {
-            case ROWS16:    launch_rows<1, 16, 2>(p, f32, s); break;
-            case ROWS32:    launch_rows<2, 16, 2>(p, f32, s); break;
-            case SMALL_1x1: launch_small_tiles<1, 1, 8, 2>(p, f32, fast_sums, s); break;
-            case SMALL_1x2: launch_small_tiles<1, 2, 4, 3>(p, f32, fast_sums, s); break;
-            case SMALL_2x2: launch_small_tiles<2, 2, 2, 4>(p, f32, fast_sums, s); break;
-            case SMALL_2x4: launch_small_tiles<2, 4, 1, 6>(p, f32, fast_sums, s); break;
+            case ROWS:       launch_rows<16, 2>(p, f32, s); break;
+            case WAVE_32x32: launch_wave_tiles<1, 1, 2>(p, f32, fast_sums, s); break;
+            case WAVE_64x32: launch_wave_tiles<1, 2, 1>(p, f32, fast_sums, s); break;
+            case WAVE_64x64: launch_wave_tiles<2, 2, 1>(p, f32, fast_sums, s); break;
             case TILE_128x128:
                 if (fast_sums) launch_tiles<2, 1, 2, 3, true>(p, f32, 1, s);
                 else           launch_tiles<2, 1, 2, 3, false>(p, f32, 1, s);

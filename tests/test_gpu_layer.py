@@ -255,6 +255,20 @@ def test_gemm_few_outputs_of_many_tokens(M, N, K, fast):
 
 
 @pytest.mark.parametrize("fast", [False, True])
+@pytest.mark.parametrize("M, N, K", [(17, 33, 16), (32, 65, 1040), (33, 64, 1024), (64, 576, 4112), (61, 3585, 3600), (65, 2049, 144), (129, 1001, 2064), (300, 577, 7184),
+                                     (1179, 577, 5136), (2001, 321, 528), (16, 4112, 4096), (5, 7000, 272), (1, 5377, 1040)])
+def test_gemm_wavefront_tiles(M, N, K, fast):
+    """Tiles of which every wavefront takes every eighth block: fewer blocks than wavefronts, as many, more, a short one."""
+    test_gemm_forms(M, N, K, fast)
+
+
+@pytest.mark.parametrize("fast", [False, True])
+@pytest.mark.parametrize("M, N, K", [(1032, 1208, 9808), (2877, 171, 14352), (1031, 1601, 9824)])
+def test_gemm_shares_of_a_long_depth(M, N, K, fast):
+    test_gemm_forms(M, N, K, fast)
+
+
+@pytest.mark.parametrize("fast", [False, True])
 @pytest.mark.parametrize("M, N, K", [(513, 6145, 128), (400, 6100, 4112), (1025, 3585, 272), (3000, 577, 1040), (3001, 640, 16), (2049, 1281, 2064), (5000, 321, 400)])
 def test_gemm_tiles_of_128(M, N, K, fast):
     """Tiles of 128 tokens and outputs: a few blocks, one, and less than one."""
