@@ -30,8 +30,6 @@ HIPCC_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     f"-I{INCLUDE}", f"-I{CSRC}",
 ]
-# A loop that starts across a line of the instruction cache: the small tiles' steps took up to 17 % longer by luck of the address
-FILE_FLAGS = {"gemm_fp8": ["-falign-loops=64"]}
 
 
 def hipcc() -> str:
@@ -82,7 +80,7 @@ def build_library(verbose: bool = False, extra_flags=()) -> Path:
 
     def compile_one(src: Path) -> Path:
         obj = OBJDIR / (src.stem + ".o")
-        cmd = [cc, *HIPCC_FLAGS, *FILE_FLAGS.get(src.stem, []), *extra_flags, "-c", str(src), "-o", str(obj)]
+        cmd = [cc, *HIPCC_FLAGS, *extra_flags, "-c", str(src), "-o", str(obj)]
         r = subprocess.run(cmd, capture_output=True, text=True)
         out = "\n".join(l for l in (r.stdout + r.stderr).splitlines()
                         if "packed-fp32-ops" not in l and "target feature" not in l)
