@@ -429,8 +429,8 @@ __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int 
 // What bounds it: what passes through LDS, 128 bytes a cycle read and written (64 come in), then the L2s and what is behind
 // them where many CUs read; the launch and one round trip where a wavefront has few blocks.  Wavefronts of 32 x 32 that share
 // the blocks of a 64 x 64 tile read each byte twice and meet at a barrier every step: 256 x 3584 x 3584 10.3 us on codes and
-// 13.0 on f16, so 9.3 and 10.6; 61 x 3584 x 3584 6.7, so 5.7 (two buffers a wavefront, one for the larger tiles);
-// 1024 x 576 x 4096 10.2, so 9.7.
+// 13.0 on f16, so 9.2 and 11.0; 61 x 3584 x 3584 6.7, so 5.5 (two buffers a wavefront, one for the larger tiles);
+// 1024 x 576 x 4096 10.2, so 9.2.
 template <int NI, int MT, int STAGES, bool FAST, bool F32>
 __global__ __launch_bounds__(512, 2) void gemm_wave_tile_kernel(GemmFp8Params p, Layout tiles)
 {
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wave_tile_kernel(GemmFp8Params p,
     constexpr int BLOCK_B = (W_ROWS + A_ROWS) * QBLOCK, STAGE = BLOCK_B + 256;
     constexpr int PITCH = W_ROWS + 4;                                                      // floats per token
     constexpr int LDS_B = std::max(8 * STAGES * STAGE, 8 * A_ROWS * PITCH * 4);
-    static_assert(STAGES <= 2 && MT <= 2 && LDS_B <= 160 * 1024);
+    static_assert((STAGES == 1 || (STAGES == 2 && MT == 1)) && MT <= 2 && LDS_B <= 160 * 1024);
     __shared__ __attribute__((aligned(1024))) unsigned char smem[LDS_B];
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
@@ -457,25 +457,31 @@ __global__ __launch_bounds__(512, 2) void gemm_wave_tile_kernel(GemmFp8Params p,
     const uint32_t last_w = (uint32_t)min(W_ROWS - 1, p.N - 1 - n0) * (uint32_t)p.K, last_a = (uint32_t)min(A_ROWS - 1, p.M - 1 - m0) * (uint32_t)p.K;
     const uint8_t* w0 = p.w + (int64_t)n0 * p.K;
     const uint8_t* a0 = p.a + (int64_t)m0 * p.K;
-    const float* as = p.a_scales + min(m0 + lane, p.M - 1);
+    // Scales: of 32 tokens and, in the other half of the lanes, the weights'; of 64 tokens, and the weights' goes to a register
+    // (asked for a block ahead: 1 - 4 % longer; with 32 tokens through a register: 4 - 7 %)
     const float* ws = p.w_scales + (int64_t)(n0 / QBLOCK) * blocks;
+    const bool token = MT == 2 || lane < 32;
+    const float* scale0 = token ? p.a_scales + min(m0 + lane, p.M - 1) : ws;
+    const int64_t scale_step = token ? p.scale_pitch : 1;
     auto request = [&](int b, uint32_t stage) {
         const int64_t at = (int64_t)b * QBLOCK;
-        const bool whole = at + QBLOCK <= p.K;
+        const uint32_t row_step = 8u * (uint32_t)p.K;
+        auto off = [&](int k, bool W) { return min(row + (uint32_t)(W ? k : k - W_ROWS / 8) * row_step, W ? last_w : last_a) + (even ^ (k & 1) * 64); };
+        if (at + QBLOCK <= p.K) {
 #pragma unroll
-        for (int k = 0; k < GROUPS; ++k) {
-            const bool W = k < W_ROWS / 8;
-            const uint32_t piece = even ^ (k & 1) * 64, off = min(row + (uint32_t)(W ? k : k - W_ROWS / 8) * 8 * (uint32_t)p.K, W ? last_w : last_a) + piece;
-            const uint8_t* from = (W ? w0 : a0) + at;
-            const uint32_t dst = mine + stage + k * 1024;
-            if (whole) {
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst), "v"(off), "s"(from) : "memory");
-            } else {                                   // columns at and past K are zeros
-                const uint8_t* src = at + piece < p.K ? from + off : reinterpret_cast<const uint8_t*>(zeros16);
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(dst), "v"(src) : "memory");
+            for (int k = 0; k < GROUPS; ++k) {
+                const bool W = k < W_ROWS / 8;
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(mine + stage + k * 1024), "v"(off(k, W)), "s"((W ? w0 : a0) + at) : "memory");
+            }
+        } else {                                       // columns at and past K are zeros
+#pragma unroll
+            for (int k = 0; k < GROUPS; ++k) {
+                const bool W = k < W_ROWS / 8;
+                const uint8_t* src = at + (even ^ (k & 1) * 64) < p.K ? (W ? w0 : a0) + at + off(k, W) : reinterpret_cast<const uint8_t*>(zeros16);
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(mine + stage + k * 1024), "v"(src) : "memory");
             }
         }
-        const float* src = as + b * p.scale_pitch;
+        const float* src = scale0 + b * scale_step;
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(mine + stage + BLOCK_B), "v"(src) : "memory");
     };
 
@@ -487,7 +493,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wave_tile_kernel(GemmFp8Params p,
     const int key = (n >> 1) & 7;
     LDS_AS unsigned char* own = lds + wave * STAGES * STAGE;
     for (int b = wave; b < blocks; b += 8) {
-        const float sw = ws[b];
+        float sw = MT == 2 ? ws[b] : 0.f;
         if (STAGES == 2 && b + 8 < blocks) wait_vmcnt<LOADS>();
         else                               wait_vmcnt<0>();
         asm volatile("" ::: "memory");
@@ -508,6 +514,7 @@ __global__ __launch_bounds__(512, 2) void gemm_wave_tile_kernel(GemmFp8Params p,
         }
 #pragma unroll
         for (int j = 0; j < MT; ++j) sa[j] = *(LDS_AS float*)(st + BLOCK_B + (j * 32 + n) * 4);
+        if (MT == 1) sw = *(LDS_AS float*)(st + BLOCK_B + 32 * 4);
         __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): the block is in registers, the next may take its place
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
@@ -582,8 +589,8 @@ struct Plan {
 // The form that a model of the times finds fastest: a launch, per round of 256 workgroups (each fills its CU) the steps over K,
 // and something from a round to the next; or the time that the operands take from memory.  us per step with few workgroups;
 // the fuller the rounds, the longer the steps, for power and the caches' rates (`crowded`: all CUs).  Fitted to 280 sizes of 17 to
-// 32768 tokens and ten (N, K), with each kind of sums: the choice takes 0.1 % longer than the best form on average, 7 % at
-// the most (with the second launch below 9 %).
+// 32768 tokens and ten (N, K), with each kind of sums: the choice takes 0.2 % longer than the best form on average, 18 %
+// at the most.
 Plan one_launch(int M, int N, int K, bool fast)
 {
     const int blocks = (K + QBLOCK - 1) / QBLOCK;
@@ -592,9 +599,9 @@ Plan one_launch(int M, int N, int K, bool fast)
     struct Times { float launch, step, crowded, round; };
     struct Shape { Form form; int blocks; Times fast, f16; };
     static const Shape shapes[] = {
-        {WAVE_32x32, 8, {2.4f, 0.70f, 1.2f, 1.f}, {2.8f, 0.75f, 1.35f, 1.f}}, {WAVE_64x32, 8, {2.4f, 1.01f, 1.35f, 1.f}, {2.8f, 1.17f, 1.4f, 1.5f}},
-        {WAVE_64x64, 8, {3.2f, 1.46f, 1.2f, 2.f}, {3.6f, 1.85f, 1.2f, 3.5f}}, {TILE_128x128, 1, {4.f, 0.336f, 1.65f, 2.f}, {4.f, 0.75f, 1.35f, 2.5f}},
-        {TILE_256x128, 1, {4.4f, 0.545f, 1.9f, 2.f}, {4.4f, 1.2f, 1.5f, 2.5f}}, {TILE_256x256, 1, {4.4f, 1.24f, 1.35f, 2.f}, {}}};
+        {WAVE_32x32, 8, {2.4f, 0.70f, 1.2f, 1.f}, {2.8f, 0.73f, 1.35f, 1.f}}, {WAVE_64x32, 8, {2.4f, 1.01f, 1.35f, 1.f}, {2.8f, 1.13f, 1.2f, 1.5f}},
+        {WAVE_64x64, 8, {3.2f, 1.46f, 1.2f, 2.f}, {3.6f, 1.85f, 1.2f, 3.5f}}, {TILE_128x128, 1, {4.f, 0.336f, 1.65f, 2.f}, {4.f, 0.75f, 1.35f, 2.f}},
+        {TILE_256x128, 1, {4.4f, 0.545f, 1.9f, 2.f}, {4.4f, 1.2f, 1.5f, 2.f}}, {TILE_256x256, 1, {4.4f, 1.24f, 1.35f, 2.f}, {}}};
     Plan best = {TILE_256x128, 1, M, 3e38f};
     for (const Shape& f : shapes) {
         if (f.form == TILE_256x256 && !fast) continue;                   // (its registers are taken on f16)
