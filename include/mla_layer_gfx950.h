@@ -21,8 +21,8 @@
  *  - rows (activations): codes [T, D], scales [ceil(D/128), T]: one scale per token
  *    and block of 128 columns (the last block may be short), the tokens of a block
  *    beside each other, as the product reads them.  scale = max|block| / 448, at
- *    least 2^-126, and 1 for a block of zeros; a code is value / scale rounded to
- *    nearest even.  A block that holds an infinity or a NaN gets a scale that is
+ *    least 2^-126, and 1 for a block of zeros; a code is value / scale, a quotient in
+ *    fp32, rounded to nearest even.  A block that holds an infinity or a NaN gets a scale that is
  *    one, so that whatever is computed from it is not finite either.
  *  - weights: codes [N, K] (one output per row, as a linear layer stores them),
  *    scales [ceil(N/128), ceil(K/128)], one per 128 x 128 block.  Any positive

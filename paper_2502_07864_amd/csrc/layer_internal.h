@@ -234,13 +234,26 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v)
 }
 
 // Scale of a block whose largest magnitude has these bits.  At least 2^-126, so that the scale and its reciprocal are
-// normal numbers: value * (1 / scale) is then value / scale within two roundings of 2^-24 before the code's own of 2^-4.
+// normal numbers.
 __device__ __forceinline__ float block_scale(uint32_t top)
 {
     const float m = __uint_as_float(top);
     if (top == 0) return 1.f;
     const float s = m / E4M3_MAX;
     return s < 1.17549435e-38f ? 1.17549435e-38f : s;      // (a NaN stays)
+}
+
+// value / scale with the rounding of a division where nothing underflows: one step from the product with the rounded
+// reciprocal, which alone is another number in a quarter of the cases and moves a value near the middle between two codes to
+// the wrong one.  (Divisions, ten instructions each, took as long as the memory in cache_store.)  The signs of zeros stay.  By an infinite
+// scale, that of a block that holds an infinity, finite values give zeros and the infinity NaN: its d is 0 here, because
+// infinity times a quotient of zero is not a number.
+struct Divisor { float d, reciprocal; };
+__device__ __forceinline__ Divisor divisor(float scale) { return {scale == __builtin_inff() ? 0.f : scale, 1.f / scale}; }
+__device__ __forceinline__ float quotient(float v, Divisor by)
+{
+    const float q = v * by.reciprocal;
+    return __builtin_fmaf(-__builtin_fmaf(q, by.d, -v), by.reciprocal, q);
 }
 
 // Cosine and sine of position * freq, times gain.  The number of turns is formed and reduced in fp64 (positions reach

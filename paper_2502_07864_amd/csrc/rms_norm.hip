@@ -100,11 +100,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(NormPar
         uint32_t top = 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k) top = max(top, c + k < p.D ? magnitude(v[i][k]) : 0u);
-        const float scale = block_scale(row_max(top)), inv = 1.f / scale;
+        const float scale = block_scale(row_max(top));
+        const Divisor by = divisor(scale);
+        auto q = [&](int k) { return quotient(v[i][k], by); };
         if (c >= p.D || !live) continue;
         if (c % QBLOCK == 0) p.scales[(int64_t)(c / QBLOCK) * p.T + row] = scale;
-        const uint32_t lo = e4m3_quad(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
-        const uint32_t hi = e4m3_quad(v[i][4] * inv, v[i][5] * inv, v[i][6] * inv, v[i][7] * inv);
+        const uint32_t lo = e4m3_quad(q(0), q(1), q(2), q(3));
+        const uint32_t hi = e4m3_quad(q(4), q(5), q(6), q(7));
         uint8_t* dst = p.codes + row * p.D + c;
         if constexpr (VEC) {
             put_words<STREAM>(dst, (words2){lo, hi});
@@ -141,11 +143,12 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(const void* w, ui
     for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
     if (tid % 64 == 0) part[tid / 64] = top;
     __syncthreads();
-    const float scale = block_scale(max(max(part[0], part[1]), max(part[2], part[3]))), inv = 1.f / scale;
+    const float scale = block_scale(max(max(part[0], part[1]), max(part[2], part[3])));
+    const Divisor by = divisor(scale);
     if (tid == 0) scales[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = scale;
     if (c < cols)
         for (int r = tid / QBLOCK; r < rows; r += 256 / QBLOCK)
-            codes[(int64_t)(n0 + r) * K + k0 + c] = (uint8_t)e4m3_quad(at(r, c) * inv, 0.f, 0.f, 0.f);
+            codes[(int64_t)(n0 + r) * K + k0 + c] = (uint8_t)e4m3_quad(quotient(at(r, c), by), 0.f, 0.f, 0.f);
 }
 
 template <bool F32, int TPR, int NV, bool NORM> void launch_rows(const NormParams& p, bool vec, bool stream, hipStream_t s)

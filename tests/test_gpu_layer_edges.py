@@ -1,0 +1,79 @@
+"""Operators around the attention at the edges of their definitions."""
+import math
+
+import pytest
+import torch
+
+from paper_2502_07864_amd import layer
+from test_gpu_layer import BF, DEV, F32, FP8, rnd
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ codes
+
+def middles():
+    """The numbers half way between two neighbouring normal codes, of both signs."""
+    m = torch.arange(8, 16, dtype=torch.float64)
+    t = torch.stack([(2 * m + 1) / 16 * 2.0 ** e for e in range(-6, 9)]).flatten()
+    t = t[t < 448]
+    return torch.cat((t, -t))
+
+
+def rows_of_middles(n, seed):
+    """[n, 256] in fp32: in every block of 128 columns 448 s and products t s with the middles t, all exact, s of 16 bits."""
+    g = torch.Generator().manual_seed(seed)
+    t = middles()
+    at = torch.randint(0, t.numel(), (n, 2, 128), generator=g)
+    t = t[at]
+    t[..., 0] = 448.0
+    s = torch.randint(1 << 15, 1 << 16, (n, 2, 1), generator=g).double() * 2.0 ** torch.randint(-40, 20, (n, 2, 1), generator=g).double()
+    x = t * s
+    assert torch.equal(x.float().double(), x)
+    return x.float().view(n, 256), t.view(n, 256), s.view(n, 2)
+
+
+def test_a_quotient_in_the_middle_goes_to_the_even_code():
+    x, t, s = rows_of_middles(2000, 1)
+    want = t.float().to(FP8).view(torch.uint8)
+    for width in (256, 255):                                    # in whole vectors and in pieces
+        codes, scales = layer.quantize_rows(x[:, :width].contiguous().to(DEV))
+        assert torch.equal(scales.t().cpu().double(), s)
+        assert torch.equal(codes.view(torch.uint8).cpu(), want[:, :width])
+
+
+def test_a_weights_quotient_in_the_middle_goes_to_the_even_code():
+    g = torch.Generator().manual_seed(3)
+    x, t, _ = rows_of_middles(128 * 9, 2)
+    s = torch.randint(1 << 15, 1 << 16, (9, 2), generator=g).double() * 2.0 ** -20
+    w = (t.view(9, 128, 2, 128) * s[:, None, :, None]).view(128 * 9, 256)
+    codes, scales = layer.quantize_weights(w.float().to(DEV))
+    assert torch.equal(scales.cpu().double(), s)
+    assert torch.equal(codes.view(torch.uint8).cpu(), t.float().to(FP8).view(torch.uint8))
+
+
+@pytest.mark.parametrize("io", [BF, F32])
+@pytest.mark.parametrize("D", [1024, 1001])
+def test_codes_are_those_of_the_quotient(io, D):
+    """Every code of many rows is the fp32 quotient's, rounded to nearest even; zeros keep their signs."""
+    x = rnd(3000, D, dtype=io, loud=True)
+    x[:, 7] = -0.0
+    codes, scales = layer.quantize_rows(x)
+    unit = scales.cpu().repeat_interleave(128, 0)[:D].t()
+    assert torch.equal(codes.view(torch.uint8).cpu(), (x.cpu().float() / unit).to(FP8).view(torch.uint8))
+
+
+def test_codes_of_a_block_with_an_infinity():
+    """Its scale is infinite, its finite values' codes are zeros, the infinity's is not a number; other blocks are as they were."""
+    x = rnd(4, 512, dtype=F32)
+    want, want_s = layer.quantize_rows(x)
+    x[1, 200] = math.inf
+    x[2, 300] = -math.inf
+    codes, scales = layer.quantize_rows(x)
+    nan = torch.isnan(codes.float())
+    assert nan.sum() == 2 and nan[1, 200] and nan[2, 300]
+    assert torch.isinf(scales[1, 1]) and torch.isinf(scales[2, 2]) and torch.isinf(scales).sum() == 2
+    assert not codes.float()[1, 128:256][~nan[1, 128:256]].any() and not codes.float()[2, 256:384][~nan[2, 256:384]].any()
+    same = torch.ones(4, 512, dtype=torch.bool, device=DEV)
+    same[1, 128:256], same[2, 256:384] = False, False
+    assert torch.equal(codes.view(torch.uint8)[same], want.view(torch.uint8)[same])
