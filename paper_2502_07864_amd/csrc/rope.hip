@@ -175,14 +175,6 @@ __device__ __forceinline__ int64_t place_of(const StoreParams& p, int r, int pos
     return (int64_t)page * p.page_size + pos % p.page_size;
 }
 
-// v / d, correctly rounded where nothing underflows: one step from the quotient by the rounded reciprocal.  (Eighteen divisions
-// a lane, ten instructions each, took as long as the memory.)
-__device__ __forceinline__ float quotient(float v, float d, float reciprocal)
-{
-    const float q = v * reciprocal;
-    return __builtin_fmaf(__builtin_fmaf(-q, d, v), reciprocal, q);
-}
-
 // A wavefront per row, four rows per workgroup, so that a workgroup needs no barrier and its rows no order.  A lane holds eight
 // values of c and a pair of k, whose turn it works out itself, NV times (512 NV >= d_c, 128 NV >= d_rope > 0).
 // 32768 rows of 576 in bf16, the latents normed, are 75 MB in 15.5 us (4.9 TB/s; the launch, a round trip for position and
@@ -260,7 +252,7 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
             for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * inv * w[k];
         }
     }
-    float scale = 1.f, inv = 1.f;
+    Divisor by = {1.f, 1.f};
     if (CACHE == MLA_FP8_E4M3) {
         uint32_t top = 0;
 #pragma unroll
@@ -274,11 +266,11 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
             if (lane + i * 64 < pairs) top = max(top, max(magnitude(re[i]), magnitude(im[i])));
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-        scale = block_scale(top);
-        inv = 1.f / scale;
+        const float scale = block_scale(top);
+        by = divisor(scale);
         if (lane == 0) p.kv_scale[at] = scale;
     }
-    auto q = [&](float x) { return quotient(x, scale, inv); };
+    auto q = [&](float x) { return quotient(x, by); };
     const int64_t o = at * n;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {

@@ -77,3 +77,31 @@ def test_codes_of_a_block_with_an_infinity():
     same = torch.ones(4, 512, dtype=torch.bool, device=DEV)
     same[1, 128:256], same[2, 256:384] = False, False
     assert torch.equal(codes.view(torch.uint8)[same], want.view(torch.uint8)[same])
+
+
+@pytest.mark.parametrize("io", [BF, F32])
+@pytest.mark.parametrize("layout", [0, 1])
+def test_cache_rows_have_the_same_bits_at_any_address(io, layout):
+    """Rows that lie on 16 bytes and rows that do not take different kernels; infinities, NaN and negative zeros among them."""
+    n, d_c, row = 60, 512, 576
+    rows = rnd(1, n, row, dtype=io, loud=True)
+    rows[0, 3, 17], rows[0, 9, 100], rows[0, 20, 511] = math.inf, -math.inf, math.nan
+    rows[0, 5, 40:90] = -0.0
+    rows[0, 6] = -0.0
+    rows[0, 9, 200:300] = -0.0
+    wide = torch.zeros((1, n, row + 3), dtype=io, device=DEV)
+    wide[..., 1:1 + row] = rows
+    freq, gain = layer.rope_frequencies(64)
+    pos, table = torch.arange(n, dtype=torch.int32, device=DEV).view(1, n), torch.tensor([[1]], dtype=torch.int32, device=DEV)
+    got = []
+    for x in (rows, wide[..., 1:1 + row]):
+        kv, scale = torch.zeros((2, 64, row), dtype=torch.uint8, device=DEV), torch.zeros((2, 64), device=DEV)
+        layer.cache_store(x, pos, freq, kv, table, d_c, gain, layout, kv_scale=scale)
+        kv = torch.where((kv & 0x7F) == 0x7F, torch.full_like(kv, 0x7F), kv)           # (a NaN's sign says nothing)
+        got.append((kv, scale))
+    assert torch.equal(got[0][0], got[1][0])
+    assert torch.equal(got[0][1].view(torch.int32), got[1][1].view(torch.int32))
+    kv, scale = got[0][0][1].view(FP8).float(), got[0][1][1]
+    for r, c in ((3, 17), (9, 100)):
+        assert torch.isinf(scale[r]) and torch.isnan(kv[r, c]) and not kv[r, :c].any() and not kv[r, c + 1:].any()
+    assert torch.isnan(scale[20]) and torch.isnan(kv[20]).all()
