@@ -132,10 +132,12 @@ int mla_gemm_fp8(const uint8_t* a, const float* a_scales, const uint8_t* w, cons
  *   kind      MLA_ROPE_PLAIN, MLA_ROPE_LINEAR, MLA_ROPE_YARN
  *   factor    >= 1: how many times longer than the original the contexts are
  *   original  context length the model was trained on (YARN)
- * YARN: with r_i = original theta_i / 2 pi turns of pair i within that length, pairs
- * of at least beta_fast turns keep theta_i, pairs of at most beta_slow get
- * theta_i / factor, those between are blended linearly in i between the (rounded)
- * places where r_i takes the two values; gain = 0.1 ln(factor) + 1.
+ * YARN (Peng et al. 2023, arXiv 2309.00071): with r_i = original theta_i / 2 pi turns
+ * of pair i within that length, pairs of at least beta_fast turns keep theta_i, pairs
+ * of at most beta_slow get theta_i / factor, those between are blended linearly in i
+ * between the places where r_i takes the two values, the former rounded down (and at
+ * least 0), the latter rounded up (which may be past the last pair: that one is then
+ * blended too); gain = 0.1 ln(factor) + 1.
  */
 int mla_rope_frequencies(double* freq, float* gain, int d_rope, double base, int kind, double factor,
                          int original, double beta_fast, double beta_slow);

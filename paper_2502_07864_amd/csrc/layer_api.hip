@@ -81,7 +81,7 @@ extern "C" int mla_rope_frequencies(double* freq, float* gain, int d_rope, doubl
         // pair (a real number) that turns `turns` times within the original length
         auto pair_at = [&](double turns) { return d_rope * std::log(original / (turns * 2.0 * M_PI)) / (2.0 * std::log(base)); };
         low = std::fmax(std::floor(pair_at(beta_fast)), 0.0);
-        high = std::fmin(std::ceil(pair_at(beta_slow)), pairs - 1.0);
+        high = std::ceil(pair_at(beta_slow));      // (beyond the last pair where even that turns more often than beta_slow)
         *gain = (float)(0.1 * std::log(factor) + 1.0);
     }
     for (int i = 0; i < pairs; ++i) {
@@ -91,7 +91,7 @@ extern "C" int mla_rope_frequencies(double* freq, float* gain, int d_rope, doubl
         } else if (kind == MLA_ROPE_LINEAR) {
             freq[i] = theta / factor;
         } else {
-            const double r = std::fmin(std::fmax((i - low) / std::fmax(high - low, 1e-3), 0.0), 1.0);
+            const double r = i >= high ? 1.0 : std::fmax((i - low) / (high - low), 0.0);
             freq[i] = theta * (1.0 - r) + theta / factor * r;
         }
     }

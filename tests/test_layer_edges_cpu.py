@@ -1,0 +1,30 @@
+"""Operators around the attention at the edges of their definitions, what needs no GPU."""
+import math
+
+import numpy as np
+import pytest
+
+from paper_2502_07864_amd import layer
+
+
+# ------------------------------------------------------------------ frequencies
+
+@pytest.mark.parametrize("d, base, factor, original", [
+    (64, 10000.0, 4.0, 65536), (64, 10000.0, 8.0, 131072), (64, 10000.0, 4.0, 1 << 30), (64, 500000.0, 16.0, 8192), (64, 10000.0, 40.0, 4096),
+    (128, 10000.0, 2.0, 100000), (32, 10000.0, 4.0, 2048), (6, 100.0, 3.0, 5000), (2, 10000.0, 4.0, 4096), (64, 10000.0, 4.0, 100), (64, 10000.0, 4.0, 5)])
+def test_yarn_frequencies_pair_by_pair(d, base, factor, original, fast=32.0, slow=1.0):
+    """Every pair against the definition, the ramp's ends among them: the ramp runs between the real numbers i at which a pair
+    turns `fast` and `slow` times in the original length, rounded outwards, wherever they lie beside the pairs."""
+    f, gain = layer.rope_frequencies(d, base, "yarn", factor, original, fast, slow, device="cpu")
+    place = lambda turns: d / 2 * math.log(original / (2 * math.pi * turns), base)        # original base^(-2 i / d) = 2 pi turns
+    low, high = max(math.floor(place(fast)), 0), math.ceil(place(slow))
+    for i in range(d // 2):
+        theta = base ** (-2 * i / d)
+        turns = original * theta / (2 * math.pi)
+        kept = 0.0 if i >= high else 1.0 if i <= low else (high - i) / (high - low)
+        np.testing.assert_allclose(f[i].item(), theta * kept + theta / factor * (1 - kept), rtol=1e-12)
+        if turns >= fast:
+            assert f[i].item() == theta
+        if turns <= slow:
+            np.testing.assert_allclose(f[i].item(), theta / factor, rtol=1e-12)
+    assert abs(gain - (0.1 * math.log(factor) + 1)) < 1e-6
