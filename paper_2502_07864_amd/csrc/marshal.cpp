@@ -5,7 +5,7 @@
 // the host set the pace below about 25 us per step.  The functions here read the tensors' fields directly and
 // call the C entry point they are given.  They accept what mla.py's checks let through, as far as it is plain torch
 // tensors, integers and floats: inputs of the expected types and shapes, tables of int32, and outputs of the
-// expected element size with room for the result (their own shape and type are the caller's).  For anything else
+// expected element size with room for the result (their own shape is the caller's, and in mla.py's calls their type).  For anything else
 // they return None without having called anything, and mla.py goes through its own checks, which raise.
 // No arithmetic, no allocation, no state beyond the entry points' addresses; the interpreter lock is released
 // around the call as ctypes does.
@@ -243,6 +243,26 @@ const at::Tensor& dense_rows(PyObject* o)
 bool is_codes(const at::Tensor& t) { return t.scalar_type() == at::kFloat8_e4m3fn || t.scalar_type() == at::kByte; }
 int64_t scale_blocks(int64_t n) { return (n + 127) / 128; }
 
+// Outputs of these calls are of the type that is written there, not only of its size (values of x's type, codes, fp32 scales).
+void* values_or_null(PyObject* o, int64_t n, const at::Tensor& x)
+{
+    void* p = room_or_null(o, n, (size_t)x.element_size());
+    require(!p || THPVariable_Unpack(o).scalar_type() == x.scalar_type());
+    return p;
+}
+uint8_t* codes_or_null(PyObject* o, int64_t n)
+{
+    void* p = room_or_null(o, n, 1);
+    require(!p || is_codes(THPVariable_Unpack(o)));
+    return static_cast<uint8_t*>(p);
+}
+float* scales_or_null(PyObject* o, int64_t n)
+{
+    void* p = room_or_null(o, n, 4);
+    require(!p || THPVariable_Unpack(o).scalar_type() == at::kFloat);
+    return static_cast<float*>(p);
+}
+
 // distance of the rows of x [T, D]
 int64_t row_pitch(const at::Tensor& x) { return x.size(0) > 1 ? x.stride(0) : x.size(1); }
 
@@ -266,12 +286,13 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
             require(r.dim() == 2 && r.size(0) == T && r.size(1) == D && r.scalar_type() == x.scalar_type());
             pr = r.data_ptr();
         }
-        void *pro = room_or_null(a[4], T * D, size_of(io)), *py = room_or_null(a[5], T * D, size_of(io)), *pc = room_or_null(a[6], T * D, 1),
-             *ps = room_or_null(a[7], T * scale_blocks(D), 4), *px = x.data_ptr(), *s = stream_of(x);
+        void *pro = values_or_null(a[4], T * D, x), *py = values_or_null(a[5], T * D, x), *px = x.data_ptr(), *s = stream_of(x);
+        uint8_t* pc = codes_or_null(a[6], T * D);
+        float* ps = scales_or_null(a[7], T * scale_blocks(D));
         const int t = dim(T), d = dim(D);
         const int64_t pitch = row_pitch(x);
         const float eps = real(a[2]);
-        return unlocked([&] { return p_rms_norm(px, pr, pw, pro, py, static_cast<uint8_t*>(pc), static_cast<float*>(ps), t, d, pitch, eps, io, s); });
+        return unlocked([&] { return p_rms_norm(px, pr, pw, pro, py, pc, ps, t, d, pitch, eps, io, s); });
     });
 }
 
@@ -279,15 +300,17 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
 PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     return guarded([&] {
-        require(n == 3);
+        require(n == 3 && a[1] != Py_None && a[2] != Py_None);
         const at::Tensor& x = dense_rows(a[0]);
         require(x.dim() == 2);
         const int64_t T = x.size(0), D = x.size(1);
         const mla_dtype io = io_type(x);
-        void *px = x.data_ptr(), *pc = room(a[1], T * D, 1), *ps = room(a[2], T * scale_blocks(D), 4), *s = stream_of(x);
+        void *px = x.data_ptr(), *s = stream_of(x);
+        uint8_t* pc = codes_or_null(a[1], T * D);
+        float* ps = scales_or_null(a[2], T * scale_blocks(D));
         const int t = dim(T), d = dim(D);
         const int64_t pitch = row_pitch(x);
-        return unlocked([&] { return p_quantize(px, static_cast<uint8_t*>(pc), static_cast<float*>(ps), t, d, pitch, io, s); });
+        return unlocked([&] { return p_quantize(px, pc, ps, t, d, pitch, io, s); });
     });
 }
 
@@ -328,8 +351,8 @@ PyObject* rope_queries(PyObject*, PyObject* const* a, Py_ssize_t n)
         const int64_t T = q.size(0), H = q.size(1), width = q.size(2), d_rope = 2 * freq.size(0), d_nope = width - d_rope;
         require(d_nope >= 0 && (H == 1 || q.stride(1) == width) && pos.dim() == 1 && pos.size(0) == T);
         const mla_dtype io = io_type(q);
-        void *pn = room_or_null(a[5], T * H * d_nope, size_of(io)), *pr = room(a[6], T * H * d_rope, size_of(io));
-        require(pn || d_nope == 0);
+        void *pn = values_or_null(a[5], T * H * d_nope, q), *pr = values_or_null(a[6], T * H * d_rope, q);
+        require(pr && (pn || d_nope == 0));
         void *pq = q.data_ptr(), *s = stream_of(q);
         const auto* pp = static_cast<const int32_t*>(pos.data_ptr());
         const auto* pf = static_cast<const double*>(freq.data_ptr());

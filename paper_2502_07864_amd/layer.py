@@ -2,8 +2,9 @@
 residual's addition and 8-bit output, projections on 8-bit codes, the queries' rotation, cache rows of new tokens.
 
 Argument marshalling only, as in ``mla.py``: torch tensors on the GPU in, device pointers and the current HIP stream
-to the C entry point of the same name, output tensors out.  Outputs that are passed in are written in place (no
-allocation); the others are allocated.  There is no fallback path.
+to the C entry point of the same name, output tensors out.  Outputs that are passed in are written in place, densely from
+their first element on (no allocation; their type and room are checked, their shape is the caller's); the others are
+allocated.  There is no fallback path.
 """
 from __future__ import annotations
 
@@ -41,6 +42,13 @@ def _like(t: Optional[torch.Tensor], x: torch.Tensor, shape, name: str):
     """A dense operand of x's type."""
     if t is not None and (t.dtype != x.dtype or tuple(t.shape) != tuple(shape)):
         raise ValueError(f"{name} must be {list(shape)} of {x.dtype}")
+    return _dev(t, name)
+
+
+def _typed(t: Optional[torch.Tensor], x: torch.Tensor, name: str):
+    """An output of x's type."""
+    if t is not None and t.dtype != x.dtype:
+        raise TypeError(f"{name} must be {x.dtype}, got {t.dtype}")
     return _dev(t, name)
 
 
@@ -106,8 +114,8 @@ def _norm(x, weight, eps, residual, residual_out, out, codes, scales):
     px, pitch = _rows(x, "x", T, D)
     if codes is not None:
         _new_codes(T, D, x.device, codes, scales)
-    args = (px, _like(residual, x, (T, D), "residual"), _like(weight, x, (D,), "weight"), _dev(residual_out, "residual_out"),
-            _dev(out, "out"), _dev(codes, "codes"), _dev(scales, "scales"), T, D, pitch, float(eps), _io_code(x), _stream(x))
+    args = (px, _like(residual, x, (T, D), "residual"), _like(weight, x, (D,), "weight"), _typed(residual_out, x, "residual_out"),
+            _typed(out, x, "out"), _dev(codes, "codes"), _dev(scales, "scales"), T, D, pitch, float(eps), _io_code(x), _stream(x))
     _room(residual_out, T * D, x.element_size(), "residual_out")
     _room(out, T * D, x.element_size(), "out")
     _room(codes, T * D, 1, "codes")
@@ -236,7 +244,7 @@ def rope_queries(q: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, g
         q_nope = torch.empty((T, H, d_nope), dtype=q.dtype, device=q.device)
     if q_rope is None:
         q_rope = torch.empty((T, H, d_rope), dtype=q.dtype, device=q.device)
-    args = (pq, _dev(positions, "positions"), _dev(freq, "freq"), _dev(q_nope, "q_nope"), _dev(q_rope, "q_rope"), T, H, d_nope,
+    args = (pq, _dev(positions, "positions"), _dev(freq, "freq"), _typed(q_nope, q, "q_nope"), _typed(q_rope, q, "q_rope"), T, H, d_nope,
             d_rope, pitch, float(gain), int(layout), _io_code(q), _stream(q))
     _room(q_nope, T * H * d_nope, q.element_size(), "q_nope")
     _room(q_rope, T * H * d_rope, q.element_size(), "q_rope")

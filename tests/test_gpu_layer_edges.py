@@ -4,8 +4,8 @@ import math
 import pytest
 import torch
 
-from paper_2502_07864_amd import layer
-from test_gpu_layer import BF, DEV, F32, FP8, rnd
+from paper_2502_07864_amd import layer, mla
+from test_gpu_layer import BF, DEV, F32, FP8, rnd, the_calls
 
 pytestmark = pytest.mark.gpu
 
@@ -105,3 +105,30 @@ def test_cache_rows_have_the_same_bits_at_any_address(io, layout):
     for r, c in ((3, 17), (9, 100)):
         assert torch.isinf(scale[r]) and torch.isnan(kv[r, c]) and not kv[r, :c].any() and not kv[r, c + 1:].any()
     assert torch.isnan(scale[20]) and torch.isnan(kv[20]).all()
+
+
+# ------------------------------------------------------------------ outputs of another type
+
+OTHER = {
+    "norm": [dict(out=torch.float16), dict(out=torch.int16), dict(residual_out=torch.float16), dict(codes=torch.int8), dict(codes=torch.bool),
+             dict(codes=torch.float8_e5m2), dict(scales=torch.int32)],
+    "quantize": [dict(codes=torch.int8), dict(codes=torch.float8_e5m2), dict(scales=torch.int32)],
+    "rope": [dict(q_nope=torch.float16), dict(q_rope=torch.float16), dict(q_rope=torch.int16)],
+}
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("name", list(OTHER))
+def test_outputs_of_another_type_are_refused(name, native, monkeypatch):
+    """Their size would do; their type is not what is written there.  Nothing is written."""
+    mla.lib()
+    f, args, outputs = the_calls()[name]
+    if not native:
+        monkeypatch.setattr(mla, "_fast", None)
+    for case in OTHER[name]:
+        a = {**args, **{k: args[k].view(torch.uint8).clone().view(t) for k, t in case.items()}}
+        with pytest.raises((ValueError, TypeError)):
+            f(**a)
+        torch.cuda.synchronize()
+        for k in outputs:
+            assert not a[k].view(torch.uint8).any(), (case, k)
