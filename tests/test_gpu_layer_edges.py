@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2502_07864_amd import layer, mla
-from test_gpu_layer import BF, DEV, F32, FP8, rnd, the_calls
+from test_gpu_layer import BF, DEV, F32, FAST_DROP, FAST_NORM, FP8, ROUND, blocks, dequantised, near, operands, rnd, the_calls
 
 pytestmark = pytest.mark.gpu
 
@@ -105,6 +105,63 @@ def test_cache_rows_have_the_same_bits_at_any_address(io, layout):
     for r, c in ((3, 17), (9, 100)):
         assert torch.isinf(scale[r]) and torch.isnan(kv[r, c]) and not kv[r, :c].any() and not kv[r, c + 1:].any()
     assert torch.isnan(scale[20]) and torch.isnan(kv[20]).all()
+
+
+# ------------------------------------------------------------------ products whose depth is shared out
+
+# sizes at which the product of either kind of sums (fast or not) writes partial sums to the workspace
+SHARED = [(136, 6088, 7184, False), (146, 6006, 8448, False), (1032, 1208, 9808, True), (2877, 171, 14352, True)]
+
+
+@pytest.mark.parametrize("M, N, K, fast", SHARED)
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_shares_of_the_depth(M, N, K, fast, dtype):
+    """Against 64 bits; the partial sums go through the workspace, and around it and the outputs nothing changes; five times
+    the same bits, whatever the workspace held."""
+    a, sa, w, sw = operands(M, N, K)
+    need = layer.gemm_fp8_workspace_bytes(M, N, K)
+    assert need >= 2 * 4 * M * N
+    room = torch.full((M * N + 512,), 7.0, dtype=dtype, device=DEV)
+    out = room[256:256 + M * N].view(M, N)
+    scratch = torch.full((need + 512,), 0xAB, dtype=torch.uint8, device=DEV)
+    flags = layer.GEMM_FAST_SUMS if fast else 0
+    layer.gemm_fp8(a, sa, w, sw, out=out, workspace=scratch[256:256 + need], flags=flags)
+    A, W = dequantised(a, sa, w, sw)
+    want, size = torch.mm(A, W.t().contiguous()), torch.mm(A.abs(), W.abs().t().contiguous())
+    near(out, want, ROUND[dtype], ((FAST_DROP if fast else 0.0) + (140 + blocks(K)) * 2.0 ** -24) * size)
+    if fast:
+        assert (out.double() - want).norm() <= (FAST_NORM + (2.0 ** -9 if dtype == BF else 0.0)) * want.norm()
+    assert (scratch[256:256 + 4 * M * N] != 0xAB).any()
+    assert (scratch[:256] == 0xAB).all() and (scratch[256 + need:] == 0xAB).all()
+    assert (room[:256] == 7).all() and (room[256 + M * N:] == 7).all()
+    first = out.clone()
+    for fill in (0, 0x7F, 0xFF, 0x55):
+        scratch.fill_(fill)
+        layer.gemm_fp8(a, sa, w, sw, out=out, workspace=scratch[256:256 + need], flags=flags)
+        assert torch.equal(out, first)
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("M, N, K, fast", SHARED[1:3])
+def test_a_workspace_is_checked_or_made(M, N, K, fast, native, monkeypatch):
+    """One that is short or off 16 bytes is refused and nothing is written; without one the binding brings its own."""
+    mla.lib()
+    if not native:
+        monkeypatch.setattr(mla, "_fast", None)
+    a, sa, w, sw = operands(M, N, K)
+    need = layer.gemm_fp8_workspace_bytes(M, N, K)
+    assert need > 0
+    flags = layer.GEMM_FAST_SUMS if fast else 0
+    out = torch.zeros((M, N), dtype=BF, device=DEV)
+    room = torch.empty(need + 16, dtype=torch.uint8, device=DEV)
+    for ws in (room[:need - 1], room[8:8 + need], room[:0]):
+        with pytest.raises(mla.MlaError) as e:
+            layer.gemm_fp8(a, sa, w, sw, out=out, workspace=ws, flags=flags)
+        assert e.value.status == -4
+    torch.cuda.synchronize()
+    assert not out.any()
+    want = layer.gemm_fp8(a, sa, w, sw, workspace=room[:need], flags=flags)
+    assert layer.gemm_fp8(a, sa, w, sw, out=out, flags=flags) is out and torch.equal(out, want)
 
 
 # ------------------------------------------------------------------ outputs of another type

@@ -4,7 +4,7 @@ import math
 import numpy as np
 import pytest
 
-from paper_2502_07864_amd import layer
+from paper_2502_07864_amd import layer, mla
 
 
 # ------------------------------------------------------------------ frequencies
@@ -28,3 +28,17 @@ def test_yarn_frequencies_pair_by_pair(d, base, factor, original, fast=32.0, slo
         if turns <= slow:
             np.testing.assert_allclose(f[i].item(), theta / factor, rtol=1e-12)
     assert abs(gain - (0.1 * math.log(factor) + 1)) < 1e-6
+
+
+# ------------------------------------------------------------------ the product's workspace
+
+@pytest.mark.parametrize("M, N, K", [(136, 6088, 7184), (146, 6006, 8448), (1032, 1208, 9808), (2877, 171, 14352)])
+def test_a_missing_workspace_is_refused(M, N, K):
+    """Sizes whose depth is shared out (with full sums or with fast ones): the workspace has to be there for either, as long as
+    they say and on 16 bytes.  (The pointers are never used: every call is refused.)"""
+    p = 0x10000
+    need = layer.gemm_fp8_workspace_bytes(M, N, K)
+    assert need >= 2 * 4 * M * N and need % (4 * M * N) == 0
+    for flags in (0, layer.GEMM_FAST_SUMS):
+        for ws, size in ((None, 0), (None, need), (p, need - 1), (p + 4, need), (p + 8, 2 * need)):
+            assert mla.lib().mla_gemm_fp8(p, p, p, p, p, ws, size, M, N, K, mla.BF16, flags, None) == -4
