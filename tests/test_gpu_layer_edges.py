@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2502_07864_amd import layer, mla
-from test_gpu_layer import BF, DEV, F32, FAST_DROP, FAST_NORM, FP8, ROUND, blocks, dequantised, near, operands, rnd, the_calls
+from test_gpu_layer import BF, DEV, F32, FAST_DROP, FAST_NORM, FP8, ROUND, blocks, dequantised, near, operands, ref_norm, rnd, the_calls
 
 pytestmark = pytest.mark.gpu
 
@@ -105,6 +105,22 @@ def test_cache_rows_have_the_same_bits_at_any_address(io, layout):
     for r, c in ((3, 17), (9, 100)):
         assert torch.isinf(scale[r]) and torch.isnan(kv[r, c]) and not kv[r, :c].any() and not kv[r, c + 1:].any()
     assert torch.isnan(scale[20]) and torch.isnan(kv[20]).all()
+
+
+# ------------------------------------------------------------------ norm
+
+def test_the_sum_may_take_the_place_of_x():
+    """residual_out is x itself, with the codes and without, in whole vectors and in pieces."""
+    for D in (4096, 1001):
+        x, r, w = rnd(70, D, dtype=BF), rnd(70, D, dtype=BF, seed=3), rnd(D, dtype=BF, seed=4)
+        want, want_s = layer.rms_norm(x, w, residual=r)
+        codes, scales, _, _ = layer.rms_norm_fp8(x, w, residual=r)
+        a, b = x.clone(), x.clone()
+        y, s = layer.rms_norm(a, w, residual=r, residual_out=a)
+        assert s is a and torch.equal(a, want_s) and torch.equal(y, want)
+        near(a, ref_norm(x, w, 1e-6, r)[0], ROUND[BF], 2.0 ** -24 * (x.double().abs() + r.double().abs()))
+        codes2, scales2, s2, _ = layer.rms_norm_fp8(b, w, residual=r, residual_out=b)
+        assert torch.equal(s2, want_s) and torch.equal(codes2.view(torch.uint8), codes.view(torch.uint8)) and torch.equal(scales2, scales)
 
 
 # ------------------------------------------------------------------ products whose depth is shared out
