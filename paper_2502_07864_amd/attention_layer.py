@@ -50,7 +50,16 @@ class AttentionLayer:
     def from_conversion(cls, cv: dict, W_Q: torch.Tensor, W_O: torch.Tensor, norm_weight: torch.Tensor, d_head: int,
                         rope: Tuple[torch.Tensor, float], **kw) -> "AttentionLayer":
         """The layer that convert.convert_layer's outputs stand for, with the query and output projections of the layer
-        that was converted (W_Q [h * d, D], W_O [D, h * d]): head i's rope rows are W_QR[i] W_Q_i."""
+        that was converted (W_Q [h * d, D], W_O [D, h * d]): head i's rope rows are W_QR[i] W_Q_i, in interleaved pairs.
+
+        rope: its d_rope / 2 = keep * d / (2 M) frequencies, of the converted layer's base.  Pair G * keep + r belongs to
+        FreqFold group G, so for any keep it may turn with the group's first frequency:
+            freq, gain = layer.rope_frequencies(d // M, base);  rope = (freq.repeat_interleave(keep), gain)
+        which is rope_frequencies(d_rope, base) for keep = 1.  For keep = M rope_frequencies(d, base) gives each pair one of
+        its group's own M frequencies, and the layer's own for M = 1.  For 1 < keep < M rope_frequencies(d_rope, base) is
+        neither."""
+        if kw.get("layout", layer.ROPE_INTERLEAVED) != layer.ROPE_INTERLEAVED:
+            raise ValueError("the conversion's rope rows are interleaved pairs")
         h, d_rope, d = cv["W_QR"].shape
         D = W_Q.shape[1]
         per_head = W_Q.double().view(h, d, D)

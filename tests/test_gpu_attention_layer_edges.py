@@ -1,0 +1,93 @@
+"""The attention layer where it meets the conversion, and its options."""
+import math
+
+import pytest
+import torch
+
+from paper_2502_07864_amd import convert, layer
+from paper_2502_07864_amd.attention_layer import AttentionLayer
+
+pytestmark = pytest.mark.gpu
+
+DEV, BF, FP8 = "cuda:0", torch.bfloat16, torch.float8_e4m3fn
+
+
+def folded_layer(M, keep, g=2, h=4, d=64, D=256, n=512):
+    """A grouped-query layer that the conversion loses next to nothing of, and what it converts to: the keys of a FreqFold
+    group are of rank `keep` (and 1 % of noise), all its pairs turn with the group's first frequency, the joint basis is whole."""
+    r = torch.Generator().manual_seed(M * 10 + keep)
+    normal = lambda *s: torch.randn(s, generator=r, dtype=torch.float64)
+    W_K = torch.empty(g * d, D, dtype=torch.float64)
+    for G in range(d // (2 * M)):
+        mix = normal(M * g, keep) / keep ** 0.5
+        for part in range(2):
+            rows = torch.tensor([j * d + 2 * (G * M + p) + part for p in range(M) for j in range(g)])
+            W_K[rows] = mix @ normal(keep, D)
+    W_K = (W_K + 0.01 * normal(g * d, D)) / D ** 0.5
+    W_V, W_Q, W_O = normal(g * d, D) / D ** 0.5, 1.5 * normal(h * d, D) / D ** 0.5, normal(D, h * d) / (h * d) ** 0.5
+    X = normal(n, D)
+    d_rope = keep * d // M
+    r_kv = 2 * g * d - d_rope
+    cv = convert.convert_layer(X.to(DEV), W_K.to(DEV), W_V.to(DEV), normal(r_kv, r_kv).to(DEV), g, h, d, M, r_kv, iters=1, keep=keep)
+    theta = torch.tensor([10000.0 ** (-2 * (l // M * M) / d) for l in range(d // 2)], dtype=torch.float64)
+    return (g, h, d, D), (W_Q, W_K, W_V, W_O), cv, theta
+
+
+def grouped_query_attention(y, dims, weights, theta):
+    """y [L, D] -> [L, D], causal, the pairs of either head's width turned by theta."""
+    (g, h, d, D), (W_Q, W_K, W_V, W_O) = dims, weights
+    L = y.shape[0]
+
+    def turned(x):
+        a = torch.arange(L, dtype=torch.float64)[:, None, None] * theta
+        re, im = x[..., 0::2], x[..., 1::2]
+        return torch.stack((re * a.cos() - im * a.sin(), re * a.sin() + im * a.cos()), -1).flatten(-2)
+    q, k, v = turned((y @ W_Q.t()).view(L, h, d)), turned((y @ W_K.t()).view(L, g, d)), (y @ W_V.t()).view(L, g, d)
+    out = torch.empty(L, h, d, dtype=torch.float64)
+    for i in range(h):
+        s = q[:, i] @ k[:, i // (h // g)].t() / d ** 0.5
+        p = torch.softmax(s.masked_fill(torch.ones(L, L).triu(1).bool(), -math.inf), -1)
+        out[:, i] = p @ v[:, i // (h // g)]
+    return out.view(L, -1) @ W_O.t()
+
+
+def decoded(lay, x):
+    """x [L, D] through single-token decode steps."""
+    L, D = x.shape
+    kv = torch.zeros((-(-L // 64), 64, lay.d_c + lay.d_rope), dtype=BF, device=DEV)
+    table = torch.arange(kv.shape[0], dtype=torch.int32, device=DEV).view(1, -1)
+    got = []
+    for t in range(L):
+        at = torch.full((1, 1), t, dtype=torch.int32, device=DEV)
+        got.append(lay.decode(x[t].view(1, 1, D), at, kv, table, at.view(1) + 1, num_splits=1)[0].view(D))
+    return torch.stack(got).double().cpu()
+
+
+# Against the unquantised layer in 64 bits.  An e4m3 code is within 2^-4 of its value, 2^-4 / sqrt(3) = 3.6e-2 in the 2-norm;
+# queries and cache rows are products of codes with codes, 5.1e-2 each; scores of 1.7 rms are then off by sqrt(2) 5.1e-2 1.7 =
+# 0.12, the softmax's weights by that share of themselves, the heads' results by that and the latents' 5.1e-2, the outputs by
+# 5.1e-2 more: 0.15, with bf16 and the noise in the keys (6e-3) far below.
+UNQUANTISED = 0.2
+
+
+@pytest.mark.parametrize("M, keep", [(1, 1), (2, 2), (2, 1), (4, 2), (4, 3)])
+def test_a_converted_layer_is_the_layer_it_was_converted_from(M, keep):
+    """convert_layer -> from_conversion -> decode, with the frequencies that the docstring names, against the grouped-query
+    layer; ordinary RoPE of the narrower key is not that layer where several components, but not all, stay under RoPE."""
+    dims, weights, cv, theta = folded_layer(M, keep)
+    g, h, d, D = dims
+    W_Q, _, _, W_O = weights
+    freq, gain = layer.rope_frequencies(d // M)
+    rope = freq.repeat_interleave(keep), gain
+    if keep == 1:
+        assert torch.equal(rope[0], layer.rope_frequencies(keep * d // M)[0])
+    lay = AttentionLayer.from_conversion(cv, W_Q.to(DEV), W_O.to(DEV), torch.ones(D, device=DEV).to(BF), d, rope)
+    x = torch.randn((40, D), generator=torch.Generator().manual_seed(7)).to(BF)
+    y = x.double() / (x.double().square().mean(-1, keepdim=True) + lay.eps).sqrt()
+    want = grouped_query_attention(y, dims, weights, theta)
+    off = lambda got: float((got - want).norm() / want.norm())
+    got = off(decoded(lay, x.to(DEV)))
+    assert got <= UNQUANTISED, got
+    if 1 < keep < M:
+        lay.freq = layer.rope_frequencies(keep * d // M)[0]
+        assert off(decoded(lay, x.to(DEV))) > UNQUANTISED

@@ -3,8 +3,10 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2502_07864_amd import layer, mla
+from paper_2502_07864_amd.attention_layer import AttentionLayer
 
 
 # ------------------------------------------------------------------ frequencies
@@ -42,3 +44,13 @@ def test_a_missing_workspace_is_refused(M, N, K):
     for flags in (0, layer.GEMM_FAST_SUMS):
         for ws, size in ((None, 0), (None, need), (p, need - 1), (p + 4, need), (p + 8, 2 * need)):
             assert mla.lib().mla_gemm_fp8(p, p, p, p, p, ws, size, M, N, K, mla.BF16, flags, None) == -4
+
+
+# ------------------------------------------------------------------ the attention layer
+
+def test_a_converted_layer_takes_interleaved_pairs_only():
+    """The rows of W_QR and W_KR are pairs of neighbours; nothing is computed before this is said."""
+    cv = dict(W_QR=torch.zeros(2, 64, 128), W_KR=torch.zeros(64, 256), W_DKV=torch.zeros(256, 256), W_UK=torch.zeros(2, 128, 256), W_UV=torch.zeros(2, 256, 128))
+    with pytest.raises(ValueError, match="interleaved"):
+        AttentionLayer.from_conversion(cv, torch.zeros(256, 256), torch.zeros(256, 256), torch.zeros(256), 128, layer.rope_frequencies(64, device="cpu"),
+                                       layout=layer.ROPE_HALF)
