@@ -65,7 +65,8 @@ class AttentionLayer:
         per_head = W_Q.double().view(h, d, D)
         rows = torch.cat((per_head, torch.bmm(cv["W_QR"].double(), per_head)), 1).view(h * (d + d_rope), D)
         bf = torch.bfloat16
-        return cls(rows.to(bf), torch.cat((cv["W_DKV"], cv["W_KR"]), 0).to(bf), cv["W_UK"].to(bf), cv["W_UV"].to(bf), W_O.to(bf),
+        # (the quantised ones in fp32: a rounding to bf16 before the codes' own would move values between two of them)
+        return cls(rows.float(), torch.cat((cv["W_DKV"], cv["W_KR"]), 0).float(), cv["W_UK"].to(bf), cv["W_UV"].to(bf), W_O.float(),
                    norm_weight, rope, d_head ** -0.5, **kw)
 
     def _before(self, x, residual, positions, kv_cache, page_table, kv_scale):

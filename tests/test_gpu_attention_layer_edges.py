@@ -91,3 +91,14 @@ def test_a_converted_layer_is_the_layer_it_was_converted_from(M, keep):
     if 1 < keep < M:
         lay.freq = layer.rope_frequencies(keep * d // M)[0]
         assert off(decoded(lay, x.to(DEV))) > UNQUANTISED
+
+
+def test_converted_weights_are_rounded_once():
+    """Their codes are those of the fp64 factors' fp32 values."""
+    (g, h, d, D), (W_Q, _, _, W_O), cv, _ = folded_layer(2, 1)
+    lay = AttentionLayer.from_conversion(cv, W_Q.to(DEV), W_O.to(DEV), torch.ones(D, device=DEV).to(BF), d, layer.rope_frequencies(32))
+    W_Q = W_Q.to(DEV).view(h, d, D)
+    rows = torch.cat((W_Q, torch.bmm(cv["W_QR"], W_Q)), 1).view(-1, D)
+    for got, want in ((lay.W_Q, rows), (lay.W_DKVR, torch.cat((cv["W_DKV"], cv["W_KR"]))), (lay.W_O, W_O.to(DEV))):
+        codes, scales = layer.quantize_weights(want.float())
+        assert torch.equal(got[0].view(torch.uint8), codes.view(torch.uint8)) and torch.equal(got[1], scales)
