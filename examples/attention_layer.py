@@ -1,7 +1,7 @@
 """A converted attention layer at work on random weights: prompts through ``prefill``, then decode steps, the step also
 from a captured graph.
 
-    python examples/attention_layer.py [--batch 16] [--prompt 1024] [--steps 32] [--cache bf16|fp8]
+    python examples/attention_layer.py [--batch 16] [--prompt 1024] [--steps 32] [--cache bf16|fp8] [--full-sums]
 """
 from __future__ import annotations
 
@@ -19,14 +19,14 @@ from paper_2502_07864_amd.attention_layer import AttentionLayer      # noqa: E40
 D, H, D_HEAD, D_C, D_ROPE, PAGE = 4096, 32, 128, 512, 64, 64
 
 
-def random_layer(g: torch.Generator) -> AttentionLayer:
+def random_layer(g: torch.Generator, gemm_flags: int) -> AttentionLayer:
     def w(*shape, fan):
         return (torch.randn(shape, generator=g, device="cuda") * fan ** -0.5).bfloat16()
     return AttentionLayer(
         W_Q=w(H * (D_HEAD + D_ROPE), D, fan=D), W_DKVR=w(D_C + D_ROPE, D, fan=D), W_UK=w(H, D_HEAD, D_C, fan=D_C),
         W_UV=w(H, D_C, D_HEAD, fan=D_C), W_O=w(D, H * D_HEAD, fan=H * D_HEAD), norm_weight=torch.ones(D, device="cuda").bfloat16(),
         rope=layer.rope_frequencies(D_ROPE, scaling="yarn", factor=8.0), softmax_scale=(D_HEAD + D_ROPE) ** -0.5,
-        latent_norm=torch.ones(D_C, device="cuda"))
+        latent_norm=torch.ones(D_C, device="cuda"), gemm_flags=gemm_flags)
 
 
 def main() -> None:
@@ -35,10 +35,11 @@ def main() -> None:
     ap.add_argument("--prompt", type=int, default=1024)
     ap.add_argument("--steps", type=int, default=32)
     ap.add_argument("--cache", choices=("bf16", "fp8"), default="bf16")
+    ap.add_argument("--full-sums", action="store_true", help="the projections' 8-bit products are added without loss (layer.GEMM_FAST_SUMS off)")
     a = ap.parse_args()
     B, L = a.batch, a.prompt
     g = torch.Generator(device="cuda").manual_seed(1)
-    lay = random_layer(g)
+    lay = random_layer(g, 0 if a.full_sums else layer.GEMM_FAST_SUMS)
     pages = -(-(L + a.steps + 4) // PAGE)
     table = torch.randperm(B * pages, generator=g, device="cuda").to(torch.int32).view(B, pages)
     fp8 = a.cache == "fp8"

@@ -23,11 +23,12 @@ class AttentionLayer:
     """W_Q [H * (d_head + d_rope), D] (per head the nope rows, then the rope rows), W_DKVR [d_c + d_rope, D], W_O [D, H *
     d_head] are quantised here, once; W_UK [H, d_head, d_c] and W_UV [H, d_c, d_head] are kept in bf16, norm_weight [D] and
     latent_norm [d_c] (None: the latents are cached as projected) in the type of the hidden states.  rope: (freq, gain) as
-    layer.rope_frequencies gives them."""
+    layer.rope_frequencies gives them.  gemm_flags: of the queries' and the output's product (layer.gemm_fp8;
+    GEMM_FAST_SUMS: both results are rounded to bf16 anyway); the cache rows, in fp32, always have full sums."""
 
     def __init__(self, W_Q: torch.Tensor, W_DKVR: torch.Tensor, W_UK: torch.Tensor, W_UV: torch.Tensor, W_O: torch.Tensor,
                  norm_weight: torch.Tensor, rope: Tuple[torch.Tensor, float], softmax_scale: float, eps: float = 1e-6,
-                 latent_norm: Optional[torch.Tensor] = None, layout: int = layer.ROPE_INTERLEAVED):
+                 latent_norm: Optional[torch.Tensor] = None, layout: int = layer.ROPE_INTERLEAVED, gemm_flags: int = 0):
         H, d_head, d_c = W_UK.shape
         self.freq, self.gain = rope
         self.H, self.d_head, self.d_c, self.d_rope = H, d_head, d_c, 2 * self.freq.numel()
@@ -44,7 +45,7 @@ class AttentionLayer:
         self.norm_weight = norm_weight
         # the cache rows come out of their product in fp32, to be rounded once where they are stored
         self.latent_norm = None if latent_norm is None else latent_norm.float()
-        self.softmax_scale, self.eps, self.layout = float(softmax_scale), float(eps), int(layout)
+        self.softmax_scale, self.eps, self.layout, self.gemm_flags = float(softmax_scale), float(eps), int(layout), int(gemm_flags)
 
     @classmethod
     def from_conversion(cls, cv: dict, W_Q: torch.Tensor, W_O: torch.Tensor, norm_weight: torch.Tensor, d_head: int,
@@ -77,14 +78,14 @@ class AttentionLayer:
         rows = layer.gemm_fp8(codes, scales, *self.W_DKVR, dtype=torch.float32)
         layer.cache_store(rows.view(B, T, -1), positions, self.freq, kv_cache, page_table, self.d_c, self.gain, self.layout,
                           self.latent_norm, self.eps, kv_scale)
-        q = layer.gemm_fp8(codes, scales, *self.W_Q, flags=layer.GEMM_FAST_SUMS)
+        q = layer.gemm_fp8(codes, scales, *self.W_Q, flags=self.gemm_flags)
         q_nope, q_rope = layer.rope_queries(q.view(B * T, self.H, -1), positions.view(B * T), self.freq, self.gain, self.layout)
         return q_nope, q_rope, (x if s is None else s).view(B, T, D)
 
     def _after(self, out, B, T):
         """Output projection of the heads' results [B, T, H, d_head]."""
         codes, scales = layer.quantize_rows(out.view(B * T, self.H * self.d_head))
-        return layer.gemm_fp8(codes, scales, *self.W_O, flags=layer.GEMM_FAST_SUMS).view(B, T, -1)
+        return layer.gemm_fp8(codes, scales, *self.W_O, flags=self.gemm_flags).view(B, T, -1)
 
     def decode(self, x: torch.Tensor, positions: torch.Tensor, kv_cache: torch.Tensor, page_table: torch.Tensor,
                seq_lens: torch.Tensor, residual: Optional[torch.Tensor] = None, kv_scale: Optional[torch.Tensor] = None,

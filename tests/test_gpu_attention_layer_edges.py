@@ -102,3 +102,29 @@ def test_converted_weights_are_rounded_once():
     for got, want in ((lay.W_Q, rows), (lay.W_DKVR, torch.cat((cv["W_DKV"], cv["W_KR"]))), (lay.W_O, W_O.to(DEV))):
         codes, scales = layer.quantize_weights(want.float())
         assert torch.equal(got[0].view(torch.uint8), codes.view(torch.uint8)) and torch.equal(got[1], scales)
+
+
+def small_layer(**kw):
+    r = torch.Generator().manual_seed(5)
+    w = lambda *s: (torch.randn(s, generator=r) * s[-1] ** -0.5).to(BF).to(DEV)
+    return AttentionLayer(w(4 * 192, 512), w(320, 512), w(4, 128, 256), w(4, 256, 128), w(512, 512), torch.ones(512, device=DEV).to(BF),
+                          layer.rope_frequencies(64), 192 ** -0.5, **kw)
+
+
+@pytest.mark.parametrize("flags", [None, 0, layer.GEMM_FAST_SUMS])
+def test_the_sums_are_the_callers_choice(flags, monkeypatch):
+    """Full sums unless the caller allows others, and those for the bf16 products only; decode and prefill alike."""
+    lay = small_layer(**({} if flags is None else {"gemm_flags": flags}))
+    asked, product = [], layer.gemm_fp8
+
+    def recorded(*a, **kw):
+        asked.append((kw.get("flags", 0), kw.get("dtype", BF)))
+        return product(*a, **kw)
+    monkeypatch.setattr(layer, "gemm_fp8", recorded)
+    kv, table = torch.zeros((2, 64, 320), dtype=BF, device=DEV), torch.zeros((1, 1), dtype=torch.int32, device=DEV)
+    x = torch.randn((1, 3, 512), generator=torch.Generator().manual_seed(1)).to(BF).to(DEV)
+    at, n = torch.arange(3, dtype=torch.int32, device=DEV).view(1, 3), torch.tensor([3], dtype=torch.int32, device=DEV)
+    for call in (lay.decode, lay.prefill):
+        asked.clear()
+        call(x, at, kv, table, n)
+        assert sorted(asked, key=str) == sorted([(0, torch.float32), (flags or 0, BF), (flags or 0, BF)], key=str)
