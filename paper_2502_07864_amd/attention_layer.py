@@ -24,11 +24,13 @@ class AttentionLayer:
     d_head] are quantised here, once; W_UK [H, d_head, d_c] and W_UV [H, d_c, d_head] are kept in bf16, norm_weight [D] and
     latent_norm [d_c] (None: the latents are cached as projected) in the type of the hidden states.  rope: (freq, gain) as
     layer.rope_frequencies gives them.  gemm_flags: of the queries' and the output's product (layer.gemm_fp8;
-    GEMM_FAST_SUMS: both results are rounded to bf16 anyway); the cache rows, in fp32, always have full sums."""
+    GEMM_FAST_SUMS: both results are rounded to bf16 anyway); the cache rows, in fp32, always have full sums.
+    latent_eps: of the latents' norm, eps where it is None."""
 
     def __init__(self, W_Q: torch.Tensor, W_DKVR: torch.Tensor, W_UK: torch.Tensor, W_UV: torch.Tensor, W_O: torch.Tensor,
                  norm_weight: torch.Tensor, rope: Tuple[torch.Tensor, float], softmax_scale: float, eps: float = 1e-6,
-                 latent_norm: Optional[torch.Tensor] = None, layout: int = layer.ROPE_INTERLEAVED, gemm_flags: int = 0):
+                 latent_norm: Optional[torch.Tensor] = None, layout: int = layer.ROPE_INTERLEAVED, gemm_flags: int = 0,
+                 latent_eps: Optional[float] = None):
         H, d_head, d_c = W_UK.shape
         self.freq, self.gain = rope
         self.H, self.d_head, self.d_c, self.d_rope = H, d_head, d_c, 2 * self.freq.numel()
@@ -45,6 +47,7 @@ class AttentionLayer:
         self.norm_weight = norm_weight
         # the cache rows come out of their product in fp32, to be rounded once where they are stored
         self.latent_norm = None if latent_norm is None else latent_norm.float()
+        self.latent_eps = float(eps if latent_eps is None else latent_eps)
         self.softmax_scale, self.eps, self.layout, self.gemm_flags = float(softmax_scale), float(eps), int(layout), int(gemm_flags)
 
     @classmethod
@@ -77,7 +80,7 @@ class AttentionLayer:
                                                  residual=None if residual is None else residual.view(B * T, D))
         rows = layer.gemm_fp8(codes, scales, *self.W_DKVR, dtype=torch.float32)
         layer.cache_store(rows.view(B, T, -1), positions, self.freq, kv_cache, page_table, self.d_c, self.gain, self.layout,
-                          self.latent_norm, self.eps, kv_scale)
+                          self.latent_norm, self.latent_eps, kv_scale)
         q = layer.gemm_fp8(codes, scales, *self.W_Q, flags=self.gemm_flags)
         q_nope, q_rope = layer.rope_queries(q.view(B * T, self.H, -1), positions.view(B * T), self.freq, self.gain, self.layout)
         return q_nope, q_rope, (x if s is None else s).view(B, T, D)

@@ -128,3 +128,20 @@ def test_the_sums_are_the_callers_choice(flags, monkeypatch):
         asked.clear()
         call(x, at, kv, table, n)
         assert sorted(asked, key=str) == sorted([(0, torch.float32), (flags or 0, BF), (flags or 0, BF)], key=str)
+
+
+@pytest.mark.parametrize("eps, latent_eps", [(1e-6, 0.5), (0.5, 1e-6), (0.25, None)])
+def test_the_two_norms_may_differ(eps, latent_eps):
+    """The cached latents against 64 bits: codes of the normed states (2^-4 of a value, 3.6e-2 in the 2-norm, the weights' taken
+    as they are), their product normed with the latents' own eps; the other norm's eps there is 10 % off and more."""
+    lay = small_layer(eps=eps, latent_eps=latent_eps, latent_norm=torch.ones(256, device=DEV))
+    kv, table = torch.zeros((1, 64, 320), dtype=BF, device=DEV), torch.zeros((1, 1), dtype=torch.int32, device=DEV)
+    x = (0.7 * torch.randn((1, 3, 512), generator=torch.Generator().manual_seed(1))).to(BF).to(DEV)
+    lay.decode(x, torch.arange(3, dtype=torch.int32, device=DEV).view(1, 3), kv, table, torch.tensor([3], dtype=torch.int32, device=DEV))
+    codes, scales = lay.W_DKVR
+    W = codes.double() * scales.double().repeat_interleave(128, 0)[:320].repeat_interleave(128, 1)
+    s = x[0].double()
+    rows = (s / (s.square().mean(-1, keepdim=True) + eps).sqrt()) @ W[:256].t().contiguous()
+    normed = lambda e: rows / (rows.square().mean(-1, keepdim=True) + e).sqrt()
+    want = normed(eps if latent_eps is None else latent_eps)
+    assert (kv[0, :3, :256].double() - want).norm() <= 5e-2 * want.norm()
