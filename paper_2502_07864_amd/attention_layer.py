@@ -40,6 +40,8 @@ class AttentionLayer:
         for name, (w, shape) in shapes.items():
             if tuple(w.shape) != shape:
                 raise ValueError(f"{name} must be {list(shape)}, got {list(w.shape)}")
+        if W_UK.dtype != torch.bfloat16 or W_UV.dtype != torch.bfloat16:
+            raise TypeError(f"W_UK and W_UV must be bfloat16, got {W_UK.dtype} and {W_UV.dtype}")
         if D % 16 or (H * d_head) % 16:
             raise ValueError("the model dimension and H * d_head must be multiples of 16")
         self.W_Q, self.W_DKVR, self.W_O = (layer.quantize_weights(w.contiguous()) for w in (W_Q, W_DKVR, W_O))

@@ -54,3 +54,14 @@ def test_a_converted_layer_takes_interleaved_pairs_only():
     with pytest.raises(ValueError, match="interleaved"):
         AttentionLayer.from_conversion(cv, torch.zeros(256, 256), torch.zeros(256, 256), torch.zeros(256), 128, layer.rope_frequencies(64, device="cpu"),
                                        layout=layer.ROPE_HALF)
+
+
+@pytest.mark.parametrize("wrong", ["W_UK", "W_UV"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_the_latents_weights_are_bf16(wrong, dtype):
+    """Said where they are given, not at the first step."""
+    z = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    w = dict(W_Q=z(4 * 192, 512), W_DKVR=z(320, 512), W_UK=z(4, 128, 256), W_UV=z(4, 256, 128), W_O=z(512, 512))
+    w[wrong] = w[wrong].to(dtype)
+    with pytest.raises(TypeError, match="bfloat16"):
+        AttentionLayer(**w, norm_weight=z(512), rope=layer.rope_frequencies(64, device="cpu"), softmax_scale=1.0)
