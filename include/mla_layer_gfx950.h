@@ -157,7 +157,8 @@ int mla_rope_frequencies(double* freq, float* gain, int d_rope, double base, int
  *   q_rope     [T, H, d_rope] (output)
  * Pair i of the rotated part turns by positions[t] freq[i] (formed in fp64; the
  * turn itself is fp32).  d_rope even, 2 to 256; d_nope >= 0, H (d_nope + d_rope)
- * up to 2^30.
+ * up to 2^30, and no more heads' rows than a grid holds (at least 2^24, whatever
+ * their width; otherwise MLA_ERR_UNSUPPORTED).
  */
 int mla_rope_queries(const void* q, const int32_t* positions, const double* freq, void* q_nope, void* q_rope,
                      int T, int H, int d_nope, int d_rope, int64_t q_pitch, float gain, int layout,

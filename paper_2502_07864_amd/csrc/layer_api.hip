@@ -108,6 +108,7 @@ extern "C" int mla_rope_queries(const void* q, const int32_t* positions, const d
     if (q_pitch < width || !(gain == gain)) return MLA_ERR_SHAPE;
     if (!io_ok(io_dtype) || !layout_ok(layout) || d_rope > 256 || width > 1 << 30 || T > MAX_ROWS) return MLA_ERR_UNSUPPORTED;
     const RopeParams p{q, positions, freq, q_nope, q_rope, T, H, d_nope, d_rope, q_pitch, gain};
+    if (!rope_queries_supported(p, layout, io_dtype)) return MLA_ERR_UNSUPPORTED;
     return status_of(launch_rope_queries(p, layout, io_dtype, static_cast<hipStream_t>(hip_stream)));
 }
 

@@ -68,6 +68,7 @@ hipError_t launch_quantize_weights(const void* w, uint8_t* codes, float* scales,
 size_t     gemm_fp8_workspace(int M, int N, int K);
 bool       gemm_fp8_supported(int M, int N, int K);      // (the grid's threads are counted in 32 bits)
 hipError_t launch_gemm_fp8(const GemmFp8Params& p, mla_dtype out, bool fast_sums, hipStream_t s);
+bool       rope_queries_supported(const RopeParams& p, int layout, mla_dtype io);      // (the same)
 hipError_t launch_rope_queries(const RopeParams& p, int layout, mla_dtype io, hipStream_t s);
 hipError_t launch_cache_store(const StoreParams& p, int layout, mla_dtype io, mla_dtype cache, hipStream_t s);
 

@@ -368,37 +368,51 @@ __global__ __launch_bounds__(256) void cache_store_any_kernel(StoreParams p)
 
 bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
-template <bool F32, bool HALF> void rope(const RopeParams& p, hipStream_t s)
+// How the queries are shared out: v values per access (0: any width and address, a workgroup per token), heads and tokens of a
+// workgroup
+struct RopePlan {
+    int v, heads, tokens;
+    int64_t grid(const RopeParams& p) const { return v ? (int64_t)((p.T + tokens - 1) / tokens) * ((p.H + heads - 1) / heads) : p.T; }
+};
+
+RopePlan rope_plan(const RopeParams& p, bool f32, bool half)
 {
     // vectors of 8 or 4 values: they have to fit the parts of a head's row, and every row to lie on their bytes
-    const int unit = HALF ? p.d_rope / 2 : p.d_rope;
+    const int unit = half ? p.d_rope / 2 : p.d_rope;
     auto fits = [&](int v) {
-        const int bytes = F32 ? 16 : 2 * v, per = bytes / (F32 ? 4 : 2);
+        const int bytes = f32 ? 16 : 2 * v, per = bytes / (f32 ? 4 : 2);
         return p.d_nope % v == 0 && unit % v == 0 && p.pitch % per == 0 && on(p.q, bytes) && on(p.q_nope, bytes) && on(p.q_rope, bytes) &&
                p.d_nope <= 4096;
     };
-    const int v = fits(8) ? 8 : fits(4) ? 4 : 0;
-    if (!v) {
-        rope_queries_any_kernel<F32, HALF><<<dim3((unsigned)p.T), dim3(256), 0, s>>>(p);
-        return;
-    }
+    RopePlan plan = {fits(8) ? 8 : fits(4) ? 4 : 0, 1, 1};
+    if (!plan.v) return plan;
     // As many heads' rows per workgroup as have 128 vectors to turn (32768 tokens x 32 heads, 8 / 16 / 32 rows: pairs 160 / 128 /
     // 141 us; 16 / 32 / 64: halves 131 / 142 / 148), fewer while that leaves CUs without one
-    const int rows = std::max(1, 128 / (p.d_rope / v));
-    int heads = std::min(p.H, rows), tokens = std::max(1, std::min(rows / heads, ROPE_TOKENS));
-    auto grid_of = [&] { return (int64_t)((p.T + tokens - 1) / tokens) * ((p.H + heads - 1) / heads); };
-    while (grid_of() < 512 && tokens > 1) tokens = (tokens + 1) / 2;
-    while (grid_of() < 512 && heads > 4) heads = (heads + 1) / 2;
-    const int groups = (p.H + heads - 1) / heads;
-    const dim3 grid((unsigned)grid_of()), block(256);
+    const int rows = std::max(1, 128 / (p.d_rope / plan.v));
+    plan.heads = std::min(p.H, rows);
+    plan.tokens = std::max(1, std::min(rows / plan.heads, ROPE_TOKENS));
+    while (plan.grid(p) < 512 && plan.tokens > 1) plan.tokens = (plan.tokens + 1) / 2;
+    while (plan.grid(p) < 512 && plan.heads > 4) plan.heads = (plan.heads + 1) / 2;
+    return plan;
+}
+
+template <bool F32, bool HALF> void rope(const RopeParams& p, hipStream_t s)
+{
+    const RopePlan plan = rope_plan(p, F32, HALF);
+    const dim3 grid((unsigned)plan.grid(p)), block(256);
+    if (!plan.v) {
+        rope_queries_any_kernel<F32, HALF><<<grid, block, 0, s>>>(p);
+        return;
+    }
+    const int groups = (p.H + plan.heads - 1) / plan.heads;
     const bool stream = (int64_t)p.T * p.H * (p.d_nope + p.d_rope) * (F32 ? 4 : 2) > STREAM_BYTES;
     auto run = [&](auto vec) {
         constexpr int V = decltype(vec)::value;
-        if (stream) rope_queries_kernel<F32, HALF, V, true><<<grid, block, 0, s>>>(p, tokens, heads, groups);
-        else        rope_queries_kernel<F32, HALF, V, false><<<grid, block, 0, s>>>(p, tokens, heads, groups);
+        if (stream) rope_queries_kernel<F32, HALF, V, true><<<grid, block, 0, s>>>(p, plan.tokens, plan.heads, groups);
+        else        rope_queries_kernel<F32, HALF, V, false><<<grid, block, 0, s>>>(p, plan.tokens, plan.heads, groups);
     };
-    if (v == 8) run(std::integral_constant<int, 8>{});
-    else        run(std::integral_constant<int, 4>{});
+    if (plan.v == 8) run(std::integral_constant<int, 8>{});
+    else             run(std::integral_constant<int, 4>{});
 }
 
 template <bool F32, bool HALF, int CACHE> void store_rows(const StoreParams& p, hipStream_t s)
@@ -420,6 +434,11 @@ template <bool F32, bool HALF> void store(const StoreParams& p, mla_dtype cache,
 }
 
 }  // namespace
+
+bool rope_queries_supported(const RopeParams& p, int layout, mla_dtype io)
+{
+    return rope_plan(p, io == MLA_F32, layout == MLA_ROPE_HALF).grid(p) < 1l << 24;              // (256 threads each)
+}
 
 hipError_t launch_rope_queries(const RopeParams& p, int layout, mla_dtype io, hipStream_t s)
 {

@@ -46,6 +46,17 @@ def test_a_missing_workspace_is_refused(M, N, K):
             assert mla.lib().mla_gemm_fp8(p, p, p, p, p, ws, size, M, N, K, mla.BF16, flags, None) == -4
 
 
+# ------------------------------------------------------------------ rotation
+
+@pytest.mark.parametrize("T, H, d_nope, d_rope, layout, io", [
+    ((1 << 23) - 1, 40, 0, 256, 0, mla.BF16), ((1 << 23) - 1, 4000, 128, 64, 0, mla.BF16), ((1 << 23) - 1, 10, 4, 256, 1, mla.F32),
+    ((1 << 23) - 1, 1 << 22, 0, 256, 0, mla.BF16), (1 << 22, 30, 4, 252, 0, mla.BF16)])
+def test_more_rows_than_a_grid_holds_are_refused(T, H, d_nope, d_rope, layout, io):
+    """(The pointers are never used.)"""
+    p = 0x10000
+    assert mla.lib().mla_rope_queries(p, p, p, p, p, T, H, d_nope, d_rope, H * (d_nope + d_rope), 1.0, layout, io, None) == -3
+
+
 # ------------------------------------------------------------------ the attention layer
 
 def test_a_converted_layer_takes_interleaved_pairs_only():
