@@ -234,16 +234,6 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v)
     return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, false));
 }
 
-// Scale of a block whose largest magnitude has these bits.  At least 2^-126, so that the scale and its reciprocal are
-// normal numbers.
-__device__ __forceinline__ float block_scale(uint32_t top)
-{
-    const float m = __uint_as_float(top);
-    if (top == 0) return 1.f;
-    const float s = m / E4M3_MAX;
-    return s < 1.17549435e-38f ? 1.17549435e-38f : s;      // (a NaN stays)
-}
-
 // value / scale with the rounding of a division where nothing underflows: one step from the product with the rounded
 // reciprocal, which alone is another number in a quarter of the cases and moves a value near the middle between two codes to
 // the wrong one.  (Divisions, ten instructions each, took as long as the memory in cache_store.)  The signs of zeros stay.  By an infinite
@@ -255,6 +245,15 @@ __device__ __forceinline__ float quotient(float v, Divisor by)
 {
     const float q = v * by.reciprocal;
     return __builtin_fmaf(-__builtin_fmaf(q, by.d, -v), by.reciprocal, q);
+}
+
+// Scale of a block whose largest magnitude has these bits.  At least 2^-126, so that the scale and its reciprocal are
+// normal numbers.  (The quotient by 448 is the division's for every magnitude of which it is kept: all 2^31 were compared.)
+__device__ __forceinline__ float block_scale(uint32_t top)
+{
+    if (top == 0) return 1.f;
+    if (top >= 0x7F800000u) return __uint_as_float(top);       // infinity, NaN
+    return fmaxf(quotient(__uint_as_float(top), {E4M3_MAX, 1.f / E4M3_MAX}), 1.17549435e-38f);
 }
 
 // Cosine and sine of position * freq, times gain.  The number of turns is formed and reduced in fp64 (positions reach
