@@ -183,8 +183,8 @@ __device__ __attribute__((aligned(16))) const uint32_t zeros16[4] = {0u, 0u, 0u,
 // one has arrived; the loads of the block after take its place and are spread over the units, because a wavefront stands
 // still while a load is accepted.
 //
-// What bounds it: power.  At 32768 x 6144 x 4096 on codes (660 - 690 us, 2390 - 2500 Tflop/s) the matrix cores are busy 70 % of the
-// cycles at 1.51 GHz of the card's 2.4.  On f16, whose instructions do half the work a cycle, 1365 us.
+// What bounds it: power.  At 32768 x 6144 x 4096 on codes (680 - 720 us from card to card, 2290 - 2430 Tflop/s) the matrix cores are busy 70 % of the
+// cycles at 1.51 GHz of the card's 2.4.  On f16, whose instructions do half the work a cycle, 1340 - 1390 us.
 template <int NI, int MT, int WN, int STAGES, bool FAST, bool F32, bool SPLIT, bool STREAM>
 __global__ __launch_bounds__(512, 2) void gemm_tile_kernel(GemmFp8Params p, int tiles_m, int tiles_n, int splits)
 {

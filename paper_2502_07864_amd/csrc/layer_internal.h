@@ -9,9 +9,10 @@ namespace mla {
 
 constexpr int QBLOCK = 128;        // columns (and weight rows) per scale
 constexpr float E4M3_MAX = 448.f;
-// Outputs beyond this many bytes go past the caches: they are read again from memory anyway, and what they would displace is
-// not (us, kept / streamed: queries of 32768 tokens x 32 heads 167 / 131, norm of 32768 x 4096 165 / 159, product of
-// 32768 x 6144 697 / 659; at 8192 tokens and below no difference)
+// Outputs of a call beyond this many bytes together go past the caches (us of the call, kept / streamed: queries of 32768 tokens x 32
+// heads 167 / 131, norm of 32768 x 4096 165 / 159, product of 32768 x 6144 697 / 659, each pair on one card; at 8192 tokens and
+// below no difference).  What it costs the call that reads them next has not been measured: of the norm's outputs the codes, a third of
+// the bytes, are read at once, by two products.
 constexpr int64_t STREAM_BYTES = (int64_t)64 << 20;
 
 struct NormParams {
@@ -236,9 +237,9 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v)
 
 // value / scale with the rounding of a division where nothing underflows: one step from the product with the rounded
 // reciprocal, which alone is another number in a quarter of the cases and moves a value near the middle between two codes to
-// the wrong one.  (Divisions, ten instructions each, took as long as the memory in cache_store.)  The signs of zeros stay.  By an infinite
-// scale, that of a block that holds an infinity, finite values give zeros and the infinity NaN: its d is 0 here, because
-// infinity times a quotient of zero is not a number.
+// the wrong one.  (Divisions, ten instructions each, took as long as the memory in cache_store.)  The signs of zeros stay.  By an
+// infinite scale, that of a block that holds an infinity, finite values give zeros and the infinity NaN: its d is 0 here,
+// because infinity times a quotient of zero is not a number.
 struct Divisor { float d, reciprocal; };
 __device__ __forceinline__ Divisor divisor(float scale) { return {scale == __builtin_inff() ? 0.f : scale, 1.f / scale}; }
 __device__ __forceinline__ float quotient(float v, Divisor by)

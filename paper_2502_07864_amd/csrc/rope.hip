@@ -132,7 +132,8 @@ __global__ __launch_bounds__(256) void rope_queries_kernel(RopeParams p, int tok
     }
 }
 
-// any widths and addresses, value by value; one workgroup per token
+// any widths and addresses, value by value; one workgroup per token (32 heads of 128 + 64 in bf16 on an odd address: 4096 tokens
+// 27 us, in vectors 15.5, 32768 tokens 280 and 128, 16 tokens 6.0 and 3.7)
 template <bool F32, bool HALF>
 __global__ __launch_bounds__(256) void rope_queries_any_kernel(RopeParams p)
 {
@@ -312,7 +313,8 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
     }
 }
 
-// any widths and addresses; one workgroup per row, the row in LDS as fp32
+// any widths and addresses, and rows without a rotated part; one workgroup per row, the row in LDS as fp32 (32768 rows of 512 + 64
+// from bf16 on an odd address: to bf16 44 us, in vectors 14, to fp8 53 and 15; of 512 + 0: 35 and 44; 64 rows 3.7 either way)
 template <bool F32, bool HALF, int CACHE>
 __global__ __launch_bounds__(256) void cache_store_any_kernel(StoreParams p)
 {

@@ -172,8 +172,8 @@ def gemm_fp8(a: torch.Tensor, a_scales: torch.Tensor, w: torch.Tensor, w_scales:
              dtype: torch.dtype = torch.bfloat16, flags: int = 0) -> torch.Tensor:
     """out [M, N] = (a * a_scales) (w * w_scales)^T;  a [M, K] and w [N, K] e4m3 codes, a_scales [ceil(K/128), M],
     w_scales [ceil(N/128), ceil(K/128)].  out float32 or bfloat16 (`dtype` where it is allocated here).
-    flags GEMM_FAST_SUMS: the matrix cores may add the 8-bit products as they are (twice the rate at many tokens,
-    results 1.5e-5 off)."""
+    flags GEMM_FAST_SUMS: the matrix cores may add the 8-bit products as they are (up to twice the rate; results 1.5e-5
+    off for random operands, at most 7 * 2^-13 of the sum of the products' magnitudes)."""
     fast = mla._fast
     if fast is not None and out is not None:
         status = fast.gemm_fp8(a, a_scales, w, w_scales, out, workspace, flags)
