@@ -236,12 +236,12 @@ def prepare(case, seed):
         s["q_nope"] = _normal(g, (B, T, H, D_HEAD)).to(io)
         s["W_UK"] = _normal(g, (H, D_HEAD, d_c), d_c ** -0.5).to(io)
         s["W_UV"] = _normal(g, (H, d_c, D_HEAD), d_c ** -0.5).to(io)
-        s["out"] = torch.empty((B, T, H, D_HEAD), dtype=io, device=DEV)
+        s["out"] = torch.empty((B, T, H, D_HEAD), dtype=io, device=DEV)       # (what a layer takes from a prompt)
     else:
         # (unit variance of the scaled scores, as absorbed queries of unit variance have it)
         s["q_abs"] = _normal(g, (B, T, H, d_c), (D_HEAD / d_c) ** 0.5).to(io)
         s["out"] = torch.empty((B, T, H, d_c), dtype=io, device=DEV)
-    s["lse"] = torch.empty((B, T, H), dtype=torch.float32, device=DEV)
+        s["lse"] = torch.empty((B, T, H), dtype=torch.float32, device=DEV)
     if kind == "tree":
         s["mask"] = torch.tensor(_signed(_masks(c, seed)), dtype=torch.int64, device=DEV)
     s["ws"] = None
@@ -273,7 +273,8 @@ def _run_own(s):
                                 kv_scale=s["kv_scale"], workspace=s["ws"], out=s["out"], lse=s["lse"])
     elif kind == "prefill":
         mla.prefill_window(s["q_nope"], s["q_rope"], s["W_UK"], s["W_UV"], s["kv"], s["table"], s["lens"], c["window"], c["sinks"],
-                           SCALE, workspace=s["ws"], out=s["out"], lse=s["lse"])
+                           SCALE, workspace=s["ws"], out=s["out"])
+        return {"out": s["out"]}
     else:
         layer.cache_move(s["kv"], s["table"], s["src"], s["dst"], kv_scale=s["kv_scale"])
         return {"kv": s["kv"], "kv_scale": s["kv_scale"]}
@@ -348,7 +349,7 @@ def _run_plain(s):
     at = _columns(c, s["lens"])
     sees = _sees(s, at)
     if kind == "prefill":
-        out, lse = torch.empty_like(s["out"]), torch.empty_like(s["lse"])
+        out = torch.empty_like(s["out"])
         for b in range(B):
             one = dict(s, table=s["table"][b:b + 1])
             x = _rows(one, at[b:b + 1], torch.float32)[0]
@@ -356,10 +357,9 @@ def _run_plain(s):
                 k = torch.cat((torch.mm(x[:, :d_c], s["W_UK"][h].float().t()), x[:, d_c:]), 1)
                 v = torch.mm(x[:, :d_c], s["W_UV"][h].float())
                 q = torch.cat((s["q_nope"][b, :, h].float(), s["q_rope"][b, :, h].float()), 1)
-                p, z, l = _softmax((torch.mm(q, k.t()) * SCALE).masked_fill_(~sees[b], -math.inf))
+                p, z, _ = _softmax((torch.mm(q, k.t()) * SCALE).masked_fill_(~sees[b], -math.inf))
                 out[b, :, h] = (torch.mm(p, v) / torch.where(z > 0, z, torch.ones_like(z))).to(out.dtype)
-                lse[b, :, h] = l
-        return {"out": out, "lse": lse}
+        return {"out": out}
     x = _rows(s, at, torch.float32)
     q = torch.cat((s["q_abs"].float(), s["q_rope"].float()), -1).view(B, T * H, -1)
     scores = torch.bmm(q, x.transpose(1, 2).contiguous()).view(B, T, H, -1) * SCALE
@@ -409,7 +409,7 @@ def exact(case, seed):
         return {"kv": kv, "kv_scale": kv_scale}
     T, H, d_c = c["tokens"], c["heads"], c["d_c"]
     out = torch.zeros(s["out"].shape, dtype=torch.float64, device=DEV)
-    lse = torch.empty(s["lse"].shape, dtype=torch.float64, device=DEV)
+    lse = torch.empty((c["batch"], T, H), dtype=torch.float64, device=DEV)
     for b, length in enumerate(lens):
         rows, allowed = _exact_visible(c, seed, b, length)
         rows, allowed = rows.to(DEV), allowed.to(DEV)
@@ -430,7 +430,7 @@ def exact(case, seed):
             scores = scores * SCALE + blocked
             lse[b, :, h] = torch.logsumexp(scores, 1)
             out[b, :, h] = torch.exp(scores - lse[b, :, h, None]) @ values
-    return {"out": out, "lse": lse}
+    return {"out": out} if kind == "prefill" else {"out": out, "lse": lse}
 
 
 # ------------------------------------------------------------------------------------------------
@@ -461,7 +461,7 @@ def work(case):
         pairs += sum(bin(m).count("1") for t in _masks(c, 0) for m in t)
     tokens = c["batch"] * T * H
     if kind == "prefill":
-        return {"bytes": rows * row_bytes + tokens * ((2 * D_HEAD + D_ROPE) * io + 4) + 2 * H * D_HEAD * d_c * io,
+        return {"bytes": rows * row_bytes + tokens * (2 * D_HEAD + D_ROPE) * io + 2 * H * D_HEAD * d_c * io,
                 "flops": 4 * d_c * D_HEAD * rows * H + 2 * (2 * D_HEAD + D_ROPE) * pairs * H}
     return {"bytes": rows * row_bytes + tokens * ((row + d_c) * io + 4) + (8 * c["batch"] * T if kind == "tree" else 0),
             "flops": 2 * (row + d_c) * pairs * H}
