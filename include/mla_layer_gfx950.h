@@ -193,6 +193,38 @@ int mla_cache_store(const void* rows, const int32_t* positions, const double* fr
                     int d_c, int d_rope, int64_t row_pitch, int page_size, int num_pages, int max_pages_per_seq,
                     float gain, int layout, float eps, mla_dtype io_dtype, mla_dtype cache_dtype, void* hip_stream);
 
+/*
+ * mla_cache_store for rows whose place is not their position (a drafted tree's: node k
+ * of depth d turns by prefix + d and is stored at prefix + k).
+ *   slots  [B, new_tokens] int32: logical position that each row is written to, with
+ *          the rules that mla_cache_store has for positions; positions, any values, are
+ *          only what the rope part turns by
+ */
+int mla_cache_store_at(const void* rows, const int32_t* positions, const int32_t* slots, const double* freq,
+                       const void* norm_weight, void* kv_cache, float* kv_scale, const int32_t* page_table, int B,
+                       int new_tokens, int d_c, int d_rope, int64_t row_pitch, int page_size, int num_pages,
+                       int max_pages_per_seq, float gain, int layout, float eps, mla_dtype io_dtype,
+                       mla_dtype cache_dtype, void* hip_stream);
+
+/*
+ * Cache rows moved within their sequences: row dst[b, i] of sequence b becomes its row
+ * src[b, i], bit for bit, with its scale; e.g. the rows of a drafted tree's accepted path
+ * to the places behind the committed rows, where the next step expects them.  All rows
+ * of a sequence are read before any of them is written, so that places may be read and
+ * written by one call.
+ *
+ *   kv_cache  [num_pages, page_size, row_bytes] bytes; kv_scale [num_pages, page_size]
+ *             fp32 or NULL
+ *   src, dst  [B, moves] int32 logical positions, moves <= 64.  An entry of which either
+ *             lies outside the table, or on a page outside the pool, is skipped (-1 where
+ *             a sequence has fewer moves).  No two entries of a call may write the same
+ *             place, nor one write what another sequence's read (pages that sequences share)
+ * B <= 65535, row_bytes <= 4096.
+ */
+int mla_cache_move(void* kv_cache, float* kv_scale, const int32_t* page_table, const int32_t* src, const int32_t* dst,
+                   int B, int moves, int row_bytes, int page_size, int num_pages, int max_pages_per_seq,
+                   void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

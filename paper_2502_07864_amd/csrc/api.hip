@@ -13,8 +13,6 @@ namespace {
 
 bool io_ok(mla_dtype t) { return t == MLA_F32 || t == MLA_BF16; }
 
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
 // The most chunks that a request of num_splits chunks per sequence is cut into: x2 or x4 where the batch is too small for num_splits
 // to give every CU a workgroup.  Workspaces are sized for it, and the uniform partition is cut so: its chunks are parts of the page
 // table's width, which sequences may fill or not, and the lengths lie in device memory.  Fewer, longer chunks for one round of
@@ -353,24 +351,6 @@ int mla_merge_out_proj_multi(const void* workspace, size_t workspace_bytes, cons
     }
     return e == hipSuccess ? MLA_OK : MLA_ERR_HIP;
 }
-
-namespace {
-// (Sized for keys with their rope part and a page table for every pair, as callers have sized it: the keys and values take four fifths
-// of the pool's room, and rope parts that have to be copied, once for all heads, and their ids what they leave.)
-struct PrefillWs {
-    size_t pool_off, rope_off, ids_off, lens_off, total;
-};
-PrefillWs prefill_ws(int B, int heads, int d_c, int max_pages)
-{
-    PrefillWs w;
-    w.pool_off = align_up((size_t)heads * 256 * d_c * 2, 256);                                   // after Wcat
-    w.rope_off = w.pool_off + (size_t)B * heads * max_pages * 64 * 256 * 2;
-    w.ids_off = w.pool_off + align_up((size_t)B * heads * max_pages * 64 * 320 * 2, 256);
-    w.lens_off = w.ids_off + align_up((size_t)B * heads * max_pages * sizeof(int32_t), 256);
-    w.total = w.lens_off + align_up((size_t)B * heads * sizeof(int32_t), 256);
-    return w;
-}
-}  // namespace
 
 size_t mla_prefill_workspace_bytes(int B, int heads, int d_c, int max_pages_per_seq)
 {

@@ -112,12 +112,12 @@ extern "C" int mla_rope_queries(const void* q, const int32_t* positions, const d
     return status_of(launch_rope_queries(p, layout, io_dtype, static_cast<hipStream_t>(hip_stream)));
 }
 
-extern "C" int mla_cache_store(const void* rows, const int32_t* positions, const double* freq, const void* norm_weight,
-                               void* kv_cache, float* kv_scale, const int32_t* page_table, int B, int new_tokens, int d_c,
-                               int d_rope, int64_t row_pitch, int page_size, int num_pages, int max_pages_per_seq, float gain,
-                               int layout, float eps, mla_dtype io_dtype, mla_dtype cache_dtype, void* hip_stream)
+extern "C" int mla_cache_store_at(const void* rows, const int32_t* positions, const int32_t* slots, const double* freq, const void* norm_weight,
+                                  void* kv_cache, float* kv_scale, const int32_t* page_table, int B, int new_tokens, int d_c,
+                                  int d_rope, int64_t row_pitch, int page_size, int num_pages, int max_pages_per_seq, float gain,
+                                  int layout, float eps, mla_dtype io_dtype, mla_dtype cache_dtype, void* hip_stream)
 {
-    if (!rows || !positions || !kv_cache || !page_table || (d_rope > 0 && !freq)) return MLA_ERR_NULL;
+    if (!rows || !positions || !slots || !kv_cache || !page_table || (d_rope > 0 && !freq)) return MLA_ERR_NULL;
     if (B <= 0 || new_tokens <= 0 || d_c <= 0 || d_rope < 0 || d_rope % 2 || page_size <= 0 || num_pages <= 0 ||
         max_pages_per_seq <= 0 || row_pitch < (int64_t)d_c + d_rope || !(gain == gain) || !(eps >= 0.f))
         return MLA_ERR_SHAPE;
@@ -126,7 +126,27 @@ extern "C" int mla_cache_store(const void* rows, const int32_t* positions, const
     if (cache_dtype != MLA_F32 && cache_dtype != MLA_BF16 && cache_dtype != MLA_FP8_E4M3) return MLA_ERR_UNSUPPORTED;
     if (cache_dtype == MLA_FP8_E4M3 && !kv_scale) return MLA_ERR_NULL;
     if (cache_dtype != MLA_FP8_E4M3 && kv_scale) return MLA_ERR_SHAPE;
-    const StoreParams p{rows, positions, freq, norm_weight, kv_cache, kv_scale, page_table, B * new_tokens, new_tokens, d_c, d_rope,
+    const StoreParams p{rows, positions, slots, freq, norm_weight, kv_cache, kv_scale, page_table, B * new_tokens, new_tokens, d_c, d_rope,
                         page_size, num_pages, max_pages_per_seq, row_pitch, gain, eps};
     return status_of(launch_cache_store(p, layout, io_dtype, cache_dtype, static_cast<hipStream_t>(hip_stream)));
+}
+
+extern "C" int mla_cache_store(const void* rows, const int32_t* positions, const double* freq, const void* norm_weight,
+                               void* kv_cache, float* kv_scale, const int32_t* page_table, int B, int new_tokens, int d_c,
+                               int d_rope, int64_t row_pitch, int page_size, int num_pages, int max_pages_per_seq, float gain,
+                               int layout, float eps, mla_dtype io_dtype, mla_dtype cache_dtype, void* hip_stream)
+{
+    return mla_cache_store_at(rows, positions, positions, freq, norm_weight, kv_cache, kv_scale, page_table, B, new_tokens, d_c, d_rope,
+                              row_pitch, page_size, num_pages, max_pages_per_seq, gain, layout, eps, io_dtype, cache_dtype, hip_stream);
+}
+
+extern "C" int mla_cache_move(void* kv_cache, float* kv_scale, const int32_t* page_table, const int32_t* src, const int32_t* dst, int B,
+                              int moves, int row_bytes, int page_size, int num_pages, int max_pages_per_seq, void* hip_stream)
+{
+    if (!kv_cache || !page_table || !src || !dst) return MLA_ERR_NULL;
+    if (B <= 0 || moves <= 0 || row_bytes <= 0 || page_size <= 0 || num_pages <= 0 || max_pages_per_seq <= 0) return MLA_ERR_SHAPE;
+    if ((int64_t)max_pages_per_seq * page_size > 0x7FFFFFFF) return MLA_ERR_SHAPE;
+    if (moves > MAX_MOVES || B > 65535 || row_bytes > 4096) return MLA_ERR_UNSUPPORTED;
+    const MoveParams p{kv_cache, kv_scale, page_table, src, dst, B, moves, row_bytes, page_size, num_pages, max_pages_per_seq};
+    return status_of(launch_cache_move(p, static_cast<hipStream_t>(hip_stream)));
 }

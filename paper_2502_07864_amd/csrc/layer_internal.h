@@ -53,6 +53,7 @@ struct RopeParams {
 struct StoreParams {
     const void* rows;
     const int32_t* positions;
+    const int32_t* slots;      // where the rows go: positions, or slots of their own
     const double* freq;
     const void* norm_weight;   // or nullptr
     void* kv;
@@ -62,6 +63,18 @@ struct StoreParams {
     int64_t pitch;
     float gain, eps;
 };
+
+// Rows of a paged cache moved within their sequences: row dst[b, i] becomes row src[b, i].
+struct MoveParams {
+    void* kv;
+    float* kv_scale;            // or nullptr
+    const int32_t* page_table;
+    const int32_t* src;
+    const int32_t* dst;
+    int B, n, row_bytes, page_size, num_pages, max_pages;
+};
+constexpr int MAX_MOVES = 64;   // per sequence
+hipError_t launch_cache_move(const MoveParams& p, hipStream_t s);
 
 // the norm (norm = true) or the codes of x as it is
 hipError_t launch_rms_norm(const NormParams& p, bool norm, mla_dtype io, hipStream_t s);

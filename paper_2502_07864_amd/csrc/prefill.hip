@@ -418,7 +418,26 @@ __global__ __launch_bounds__(256) void prefill_rope_kernel(const uint16_t* kv, c
         dst[at * 64 * 64 + i] = kv[((size_t)page * 64 + (i >> 6)) * (d_c + 64) + d_c + (i & 63)];
 }
 
+// one workgroup per sequence; at most `width` pages each, which the caller has worked out from the same sizes
+__global__ __launch_bounds__(256) void window_pages_kernel(const int32_t* page_table, const int32_t* seq_lens, int32_t* pages, int32_t* lens,
+                                                           int q_len, int max_pages, int width, int window, int sinks)
+{
+    const int b = blockIdx.x, L = max(0, min(seq_lens[b], max_pages * 64));
+    const int64_t first = (int64_t)L - q_len - window + 1;                 // first row of the first query's window
+    const int head = (min(sinks, L) + 63) / 64, skip = max(0, (int)(max(first, (int64_t)0) / 64) - head);
+    if (threadIdx.x == 0) lens[b] = L - skip * 64;
+    const int n = min(width, (L + 63) / 64 - skip);
+    for (int i = threadIdx.x; i < n; i += 256) pages[(size_t)b * width + i] = page_table[(size_t)b * max_pages + (i < head ? i : i + skip)];
+}
+
 }  // namespace
+
+hipError_t launch_window_pages(const int32_t* page_table, const int32_t* seq_lens, int32_t* pages, int32_t* lens, int B, int q_len,
+                               int max_pages, int width, int window, int sinks, hipStream_t s)
+{
+    window_pages_kernel<<<dim3(B), 256, 0, s>>>(page_table, seq_lens, pages, lens, q_len, max_pages, width, window, sinks);
+    return hipGetLastError();
+}
 
 bool prefill_supported(int d_head, int d_c, int d_rope, int page_size, mla_dtype io, mla_dtype cache)
 {

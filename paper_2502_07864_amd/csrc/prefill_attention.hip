@@ -43,6 +43,10 @@ constexpr int PA_DR = 64;                   // and of its rope part
 constexpr int PA_DV = 128;                  // dimensions of a value
 constexpr int PA_ROWS = 128;                // query rows per workgroup
 
+// WINDOW: a query sees the keys of its window and the first ones only (p.window, p.sinks), and a workgroup meets the pages that its
+// queries see: the sinks' and, behind a jump, those from the first query's window on.  Keys are numbered as the pool has them; where
+// that leaves out pages that no query of the call sees, the windows lie behind the sinks' pages all the same.
+template <bool WINDOW>
 __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(PrefillParams p)
 {
     constexpr int ROWB = PA_DK * 2, ROPEB = PA_DR * 2;            // 256 and 128 bytes per key
@@ -135,14 +139,23 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
         store_nothing();
         return;
     }
-    const int t1 = (row1 + TILE_ROWS - 1) / TILE_ROWS;            // tiles [0, t1)
     // first key that some query row of this workgroup must not see (its first row sees the least)
     const int causal_from = visible(hb);
+    // pages [0, head) and, behind the jump, from head + jump on
+    int head = 0, jump = 0;
+    if constexpr (WINDOW) {
+        const int64_t first = (int64_t)causal_from - p.window;    // first key of the first query's window
+        head = (min(p.sinks, row1) + 63) / 64;
+        jump = max(0, (int)(max(first, (int64_t)0) / 64) - head);
+    }
+    auto page_of = [&](int u) { return !WINDOW || u < head ? u : u + jump; };
+    auto row_of = [&](int t) { return !WINDOW || t < 2 * head ? t * TILE_ROWS : t * TILE_ROWS + jump * 64; };
+    const int t1 = (row1 + TILE_ROWS - 1) / TILE_ROWS - 2 * jump; // tiles [0, t1), without those jumped over
 
     // Page ids, 64 at a time, a lane each (asked for beside the queries; a scalar load in every step was a wait in every step), and
     // whether all pages are there.  Of a page the cache does not have the values are zeros, and no query sees its keys.
     const int pages = (t1 + 1) / 2;
-    auto ids_from = [&](int u) { return u + lane < pages ? ptab[u + lane] : 0; };
+    auto ids_from = [&](int u) { return u + lane < pages ? ptab[page_of(u + lane)] : 0; };
     const int32_t first_ids = ids_from(0), more_ids[3] = {ids_from(64), ids_from(128), ids_from(192)};
     auto missing = [&](int32_t id) { return (uint32_t)id >= (uint32_t)p.num_pages; };
     auto usable = [&](int32_t id) { return missing(id) ? 0 : id; };
@@ -190,13 +203,14 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     // unit u (2 u < t1): all of its page behind the first tile's keys (the second tile's, where they are not asked for, are there but
     // never used), and the next page's first keys if there is one.  Returns the number of loads this thread issued (uniform).
     auto fetch_unit = [&](int u) -> int {
-        const unsigned char* src = pool + (size_t)u * PAGE_B + K_B;
+        const unsigned char* src = pool + (size_t)page_of(u) * PAGE_B + K_B;
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)((u & 1) * SLOT_B + wave * 1024));
         fetch_keys(src, dst, AtK1{});
         values_to(src, dst);
         load16(rope + rope_page / 2, roff, dst, AtR1{});
         if (2 * u + 2 >= t1) return NLK + NLV + 1;
-        fetch_keys(src + K2, dst, AtK2{});
+        if constexpr (WINDOW) fetch_keys(pool + (size_t)page_of(u + 1) * PAGE_B, dst, AtK2{});
+        else                  fetch_keys(src + K2, dst, AtK2{});
         if (((u + 1) & 63) == 0) {
             ids = usable(ids_from(u + 1));
             asm volatile("" : "+v"(ids));       // (waited for here: behind the branch everybody would, for everything)
@@ -208,7 +222,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     // the first tile's keys are there
     auto start = [&]() {
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)(SLOT_B + wave * 1024));
-        fetch_keys(pool, dst, AtK2{});
+        fetch_keys(pool + (size_t)page_of(0) * PAGE_B, dst, AtK2{});
         rope = rope_of(0);
         load16(rope, roff, dst, AtR2{});
         if (fetch_unit(0) > NLK + NLV + 1) wait_vmcnt<2 * NLK + NLV + 2>();
@@ -221,9 +235,15 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     for (int u = 256; u < pages; u += 64) hole |= missing(ids_from(u));
     const bool all_there = !__any(hole);
     // keys of tile t that are there
-    auto rows_valid = [&](int t) { return all_there || !missing(((const CONST_AS int32_t*)ptab)[t >> 1]) ? min(TILE_ROWS, row1 - t * TILE_ROWS) : 0; };
+    auto rows_valid = [&](int t) { return all_there || !missing(((const CONST_AS int32_t*)ptab)[page_of(t >> 1)]) ? min(TILE_ROWS, row1 - row_of(t)) : 0; };
     // leading tiles that every query row of this workgroup sees whole
     const int n_full = all_there ? max(0, min(causal_from, row1)) / TILE_ROWS : 0;
+    const int64_t last_from = (int64_t)visible(min(hb + PA_ROWS, p.q_len) - 1) - p.window;      // (WINDOW) first key of the last query's window
+    auto seen_whole = [&](int t) {
+        if constexpr (!WINDOW) return t < n_full;
+        const int row = row_of(t);
+        return all_there && row + TILE_ROWS <= min(causal_from, row1) && (row >= last_from || row + TILE_ROWS <= p.sinks);
+    };
 
     // ---- per-lane state: this lane's queries = column n of the D tiles of the two groups
     float m_ref[2] = {-INFINITY, -INFINITY};   // reference of the exponentials (log2 units)
@@ -260,12 +280,49 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
         v = fmaxf(v, __shfl_xor(v, 16));
         return fmaxf(v, __shfl_xor(v, 32));
     };
+    // (WINDOW) A key that a query does not see has the weight zero, but its values may be infinite or NaN (then its scores are, too):
+    // such values become zeros before they are multiplied.  Whoever sees the key has a NaN for its weight, or the weight zero where
+    // the score is -inf.  Every wavefront that met one does this for itself, and it does not matter who comes first.
+    bool dirty = false;
+    auto clean_values = [&](int at) {
+        for (int u = lane; u < V_B / 16; u += 64) {
+            LDS_AS u32x4* unit = (LDS_AS u32x4*)(lds + at + u * 16);
+            u32x4 v = *unit;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                if ((v[d] & 0x7F80u) == 0x7F80u) v[d] &= 0xFFFF0000u;
+                if ((v[d] & 0x7F800000u) == 0x7F800000u) v[d] &= 0xFFFFu;
+            }
+            *unit = v;
+        }
+        dirty = false;
+    };
     // keys a query must not see (or that are not there) at -inf
     auto mask = [&](Scores& x, int t) {
         // (few tiles take this: what it compares with is worked out here and not kept in registers)
         const int n_valid = rows_valid(t);
         int first = 4 * g;
         asm volatile("" : "+v"(first));
+        if constexpr (WINDOW) {
+            bool odd = false;
+            const int key = row_of(t) + first;
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+                const int end = visible(hb + my_row + hi * 16);
+                const int64_t from = (int64_t)end - p.window;
+#pragma unroll
+                for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int at = rb * 16 + i, j = key + at;
+                        if (first + at < n_valid && j < end && (j >= from || j < p.sinks)) continue;
+                        odd |= !(fabsf(x[rb][hi][i]) < INFINITY);
+                        x[rb][hi][i] = -INFINITY;
+                    }
+            }
+            dirty = __any(odd);
+            return;
+        }
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
             const int seen = min(n_valid, visible(hb + my_row + hi * 16) - t * TILE_ROWS) - first;
@@ -294,7 +351,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
         }
         __syncthreads();
     };
-    const bool late_values = row1 < L && row1 % TILE_ROWS != 0;
+    const bool late_values = !WINDOW && row1 < L && row1 % TILE_ROWS != 0;
 
     // ---- one step: S^T of the next tile (QK), the weights of this one from its scores x, the normaliser and the
     // values (PV).  The weights (two exponentials, a conversion and two multiply-adds per pair of scores) are
@@ -400,7 +457,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
             for (int ct = 0; ct < NCT; ++ct) oacc[hi][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
         auto look_at = [&](Scores& x, int t) {   // scores of tile t, just made
-            if (__builtin_expect(t >= n_full, 0)) mask(x, t);
+            if (__builtin_expect(!seen_whole(t), 0)) mask(x, t);
             raise_top(x);
             if (unset) set_reference(x);
         };
@@ -421,9 +478,11 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
             rk(unit, false, 1);
             if (t + 2 < t1) fetch_unit((t >> 1) + 1);
             if (late_values && t + 2 >= t1) drop_late_values(t1 - 1);
+            if (WINDOW && __builtin_expect(dirty, 0)) clean_values((int)unit + V0);
             step(Yes{}, No{}, unit, x, y);
             if (t + 1 >= t1) break;
             look_at(y, t + 1);
+            if (WINDOW && __builtin_expect(dirty, 0)) clean_values((int)unit + V1);
             step(Yes{}, Yes{}, unit, y, x);
             if (t + 2 < t1) look_at(x, t + 2);
             unit = SLOT_B - unit;
@@ -483,7 +542,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
         for (int hi = 0; hi < 2; ++hi)
             if (my_row + hi * 16 < HL)
                 p.lse[io_row(hb + my_row + hi * 16)] =
-                    lt[hi] > 0.f ? (m_ref[hi] + __builtin_amdgcn_logf(lt[hi])) * LN2 : -INFINITY;
+                    (WINDOW ? lt[hi] != 0.f : lt[hi] > 0.f) ? (m_ref[hi] + __builtin_amdgcn_logf(lt[hi])) * LN2 : -INFINITY;
     }
 }
 
@@ -495,7 +554,8 @@ hipError_t launch_prefill_attention(const PrefillParams& p, hipStream_t s)
     const long long Z = (p.q_len + PA_ROWS - 1) / PA_ROWS;
     const long long nwg = ((long long)p.pairs + 7) / 8 * 8 * Z;
     if (nwg > 0x7FFFFFFFLL) return hipErrorInvalidValue;
-    prefill_attention_kernel<<<dim3((unsigned)nwg), dim3(MF_THREADS), 0, s>>>(p);
+    if (p.window > 0) prefill_attention_kernel<true><<<dim3((unsigned)nwg), dim3(MF_THREADS), 0, s>>>(p);
+    else              prefill_attention_kernel<false><<<dim3((unsigned)nwg), dim3(MF_THREADS), 0, s>>>(p);
     return hipGetLastError();
 }
 

@@ -19,7 +19,24 @@ struct PrefillParams {
     void* out;                  // [B, q_len, heads, 128] bf16
     float* lse;                 // [B, q_len, heads], or nullptr
     float scale;
+    int window = 0, sinks = 0;  // window > 0: a query at row t sees the rows from t - window + 1 on, and those below sinks
 };
+
+// The workspace.  (Sized for keys with their rope part and a page table for every pair, as callers have sized it: the keys and values
+// take four fifths of the pool's room, and rope parts that have to be copied, once for all heads, and their ids what they leave.)
+struct PrefillWs {
+    size_t pool_off, rope_off, ids_off, lens_off, total;
+};
+inline PrefillWs prefill_ws(int B, int heads, int d_c, int max_pages)
+{
+    PrefillWs w;
+    w.pool_off = align_up((size_t)heads * 256 * d_c * 2, 256);                                   // after Wcat
+    w.rope_off = w.pool_off + (size_t)B * heads * max_pages * 64 * 256 * 2;
+    w.ids_off = w.pool_off + align_up((size_t)B * heads * max_pages * 64 * 320 * 2, 256);
+    w.lens_off = w.ids_off + align_up((size_t)B * heads * max_pages * sizeof(int32_t), 256);
+    w.total = w.lens_off + align_up((size_t)B * heads * sizeof(int32_t), 256);
+    return w;
+}
 
 bool       prefill_supported(int d_head, int d_c, int d_rope, int page_size, mla_dtype io, mla_dtype cache);
 // materialise [W_UK c | W_UV c] per pair into pool2, and the pairs' lengths
@@ -31,6 +48,10 @@ hipError_t launch_prefill_materialise(const void* kv, const int32_t* page_table,
 // ids there, [B, max_pages] (-1: not in the cache)
 hipError_t launch_prefill_rope(const void* kv, const int32_t* page_table, const int32_t* seq_lens, void* dst, int32_t* ids,
                                int B, int d_c, int num_pages, int max_pages, hipStream_t s);
+// The pages that some query of a call with a window sees (the sinks', then from the first query's window on), as a page table of
+// their own and the sequences' lengths without the rows left out between them
+hipError_t launch_window_pages(const int32_t* page_table, const int32_t* seq_lens, int32_t* pages, int32_t* lens, int B, int q_len,
+                               int max_pages, int width, int window, int sinks, hipStream_t s);
 hipError_t launch_prefill_attention(const PrefillParams& p, hipStream_t s);
 
 }  // namespace mla

@@ -167,7 +167,7 @@ __global__ __launch_bounds__(256) void rope_queries_any_kernel(RopeParams p)
 
 constexpr int MAX_ROW = 1024;
 
-// where row r, of position pos, goes: its row of the pool, or -1 where it has no place
+// where row r, of logical position pos, goes: its row of the pool, or -1 where it has no place
 __device__ __forceinline__ int64_t place_of(const StoreParams& p, int r, int pos)
 {
     if (pos < 0 || pos >= p.max_pages * p.page_size) return -1;                    // outside the table
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
     const int64_t row = (int64_t)r * p.pitch;
     const uint16_t* halves = static_cast<const uint16_t*>(p.rows) + row;
     const float* words = static_cast<const float*>(p.rows) + row;
-    const int pos = p.positions[r];
+    const int pos = p.positions[r], slot = p.slots[r];
     RawVec<F32, 8> v_raw[NV], w_raw[NV];
     float re[NV], im[NV];
     uint32_t k_raw[NV];
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreParams p)
         for (int i = 0; i < NV; ++i) w_raw[i] = raw_vec<F32, 8>(p.norm_weight, min(lane + i * 64, cv - 1) * 8);
     }
     __builtin_amdgcn_sched_barrier(0);
-    const int64_t at = place_of(p, r, pos);
+    const int64_t at = place_of(p, r, slot);
     if (at < 0) return;
     float v[NV][8];
 #pragma unroll
@@ -323,8 +323,8 @@ __global__ __launch_bounds__(256) void cache_store_any_kernel(StoreParams p)
     __shared__ uint32_t tops[4];
     const int r = blockIdx.x, tid = threadIdx.x;
     const int n = p.d_c + p.d_rope, pairs = p.d_rope / 2;
-    const int pos = p.positions[r];
-    const int64_t at = place_of(p, r, pos);
+    const int pos = p.positions[r], slot = p.slots[r];
+    const int64_t at = place_of(p, r, slot);
     if (at < 0) return;
     auto load = [&](const void* base, int64_t i) {
         return F32 ? static_cast<const float*>(base)[i] : bf16_bits_to_f32(static_cast<const uint16_t*>(base)[i]);

@@ -255,11 +255,12 @@ def rope_queries(q: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, g
 def cache_store(rows: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, kv_cache: torch.Tensor,
                 page_table: torch.Tensor, d_c: int, gain: float = 1.0, layout: int = ROPE_INTERLEAVED,
                 norm_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
-                kv_scale: Optional[torch.Tensor] = None) -> None:
+                kv_scale: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None) -> None:
     """Writes rows [B, new, d_c + d_rope] (may be apart) into kv_cache at logical positions [B, new]: the latent part
-    as it is or RMS-normed with norm_weight [d_c], the rope part turned by positions * freq."""
+    as it is or RMS-normed with norm_weight [d_c], the rope part turned by positions * freq.  slots [B, new]: logical
+    positions that the rows are written to where these are not what they turn by (a drafted tree's nodes)."""
     fast = mla._fast
-    if fast is not None:
+    if fast is not None and slots is None:
         status = fast.cache_store(rows, positions, freq, kv_cache, page_table, d_c, gain, layout, norm_weight, eps, kv_scale)
         if status == 0:
             return
@@ -283,8 +284,35 @@ def cache_store(rows: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor,
     px, pitch = _rows(rows, "rows", 1, row)[0], pitch if B * T > 1 else row
     if kv_scale is not None and (kv_scale.dtype != torch.float32 or tuple(kv_scale.shape) != (num_pages, page_size)):
         raise ValueError("kv_scale must be float32 [num_pages, page_size]")
-    args = (px, _dev(positions, "positions"), _dev(freq, "freq"), _like(norm_weight, rows, (int(d_c),), "norm_weight"),
+    if slots is not None and (slots.dtype != torch.int32 or slots.shape != (B, T) or slots.device != rows.device):
+        raise ValueError(f"slots must be int32 [B, new] on {rows.device}")
+    args = (_dev(freq, "freq"), _like(norm_weight, rows, (int(d_c),), "norm_weight"),
             _dev(kv_cache, "kv_cache"), _dev(kv_scale, "kv_scale"), _dev(page_table, "page_table"), B, T, int(d_c), d_rope, pitch,
             page_size, num_pages, page_table.shape[1], float(gain), int(layout), float(eps), _io_code(rows), _cache_code(kv_cache),
             _stream(rows))
-    _check(lib().mla_cache_store(*args), "mla_cache_store")
+    turns = (px, _dev(positions, "positions"))
+    if slots is None:
+        _check(lib().mla_cache_store(*turns, *args), "mla_cache_store")
+    else:
+        _check(lib().mla_cache_store_at(*turns, _dev(slots, "slots"), *args), "mla_cache_store_at")
+
+
+def cache_move(kv_cache: torch.Tensor, page_table: torch.Tensor, src: torch.Tensor, dst: torch.Tensor,
+               kv_scale: Optional[torch.Tensor] = None) -> None:
+    """Row dst[b, i] of sequence b becomes its row src[b, i], bit for bit, with its scale; src and dst [B, moves] int32
+    logical positions, moves <= 64, -1 for none.  All rows of a sequence are read before any is written."""
+    if kv_cache.dim() != 3 or page_table.dim() != 2 or src.dim() != 2:
+        raise ValueError("kv_cache must be [num_pages, page_size, d_c + d_rope], page_table [B, max_pages_per_seq], src [B, moves]")
+    num_pages, page_size, row = kv_cache.shape
+    B, n = src.shape
+    if page_table.dtype != torch.int32 or src.dtype != torch.int32 or dst.dtype != torch.int32:
+        raise TypeError("page_table, src and dst must be int32")
+    if page_table.shape[0] != B or dst.shape != src.shape:
+        raise ValueError("page_table must be [B, max_pages_per_seq], dst [B, moves]")
+    if (kv_scale is not None) != (_cache_code(kv_cache) == mla.FP8_E4M3):
+        raise ValueError("an 8-bit cache has scales, others have none")
+    if kv_scale is not None and (kv_scale.dtype != torch.float32 or tuple(kv_scale.shape) != (num_pages, page_size)):
+        raise ValueError("kv_scale must be float32 [num_pages, page_size]")
+    mla._together(kv_cache, kv_scale=kv_scale, page_table=page_table, src=src, dst=dst)
+    mla._call_on(kv_cache, "mla_cache_move", _dev(kv_cache, "kv_cache"), _dev(kv_scale, "kv_scale"), _dev(page_table, "page_table"),
+                 _dev(src, "src"), _dev(dst, "dst"), B, n, row * kv_cache.element_size(), page_size, num_pages, page_table.shape[1])

@@ -31,7 +31,10 @@ EXPORTS = ("mla_status_string", "mla_version", "mla_absorb_q", "mla_out_proj",
            "mla_static_scratch_bytes", "mla_decode_paged_static", "mla_diag_stream_tiles",
            # the operators around the attention (include/mla_layer_gfx950.h), called from layer.py
            "mla_rms_norm", "mla_quantize_rows", "mla_quantize_weights", "mla_gemm_fp8_workspace_bytes", "mla_gemm_fp8",
-           "mla_rope_frequencies", "mla_rope_queries", "mla_cache_store")
+           "mla_rope_frequencies", "mla_rope_queries", "mla_cache_store", "mla_cache_store_at", "mla_cache_move",
+           # masked attention (include/mla_masked_gfx950.h)
+           "mla_decode_tree_workspace_bytes", "mla_decode_paged_tree", "mla_decode_window_workspace_bytes", "mla_decode_paged_window",
+           "mla_prefill_window_workspace_bytes", "mla_prefill_window")
 
 
 class MlaError(RuntimeError):
@@ -121,6 +124,22 @@ def lib() -> ctypes.CDLL:
         L.mla_rope_queries.argtypes = [vp] * 5 + [i, i, i, i, i64, f, i, i, vp]
         L.mla_cache_store.restype = i
         L.mla_cache_store.argtypes = [vp] * 7 + [i, i, i, i, i64, i, i, i, f, i, f, i, i, vp]
+        L.mla_cache_store_at.restype = i
+        L.mla_cache_store_at.argtypes = [vp] * 8 + [i, i, i, i, i64, i, i, i, f, i, f, i, i, vp]
+        L.mla_cache_move.restype = i
+        L.mla_cache_move.argtypes = [vp] * 5 + [i] * 6 + [vp]
+        L.mla_decode_tree_workspace_bytes.restype = ctypes.c_size_t
+        L.mla_decode_tree_workspace_bytes.argtypes = [i] * 5
+        L.mla_decode_paged_tree.restype = i
+        L.mla_decode_paged_tree.argtypes = [vp] * 7 + [i64, vp, vp, vp, ctypes.c_size_t] + [i] * 8 + [f, i, i, u, vp]
+        L.mla_decode_window_workspace_bytes.restype = ctypes.c_size_t
+        L.mla_decode_window_workspace_bytes.argtypes = [i] * 7
+        L.mla_decode_paged_window.restype = i
+        L.mla_decode_paged_window.argtypes = [vp] * 9 + [ctypes.c_size_t] + [i] * 10 + [f, i, i, u, vp]
+        L.mla_prefill_window_workspace_bytes.restype = ctypes.c_size_t
+        L.mla_prefill_window_workspace_bytes.argtypes = [i] * 7
+        L.mla_prefill_window.restype = i
+        L.mla_prefill_window.argtypes = [vp] * 10 + [ctypes.c_size_t] + [i] * 11 + [f, i, i, vp]
         _lib, _fast = L, _load_marshal(L)
     return _lib
 
@@ -430,6 +449,156 @@ def prefill_mha(q_nope: torch.Tensor, q_rope: torch.Tensor, W_UK: torch.Tensor, 
         workspace.numel() * workspace.element_size(), B, T, H, d_head, d_c, d_rope, page_size, num_pages,
         page_table.shape[1], float(softmax_scale), _io_code(q_nope), _cache_code(kv_cache),
         _stream(q_nope)), "mla_prefill_mha")
+    return (out, lse) if lse is not None else out
+
+
+# Masked attention (include/mla_masked_gfx950.h).  These calls check the shapes of everything they write, and run on the
+# device of their tensors whichever is current.
+
+def _together(first: torch.Tensor, **others: Optional[torch.Tensor]):
+    for name, t in others.items():
+        if t is not None and t.device != first.device:
+            raise ValueError(f"{name} must be on {first.device}, got {t.device}")
+
+
+def _call_on(t: torch.Tensor, name: str, *args):
+    if t.device.index == torch.cuda.current_device():
+        status = getattr(lib(), name)(*args, _stream(t))
+    else:
+        with torch.cuda.device(t.device):
+            status = getattr(lib(), name)(*args, _stream(t))
+    _check(status, name)
+
+
+def _result(t: Optional[torch.Tensor], like: torch.Tensor, shape, dtype: torch.dtype, name: str) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)} of {dtype}, got {list(t.shape)} of {t.dtype}")
+    return t
+
+
+def _decode_masked(q_abs, q_rope, kv_cache, page_table, lens, kv_scale):
+    """Shapes of a decode call with q_len query tokens per sequence: (B, T, H, d_c, d_rope)."""
+    if q_abs.dim() != 4 or kv_cache.dim() != 3:
+        raise ValueError("q_abs must be [B, q_len, H, d_c], kv_cache [num_pages, page_size, d_c + d_rope]")
+    B, T, H, d_c = q_abs.shape
+    num_pages, page_size, row = kv_cache.shape
+    d_rope = row - d_c
+    if d_rope < 0:
+        raise ValueError("cache rows are shorter than d_c")
+    if d_rope and (q_rope is None or tuple(q_rope.shape) != (B, T, H, d_rope) or q_rope.dtype != q_abs.dtype):
+        raise ValueError("q_rope must be [B, q_len, H, d_rope] of q_abs's dtype")
+    if page_table.dtype != torch.int32 or lens.dtype != torch.int32:
+        raise TypeError("page_table and lengths must be int32")
+    if page_table.dim() != 2 or page_table.shape[0] != B or lens.shape != (B,):
+        raise ValueError("page_table must be [B, max_pages_per_seq], lengths [B]")
+    if kv_scale is not None and (kv_scale.dtype != torch.float32 or tuple(kv_scale.shape) != (num_pages, page_size)):
+        raise ValueError("kv_scale must be float32 [num_pages, page_size]")
+    return B, T, H, d_c, d_rope
+
+
+def decode_tree_workspace_bytes(B: int, q_len: int, H: int, d_c: int, max_rows: int) -> int:
+    """max_rows: page_size * max_pages_per_seq."""
+    return int(lib().mla_decode_tree_workspace_bytes(B, q_len, H, d_c, max_rows))
+
+
+def decode_paged_tree(q_abs: torch.Tensor, q_rope: Optional[torch.Tensor], kv_cache: torch.Tensor, page_table: torch.Tensor,
+                      prefix_lens: torch.Tensor, tree_mask: torch.Tensor, softmax_scale: float,
+                      kv_scale: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, return_lse: bool = False,
+                      flags: int = 0):
+    """Paged absorbed attention of a drafted tree's tokens.  q_abs [B,q_len,H,d_c], q_rope [B,q_len,H,d_rope]; the cache
+    holds prefix_lens[b] committed rows and behind them the drafted tokens' rows, token k's at position prefix + k; token i
+    sees the committed rows and drafted row k iff bit k of tree_mask[b, i] is set (int64 [B, q_len], or [q_len]: one tree
+    for all; q_len <= 64).  Returns o_lat [B,q_len,H,d_c] (and lse [B,q_len,H] fp32 if return_lse or lse given)."""
+    B, T, H, d_c, d_rope = _decode_masked(q_abs, q_rope, kv_cache, page_table, prefix_lens, kv_scale)
+    if tree_mask.dtype not in (torch.int64, torch.uint64):
+        raise TypeError("tree_mask must be int64 or uint64")
+    if tuple(tree_mask.shape) not in ((B, T), (T,)):
+        raise ValueError("tree_mask must be [B, q_len] or [q_len]")
+    num_pages, page_size, _ = kv_cache.shape
+    out = _result(out, q_abs, (B, T, H, d_c), q_abs.dtype, "out")
+    if lse is not None or return_lse:
+        lse = _result(lse, q_abs, (B, T, H), torch.float32, "lse")
+    if workspace is None:
+        workspace = torch.empty(max(256, decode_tree_workspace_bytes(B, T, H, d_c, page_size * page_table.shape[1])), dtype=torch.uint8,
+                                device=q_abs.device)
+    _together(q_abs, q_rope=q_rope, kv_cache=kv_cache, kv_scale=kv_scale, page_table=page_table, prefix_lens=prefix_lens,
+              tree_mask=tree_mask, workspace=workspace, out=out, lse=lse)
+    _call_on(q_abs, "mla_decode_paged_tree", _dev(q_abs, "q_abs"), _dev(q_rope, "q_rope"), _dev(kv_cache, "kv_cache"), _dev(kv_scale, "kv_scale"),
+             _dev(page_table, "page_table"), _dev(prefix_lens, "prefix_lens"), _dev(tree_mask, "tree_mask"), T if tree_mask.dim() == 2 else 0,
+             _dev(out, "out"), _dev(lse, "lse"), _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), B, T, H, d_c,
+             d_rope, page_size, num_pages, page_table.shape[1], float(softmax_scale), _io_code(q_abs), _cache_code(kv_cache), int(flags))
+    return (out, lse) if lse is not None else out
+
+
+def decode_window_workspace_bytes(B: int, q_len: int, H: int, d_c: int, max_rows: int, window: int, sinks: int) -> int:
+    """max_rows: page_size * max_pages_per_seq."""
+    return int(lib().mla_decode_window_workspace_bytes(B, q_len, H, d_c, max_rows, window, sinks))
+
+
+def decode_paged_window(q_abs: torch.Tensor, q_rope: Optional[torch.Tensor], kv_cache: torch.Tensor, page_table: torch.Tensor,
+                        seq_lens: torch.Tensor, window: int, sinks: int, softmax_scale: float,
+                        kv_scale: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, return_lse: bool = False,
+                        flags: int = 0):
+    """decode_paged_multi with a sliding window and a few first rows that stay visible: token i, at position
+    t = seq_len - q_len + i, sees row j <= t iff j > t - window or j < sinks.  Pages whose rows no token sees are not read
+    and may have been given back (-1 in the table)."""
+    B, T, H, d_c, d_rope = _decode_masked(q_abs, q_rope, kv_cache, page_table, seq_lens, kv_scale)
+    num_pages, page_size, _ = kv_cache.shape
+    out = _result(out, q_abs, (B, T, H, d_c), q_abs.dtype, "out")
+    if lse is not None or return_lse:
+        lse = _result(lse, q_abs, (B, T, H), torch.float32, "lse")
+    if workspace is None:
+        need = decode_window_workspace_bytes(B, T, H, d_c, page_size * page_table.shape[1], window, sinks)
+        workspace = torch.empty(max(256, need), dtype=torch.uint8, device=q_abs.device)
+    _together(q_abs, q_rope=q_rope, kv_cache=kv_cache, kv_scale=kv_scale, page_table=page_table, seq_lens=seq_lens, workspace=workspace,
+              out=out, lse=lse)
+    _call_on(q_abs, "mla_decode_paged_window", _dev(q_abs, "q_abs"), _dev(q_rope, "q_rope"), _dev(kv_cache, "kv_cache"), _dev(kv_scale, "kv_scale"),
+             _dev(page_table, "page_table"), _dev(seq_lens, "seq_lens"), _dev(out, "out"), _dev(lse, "lse"), _dev(workspace, "workspace"),
+             workspace.numel() * workspace.element_size(), B, T, H, d_c, d_rope, page_size, num_pages, page_table.shape[1], int(window),
+             int(sinks), float(softmax_scale), _io_code(q_abs), _cache_code(kv_cache), int(flags))
+    return (out, lse) if lse is not None else out
+
+
+def prefill_window_workspace_bytes(B: int, q_len: int, H: int, d_c: int, max_pages_per_seq: int, window: int, sinks: int) -> int:
+    return int(lib().mla_prefill_window_workspace_bytes(B, q_len, H, d_c, max_pages_per_seq, window, sinks))
+
+
+def prefill_window(q_nope: torch.Tensor, q_rope: torch.Tensor, W_UK: torch.Tensor, W_UV: torch.Tensor, kv_cache: torch.Tensor,
+                   page_table: torch.Tensor, seq_lens: torch.Tensor, window: int, sinks: int, softmax_scale: float,
+                   workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   lse: Optional[torch.Tensor] = None, return_lse: bool = False):
+    """prefill_mha under decode_paged_window's mask; keys and values are materialised for the rows that some token of the
+    call sees.  q_nope [B,q_len,H,d_head], q_rope [B,q_len,H,d_rope] -> out [B,q_len,H,d_head] (and lse [B,q_len,H])."""
+    if q_nope.dim() != 4 or W_UK.dim() != 3 or kv_cache.dim() != 3:
+        raise ValueError("q_nope must be [B, q_len, H, d_head], W_UK [H, d_head, d_c], kv_cache [num_pages, page_size, d_c + d_rope]")
+    B, T, H, d_head = q_nope.shape
+    H2, d_head2, d_c = W_UK.shape
+    num_pages, page_size, row = kv_cache.shape
+    d_rope = row - d_c
+    if (H2, d_head2) != (H, d_head) or tuple(W_UV.shape) != (H, d_c, d_head) or W_UK.dtype != q_nope.dtype or W_UV.dtype != q_nope.dtype:
+        raise ValueError("W_UK must be [H, d_head, d_c] and W_UV [H, d_c, d_head] of q_nope's dtype")
+    if tuple(q_rope.shape) != (B, T, H, d_rope) or q_rope.dtype != q_nope.dtype:
+        raise ValueError("q_rope must be [B, q_len, H, d_rope] of q_nope's dtype")
+    if page_table.dtype != torch.int32 or seq_lens.dtype != torch.int32:
+        raise TypeError("page_table and seq_lens must be int32")
+    if page_table.dim() != 2 or page_table.shape[0] != B or seq_lens.shape != (B,):
+        raise ValueError("page_table must be [B, max_pages_per_seq], seq_lens [B]")
+    out = _result(out, q_nope, (B, T, H, d_head), q_nope.dtype, "out")
+    if lse is not None or return_lse:
+        lse = _result(lse, q_nope, (B, T, H), torch.float32, "lse")
+    if workspace is None:
+        workspace = torch.empty(max(256, prefill_window_workspace_bytes(B, T, H, d_c, page_table.shape[1], window, sinks)),
+                                dtype=torch.uint8, device=q_nope.device)
+    _together(q_nope, q_rope=q_rope, W_UK=W_UK, W_UV=W_UV, kv_cache=kv_cache, page_table=page_table, seq_lens=seq_lens,
+              workspace=workspace, out=out, lse=lse)
+    _call_on(q_nope, "mla_prefill_window", _dev(q_nope, "q_nope"), _dev(q_rope, "q_rope"), _dev(W_UK, "W_UK"), _dev(W_UV, "W_UV"),
+             _dev(kv_cache, "kv_cache"), _dev(page_table, "page_table"), _dev(seq_lens, "seq_lens"), _dev(out, "out"), _dev(lse, "lse"),
+             _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), B, T, H, d_head, d_c, d_rope, page_size, num_pages,
+             page_table.shape[1], int(window), int(sinks), float(softmax_scale), _io_code(q_nope), _cache_code(kv_cache))
     return (out, lse) if lse is not None else out
 
 
