@@ -1,0 +1,604 @@
+// Masked attention over the latent cache on the matrix cores (bf16 queries, bf16 or fp8 cache): 128 query rows per workgroup.
+//
+//   S^T [keys x rows]  = K [keys x (d_c + 64)] . Q^T [(d_c + 64) x rows]
+//   O^T [d_c x rows]  += V^T [d_c x keys] . P^T [keys x rows],      V = the first d_c columns of K
+//
+// A wavefront owns 32 query rows (two groups of 16), their queries in registers for as long as it lives, their whole outputs
+// (d_c x 32 fp32 values) and a softmax of its own: no exchange of scores or weights, one workgroup barrier per tile of 32 keys.
+// Both contractions run on v_mfma_f32_16x16x32_bf16 with every LDS read feeding two of them.  The second one needs the tile
+// transposed: each wavefront transposes a quarter of the columns (transposing LDS reads, one 16-byte write per lane and 16
+// columns) for all four, so that the values are read in plain 128-bit reads.  Transposing reads by everybody would be
+// 64 x 26 cycles of LDS issue a tile and wavefront beside the 36 x 17 of the scores, more than the 2176 cycles of matrix
+// instructions; so it is 68 x 17 + 16 x 26 + 8 x 17 = 1708.
+//
+// A step scores tile i + 1 (and weighs tile i between its matrix instructions), then accumulates tile i (and transposes tile
+// i + 1), while tile i + 2 is on its way (direct-to-LDS loads; fp8 codes through registers, widened to bf16, which is exact).
+// Two slots for tiles and two for their transposes: 136 KB of LDS at d_c = 512, one workgroup per CU.
+//
+// The reference of a query row's exponentials is the maximum of the first tile with a row it sees, and nothing is rescaled; where a
+// score exceeds it by more than 2^64 the chunk is done again against the exact maxima.  The normaliser sums the weights before
+// their rounding to bf16 in fp32; the weights' rounding (2^-8 of each) is the price of the bf16 instructions.
+//
+// Keys that a row does not see get the score -inf, in the tiles that need it.  There every wavefront also looks for values that are
+// not finite in the columns it has transposed; where there are any, they are cleared before anybody multiplies, and the rows that do see
+// such a key end as NaN.
+#include "masked_internal.h"
+#include "mfma_tile.h"
+#include <type_traits>
+
+namespace mla {
+namespace {
+
+constexpr int MT_ROWS = MK_TALL_ROWS;        // query rows per workgroup
+
+template <int D_C, bool FP8>
+__global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams p)
+{
+    constexpr int ROW = D_C + 64, ROWB = ROW * 2;       // of a tile in LDS (bf16)
+    constexpr int CPR = ROWB / 16;                      // 16-byte chunks per row (72 / 40)
+    constexpr int TILE_B = MK_TILE * ROWB;
+    constexpr int NLOAD = TILE_B / (MF_THREADS * 16);   // 16-byte loads per thread and bf16 tile (9 / 5)
+    constexpr int NKS = ROW / 32;                       // k-steps of the scores (18 / 10)
+    constexpr int NCT = D_C / 16;                       // column tiles of the values (32 / 16)
+    constexpr int VT_B = D_C * MK_TILE * 2;             // a transposed tile
+    constexpr int CODES = MK_TILE * ROW / 16;           // 16-byte pieces of an fp8 tile (1152 / 640)
+    constexpr int NCODE = (CODES + MF_THREADS - 1) / MF_THREADS;     // per thread (5 / 3, the last by some)
+
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * TILE_B + 2 * VT_B];
+    __shared__ __attribute__((aligned(16))) float ks_smem[2][MK_TILE];        // scales of an fp8 tile's rows
+    __shared__ uint64_t tree_smem[64];
+    __shared__ __attribute__((aligned(16))) uint32_t odd_smem[2][4];          // keys of a tile whose values are not all finite, by wavefront
+    LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
+    LDS_AS float* ks_lds = (LDS_AS float*)ks_smem;
+    LDS_AS uint32_t* odd_lds = (LDS_AS uint32_t*)odd_smem;
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, g = lane >> 4;
+
+    // the groups of query rows of one chunk get linear ids 8 apart: same XCD, same time, so all but the first find the rows in its L2
+    const int Z = (p.H + MT_ROWS - 1) / MT_ROWS;
+    const int id = blockIdx.x, rr = id >> 3;
+    const int wg = (rr / Z) * 8 + (id & 7), zi = rr % Z;
+    if (wg >= p.B * p.num_splits) return;               // padding of the last group of 8
+    const int split = wg % p.num_splits, b = wg / p.num_splits;
+    const int hb = zi * MT_ROWS, HL = min(MT_ROWS, p.H - hb);
+
+    const bool tree = p.tree != nullptr;
+    const int32_t len = ((const CONST_AS int32_t*)p.lens)[b];
+    const Reach reach = reach_of(len, p.q_len, p.max_pages * p.page_size, tree, p.window, p.sinks);
+    const int v0 = chunk_start(reach.tiles, split, p.num_splits), v1 = chunk_start(reach.tiles, split + 1, p.num_splits);
+
+    const int nrow = min(32, HL - wave * 32);           // this wavefront's query rows (may be none: it still loads and transposes)
+    auto part_of = [&](int r) { return part_index(b, hb + wave * 32 + r, split, p.H, p.num_splits); };
+    if (v0 >= v1) {                                     // nothing to see
+        for (int r = 0; r < nrow; ++r) {
+            if (p.num_splits == 1)
+                for (int c = lane * 8; c < D_C; c += 512)
+                    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.o_part) + part_of(r) * D_C + c) = (u32x4){0u, 0u, 0u, 0u};
+            if (lane == 0 && p.lse_part) p.lse_part[part_of(r)] = -INFINITY;
+        }
+        return;
+    }
+
+    // ---- tiles: v is a tile's number without the gap; its rows lie on one page (page sizes are multiples of 32)
+    const CONST_AS int32_t* ptab = (const CONST_AS int32_t*)(p.page_table + (size_t)b * p.max_pages);
+    const int per_page = p.page_size / MK_TILE;
+    struct Place {
+        int row;          // first row of the tile in the sequence
+        int valid;        // rows that are there
+        size_t at;        // and in the pool
+    };
+    auto place_of = [&](int v) {
+        const int t = reach.tile(min(v, v1 - 1)), q = t / per_page;
+        const int page = ptab[q];
+        const bool there = page >= 0 && page < p.num_pages;
+        return Place{t * MK_TILE, there ? min(MK_TILE, reach.end - t * MK_TILE) : 0, (size_t)(there ? page : 0) * p.page_size + (t - q * per_page) * MK_TILE};
+    };
+
+    const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
+    uint32_t goff[NLOAD];                               // bf16: this thread's pieces, chunk c of row r at position c ^ key(r)
+    if constexpr (!FP8) {
+#pragma unroll
+        for (int k = 0; k < NLOAD; ++k) {
+            const int q = k * MF_THREADS + tid, r = q / CPR, c = q % CPR;
+            goff[k] = (uint32_t)(r * ROWB + ((c ^ swz_key(r)) << 4));
+        }
+    }
+    u32x4 codes[FP8 ? NCODE : 1];
+    float my_scale = 1.f;
+    // tile v -> slot v & 1: the loads (fp8: into registers)
+    auto request = [&](const Place& at, int v) {
+        if (at.valid <= 0) return;                      // a page outside the pool is never dereferenced
+        if constexpr (FP8) {
+            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + at.at * ROW;
+#pragma unroll
+            for (int k = 0; k < NCODE; ++k) {
+                const int q = min(k * MF_THREADS + tid, CODES - 1);
+                codes[k] = *reinterpret_cast<const u32x4*>(src + q * 16);
+            }
+            if (tid < MK_TILE) my_scale = tid < at.valid ? p.kv_scale[at.at + tid] : 1.f;
+        } else {
+            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + at.at * ROWB;
+            const uint32_t dst = lds_base + (uint32_t)((v & 1) * TILE_B + wave * 1024);
+#pragma unroll
+            for (int k = 0; k < NLOAD; ++k) {
+                const uint32_t m0v = __builtin_amdgcn_readfirstlane(dst + k * 4096);
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                             :: "s"(m0v), "v"(goff[k]), "s"(src) : "memory");
+            }
+        }
+    };
+    // (fp8) the requested codes, widened, into the slot of tile v
+    auto put = [&](int v) {
+        if constexpr (FP8) {
+            LDS_AS unsigned char* slot = lds + (v & 1) * TILE_B;
+#pragma unroll
+            for (int k = 0; k < NCODE; ++k) {
+                const int q = k * MF_THREADS + tid;
+                if (q >= CODES) continue;
+                const int r = q / (CPR / 2), c = q % (CPR / 2) * 2;
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[k][i], 1.f, false));
+                    w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[k][i], 1.f, true));
+                }
+                *(LDS_AS u32x4*)(slot + r * ROWB + ((c ^ swz_key(r)) << 4)) = (u32x4){w[0], w[1], w[2], w[3]};
+                *(LDS_AS u32x4*)(slot + r * ROWB + (((c + 1) ^ swz_key(r)) << 4)) = (u32x4){w[4], w[5], w[6], w[7]};
+            }
+            if (tid < MK_TILE) ks_lds[(v & 1) * MK_TILE + tid] = my_scale;
+        }
+    };
+
+    // the first tile, and (fp8) the second one's codes
+    Place here, next, after;
+    auto start = [&]() {
+        here = place_of(v0);
+        next = place_of(v0 + 1);
+        request(here, v0);
+        if constexpr (FP8) {
+            put(v0);
+            request(next, v0 + 1);
+        }
+    };
+    start();
+
+    // ---- this wavefront's query rows -> registers (B operands of the scores).  A negative scale changes their sign: the largest score is
+    // then the largest scaled one
+    bf16x8 qreg[2][NKS];
+    {
+        const uint16_t* qa = static_cast<const uint16_t*>(p.q_abs) + (size_t)b * p.H * D_C;
+        const uint16_t* qr = static_cast<const uint16_t*>(p.q_rope) + (size_t)b * p.H * 64;
+        const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+            const size_t row = hb + min(wave * 32 + hi * 16 + n, HL - 1);
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) {
+                u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + ks * 32 + g * 8)
+                                        : *reinterpret_cast<const u32x4*>(qr + row * 64 + (ks - D_C / 32) * 32 + g * 8);
+                v ^= (u32x4){flip, flip, flip, flip};
+                qreg[hi][ks] = __builtin_bit_cast(bf16x8, v);
+            }
+        }
+    }
+    if (tree && tid < p.q_len) tree_smem[tid] = p.tree[b * p.tree_pitch + tid] & (p.q_len < 64 ? (1ull << p.q_len) - 1 : ~0ull);
+    const int token[2] = {(hb + min(wave * 32 + n, HL - 1)) / p.heads, (hb + min(wave * 32 + 16 + n, HL - 1)) / p.heads};
+    const int first_at = reach.base + hb / p.heads, last_at = reach.base + (hb + HL - 1) / p.heads;     // (a window) positions of the workgroup's tokens
+
+    // ---- per-lane state: this lane's queries = column n of the D tiles of the two groups
+    float m_ref[2] = {-INFINITY, -INFINITY};   // reference of the exponentials (log2 units)
+    float l_run[2] = {0.f, 0.f};               // this lane's share of the normaliser
+    f32x4 oacc[2][NCT];
+    // (never zero: a masked score is -inf and has to stay it)
+    const float sc = fmaxf(fabsf(p.scale) * LOG2E, 1.17549435e-38f);
+
+    // score A operand: key row 16 rb + n, chunk 4 ks + g
+    uint32_t a_base[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) a_base[e] = (uint32_t)(n * ROWB) + ((((uint32_t)(4 * e + g)) ^ (uint32_t)swz_key(n)) << 4);
+    // transposing reads: the lane supplies tile row 4g + (n >> 2) (and 16 more), 8 bytes at column 16 ct + 4 (n & 3)
+    uint32_t t_base[4];
+    {
+        const int r = g * 4 + (n >> 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            t_base[e] = (uint32_t)(r * ROWB) + ((((uint32_t)(2 * e) + (uint32_t)((n & 3) >> 1)) ^ (uint32_t)swz_key(r)) << 4) + (uint32_t)((n & 1) * 8);
+    }
+    LDS_AS unsigned char* const vt = lds + 2 * TILE_B;
+
+    typedef f32x4 Scores[2][2];                // [block of 16 keys][query group]: keys 16 rb + 4g + i of query n
+    f32x4 ksc[2];                              // (fp8) scales of this lane's keys
+    bool poisoned[2] = {false, false};         // one of this lane's keys that its query sees was not finite
+
+    // rows of the tile (bit: row) that the lane's query of group hi sees
+    auto visible = [&](const Place& at, int hi) -> uint32_t {
+        auto low = [](int k) -> uint32_t { return k <= 0 ? 0u : k >= 32 ? ~0u : (1u << k) - 1u; };
+        uint32_t sees;
+        if (tree) {
+            const uint64_t m = tree_smem[token[hi]];
+            const int d = reach.base - at.row;             // committed rows of the tile
+            sees = d >= 32 ? ~0u : d > 0 ? (uint32_t)(m << d) | low(d) : d > -64 ? (uint32_t)(m >> -d) : 0u;
+        } else {
+            const int t = reach.base + token[hi];
+            const int64_t from = (int64_t)t - p.window + 1 - at.row;
+            const uint32_t old = low(from < 0 ? 0 : from > 32 ? 32 : (int)from), sunk = low(p.sinks - at.row);
+            sees = low(t + 1 - at.row) & (~old | sunk);
+        }
+        return sees & low(at.valid);
+    };
+    auto seen_whole = [&](const Place& at) {
+        if (at.valid < MK_TILE) return false;
+        if (tree) return at.row + MK_TILE <= reach.base;
+        return at.row + MK_TILE - 1 <= first_at && ((int64_t)at.row > (int64_t)last_at - p.window || at.row + MK_TILE <= p.sinks);
+    };
+    auto mask = [&](Scores& x, const Place& at, int v) {
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+            const uint32_t sees = visible(at, hi) >> (4 * g);
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (sees >> (rb * 16 + i) & 1u) {
+                        if (FP8) poisoned[hi] |= !(fabsf(ksc[rb][i]) < INFINITY);
+                    } else {
+                        x[rb][hi][i] = -INFINITY;
+                    }
+                }
+        }
+        if constexpr (FP8) {                   // (nothing is multiplied with a scale that is not finite)
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ksc[rb][i] = fabsf(ksc[rb][i]) < INFINITY ? ksc[rb][i] : 0.f;
+        }
+        // a lane holds keys 4g .. 4g + 3 and 16 on of a column
+        uint32_t odd[4] = {0u, 0u, 0u, 0u};
+        LDS_AS unsigned char* const share = vt + (v & 1) * VT_B + wave * (VT_B / 4) + lane * 16;
+        for (int k = 0; k < NCT / 4; ++k) {
+            const u32x4 w = *(LDS_AS u32x4*)(share + k * 1024);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) odd[d] |= ((w[d] & 0x7F80u) == 0x7F80u ? 1u : 0u) | ((w[d] & 0x7F800000u) == 0x7F800000u ? 2u : 0u);
+        }
+        uint32_t keys = 0;
+        if (__builtin_expect(__any(odd[0] | odd[1] | odd[2] | odd[3]), 0)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint64_t who = __ballot(odd[j >> 1] >> (j & 1) & 1u);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (who >> (16 * q) & 0xFFFFu) keys |= 1u << ((j < 4 ? j : 12 + j) + 4 * q);
+            }
+        }
+        if (lane == 0) odd_lds[(v & 1) * 4 + wave] = keys;
+    };
+    // behind the barrier: the keys that some wavefront found; the rows that see them, and their values
+    auto clean = [&](const Place& at, int v) {
+        const u32x4 found = *(LDS_AS u32x4*)(odd_lds + (v & 1) * 4);
+        const uint32_t keys = found[0] | found[1] | found[2] | found[3];
+        if (__builtin_expect(keys == 0, 1)) return;
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) poisoned[hi] |= (visible(at, hi) & keys & (0x000F000Fu << (4 * g))) != 0;
+        // (every wavefront for itself: it does not matter who comes first)
+        LDS_AS unsigned char* const tile = vt + (v & 1) * VT_B;
+        for (int u = lane; u < VT_B / 16; u += 64) {
+            LDS_AS u32x4* unit = (LDS_AS u32x4*)(tile + u * 16);
+            u32x4 w = *unit;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                if ((w[d] & 0x7F80u) == 0x7F80u) w[d] &= 0xFFFF0000u;
+                if ((w[d] & 0x7F800000u) == 0x7F800000u) w[d] &= 0xFFFFu;
+            }
+            *unit = w;
+        }
+    };
+    float top[2] = {-INFINITY, -INFINITY};     // largest score of the sweep so far, this lane's keys (unscaled)
+    auto max3 = [](float a, float b, float c) {
+        float r;                    // (a NaN loses, as in fmaxf; written out: fmaxf would quieten every operand first)
+        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+        return r;
+    };
+    auto raise_top = [&](const Scores& x) {
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) top[hi] = max3(max3(top[hi], x[rb][hi][0], x[rb][hi][1]), x[rb][hi][2], x[rb][hi][3]);
+    };
+    // maximum over the four lane groups (all 32 keys of a tile), on every lane
+    auto over_groups = [&](float v) {
+        v = fmaxf(v, __shfl_xor(v, 16));
+        return fmaxf(v, __shfl_xor(v, 32));
+    };
+    // the reference of a query row: the maximum of its first tile with a row that it sees
+    bool unset = true;
+    auto set_reference = [&](const Scores& x) {
+        bool left = false;
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+            float tm = max3(x[0][hi][0], x[0][hi][1], x[0][hi][2]);
+            tm = max3(tm, x[0][hi][3], x[1][hi][0]);
+            tm = over_groups(max3(max3(tm, x[1][hi][1], x[1][hi][2]), x[1][hi][3], tm));
+            if (m_ref[hi] == -INFINITY) m_ref[hi] = tm == -INFINITY ? tm : tm * sc;
+            left |= m_ref[hi] == -INFINITY;
+        }
+        unset = __any(left);
+    };
+    // scores of a tile, just made: scaled (fp8) and masked
+    auto look_at = [&](Scores& x, const Place& at, int v) {
+        if constexpr (FP8) {
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) {
+                ksc[rb] = *(LDS_AS f32x4*)(ks_lds + (v & 1) * MK_TILE + rb * 16 + g * 4);
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) x[rb][hi] *= ksc[rb];
+            }
+        }
+        if (__builtin_expect(!seen_whole(at), 0)) mask(x, at, v);
+        raise_top(x);
+        if (unset) set_reference(x);
+    };
+
+    // ---- a step: S^T of the tile in `keys` and the weights of the tile before from its scores x (PV); then its values from `values`,
+    // and the transpose of the former tile into `to`
+    auto step = [&](auto pv_tag, LDS_AS unsigned char* keys, LDS_AS unsigned char* values, LDS_AS unsigned char* to, const Scores& x, Scores& y) {
+        constexpr bool PV = decltype(pv_tag)::value;
+        constexpr int AHEAD = 2;               // k-steps that the key reads run ahead
+        constexpr int SHARE = NCT / 4;         // column tiles that this wavefront transposes (8 / 4)
+        bf16x8 ka[2][NKS], va[NCT];
+        float m_use[2];
+        uint32_t w[2][4];
+        auto rk = [&](int ks) {
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) ka[rb][ks] = *(LDS_AS bf16x8*)(keys + a_base[ks & 1] + (ks >> 1) * 128 + rb * 16 * ROWB);
+        };
+        auto rv = [&](int ct) { va[ct] = *(LDS_AS bf16x8*)(values + ct * 1024 + lane * 16); };
+        auto weigh = [&](int j) {              // pair j of 8: query group j / 4, keys 2 (j % 4) and the one after
+            const int hi = j >> 2, rb = (j >> 1) & 1, i = 2 * (j & 1);
+            float e0 = fast_exp2(fmaf(x[rb][hi][i], sc, -m_use[hi])), e1 = fast_exp2(fmaf(x[rb][hi][i + 1], sc, -m_use[hi]));
+            l_run[hi] += e0 + e1;
+            if constexpr (FP8) { e0 *= ksc[rb][i]; e1 *= ksc[rb][i + 1]; }
+            w[hi][2 * rb + (j & 1)] = pack_bf16x2(e0, e1);
+        };
+        s16x4 lo[SHARE], up[SHARE];
+        auto rt = [&](int k) {                 // column tile wave * SHARE + k
+            LDS_AS unsigned char* at = keys + t_base[k & 3] + ((wave * SHARE + k) >> 2) * 128;
+            lo[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)at);
+            up[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(at + 16 * ROWB));
+        };
+        auto wt = [&](int k) {
+            *(LDS_AS bf16x8*)(to + (wave * SHARE + k) * 1024 + lane * 16) =
+                __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo[k], up[k], 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        if constexpr (PV) {
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) m_use[hi] = m_ref[hi] == -INFINITY ? 0.f : m_ref[hi];
+        }
+#pragma unroll
+        for (int ks = 0; ks < AHEAD; ++ks) rk(ks);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+            if (ks + AHEAD < NKS) rk(ks + AHEAD);
+            else if (PV) {
+                rv(2 * (ks + AHEAD - NKS));
+                rv(2 * (ks + AHEAD - NKS) + 1);
+            }
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi)
+                    y[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[rb][ks], qreg[hi][ks], ks == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : y[rb][hi], 0, 0, 0);
+            if constexpr (PV) {
+                if (ks < 8) weigh(ks);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        bf16x8 pb[2];
+        if constexpr (PV) {
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) pb[hi] = __builtin_bit_cast(bf16x8, (u32x4){w[hi][0], w[hi][1], w[hi][2], w[hi][3]});
+        }
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) {
+            if (PV && ct + 4 < NCT) rv(ct + 4);
+            if (ct % 4 == 0) rt(ct / 4);
+            if (ct % 4 == 2) wt(ct / 4);
+            if constexpr (PV) {
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) oacc[hi][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[ct], pb[hi], oacc[hi][ct], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+
+    // ---- sweeps over the tiles.  ACCUMULATE against the references (set on the way where they are not yet); if some score exceeded its
+    // reference by more than FAST_GAP (rare), a sweep for the exact maxima (it accumulates too, which is not used) and the
+    // accumulation again against them.
+    enum { ACCUMULATE, MAXIMA, ACCUMULATE_AGAIN };
+    auto slot = [&](int v) { return lds + (v & 1) * TILE_B; };
+    auto turned = [&](int v) { return vt + (v & 1) * VT_B; };
+    for (int pass = ACCUMULATE;;) {
+        Scores x, y;
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+            l_run[hi] = 0.f;
+            top[hi] = -INFINITY;
+            poisoned[hi] = false;
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) oacc[hi][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+        if constexpr (!FP8) wait_vmcnt<0>();
+        __syncthreads();
+        if constexpr (!FP8) {
+            if (v0 + 1 < v1) request(next, v0 + 1);
+        }
+        step(No{}, slot(v0), turned(v0), turned(v0), x, x);
+        look_at(x, here, v0);
+        for (int v = v0; v < v1; ++v) {
+            after = place_of(v + 2);
+            if constexpr (FP8) {
+                if (v + 1 < v1) put(v + 1);
+            } else {
+                wait_vmcnt<0>();
+            }
+            __syncthreads();     // tile v + 1 and the transpose of tile v are there; everybody is done with tile v and the transpose before
+            if (v + 2 < v1) request(after, v + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            if (__builtin_expect(!seen_whole(here), 0)) clean(here, v);
+            step(Yes{}, slot(v + 1), turned(v), turned(v + 1), x, y);
+            if (v + 1 < v1) look_at(y, next, v + 1);
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) x[rb][hi] = y[rb][hi];
+            here = next;
+            next = after;
+        }
+        if (pass == ACCUMULATE_AGAIN) break;
+        if (pass == ACCUMULATE) {
+            // (an infinite score makes a NaN of its row either way, and no other row shall be the worse for it)
+            const bool jumped = (top[0] * sc > m_ref[0] + FAST_GAP && top[0] < INFINITY) || (top[1] * sc > m_ref[1] + FAST_GAP && top[1] < INFINITY);
+            if (__builtin_expect(!__syncthreads_or(jumped), 1)) break;
+            pass = MAXIMA;
+            unset = false;
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+                const float tm = over_groups(top[hi]);
+                m_ref[hi] = tm == -INFINITY ? tm : tm * sc;
+            }
+            pass = ACCUMULATE_AGAIN;
+        }
+        start();
+    }
+    __syncthreads();             // everybody is done with the tiles
+
+    // ---- normalise, and transpose through LDS (a lane holds 4 consecutive columns of its query per column tile) for whole rows.
+    // fp32 partials go in two halves of the columns, which the space takes.
+    float lt[2], inv[2];
+#pragma unroll
+    for (int hi = 0; hi < 2; ++hi) {
+        float l = l_run[hi] + __shfl_xor(l_run[hi], 16);
+        lt[hi] = l + __shfl_xor(l, 32);
+        inv[hi] = lt[hi] == 0.f ? 0.f : 1.f / lt[hi];
+        const uint64_t who = __ballot(poisoned[hi]);
+        if ((who | who >> 16 | who >> 32 | who >> 48) >> n & 1u) inv[hi] = __uint_as_float(0x7FC00000u);
+    }
+    constexpr int RSO = D_C * 2 + 32;           // row stride of the transposed block (padded)
+    static_assert(4 * 32 * RSO <= 2 * TILE_B + 2 * VT_B, "exchange space must fit");
+    LDS_AS unsigned char* mine = lds + wave * (32 * RSO);
+    if (p.num_splits == 1) {
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) {
+                const f32x4 o = oacc[hi][ct] * inv[hi];
+                *(LDS_AS u32x2*)(mine + (hi * 16 + n) * RSO + (ct * 16 + g * 4) * 2) = (u32x2){pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+            }
+        constexpr int LPR = D_C / 8;            // lanes of a row (64 / 32)
+        for (int r = lane / LPR; r < nrow; r += 64 / LPR) {
+            const int c = lane % LPR;
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.o_part) + part_of(r) * D_C + c * 8) = *(LDS_AS u32x4*)(mine + r * RSO + c * 16);
+        }
+    } else {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+                for (int ct = 0; ct < NCT / 2; ++ct)
+                    *(LDS_AS f32x4*)(mine + (hi * 16 + n) * RSO + (ct * 16 + g * 4) * 4) = oacc[hi][half * (NCT / 2) + ct] * inv[hi];
+            constexpr int LPR = D_C / 8;        // lanes of half a row in fp32
+            for (int r = lane / LPR; r < nrow; r += 64 / LPR) {
+                const int c = lane % LPR;
+                *reinterpret_cast<u32x4*>(static_cast<float*>(p.o_part) + part_of(r) * D_C + half * (D_C / 2) + c * 4) = *(LDS_AS u32x4*)(mine + r * RSO + c * 16);
+            }
+        }
+    }
+    if (g == 0 && p.lse_part) {
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi)
+            if (hi * 16 + n < nrow)
+                p.lse_part[part_of(hi * 16 + n)] = lt[hi] == 0.f ? -INFINITY : (m_ref[hi] == -INFINITY ? 0.f : m_ref[hi]) * LN2 + __builtin_amdgcn_logf(lt[hi]) * LN2;
+    }
+}
+
+// ---- chunks merged: lse = log sum_s e^{lse_s}, o = sum_s e^{lse_s - lse} o_s.  A wavefront per query row and 256 columns; lane s
+// holds the log-sum-exp of chunk s (at most 64).  The partials are fp32: rounded to bf16 they would be off by as much again as the
+// result's own rounding.
+template <bool BF16>
+__global__ __launch_bounds__(256) void masked_merge_kernel(MaskedParams p, void* o_lat, float* lse)
+{
+    const int lane = threadIdx.x & 63, blocks = (p.d_c + 255) / 256;
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (w >= (int64_t)p.B * p.H * blocks) return;
+    const int64_t row = w / blocks;
+    const int c = (int)(w % blocks) * 256 + lane * 4, S = p.num_splits;
+    const float ls = lane < S ? p.lse_part[row * S + lane] : -INFINITY;
+    const bool in = c < p.d_c;
+    const float* src = static_cast<const float*>(p.o_part) + row * S * p.d_c + (in ? c : 0);
+    constexpr int BATCH = 8;
+    float4 v[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) v[i] = *reinterpret_cast<const float4*>(src + (int64_t)min(i, S - 1) * p.d_c);
+    const float m = wave_max(ls), ref = m == -INFINITY ? 0.f : m;
+    const float e = expf(ls - ref), z = wave_sum(e);           // (a NaN stays one)
+    const float wt = z == 0.f ? 0.f : e / z;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < S; s0 += BATCH) {
+        if (s0) {
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) v[i] = *reinterpret_cast<const float4*>(src + (int64_t)min(s0 + i, S - 1) * p.d_c);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const float k = s0 + i < S ? lane_value(wt, s0 + i) : 0.f;
+            const bool live = k != 0.f;                        // (rows of empty chunks were never written)
+            acc.x = fmaf(k, live ? v[i].x : 0.f, acc.x); acc.y = fmaf(k, live ? v[i].y : 0.f, acc.y);
+            acc.z = fmaf(k, live ? v[i].z : 0.f, acc.z); acc.w = fmaf(k, live ? v[i].w : 0.f, acc.w);
+        }
+    }
+    if (in) {
+        if (BF16)
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(o_lat) + row * p.d_c + c) = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+        else
+            *reinterpret_cast<float4*>(static_cast<float*>(o_lat) + row * p.d_c + c) = acc;
+    }
+    if (lse && c == 0) lse[row] = z == 0.f ? -INFINITY : m == -INFINITY ? z : m + logf(z);
+}
+
+}  // namespace
+
+bool masked_tall_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache)
+{
+    auto on16 = [](const void* q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
+    return io == MLA_BF16 && (cache == MLA_BF16 || cache == MLA_FP8_E4M3) && p.d_rope == 64 && (p.d_c == 256 || p.d_c == 512) &&
+           p.page_size % MK_TILE == 0 && on16(p.q_abs) && on16(p.q_rope) && on16(p.kv);
+}
+
+hipError_t launch_masked_tall(const MaskedParams& p, mla_dtype cache, hipStream_t s)
+{
+    const unsigned chunks = ((unsigned)p.B * p.num_splits + 7) / 8 * 8, Z = (unsigned)((p.H + MT_ROWS - 1) / MT_ROWS);
+    const dim3 grid(chunks * Z), block(MF_THREADS);
+    if (cache == MLA_BF16 && p.d_c == 512)      masked_tall_kernel<512, false><<<grid, block, 0, s>>>(p);
+    else if (cache == MLA_BF16)                 masked_tall_kernel<256, false><<<grid, block, 0, s>>>(p);
+    else if (p.d_c == 512)                      masked_tall_kernel<512, true><<<grid, block, 0, s>>>(p);
+    else                                        masked_tall_kernel<256, true><<<grid, block, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t launch_masked_merge(const MaskedParams& p, void* o_lat, float* lse, mla_dtype io, hipStream_t s)
+{
+    const int64_t waves = (int64_t)p.B * p.H * ((p.d_c + 255) / 256);
+    const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
+    if (io == MLA_BF16) masked_merge_kernel<true><<<grid, block, 0, s>>>(p, o_lat, lse);
+    else                masked_merge_kernel<false><<<grid, block, 0, s>>>(p, o_lat, lse);
+    return hipGetLastError();
+}
+
+}  // namespace mla

@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * PM_WAVES) void masked_portable_kernel(MaskedPa
                 if (l_s[w][h] != 0.f) add4(o, f[w], *reinterpret_cast<const float4*>(&o_s[w][h][col]));
             const float inv = nothing ? 0.f : 1.f / lt;
             o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-            if constexpr (std::is_same_v<QT, bf16_tag>)
+            if (std::is_same_v<QT, bf16_tag> && p.num_splits == 1)
                 *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o_part) + pi * p.d_c + col) =
                     make_uint2(f32_to_bf16_bits(o.x) | (f32_to_bf16_bits(o.y) << 16), f32_to_bf16_bits(o.z) | (f32_to_bf16_bits(o.w) << 16));
             else

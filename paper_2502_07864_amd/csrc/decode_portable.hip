@@ -422,7 +422,7 @@ __global__ __launch_bounds__(128) void merge_kernel(MergeParams p)
             *reinterpret_cast<float4*>(static_cast<float*>(p.o_lat) + out_base + c) = acc[i];
         }
     }
-    if (p.lse && tid == 0) p.lse[(size_t)b * p.H + h] = z == 0.f ? -INFINITY : m + logf(z);    // (a NaN stays one)
+    if (p.lse && tid == 0) p.lse[(size_t)b * p.H + h] = z > 0.f ? m + logf(z) : -INFINITY;
 }
 
 // Streaming variant for d_c a multiple of 256: one wavefront per (sequence, head, block of 256
@@ -490,7 +490,7 @@ __global__ __launch_bounds__(256) void merge_wave_kernel(MergeParams p)
     } else {
         *reinterpret_cast<float4*>(static_cast<float*>(p.o_lat) + o) = acc;
     }
-    if (p.lse && cb == 0 && lane == 0) p.lse[bh] = cw.z == 0.f ? -INFINITY : cw.m + logf(cw.z);
+    if (p.lse && cb == 0 && lane == 0) p.lse[bh] = cw.z > 0.f ? cw.m + logf(cw.z) : -INFINITY;
 }
 
 // ---- page gather (byte exact) ---------------------------------------------

@@ -32,7 +32,6 @@ struct Plan {
     size_t lse_off, total;      // of the workspace (S > 1)
 };
 
-// (a call's kernel depends on types that the workspace's size does not: sized for the one that cuts finest)
 Plan plan_of(int B, int64_t H, int d_c, int64_t tiles, int rows)
 {
     Plan p;
@@ -44,7 +43,9 @@ Plan plan_of(int B, int64_t H, int d_c, int64_t tiles, int rows)
 
 size_t workspace_bytes_for(int B, int q_len, int heads, int d_c, int64_t tiles)
 {
-    return plan_of(B, (int64_t)q_len * heads, d_c, tiles, MK_PORTABLE_ROWS).total;
+    // (which kernel a call takes hangs on its types, which are not asked for here)
+    const int64_t H = (int64_t)q_len * heads;
+    return std::max(plan_of(B, H, d_c, tiles, MK_PORTABLE_ROWS).total, plan_of(B, H, d_c, tiles, MK_TALL_ROWS).total);
 }
 
 bool sizes_ok(int B, int q_len, int heads, int d_c, int max_rows)
@@ -75,7 +76,8 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
     const int64_t tiles = most_tiles(p.q_len, (int64_t)p.max_pages * p.page_size, tree, p.window, p.sinks);
     const size_t need = workspace_bytes_for(p.B, p.q_len, p.heads, p.d_c, tiles);
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return MLA_ERR_WORKSPACE;
-    const Plan plan = plan_of(p.B, H, p.d_c, tiles, MK_PORTABLE_ROWS);
+    const bool tall = !(flags & MLA_FLAG_PORTABLE_KERNEL) && masked_tall_supported(p, io, cache);
+    const Plan plan = plan_of(p.B, H, p.d_c, tiles, tall ? MK_TALL_ROWS : MK_PORTABLE_ROWS);
     p.num_splits = plan.S;
     if (plan.S == 1) {
         p.o_part = o_lat;
@@ -85,13 +87,8 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
         p.lse_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.lse_off);
     }
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    hipError_t e = launch_masked_portable(p, io, cache, stream);
-    if (e == hipSuccess && plan.S > 1) {
-        MergeParams m;
-        m.o_part = p.o_part; m.lse_part = p.lse_part; m.plan = nullptr; m.o_lat = o_lat; m.lse = lse;
-        m.B = p.B; m.H = p.H; m.d_c = p.d_c; m.num_splits = plan.S;
-        e = launch_merge(m, io, stream);
-    }
+    hipError_t e = tall ? launch_masked_tall(p, cache, stream) : launch_masked_portable(p, io, cache, stream);
+    if (e == hipSuccess && plan.S > 1) e = launch_masked_merge(p, o_lat, lse, io, stream);
     return e == hipSuccess ? MLA_OK : MLA_ERR_HIP;
 }
 

@@ -15,7 +15,7 @@ struct MaskedParams {
     const int32_t* lens;        // [B]: committed rows (a tree), or all of them (a window)
     const uint64_t* tree;       // [B, q_len] drafted rows that a token sees; nullptr: a window
     int64_t tree_pitch;
-    void* o_part;               // [B, H, S, d_c]  chunk-normalised outputs in the io dtype (S = 1: the output itself)
+    void* o_part;               // [B, H, S, d_c]  chunk-normalised outputs in fp32 (S = 1: the output itself, in the io dtype)
     float* lse_part;            // [B, H, S]       (S = 1: the output's, or nullptr)
     int B, H, d_c, d_rope, page_size, num_pages, max_pages, num_splits;
     int q_len, heads, window, sinks;
@@ -70,5 +70,11 @@ __host__ __device__ __forceinline__ int chunk_start(int tiles, int s, int S) { r
 // portable scalar-FMA kernel: every type pair, width and page size of mla_decode_paged
 hipError_t launch_masked_portable(const MaskedParams& p, mla_dtype io, mla_dtype cache, hipStream_t s);
 constexpr int MK_PORTABLE_ROWS = 4;       // query rows of a workgroup
+// matrix-core kernel
+bool       masked_tall_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache);
+hipError_t launch_masked_tall(const MaskedParams& p, mla_dtype cache, hipStream_t s);
+constexpr int MK_TALL_ROWS = 128;
+// the chunks' results (S > 1) merged
+hipError_t launch_masked_merge(const MaskedParams& p, void* o_lat, float* lse, mla_dtype io, hipStream_t s);
 
 }  // namespace mla
