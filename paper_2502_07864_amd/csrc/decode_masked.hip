@@ -31,6 +31,20 @@ namespace {
 
 constexpr int MT_ROWS = MK_TALL_ROWS;        // query rows per workgroup
 
+// Swizzle of piece 64 k + lane of eight rows of PPR pieces each, as bits of an address: (row & 6) << 4.  A comparison or two per piece
+// instead of a register kept (or, as there are none left, spilled) for each.
+template <int PPR> __device__ __forceinline__ uint32_t piece_key(int k, int lane)
+{
+    const int first = k * 64 / PPR / 2;              // half the row of lane 0
+    uint32_t half = (uint32_t)first;
+#pragma unroll
+    for (int i = 1; i <= 2; ++i) {
+        const int from = 2 * (first + i) * PPR - 64 * k;
+        if (from < 64) half += lane >= from;
+    }
+    return half << 5;
+}
+
 template <int D_C, bool FP8>
 __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams p)
 {
@@ -41,12 +55,14 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     constexpr int NKS = ROW / 32;                       // k-steps of the scores (18 / 10)
     constexpr int NCT = D_C / 16;                       // column tiles of the values (32 / 16)
     constexpr int VT_B = D_C * MK_TILE * 2;             // a transposed tile
-    constexpr int CODES = MK_TILE * ROW / 16;           // 16-byte pieces of an fp8 tile (1152 / 640)
-    constexpr int NCODE = (CODES + MF_THREADS - 1) / MF_THREADS;     // per thread (5 / 3, the last by some)
+    constexpr int NQ = D_C == 512 ? NKS - 2 : NKS;      // k-steps whose queries stay in registers; those of the rope part don't fit, and lie in LDS
+    constexpr int CPC = ROW / 16;                       // 16-byte pieces per fp8 row (36 / 20)
+    constexpr int NCODE = (8 * CPC + 63) / 64;          // per lane, of eight rows (5 / 3, the last by half of the lanes)
 
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * TILE_B + 2 * VT_B];
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * TILE_B + 2 * VT_B + (NKS - NQ) * 2 * MF_THREADS * 16];
     __shared__ __attribute__((aligned(16))) float ks_smem[2][MK_TILE];        // scales of an fp8 tile's rows
     __shared__ uint64_t tree_smem[64];
+    __shared__ int token_smem[MT_ROWS];
     __shared__ __attribute__((aligned(16))) uint32_t odd_smem[2][4];          // keys of a tile whose values are not all finite, by wavefront
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
     LDS_AS float* ks_lds = (LDS_AS float*)ks_smem;
@@ -81,81 +97,84 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         return;
     }
 
-    // ---- tiles: v is a tile's number without the gap; its rows lie on one page (page sizes are multiples of 32)
-    const CONST_AS int32_t* ptab = (const CONST_AS int32_t*)(p.page_table + (size_t)b * p.max_pages);
+    // ---- tiles: v is a tile's number without the gap; its rows lie on one page (page sizes are multiples of 32).  Where they lie, 64 tiles at
+    // a time, a lane each (a scalar load on every step, out of order with the LDS reads, would make each of their waits a wait
+    // for everything): the tile's number in the pool, -1 where its page is not there.
+    const int32_t* const ptab = p.page_table + (size_t)b * p.max_pages;
     const int per_page = p.page_size / MK_TILE;
-    struct Place {
-        int row;          // first row of the tile in the sequence
-        int valid;        // rows that are there
-        size_t at;        // and in the pool
-    };
-    auto place_of = [&](int v) {
-        const int t = reach.tile(min(v, v1 - 1)), q = t / per_page;
+    auto ids_from = [&](int v) {
+        const int t = reach.tile(min(v + lane, v1 - 1)), q = t / per_page;
         const int page = ptab[q];
-        const bool there = page >= 0 && page < p.num_pages;
-        return Place{t * MK_TILE, there ? min(MK_TILE, reach.end - t * MK_TILE) : 0, (size_t)(there ? page : 0) * p.page_size + (t - q * per_page) * MK_TILE};
+        return page >= 0 && page < p.num_pages ? page * per_page + (t - q * per_page) : -1;
+    };
+    int32_t ids = 0, ids_after = 0;                     // of the tiles v0 + 64 k on, and the 64 behind them
+    auto tile_at = [&](int v) -> int {                  // (v: in the order of the sweep)
+        if (((v - v0) & 63) == 0) {
+            ids = v == v0 ? ids_from(v0) : ids_after;
+            if (v + 64 < v1) ids_after = ids_from(v + 64);
+        }
+        return __builtin_amdgcn_readlane(ids, (v - v0) & 63);
     };
 
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
-    uint32_t goff[NLOAD];                               // bf16: this thread's pieces, chunk c of row r at position c ^ key(r)
-    if constexpr (!FP8) {
-#pragma unroll
-        for (int k = 0; k < NLOAD; ++k) {
-            const int q = k * MF_THREADS + tid, r = q / CPR, c = q % CPR;
-            goff[k] = (uint32_t)(r * ROWB + ((c ^ swz_key(r)) << 4));
-        }
-    }
+    // A wavefront loads eight rows of a tile, which lie one behind the other as they do in the pool, 64 pieces at a time; chunk c of row r at
+    // position c ^ key(r).
+    auto my_lane = [&]() -> int {                       // (worked out where it is needed)
+        uint32_t all = ~0u;
+        asm volatile("" : "+s"(all));
+        return (int)__builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0u));
+    };
     u32x4 codes[FP8 ? NCODE : 1];
     float my_scale = 1.f;
-    // tile v -> slot v & 1: the loads (fp8: into registers)
-    auto request = [&](const Place& at, int v) {
-        if (at.valid <= 0) return;                      // a page outside the pool is never dereferenced
+    // tile v, number `at` in the pool -> slot v & 1: the loads (fp8: into registers)
+    auto request = [&](int at, int v) {
+        if (at < 0) return;                             // a page outside the pool is never dereferenced
+        const int l = my_lane();
         if constexpr (FP8) {
-            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + at.at * ROW;
+            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * (MK_TILE * ROW) + wave * (8 * ROW);
 #pragma unroll
-            for (int k = 0; k < NCODE; ++k) {
-                const int q = min(k * MF_THREADS + tid, CODES - 1);
-                codes[k] = *reinterpret_cast<const u32x4*>(src + q * 16);
-            }
-            if (tid < MK_TILE) my_scale = tid < at.valid ? p.kv_scale[at.at + tid] : 1.f;
+            for (int k = 0; k < NCODE; ++k) codes[k] = *reinterpret_cast<const u32x4*>(src + min(k * 64 + l, 8 * CPC - 1) * 16);
+            my_scale = p.kv_scale[(size_t)at * MK_TILE + (l & (MK_TILE - 1))];
         } else {
-            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + at.at * ROWB;
-            const uint32_t dst = lds_base + (uint32_t)((v & 1) * TILE_B + wave * 1024);
+            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * TILE_B + wave * (8 * ROWB);
+            const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)((v & 1) * TILE_B + wave * (8 * ROWB)));
 #pragma unroll
             for (int k = 0; k < NLOAD; ++k) {
-                const uint32_t m0v = __builtin_amdgcn_readfirstlane(dst + k * 4096);
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                             :: "s"(m0v), "v"(goff[k]), "s"(src) : "memory");
+                const uint32_t off = ((uint32_t)l * 16) ^ piece_key<CPR>(k, l);
+                asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                             :: "s"(dst), "v"(off), "s"(src + k * 1024), "i"(k * 1024) : "memory", "scc");
             }
         }
     };
     // (fp8) the requested codes, widened, into the slot of tile v
     auto put = [&](int v) {
         if constexpr (FP8) {
-            LDS_AS unsigned char* slot = lds + (v & 1) * TILE_B;
+            const int l = my_lane();
+            LDS_AS unsigned char* rows = lds + (v & 1) * TILE_B + wave * (8 * ROWB);
 #pragma unroll
             for (int k = 0; k < NCODE; ++k) {
-                const int q = k * MF_THREADS + tid;
-                if (q >= CODES) continue;
-                const int r = q / (CPR / 2), c = q % (CPR / 2) * 2;
+                const int q = k * 64 + l;
+                if (8 * CPC % 64 && k == NCODE - 1 && q >= 8 * CPC) continue;
                 uint32_t w[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[k][i], 1.f, false));
                     w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[k][i], 1.f, true));
                 }
-                *(LDS_AS u32x4*)(slot + r * ROWB + ((c ^ swz_key(r)) << 4)) = (u32x4){w[0], w[1], w[2], w[3]};
-                *(LDS_AS u32x4*)(slot + r * ROWB + (((c + 1) ^ swz_key(r)) << 4)) = (u32x4){w[4], w[5], w[6], w[7]};
+                // (the key is even: the second half's place is beside the first's)
+                const uint32_t to = (uint32_t)(q * 32) ^ piece_key<CPC>(k, l);
+                *(LDS_AS u32x4*)(rows + to) = (u32x4){w[0], w[1], w[2], w[3]};
+                *(LDS_AS u32x4*)(rows + (to ^ 16)) = (u32x4){w[4], w[5], w[6], w[7]};
             }
-            if (tid < MK_TILE) ks_lds[(v & 1) * MK_TILE + tid] = my_scale;
+            if (wave == 0 && l < MK_TILE) ks_lds[(v & 1) * MK_TILE + l] = my_scale;
         }
     };
 
     // the first tile, and (fp8) the second one's codes
-    Place here, next, after;
+    int here, next, after;
     auto start = [&]() {
-        here = place_of(v0);
-        next = place_of(v0 + 1);
+        here = tile_at(v0);
+        next = tile_at(v0 + 1);
         request(here, v0);
         if constexpr (FP8) {
             put(v0);
@@ -166,7 +185,8 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 
     // ---- this wavefront's query rows -> registers (B operands of the scores).  A negative scale changes their sign: the largest score is
     // then the largest scaled one
-    bf16x8 qreg[2][NKS];
+    bf16x8 qreg[2][NQ];
+    LDS_AS unsigned char* const q_lds = lds + 2 * TILE_B + 2 * VT_B + wave * ((NKS - NQ) * 2 * 1024) + lane * 16;      // this lane's, written and read by it alone
     {
         const uint16_t* qa = static_cast<const uint16_t*>(p.q_abs) + (size_t)b * p.H * D_C;
         const uint16_t* qr = static_cast<const uint16_t*>(p.q_rope) + (size_t)b * p.H * 64;
@@ -179,13 +199,25 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
                 u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + ks * 32 + g * 8)
                                         : *reinterpret_cast<const u32x4*>(qr + row * 64 + (ks - D_C / 32) * 32 + g * 8);
                 v ^= (u32x4){flip, flip, flip, flip};
-                qreg[hi][ks] = __builtin_bit_cast(bf16x8, v);
+                if (ks < NQ) qreg[hi][ks] = __builtin_bit_cast(bf16x8, v);
+                else         *(LDS_AS u32x4*)(q_lds + ((ks - NQ) * 2 + hi) * 1024) = v;
             }
         }
     }
     if (tree && tid < p.q_len) tree_smem[tid] = p.tree[b * p.tree_pitch + tid] & (p.q_len < 64 ? (1ull << p.q_len) - 1 : ~0ull);
-    const int token[2] = {(hb + min(wave * 32 + n, HL - 1)) / p.heads, (hb + min(wave * 32 + 16 + n, HL - 1)) / p.heads};
-    const int first_at = reach.base + hb / p.heads, last_at = reach.base + (hb + HL - 1) / p.heads;     // (a window) positions of the workgroup's tokens
+    if (tid < MT_ROWS) token_smem[tid] = (hb + min(tid, HL - 1)) / p.heads;        // (both are read in few tiles)
+    // tiles that all query rows of the workgroup see whole: [0, whole) and [whole_from, whole_to)
+    int whole, whole_from = 0, whole_to = 0;
+    if (tree) {
+        whole = reach.base / MK_TILE;
+    } else {
+        const int first = reach.base + hb / p.heads, last = reach.base + (hb + HL - 1) / p.heads;       // positions of its tokens
+        const int64_t outside = (int64_t)last - p.window;                                               // last row before all windows meet
+        whole = max(0, min(p.sinks, first + 1)) / MK_TILE;
+        whole_from = (outside < 0 ? 0 : (int)(outside / MK_TILE) + 1) - reach.skip;
+        whole_to = max(0, first + 1) / MK_TILE - reach.skip;
+    }
+    auto seen_whole = [&](int v, int at) { return at >= 0 && (v < whole || (v >= whole_from && v < whole_to)); };
 
     // ---- per-lane state: this lane's queries = column n of the D tiles of the two groups
     float m_ref[2] = {-INFINITY, -INFINITY};   // reference of the exponentials (log2 units)
@@ -212,31 +244,27 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     f32x4 ksc[2];                              // (fp8) scales of this lane's keys
     bool poisoned[2] = {false, false};         // one of this lane's keys that its query sees was not finite
 
-    // rows of the tile (bit: row) that the lane's query of group hi sees
-    auto visible = [&](const Place& at, int hi) -> uint32_t {
+    // rows of tile v (bit: row) that the lane's query of group hi sees
+    auto visible = [&](int v, int at, int hi) -> uint32_t {
         auto low = [](int k) -> uint32_t { return k <= 0 ? 0u : k >= 32 ? ~0u : (1u << k) - 1u; };
+        const int row = reach.tile(v) * MK_TILE, token = token_smem[wave * 32 + hi * 16 + (my_lane() & 15)];
         uint32_t sees;
         if (tree) {
-            const uint64_t m = tree_smem[token[hi]];
-            const int d = reach.base - at.row;             // committed rows of the tile
+            const uint64_t m = tree_smem[token];
+            const int d = reach.base - row;                // committed rows of the tile
             sees = d >= 32 ? ~0u : d > 0 ? (uint32_t)(m << d) | low(d) : d > -64 ? (uint32_t)(m >> -d) : 0u;
         } else {
-            const int t = reach.base + token[hi];
-            const int64_t from = (int64_t)t - p.window + 1 - at.row;
-            const uint32_t old = low(from < 0 ? 0 : from > 32 ? 32 : (int)from), sunk = low(p.sinks - at.row);
-            sees = low(t + 1 - at.row) & (~old | sunk);
+            const int t = reach.base + token;
+            const int64_t from = (int64_t)t - p.window + 1 - row;
+            const uint32_t old = low(from < 0 ? 0 : from > 32 ? 32 : (int)from), sunk = low(p.sinks - row);
+            sees = low(t + 1 - row) & (~old | sunk);
         }
-        return sees & low(at.valid);
+        return at < 0 ? 0u : sees & low(reach.end - row);
     };
-    auto seen_whole = [&](const Place& at) {
-        if (at.valid < MK_TILE) return false;
-        if (tree) return at.row + MK_TILE <= reach.base;
-        return at.row + MK_TILE - 1 <= first_at && ((int64_t)at.row > (int64_t)last_at - p.window || at.row + MK_TILE <= p.sinks);
-    };
-    auto mask = [&](Scores& x, const Place& at, int v) {
+    auto mask = [&](Scores& x, int v, int at) {
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
-            const uint32_t sees = visible(at, hi) >> (4 * g);
+            const uint32_t sees = visible(v, at, hi) >> (4 * g);
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
@@ -275,12 +303,12 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         if (lane == 0) odd_lds[(v & 1) * 4 + wave] = keys;
     };
     // behind the barrier: the keys that some wavefront found; the rows that see them, and their values
-    auto clean = [&](const Place& at, int v) {
+    auto clean = [&](int v, int at) {
         const u32x4 found = *(LDS_AS u32x4*)(odd_lds + (v & 1) * 4);
         const uint32_t keys = found[0] | found[1] | found[2] | found[3];
         if (__builtin_expect(keys == 0, 1)) return;
 #pragma unroll
-        for (int hi = 0; hi < 2; ++hi) poisoned[hi] |= (visible(at, hi) & keys & (0x000F000Fu << (4 * g))) != 0;
+        for (int hi = 0; hi < 2; ++hi) poisoned[hi] |= (visible(v, at, hi) & keys & (0x000F000Fu << (4 * g))) != 0;
         // (every wavefront for itself: it does not matter who comes first)
         LDS_AS unsigned char* const tile = vt + (v & 1) * VT_B;
         for (int u = lane; u < VT_B / 16; u += 64) {
@@ -326,7 +354,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         unset = __any(left);
     };
     // scores of a tile, just made: scaled (fp8) and masked
-    auto look_at = [&](Scores& x, const Place& at, int v) {
+    auto look_at = [&](Scores& x, int v, int at) {
         if constexpr (FP8) {
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb) {
@@ -335,7 +363,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
                 for (int hi = 0; hi < 2; ++hi) x[rb][hi] *= ksc[rb];
             }
         }
-        if (__builtin_expect(!seen_whole(at), 0)) mask(x, at, v);
+        if (__builtin_expect(!seen_whole(v, at), 0)) mask(x, v, at);
         raise_top(x);
         if (unset) set_reference(x);
     };
@@ -344,7 +372,8 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     // and the transpose of the former tile into `to`
     auto step = [&](auto pv_tag, LDS_AS unsigned char* keys, LDS_AS unsigned char* values, LDS_AS unsigned char* to, const Scores& x, Scores& y) {
         constexpr bool PV = decltype(pv_tag)::value;
-        constexpr int AHEAD = 2;               // k-steps that the key reads run ahead
+        static constexpr int AHEAD = 4;               // k-steps that the key reads run ahead, one wavefront per SIMD with nothing else to hide them
+        static constexpr int VAHEAD = 4;              // column tiles that the value reads do
         constexpr int SHARE = NCT / 4;         // column tiles that this wavefront transposes (8 / 4)
         bf16x8 ka[2][NKS], va[NCT];
         float m_use[2];
@@ -352,6 +381,11 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         auto rk = [&](int ks) {
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb) ka[rb][ks] = *(LDS_AS bf16x8*)(keys + a_base[ks & 1] + (ks >> 1) * 128 + rb * 16 * ROWB);
+        };
+        bf16x8 qa[NKS - NQ + 1][2];            // (one more: an array may not be empty)
+        auto rq = [&](int ks) {
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) qa[ks - NQ][hi] = *(LDS_AS bf16x8*)(q_lds + ((ks - NQ) * 2 + hi) * 1024);
         };
         auto rv = [&](int ct) { va[ct] = *(LDS_AS bf16x8*)(values + ct * 1024 + lane * 16); };
         auto weigh = [&](int j) {              // pair j of 8: query group j / 4, keys 2 (j % 4) and the one after
@@ -381,17 +415,25 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) {
             if (ks + AHEAD < NKS) rk(ks + AHEAD);
-            else if (PV) {
-                rv(2 * (ks + AHEAD - NKS));
-                rv(2 * (ks + AHEAD - NKS) + 1);
+            if (NQ < NKS && ks + 2 >= NQ && ks + 2 < NKS) rq(ks + 2);
+            if (PV && ks + AHEAD >= NKS) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (2 * (ks + AHEAD - NKS) + i < VAHEAD) rv(2 * (ks + AHEAD - NKS) + i);
             }
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi)
-                    y[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[rb][ks], qreg[hi][ks], ks == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : y[rb][hi], 0, 0, 0);
+                    y[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[rb][ks], ks < NQ ? qreg[hi][ks < NQ ? ks : 0] : qa[ks < NQ ? 0 : ks - NQ][hi], ks == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : y[rb][hi], 0, 0, 0);
             if constexpr (PV) {
                 if (ks < 8) weigh(ks);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // an LDS read
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);     // a matrix instruction
+                    __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);     // vector instructions in its shadow
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -402,15 +444,16 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         }
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) {
-            if (PV && ct + 4 < NCT) rv(ct + 4);
+            if (PV && ct + VAHEAD < NCT) rv(ct + VAHEAD);
             if (ct % 4 == 0) rt(ct / 4);
-            if (ct % 4 == 2) wt(ct / 4);
+            if (ct >= 6 && (ct - 6) % 4 == 0) wt((ct - 6) / 4);
             if constexpr (PV) {
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) oacc[hi][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[ct], pb[hi], oacc[hi][ct], 0, 0, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        wt(SHARE - 1);
     };
     using Yes = std::true_type;
     using No = std::false_type;
@@ -437,26 +480,29 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             if (v0 + 1 < v1) request(next, v0 + 1);
         }
         step(No{}, slot(v0), turned(v0), turned(v0), x, x);
-        look_at(x, here, v0);
-        for (int v = v0; v < v1; ++v) {
-            after = place_of(v + 2);
+        look_at(x, v0, here);
+        auto iterate = [&](int v, Scores& x, Scores& y) {
+            after = v + 2 < v1 ? tile_at(v + 2) : -1;
             if constexpr (FP8) {
                 if (v + 1 < v1) put(v + 1);
             } else {
                 wait_vmcnt<0>();
             }
             __syncthreads();     // tile v + 1 and the transpose of tile v are there; everybody is done with tile v and the transpose before
-            if (v + 2 < v1) request(after, v + 2);
+            request(after, v + 2);
             __builtin_amdgcn_sched_barrier(0);
-            if (__builtin_expect(!seen_whole(here), 0)) clean(here, v);
+            if (__builtin_expect(!seen_whole(v, here), 0)) clean(v, here);
             step(Yes{}, slot(v + 1), turned(v), turned(v + 1), x, y);
-            if (v + 1 < v1) look_at(y, next, v + 1);
+            if (v + 1 < v1) look_at(y, v + 1, next);
+            here = next;
+            next = after;
+        };
+        for (int v = v0; v < v1; ++v) {
+            iterate(v, x, y);
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) x[rb][hi] = y[rb][hi];
-            here = next;
-            next = after;
         }
         if (pass == ACCUMULATE_AGAIN) break;
         if (pass == ACCUMULATE) {
@@ -578,7 +624,7 @@ bool masked_tall_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache)
 {
     auto on16 = [](const void* q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
     return io == MLA_BF16 && (cache == MLA_BF16 || cache == MLA_FP8_E4M3) && p.d_rope == 64 && (p.d_c == 256 || p.d_c == 512) &&
-           p.page_size % MK_TILE == 0 && on16(p.q_abs) && on16(p.q_rope) && on16(p.kv);
+           p.page_size % MK_TILE == 0 && (int64_t)p.num_pages * (p.page_size / MK_TILE) <= 0x7FFFFFFF && on16(p.q_abs) && on16(p.q_rope) && on16(p.kv);
 }
 
 hipError_t launch_masked_tall(const MaskedParams& p, mla_dtype cache, hipStream_t s)
