@@ -51,6 +51,8 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     constexpr int ROW = D_C + 64, ROWB = ROW * 2;       // of a tile in LDS (bf16)
     constexpr int CPR = ROWB / 16;                      // 16-byte chunks per row (72 / 40)
     constexpr int TILE_B = MK_TILE * ROWB;
+    constexpr int NT = D_C == 512 ? 1 : 2;              // tiles of a step (as many as fit twice into the LDS, with their transposes)
+    constexpr int NRB = 2 * NT;                         // and their blocks of 16 keys
     constexpr int NLOAD = TILE_B / (MF_THREADS * 16);   // 16-byte loads per thread and bf16 tile (9 / 5)
     constexpr int NKS = ROW / 32;                       // k-steps of the scores (18 / 10)
     constexpr int NCT = D_C / 16;                       // column tiles of the values (32 / 16)
@@ -59,11 +61,11 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     constexpr int CPC = ROW / 16;                       // 16-byte pieces per fp8 row (36 / 20)
     constexpr int NCODE = (8 * CPC + 63) / 64;          // per lane, of eight rows (5 / 3, the last by half of the lanes)
 
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * TILE_B + 2 * VT_B + (NKS - NQ) * 2 * MF_THREADS * 16];
-    __shared__ __attribute__((aligned(16))) float ks_smem[2][MK_TILE];        // scales of an fp8 tile's rows
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * NT * (TILE_B + VT_B) + (NKS - NQ) * 2 * MF_THREADS * 16];
+    __shared__ __attribute__((aligned(16))) float ks_smem[2][NT * MK_TILE];        // scales of an fp8 tile's rows
     __shared__ uint64_t tree_smem[64];
     __shared__ int token_smem[MT_ROWS];
-    __shared__ __attribute__((aligned(16))) uint32_t odd_smem[2][4];          // keys of a tile whose values are not all finite, by wavefront
+    __shared__ __attribute__((aligned(16))) uint32_t odd_smem[2][NT][4];          // keys of a tile whose values are not all finite, by wavefront
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
     LDS_AS float* ks_lds = (LDS_AS float*)ks_smem;
     LDS_AS uint32_t* odd_lds = (LDS_AS uint32_t*)odd_smem;
@@ -77,7 +79,18 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     const int id = blockIdx.x, rr = id >> 3;
     const int wg = (rr / Z) * 8 + (id & 7), zi = rr % Z;
     if (wg >= p.B * p.num_splits) return;               // padding of the last group of 8
-    const int split = wg % p.num_splits, b = wg / p.num_splits;
+    const int split = wg % p.num_splits;
+    int b = wg / p.num_splits;
+    // the longest sequences first (up to 64 of them: every workgroup ranks the lengths by itself): a long one started last would run on alone
+    if (p.B > 1 && p.B <= 64) {
+        const int mine = lane < p.B ? p.lens[lane] : -1;
+        int rank = 0;
+        for (int j = 0; j < p.B; ++j) {
+            const int other = __builtin_amdgcn_readlane(mine, j);
+            rank += other > mine || (other == mine && j < lane);
+        }
+        b = __builtin_amdgcn_readfirstlane(__builtin_ffsll((long long)__ballot(lane < p.B && rank == b)) - 1);
+    }
     const int hb = zi * MT_ROWS, HL = min(MT_ROWS, p.H - hb);
 
     const bool tree = p.tree != nullptr;
@@ -124,20 +137,21 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         asm volatile("" : "+s"(all));
         return (int)__builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0u));
     };
-    u32x4 codes[FP8 ? NCODE : 1];
-    float my_scale = 1.f;
-    // tile v, number `at` in the pool -> slot v & 1: the loads (fp8: into registers)
-    auto request = [&](int at, int v) {
+    u32x4 codes[FP8 ? NT * NCODE : 1];
+    float my_scale[NT];
+    // tile t of step u, number `at` in the pool -> its place in slot u & 1: the loads (fp8: into registers)
+    auto request = [&](int at, int u, auto tile_tag) {
+        constexpr int t = decltype(tile_tag)::value;
         if (at < 0) return;                             // a page outside the pool is never dereferenced
         const int l = my_lane();
         if constexpr (FP8) {
             const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * (MK_TILE * ROW) + wave * (8 * ROW);
 #pragma unroll
-            for (int k = 0; k < NCODE; ++k) codes[k] = *reinterpret_cast<const u32x4*>(src + min(k * 64 + l, 8 * CPC - 1) * 16);
-            my_scale = p.kv_scale[(size_t)at * MK_TILE + (l & (MK_TILE - 1))];
+            for (int k = 0; k < NCODE; ++k) codes[t * NCODE + k] = *reinterpret_cast<const u32x4*>(src + min(k * 64 + l, 8 * CPC - 1) * 16);
+            my_scale[t] = p.kv_scale[(size_t)at * MK_TILE + (l & (MK_TILE - 1))];
         } else {
             const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * TILE_B + wave * (8 * ROWB);
-            const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)((v & 1) * TILE_B + wave * (8 * ROWB)));
+            const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)((u & 1) * (NT * TILE_B) + t * TILE_B + wave * (8 * ROWB)));
 #pragma unroll
             for (int k = 0; k < NLOAD; ++k) {
                 const uint32_t off = ((uint32_t)l * 16) ^ piece_key<CPR>(k, l);
@@ -146,39 +160,54 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             }
         }
     };
-    // (fp8) the requested codes, widened, into the slot of tile v
-    auto put = [&](int v) {
+    // (fp8) the requested codes, widened, into the slot of step u
+    auto put = [&](int u) {
         if constexpr (FP8) {
             const int l = my_lane();
-            LDS_AS unsigned char* rows = lds + (v & 1) * TILE_B + wave * (8 * ROWB);
 #pragma unroll
-            for (int k = 0; k < NCODE; ++k) {
+            for (int tk = 0; tk < NT * NCODE; ++tk) {
+                const int t = tk / NCODE, k = tk % NCODE;
+                LDS_AS unsigned char* rows = lds + (u & 1) * (NT * TILE_B) + t * TILE_B + wave * (8 * ROWB);
                 const int q = k * 64 + l;
                 if (8 * CPC % 64 && k == NCODE - 1 && q >= 8 * CPC) continue;
                 uint32_t w[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[k][i], 1.f, false));
-                    w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[k][i], 1.f, true));
+                    w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[tk][i], 1.f, false));
+                    w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[tk][i], 1.f, true));
                 }
                 // (the key is even: the second half's place is beside the first's)
                 const uint32_t to = (uint32_t)(q * 32) ^ piece_key<CPC>(k, l);
                 *(LDS_AS u32x4*)(rows + to) = (u32x4){w[0], w[1], w[2], w[3]};
                 *(LDS_AS u32x4*)(rows + (to ^ 16)) = (u32x4){w[4], w[5], w[6], w[7]};
             }
-            if (wave == 0 && l < MK_TILE) ks_lds[(v & 1) * MK_TILE + l] = my_scale;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                if (wave == t && l < MK_TILE) ks_lds[(u & 1) * (NT * MK_TILE) + t * MK_TILE + l] = my_scale[t];
         }
     };
 
-    // the first tile, and (fp8) the second one's codes
-    int here, next, after;
+    // the first step's tiles, and (fp8) the second one's codes.  Tiles of a step: their numbers in the pool
+    struct Places { int at[NT]; };
+    auto places = [&](int u) {
+        Places s;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) s.at[t] = v0 + NT * u + t < v1 ? tile_at(v0 + NT * u + t) : -1;
+        return s;
+    };
+    auto request_all = [&](const Places& s, int u) {
+        request(s.at[0], u, std::integral_constant<int, 0>{});
+        if constexpr (NT > 1) request(s.at[1], u, std::integral_constant<int, NT - 1>{});
+    };
+    const int steps = (v1 - v0 + NT - 1) / NT;
+    Places here, next, after;
     auto start = [&]() {
-        here = tile_at(v0);
-        next = tile_at(v0 + 1);
-        request(here, v0);
+        here = places(0);
+        next = places(1);
+        request_all(here, 0);
         if constexpr (FP8) {
-            put(v0);
-            request(next, v0 + 1);
+            put(0);
+            request_all(next, 1);
         }
     };
     start();
@@ -186,7 +215,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     // ---- this wavefront's query rows -> registers (B operands of the scores).  A negative scale changes their sign: the largest score is
     // then the largest scaled one
     bf16x8 qreg[2][NQ];
-    LDS_AS unsigned char* const q_lds = lds + 2 * TILE_B + 2 * VT_B + wave * ((NKS - NQ) * 2 * 1024) + lane * 16;      // this lane's, written and read by it alone
+    LDS_AS unsigned char* const q_lds = lds + 2 * NT * (TILE_B + VT_B) + wave * ((NKS - NQ) * 2 * 1024) + lane * 16;      // this lane's, written and read by it alone
     {
         const uint16_t* qa = static_cast<const uint16_t*>(p.q_abs) + (size_t)b * p.H * D_C;
         const uint16_t* qr = static_cast<const uint16_t*>(p.q_rope) + (size_t)b * p.H * 64;
@@ -238,10 +267,10 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         for (int e = 0; e < 4; ++e)
             t_base[e] = (uint32_t)(r * ROWB) + ((((uint32_t)(2 * e) + (uint32_t)((n & 3) >> 1)) ^ (uint32_t)swz_key(r)) << 4) + (uint32_t)((n & 1) * 8);
     }
-    LDS_AS unsigned char* const vt = lds + 2 * TILE_B;
+    LDS_AS unsigned char* const vt = lds + 2 * NT * TILE_B;
 
-    typedef f32x4 Scores[2][2];                // [block of 16 keys][query group]: keys 16 rb + 4g + i of query n
-    f32x4 ksc[2];                              // (fp8) scales of this lane's keys
+    typedef f32x4 Scores[NRB][2];              // [block of 16 keys][query group]: keys 16 rb + 4g + i of query n
+    f32x4 ksc[NRB];                            // (fp8) scales of this lane's keys
     bool poisoned[2] = {false, false};         // one of this lane's keys that its query sees was not finite
 
     // rows of tile v (bit: row) that the lane's query of group hi sees
@@ -261,7 +290,8 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         }
         return at < 0 ? 0u : sees & low(reach.end - row);
     };
-    auto mask = [&](Scores& x, int v, int at) {
+    // tile t of step u (tile v of the sequence)
+    auto mask = [&](Scores& x, int u, int t, int v, int at) {
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
             const uint32_t sees = visible(v, at, hi) >> (4 * g);
@@ -270,9 +300,9 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (sees >> (rb * 16 + i) & 1u) {
-                        if (FP8) poisoned[hi] |= !(fabsf(ksc[rb][i]) < INFINITY);
+                        if (FP8) poisoned[hi] |= !(fabsf(ksc[2 * t + rb][i]) < INFINITY);
                     } else {
-                        x[rb][hi][i] = -INFINITY;
+                        x[2 * t + rb][hi][i] = -INFINITY;
                     }
                 }
         }
@@ -280,11 +310,11 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) ksc[rb][i] = fabsf(ksc[rb][i]) < INFINITY ? ksc[rb][i] : 0.f;
+                for (int i = 0; i < 4; ++i) ksc[2 * t + rb][i] = fabsf(ksc[2 * t + rb][i]) < INFINITY ? ksc[2 * t + rb][i] : 0.f;
         }
         // a lane holds keys 4g .. 4g + 3 and 16 on of a column
         uint32_t odd[4] = {0u, 0u, 0u, 0u};
-        LDS_AS unsigned char* const share = vt + (v & 1) * VT_B + wave * (VT_B / 4) + lane * 16;
+        LDS_AS unsigned char* const share = vt + (u & 1) * (NT * VT_B) + t * VT_B + wave * (VT_B / 4) + lane * 16;
         for (int k = 0; k < NCT / 4; ++k) {
             const u32x4 w = *(LDS_AS u32x4*)(share + k * 1024);
 #pragma unroll
@@ -300,19 +330,19 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
                     if (who >> (16 * q) & 0xFFFFu) keys |= 1u << ((j < 4 ? j : 12 + j) + 4 * q);
             }
         }
-        if (lane == 0) odd_lds[(v & 1) * 4 + wave] = keys;
+        if (lane == 0) odd_lds[((u & 1) * NT + t) * 4 + wave] = keys;
     };
     // behind the barrier: the keys that some wavefront found; the rows that see them, and their values
-    auto clean = [&](int v, int at) {
-        const u32x4 found = *(LDS_AS u32x4*)(odd_lds + (v & 1) * 4);
+    auto clean = [&](int u, int t, int v, int at) {
+        const u32x4 found = *(LDS_AS u32x4*)(odd_lds + ((u & 1) * NT + t) * 4);
         const uint32_t keys = found[0] | found[1] | found[2] | found[3];
         if (__builtin_expect(keys == 0, 1)) return;
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) poisoned[hi] |= (visible(v, at, hi) & keys & (0x000F000Fu << (4 * g))) != 0;
         // (every wavefront for itself: it does not matter who comes first)
-        LDS_AS unsigned char* const tile = vt + (v & 1) * VT_B;
-        for (int u = lane; u < VT_B / 16; u += 64) {
-            LDS_AS u32x4* unit = (LDS_AS u32x4*)(tile + u * 16);
+        LDS_AS unsigned char* const tile = vt + (u & 1) * (NT * VT_B) + t * VT_B;
+        for (int i = lane; i < VT_B / 16; i += 64) {
+            LDS_AS u32x4* unit = (LDS_AS u32x4*)(tile + i * 16);
             u32x4 w = *unit;
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
@@ -332,7 +362,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi)
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb) top[hi] = max3(max3(top[hi], x[rb][hi][0], x[rb][hi][1]), x[rb][hi][2], x[rb][hi][3]);
+            for (int rb = 0; rb < NRB; ++rb) top[hi] = max3(max3(top[hi], x[rb][hi][0], x[rb][hi][1]), x[rb][hi][2], x[rb][hi][3]);
     };
     // maximum over the four lane groups (all 32 keys of a tile), on every lane
     auto over_groups = [&](float v) {
@@ -345,64 +375,70 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         bool left = false;
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
-            float tm = max3(x[0][hi][0], x[0][hi][1], x[0][hi][2]);
-            tm = max3(tm, x[0][hi][3], x[1][hi][0]);
-            tm = over_groups(max3(max3(tm, x[1][hi][1], x[1][hi][2]), x[1][hi][3], tm));
+            float tm = -INFINITY;
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) tm = max3(max3(tm, x[rb][hi][0], x[rb][hi][1]), x[rb][hi][2], x[rb][hi][3]);
+            tm = over_groups(tm);
             if (m_ref[hi] == -INFINITY) m_ref[hi] = tm == -INFINITY ? tm : tm * sc;
             left |= m_ref[hi] == -INFINITY;
         }
         unset = __any(left);
     };
-    // scores of a tile, just made: scaled (fp8) and masked
-    auto look_at = [&](Scores& x, int v, int at) {
+    // scores of step u, just made: scaled (fp8) and masked
+    auto look_at = [&](Scores& x, int u, const Places& s) {
         if constexpr (FP8) {
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb) {
-                ksc[rb] = *(LDS_AS f32x4*)(ks_lds + (v & 1) * MK_TILE + rb * 16 + g * 4);
+            for (int rb = 0; rb < NRB; ++rb) {
+                ksc[rb] = *(LDS_AS f32x4*)(ks_lds + (u & 1) * (NT * MK_TILE) + rb * 16 + g * 4);
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) x[rb][hi] *= ksc[rb];
             }
         }
-        if (__builtin_expect(!seen_whole(v, at), 0)) mask(x, v, at);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            if (__builtin_expect(!seen_whole(v0 + NT * u + t, s.at[t]), 0)) mask(x, u, t, v0 + NT * u + t, s.at[t]);
         raise_top(x);
         if (unset) set_reference(x);
     };
 
-    // ---- a step: S^T of the tile in `keys` and the weights of the tile before from its scores x (PV); then its values from `values`,
-    // and the transpose of the former tile into `to`
+    // ---- a step: S^T of the tiles in `keys` and the weights of those before from their scores x (PV); then their values from `values`,
+    // and the transposes of the former tiles into `to`
     auto step = [&](auto pv_tag, LDS_AS unsigned char* keys, LDS_AS unsigned char* values, LDS_AS unsigned char* to, const Scores& x, Scores& y) {
         constexpr bool PV = decltype(pv_tag)::value;
-        static constexpr int AHEAD = 4;               // k-steps that the key reads run ahead, one wavefront per SIMD with nothing else to hide them
-        static constexpr int VAHEAD = 4;              // column tiles that the value reads do
-        constexpr int SHARE = NCT / 4;         // column tiles that this wavefront transposes (8 / 4)
-        bf16x8 ka[2][NKS], va[NCT];
+        static constexpr int AHEAD = NT == 1 ? 4 : 2;     // k-steps that the key reads run ahead, one wavefront per SIMD with nothing else to hide them
+        static constexpr int VAHEAD = 4;                  // column tiles that the value reads do
+        static constexpr int SHARE = NT * NCT / 4;        // column tiles that this wavefront transposes (8)
+        bf16x8 ka[NRB][NKS], va[NT][NCT];
         float m_use[2];
-        uint32_t w[2][4];
+        uint32_t w[2][4 * NT];
         auto rk = [&](int ks) {
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb) ka[rb][ks] = *(LDS_AS bf16x8*)(keys + a_base[ks & 1] + (ks >> 1) * 128 + rb * 16 * ROWB);
+            for (int rb = 0; rb < NRB; ++rb) ka[rb][ks] = *(LDS_AS bf16x8*)(keys + a_base[ks & 1] + (ks >> 1) * 128 + rb * 16 * ROWB);
         };
         bf16x8 qa[NKS - NQ + 1][2];            // (one more: an array may not be empty)
         auto rq = [&](int ks) {
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) qa[ks - NQ][hi] = *(LDS_AS bf16x8*)(q_lds + ((ks - NQ) * 2 + hi) * 1024);
         };
-        auto rv = [&](int ct) { va[ct] = *(LDS_AS bf16x8*)(values + ct * 1024 + lane * 16); };
-        auto weigh = [&](int j) {              // pair j of 8: query group j / 4, keys 2 (j % 4) and the one after
-            const int hi = j >> 2, rb = (j >> 1) & 1, i = 2 * (j & 1);
+        auto rv = [&](int ct) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) va[t][ct] = *(LDS_AS bf16x8*)(values + t * VT_B + ct * 1024 + lane * 16);
+        };
+        auto weigh = [&](int j) {              // pair j of 8 NT: query group j / (4 NT), keys 2 (j % (4 NT)) and the one after
+            const int hi = j / (4 * NT), k = j % (4 * NT), rb = k >> 1, i = 2 * (k & 1);
             float e0 = fast_exp2(fmaf(x[rb][hi][i], sc, -m_use[hi])), e1 = fast_exp2(fmaf(x[rb][hi][i + 1], sc, -m_use[hi]));
             l_run[hi] += e0 + e1;
             if constexpr (FP8) { e0 *= ksc[rb][i]; e1 *= ksc[rb][i + 1]; }
-            w[hi][2 * rb + (j & 1)] = pack_bf16x2(e0, e1);
+            w[hi][k] = pack_bf16x2(e0, e1);
         };
         s16x4 lo[SHARE], up[SHARE];
-        auto rt = [&](int k) {                 // column tile wave * SHARE + k
-            LDS_AS unsigned char* at = keys + t_base[k & 3] + ((wave * SHARE + k) >> 2) * 128;
+        auto rt = [&](int k) {                 // column tile wave * NCT / 4 + k of a tile, the next tile's behind them
+            LDS_AS unsigned char* at = keys + (k / (NCT / 4)) * TILE_B + t_base[k & 3] + ((wave * (NCT / 4) + k % (NCT / 4)) >> 2) * 128;
             lo[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)at);
             up[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(at + 16 * ROWB));
         };
         auto wt = [&](int k) {
-            *(LDS_AS bf16x8*)(to + (wave * SHARE + k) * 1024 + lane * 16) =
+            *(LDS_AS bf16x8*)(to + (k / (NCT / 4)) * VT_B + (wave * (NCT / 4) + k % (NCT / 4)) * 1024 + lane * 16) =
                 __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo[k], up[k], 0, 1, 2, 3, 4, 5, 6, 7));
         };
         if constexpr (PV) {
@@ -422,14 +458,18 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
                     if (2 * (ks + AHEAD - NKS) + i < VAHEAD) rv(2 * (ks + AHEAD - NKS) + i);
             }
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb)
+            for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi)
-                    y[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[rb][ks], ks < NQ ? qreg[hi][ks < NQ ? ks : 0] : qa[ks < NQ ? 0 : ks - NQ][hi], ks == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : y[rb][hi], 0, 0, 0);
+                    y[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[rb][ks], ks < NQ ? qreg[hi][ks < NQ ? ks : 0] : qa[ks < NQ ? 0 : ks - NQ][hi],
+                                                                        ks == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : y[rb][hi], 0, 0, 0);
             if constexpr (PV) {
-                if (ks < 8) weigh(ks);
+                if (ks < 8) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < NT; ++i) weigh(NT * ks + i);
+                }
+#pragma unroll
+                for (int i = 0; i < 2 * NRB; ++i) {
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // an LDS read
                     __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);     // a matrix instruction
                     __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);     // vector instructions in its shadow
@@ -437,19 +477,24 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        bf16x8 pb[2];
+        bf16x8 pb[NT][2];
         if constexpr (PV) {
 #pragma unroll
-            for (int hi = 0; hi < 2; ++hi) pb[hi] = __builtin_bit_cast(bf16x8, (u32x4){w[hi][0], w[hi][1], w[hi][2], w[hi][3]});
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) pb[t][hi] = __builtin_bit_cast(bf16x8, (u32x4){w[hi][4 * t], w[hi][4 * t + 1], w[hi][4 * t + 2], w[hi][4 * t + 3]});
         }
+        constexpr int EVERY = NCT / SHARE;     // a column tile is transposed beside so many (4 / 2)
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) {
             if (PV && ct + VAHEAD < NCT) rv(ct + VAHEAD);
-            if (ct % 4 == 0) rt(ct / 4);
-            if (ct >= 6 && (ct - 6) % 4 == 0) wt((ct - 6) / 4);
+            if (ct % EVERY == 0) rt(ct / EVERY);
+            if (ct >= EVERY + EVERY / 2 && (ct - EVERY / 2) % EVERY == 0) wt((ct - EVERY / 2) / EVERY - 1);
             if constexpr (PV) {
 #pragma unroll
-                for (int hi = 0; hi < 2; ++hi) oacc[hi][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[ct], pb[hi], oacc[hi][ct], 0, 0, 0);
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int hi = 0; hi < 2; ++hi) oacc[hi][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[t][ct], pb[t][hi], oacc[hi][ct], 0, 0, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -462,8 +507,8 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     // reference by more than FAST_GAP (rare), a sweep for the exact maxima (it accumulates too, which is not used) and the
     // accumulation again against them.
     enum { ACCUMULATE, MAXIMA, ACCUMULATE_AGAIN };
-    auto slot = [&](int v) { return lds + (v & 1) * TILE_B; };
-    auto turned = [&](int v) { return vt + (v & 1) * VT_B; };
+    auto slot = [&](int u) { return lds + (u & 1) * (NT * TILE_B); };
+    auto turned = [&](int u) { return vt + (u & 1) * (NT * VT_B); };
     for (int pass = ACCUMULATE;;) {
         Scores x, y;
 #pragma unroll
@@ -476,33 +521,30 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         }
         if constexpr (!FP8) wait_vmcnt<0>();
         __syncthreads();
-        if constexpr (!FP8) {
-            if (v0 + 1 < v1) request(next, v0 + 1);
-        }
-        step(No{}, slot(v0), turned(v0), turned(v0), x, x);
-        look_at(x, v0, here);
-        auto iterate = [&](int v, Scores& x, Scores& y) {
-            after = v + 2 < v1 ? tile_at(v + 2) : -1;
+        if constexpr (!FP8) request_all(next, 1);
+        step(No{}, slot(0), turned(0), turned(0), x, x);
+        look_at(x, 0, here);
+        for (int u = 0; u < steps; ++u) {
+            after = places(u + 2);
             if constexpr (FP8) {
-                if (v + 1 < v1) put(v + 1);
+                if (u + 1 < steps) put(u + 1);
             } else {
                 wait_vmcnt<0>();
             }
-            __syncthreads();     // tile v + 1 and the transpose of tile v are there; everybody is done with tile v and the transpose before
-            request(after, v + 2);
+            __syncthreads();     // the tiles of step u + 1 and the transposes of those of step u are there; everybody is done with what lay before
+            request_all(after, u + 2);
             __builtin_amdgcn_sched_barrier(0);
-            if (__builtin_expect(!seen_whole(v, here), 0)) clean(v, here);
-            step(Yes{}, slot(v + 1), turned(v), turned(v + 1), x, y);
-            if (v + 1 < v1) look_at(y, v + 1, next);
-            here = next;
-            next = after;
-        };
-        for (int v = v0; v < v1; ++v) {
-            iterate(v, x, y);
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb)
+            for (int t = 0; t < NT; ++t)
+                if (__builtin_expect(!seen_whole(v0 + NT * u + t, here.at[t]), 0)) clean(u, t, v0 + NT * u + t, here.at[t]);
+            step(Yes{}, slot(u + 1), turned(u), turned(u + 1), x, y);
+            if (u + 1 < steps) look_at(y, u + 1, next);
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) x[rb][hi] = y[rb][hi];
+            here = next;
+            next = after;
         }
         if (pass == ACCUMULATE_AGAIN) break;
         if (pass == ACCUMULATE) {
@@ -536,7 +578,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         if ((who | who >> 16 | who >> 32 | who >> 48) >> n & 1u) inv[hi] = __uint_as_float(0x7FC00000u);
     }
     constexpr int RSO = D_C * 2 + 32;           // row stride of the transposed block (padded)
-    static_assert(4 * 32 * RSO <= 2 * TILE_B + 2 * VT_B, "exchange space must fit");
+    static_assert(4 * 32 * RSO <= 2 * NT * (TILE_B + VT_B), "exchange space must fit");
     LDS_AS unsigned char* mine = lds + wave * (32 * RSO);
     if (p.num_splits == 1) {
 #pragma unroll
