@@ -191,7 +191,10 @@ int mla_prefill_window(const void* q_nope, const void* q_rope, const void* W_UK,
         p.page_table = ids; p.num_pages = B * width;
     }
     p.pairs = (int)pairs; p.q_len = q_len; p.heads = heads; p.out = out; p.lse = lse;
-    p.scale = softmax_scale; p.window = window; p.sinks = sinks;
+    p.scale = softmax_scale;
+    // (a window or sinks past the table's end are all that there is)
+    const int rows = max_pages_per_seq * page_size;
+    p.window = std::min(window, rows); p.sinks = std::min(sinks, rows);
     e = launch_prefill_attention(p, stream);
     return e == hipSuccess ? MLA_OK : MLA_ERR_HIP;
 }

@@ -144,9 +144,8 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     // pages [0, head) and, behind the jump, from head + jump on
     int head = 0, jump = 0;
     if constexpr (WINDOW) {
-        const int64_t first = (int64_t)causal_from - p.window;    // first key of the first query's window
         head = (min(p.sinks, row1) + 63) / 64;
-        jump = max(0, (int)(max(first, (int64_t)0) / 64) - head);
+        jump = max(0, max(causal_from - p.window, 0) / 64 - head);          // (from the first key of the first query's window on)
     }
     auto page_of = [&](int u) { return !WINDOW || u < head ? u : u + jump; };
     auto row_of = [&](int t) { return !WINDOW || t < 2 * head ? t * TILE_ROWS : t * TILE_ROWS + jump * 64; };
@@ -176,17 +175,37 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
 #pragma unroll
     for (int k = 0; k < NLV; ++k) voff[k] = (uint32_t)(P * 16 + V0 + k * 4096);      // values: as they lie
     const uint32_t roff = (uint32_t)((P >> 3) * p.rope_pitch + (((P & 7) ^ (P >> 4 & 7)) << 4));
+    auto my_lane = [&]() -> int {                // (worked out where it is needed)
+        uint32_t all = ~0u;
+        asm volatile("" : "+s"(all));
+        return (int)__builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0u));
+    };
+    auto rope_off = [&]() -> uint32_t {
+        if constexpr (!WINDOW) return roff;
+        const int l = my_lane(), Q = wave * 64 + l;
+        return (uint32_t)((Q >> 3) * p.rope_pitch + (((Q & 7) ^ (Q >> 4 & 7)) << 4));
+    };
     const unsigned char* pool = static_cast<const unsigned char*>(p.pool) + (size_t)b * p.max_pages * PAGE_B;
     auto load16 = [&](const unsigned char* base, uint32_t off, uint32_t dst, auto at) {   // (base and dst are uniform)
         asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                      :: "s"(dst), "v"(off), "s"(base), "i"(decltype(at)::value) : "memory", "scc");
     };
+    // (WINDOW: one register for the places of all pieces, their distances in the base; its masks want the others, and a reload of a spilled
+    // one waits for every load before it)
     auto fetch_keys = [&](const unsigned char* src, uint32_t dst, auto at) {
         load16(src, koff[0], dst, at);
-        load16(src, koff[1], dst, std::integral_constant<int, decltype(at)::value + 4096>{});
+        load16(WINDOW ? src + 4096 : src, koff[WINDOW ? 0 : 1], dst, std::integral_constant<int, decltype(at)::value + 4096>{});
     };
     static_assert(NLK == 2 && NLV == 4);
     auto values_to = [&](const unsigned char* src, uint32_t dst) {
+        if constexpr (WINDOW) {
+            const unsigned char* mine = src + V0 + wave * 1024;
+            load16(mine, (uint32_t)(lane * 16), dst, std::integral_constant<int, V0>{});
+            load16(mine + 4096, (uint32_t)(lane * 16), dst, std::integral_constant<int, V0 + 4096>{});
+            load16(mine + 8192, (uint32_t)(lane * 16), dst, std::integral_constant<int, V0 + 8192>{});
+            load16(mine + 12288, (uint32_t)(lane * 16), dst, std::integral_constant<int, V0 + 12288>{});
+            return;
+        }
         load16(src, voff[0], dst, std::integral_constant<int, V0>{});
         load16(src, voff[1], dst, std::integral_constant<int, V0 + 4096>{});
         load16(src, voff[2], dst, std::integral_constant<int, V0 + 8192>{});
@@ -207,7 +226,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)((u & 1) * SLOT_B + wave * 1024));
         fetch_keys(src, dst, AtK1{});
         values_to(src, dst);
-        load16(rope + rope_page / 2, roff, dst, AtR1{});
+        load16(rope + rope_page / 2, rope_off(), dst, AtR1{});
         if (2 * u + 2 >= t1) return NLK + NLV + 1;
         if constexpr (WINDOW) fetch_keys(pool + (size_t)page_of(u + 1) * PAGE_B, dst, AtK2{});
         else                  fetch_keys(src + K2, dst, AtK2{});
@@ -216,7 +235,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
             asm volatile("" : "+v"(ids));       // (waited for here: behind the branch everybody would, for everything)
         }
         rope = rope_of(u + 1);
-        load16(rope, roff, dst, AtR2{});
+        load16(rope, rope_off(), dst, AtR2{});
         return 2 * NLK + NLV + 2;
     };
     // the first tile's keys are there
@@ -224,7 +243,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)(SLOT_B + wave * 1024));
         fetch_keys(pool + (size_t)page_of(0) * PAGE_B, dst, AtK2{});
         rope = rope_of(0);
-        load16(rope, roff, dst, AtR2{});
+        load16(rope, rope_off(), dst, AtR2{});
         if (fetch_unit(0) > NLK + NLV + 1) wait_vmcnt<2 * NLK + NLV + 2>();
         else                               wait_vmcnt<NLK + NLV + 1>();
         __syncthreads();
@@ -238,11 +257,19 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     auto rows_valid = [&](int t) { return all_there || !missing(((const CONST_AS int32_t*)ptab)[page_of(t >> 1)]) ? min(TILE_ROWS, row1 - row_of(t)) : 0; };
     // leading tiles that every query row of this workgroup sees whole
     const int n_full = all_there ? max(0, min(causal_from, row1)) / TILE_ROWS : 0;
-    const int64_t last_from = (int64_t)visible(min(hb + PA_ROWS, p.q_len) - 1) - p.window;      // (WINDOW) first key of the last query's window
+    // (WINDOW) [0, whole) and [whole_from, whole_to): of the sinks, and from the last query's first key to the first query's last
+    int whole = 0, whole_from = 0, whole_to = 0;
+    if constexpr (WINDOW) {
+        if (all_there) {
+            const int end = max(0, min(causal_from, row1)), from = max(0, visible(min(hb + PA_ROWS, p.q_len) - 1) - p.window);
+            whole = min(p.sinks, end) / TILE_ROWS;
+            whole_from = (from + TILE_ROWS - 1) / TILE_ROWS - 2 * jump;
+            whole_to = end / TILE_ROWS - 2 * jump;
+        }
+    }
     auto seen_whole = [&](int t) {
-        if constexpr (!WINDOW) return t < n_full;
-        const int row = row_of(t);
-        return all_there && row + TILE_ROWS <= min(causal_from, row1) && (row >= last_from || row + TILE_ROWS <= p.sinks);
+        if constexpr (WINDOW) return t < whole || (t >= whole_from && t < whole_to);
+        else                  return t < n_full;
     };
 
     // ---- per-lane state: this lane's queries = column n of the D tiles of the two groups
@@ -257,7 +284,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     // score A operand: key row 16 rb + n, chunk 4 ks + g (ks 4, 5: chunk 4 (ks - 4) + g of its rope part)
     uint32_t a_base[NKS];
 #pragma unroll
-    for (int ks = 0; ks < NKS; ++ks)
+    for (int ks = 0; ks < NKS; ++ks)              // (WINDOW: those of k-steps 0 and 4; the others differ in bits 6 and 7)
         a_base[ks] = ks < 4 ? (uint32_t)(n * ROWB + (((4 * ks + g) ^ n) << 4)) : (uint32_t)(n * ROPEB + (((4 * (ks - 4) + g) ^ (n >> 1)) << 4));
     // value A operand: dimension 16 ct + n, the eight keys of lane group g
     const uint32_t v_base = (uint32_t)(lane * 16);
@@ -304,18 +331,21 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
         int first = 4 * g;
         asm volatile("" : "+v"(first));
         if constexpr (WINDOW) {
+            const int l = my_lane(), mine = hb + wave * 32 + (l & 15);
+            first = l >> 4 << 2;
+            // keys of the tile that the query sees, a bit each; the lane's from bit 0 on
+            auto low = [](int k) -> uint32_t { return k <= 0 ? 0u : k >= 32 ? ~0u : (1u << k) - 1u; };
             bool odd = false;
-            const int key = row_of(t) + first;
+            const int row = row_of(t);
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) {
-                const int end = visible(hb + my_row + hi * 16);
-                const int64_t from = (int64_t)end - p.window;
+                const int end = visible(mine + hi * 16) - row;
+                const uint32_t sees = (low(min(end, n_valid)) & (~low(end - p.window) | low(p.sinks - row))) >> first;
 #pragma unroll
                 for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int at = rb * 16 + i, j = key + at;
-                        if (first + at < n_valid && j < end && (j >= from || j < p.sinks)) continue;
+                        if (sees >> (rb * 16 + i) & 1u) continue;
                         odd |= !(fabsf(x[rb][hi][i]) < INFINITY);
                         x[rb][hi][i] = -INFINITY;
                     }
@@ -362,9 +392,13 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     // PV = false: the scores alone (the first tile's).
     bf16x8 ka[2][NKS];
     auto rk = [&](uint32_t unit, bool second, int ks) {
+        uint32_t a = a_base[WINDOW ? ks & 4 : ks];
+        if constexpr (WINDOW) {
+            if (ks & 3) asm volatile("v_xor_b32 %0, %1, %0" : "+v"(a) : "i"((ks & 3) << 6));
+        }
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb)
-            ka[rb][ks] = *(LDS_AS bf16x8*)(lds + unit + a_base[ks] + (ks < 4 ? (second ? K2 : K1) + rb * 16 * ROWB : (second ? R2 : R1) + rb * 16 * ROPEB));
+            ka[rb][ks] = *(LDS_AS bf16x8*)(lds + unit + a + (ks < 4 ? (second ? K2 : K1) + rb * 16 * ROWB : (second ? R2 : R1) + rb * 16 * ROPEB));
     };
     auto step = [&](auto pv_tag, auto second_tag, uint32_t unit, const Scores& x, Scores& y) {
         constexpr bool PV = decltype(pv_tag)::value, SECOND = decltype(second_tag)::value;
