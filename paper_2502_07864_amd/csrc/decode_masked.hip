@@ -19,31 +19,16 @@
 // score exceeds it by more than 2^64 the chunk is done again against the exact maxima.  The normaliser sums the weights before
 // their rounding to bf16 in fp32; the weights' rounding (2^-8 of each) is the price of the bf16 instructions.
 //
-// Keys that a row does not see get the score -inf, in the tiles that need it.  There every wavefront also looks for values that are
-// not finite in the columns it has transposed; where there are any, they are cleared before anybody multiplies, and the rows that do see
-// such a key end as NaN.
-#include "masked_internal.h"
-#include "mfma_tile.h"
+// Keys that a row does not see get the score -inf, in the tiles that need it.  A key that is not finite has scores that are not: where
+// a wavefront meets one that some row of its own does not see, it clears what is not finite from the transposed tile before
+// it multiplies (0 times infinity would be a NaN), and the rows that do see the key end as NaN.
+#include "masked_tile.h"
 #include <type_traits>
 
 namespace mla {
 namespace {
 
 constexpr int MT_ROWS = MK_TALL_ROWS;        // query rows per workgroup
-
-// Swizzle of piece 64 k + lane of eight rows of PPR pieces each, as bits of an address: (row & 6) << 4.  A comparison or two per piece
-// instead of a register kept (or, as there are none left, spilled) for each.
-template <int PPR> __device__ __forceinline__ uint32_t piece_key(int k, int lane)
-{
-    const int first = k * 64 / PPR / 2;              // half the row of lane 0
-    uint32_t half = (uint32_t)first;
-#pragma unroll
-    for (int i = 1; i <= 2; ++i) {
-        const int from = 2 * (first + i) * PPR - 64 * k;
-        if (from < 64) half += lane >= from;
-    }
-    return half << 5;
-}
 
 template <int D_C, bool FP8>
 __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams p)
@@ -65,10 +50,8 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     __shared__ __attribute__((aligned(16))) float ks_smem[2][NT * MK_TILE];        // scales of an fp8 tile's rows
     __shared__ uint64_t tree_smem[64];
     __shared__ int token_smem[MT_ROWS];
-    __shared__ __attribute__((aligned(16))) uint32_t odd_smem[2][NT][4];          // keys of a tile whose values are not all finite, by wavefront
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
     LDS_AS float* ks_lds = (LDS_AS float*)ks_smem;
-    LDS_AS uint32_t* odd_lds = (LDS_AS uint32_t*)odd_smem;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -77,20 +60,9 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     // the groups of query rows of one chunk get linear ids 8 apart: same XCD, same time, so all but the first find the rows in its L2
     const int Z = (p.H + MT_ROWS - 1) / MT_ROWS;
     const int id = blockIdx.x, rr = id >> 3;
-    const int wg = (rr / Z) * 8 + (id & 7), zi = rr % Z;
+    const int zi = (int)((unsigned)rr % (unsigned)Z), wg = (rr - zi) / Z * 8 + (id & 7);
     if (wg >= p.B * p.num_splits) return;               // padding of the last group of 8
-    const int split = wg % p.num_splits;
-    int b = wg / p.num_splits;
-    // the longest sequences first (up to 64 of them: every workgroup ranks the lengths by itself): a long one started last would run on alone
-    if (p.B > 1 && p.B <= 64) {
-        const int mine = lane < p.B ? p.lens[lane] : -1;
-        int rank = 0;
-        for (int j = 0; j < p.B; ++j) {
-            const int other = __builtin_amdgcn_readlane(mine, j);
-            rank += other > mine || (other == mine && j < lane);
-        }
-        b = __builtin_amdgcn_readfirstlane(__builtin_ffsll((long long)__ballot(lane < p.B && rank == b)) - 1);
-    }
+    const int split = (int)((unsigned)wg % (unsigned)p.num_splits), b = sequence_at(p, (int)((unsigned)wg / (unsigned)p.num_splits), lane);
     const int hb = zi * MT_ROWS, HL = min(MT_ROWS, p.H - hb);
 
     const bool tree = p.tree != nullptr;
@@ -123,27 +95,27 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     int32_t ids = 0, ids_after = 0;                     // of the tiles v0 + 64 k on, and the 64 behind them
     auto tile_at = [&](int v) -> int {                  // (v: in the order of the sweep)
         if (((v - v0) & 63) == 0) {
-            ids = v == v0 ? ids_from(v0) : ids_after;
+            ids = ids_after;
             if (v + 64 < v1) ids_after = ids_from(v + 64);
         }
         return __builtin_amdgcn_readlane(ids, (v - v0) & 63);
+    };
+    auto tile_now = [&](int v) -> int {                 // (the first ones: a scalar load each, which waits for no vector load)
+        const int t = reach.tile(v), q = t / per_page;
+        const int page = ((const CONST_AS int32_t*)ptab)[q];
+        return page >= 0 && page < p.num_pages ? page * per_page + (t - q * per_page) : -1;
     };
 
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
     // A wavefront loads eight rows of a tile, which lie one behind the other as they do in the pool, 64 pieces at a time; chunk c of row r at
     // position c ^ key(r).
-    auto my_lane = [&]() -> int {                       // (worked out where it is needed)
-        uint32_t all = ~0u;
-        asm volatile("" : "+s"(all));
-        return (int)__builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0u));
-    };
     u32x4 codes[FP8 ? NT * NCODE : 1];
     float my_scale[NT];
     // tile t of step u, number `at` in the pool -> its place in slot u & 1: the loads (fp8: into registers)
     auto request = [&](int at, int u, auto tile_tag) {
         constexpr int t = decltype(tile_tag)::value;
         if (at < 0) return;                             // a page outside the pool is never dereferenced
-        const int l = my_lane();
+        const int l = lane_again();
         if constexpr (FP8) {
             const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * (MK_TILE * ROW) + wave * (8 * ROW);
 #pragma unroll
@@ -163,7 +135,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     // (fp8) the requested codes, widened, into the slot of step u
     auto put = [&](int u) {
         if constexpr (FP8) {
-            const int l = my_lane();
+            const int l = lane_again();
 #pragma unroll
             for (int tk = 0; tk < NT * NCODE; ++tk) {
                 const int t = tk / NCODE, k = tk % NCODE;
@@ -189,10 +161,10 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 
     // the first step's tiles, and (fp8) the second one's codes.  Tiles of a step: their numbers in the pool
     struct Places { int at[NT]; };
-    auto places = [&](int u) {
+    auto places = [&](int u, auto at) {
         Places s;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) s.at[t] = v0 + NT * u + t < v1 ? tile_at(v0 + NT * u + t) : -1;
+        for (int t = 0; t < NT; ++t) s.at[t] = v0 + NT * u + t < v1 ? at(v0 + NT * u + t) : -1;
         return s;
     };
     auto request_all = [&](const Places& s, int u) {
@@ -202,9 +174,11 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     const int steps = (v1 - v0 + NT - 1) / NT;
     Places here, next, after;
     auto start = [&]() {
-        here = places(0);
-        next = places(1);
+        here = places(0, tile_now);
+        next = places(1, tile_now);
         request_all(here, 0);
+        ids = ids_from(v0);
+        if (v0 + 64 < v1) ids_after = ids_from(v0 + 64);
         if constexpr (FP8) {
             put(0);
             request_all(next, 1);
@@ -233,20 +207,10 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             }
         }
     }
-    if (tree && tid < p.q_len) tree_smem[tid] = p.tree[b * p.tree_pitch + tid] & (p.q_len < 64 ? (1ull << p.q_len) - 1 : ~0ull);
+    if (tree && tid < p.q_len) tree_smem[tid] = tree_word(p, b, tid);
     if (tid < MT_ROWS) token_smem[tid] = (hb + min(tid, HL - 1)) / p.heads;        // (both are read in few tiles)
-    // tiles that all query rows of the workgroup see whole: [0, whole) and [whole_from, whole_to)
-    int whole, whole_from = 0, whole_to = 0;
-    if (tree) {
-        whole = reach.base / MK_TILE;
-    } else {
-        const int first = reach.base + hb / p.heads, last = reach.base + (hb + HL - 1) / p.heads;       // positions of its tokens
-        const int64_t outside = (int64_t)last - p.window;                                               // last row before all windows meet
-        whole = max(0, min(p.sinks, first + 1)) / MK_TILE;
-        whole_from = (outside < 0 ? 0 : (int)(outside / MK_TILE) + 1) - reach.skip;
-        whole_to = max(0, first + 1) / MK_TILE - reach.skip;
-    }
-    auto seen_whole = [&](int v, int at) { return at >= 0 && (v < whole || (v >= whole_from && v < whole_to)); };
+    const WholeTiles whole = whole_tiles(p, reach, hb / p.heads, (hb + HL - 1) / p.heads);
+    auto seen_whole = [&](int v, int at) { return at >= 0 && whole.holds(v); };
 
     // ---- per-lane state: this lane's queries = column n of the D tiles of the two groups
     float m_ref[2] = {-INFINITY, -INFINITY};   // reference of the exponentials (log2 units)
@@ -272,26 +236,16 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     typedef f32x4 Scores[NRB][2];              // [block of 16 keys][query group]: keys 16 rb + 4g + i of query n
     f32x4 ksc[NRB];                            // (fp8) scales of this lane's keys
     bool poisoned[2] = {false, false};         // one of this lane's keys that its query sees was not finite
+    bool dirty[NT] = {};                       // one that some query of the wavefront does not see was not, in tile t of the step
 
     // rows of tile v (bit: row) that the lane's query of group hi sees
     auto visible = [&](int v, int at, int hi) -> uint32_t {
-        auto low = [](int k) -> uint32_t { return k <= 0 ? 0u : k >= 32 ? ~0u : (1u << k) - 1u; };
-        const int row = reach.tile(v) * MK_TILE, token = token_smem[wave * 32 + hi * 16 + (my_lane() & 15)];
-        uint32_t sees;
-        if (tree) {
-            const uint64_t m = tree_smem[token];
-            const int d = reach.base - row;                // committed rows of the tile
-            sees = d >= 32 ? ~0u : d > 0 ? (uint32_t)(m << d) | low(d) : d > -64 ? (uint32_t)(m >> -d) : 0u;
-        } else {
-            const int t = reach.base + token;
-            const int64_t from = (int64_t)t - p.window + 1 - row;
-            const uint32_t old = low(from < 0 ? 0 : from > 32 ? 32 : (int)from), sunk = low(p.sinks - row);
-            sees = low(t + 1 - row) & (~old | sunk);
-        }
-        return at < 0 ? 0u : sees & low(reach.end - row);
+        const int token = token_smem[wave * 32 + hi * 16 + (lane_again() & 15)];
+        return at < 0 ? 0u : visible_rows(p, reach, reach.tile(v) * MK_TILE, token, tree ? tree_smem[token] : 0);
     };
-    // tile t of step u (tile v of the sequence)
-    auto mask = [&](Scores& x, int u, int t, int v, int at) {
+    // tile t of the step (tile v of the sequence)
+    auto mask = [&](Scores& x, int t, int v, int at) {
+        bool odd = false;
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
             const uint32_t sees = visible(v, at, hi) >> (4 * g);
@@ -299,75 +253,39 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
+                    const bool bad = !(fabsf(x[2 * t + rb][hi][i]) < INFINITY);
                     if (sees >> (rb * 16 + i) & 1u) {
-                        if (FP8) poisoned[hi] |= !(fabsf(ksc[2 * t + rb][i]) < INFINITY);
+                        poisoned[hi] |= bad;
                     } else {
+                        odd |= bad;
                         x[2 * t + rb][hi][i] = -INFINITY;
                     }
                 }
         }
-        if constexpr (FP8) {                   // (nothing is multiplied with a scale that is not finite)
+        dirty[t] = __any(odd);
+        if (FP8 && dirty[t]) {                 // (nothing is multiplied with a scale that is not finite)
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) ksc[2 * t + rb][i] = fabsf(ksc[2 * t + rb][i]) < INFINITY ? ksc[2 * t + rb][i] : 0.f;
         }
-        // a lane holds keys 4g .. 4g + 3 and 16 on of a column
-        uint32_t odd[4] = {0u, 0u, 0u, 0u};
-        LDS_AS unsigned char* const share = vt + (u & 1) * (NT * VT_B) + t * VT_B + wave * (VT_B / 4) + lane * 16;
-        for (int k = 0; k < NCT / 4; ++k) {
-            const u32x4 w = *(LDS_AS u32x4*)(share + k * 1024);
-#pragma unroll
-            for (int d = 0; d < 4; ++d) odd[d] |= ((w[d] & 0x7F80u) == 0x7F80u ? 1u : 0u) | ((w[d] & 0x7F800000u) == 0x7F800000u ? 2u : 0u);
-        }
-        uint32_t keys = 0;
-        if (__builtin_expect(__any(odd[0] | odd[1] | odd[2] | odd[3]), 0)) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint64_t who = __ballot(odd[j >> 1] >> (j & 1) & 1u);
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (who >> (16 * q) & 0xFFFFu) keys |= 1u << ((j < 4 ? j : 12 + j) + 4 * q);
-            }
-        }
-        if (lane == 0) odd_lds[((u & 1) * NT + t) * 4 + wave] = keys;
     };
-    // behind the barrier: the keys that some wavefront found; the rows that see them, and their values
-    auto clean = [&](int u, int t, int v, int at) {
-        const u32x4 found = *(LDS_AS u32x4*)(odd_lds + ((u & 1) * NT + t) * 4);
-        const uint32_t keys = found[0] | found[1] | found[2] | found[3];
-        if (__builtin_expect(keys == 0, 1)) return;
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi) poisoned[hi] |= (visible(v, at, hi) & keys & (0x000F000Fu << (4 * g))) != 0;
-        // (every wavefront for itself: it does not matter who comes first)
-        LDS_AS unsigned char* const tile = vt + (u & 1) * (NT * VT_B) + t * VT_B;
+    // (every wavefront that has to does this for itself: it does not matter who comes first)
+    auto clean = [&](LDS_AS unsigned char* tile) {
         for (int i = lane; i < VT_B / 16; i += 64) {
             LDS_AS u32x4* unit = (LDS_AS u32x4*)(tile + i * 16);
             u32x4 w = *unit;
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                if ((w[d] & 0x7F80u) == 0x7F80u) w[d] &= 0xFFFF0000u;
-                if ((w[d] & 0x7F800000u) == 0x7F800000u) w[d] &= 0xFFFFu;
-            }
+            for (int d = 0; d < 4; ++d) w[d] = finite_halves(w[d]);
             *unit = w;
         }
     };
     float top[2] = {-INFINITY, -INFINITY};     // largest score of the sweep so far, this lane's keys (unscaled)
-    auto max3 = [](float a, float b, float c) {
-        float r;                    // (a NaN loses, as in fmaxf; written out: fmaxf would quieten every operand first)
-        asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-        return r;
-    };
     auto raise_top = [&](const Scores& x) {
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi)
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) top[hi] = max3(max3(top[hi], x[rb][hi][0], x[rb][hi][1]), x[rb][hi][2], x[rb][hi][3]);
-    };
-    // maximum over the four lane groups (all 32 keys of a tile), on every lane
-    auto over_groups = [&](float v) {
-        v = fmaxf(v, __shfl_xor(v, 16));
-        return fmaxf(v, __shfl_xor(v, 32));
+            for (int rb = 0; rb < NRB; ++rb) top[hi] = max_of(max_of(top[hi], x[rb][hi][0], x[rb][hi][1]), x[rb][hi][2], x[rb][hi][3]);
     };
     // the reference of a query row: the maximum of its first tile with a row that it sees
     bool unset = true;
@@ -377,7 +295,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         for (int hi = 0; hi < 2; ++hi) {
             float tm = -INFINITY;
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) tm = max3(max3(tm, x[rb][hi][0], x[rb][hi][1]), x[rb][hi][2], x[rb][hi][3]);
+            for (int rb = 0; rb < NRB; ++rb) tm = max_of(max_of(tm, x[rb][hi][0], x[rb][hi][1]), x[rb][hi][2], x[rb][hi][3]);
             tm = over_groups(tm);
             if (m_ref[hi] == -INFINITY) m_ref[hi] = tm == -INFINITY ? tm : tm * sc;
             left |= m_ref[hi] == -INFINITY;
@@ -396,7 +314,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-            if (__builtin_expect(!seen_whole(v0 + NT * u + t, s.at[t]), 0)) mask(x, u, t, v0 + NT * u + t, s.at[t]);
+            if (__builtin_expect(!seen_whole(v0 + NT * u + t, s.at[t]), 0)) mask(x, t, v0 + NT * u + t, s.at[t]);
         raise_top(x);
         if (unset) set_reference(x);
     };
@@ -525,7 +443,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         step(No{}, slot(0), turned(0), turned(0), x, x);
         look_at(x, 0, here);
         for (int u = 0; u < steps; ++u) {
-            after = places(u + 2);
+            after = places(u + 2, tile_at);
             if constexpr (FP8) {
                 if (u + 1 < steps) put(u + 1);
             } else {
@@ -536,7 +454,10 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                if (__builtin_expect(!seen_whole(v0 + NT * u + t, here.at[t]), 0)) clean(u, t, v0 + NT * u + t, here.at[t]);
+                if (__builtin_expect(dirty[t], 0)) {
+                    clean(turned(u) + t * VT_B);
+                    dirty[t] = false;
+                }
             step(Yes{}, slot(u + 1), turned(u), turned(u + 1), x, y);
             if (u + 1 < steps) look_at(y, u + 1, next);
 #pragma unroll

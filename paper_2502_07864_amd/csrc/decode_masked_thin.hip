@@ -1,0 +1,347 @@
+// Masked attention over the latent cache on the matrix cores for few query rows (bf16 queries and cache): 32 query rows per workgroup.
+//
+//   S^T [keys x 32] = K [keys x (d_c + 64)] . Q^T,   O^T [d_c x 32] += V^T [d_c x keys] . P^T,   V = the first d_c columns of K
+//
+// Few rows are bound by the stream of the cache.  The four wavefronts of a workgroup have the same 32 query rows and take the chunk's
+// tiles of 32 keys in turn, each with a place of its own in the LDS and a softmax of its own: no barrier until the end, where the four
+// results are joined.  A wavefront waits for its tile, scores, weighs and accumulates it, and asks for its next one; while one waits the
+// others compute, so that two or three tiles of a CU are on their way at any time, and a chunk of up to four tiles is one round trip.
+//
+// References of the exponentials, masks and keys that are not finite: as in the kernel for many rows (decode_masked.hip), but that a
+// wavefront goes over its tiles again by itself where a score exceeds its reference by more than 2^64.
+#include "masked_tile.h"
+#include <type_traits>
+
+namespace mla {
+namespace {
+
+template <int D_C>
+__global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams p)
+{
+    constexpr int ROW = D_C + 64, ROWB = ROW * 2, CPR = ROWB / 16;
+    constexpr int TILE_B = MK_TILE * ROWB;
+    constexpr int NLOAD = TILE_B / 1024;                // 16-byte loads per lane and tile (36 / 20)
+    constexpr int NKS = ROW / 32, NCT = D_C / 16;
+
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE_B];
+    __shared__ uint64_t tree_smem[64];
+    __shared__ float m_smem[4][32], l_smem[4][32];
+    LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, g = lane >> 4;
+
+    // the groups of query rows of one chunk get linear ids 8 apart: same XCD, same time, so all but the first find the rows in its L2
+    const int Z = (p.H + MK_THIN_ROWS - 1) / MK_THIN_ROWS;
+    const int id = blockIdx.x, rr = id >> 3;
+    const int zi = (int)((unsigned)rr % (unsigned)Z), wg = (rr - zi) / Z * 8 + (id & 7);
+    if (wg >= p.B * p.num_splits) return;               // padding of the last group of 8
+    const int split = (int)((unsigned)wg % (unsigned)p.num_splits), b = sequence_at(p, (int)((unsigned)wg / (unsigned)p.num_splits), lane);
+    const int hb = zi * MK_THIN_ROWS, HL = min(MK_THIN_ROWS, p.H - hb);
+
+    const bool tree = p.tree != nullptr;
+    const Reach reach = reach_of(((const CONST_AS int32_t*)p.lens)[b], p.q_len, p.max_pages * p.page_size, tree, p.window, p.sinks);
+    const int v0 = chunk_start(reach.tiles, split, p.num_splits), v1 = chunk_start(reach.tiles, split + 1, p.num_splits);
+    auto part_of = [&](int r) { return part_index(b, hb + r, split, p.H, p.num_splits); };
+    if (v0 >= v1) {                                     // nothing to see
+        for (int r = wave; r < HL; r += 4) {
+            if (p.num_splits == 1)
+                for (int c = lane * 8; c < D_C; c += 512)
+                    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.o_part) + part_of(r) * D_C + c) = (u32x4){0u, 0u, 0u, 0u};
+            if (lane == 0 && p.lse_part) p.lse_part[part_of(r)] = -INFINITY;
+        }
+        return;
+    }
+
+    // ---- this wavefront's tiles: v0 + wave, + 4, ...; where they lie in the pool (-1: not there), 64 of them at a time, a lane each
+    const int32_t* const ptab = p.page_table + (size_t)b * p.max_pages;
+    const int per_page = p.page_size / MK_TILE;
+    auto place = [&](int v, auto table) {
+        const int t = reach.tile(min(v, v1 - 1)), q = t / per_page;
+        const int page = table[q];
+        return page >= 0 && page < p.num_pages ? page * per_page + (t - q * per_page) : -1;
+    };
+    LDS_AS unsigned char* const tile = lds + wave * TILE_B;
+    const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tile);
+    auto request = [&](int at) {
+        if (at < 0) return;                             // a page outside the pool is never dereferenced
+        const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * TILE_B;
+        const int l = lane_again();
+#pragma unroll
+        for (int k = 0; k < NLOAD; ++k) {
+            const uint32_t off = ((uint32_t)l * 16) ^ piece_key<CPR>(k, l);
+            asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                         :: "s"(dst), "v"(off), "s"(src + k * 1024), "i"(k * 1024) : "memory", "scc");
+        }
+    };
+    int at;
+    int32_t ids;
+    auto start = [&]() {
+        at = v0 + wave < v1 ? place(v0 + wave, (const CONST_AS int32_t*)ptab) : -1;
+        request(at);
+        ids = place(v0 + wave + 4 * lane, ptab);
+    };
+    start();
+
+    // ---- the query rows -> registers (B operands of the scores; a negative scale changes their sign)
+    bf16x8 qreg[2][NKS];
+    {
+        const uint16_t* qa = static_cast<const uint16_t*>(p.q_abs) + (size_t)b * p.H * D_C;
+        const uint16_t* qr = static_cast<const uint16_t*>(p.q_rope) + (size_t)b * p.H * 64;
+        const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+            const size_t row = hb + min(hi * 16 + n, HL - 1);
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) {
+                u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + ks * 32 + g * 8)
+                                        : *reinterpret_cast<const u32x4*>(qr + row * 64 + (ks - D_C / 32) * 32 + g * 8);
+                v ^= (u32x4){flip, flip, flip, flip};
+                qreg[hi][ks] = __builtin_bit_cast(bf16x8, v);
+            }
+        }
+    }
+    if (tree) {
+        if (tid < p.q_len) tree_smem[tid] = tree_word(p, b, tid);
+        __syncthreads();
+    }
+    const WholeTiles whole = whole_tiles(p, reach, hb / p.heads, (hb + HL - 1) / p.heads);
+    int token[2];
+#pragma unroll
+    for (int hi = 0; hi < 2; ++hi) token[hi] = (hb + min(hi * 16 + n, HL - 1)) / p.heads;
+
+    // ---- per-lane state: this lane's queries = column n of the D tiles of the two groups
+    float m_ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+    bool poisoned[2] = {false, false};
+    f32x4 oacc[2][NCT];
+    const float sc = fmaxf(fabsf(p.scale) * LOG2E, 1.17549435e-38f);     // (never zero: a masked score is -inf and has to stay it)
+
+    // score A operand: key row 16 rb + n, chunk 4 ks + g; transposing reads: tile row 4g + (n >> 2) (and 16 more), 8 bytes at column 16 ct + 4 (n & 3)
+    uint32_t a_base[2], t_base[4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) a_base[e] = (uint32_t)(n * ROWB) + ((((uint32_t)(4 * e + g)) ^ (uint32_t)swz_key(n)) << 4);
+    {
+        const int r = g * 4 + (n >> 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            t_base[e] = (uint32_t)(r * ROWB) + ((((uint32_t)(2 * e) + (uint32_t)((n & 3) >> 1)) ^ (uint32_t)swz_key(r)) << 4) + (uint32_t)((n & 1) * 8);
+    }
+
+    // ---- sweeps over the tiles: ACCUMULATE against the references, and where some score exceeded its own by more than FAST_GAP (rare) one
+    // for the exact maxima (it accumulates too, which is not used) and one against them
+    enum { ACCUMULATE, MAXIMA, ACCUMULATE_AGAIN };
+    bool unset = true;
+    for (int pass = ACCUMULATE;;) {
+        float top[2] = {-INFINITY, -INFINITY};          // largest score of the sweep so far, this lane's keys (unscaled)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+            l_run[hi] = 0.f;
+            poisoned[hi] = false;
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) oacc[hi][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+        int turn = 0;
+        for (int v = v0 + wave; v < v1; v += 4, ++turn) {
+            if (turn && (turn & 63) == 0) ids = place(v + 4 * lane, ptab);
+            wait_vmcnt<0>();
+            __builtin_amdgcn_sched_barrier(0);
+
+            // ---- scores
+            f32x4 x[2][2];
+            {
+                bf16x8 ka[2][NKS];
+                auto rk = [&](int ks) {
+#pragma unroll
+                    for (int rb = 0; rb < 2; ++rb) ka[rb][ks] = *(LDS_AS bf16x8*)(tile + a_base[ks & 1] + (ks >> 1) * 128 + rb * 16 * ROWB);
+                };
+                static constexpr int AHEAD = 4;
+#pragma unroll
+                for (int ks = 0; ks < AHEAD; ++ks) rk(ks);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int ks = 0; ks < NKS; ++ks) {
+                    if (ks + AHEAD < NKS) rk(ks + AHEAD);
+#pragma unroll
+                    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                        for (int hi = 0; hi < 2; ++hi)
+                            x[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[rb][ks], qreg[hi][ks], ks == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : x[rb][hi], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (__builtin_expect(at < 0 || !whole.holds(v), 0)) {
+                bool odd = false;
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) {
+                    const uint32_t sees = (at < 0 ? 0u : visible_rows(p, reach, reach.tile(v) * MK_TILE, token[hi], tree ? tree_smem[token[hi]] : 0)) >> (4 * g);
+#pragma unroll
+                    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const bool bad = !(fabsf(x[rb][hi][i]) < INFINITY);
+                            if (sees >> (rb * 16 + i) & 1u) {
+                                poisoned[hi] |= bad;
+                            } else {
+                                odd |= bad;
+                                x[rb][hi][i] = -INFINITY;
+                            }
+                        }
+                }
+                if (__builtin_expect(__any(odd), 0))        // values that are not finite, of keys that somebody does not see
+                    for (int i = lane; i < TILE_B / 16; i += 64) {
+                        LDS_AS u32x4* unit = (LDS_AS u32x4*)(tile + i * 16);
+                        u32x4 w = *unit;
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) w[d] = finite_halves(w[d]);
+                        *unit = w;
+                    }
+            }
+            // ---- weights
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+                for (int rb = 0; rb < 2; ++rb) top[hi] = max_of(max_of(top[hi], x[rb][hi][0], x[rb][hi][1]), x[rb][hi][2], x[rb][hi][3]);
+            if (unset) {                                    // the reference of a query row: the maximum of its first tile with a row that it sees
+                bool left = false;
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) {
+                    const float t = over_groups(top[hi]);   // (no tile before had one: the maximum so far is this tile's)
+                    if (m_ref[hi] == -INFINITY && t != -INFINITY) m_ref[hi] = t * sc;
+                    left |= m_ref[hi] == -INFINITY;
+                }
+                unset = __any(left);
+            }
+            bf16x8 pb[2];
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+                const float m_use = m_ref[hi] == -INFINITY ? 0.f : m_ref[hi];
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float e0 = fast_exp2(fmaf(x[k >> 1][hi][2 * (k & 1)], sc, -m_use)), e1 = fast_exp2(fmaf(x[k >> 1][hi][2 * (k & 1) + 1], sc, -m_use));
+                    l_run[hi] += e0 + e1;
+                    w[k] = pack_bf16x2(e0, e1);
+                }
+                pb[hi] = __builtin_bit_cast(bf16x8, (u32x4){w[0], w[1], w[2], w[3]});
+            }
+            // ---- values
+            {
+                s16x4 lo[NCT], up[NCT];
+                auto rt = [&](int ct) {
+                    LDS_AS unsigned char* from = tile + t_base[ct & 3] + (ct >> 2) * 128;
+                    lo[ct] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)from);
+                    up[ct] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(from + 16 * ROWB));
+                };
+                static constexpr int AHEAD = 4;
+#pragma unroll
+                for (int ct = 0; ct < AHEAD; ++ct) rt(ct);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int ct = 0; ct < NCT; ++ct) {
+                    if (ct + AHEAD < NCT) rt(ct + AHEAD);
+                    const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo[ct], up[ct], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int hi = 0; hi < 2; ++hi) oacc[hi][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[hi], oacc[hi][ct], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            // (every read of the tile has been waited for: its place is free)
+            if (v + 4 < v1) {
+                at = __builtin_amdgcn_readlane(ids, (turn + 1) & 63);
+                if (((turn + 1) & 63) == 0) at = place(v + 4, (const CONST_AS int32_t*)ptab);
+                request(at);
+            }
+        }
+        if (pass == ACCUMULATE_AGAIN) break;
+        if (pass == ACCUMULATE) {
+            // (an infinite score makes a NaN of its row either way, and no other row shall be the worse for it)
+            const bool jumped = (top[0] * sc > m_ref[0] + FAST_GAP && top[0] < INFINITY) || (top[1] * sc > m_ref[1] + FAST_GAP && top[1] < INFINITY);
+            if (__builtin_expect(!__any(jumped), 1)) break;
+            pass = MAXIMA;
+            unset = false;
+        } else {
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+                const float t = over_groups(top[hi]);
+                m_ref[hi] = t == -INFINITY ? t : t * sc;
+            }
+            pass = ACCUMULATE_AGAIN;
+        }
+        start();
+    }
+
+    // ---- the four wavefronts joined: reference and normaliser of every row, then the columns in two halves through the LDS
+    float lt[2];
+#pragma unroll
+    for (int hi = 0; hi < 2; ++hi) {
+        float l = l_run[hi] + __shfl_xor(l_run[hi], 16);
+        lt[hi] = l + __shfl_xor(l, 32);
+        const uint64_t who = __ballot(poisoned[hi]);
+        if ((who | who >> 16 | who >> 32 | who >> 48) >> n & 1u) poisoned[hi] = true;
+        if (g == 0) {
+            m_smem[wave][hi * 16 + n] = m_ref[hi];
+            l_smem[wave][hi * 16 + n] = lt[hi];
+        }
+    }
+    __syncthreads();
+    float f[2];                                         // of this wavefront's sums
+#pragma unroll
+    for (int hi = 0; hi < 2; ++hi) {
+        const int r = hi * 16 + n;
+        float m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, m_smem[w][r]);
+        const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float lw = l_smem[w][r], mw = m_smem[w][r];
+            if (lw != 0.f) l += lw * (mw == -INFINITY ? 1.f : fast_exp2(mw - ref));       // (-inf with a sum: a NaN)
+        }
+        f[hi] = lt[hi] == 0.f ? 0.f : (m_ref[hi] == -INFINITY ? 1.f : fast_exp2(m_ref[hi] - ref)) / l;
+        if (poisoned[hi]) f[hi] = __uint_as_float(0x7FC00000u);
+        if (wave == 0 && g == 0 && r < HL && p.lse_part) p.lse_part[part_of(r)] = l == 0.f ? -INFINITY : ref * LN2 + __builtin_amdgcn_logf(l) * LN2;
+    }
+    constexpr int RSO = D_C * 2 + 16;                   // bytes from row to row of half the columns in fp32 (padded)
+    static_assert(32 * RSO <= TILE_B, "exchange space must fit in a tile's place");
+    constexpr int LPR = D_C / 8;                        // lanes of half a row, four columns each
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if (half) __syncthreads();
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+            for (int ct = 0; ct < NCT / 2; ++ct)
+                *(LDS_AS f32x4*)(tile + (hi * 16 + n) * RSO + (ct * 16 + g * 4) * 4) = oacc[hi][half * (NCT / 2) + ct] * f[hi];
+        __syncthreads();
+        for (int r = tid / LPR; r < HL; r += MF_THREADS / LPR) {
+            const int c = tid % LPR;
+            f32x4 o = *(LDS_AS f32x4*)(lds + r * RSO + c * 16);
+#pragma unroll
+            for (int w = 1; w < 4; ++w) o += *(LDS_AS f32x4*)(lds + w * TILE_B + r * RSO + c * 16);
+            const size_t to = part_of(r) * D_C + half * (D_C / 2) + c * 4;
+            if (p.num_splits == 1)
+                *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.o_part) + to) = (u32x2){pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+            else
+                *reinterpret_cast<f32x4*>(static_cast<float*>(p.o_part) + to) = o;
+        }
+    }
+}
+
+}  // namespace
+
+bool masked_thin_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache)
+{
+    // Up to 64 rows: each group of 32 reads the tiles again (from L2), where the kernel for many rows is bound by a tile's round trip
+    return masked_tall_supported(p, io, cache) && cache == MLA_BF16 && p.H <= 64;
+}
+
+hipError_t launch_masked_thin(const MaskedParams& p, hipStream_t s)
+{
+    const unsigned chunks = ((unsigned)p.B * p.num_splits + 7) / 8 * 8, Z = (unsigned)((p.H + MK_THIN_ROWS - 1) / MK_THIN_ROWS);
+    if (p.d_c == 512) masked_thin_kernel<512><<<dim3(chunks * Z), dim3(MF_THREADS), 0, s>>>(p);
+    else              masked_thin_kernel<256><<<dim3(chunks * Z), dim3(MF_THREADS), 0, s>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace mla

@@ -10,10 +10,12 @@
 // No arithmetic, no allocation, no state beyond the entry points' addresses; the interpreter lock is released
 // around the call as ctypes does.
 #include <torch/csrc/autograd/python_variable.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
 #include "mla_gfx950.h"
 #include "mla_layer_gfx950.h"
+#include "mla_masked_gfx950.h"
 
 namespace {
 
@@ -28,6 +30,9 @@ decltype(&mla_quantize_rows) p_quantize;
 decltype(&mla_gemm_fp8) p_gemm_fp8;
 decltype(&mla_rope_queries) p_rope;
 decltype(&mla_cache_store) p_store;
+decltype(&mla_decode_paged_tree) p_tree;
+decltype(&mla_decode_paged_window) p_window;
+decltype(&mla_cache_move) p_move;
 
 struct No {};   // the arguments are not of the plain kind
 
@@ -399,11 +404,101 @@ PyObject* cache_store(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
-// (addresses of the eleven entry points, in the order above)
+// the tensors of a masked call lie together, on the current device (elsewhere the binding makes theirs the current one)
+void together(const at::Tensor& first, PyObject* const* others, int n)
+{
+    require(first.device().index() == c10::hip::current_device());
+    for (int i = 0; i < n; ++i)
+        if (others[i] != Py_None) require(THPVariable_CheckExact(others[i]) && THPVariable_Unpack(others[i]).device() == first.device());
+}
+
+// (q_abs [B, T, H, d_c], q_rope | None, kv_cache, page_table, lens, kv_scale | None, workspace, out, lse | None, tree_mask | None, window, sinks,
+//  scale, flags)
+PyObject* decode_masked(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        require(n == 14);
+        const at::Tensor &q = tensor(a[0]), &kv = tensor(a[2]), &table = tensor(a[3]), &lens = tensor(a[4]), &ws = tensor(a[6]);
+        together(q, a + 1, 9);
+        require(q.dim() == 4 && kv.dim() == 3 && table.dim() == 2 && lens.dim() == 1);
+        const int64_t B = q.size(0), T = q.size(1), H = q.size(2), d_c = q.size(3), pages = kv.size(0), page = kv.size(1), d_rope = kv.size(2) - d_c;
+        require(d_rope >= 0);
+        void* pr = nullptr;
+        if (d_rope) {
+            const at::Tensor& r = tensor(a[1]);
+            require(r.dim() == 4 && r.size(0) == B && r.size(1) == T && r.size(2) == H && r.size(3) == d_rope && r.scalar_type() == q.scalar_type());
+            pr = r.data_ptr();
+        } else {
+            require(a[1] == Py_None);
+        }
+        require(table.scalar_type() == at::kInt && lens.scalar_type() == at::kInt && table.size(0) == B && lens.size(0) == B);
+        const float* ps = nullptr;
+        if (a[5] != Py_None) {
+            const at::Tensor& s = tensor(a[5]);
+            require(s.scalar_type() == at::kFloat && s.dim() == 2 && s.size(0) == pages && s.size(1) == page);
+            ps = static_cast<const float*>(s.data_ptr());
+        }
+        const mla_dtype io = io_type(q), cache = cache_type(kv);
+        const at::Tensor& out = tensor(a[7]);
+        require(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type());
+        float* pl = nullptr;
+        if (a[8] != Py_None) {
+            const at::Tensor& l = tensor(a[8]);
+            require(l.scalar_type() == at::kFloat && l.dim() == 3 && l.size(0) == B && l.size(1) == T && l.size(2) == H);
+            pl = static_cast<float*>(l.data_ptr());
+        }
+        void *pq = q.data_ptr(), *pkv = kv.data_ptr(), *pws = ws.data_ptr(), *po = out.data_ptr(), *s = stream_of(q);
+        const auto* pt = static_cast<const int32_t*>(table.data_ptr());
+        const auto* pn = static_cast<const int32_t*>(lens.data_ptr());
+        const size_t bytes = ws.nbytes();
+        const int b = dim(B), t = dim(T), h = dim(H), dc = dim(d_c), dr = dim(d_rope), pg = dim(page), np = dim(pages), mp = dim(table.size(1)),
+                  window = (int)integer(a[10]), sinks = (int)integer(a[11]), flags = (int)integer(a[13]);
+        const float scale = real(a[12]);
+        if (a[9] == Py_None)
+            return unlocked([&] {
+                return p_window(pq, pr, pkv, ps, pt, pn, po, pl, pws, bytes, b, t, h, dc, dr, pg, np, mp, window, sinks, scale, io, cache, (unsigned)flags, s);
+            });
+        const at::Tensor& m = tensor(a[9]);
+        require(m.scalar_type() == at::kLong && ((m.dim() == 2 && m.size(0) == B && m.size(1) == T) || (m.dim() == 1 && m.size(0) == T)));
+        const auto* pm = static_cast<const uint64_t*>(m.data_ptr());
+        const int64_t pitch = m.dim() == 2 ? T : 0;
+        return unlocked([&] {
+            return p_tree(pq, pr, pkv, ps, pt, pn, pm, pitch, po, pl, pws, bytes, b, t, h, dc, dr, pg, np, mp, scale, io, cache, (unsigned)flags, s);
+        });
+    });
+}
+
+// (kv_cache, kv_scale | None, page_table, src, dst)
+PyObject* cache_move(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        require(n == 5);
+        const at::Tensor &kv = tensor(a[0]), &table = tensor(a[2]), &src = tensor(a[3]), &dst = tensor(a[4]);
+        together(kv, a + 1, 4);
+        require(kv.dim() == 3 && table.dim() == 2 && src.dim() == 2 && dst.sizes() == src.sizes() && table.size(0) == src.size(0));
+        require(table.scalar_type() == at::kInt && src.scalar_type() == at::kInt && dst.scalar_type() == at::kInt);
+        float* ps = nullptr;
+        require((a[1] != Py_None) == (cache_type(kv) == MLA_FP8_E4M3));
+        if (a[1] != Py_None) {
+            const at::Tensor& s = tensor(a[1]);
+            require(s.scalar_type() == at::kFloat && s.dim() == 2 && s.size(0) == kv.size(0) && s.size(1) == kv.size(1));
+            ps = static_cast<float*>(s.data_ptr());
+        }
+        void *pkv = kv.data_ptr(), *s = stream_of(kv);
+        const auto* pt = static_cast<const int32_t*>(table.data_ptr());
+        const auto* p0 = static_cast<const int32_t*>(src.data_ptr());
+        const auto* p1 = static_cast<const int32_t*>(dst.data_ptr());
+        const int b = dim(src.size(0)), m = dim(src.size(1)), row = dim(kv.size(2) * kv.element_size()), page = dim(kv.size(1)), pages = dim(kv.size(0)),
+                  mp = dim(table.size(1));
+        return unlocked([&] { return p_move(pkv, ps, pt, p0, p1, b, m, row, page, pages, mp, s); });
+    });
+}
+
+// (addresses of the fourteen entry points, in the order above)
 PyObject* bind(PyObject*, PyObject* args)
 {
-    unsigned long long p[11];
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKKK", p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6, p + 7, p + 8, p + 9, p + 10)) return nullptr;
+    unsigned long long p[14];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKK", p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6, p + 7, p + 8, p + 9, p + 10, p + 11, p + 12, p + 13)) return nullptr;
     p_absorb_q = reinterpret_cast<decltype(p_absorb_q)>(p[0]);
     p_out_proj = reinterpret_cast<decltype(p_out_proj)>(p[1]);
     p_decode = reinterpret_cast<decltype(p_decode)>(p[2]);
@@ -415,12 +510,16 @@ PyObject* bind(PyObject*, PyObject* args)
     p_gemm_fp8 = reinterpret_cast<decltype(p_gemm_fp8)>(p[8]);
     p_rope = reinterpret_cast<decltype(p_rope)>(p[9]);
     p_store = reinterpret_cast<decltype(p_store)>(p[10]);
+    p_tree = reinterpret_cast<decltype(p_tree)>(p[11]);
+    p_window = reinterpret_cast<decltype(p_window)>(p[12]);
+    p_move = reinterpret_cast<decltype(p_move)>(p[13]);
     Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(absorb_q), FAST(out_proj), FAST(decode), FAST(merge_out_proj), FAST(merge_partials), FAST(cache_append),
                          FAST(rms_norm), FAST(quantize_rows), FAST(gemm_fp8), FAST(rope_queries), FAST(cache_store),
+                         FAST(decode_masked), FAST(cache_move),
                          {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 

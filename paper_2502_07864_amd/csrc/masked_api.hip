@@ -19,7 +19,7 @@ int chunks(int B, int64_t H, int rows, int64_t tiles)
     if (groups >= 4096) return 1;       // (rounds enough; and what is left fits the merge's grid)
     int best = 1;
     double least = 1e300;
-    for (int s = 1; s <= 64 && s <= tiles; ++s) {
+    for (int s = 1; s <= MK_MAX_CHUNKS && s <= tiles; ++s) {
         const double rounds = (double)((groups * s + 255) / 256);
         const double cost = rounds * ((double)((tiles + s - 1) / s) + 5.0) + (s > 1 ? 3.0 + 4e-4 * (double)(B * H) * s : 0.0);
         if (cost < least * 0.999) { least = cost; best = s; }
@@ -45,7 +45,9 @@ size_t workspace_bytes_for(int B, int q_len, int heads, int d_c, int64_t tiles)
 {
     // (which kernel a call takes hangs on its types, which are not asked for here)
     const int64_t H = (int64_t)q_len * heads;
-    return std::max(plan_of(B, H, d_c, tiles, MK_PORTABLE_ROWS).total, plan_of(B, H, d_c, tiles, MK_TALL_ROWS).total);
+    size_t most = 0;
+    for (int rows : {MK_PORTABLE_ROWS, MK_THIN_ROWS, MK_TALL_ROWS}) most = std::max(most, plan_of(B, H, d_c, tiles, rows).total);
+    return most;
 }
 
 bool sizes_ok(int B, int q_len, int heads, int d_c, int max_rows)
@@ -62,6 +64,10 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
         p.max_pages <= 0 || !(p.scale == p.scale) || (!tree && (p.window < 1 || p.sinks < 0)) || p.tree_pitch < 0)
         return MLA_ERR_SHAPE;
     if ((int64_t)p.max_pages * p.page_size > 0x7FFFFFFF) return MLA_ERR_SHAPE;
+    if ((int64_t)p.max_pages * p.page_size > MK_MAX_ROWS) return MLA_ERR_UNSUPPORTED;
+    // (a window or sinks past the table's end are all that there is)
+    p.window = std::min(p.window, p.max_pages * p.page_size);
+    p.sinks = std::min(p.sinks, p.max_pages * p.page_size);
     if (tree && p.tree_pitch > 0 && p.tree_pitch < p.q_len) return MLA_ERR_SHAPE;
     if (io != MLA_F32 && io != MLA_BF16) return MLA_ERR_UNSUPPORTED;
     if (cache != MLA_F32 && cache != MLA_BF16 && cache != MLA_FP8_E4M3) return MLA_ERR_UNSUPPORTED;
@@ -73,11 +79,11 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
     const int64_t H = (int64_t)p.q_len * p.heads;
     if (H > MAX_QUERY_ROWS || (tree && p.q_len > 64)) return MLA_ERR_UNSUPPORTED;
     p.H = (int)H;
+    const bool matrix = !(flags & MLA_FLAG_PORTABLE_KERNEL) && masked_tall_supported(p, io, cache), thin = matrix && masked_thin_supported(p, io, cache);
     const int64_t tiles = most_tiles(p.q_len, (int64_t)p.max_pages * p.page_size, tree, p.window, p.sinks);
     const size_t need = workspace_bytes_for(p.B, p.q_len, p.heads, p.d_c, tiles);
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return MLA_ERR_WORKSPACE;
-    const bool tall = !(flags & MLA_FLAG_PORTABLE_KERNEL) && masked_tall_supported(p, io, cache);
-    const Plan plan = plan_of(p.B, H, p.d_c, tiles, tall ? MK_TALL_ROWS : MK_PORTABLE_ROWS);
+    const Plan plan = plan_of(p.B, H, p.d_c, tiles, thin ? MK_THIN_ROWS : matrix ? MK_TALL_ROWS : MK_PORTABLE_ROWS);
     p.num_splits = plan.S;
     if (plan.S == 1) {
         p.o_part = o_lat;
@@ -87,7 +93,7 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
         p.lse_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.lse_off);
     }
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    hipError_t e = tall ? launch_masked_tall(p, cache, stream) : launch_masked_portable(p, io, cache, stream);
+    hipError_t e = thin ? launch_masked_thin(p, stream) : matrix ? launch_masked_tall(p, cache, stream) : launch_masked_portable(p, io, cache, stream);
     if (e == hipSuccess && plan.S > 1) e = launch_masked_merge(p, o_lat, lse, io, stream);
     return e == hipSuccess ? MLA_OK : MLA_ERR_HIP;
 }
@@ -162,6 +168,7 @@ int mla_prefill_window(const void* q_nope, const void* q_rope, const void* W_UK,
         return MLA_ERR_SHAPE;
     if ((int64_t)max_pages_per_seq * page_size > 0x7FFFFFFF) return MLA_ERR_SHAPE;
     if (!prefill_supported(d_head, d_c, d_rope, page_size, io_dtype, cache_dtype)) return MLA_ERR_UNSUPPORTED;
+    if ((int64_t)max_pages_per_seq * page_size > MK_MAX_ROWS || q_len > MK_MAX_ROWS / 2) return MLA_ERR_UNSUPPORTED;
     const int width = reachable_pages(q_len, max_pages_per_seq, window, sinks);
     const int64_t pairs = (int64_t)B * heads;
     if (pairs > 65535 || width > 65535 * 16 || pairs * width > 0x7FFFFFFF || (pairs + 7) / 8 * 8 * (((int64_t)q_len + 63) / 64) > 0x7FFFFFFF)

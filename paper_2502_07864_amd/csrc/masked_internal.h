@@ -47,9 +47,9 @@ __host__ __device__ __forceinline__ Reach reach_of(int len, int q_len, int cap, 
     r.base = len - q_len;
     r.end = len;
     r.tiles = (len + MK_TILE - 1) / MK_TILE;
-    const int64_t first = (int64_t)r.base - window + 1;       // first row of token 0's window
-    const int first_tile = first > 0 ? (int)(first / MK_TILE) : 0;
-    r.head = (int)(((int64_t)(sinks < len ? sinks : len) + MK_TILE - 1) / MK_TILE);
+    const int first = r.base - window + 1;                    // first row of token 0's window (the entry points see to it that it fits)
+    const int first_tile = first > 0 ? first / MK_TILE : 0;
+    r.head = ((sinks < len ? sinks : len) + MK_TILE - 1) / MK_TILE;
     if (first_tile > r.head) r.skip = first_tile - r.head;
     r.tiles -= r.skip;
     return r;
@@ -64,8 +64,11 @@ inline int64_t most_tiles(int q_len, int64_t cap, bool tree, int window, int sin
     return some < all ? some : all;
 }
 
-// chunk s of S: tiles [first, last)
-__host__ __device__ __forceinline__ int chunk_start(int tiles, int s, int S) { return (int)((int64_t)tiles * s / S); }
+constexpr int MK_MAX_ROWS = 1 << 30;      // of a page table: windows, sinks and their sums fit 32 bits, and
+constexpr int MK_MAX_CHUNKS = 64;         // so does a tile's number times this
+
+// chunk s of S: tiles [chunk_start(s), chunk_start(s + 1))
+__host__ __device__ __forceinline__ int chunk_start(int tiles, int s, int S) { return (int)((unsigned)tiles * (unsigned)s / (unsigned)S); }
 
 // portable scalar-FMA kernel: every type pair, width and page size of mla_decode_paged
 hipError_t launch_masked_portable(const MaskedParams& p, mla_dtype io, mla_dtype cache, hipStream_t s);
@@ -74,6 +77,10 @@ constexpr int MK_PORTABLE_ROWS = 4;       // query rows of a workgroup
 bool       masked_tall_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache);
 hipError_t launch_masked_tall(const MaskedParams& p, mla_dtype cache, hipStream_t s);
 constexpr int MK_TALL_ROWS = 128;
+// the same with 32 query rows per workgroup, whose wavefronts take the tiles in turn (bf16 caches)
+bool       masked_thin_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache);
+hipError_t launch_masked_thin(const MaskedParams& p, hipStream_t s);
+constexpr int MK_THIN_ROWS = 32;
 // the chunks' results (S > 1) merged
 hipError_t launch_masked_merge(const MaskedParams& p, void* o_lat, float* lse, mla_dtype io, hipStream_t s);
 

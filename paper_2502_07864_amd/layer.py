@@ -301,6 +301,11 @@ def cache_move(kv_cache: torch.Tensor, page_table: torch.Tensor, src: torch.Tens
                kv_scale: Optional[torch.Tensor] = None) -> None:
     """Row dst[b, i] of sequence b becomes its row src[b, i], bit for bit, with its scale; src and dst [B, moves] int32
     logical positions, moves <= 64, -1 for none.  All rows of a sequence are read before any is written."""
+    if mla._fast is not None:
+        status = mla._fast.cache_move(kv_cache, kv_scale, page_table, src, dst)
+        if status is not None:
+            _check(status, "mla_cache_move")
+            return
     if kv_cache.dim() != 3 or page_table.dim() != 2 or src.dim() != 2:
         raise ValueError("kv_cache must be [num_pages, page_size, d_c + d_rope], page_table [B, max_pages_per_seq], src [B, moves]")
     num_pages, page_size, row = kv_cache.shape

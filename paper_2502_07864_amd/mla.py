@@ -54,7 +54,7 @@ def _load_marshal(L: ctypes.CDLL):
     _marshal.bind(*(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in
                     ("mla_absorb_q", "mla_out_proj", "mla_decode_paged_multi", "mla_merge_out_proj_multi",
                      "mla_merge_partials", "mla_cache_append", "mla_rms_norm", "mla_quantize_rows", "mla_gemm_fp8",
-                     "mla_rope_queries", "mla_cache_store")))
+                     "mla_rope_queries", "mla_cache_store", "mla_decode_paged_tree", "mla_decode_paged_window", "mla_cache_move")))
     return _marshal
 
 
@@ -512,6 +512,12 @@ def decode_paged_tree(q_abs: torch.Tensor, q_rope: Optional[torch.Tensor], kv_ca
     holds prefix_lens[b] committed rows and behind them the drafted tokens' rows, token k's at position prefix + k; token i
     sees the committed rows and drafted row k iff bit k of tree_mask[b, i] is set (int64 [B, q_len], or [q_len]: one tree
     for all; q_len <= 64).  Returns o_lat [B,q_len,H,d_c] (and lse [B,q_len,H] fp32 if return_lse or lse given)."""
+    if _fast is not None and workspace is not None and out is not None and not (return_lse and lse is None) and tree_mask is not None:
+        status = _fast.decode_masked(q_abs, q_rope, kv_cache, page_table, prefix_lens, kv_scale, workspace, out, lse, tree_mask, 1, 0,
+                                     softmax_scale, flags)
+        if status is not None:
+            _check(status, "mla_decode_paged_tree")
+            return (out, lse) if lse is not None else out
     B, T, H, d_c, d_rope = _decode_masked(q_abs, q_rope, kv_cache, page_table, prefix_lens, kv_scale)
     if tree_mask.dtype not in (torch.int64, torch.uint64):
         raise TypeError("tree_mask must be int64 or uint64")
@@ -546,6 +552,12 @@ def decode_paged_window(q_abs: torch.Tensor, q_rope: Optional[torch.Tensor], kv_
     """decode_paged_multi with a sliding window and a few first rows that stay visible: token i, at position
     t = seq_len - q_len + i, sees row j <= t iff j > t - window or j < sinks.  Pages whose rows no token sees are not read
     and may have been given back (-1 in the table)."""
+    if _fast is not None and workspace is not None and out is not None and not (return_lse and lse is None):
+        status = _fast.decode_masked(q_abs, q_rope, kv_cache, page_table, seq_lens, kv_scale, workspace, out, lse, None, window, sinks,
+                                     softmax_scale, flags)
+        if status is not None:
+            _check(status, "mla_decode_paged_window")
+            return (out, lse) if lse is not None else out
     B, T, H, d_c, d_rope = _decode_masked(q_abs, q_rope, kv_cache, page_table, seq_lens, kv_scale)
     num_pages, page_size, _ = kv_cache.shape
     out = _result(out, q_abs, (B, T, H, d_c), q_abs.dtype, "out")
