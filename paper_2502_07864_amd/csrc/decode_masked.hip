@@ -193,18 +193,27 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     {
         const uint16_t* qa = static_cast<const uint16_t*>(p.q_abs) + (size_t)b * p.H * D_C;
         const uint16_t* qr = static_cast<const uint16_t*>(p.q_rope) + (size_t)b * p.H * 64;
-        const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
             const size_t row = hb + min(wave * 32 + hi * 16 + n, HL - 1);
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks) {
-                u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + ks * 32 + g * 8)
+                const u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + ks * 32 + g * 8)
                                         : *reinterpret_cast<const u32x4*>(qr + row * 64 + (ks - D_C / 32) * 32 + g * 8);
-                v ^= (u32x4){flip, flip, flip, flip};
                 if (ks < NQ) qreg[hi][ks] = __builtin_bit_cast(bf16x8, v);
                 else         *(LDS_AS u32x4*)(q_lds + ((ks - NQ) * 2 + hi) * 1024) = v;
             }
+        }
+        if (p.scale < 0.f) {
+            asm volatile("");                           // (a branch, not 144 instructions for everybody)
+            const u32x4 sign = (u32x4){0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+                for (int ks = 0; ks < NKS; ++ks) {
+                    if (ks < NQ) qreg[hi][ks] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, qreg[hi][ks]) ^ sign);
+                    else         *(LDS_AS u32x4*)(q_lds + ((ks - NQ) * 2 + hi) * 1024) ^= sign;
+                }
         }
     }
     if (tree && tid < p.q_len) tree_smem[tid] = tree_word(p, b, tid);

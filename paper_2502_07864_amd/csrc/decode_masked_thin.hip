@@ -7,6 +7,9 @@
 // results are joined.  A wavefront waits for its tile, scores, weighs and accumulates it, and asks for its next one; while one waits the
 // others compute, so that two or three tiles of a CU are on their way at any time, and a chunk of up to four tiles is one round trip.
 //
+// A small call is bound by round trips (length, page, tile, and one for whatever of the code comes first: what runs once is kept short,
+// loops instead of their copies).
+//
 // References of the exponentials, masks and keys that are not finite: as in the kernel for many rows (decode_masked.hip), but that a
 // wavefront goes over its tiles again by itself where a score exceeds its reference by more than 2^64.
 #include "masked_tile.h"
@@ -20,12 +23,13 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 {
     constexpr int ROW = D_C + 64, ROWB = ROW * 2, CPR = ROWB / 16;
     constexpr int TILE_B = MK_TILE * ROWB;
-    constexpr int NLOAD = TILE_B / 1024;                // 16-byte loads per lane and tile (36 / 20)
     constexpr int NKS = ROW / 32, NCT = D_C / 16;
 
     __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE_B];
     __shared__ uint64_t tree_smem[64];
-    __shared__ float m_smem[4][32], l_smem[4][32];
+    __shared__ float m_smem[4][32], l_smem[4][32];      // reference and normaliser of every wavefront's rows
+    __shared__ __attribute__((aligned(16))) float f_smem[32][4];         // and factor
+    __shared__ uint8_t bad_smem[4][32];
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -68,11 +72,16 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
         if (at < 0) return;                             // a page outside the pool is never dereferenced
         const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * TILE_B;
         const int l = lane_again();
+        constexpr int EIGHT = CPR / 8;                  // loads of eight rows, after which the swizzle repeats
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int k = 0; k < NLOAD; ++k) {
-            const uint32_t off = ((uint32_t)l * 16) ^ piece_key<CPR>(k, l);
-            asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                         :: "s"(dst), "v"(off), "s"(src + k * 1024), "i"(k * 1024) : "memory", "scc");
+            for (int k = 0; k < EIGHT; ++k) {
+                const uint32_t off = ((uint32_t)l * 16) ^ piece_key<CPR>(k, l);
+                const uint32_t to = dst + (uint32_t)(i * EIGHT + k) * 1024u;
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(to), "v"(off), "s"(src + k * 1024) : "memory");
+            }
+            src += EIGHT * 1024;
         }
     };
     int at;
@@ -89,18 +98,24 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
     {
         const uint16_t* qa = static_cast<const uint16_t*>(p.q_abs) + (size_t)b * p.H * D_C;
         const uint16_t* qr = static_cast<const uint16_t*>(p.q_rope) + (size_t)b * p.H * 64;
-        const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
             const size_t row = hb + min(hi * 16 + n, HL - 1);
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks) {
-                u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + ks * 32 + g * 8)
+                const u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + ks * 32 + g * 8)
                                         : *reinterpret_cast<const u32x4*>(qr + row * 64 + (ks - D_C / 32) * 32 + g * 8);
-                v ^= (u32x4){flip, flip, flip, flip};
                 qreg[hi][ks] = __builtin_bit_cast(bf16x8, v);
             }
         }
+    }
+    if (p.scale < 0.f) {
+        asm volatile("");                               // (a branch, not 144 instructions for everybody)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks)
+                qreg[hi][ks] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, qreg[hi][ks]) ^ (u32x4){0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u});
     }
     if (tree) {
         if (tid < p.q_len) tree_smem[tid] = tree_word(p, b, tid);
@@ -271,36 +286,31 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
         start();
     }
 
-    // ---- the four wavefronts joined: reference and normaliser of every row, then the columns in two halves through the LDS
-    float lt[2];
+    // ---- the four wavefronts joined: each one's factor for every row, then the columns in two halves through the LDS
 #pragma unroll
     for (int hi = 0; hi < 2; ++hi) {
         float l = l_run[hi] + __shfl_xor(l_run[hi], 16);
-        lt[hi] = l + __shfl_xor(l, 32);
+        l += __shfl_xor(l, 32);
         const uint64_t who = __ballot(poisoned[hi]);
-        if ((who | who >> 16 | who >> 32 | who >> 48) >> n & 1u) poisoned[hi] = true;
         if (g == 0) {
             m_smem[wave][hi * 16 + n] = m_ref[hi];
-            l_smem[wave][hi * 16 + n] = lt[hi];
+            l_smem[wave][hi * 16 + n] = l;
+            bad_smem[wave][hi * 16 + n] = (who | who >> 16 | who >> 32 | who >> 48) >> n & 1u;
         }
     }
     __syncthreads();
-    float f[2];                                         // of this wavefront's sums
-#pragma unroll
-    for (int hi = 0; hi < 2; ++hi) {
-        const int r = hi * 16 + n;
-        float m = -INFINITY, l = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) m = fmaxf(m, m_smem[w][r]);
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float lw = l_smem[w][r], mw = m_smem[w][r];
-            if (lw != 0.f) l += lw * (mw == -INFINITY ? 1.f : fast_exp2(mw - ref));       // (-inf with a sum: a NaN)
+    if (tid < 128) {
+        const int w = tid >> 5, r = tid & 31;
+        const float m = fmaxf(fmaxf(m_smem[0][r], m_smem[1][r]), fmaxf(m_smem[2][r], m_smem[3][r])), ref = m == -INFINITY ? 0.f : m;
+        float l = 0.f, mine = 0.f;
+        for (int k = 0; k < 4; ++k) {
+            const float lk = l_smem[k][r], mk = m_smem[k][r];
+            const float e = lk == 0.f ? 0.f : mk == -INFINITY ? 1.f : fast_exp2(mk - ref);       // (-inf with a sum: a NaN)
+            if (lk != 0.f) l += lk * e;
+            if (k == w) mine = e;
         }
-        f[hi] = lt[hi] == 0.f ? 0.f : (m_ref[hi] == -INFINITY ? 1.f : fast_exp2(m_ref[hi] - ref)) / l;
-        if (poisoned[hi]) f[hi] = __uint_as_float(0x7FC00000u);
-        if (wave == 0 && g == 0 && r < HL && p.lse_part) p.lse_part[part_of(r)] = l == 0.f ? -INFINITY : ref * LN2 + __builtin_amdgcn_logf(l) * LN2;
+        f_smem[r][w] = bad_smem[w][r] ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : mine / l;
+        if (w == 0 && r < HL && p.lse_part) p.lse_part[part_of(r)] = l == 0.f ? -INFINITY : ref * LN2 + __builtin_amdgcn_logf(l) * LN2;
     }
     constexpr int RSO = D_C * 2 + 16;                   // bytes from row to row of half the columns in fp32 (padded)
     static_assert(32 * RSO <= TILE_B, "exchange space must fit in a tile's place");
@@ -311,19 +321,38 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi)
 #pragma unroll
-            for (int ct = 0; ct < NCT / 2; ++ct)
-                *(LDS_AS f32x4*)(tile + (hi * 16 + n) * RSO + (ct * 16 + g * 4) * 4) = oacc[hi][half * (NCT / 2) + ct] * f[hi];
+            for (int ct = 0; ct < NCT / 2; ++ct) *(LDS_AS f32x4*)(tile + (hi * 16 + n) * RSO + (ct * 16 + g * 4) * 4) = oacc[hi][half * (NCT / 2) + ct];
         __syncthreads();
-        for (int r = tid / LPR; r < HL; r += MF_THREADS / LPR) {
-            const int c = tid % LPR;
-            f32x4 o = *(LDS_AS f32x4*)(lds + r * RSO + c * 16);
+        constexpr int STEP = MF_THREADS / LPR, TURNS = 32 / STEP, BATCH = 4;      // rows at a time; (all reads of a batch on their way before any is used)
+        const int c = tid % LPR;
+#pragma unroll 1
+        for (int k0 = 0; k0 < TURNS; k0 += BATCH) {
+            f32x4 part[BATCH][4];
+            float f[BATCH][4];
 #pragma unroll
-            for (int w = 1; w < 4; ++w) o += *(LDS_AS f32x4*)(lds + w * TILE_B + r * RSO + c * 16);
-            const size_t to = part_of(r) * D_C + half * (D_C / 2) + c * 4;
-            if (p.num_splits == 1)
-                *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.o_part) + to) = (u32x2){pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
-            else
-                *reinterpret_cast<f32x4*>(static_cast<float*>(p.o_part) + to) = o;
+            for (int k = 0; k < BATCH; ++k)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int r = tid / LPR + (k0 + k) * STEP;
+                    part[k][w] = *(LDS_AS f32x4*)(lds + w * TILE_B + r * RSO + c * 16);
+                    f[k][w] = f_smem[r][w];
+                }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const int r = tid / LPR + (k0 + k) * STEP;
+                f32x4 o = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < 4; ++w)             // (what a wavefront without a row that counts has is nothing, not even times zero)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = fmaf(f[k][w], f[k][w] != 0.f ? part[k][w][i] : 0.f, o[i]);
+                if (r >= HL) continue;
+                const size_t to = part_of(r) * D_C + half * (D_C / 2) + c * 4;
+                if (p.num_splits == 1)
+                    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.o_part) + to) = (u32x2){pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+                else
+                    *reinterpret_cast<f32x4*>(static_cast<float*>(p.o_part) + to) = o;
+            }
         }
     }
 }
