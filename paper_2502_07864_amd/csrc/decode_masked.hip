@@ -28,26 +28,29 @@
 namespace mla {
 namespace {
 
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+
 constexpr int MT_ROWS = MK_TALL_ROWS;        // query rows per workgroup
 
 template <int D_C, bool FP8>
 __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams p)
 {
-    constexpr int ROW = D_C + 64, ROWB = ROW * 2;       // of a tile in LDS (bf16)
-    constexpr int CPR = ROWB / 16;                      // 16-byte chunks per row (72 / 40)
+    constexpr int ROW = D_C + 64, ROWB = FP8 ? ROW : ROW * 2;
+    constexpr int CPR = ROWB / 16;                      // 16-byte chunks per row (bf16: 72 / 40, fp8: 36 / 20)
     constexpr int TILE_B = MK_TILE * ROWB;
     constexpr int NT = D_C == 512 ? 1 : 2;              // tiles of a step (as many as fit twice into the LDS, with their transposes)
     constexpr int NRB = 2 * NT;                         // and their blocks of 16 keys
-    constexpr int NLOAD = TILE_B / (MF_THREADS * 16);   // 16-byte loads per thread and bf16 tile (9 / 5)
+    constexpr int RING = FP8 ? 3 : 2;                   // places for a step's tiles
+    constexpr int NLOAD = TILE_B / (MF_THREADS * 16);   // (bf16) 16-byte loads per thread and tile (9 / 5)
+    constexpr int FLOAD = 8 * ROWB / 1024;              // (fp8) loads of 1 KB for eight rows of a tile (4 / 2), and one of half as much
     constexpr int NKS = ROW / 32;                       // k-steps of the scores (18 / 10)
     constexpr int NCT = D_C / 16;                       // column tiles of the values (32 / 16)
     constexpr int VT_B = D_C * MK_TILE * 2;             // a transposed tile
-    constexpr int NQ = D_C == 512 ? NKS - 2 : NKS;      // k-steps whose queries stay in registers; those of the rope part don't fit, and lie in LDS
-    constexpr int CPC = ROW / 16;                       // 16-byte pieces per fp8 row (36 / 20)
-    constexpr int NCODE = (8 * CPC + 63) / 64;          // per lane, of eight rows (5 / 3, the last by half of the lanes)
+    constexpr int NQ = D_C == 256 ? NKS : FP8 ? NKS - 4 : NKS - 2;      // k-steps whose queries stay in registers; the last ones' don't fit, and lie in LDS
 
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * NT * (TILE_B + VT_B) + (NKS - NQ) * 2 * MF_THREADS * 16];
-    __shared__ __attribute__((aligned(16))) float ks_smem[2][NT * MK_TILE];        // scales of an fp8 tile's rows
+    constexpr int VT_AT = RING * NT * TILE_B;           // the transposes lie behind the tiles, the queries' rope parts behind them
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[VT_AT + 2 * NT * VT_B + (NKS - NQ) * 2 * MF_THREADS * 16];
+    __shared__ __attribute__((aligned(16))) float ks_smem[FP8 ? RING : 1][64];     // (fp8) scales of a step's rows
     __shared__ uint64_t tree_smem[64];
     __shared__ int token_smem[MT_ROWS];
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
@@ -109,57 +112,21 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
     // A wavefront loads eight rows of a tile, which lie one behind the other as they do in the pool, 64 pieces at a time; chunk c of row r at
     // position c ^ key(r).
-    u32x4 codes[FP8 ? NT * NCODE : 1];
-    float my_scale[NT];
-    // tile t of step u, number `at` in the pool -> its place in slot u & 1: the loads (fp8: into registers)
+    // tile t of step u, number `at` in the pool -> its place in slot u % RING
     auto request = [&](int at, int u, auto tile_tag) {
         constexpr int t = decltype(tile_tag)::value;
         if (at < 0) return;                             // a page outside the pool is never dereferenced
         const int l = lane_again();
-        if constexpr (FP8) {
-            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * (MK_TILE * ROW) + wave * (8 * ROW);
+        const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * TILE_B + wave * (8 * ROWB);
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)((u & 1) * (NT * TILE_B) + t * TILE_B + wave * (8 * ROWB)));
 #pragma unroll
-            for (int k = 0; k < NCODE; ++k) codes[t * NCODE + k] = *reinterpret_cast<const u32x4*>(src + min(k * 64 + l, 8 * CPC - 1) * 16);
-            my_scale[t] = p.kv_scale[(size_t)at * MK_TILE + (l & (MK_TILE - 1))];
-        } else {
-            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * TILE_B + wave * (8 * ROWB);
-            const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)((u & 1) * (NT * TILE_B) + t * TILE_B + wave * (8 * ROWB)));
-#pragma unroll
-            for (int k = 0; k < NLOAD; ++k) {
-                const uint32_t off = ((uint32_t)l * 16) ^ piece_key<CPR>(k, l);
-                asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                             :: "s"(dst), "v"(off), "s"(src + k * 1024), "i"(k * 1024) : "memory", "scc");
-            }
+        for (int k = 0; k < NLOAD; ++k) {
+            const uint32_t off = ((uint32_t)l * 16) ^ piece_key<CPR>(k, l);
+            asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                         :: "s"(dst), "v"(off), "s"(src + k * 1024), "i"(k * 1024) : "memory", "scc");
         }
     };
-    // (fp8) the requested codes, widened, into the slot of step u
-    auto put = [&](int u) {
-        if constexpr (FP8) {
-            const int l = lane_again();
-#pragma unroll
-            for (int tk = 0; tk < NT * NCODE; ++tk) {
-                const int t = tk / NCODE, k = tk % NCODE;
-                LDS_AS unsigned char* rows = lds + (u & 1) * (NT * TILE_B) + t * TILE_B + wave * (8 * ROWB);
-                const int q = k * 64 + l;
-                if (8 * CPC % 64 && k == NCODE - 1 && q >= 8 * CPC) continue;
-                uint32_t w[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[tk][i], 1.f, false));
-                    w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[tk][i], 1.f, true));
-                }
-                // (the key is even: the second half's place is beside the first's)
-                const uint32_t to = (uint32_t)(q * 32) ^ piece_key<CPC>(k, l);
-                *(LDS_AS u32x4*)(rows + to) = (u32x4){w[0], w[1], w[2], w[3]};
-                *(LDS_AS u32x4*)(rows + (to ^ 16)) = (u32x4){w[4], w[5], w[6], w[7]};
-            }
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (wave == t && l < MK_TILE) ks_lds[(u & 1) * (NT * MK_TILE) + t * MK_TILE + l] = my_scale[t];
-        }
-    };
-
-    // the first step's tiles, and (fp8) the second one's codes.  Tiles of a step: their numbers in the pool
+    // Tiles of a step: their numbers in the pool
     struct Places { int at[NT]; };
     auto places = [&](int u, auto at) {
         Places s;
@@ -167,29 +134,65 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         for (int t = 0; t < NT; ++t) s.at[t] = v0 + NT * u + t < v1 ? at(v0 + NT * u + t) : -1;
         return s;
     };
+    // (fp8) Codes as they are, chunk c of row r at position c ^ (r >> 2 & 2), which is one key for a wavefront's rows.  Every wavefront makes the same number of
+    // loads on every step, so that they can be waited for by count: tiles that are not there are some tile, which nobody sees.
+    constexpr int PER_STEP = NT * (FLOAD + 1) + 1;
+    auto request_codes = [&](const Places& s, int u) {
+        const int l = lane_again();
+        const uint32_t slot = (uint32_t)u % RING, off = (uint32_t)(l * 16) ^ (uint32_t)((wave & 1) << 5);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)max(s.at[t], 0) * TILE_B + wave * (8 * ROWB);
+            const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + slot * (NT * TILE_B) + (uint32_t)(t * TILE_B + wave * (8 * ROWB)));
+#pragma unroll
+            for (int k = 0; k < FLOAD; ++k)
+                asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                             :: "s"(dst), "v"(off), "s"(src + k * 1024), "i"(k * 1024) : "memory", "scc");
+            if (l < 32)
+                asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                             :: "s"(dst), "v"(off), "s"(src + FLOAD * 1024), "i"(FLOAD * 1024) : "memory", "scc");
+        }
+        // scales: 64 of them, two tiles' or one's twice, by everybody to the same place
+        const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ks_lds + slot * 256);
+        const float* mine = p.kv_scale + (size_t)max(l < MK_TILE ? s.at[0] : s.at[NT - 1], 0) * MK_TILE + (l & (MK_TILE - 1));
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(dst), "v"(mine) : "memory");
+    };
     auto request_all = [&](const Places& s, int u) {
-        request(s.at[0], u, std::integral_constant<int, 0>{});
-        if constexpr (NT > 1) request(s.at[1], u, std::integral_constant<int, NT - 1>{});
+        if constexpr (FP8) {
+            request_codes(s, u);
+        } else {
+            request(s.at[0], u, std::integral_constant<int, 0>{});
+            if constexpr (NT > 1) request(s.at[1], u, std::integral_constant<int, NT - 1>{});
+        }
+    };
+    // the tiles of the step after this one are there, (fp8) those of the one after that may be on their way
+    auto wait_for_step = [&]() {
+        if constexpr (FP8) {
+            wait_vmcnt<PER_STEP>();
+        } else {
+            wait_vmcnt<0>();
+        }
     };
     const int steps = (v1 - v0 + NT - 1) / NT;
-    Places here, next, after;
+    Places here, next, after, later;                 // of this step and those after it
     auto start = [&]() {
         here = places(0, tile_now);
         next = places(1, tile_now);
         request_all(here, 0);
+        if constexpr (FP8) {
+            request_all(next, 1);
+            after = places(2, tile_now);
+            request_all(after, 2);
+        }
         ids = ids_from(v0);
         if (v0 + 64 < v1) ids_after = ids_from(v0 + 64);
-        if constexpr (FP8) {
-            put(0);
-            request_all(next, 1);
-        }
     };
     start();
 
     // ---- this wavefront's query rows -> registers (B operands of the scores).  A negative scale changes their sign: the largest score is
     // then the largest scaled one
     bf16x8 qreg[2][NQ];
-    LDS_AS unsigned char* const q_lds = lds + 2 * NT * (TILE_B + VT_B) + wave * ((NKS - NQ) * 2 * 1024) + lane * 16;      // this lane's, written and read by it alone
+    LDS_AS unsigned char* const q_lds = lds + VT_AT + 2 * NT * VT_B + wave * ((NKS - NQ) * 2 * 1024) + lane * 16;      // this lane's, written and read by it alone
     {
         const uint16_t* qa = static_cast<const uint16_t*>(p.q_abs) + (size_t)b * p.H * D_C;
         const uint16_t* qr = static_cast<const uint16_t*>(p.q_rope) + (size_t)b * p.H * 64;
@@ -198,8 +201,9 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             const size_t row = hb + min(wave * 32 + hi * 16 + n, HL - 1);
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks) {
-                const u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + ks * 32 + g * 8)
-                                        : *reinterpret_cast<const u32x4*>(qr + row * 64 + (ks - D_C / 32) * 32 + g * 8);
+                // (fp8: a lane reads 16 codes at a time, eight for each of two k-steps)
+                const int kl = ks < D_C / 32 ? ks : ks - D_C / 32, col = FP8 ? (kl >> 1) * 64 + g * 16 + (kl & 1) * 8 : kl * 32 + g * 8;
+                const u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + col) : *reinterpret_cast<const u32x4*>(qr + row * 64 + col);
                 if (ks < NQ) qreg[hi][ks] = __builtin_bit_cast(bf16x8, v);
                 else         *(LDS_AS u32x4*)(q_lds + ((ks - NQ) * 2 + hi) * 1024) = v;
             }
@@ -228,21 +232,30 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     // (never zero: a masked score is -inf and has to stay it)
     const float sc = fmaxf(fabsf(p.scale) * LOG2E, 1.17549435e-38f);
 
-    // score A operand: key row 16 rb + n, chunk 4 ks + g
-    uint32_t a_base[2];
+    // Keys: in bf16 tiles row i of a block rb of 16 scores is key 16 rb + i, so that a lane ends with keys 4g .. 4g + 3 and 16 on, as two
+    // transposing reads of 16-bit values give them; in fp8 tiles key 8 (i / 4) + 4 rb + i % 4, keys 8g .. 8g + 7, as one of 8-bit values does.
+    constexpr int LANE_KEYS = FP8 ? 8 : 4, BLOCK_KEYS = FP8 ? 4 : 16;         // key LANE_KEYS g + BLOCK_KEYS rb + i
+    // score A operand: chunk 4 ks + g (fp8: 4 (ks / 2) + g)
+    uint32_t a_base[2], t_base[4];
+    if constexpr (FP8) {
+        const int row = 8 * (n >> 2) + (n & 3);
+        a_base[0] = a_base[1] = (uint32_t)(row * ROWB) + (((uint32_t)g ^ (uint32_t)(row >> 2 & 2)) << 4);
+        // transposing reads: the lane supplies row 8g + n / 2, 8 bytes at column 16 ct + 8 (n % 2)
+        const int from = 8 * g + (n >> 1);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) a_base[e] = (uint32_t)(n * ROWB) + ((((uint32_t)(4 * e + g)) ^ (uint32_t)swz_key(n)) << 4);
-    // transposing reads: the lane supplies tile row 4g + (n >> 2) (and 16 more), 8 bytes at column 16 ct + 4 (n & 3)
-    uint32_t t_base[4];
-    {
-        const int r = g * 4 + (n >> 2);
+        for (int e = 0; e < 4; ++e) t_base[e] = (uint32_t)(from * ROWB) + (((uint32_t)e ^ (uint32_t)(from >> 2 & 2)) << 4) + (uint32_t)((n & 1) * 8);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) a_base[e] = (uint32_t)(n * ROWB) + ((((uint32_t)(4 * e + g)) ^ (uint32_t)swz_key(n)) << 4);
+        // transposing reads: the lane supplies tile row 4g + (n >> 2) (and 16 more), 8 bytes at column 16 ct + 4 (n & 3)
+        const int from = g * 4 + (n >> 2);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            t_base[e] = (uint32_t)(r * ROWB) + ((((uint32_t)(2 * e) + (uint32_t)((n & 3) >> 1)) ^ (uint32_t)swz_key(r)) << 4) + (uint32_t)((n & 1) * 8);
+            t_base[e] = (uint32_t)(from * ROWB) + ((((uint32_t)(2 * e) + (uint32_t)((n & 3) >> 1)) ^ (uint32_t)swz_key(from)) << 4) + (uint32_t)((n & 1) * 8);
     }
-    LDS_AS unsigned char* const vt = lds + 2 * NT * TILE_B;
+    LDS_AS unsigned char* const vt = lds + VT_AT;
 
-    typedef f32x4 Scores[NRB][2];              // [block of 16 keys][query group]: keys 16 rb + 4g + i of query n
+    typedef f32x4 Scores[NRB][2];              // [block of 16 keys][query group]: the lane's keys of query n
     f32x4 ksc[NRB];                            // (fp8) scales of this lane's keys
     bool poisoned[2] = {false, false};         // one of this lane's keys that its query sees was not finite
     bool dirty[NT] = {};                       // one that some query of the wavefront does not see was not, in tile t of the step
@@ -257,13 +270,13 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         bool odd = false;
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
-            const uint32_t sees = visible(v, at, hi) >> (4 * g);
+            const uint32_t sees = visible(v, at, hi) >> (LANE_KEYS * g);
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const bool bad = !(fabsf(x[2 * t + rb][hi][i]) < INFINITY);
-                    if (sees >> (rb * 16 + i) & 1u) {
+                    if (sees >> (rb * BLOCK_KEYS + i) & 1u) {
                         poisoned[hi] |= bad;
                     } else {
                         odd |= bad;
@@ -316,7 +329,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         if constexpr (FP8) {
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) {
-                ksc[rb] = *(LDS_AS f32x4*)(ks_lds + (u & 1) * (NT * MK_TILE) + rb * 16 + g * 4);
+                ksc[rb] = *(LDS_AS f32x4*)(ks_lds + (int)((unsigned)u % RING) * 64 + (rb >> 1) * MK_TILE + g * 8 + (rb & 1) * 4);
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) x[rb][hi] *= ksc[rb];
             }
@@ -336,9 +349,26 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         static constexpr int VAHEAD = 4;                  // column tiles that the value reads do
         static constexpr int SHARE = NT * NCT / 4;        // column tiles that this wavefront transposes (8)
         bf16x8 ka[NRB][NKS], va[NT][NCT];
+        u32x4 raw[NRB][NKS / 2];               // (fp8) the codes of two k-steps
         float m_use[2];
         uint32_t w[2][4 * NT];
+        auto widened = [&](uint32_t lo, uint32_t up) -> bf16x8 {
+            auto two = [&](uint32_t v, auto high) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, decltype(high)::value)); };
+            return __builtin_bit_cast(bf16x8, (u32x4){two(lo, std::false_type{}), two(lo, std::true_type{}), two(up, std::false_type{}), two(up, std::true_type{})});
+        };
+        auto key_of = [&](int rb, int ks) -> bf16x8 {
+            if constexpr (FP8) return widened(raw[rb][ks / 2][ks % 2 * 2], raw[rb][ks / 2][ks % 2 * 2 + 1]);
+            else               return ka[rb][ks];
+        };
         auto rk = [&](int ks) {
+            if constexpr (FP8) {
+                if (ks % 2 == 0) {
+#pragma unroll
+                    for (int rb = 0; rb < NRB; ++rb)
+                        raw[rb][ks / 2] = *(LDS_AS u32x4*)(keys + a_base[0] + ks / 2 * 64 + (rb >> 1) * TILE_B + (rb & 1) * 4 * ROWB);
+                }
+                return;
+            }
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) ka[rb][ks] = *(LDS_AS bf16x8*)(keys + a_base[ks & 1] + (ks >> 1) * 128 + rb * 16 * ROWB);
         };
@@ -359,14 +389,19 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             w[hi][k] = pack_bf16x2(e0, e1);
         };
         s16x4 lo[SHARE], up[SHARE];
+        u32x2 column[SHARE];
         auto rt = [&](int k) {                 // column tile wave * NCT / 4 + k of a tile, the next tile's behind them
-            LDS_AS unsigned char* at = keys + (k / (NCT / 4)) * TILE_B + t_base[k & 3] + ((wave * (NCT / 4) + k % (NCT / 4)) >> 2) * 128;
+            LDS_AS unsigned char* at = keys + (k / (NCT / 4)) * TILE_B + t_base[k & 3] + ((wave * (NCT / 4) + k % (NCT / 4)) >> 2) * (FP8 ? 64 : 128);
+            if constexpr (FP8) {
+                column[k] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_AS i32x2*)at));
+                return;
+            }
             lo[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)at);
             up[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(at + 16 * ROWB));
         };
         auto wt = [&](int k) {
-            *(LDS_AS bf16x8*)(to + (k / (NCT / 4)) * VT_B + (wave * (NCT / 4) + k % (NCT / 4)) * 1024 + lane * 16) =
-                __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo[k], up[k], 0, 1, 2, 3, 4, 5, 6, 7));
+            const bf16x8 v = FP8 ? widened(column[k][0], column[k][1]) : __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo[k], up[k], 0, 1, 2, 3, 4, 5, 6, 7));
+            *(LDS_AS bf16x8*)(to + (k / (NCT / 4)) * VT_B + (wave * (NCT / 4) + k % (NCT / 4)) * 1024 + lane * 16) = v;
         };
         if constexpr (PV) {
 #pragma unroll
@@ -384,11 +419,14 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
                 for (int i = 0; i < 2; ++i)
                     if (2 * (ks + AHEAD - NKS) + i < VAHEAD) rv(2 * (ks + AHEAD - NKS) + i);
             }
+            bf16x8 kk[NRB];
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) kk[rb] = key_of(rb, ks);
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi)
-                    y[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[rb][ks], ks < NQ ? qreg[hi][ks < NQ ? ks : 0] : qa[ks < NQ ? 0 : ks - NQ][hi],
+                    y[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[rb], ks < NQ ? qreg[hi][ks < NQ ? ks : 0] : qa[ks < NQ ? 0 : ks - NQ][hi],
                                                                         ks == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : y[rb][hi], 0, 0, 0);
             if constexpr (PV) {
                 if (ks < 8) {
@@ -434,7 +472,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     // reference by more than FAST_GAP (rare), a sweep for the exact maxima (it accumulates too, which is not used) and the
     // accumulation again against them.
     enum { ACCUMULATE, MAXIMA, ACCUMULATE_AGAIN };
-    auto slot = [&](int u) { return lds + (u & 1) * (NT * TILE_B); };
+    auto slot = [&](int u) { return lds + (int)((unsigned)u % RING) * (NT * TILE_B); };
     auto turned = [&](int u) { return vt + (u & 1) * (NT * VT_B); };
     for (int pass = ACCUMULATE;;) {
         Scores x, y;
@@ -446,20 +484,24 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 #pragma unroll
             for (int ct = 0; ct < NCT; ++ct) oacc[hi][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
-        if constexpr (!FP8) wait_vmcnt<0>();
+        // bf16: step 0 is there, step 1 is asked for; fp8: steps 0 to 2 are
+        wait_vmcnt<0>();
         __syncthreads();
-        if constexpr (!FP8) request_all(next, 1);
+        if constexpr (FP8) later = after;
+        else               request_all(next, 1);
         step(No{}, slot(0), turned(0), turned(0), x, x);
         look_at(x, 0, here);
         for (int u = 0; u < steps; ++u) {
-            after = places(u + 2, tile_at);
+            after = FP8 ? later : places(u + 2, tile_at);
             if constexpr (FP8) {
-                if (u + 1 < steps) put(u + 1);
+                later = places(u + 3, tile_at);
+                if (u) wait_for_step();
             } else {
-                wait_vmcnt<0>();
+                wait_for_step();
             }
             __syncthreads();     // the tiles of step u + 1 and the transposes of those of step u are there; everybody is done with what lay before
-            request_all(after, u + 2);
+            if constexpr (FP8) request_all(later, u + 3);
+            else               request_all(after, u + 2);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
@@ -480,10 +522,12 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         if (pass == ACCUMULATE) {
             // (an infinite score makes a NaN of its row either way, and no other row shall be the worse for it)
             const bool jumped = (top[0] * sc > m_ref[0] + FAST_GAP && top[0] < INFINITY) || (top[1] * sc > m_ref[1] + FAST_GAP && top[1] < INFINITY);
+            wait_vmcnt<0>();     // (fp8: nothing is on its way to the places that are asked for again)
             if (__builtin_expect(!__syncthreads_or(jumped), 1)) break;
             pass = MAXIMA;
             unset = false;
         } else {
+            wait_vmcnt<0>();
             __syncthreads();
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) {
@@ -494,6 +538,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         }
         start();
     }
+    wait_vmcnt<0>();             // (fp8: what was asked for beyond the last step)
     __syncthreads();             // everybody is done with the tiles
 
     // ---- normalise, and transpose through LDS (a lane holds 4 consecutive columns of its query per column tile) for whole rows.
@@ -508,7 +553,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         if ((who | who >> 16 | who >> 32 | who >> 48) >> n & 1u) inv[hi] = __uint_as_float(0x7FC00000u);
     }
     constexpr int RSO = D_C * 2 + 32;           // row stride of the transposed block (padded)
-    static_assert(4 * 32 * RSO <= 2 * NT * (TILE_B + VT_B), "exchange space must fit");
+    static_assert(4 * 32 * RSO <= sizeof(smem), "exchange space must fit");
     LDS_AS unsigned char* mine = lds + wave * (32 * RSO);
     if (p.num_splits == 1) {
 #pragma unroll
