@@ -149,11 +149,31 @@ static int reachable_pages(int q_len, int max_pages, int window, int sinks)
     return (int)std::min<int64_t>(n, max_pages);
 }
 
+// How many chunks the pages that 128 query rows of a prompt see are cut into: the S that ends first if a round of workgroups (two per CU)
+// takes as long as its pages and four more for start and end, and the merge another four.  Not split / split like this (whole call, us; 28 heads,
+// d_c = 256): 2 x 136 tokens on 10539 under 4096 169 / 124 (S = 4; 2 chunks 126, 8 chunks 132), 64 tokens of one prompt 129 / 51 (S = 13),
+// 500 of one at d_c = 512 165 / 119, 2 x 136 under 1024 60 / 52.  8 x 500 under 1024 has 896 groups and stays as it is: 190, in two chunks 251.
+static int prefill_chunks(int64_t pairs, int q_len, int width, int window, int sinks)
+{
+    const int64_t groups = pairs * (((int64_t)q_len + 127) / 128);
+    const int64_t pages = std::min<int64_t>(width, ((int64_t)sinks + 63) / 64 + ((int64_t)window + 127 + 62) / 64 + 1);
+    int best = 1;
+    double least = 1e300;
+    for (int s = 1; s <= 16 && s <= pages && groups * s <= 1024; ++s) {
+        const double cost = (double)((groups * s + 511) / 512) * ((double)((pages + s - 1) / s) + 4.0) + (s > 1 ? 4.0 : 0.0);
+        if (cost < least * 0.999) { least = cost; best = s; }
+    }
+    return best;
+}
+
 size_t mla_prefill_window_workspace_bytes(int B, int q_len, int heads, int d_c, int max_pages_per_seq, int window, int sinks)
 {
     if (B <= 0 || q_len <= 0 || heads <= 0 || d_c <= 0 || max_pages_per_seq <= 0 || window < 1 || sinks < 0) return 0;
     const int width = reachable_pages(q_len, max_pages_per_seq, window, sinks);
-    return prefill_ws(B, heads, d_c, width).total + align_up((size_t)B * (width + 1) * sizeof(int32_t), 256);
+    const int S = prefill_chunks((int64_t)B * heads, q_len, width, window, sinks);
+    const size_t rows = (size_t)B * q_len * heads;
+    return prefill_ws(B, heads, d_c, width).total + align_up((size_t)B * (width + 1) * sizeof(int32_t), 256) +
+           (S > 1 ? align_up(rows * S * 128 * sizeof(float), 256) + align_up(rows * S * sizeof(float), 256) : 0);
 }
 
 int mla_prefill_window(const void* q_nope, const void* q_rope, const void* W_UK, const void* W_UV, const void* kv_cache,
@@ -202,7 +222,18 @@ int mla_prefill_window(const void* q_nope, const void* q_rope, const void* W_UK,
     // (a window or sinks past the table's end are all that there is)
     const int rows = max_pages_per_seq * page_size;
     p.window = std::min(window, rows); p.sinks = std::min(sinks, rows);
+    p.splits = prefill_chunks(pairs, q_len, width, window, sinks);
+    if (p.splits > 1) {
+        const size_t rows = (size_t)pairs * q_len;
+        p.o_part = reinterpret_cast<float*>(ws + wl.total + align_up((size_t)B * (width + 1) * sizeof(int32_t), 256));
+        p.lse_part = reinterpret_cast<float*>(reinterpret_cast<char*>(p.o_part) + align_up(rows * p.splits * 128 * sizeof(float), 256));
+    }
     e = launch_prefill_attention(p, stream);
+    if (e == hipSuccess && p.splits > 1) {
+        MaskedParams m = {};
+        m.B = B; m.H = q_len * heads; m.d_c = d_head; m.num_splits = p.splits; m.o_part = p.o_part; m.lse_part = p.lse_part;
+        e = launch_masked_merge(m, out, lse, io_dtype, stream);
+    }
     return e == hipSuccess ? MLA_OK : MLA_ERR_HIP;
 }
 

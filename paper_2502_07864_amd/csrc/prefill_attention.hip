@@ -74,8 +74,9 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     // 389 us in the order of the batch, 346 longest first.
     const int Z = (p.q_len + PA_ROWS - 1) / PA_ROWS;
     const int id = blockIdx.x, rr = id >> 3;
-    const int zi = Z - 1 - rr % Z;
-    int b = (rr / Z) * 8 + (id & 7);
+    const int S = WINDOW ? p.splits : 1, split = WINDOW ? rr % S : 0;
+    const int zi = Z - 1 - rr / S % Z;
+    int b = (rr / S / Z) * 8 + (id & 7);
     if (b >= p.pairs) return;                       // padding of the last group of 8
     const int nseq = p.pairs / p.heads;
     if (nseq > 1 && nseq <= 64) {
@@ -130,6 +131,10 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     // keys [0, row1): what the last query row of the workgroup sees (the rows are ordered by token)
     const int row1 = min(L, visible(min(hb + PA_ROWS, p.q_len) - 1));
     auto store_nothing = [&]() {                // zeros and -inf for the rows of this workgroup
+        if (S > 1) {                            // (partial rows of weight zero are not read)
+            if (tid < HL) p.lse_part[io_row(hb + tid) * S + split] = -INFINITY;
+            return;
+        }
         for (int i = tid; i < HL * (PA_DV / 4); i += MF_THREADS)
             *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + io_row(hb + i / (PA_DV / 4)) * PA_DV +
                                       (i % (PA_DV / 4)) * 4) = (u32x2){0u, 0u};
@@ -142,14 +147,26 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     // first key that some query row of this workgroup must not see (its first row sees the least)
     const int causal_from = visible(hb);
     // pages [0, head) and, behind the jump, from head + jump on
-    int head = 0, jump = 0;
+    int head = 0, jump = 0, u0 = 0, t1 = (row1 + TILE_ROWS - 1) / TILE_ROWS;        // u0: the chunk's first page
     if constexpr (WINDOW) {
         head = (min(p.sinks, row1) + 63) / 64;
         jump = max(0, max(causal_from - p.window, 0) / 64 - head);          // (from the first key of the first query's window on)
+        t1 -= 2 * jump;                         // tiles [0, t1), without those jumped over
+        if (S > 1) {                            // pages [u0, its end) of them are this workgroup's, [0, t1) from here on
+            const int all = (t1 + 1) / 2;
+            u0 = (int)((unsigned)(all * split) / (unsigned)S);
+            t1 = min(t1, 2 * (int)((unsigned)(all * (split + 1)) / (unsigned)S)) - 2 * u0;
+            if (t1 <= 0) {
+                store_nothing();
+                return;
+            }
+            head -= u0;
+            jump += u0;
+        }
     }
-    auto page_of = [&](int u) { return !WINDOW || u < head ? u : u + jump; };
-    auto row_of = [&](int t) { return !WINDOW || t < 2 * head ? t * TILE_ROWS : t * TILE_ROWS + jump * 64; };
-    const int t1 = (row1 + TILE_ROWS - 1) / TILE_ROWS - 2 * jump; // tiles [0, t1), without those jumped over
+    // (a chunk's page u is page u0 + u, which is among the first ones as long as u < head)
+    auto page_of = [&](int u) { return !WINDOW ? u : u < head ? u + u0 : u + jump; };
+    auto row_of = [&](int t) { return !WINDOW ? t * TILE_ROWS : t * TILE_ROWS + (t < 2 * head ? u0 : jump) * 64; };
 
     // Page ids, 64 at a time, a lane each (asked for beside the queries; a scalar load in every step was a wait in every step), and
     // whether all pages are there.  Of a page the cache does not have the values are zeros, and no query sees its keys.
@@ -257,12 +274,13 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     auto rows_valid = [&](int t) { return all_there || !missing(((const CONST_AS int32_t*)ptab)[page_of(t >> 1)]) ? min(TILE_ROWS, row1 - row_of(t)) : 0; };
     // leading tiles that every query row of this workgroup sees whole
     const int n_full = all_there ? max(0, min(causal_from, row1)) / TILE_ROWS : 0;
-    // (WINDOW) [0, whole) and [whole_from, whole_to): of the sinks, and from the last query's first key to the first query's last
+    // (WINDOW) [0, whole) and [whole_from, whole_to), those that every query row of the wavefront sees whole: of the sinks, and from its last
+    // query's first key to its first query's last
     int whole = 0, whole_from = 0, whole_to = 0;
     if constexpr (WINDOW) {
         if (all_there) {
-            const int end = max(0, min(causal_from, row1)), from = max(0, visible(min(hb + PA_ROWS, p.q_len) - 1) - p.window);
-            whole = min(p.sinks, end) / TILE_ROWS;
+            const int mine = hb + wave * 32, end = max(0, min(visible(mine), row1)), from = max(0, visible(min(mine + 32, p.q_len) - 1) - p.window);
+            whole = min(p.sinks, end) / TILE_ROWS - 2 * u0;
             whole_from = (from + TILE_ROWS - 1) / TILE_ROWS - 2 * jump;
             whole_to = end / TILE_ROWS - 2 * jump;
         }
@@ -335,22 +353,22 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
             first = l >> 4 << 2;
             // keys of the tile that the query sees, a bit each; the lane's from bit 0 on
             auto low = [](int k) -> uint32_t { return k <= 0 ? 0u : k >= 32 ? ~0u : (1u << k) - 1u; };
-            bool odd = false;
+            float odd = 0.f;
             const int row = row_of(t);
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) {
                 const int end = visible(mine + hi * 16) - row;
-                const uint32_t sees = (low(min(end, n_valid)) & (~low(end - p.window) | low(p.sinks - row))) >> first;
+                const uint32_t unseen = ~(low(min(end, n_valid)) & (~low(end - p.window) | low(p.sinks - row))) >> first;
 #pragma unroll
                 for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (sees >> (rb * 16 + i) & 1u) continue;
-                        odd |= !(fabsf(x[rb][hi][i]) < INFINITY);
-                        x[rb][hi][i] = -INFINITY;
+                        odd = fmaf(x[rb][hi][i], 0.f, odd);                  // (not zero any more if it is infinite or NaN)
+                        const uint32_t gone = (uint32_t)__builtin_amdgcn_sbfe((int)unseen, rb * 16 + i, 1), s = __float_as_uint(x[rb][hi][i]);
+                        x[rb][hi][i] = __uint_as_float((s & ~gone) | (0xFF800000u & gone));
                     }
             }
-            dirty = __any(odd);
+            dirty = __any(!(odd == 0.f));
             return;
         }
 #pragma unroll
@@ -551,6 +569,30 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
     static_assert(4 * 32 * RSO <= SLOT_B, "exchange space must fit in a slot");    // (the flags lie in the other one)
     LDS_AS unsigned char* mine = lds + wave * (32 * RSO);
     float lt[2];
+    const int nrow = min(32, HL - wave * 32);
+    if (WINDOW && S > 1) {                      // the chunk's rows stay in fp32 for the merge, half of the columns at a time
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+                const float l = lacc[hi][0], inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+                for (int ct = 0; ct < NCT / 2; ++ct)
+                    *(LDS_AS f32x4*)(mine + (hi * 16 + n) * RSO + (ct * 16 + g * 4) * 4) = oacc[hi][half * (NCT / 2) + ct] * inv;
+            }
+            for (int r = lane >> 4; r < nrow; r += 4)
+                *reinterpret_cast<u32x4*>(p.o_part + (io_row(hb + wave * 32 + r) * S + split) * PA_DV + half * (PA_DV / 2) + (lane & 15) * 4) =
+                    *(LDS_AS u32x4*)(mine + r * RSO + (lane & 15) * 16);
+        }
+        if (g == 0) {
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi)
+                if (hi * 16 + n < nrow)
+                    p.lse_part[io_row(hb + my_row + hi * 16) * S + split] =
+                        lacc[hi][0] != 0.f ? (m_ref[hi] + __builtin_amdgcn_logf(lacc[hi][0])) * LN2 : -INFINITY;
+        }
+        return;
+    }
 #pragma unroll
     for (int hi = 0; hi < 2; ++hi) {
         lt[hi] = lacc[hi][0];
@@ -562,7 +604,6 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
                 (u32x2){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
         }
     }
-    const int nrow = min(32, HL - wave * 32);
 #pragma unroll
     for (int r0 = 0; r0 < 32; r0 += 4) {
         const int r = r0 + (lane >> 4), c = lane & 15;   // 16 lanes x 16 bytes = one row
@@ -587,8 +628,8 @@ hipError_t launch_prefill_attention(const PrefillParams& p, hipStream_t s)
     if (!p.out || p.heads < 1) return hipErrorInvalidValue;
     const long long Z = (p.q_len + PA_ROWS - 1) / PA_ROWS;
     const long long nwg = ((long long)p.pairs + 7) / 8 * 8 * Z;
-    if (nwg > 0x7FFFFFFFLL) return hipErrorInvalidValue;
-    if (p.window > 0) prefill_attention_kernel<true><<<dim3((unsigned)nwg), dim3(MF_THREADS), 0, s>>>(p);
+    if (p.splits < 1 || nwg * p.splits > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    if (p.window > 0) prefill_attention_kernel<true><<<dim3((unsigned)(nwg * p.splits)), dim3(MF_THREADS), 0, s>>>(p);
     else              prefill_attention_kernel<false><<<dim3((unsigned)nwg), dim3(MF_THREADS), 0, s>>>(p);
     return hipGetLastError();
 }

@@ -20,6 +20,9 @@ struct PrefillParams {
     float* lse;                 // [B, q_len, heads], or nullptr
     float scale;
     int window = 0, sinks = 0;  // window > 0: a query at row t sees the rows from t - window + 1 on, and those below sinks
+    int splits = 1;             // (window) chunks that the pages of 128 query rows are cut into; with more than one the rows go to
+    float* o_part = nullptr;    // [B, q_len, heads, splits, 128] and
+    float* lse_part = nullptr;  // [B, q_len, heads, splits]
 };
 
 // The workspace.  (Sized for keys with their rope part and a page table for every pair, as callers have sized it: the keys and values
