@@ -324,26 +324,36 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         }
         unset = __any(left);
     };
-    // scores of step u, just made: scaled (fp8) and masked
+    // scores of step u, just made: masked.  (fp8: scaled, and their maximum taken as if all were seen, beside the products with the values.
+    // 4 sequences of 128k: 1127 us with both here, 1103; in the bf16 forms it costs the registers that keep the queries.)
+    float glanced[2];
     auto look_at = [&](Scores& x, int u, const Places& s) {
-        if constexpr (FP8) {
+        if constexpr (!FP8) {
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) {
-                ksc[rb] = *(LDS_AS f32x4*)(ks_lds + (int)((unsigned)u % RING) * 64 + (rb >> 1) * MK_TILE + g * 8 + (rb & 1) * 4);
-#pragma unroll
-                for (int hi = 0; hi < 2; ++hi) x[rb][hi] *= ksc[rb];
-            }
+            for (int t = 0; t < NT; ++t)
+                if (__builtin_expect(!seen_whole(v0 + NT * u + t, s.at[t]), 0)) mask(x, t, v0 + NT * u + t, s.at[t]);
+            raise_top(x);
+            if (unset) set_reference(x);
+            return;
         }
+        bool whole_step = true;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-            if (__builtin_expect(!seen_whole(v0 + NT * u + t, s.at[t]), 0)) mask(x, t, v0 + NT * u + t, s.at[t]);
-        raise_top(x);
+        for (int t = 0; t < NT; ++t) whole_step &= seen_whole(v0 + NT * u + t, s.at[t]);
+        if (__builtin_expect(whole_step, 1)) {
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) top[hi] = fmaxf(top[hi], glanced[hi]);
+        } else {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                if (!seen_whole(v0 + NT * u + t, s.at[t])) mask(x, t, v0 + NT * u + t, s.at[t]);
+            raise_top(x);
+        }
         if (unset) set_reference(x);
     };
 
     // ---- a step: S^T of the tiles in `keys` and the weights of those before from their scores x (PV); then their values from `values`,
     // and the transposes of the former tiles into `to`
-    auto step = [&](auto pv_tag, LDS_AS unsigned char* keys, LDS_AS unsigned char* values, LDS_AS unsigned char* to, const Scores& x, Scores& y) {
+    auto step = [&](auto pv_tag, LDS_AS unsigned char* keys, LDS_AS float* scales, LDS_AS unsigned char* values, LDS_AS unsigned char* to, const Scores& x, Scores& y) {
         constexpr bool PV = decltype(pv_tag)::value;
         static constexpr int AHEAD = NT == 1 ? 4 : 2;     // k-steps that the key reads run ahead, one wavefront per SIMD with nothing else to hide them
         static constexpr int VAHEAD = 4;                  // column tiles that the value reads do
@@ -403,6 +413,12 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             const bf16x8 v = FP8 ? widened(column[k][0], column[k][1]) : __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo[k], up[k], 0, 1, 2, 3, 4, 5, 6, 7));
             *(LDS_AS bf16x8*)(to + (k / (NCT / 4)) * VT_B + (wave * (NCT / 4) + k % (NCT / 4)) * 1024 + lane * 16) = v;
         };
+        auto glance = [&](int k) {             // block k / 2 of the scores just made, query group k % 2: scaled (fp8), and their maximum
+            const int rb = k >> 1, hi = k & 1;
+            y[rb][hi] *= ksc[rb];
+            if (rb == 0) glanced[hi] = max_of(max_of(y[rb][hi][0], y[rb][hi][0], y[rb][hi][1]), y[rb][hi][2], y[rb][hi][3]);
+            else         glanced[hi] = max_of(max_of(glanced[hi], y[rb][hi][0], y[rb][hi][1]), y[rb][hi][2], y[rb][hi][3]);
+        };
         if constexpr (PV) {
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) m_use[hi] = m_ref[hi] == -INFINITY ? 0.f : m_ref[hi];
@@ -443,6 +459,10 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             __builtin_amdgcn_sched_barrier(0);
         }
         bf16x8 pb[NT][2];
+        if constexpr (FP8) {                   // (the weights have theirs)
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) ksc[rb] = *(LDS_AS f32x4*)(scales + (rb >> 1) * MK_TILE + g * 8 + (rb & 1) * 4);
+        }
         if constexpr (PV) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
@@ -455,6 +475,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             if (PV && ct + VAHEAD < NCT) rv(ct + VAHEAD);
             if (ct % EVERY == 0) rt(ct / EVERY);
             if (ct >= EVERY + EVERY / 2 && (ct - EVERY / 2) % EVERY == 0) wt((ct - EVERY / 2) / EVERY - 1);
+            if (FP8 && ct >= NCT / 2 && ct < NCT / 2 + 2 * NRB) glance(ct - NCT / 2);
             if constexpr (PV) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
@@ -473,6 +494,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     // accumulation again against them.
     enum { ACCUMULATE, MAXIMA, ACCUMULATE_AGAIN };
     auto slot = [&](int u) { return lds + (int)((unsigned)u % RING) * (NT * TILE_B); };
+    auto scales_of = [&](int u) { return ks_lds + (FP8 ? (int)((unsigned)u % RING) * 64 : 0); };
     auto turned = [&](int u) { return vt + (u & 1) * (NT * VT_B); };
     for (int pass = ACCUMULATE;;) {
         Scores x, y;
@@ -489,7 +511,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         __syncthreads();
         if constexpr (FP8) later = after;
         else               request_all(next, 1);
-        step(No{}, slot(0), turned(0), turned(0), x, x);
+        step(No{}, slot(0), scales_of(0), turned(0), turned(0), x, x);
         look_at(x, 0, here);
         for (int u = 0; u < steps; ++u) {
             after = FP8 ? later : places(u + 2, tile_at);
@@ -509,7 +531,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
                     clean(turned(u) + t * VT_B);
                     dirty[t] = false;
                 }
-            step(Yes{}, slot(u + 1), turned(u), turned(u + 1), x, y);
+            step(Yes{}, slot(u + 1), scales_of(u + 1), turned(u), turned(u + 1), x, y);
             if (u + 1 < steps) look_at(y, u + 1, next);
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb)
