@@ -359,12 +359,6 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 
 }  // namespace
 
-bool masked_thin_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache)
-{
-    // Up to 64 rows: each group of 32 reads the tiles again (from L2), where the kernel for many rows is bound by a tile's round trip
-    return masked_tall_supported(p, io, cache) && cache == MLA_BF16 && p.H <= 64;
-}
-
 hipError_t launch_masked_thin(const MaskedParams& p, hipStream_t s)
 {
     const unsigned chunks = ((unsigned)p.B * p.num_splits + 7) / 8 * 8, Z = (unsigned)((p.H + MK_THIN_ROWS - 1) / MK_THIN_ROWS);

@@ -10,32 +10,36 @@ namespace {
 
 constexpr int MAX_QUERY_ROWS = 8192;      // of a sequence
 
-// How many chunks a sequence's tiles are cut into, for a kernel whose workgroups take `rows` query rows: the S that ends first if
-// a round of workgroups (one per CU) takes as long as its tiles and five more for start and end, and the merge three and what its
-// partial rows take to be written and read.  The sequences are taken to be as long as the table allows.
-int chunks(int B, int64_t H, int rows, int64_t tiles)
-{
-    const int64_t groups = B * ((H + rows - 1) / rows);
-    if (groups >= 4096) return 1;       // (rounds enough; and what is left fits the merge's grid)
-    int best = 1;
-    double least = 1e300;
-    for (int s = 1; s <= MK_MAX_CHUNKS && s <= tiles; ++s) {
-        const double rounds = (double)((groups * s + 255) / 256);
-        const double cost = rounds * ((double)((tiles + s - 1) / s) + 5.0) + (s > 1 ? 3.0 + 4e-4 * (double)(B * H) * s : 0.0);
-        if (cost < least * 0.999) { least = cost; best = s; }
-    }
-    return best;
-}
+// Kernels by the query rows that a workgroup takes, and what a call with one of them takes in us, near enough to choose by: a round of
+// workgroups (one per CU; a chunk's groups of rows run on one XCD of 32, so it is the fullest that counts) its tiles and a start and end; the
+// merge, if there are chunks, its launch and what the partial rows take to be written and read.  Measured at d_c = 512; a tile and a
+// partial row grow with the row.  The sequences are taken to be as long as the table allows.
+struct Kernel {
+    int rows;
+    double tile, start;
+};
+constexpr Kernel PORTABLE = {MK_PORTABLE_ROWS, 2.1, 11.0}, THIN = {MK_THIN_ROWS, 0.7, 7.0}, TALL = {MK_TALL_ROWS, 2.1, 11.0};
 
 struct Plan {
-    int S;
+    int S;                      // chunks that a sequence's tiles are cut into: those that end first
+    double cost;
     size_t lse_off, total;      // of the workspace (S > 1)
 };
 
-Plan plan_of(int B, int64_t H, int d_c, int64_t tiles, int rows)
+Plan plan_of(int B, int64_t H, int d_c, int64_t tiles, const Kernel& k)
 {
-    Plan p;
-    p.S = chunks(B, H, rows, tiles);
+    const int64_t Z = (H + k.rows - 1) / k.rows;
+    const double wide = (d_c + 64) / 576.0;
+    auto cost = [&](int s) {
+        const double rounds = (double)((((int64_t)B * s + 7) / 8 * Z + 31) / 32);
+        return rounds * ((double)((tiles + s - 1) / s) * k.tile * wide + k.start) + (s > 1 ? 6.0 + 8e-4 * wide * (double)(B * H) * s : 0.0);
+    };
+    Plan p = {1, cost(1), 0, 0};
+    for (int s = 2; s <= MK_MAX_CHUNKS && s <= tiles && B * Z < 4096; ++s)          // (4096: rounds enough; and what is left fits the merge's grid)
+        if (const double c = cost(s); c < p.cost * 0.999) {
+            p.S = s;
+            p.cost = c;
+        }
     p.lse_off = align_up((size_t)B * H * p.S * d_c * sizeof(float), 256);
     p.total = p.S > 1 ? p.lse_off + align_up((size_t)B * H * p.S * sizeof(float), 256) : 0;
     return p;
@@ -46,7 +50,7 @@ size_t workspace_bytes_for(int B, int q_len, int heads, int d_c, int64_t tiles)
     // (which kernel a call takes hangs on its types, which are not asked for here)
     const int64_t H = (int64_t)q_len * heads;
     size_t most = 0;
-    for (int rows : {MK_PORTABLE_ROWS, MK_THIN_ROWS, MK_TALL_ROWS}) most = std::max(most, plan_of(B, H, d_c, tiles, rows).total);
+    for (const Kernel& k : {PORTABLE, THIN, TALL}) most = std::max(most, plan_of(B, H, d_c, tiles, k).total);
     return most;
 }
 
@@ -79,11 +83,20 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
     const int64_t H = (int64_t)p.q_len * p.heads;
     if (H > MAX_QUERY_ROWS || (tree && p.q_len > 64)) return MLA_ERR_UNSUPPORTED;
     p.H = (int)H;
-    const bool matrix = !(flags & MLA_FLAG_PORTABLE_KERNEL) && masked_tall_supported(p, io, cache), thin = matrix && masked_thin_supported(p, io, cache);
     const int64_t tiles = most_tiles(p.q_len, (int64_t)p.max_pages * p.page_size, tree, p.window, p.sinks);
+    const bool matrix = !(flags & MLA_FLAG_PORTABLE_KERNEL) && masked_tall_supported(p, io, cache);
     const size_t need = workspace_bytes_for(p.B, p.q_len, p.heads, p.d_c, tiles);
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return MLA_ERR_WORKSPACE;
-    const Plan plan = plan_of(p.B, H, p.d_c, tiles, thin ? MK_THIN_ROWS : matrix ? MK_TALL_ROWS : MK_PORTABLE_ROWS);
+    // Groups of 32 rows read the tiles again for each (from L2), 128 rows wait longer for theirs: few rows or short chunks of them are better
+    // off as groups of 32 (one token or tree of 256 rows on 1000 / 16000 / 64000 rows: 24.7, 42, 86 us by 128, 21.9, 34, 66 by 32), many are not
+    // (16 x 560 rows on 4000: 117, 189; 2 x 256 on 64000: 101, 109).
+    Plan plan = plan_of(p.B, H, p.d_c, tiles, matrix ? TALL : PORTABLE);
+    bool thin = false;
+    if (matrix && cache == MLA_BF16) {
+        const Plan few = plan_of(p.B, H, p.d_c, tiles, THIN);
+        thin = few.cost < plan.cost;
+        if (thin) plan = few;
+    }
     p.num_splits = plan.S;
     if (plan.S == 1) {
         p.o_part = o_lat;

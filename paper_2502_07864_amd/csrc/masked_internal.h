@@ -78,7 +78,6 @@ bool       masked_tall_supported(const MaskedParams& p, mla_dtype io, mla_dtype 
 hipError_t launch_masked_tall(const MaskedParams& p, mla_dtype cache, hipStream_t s);
 constexpr int MK_TALL_ROWS = 128;
 // the same with 32 query rows per workgroup, whose wavefronts take the tiles in turn (bf16 caches)
-bool       masked_thin_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache);
 hipError_t launch_masked_thin(const MaskedParams& p, hipStream_t s);
 constexpr int MK_THIN_ROWS = 32;
 // the chunks' results (S > 1) merged
