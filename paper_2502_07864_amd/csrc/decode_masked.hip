@@ -382,6 +382,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb) ka[rb][ks] = *(LDS_AS bf16x8*)(keys + a_base[ks & 1] + (ks >> 1) * 128 + rb * 16 * ROWB);
         };
+        bf16x8 kk[2][NRB];
         bf16x8 qa[NKS - NQ + 1][2];            // (one more: an array may not be empty)
         auto rq = [&](int ks) {
 #pragma unroll
@@ -435,25 +436,28 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
                 for (int i = 0; i < 2; ++i)
                     if (2 * (ks + AHEAD - NKS) + i < VAHEAD) rv(2 * (ks + AHEAD - NKS) + i);
             }
-            bf16x8 kk[NRB];
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) kk[rb] = key_of(rb, ks);
+            for (int rb = 0; rb < NRB; ++rb) {
+                kk[ks & 1][rb] = FP8 && ks ? kk[ks & 1][rb] : key_of(rb, ks);
+                if (FP8 && ks + 1 < NKS) kk[~ks & 1][rb] = key_of(rb, ks + 1);      // (widened beside the matrix instructions before)
+            }
 #pragma unroll
             for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi)
-                    y[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[rb], ks < NQ ? qreg[hi][ks < NQ ? ks : 0] : qa[ks < NQ ? 0 : ks - NQ][hi],
+                    y[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[ks & 1][rb], ks < NQ ? qreg[hi][ks < NQ ? ks : 0] : qa[ks < NQ ? 0 : ks - NQ][hi],
                                                                         ks == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : y[rb][hi], 0, 0, 0);
             if constexpr (PV) {
-                if (ks < 8) {
-#pragma unroll
-                    for (int i = 0; i < NT; ++i) weigh(NT * ks + i);
+                if (NT == 2 && ks < 8) {
+                    weigh(2 * ks);
+                    weigh(2 * ks + 1);
                 }
+                if (NT == 1 && ks < 16 && ks % 2 == 0) weigh(ks / 2);
 #pragma unroll
                 for (int i = 0; i < 2 * NRB; ++i) {
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // an LDS read
                     __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);     // a matrix instruction
-                    __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);     // vector instructions in its shadow
+                    __builtin_amdgcn_sched_group_barrier(0x2, FP8 ? 4 : 3, 0);     // vector instructions in its shadow
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
