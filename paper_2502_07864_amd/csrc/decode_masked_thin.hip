@@ -39,7 +39,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
     // the groups of query rows of one chunk get linear ids 8 apart: same XCD, same time, so all but the first find the rows in its L2
     const int Z = (p.H + MK_THIN_ROWS - 1) / MK_THIN_ROWS;
     const int id = blockIdx.x, rr = id >> 3;
-    const int zi = (int)((unsigned)rr % (unsigned)Z), wg = (rr - zi) / Z * 8 + (id & 7);
+    const int zi = (int)((unsigned)rr % (unsigned)Z), wg = chunk_at((rr - zi) / Z, id & 7);
     if (wg >= p.B * p.num_splits) return;               // padding of the last group of 8
     const int split = (int)((unsigned)wg % (unsigned)p.num_splits), b = sequence_at(p, (int)((unsigned)wg / (unsigned)p.num_splits), lane);
     const int hb = zi * MK_THIN_ROWS, HL = min(MK_THIN_ROWS, p.H - hb);
