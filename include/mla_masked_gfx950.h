@@ -61,7 +61,7 @@ size_t mla_decode_tree_workspace_bytes(int B, int q_len, int heads, int d_c, int
  *
  * q_len <= 64, q_len * heads <= 8192.  io / cache dtype pairs, d_c, d_rope and page_size
  * as for mla_decode_paged.  The matrix-core kernels are used for BF16 io with a BF16 or
- * FP8 cache, page_size a multiple of 32, d_rope 64 and d_c in {256, 512}; everything else
+ * FP8 cache, page_size a multiple of 16, d_rope 64 and d_c in {256, 512}; everything else
  * runs on the portable scalar-FMA kernel.  Sums and softmax statistics are fp32; with BF16
  * io the weights of the value sums and the partial results that are merged are rounded to
  * bf16.

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 
     constexpr int VT_AT = RING * NT * TILE_B;           // the transposes lie behind the tiles, the queries' rope parts behind them
     __shared__ __attribute__((aligned(1024))) unsigned char smem[VT_AT + 2 * NT * VT_B + (NKS - NQ) * 2 * MF_THREADS * 16];
-    __shared__ __attribute__((aligned(16))) float ks_smem[FP8 ? RING : 1][64];     // (fp8) scales of a step's rows
+    __shared__ __attribute__((aligned(16))) float ks_smem[FP8 ? RING : 1][NT * 2][32];     // (fp8) scales of a step's rows, the 16 of a half tile twice
     __shared__ uint64_t tree_smem[64];
     __shared__ int token_smem[MT_ROWS];
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
@@ -85,39 +85,35 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         return;
     }
 
-    // ---- tiles: v is a tile's number without the gap; its rows lie on one page (page sizes are multiples of 32).  Where they lie, 64 tiles at
-    // a time, a lane each (a scalar load on every step, out of order with the LDS reads, would make each of their waits a wait
-    // for everything): the tile's number in the pool, -1 where its page is not there.
+    // ---- tiles: v is a tile's number without the gap.  Where their halves lie, 32 tiles at a time, a lane each (a scalar load on every step,
+    // out of order with the LDS reads, would make each of their waits a wait for everything).
     const int32_t* const ptab = p.page_table + (size_t)b * p.max_pages;
-    const int per_page = p.page_size / MK_TILE;
-    auto ids_from = [&](int v) {
-        const int t = reach.tile(min(v + lane, v1 - 1)), q = t / per_page;
-        const int page = ptab[q];
-        return page >= 0 && page < p.num_pages ? page * per_page + (t - q * per_page) : -1;
-    };
-    int32_t ids = 0, ids_after = 0;                     // of the tiles v0 + 64 k on, and the 64 behind them
-    auto tile_at = [&](int v) -> int {                  // (v: in the order of the sweep)
-        if (((v - v0) & 63) == 0) {
-            ids = ids_after;
-            if (v + 64 < v1) ids_after = ids_from(v + 64);
+    const int per_page = p.page_size / 16;
+    auto half_of = [&](int v) { return 2 * reach.tile(min(v + (lane >> 1), v1 - 1)) + (lane & 1); };
+    auto pages_from = [&](int v) { return half_page(p, ptab, per_page, half_of(v)); };
+    int32_t ids = 0, pages = 0;                         // the places of tiles v0 + 32 k on, and the page ids of the 32 behind them, looked at no
+                                                        // sooner than they are needed (who waits for them waits for tiles)
+    auto tile_at = [&](int v) -> Place {                // (v: in the order of the sweep)
+        const int i = (v - v0) & 31;
+        if (i == 0) {
+            ids = half_at(p, pages, per_page, half_of(v));
+            pages = pages_from(v + 32);
         }
-        return __builtin_amdgcn_readlane(ids, (v - v0) & 63);
+        return Place{(int)__builtin_amdgcn_readlane(ids, 2 * i), (int)__builtin_amdgcn_readlane(ids, 2 * i + 1)};
     };
-    auto tile_now = [&](int v) -> int {                 // (the first ones: a scalar load each, which waits for no vector load)
-        const int t = reach.tile(v), q = t / per_page;
-        const int page = ((const CONST_AS int32_t*)ptab)[q];
-        return page >= 0 && page < p.num_pages ? page * per_page + (t - q * per_page) : -1;
-    };
+    auto tile_now = [&](int v) { return tile_place(p, (const CONST_AS int32_t*)ptab, per_page, reach.tile(v)); };      // (the first ones: scalar loads, which wait for no vector load)
 
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
     // A wavefront loads eight rows of a tile, which lie one behind the other as they do in the pool, 64 pieces at a time; chunk c of row r at
     // position c ^ key(r).
-    // tile t of step u, number `at` in the pool -> its place in slot u % RING
-    auto request = [&](int at, int u, auto tile_tag) {
+    auto mine_of = [&](const Place& s) { return wave < 2 ? s.lo : s.hi; };
+    // tile t of step u -> its place in slot u % RING
+    auto request = [&](const Place& s, int u, auto tile_tag) {
         constexpr int t = decltype(tile_tag)::value;
+        const int at = mine_of(s);
         if (at < 0) return;                             // a page outside the pool is never dereferenced
         const int l = lane_again();
-        const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * TILE_B + wave * (8 * ROWB);
+        const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * (TILE_B / 2) + (wave & 1) * (8 * ROWB);
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)((u & 1) * (NT * TILE_B) + t * TILE_B + wave * (8 * ROWB)));
 #pragma unroll
         for (int k = 0; k < NLOAD; ++k) {
@@ -126,36 +122,42 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
                          :: "s"(dst), "v"(off), "s"(src + k * 1024), "i"(k * 1024) : "memory", "scc");
         }
     };
-    // Tiles of a step: their numbers in the pool
-    struct Places { int at[NT]; };
+    // Tiles of a step
+    struct Places { Place at[NT]; };
+    auto there = [&](const Places& s) {                 // which of their halves are, a bit each
+        uint32_t bits = 0;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) bits |= (uint32_t)(s.at[t].lo >= 0) << 2 * t | (uint32_t)(s.at[t].hi >= 0) << (2 * t + 1);
+        return bits;
+    };
     auto places = [&](int u, auto at) {
         Places s;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) s.at[t] = v0 + NT * u + t < v1 ? at(v0 + NT * u + t) : -1;
+        for (int t = 0; t < NT; ++t) s.at[t] = v0 + NT * u + t < v1 ? at(v0 + NT * u + t) : Place{-1, -1};
         return s;
     };
     // (fp8) Codes as they are, chunk c of row r at position c ^ (r >> 2 & 2), which is one key for a wavefront's rows.  Every wavefront makes the same number of
     // loads on every step, so that they can be waited for by count: tiles that are not there are some tile, which nobody sees.
-    constexpr int PER_STEP = NT * (FLOAD + 1) + 1;
+    constexpr int PER_STEP = NT * (FLOAD + 2);
     auto request_codes = [&](const Places& s, int u) {
         const int l = lane_again();
         const uint32_t slot = (uint32_t)u % RING, off = (uint32_t)(l * 16) ^ (uint32_t)((wave & 1) << 5);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)max(s.at[t], 0) * TILE_B + wave * (8 * ROWB);
+            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)max(mine_of(s.at[t]), 0) * (TILE_B / 2) + (wave & 1) * (8 * ROWB);
             const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + slot * (NT * TILE_B) + (uint32_t)(t * TILE_B + wave * (8 * ROWB)));
 #pragma unroll
             for (int k = 0; k < FLOAD; ++k)
                 asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                              :: "s"(dst), "v"(off), "s"(src + k * 1024), "i"(k * 1024) : "memory", "scc");
+            // the last half of a load's bytes, and the half tile's scales (both its wavefronts bring them)
+            const float* scales = p.kv_scale + (size_t)max(mine_of(s.at[t]), 0) * 16;
+            const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ks_lds + (slot * NT + (uint32_t)t) * 256u + (uint32_t)(wave >> 1) * 128u);
             if (l < 32)
-                asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                             :: "s"(dst), "v"(off), "s"(src + FLOAD * 1024), "i"(FLOAD * 1024) : "memory", "scc");
+                asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+                             "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dword %5, %6"
+                             :: "s"(dst), "v"(off), "s"(src + FLOAD * 1024), "i"(FLOAD * 1024), "s"(to), "v"((uint32_t)((l & 15) * 4)), "s"(scales) : "memory", "scc");
         }
-        // scales: 64 of them, two tiles' or one's twice, by everybody to the same place
-        const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ks_lds + slot * 256);
-        const float* mine = p.kv_scale + (size_t)max(l < MK_TILE ? s.at[0] : s.at[NT - 1], 0) * MK_TILE + (l & (MK_TILE - 1));
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(dst), "v"(mine) : "memory");
     };
     auto request_all = [&](const Places& s, int u) {
         if constexpr (FP8) {
@@ -174,18 +176,22 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         }
     };
     const int steps = (v1 - v0 + NT - 1) / NT;
-    Places here, next, after, later;                 // of this step and those after it
+    uint32_t here, next, after = 0;                     // what is there of this step's tiles, the next one's, the one's after it (fp8)
+    Places second;
     auto start = [&]() {
-        here = places(0, tile_now);
-        next = places(1, tile_now);
-        request_all(here, 0);
+        const Places first = places(0, tile_now);
+        second = places(1, tile_now);
+        here = there(first);
+        next = there(second);
+        request_all(first, 0);
         if constexpr (FP8) {
-            request_all(next, 1);
-            after = places(2, tile_now);
-            request_all(after, 2);
+            request_all(second, 1);
+            const Places third = places(2, tile_now);
+            after = there(third);
+            request_all(third, 2);
         }
-        ids = ids_from(v0);
-        if (v0 + 64 < v1) ids_after = ids_from(v0 + 64);
+        ids = half_at(p, pages_from(v0), per_page, half_of(v0));
+        pages = pages_from(v0 + 32);
     };
     start();
 
@@ -223,7 +229,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     if (tree && tid < p.q_len) tree_smem[tid] = tree_word(p, b, tid);
     if (tid < MT_ROWS) token_smem[tid] = (hb + min(tid, HL - 1)) / p.heads;        // (both are read in few tiles)
     const WholeTiles whole = whole_tiles(p, reach, hb / p.heads, (hb + HL - 1) / p.heads);
-    auto seen_whole = [&](int v, int at) { return at >= 0 && whole.holds(v); };
+    auto seen_whole = [&](int v, uint32_t halves) { return halves == 3 && whole.holds(v); };      // (halves: the tile's bits)
 
     // ---- per-lane state: this lane's queries = column n of the D tiles of the two groups
     float m_ref[2] = {-INFINITY, -INFINITY};   // reference of the exponentials (log2 units)
@@ -261,16 +267,16 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     bool dirty[NT] = {};                       // one that some query of the wavefront does not see was not, in tile t of the step
 
     // rows of tile v (bit: row) that the lane's query of group hi sees
-    auto visible = [&](int v, int at, int hi) -> uint32_t {
+    auto visible = [&](int v, uint32_t halves, int hi) -> uint32_t {
         const int token = token_smem[wave * 32 + hi * 16 + (lane_again() & 15)];
-        return at < 0 ? 0u : visible_rows(p, reach, reach.tile(v) * MK_TILE, token, tree ? tree_smem[token] : 0);
+        return ((halves & 1 ? 0xFFFFu : 0u) | (halves & 2 ? 0xFFFF0000u : 0u)) & visible_rows(p, reach, reach.tile(v) * MK_TILE, token, tree ? tree_smem[token] : 0);
     };
     // tile t of the step (tile v of the sequence)
-    auto mask = [&](Scores& x, int t, int v, int at) {
+    auto mask = [&](Scores& x, int t, int v, uint32_t halves) {
         bool odd = false;
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
-            const uint32_t sees = visible(v, at, hi) >> (LANE_KEYS * g);
+            const uint32_t sees = visible(v, halves, hi) >> (LANE_KEYS * g);
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
@@ -327,25 +333,25 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     // scores of step u, just made: masked.  (fp8: scaled, and their maximum taken as if all were seen, beside the products with the values.
     // 4 sequences of 128k: 1127 us with both here, 1103; in the bf16 forms it costs the registers that keep the queries.)
     float glanced[2];
-    auto look_at = [&](Scores& x, int u, const Places& s) {
+    auto look_at = [&](Scores& x, int u, uint32_t bits) {
         if constexpr (!FP8) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                if (__builtin_expect(!seen_whole(v0 + NT * u + t, s.at[t]), 0)) mask(x, t, v0 + NT * u + t, s.at[t]);
+                if (__builtin_expect(!seen_whole(v0 + NT * u + t, bits >> 2 * t & 3), 0)) mask(x, t, v0 + NT * u + t, bits >> 2 * t & 3);
             raise_top(x);
             if (unset) set_reference(x);
             return;
         }
         bool whole_step = true;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) whole_step &= seen_whole(v0 + NT * u + t, s.at[t]);
+        for (int t = 0; t < NT; ++t) whole_step &= seen_whole(v0 + NT * u + t, bits >> 2 * t & 3);
         if (__builtin_expect(whole_step, 1)) {
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) top[hi] = fmaxf(top[hi], glanced[hi]);
         } else {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                if (!seen_whole(v0 + NT * u + t, s.at[t])) mask(x, t, v0 + NT * u + t, s.at[t]);
+                if (!seen_whole(v0 + NT * u + t, bits >> 2 * t & 3)) mask(x, t, v0 + NT * u + t, bits >> 2 * t & 3);
             raise_top(x);
         }
         if (unset) set_reference(x);
@@ -465,7 +471,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         bf16x8 pb[NT][2];
         if constexpr (FP8) {                   // (the weights have theirs)
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) ksc[rb] = *(LDS_AS f32x4*)(scales + (rb >> 1) * MK_TILE + g * 8 + (rb & 1) * 4);
+            for (int rb = 0; rb < NRB; ++rb) ksc[rb] = *(LDS_AS f32x4*)(scales + (rb >> 1) * 64 + (g >> 1) * 32 + (g & 1) * 8 + (rb & 1) * 4);
         }
         if constexpr (PV) {
 #pragma unroll
@@ -498,7 +504,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     // accumulation again against them.
     enum { ACCUMULATE, MAXIMA, ACCUMULATE_AGAIN };
     auto slot = [&](int u) { return lds + (int)((unsigned)u % RING) * (NT * TILE_B); };
-    auto scales_of = [&](int u) { return ks_lds + (FP8 ? (int)((unsigned)u % RING) * 64 : 0); };
+    auto scales_of = [&](int u) { return ks_lds + (FP8 ? (int)((unsigned)u % RING) * (NT * 64) : 0); };
     auto turned = [&](int u) { return vt + (u & 1) * (NT * VT_B); };
     for (int pass = ACCUMULATE;;) {
         Scores x, y;
@@ -513,21 +519,19 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         // bf16: step 0 is there, step 1 is asked for; fp8: steps 0 to 2 are
         wait_vmcnt<0>();
         __syncthreads();
-        if constexpr (FP8) later = after;
-        else               request_all(next, 1);
+        if constexpr (!FP8) request_all(second, 1);
         step(No{}, slot(0), scales_of(0), turned(0), turned(0), x, x);
         look_at(x, 0, here);
         for (int u = 0; u < steps; ++u) {
-            after = FP8 ? later : places(u + 2, tile_at);
+            const Places wanted = places(u + (FP8 ? 3 : 2), tile_at);
             if constexpr (FP8) {
-                later = places(u + 3, tile_at);
                 if (u) wait_for_step();
             } else {
                 wait_for_step();
             }
             __syncthreads();     // the tiles of step u + 1 and the transposes of those of step u are there; everybody is done with what lay before
-            if constexpr (FP8) request_all(later, u + 3);
-            else               request_all(after, u + 2);
+            request_all(wanted, u + (FP8 ? 3 : 2));
+            const uint32_t last = there(wanted);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
@@ -541,8 +545,8 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) x[rb][hi] = y[rb][hi];
-            here = next;
-            next = after;
+            next = FP8 ? after : last;
+            after = last;
         }
         if (pass == ACCUMULATE_AGAIN) break;
         if (pass == ACCUMULATE) {
@@ -667,7 +671,7 @@ bool masked_tall_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache)
 {
     auto on16 = [](const void* q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
     return io == MLA_BF16 && (cache == MLA_BF16 || cache == MLA_FP8_E4M3) && p.d_rope == 64 && (p.d_c == 256 || p.d_c == 512) &&
-           p.page_size % MK_TILE == 0 && (int64_t)p.num_pages * (p.page_size / MK_TILE) <= 0x7FFFFFFF && on16(p.q_abs) && on16(p.q_rope) && on16(p.kv);
+           p.page_size % 16 == 0 && (int64_t)p.num_pages * (p.page_size / 16) <= 0x7FFFFFFF && on16(p.q_abs) && on16(p.q_rope) && on16(p.kv);
 }
 
 hipError_t launch_masked_tall(const MaskedParams& p, mla_dtype cache, hipStream_t s)

@@ -58,38 +58,38 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
         return;
     }
 
-    // ---- this wavefront's tiles: v0 + wave, + 4, ...; where they lie in the pool (-1: not there), 64 of them at a time, a lane each
+    // ---- this wavefront's tiles: v0 + wave, + 4, ...; where their halves lie, 32 tiles at a time, a lane each
     const int32_t* const ptab = p.page_table + (size_t)b * p.max_pages;
-    const int per_page = p.page_size / MK_TILE;
-    auto place = [&](int v, auto table) {
-        const int t = reach.tile(min(v, v1 - 1)), q = t / per_page;
-        const int page = table[q];
-        return page >= 0 && page < p.num_pages ? page * per_page + (t - q * per_page) : -1;
+    const int per_page = p.page_size / 16;
+    auto ids_from = [&](int v) {
+        const int k = 2 * reach.tile(min(v + 4 * (lane >> 1), v1 - 1)) + (lane & 1);
+        return half_at(p, half_page(p, ptab, per_page, k), per_page, k);
     };
     LDS_AS unsigned char* const tile = lds + wave * TILE_B;
     const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tile);
-    auto request = [&](int at) {
-        if (at < 0) return;                             // a page outside the pool is never dereferenced
-        const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)at * TILE_B;
+    auto request = [&](const Place& s) {
         const int l = lane_again();
         constexpr int EIGHT = CPR / 8;                  // loads of eight rows, after which the swizzle repeats
 #pragma unroll 1
         for (int i = 0; i < 4; ++i) {
+            const int half = i < 2 ? s.lo : s.hi;
+            if (half < 0) continue;                     // a page outside the pool is never dereferenced
+            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)half * (TILE_B / 2) + (i & 1) * (EIGHT * 1024);
 #pragma unroll
             for (int k = 0; k < EIGHT; ++k) {
                 const uint32_t off = ((uint32_t)l * 16) ^ piece_key<CPR>(k, l);
                 const uint32_t to = dst + (uint32_t)(i * EIGHT + k) * 1024u;
                 asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(to), "v"(off), "s"(src + k * 1024) : "memory");
             }
-            src += EIGHT * 1024;
         }
     };
-    int at;
+    Place at;
     int32_t ids;
     auto start = [&]() {
-        at = v0 + wave < v1 ? place(v0 + wave, (const CONST_AS int32_t*)ptab) : -1;
+        at = Place{-1, -1};
+        if (v0 + wave < v1) at = tile_place(p, (const CONST_AS int32_t*)ptab, per_page, reach.tile(v0 + wave));
         request(at);
-        ids = place(v0 + wave + 4 * lane, ptab);
+        ids = ids_from(v0 + wave);
     };
     start();
 
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
         }
         int turn = 0;
         for (int v = v0 + wave; v < v1; v += 4, ++turn) {
-            if (turn && (turn & 63) == 0) ids = place(v + 4 * lane, ptab);
+            if (turn && (turn & 31) == 0) ids = ids_from(v);
             wait_vmcnt<0>();
             __builtin_amdgcn_sched_barrier(0);
 
@@ -185,11 +185,11 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            if (__builtin_expect(at < 0 || !whole.holds(v), 0)) {
+            if (__builtin_expect(!at.whole() || !whole.holds(v), 0)) {
                 bool odd = false;
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) {
-                    const uint32_t sees = (at < 0 ? 0u : visible_rows(p, reach, reach.tile(v) * MK_TILE, token[hi], tree ? tree_smem[token[hi]] : 0)) >> (4 * g);
+                    const uint32_t sees = (at.rows() & visible_rows(p, reach, reach.tile(v) * MK_TILE, token[hi], tree ? tree_smem[token[hi]] : 0)) >> (4 * g);
 #pragma unroll
                     for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
@@ -263,8 +263,9 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
             }
             // (every read of the tile has been waited for: its place is free)
             if (v + 4 < v1) {
-                at = __builtin_amdgcn_readlane(ids, (turn + 1) & 63);
-                if (((turn + 1) & 63) == 0) at = place(v + 4, (const CONST_AS int32_t*)ptab);
+                const int i = 2 * ((turn + 1) & 31);
+                at = Place{(int)__builtin_amdgcn_readlane(ids, i), (int)__builtin_amdgcn_readlane(ids, i + 1)};
+                if (i == 0) at = tile_place(p, (const CONST_AS int32_t*)ptab, per_page, reach.tile(v + 4));
                 request(at);
             }
         }

@@ -45,6 +45,29 @@ __device__ __forceinline__ int sequence_at(const MaskedParams& p, int i, int lan
     return __builtin_amdgcn_readfirstlane(__builtin_ffsll((long long)__ballot(lane < p.B && rank == i)) - 1);
 }
 
+// Where the two halves of a tile, 16 rows each, lie in the pool, as numbers of 16 rows (page sizes are multiples of 16); -1: not there
+struct Place {
+    int lo, hi;
+    __device__ __forceinline__ bool whole() const { return lo >= 0 && hi >= 0; }
+    __device__ __forceinline__ uint32_t rows() const { return (lo >= 0 ? 0xFFFFu : 0u) | (hi >= 0 ? 0xFFFF0000u : 0u); }
+};
+// rows 16 k .. 16 k + 15 of the sequence, in two parts: the page's id, and what follows from it
+__device__ __forceinline__ int half_page(const MaskedParams& p, const int32_t* table, int per_page, int k) { return table[min(k / per_page, p.max_pages - 1)]; }
+__device__ __forceinline__ int half_at(const MaskedParams& p, int page, int per_page, int k)
+{
+    const int q = k / per_page;
+    return q < p.max_pages && page >= 0 && page < p.num_pages ? page * per_page + (k - q * per_page) : -1;
+}
+template <typename Table>
+__device__ __forceinline__ Place tile_place(const MaskedParams& p, Table table, int per_page, int tile)
+{
+    const int q = 2 * tile / per_page, r = 2 * tile - q * per_page;
+    const bool on = r + 1 < per_page;                   // the second half lies on the same page
+    const int q2 = on ? q : q + 1, first = table[q], second = table[min(q2, p.max_pages - 1)];
+    auto at = [&](int page, int r) { return page >= 0 && page < p.num_pages ? page * per_page + r : -1; };
+    return Place{at(first, r), q2 < p.max_pages ? at(second, on ? r + 1 : 0) : -1};
+}
+
 // Tiles that all of the tokens [first, last] see whole, where their pages are there: [0, whole) and [from, to)
 struct WholeTiles {
     int whole, from, to;

@@ -45,6 +45,34 @@ def test_many_rows_pages(page):
     run_tree("bf16", crowd([95, 96, 97, 300]), 20, 28, page=page)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("d_c", [256, 512])
+@pytest.mark.parametrize("page", [16, 48, 80])
+def test_pages_that_end_inside_a_tile(kind, d_c, page):
+    run_tree(kind, [0, 15, 16, 17, 47, 48, 49, 500], 5, 28, d_c, page=page)
+    run_tree(kind, crowd([47, 95, 96, 97, 300]), 20, 28, d_c, page=page)
+    run_window(kind, [15, 16, 17, 700, 1111], 3, 20, 100, 20, d_c, page=page)
+    run_window(kind, [3000], 1, 32, 2500, 4, d_c, page=page)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("H, T", [(28, 20), (8, 4)])
+def test_half_tiles_that_are_not_there(kind, H, T):
+    """Pages of 16 rows: either half of a tile may be missing, and the table may end inside one."""
+    prefix, cache = crowd([200, 90, 23]), FP8 if kind == "fp8" else BF
+    c = Cache([p + T for p in prefix], 512, 64, 16, cache, 3)
+    a, b, e = prefix.index(200), prefix.index(90), prefix.index(23)
+    c.table[a, 0], c.table[a, 3], c.table[a, 10], c.table[b, 1], c.table[e, 0] = -1, c.kv.shape[0], 1 << 30, -5, -1
+    masks = [tree_of(T, 5 + k) for k in range(64)]
+    q, qr = queries(64, T, H, 512, 64, BF)
+    mask = torch.tensor(masks, dtype=torch.int64, device=DEV)
+    lens = torch.tensor(prefix, dtype=torch.int32, device=DEV)
+    for width in (c.table.shape[1], 3):
+        c.table = c.table[:, :width].contiguous()
+        check(c, q, qr, tree_sees([min(p, 16 * width) for p in prefix], masks, T, min(200 + T, 16 * width)),
+              lambda: mla.decode_paged_tree(q, qr, c.kv, c.table, lens, mask, SCALE, kv_scale=c.scale, return_lse=True), BF)
+
+
 @pytest.mark.parametrize("scale", [-SCALE, 0.0, 3.0])
 def test_many_rows_scales(scale):
     run_tree("bf16", crowd([40, 300]), 20, 28, scale=scale)
