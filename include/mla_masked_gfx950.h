@@ -59,12 +59,13 @@ size_t mla_decode_tree_workspace_bytes(int B, int q_len, int heads, int d_c, int
  *              that is 0); scratch
  *   flags  MLA_FLAG_DEFAULT or MLA_FLAG_PORTABLE_KERNEL
  *
- * q_len <= 64, q_len * heads <= 8192.  io / cache dtype pairs, d_c, d_rope and page_size
- * as for mla_decode_paged.  The matrix-core kernels are used for BF16 io with a BF16 or
+ * q_len <= 64, q_len * heads <= 8192, max_pages_per_seq * page_size <= 2^30 (else
+ * MLA_ERR_UNSUPPORTED).  io / cache dtype pairs, d_c, d_rope and page_size as for
+ * mla_decode_paged.  The matrix-core kernels are used for BF16 io with a BF16 or
  * FP8 cache, page_size a multiple of 16, d_rope 64 and d_c in {256, 512}; everything else
- * runs on the portable scalar-FMA kernel.  Sums and softmax statistics are fp32; with BF16
- * io the weights of the value sums and the partial results that are merged are rounded to
- * bf16.
+ * runs on the portable scalar-FMA kernel.  Sums, softmax statistics and the partial results
+ * that are merged are fp32; on the matrix cores the weights of the value sums are rounded to
+ * bf16 (the normaliser sums them before).  One call gives the same bits every time.
  */
 int mla_decode_paged_tree(const void* q_abs, const void* q_rope, const void* kv_cache, const float* kv_scale,
                           const int32_t* page_table, const int32_t* prefix_lens, const uint64_t* tree_mask,
@@ -99,7 +100,8 @@ int mla_decode_paged_window(const void* q_abs, const void* q_rope, const void* k
 
 /*
  * Bytes of device workspace mla_prefill_window needs (mla_prefill_mha's for the pages
- * that a call can reach, and a table of them).  Pure host function; 0 if an argument is
+ * that a call can reach, a table of them, and partial results where few query rows have
+ * their keys cut into chunks).  Pure host function; 0 if an argument is
  * invalid.
  */
 size_t mla_prefill_window_workspace_bytes(int B, int q_len, int heads, int d_c, int max_pages_per_seq, int window,
@@ -111,7 +113,8 @@ size_t mla_prefill_window_workspace_bytes(int B, int q_len, int heads, int d_c, 
  * of the call sees and no others).
  *   lse [B, q_len, heads] fp32 (output, may be NULL)
  *   workspace  mla_prefill_window_workspace_bytes bytes, 256-byte aligned; scratch
- * Everything else, the sizes supported included, as for mla_prefill_mha.
+ * Everything else, the sizes supported included, as for mla_prefill_mha; q_len <= 2^29 and
+ * max_pages_per_seq * page_size <= 2^30.
  */
 int mla_prefill_window(const void* q_nope, const void* q_rope, const void* W_UK, const void* W_UV,
                        const void* kv_cache, const int32_t* page_table, const int32_t* seq_lens, void* out, float* lse,

@@ -12,12 +12,23 @@
 // instructions; so it is 68 x 17 + 16 x 26 + 8 x 17 = 1708.
 //
 // A step scores tile i + 1 (and weighs tile i between its matrix instructions), then accumulates tile i (and transposes tile
-// i + 1), while tile i + 2 is on its way (direct-to-LDS loads; fp8 codes through registers, widened to bf16, which is exact).
-// Two slots for tiles and two for their transposes: 136 KB of LDS at d_c = 512, one workgroup per CU.
+// i + 1), while tile i + 2 is on its way (direct-to-LDS loads).  Two slots for tiles and two for their transposes: 136 KB of LDS at
+// d_c = 512, one workgroup per CU; at d_c = 256 a step is two tiles.  A bf16 tile waits for all loads at once; an fp8 one is half as
+// wide, so that three slots fit and two are on their way, waited for by count.
+//
+// fp8 codes stay in LDS as they are and are widened to bf16, which is exact, where they are read: the keys beside the matrix instructions of the
+// 32 dimensions before, the values once, when their tile is transposed.  The row's scale goes to the scores and the weights.  (Widened on the way into LDS, through
+// registers, 31 tokens x 32 heads on 4 x 131072 rows took 1678 us.)
+//
+// Measured (whole calls): that case 1074 us, 1.05 PFLOP/s; 16 x 32 on 16 x 8192 bf16 rows 162 us, 0.90; 63 x 28 on 64 sequences of 512 .. 4096 rows at
+// d_c = 256 352 us, 0.74; a large library product reaches 1.35.  Bound by the one wavefront per SIMD that the registers leave: matrix pipes busy 31 to
+// 44 % of the cycles, the wavefronts issue 50 to 61 % of theirs, and wait for tiles, LDS and barriers 20 to 25 %.  What had most weight on the way: no
+// spilled register may be read back in the loop, since the wait for it is a wait for the tiles requested before it.  Not taken, for they were slower: two steps
+// unrolled (the sums move between register files), more keys read ahead, the scores' maximum beside the value products in the bf16 forms.
 //
 // The reference of a query row's exponentials is the maximum of the first tile with a row it sees, and nothing is rescaled; where a
 // score exceeds it by more than 2^64 the chunk is done again against the exact maxima.  The normaliser sums the weights before
-// their rounding to bf16 in fp32; the weights' rounding (2^-8 of each) is the price of the bf16 instructions.
+// their rounding to bf16 in fp32; the weights' rounding (2^-8 of each) is the price of the bf16 instructions.  Chunks' results stay in fp32.
 //
 // Keys that a row does not see get the score -inf, in the tiles that need it.  A key that is not finite has scores that are not: where
 // a wavefront meets one that some row of its own does not see, it clears what is not finite from the transposed tile before
@@ -622,7 +633,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 }
 
 // ---- chunks merged: lse = log sum_s e^{lse_s}, o = sum_s e^{lse_s - lse} o_s.  A wavefront per query row and 256 columns; lane s
-// holds the log-sum-exp of chunk s (at most 64).  The partials are fp32: rounded to bf16 they would be off by as much again as the
+// holds the log-sum-exp of chunk s (at most 64).  8192 rows in 4 chunks, 67 MB: 13 us, 5.2 TB/s; 64 rows 4 us.  The partials are fp32: rounded to bf16 they would be off by as much again as the
 // result's own rounding.
 template <bool BF16>
 __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedParams p, void* o_lat, float* lse)

@@ -10,6 +10,9 @@
 // A small call is bound by round trips (length, page, tile, and one for whatever of the code comes first: what runs once is kept short,
 // loops instead of their copies).
 //
+// Measured: 64 sequences x 32 rows under a window of 4096 76 us in the kernel, 303 MB, 4.0 TB/s (one workgroup per CU: 147 KB of tiles, two or three of the four on
+// their way); a window of 4096 of one sequence 15 us, of which 4 are the join; 256 rows on 1000 cached ones 18, where the kernel for many rows takes 20.
+//
 // References of the exponentials, masks and keys that are not finite: as in the kernel for many rows (decode_masked.hip), but that a
 // wavefront goes over its tiles again by itself where a score exceeds its reference by more than 2^64.
 #include "masked_tile.h"
