@@ -32,7 +32,7 @@ Plan plan_of(int B, int64_t H, int d_c, int64_t tiles, const Kernel& k)
     const double wide = (d_c + 64) / 576.0;
     auto cost = [&](int s) {
         const double rounds = (double)((((int64_t)B * s + 7) / 8 * Z + 31) / 32);
-        return rounds * ((double)((tiles + s - 1) / s) * k.tile * wide + k.start) + (s > 1 ? 6.0 + 8e-4 * wide * (double)(B * H) * s : 0.0);
+        return rounds * ((double)((tiles + s - 1) / s) * k.tile * wide + k.start) + (s > 1 ? 6.0 + 6e-4 * wide * (double)(B * H) * s : 0.0);
     };
     Plan p = {1, cost(1), 0, 0};
     for (int s = 2; s <= MK_MAX_CHUNKS && s <= tiles && B * Z < 4096; ++s)          // (4096: rounds enough; and what is left fits the merge's grid)
@@ -88,8 +88,8 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
     const size_t need = workspace_bytes_for(p.B, p.q_len, p.heads, p.d_c, tiles);
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return MLA_ERR_WORKSPACE;
     // Groups of 32 rows read the tiles again for each (from L2), 128 rows wait longer for theirs: few rows or short chunks of them are better
-    // off as groups of 32 (one token or tree of 256 rows on 1000 / 16000 / 64000 rows: 24.7, 42, 86 us by 128, 21.9, 34, 66 by 32), many are not
-    // (16 x 560 rows on 4000: 117, 189; 2 x 256 on 64000: 101, 109).
+    // off as groups of 32 (256 rows on 1000 / 16000 / 64000 rows: 24.7, 42, 86 us by 128, 21.9, 34, 66 by 32), many are not
+    // (16 x 560 rows on 4000: 116, 192; 2 x 256 on 64000: 101, 112).
     Plan plan = plan_of(p.B, H, p.d_c, tiles, matrix ? TALL : PORTABLE);
     bool thin = false;
     if (matrix && cache == MLA_BF16) {
