@@ -455,6 +455,11 @@ def prefill_mha(q_nope: torch.Tensor, q_rope: torch.Tensor, W_UK: torch.Tensor, 
 # Masked attention (include/mla_masked_gfx950.h).  These calls check the shapes of everything they write, and run on the
 # device of their tensors whichever is current.
 
+def _rows(n: int) -> int:
+    """A window or sinks as a C int: more than there can be is as much as there is."""
+    return max(-1, min(int(n), 0x7FFFFFFF))
+
+
 def _together(first: torch.Tensor, **others: Optional[torch.Tensor]):
     for name, t in others.items():
         if t is not None and t.device != first.device:
@@ -541,7 +546,7 @@ def decode_paged_tree(q_abs: torch.Tensor, q_rope: Optional[torch.Tensor], kv_ca
 
 def decode_window_workspace_bytes(B: int, q_len: int, H: int, d_c: int, max_rows: int, window: int, sinks: int) -> int:
     """max_rows: page_size * max_pages_per_seq."""
-    return int(lib().mla_decode_window_workspace_bytes(B, q_len, H, d_c, max_rows, window, sinks))
+    return int(lib().mla_decode_window_workspace_bytes(B, q_len, H, d_c, max_rows, _rows(window), _rows(sinks)))
 
 
 def decode_paged_window(q_abs: torch.Tensor, q_rope: Optional[torch.Tensor], kv_cache: torch.Tensor, page_table: torch.Tensor,
@@ -570,13 +575,13 @@ def decode_paged_window(q_abs: torch.Tensor, q_rope: Optional[torch.Tensor], kv_
               out=out, lse=lse)
     _call_on(q_abs, "mla_decode_paged_window", _dev(q_abs, "q_abs"), _dev(q_rope, "q_rope"), _dev(kv_cache, "kv_cache"), _dev(kv_scale, "kv_scale"),
              _dev(page_table, "page_table"), _dev(seq_lens, "seq_lens"), _dev(out, "out"), _dev(lse, "lse"), _dev(workspace, "workspace"),
-             workspace.numel() * workspace.element_size(), B, T, H, d_c, d_rope, page_size, num_pages, page_table.shape[1], int(window),
-             int(sinks), float(softmax_scale), _io_code(q_abs), _cache_code(kv_cache), int(flags))
+             workspace.numel() * workspace.element_size(), B, T, H, d_c, d_rope, page_size, num_pages, page_table.shape[1], _rows(window),
+             _rows(sinks), float(softmax_scale), _io_code(q_abs), _cache_code(kv_cache), int(flags))
     return (out, lse) if lse is not None else out
 
 
 def prefill_window_workspace_bytes(B: int, q_len: int, H: int, d_c: int, max_pages_per_seq: int, window: int, sinks: int) -> int:
-    return int(lib().mla_prefill_window_workspace_bytes(B, q_len, H, d_c, max_pages_per_seq, window, sinks))
+    return int(lib().mla_prefill_window_workspace_bytes(B, q_len, H, d_c, max_pages_per_seq, _rows(window), _rows(sinks)))
 
 
 def prefill_window(q_nope: torch.Tensor, q_rope: torch.Tensor, W_UK: torch.Tensor, W_UV: torch.Tensor, kv_cache: torch.Tensor,
@@ -610,7 +615,7 @@ def prefill_window(q_nope: torch.Tensor, q_rope: torch.Tensor, W_UK: torch.Tenso
     _call_on(q_nope, "mla_prefill_window", _dev(q_nope, "q_nope"), _dev(q_rope, "q_rope"), _dev(W_UK, "W_UK"), _dev(W_UV, "W_UV"),
              _dev(kv_cache, "kv_cache"), _dev(page_table, "page_table"), _dev(seq_lens, "seq_lens"), _dev(out, "out"), _dev(lse, "lse"),
              _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), B, T, H, d_head, d_c, d_rope, page_size, num_pages,
-             page_table.shape[1], int(window), int(sinks), float(softmax_scale), _io_code(q_nope), _cache_code(kv_cache))
+             page_table.shape[1], _rows(window), _rows(sinks), float(softmax_scale), _io_code(q_nope), _cache_code(kv_cache))
     return (out, lse) if lse is not None else out
 
 

@@ -250,3 +250,19 @@ def test_rows_past_four_gigabytes(kind):
     want = c.kv.view(torch.uint8).view(-1, 576 * c.kv.element_size())[c.places(0, [300, 302])].clone()
     layer.cache_move(c.kv, c.table[:1], src, torch.tensor([[10, 11]], dtype=torch.int32, device=DEV), kv_scale=c.scale)
     assert torch.equal(c.kv.view(torch.uint8).view(-1, 576 * c.kv.element_size())[c.places(0, [10, 11])], want)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+def test_results_off_sixteen_bytes(kind):
+    """Outputs that begin anywhere, whole and in chunks."""
+    for T, H, prefix in ((6, 32, [700, 40]), (20, 28, crowd([90]))):
+        (ref, lse), c, (q, qr), mask, lens = run_tree(kind, prefix, T, H)
+        room, room2 = torch.full((q.numel() + 9,), 7.0, dtype=BF, device=DEV), torch.full((lse.numel() + 3,), 7.0, device=DEV)
+        out, l2 = room[1:-8].view(q.shape), room2[1:-2].view(lse.shape)
+        mla.decode_paged_tree(q, qr, c.kv, c.table, lens, mask, SCALE, kv_scale=c.scale, out=out, lse=l2)
+        assert torch.equal(out, ref) and torch.equal(l2, lse)
+        assert (room[:1] == 7).all() and (room[-8:] == 7).all() and (room2[:1] == 7).all() and (room2[-2:] == 7).all()
+        n, wide = lens + T, 2 ** 32 + 3
+        a = mla.decode_paged_window(q, qr, c.kv, c.table, n, wide, wide, SCALE, kv_scale=c.scale)
+        b = mla.decode_paged_window(q, qr, c.kv, c.table, n, 2 ** 31 - 1, 0, SCALE, kv_scale=c.scale)
+        assert (a.double() - b.double()).abs().max() <= 0.02 * b.double().abs().max()

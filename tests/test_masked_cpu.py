@@ -127,3 +127,12 @@ def test_binding_refusals():
     bad(ValueError, layer.cache_move, kv, table, src, src, torch.zeros(2, 64))
     bad(ValueError, layer.cache_move, kv.to(torch.float8_e4m3fn), table, src, src)
     bad(ValueError, layer.cache_move, kv, table, src, src)                                          # not on the GPU
+
+
+def test_windows_past_32_bits_are_wide_ones():
+    wide = mla.decode_window_workspace_bytes(4, 1, 32, 512, 8192, 2 ** 31 - 1, 0)
+    for big in (2 ** 31, 2 ** 32 + 64, 2 ** 40):
+        assert mla.decode_window_workspace_bytes(4, 1, 32, 512, 8192, big, 0) == wide
+        assert mla.decode_window_workspace_bytes(4, 1, 32, 512, 8192, 64, big) == wide
+        assert mla.prefill_window_workspace_bytes(1, 100, 8, 512, 1000, big, big) == mla.prefill_window_workspace_bytes(1, 100, 8, 512, 1000, 64000, 64000)
+        assert mla.decode_window_workspace_bytes(4, 1, 32, 512, 8192, -big, 0) == 0
