@@ -379,10 +379,6 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         u32x4 raw[NRB][NKS / 2];               // (fp8) the codes of two k-steps
         float m_use[2];
         uint32_t w[2][4 * NT];
-        auto widened = [&](uint32_t lo, uint32_t up) -> bf16x8 {
-            auto two = [&](uint32_t v, auto high) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, decltype(high)::value)); };
-            return __builtin_bit_cast(bf16x8, (u32x4){two(lo, std::false_type{}), two(lo, std::true_type{}), two(up, std::false_type{}), two(up, std::true_type{})});
-        };
         auto key_of = [&](int rb, int ks) -> bf16x8 {
             if constexpr (FP8) return widened(raw[rb][ks / 2][ks % 2 * 2], raw[rb][ks / 2][ks % 2 * 2 + 1]);
             else               return ka[rb][ks];

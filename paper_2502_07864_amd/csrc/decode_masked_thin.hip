@@ -1,17 +1,20 @@
-// Masked attention over the latent cache on the matrix cores for few query rows (bf16 queries and cache): 32 query rows per workgroup.
+// Masked attention over the latent cache on the matrix cores for few query rows (bf16 queries, bf16 or fp8 cache): 32 query rows per workgroup.
 //
 //   S^T [keys x 32] = K [keys x (d_c + 64)] . Q^T,   O^T [d_c x 32] += V^T [d_c x keys] . P^T,   V = the first d_c columns of K
 //
 // Few rows are bound by the stream of the cache.  The four wavefronts of a workgroup have the same 32 query rows and take the chunk's
 // tiles of 32 keys in turn, each with a place of its own in the LDS and a softmax of its own: no barrier until the end, where the four
 // results are joined.  A wavefront waits for its tile, scores, weighs and accumulates it, and asks for its next one; while one waits the
-// others compute, so that two or three tiles of a CU are on their way at any time, and a chunk of up to four tiles is one round trip.
+// others compute, so that two or three tiles of a CU are on their way at any time, and a chunk of up to four tiles is one round trip.  fp8 tiles are half as
+// wide: a wavefront has two places, and asks two tiles ahead; codes are widened to bf16 (exactly) where they are read, the row's scale goes to
+// scores and weights.
 //
 // A small call is bound by round trips (length, page, tile, and one for whatever of the code comes first: what runs once is kept short,
 // loops instead of their copies).
 //
 // Measured: 64 sequences x 32 rows under a window of 4096 76 us in the kernel, 303 MB, 4.0 TB/s (one workgroup per CU: 147 KB of tiles, two or three of the four on
-// their way); a window of 4096 of one sequence 15 us, of which 4 are the join; 256 rows on 1000 cached ones 18, where the kernel for many rows takes 20.
+// their way); a window of 4096 of one sequence 15 us, of which 4 are the join; 256 rows on 1000 cached ones 18, where the kernel for many rows takes 20.  fp8: 16 sequences of 64000 rows, 32
+// query rows, 130 us a call, 4.5 TB/s (on the kernel for many rows 292).
 //
 // References of the exponentials, masks and keys that are not finite: as in the kernel for many rows (decode_masked.hip), but that a
 // wavefront goes over its tiles again by itself where a score exceeds its reference by more than 2^64.
@@ -21,14 +24,18 @@
 namespace mla {
 namespace {
 
-template <int D_C>
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+
+template <int D_C, bool FP8>
 __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams p)
 {
-    constexpr int ROW = D_C + 64, ROWB = ROW * 2, CPR = ROWB / 16;
+    constexpr int ROW = D_C + 64, ROWB = FP8 ? ROW : ROW * 2, CPR = ROWB / 16;
     constexpr int TILE_B = MK_TILE * ROWB;
     constexpr int NKS = ROW / 32, NCT = D_C / 16;
+    constexpr int PLACES = FP8 ? 2 : 1, PLACE_B = PLACES * TILE_B;       // of a wavefront
 
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE_B];
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * PLACE_B];
+    __shared__ __attribute__((aligned(16))) float ks_smem[FP8 ? 4 : 1][2][64];     // (fp8) scales of the rows of a tile, twice
     __shared__ uint64_t tree_smem[64];
     __shared__ float m_smem[4][32], l_smem[4][32];      // reference and normaliser of every wavefront's rows
     __shared__ __attribute__((aligned(16))) float f_smem[32][4];         // and factor
@@ -68,11 +75,32 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
         const int k = 2 * reach.tile(min(v + 4 * (lane >> 1), v1 - 1)) + (lane & 1);
         return half_at(p, half_page(p, ptab, per_page, k), per_page, k);
     };
-    LDS_AS unsigned char* const tile = lds + wave * TILE_B;
-    const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tile);
-    auto request = [&](const Place& s) {
+    LDS_AS unsigned char* const mine = lds + wave * PLACE_B;
+    LDS_AS float* const my_scales = (LDS_AS float*)ks_smem[FP8 ? wave : 0][0];
+    const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)mine);
+    // (fp8) codes as they are, chunk c of row r at position c ^ (r >> 2 & 2), and the scales; always as many loads, so that they can be waited
+    // for by count: a half that is not there is some other, which nobody sees
+    constexpr int PER_TILE = FP8 ? TILE_B / 1024 + 1 : 0;
+    auto request = [&](const Place& s, int slot) {
         const int l = lane_again();
-        constexpr int EIGHT = CPR / 8;                  // loads of eight rows, after which the swizzle repeats
+        if constexpr (FP8) {
+            const uint32_t to = dst + (uint32_t)slot * TILE_B;
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)max(h ? s.hi : s.lo, 0) * (TILE_B / 2);
+#pragma unroll
+                for (int k = 0; k < TILE_B / 2048; ++k) {
+                    const uint32_t off = (uint32_t)(l * 16) ^ (k * 64 + l >= 8 * CPR ? 32u : 0u), at = to + (uint32_t)h * (TILE_B / 2) + (uint32_t)k * 1024u;
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(at), "v"(off), "s"(src + k * 1024) : "memory");
+                }
+            }
+            const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)my_scales + (uint32_t)slot * 256u);
+            const int low = s.lo, high = s.hi;
+            const float* from = p.kv_scale + (size_t)max(l & 16 ? high : low, 0) * 16 + (l & 15);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(at), "v"(from) : "memory");
+            return;
+        }
+        constexpr int EIGHT = FP8 ? 1 : CPR / 8;        // loads of eight rows, after which the swizzle repeats
 #pragma unroll 1
         for (int i = 0; i < 4; ++i) {
             const int half = i < 2 ? s.lo : s.hi;
@@ -86,12 +114,19 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
             }
         }
     };
-    Place at;
+    Place at, next = Place{-1, -1};                     // of this tile, (fp8) and of the wavefront's next one
     int32_t ids;
+    auto place_now = [&](int v) { return tile_place(p, (const CONST_AS int32_t*)ptab, per_page, reach.tile(v)); };
     auto start = [&]() {
         at = Place{-1, -1};
-        if (v0 + wave < v1) at = tile_place(p, (const CONST_AS int32_t*)ptab, per_page, reach.tile(v0 + wave));
-        request(at);
+        if (v0 + wave < v1) {
+            at = place_now(v0 + wave);
+            request(at, 0);
+        }
+        if (FP8 && v0 + wave + 4 < v1) {
+            next = place_now(v0 + wave + 4);
+            request(next, 1);
+        }
         ids = ids_from(v0 + wave);
     };
     start();
@@ -106,8 +141,9 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
             const size_t row = hb + min(hi * 16 + n, HL - 1);
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks) {
-                const u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + ks * 32 + g * 8)
-                                        : *reinterpret_cast<const u32x4*>(qr + row * 64 + (ks - D_C / 32) * 32 + g * 8);
+                // (fp8: a lane reads 16 codes at a time, eight for each of two k-steps)
+                const int kl = ks < D_C / 32 ? ks : ks - D_C / 32, col = FP8 ? (kl >> 1) * 64 + g * 16 + (kl & 1) * 8 : kl * 32 + g * 8;
+                const u32x4 v = ks < D_C / 32 ? *reinterpret_cast<const u32x4*>(qa + row * D_C + col) : *reinterpret_cast<const u32x4*>(qr + row * 64 + col);
                 qreg[hi][ks] = __builtin_bit_cast(bf16x8, v);
             }
         }
@@ -135,16 +171,23 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
     f32x4 oacc[2][NCT];
     const float sc = fmaxf(fabsf(p.scale) * LOG2E, 1.17549435e-38f);     // (never zero: a masked score is -inf and has to stay it)
 
-    // score A operand: key row 16 rb + n, chunk 4 ks + g; transposing reads: tile row 4g + (n >> 2) (and 16 more), 8 bytes at column 16 ct + 4 (n & 3)
+    // keys and places of the reads: as in the kernel for many rows
+    constexpr int LANE_KEYS = FP8 ? 8 : 4, BLOCK_KEYS = FP8 ? 4 : 16;         // key LANE_KEYS g + BLOCK_KEYS rb + i
     uint32_t a_base[2], t_base[4];
+    if constexpr (FP8) {
+        const int row = 8 * (n >> 2) + (n & 3), from = 8 * g + (n >> 1);
+        a_base[0] = a_base[1] = (uint32_t)(row * ROWB) + (((uint32_t)g ^ (uint32_t)(row >> 2 & 2)) << 4);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) a_base[e] = (uint32_t)(n * ROWB) + ((((uint32_t)(4 * e + g)) ^ (uint32_t)swz_key(n)) << 4);
-    {
+        for (int e = 0; e < 4; ++e) t_base[e] = (uint32_t)(from * ROWB) + (((uint32_t)e ^ (uint32_t)(from >> 2 & 2)) << 4) + (uint32_t)((n & 1) * 8);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) a_base[e] = (uint32_t)(n * ROWB) + ((((uint32_t)(4 * e + g)) ^ (uint32_t)swz_key(n)) << 4);
         const int r = g * 4 + (n >> 2);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             t_base[e] = (uint32_t)(r * ROWB) + ((((uint32_t)(2 * e) + (uint32_t)((n & 3) >> 1)) ^ (uint32_t)swz_key(r)) << 4) + (uint32_t)((n & 1) * 8);
     }
+    f32x4 ksc[2];                                       // (fp8) scales of this lane's keys
 
     // ---- sweeps over the tiles: ACCUMULATE against the references, and where some score exceeded its own by more than FAST_GAP (rare) one
     // for the exact maxima (it accumulates too, which is not used) and one against them
@@ -162,14 +205,28 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
         int turn = 0;
         for (int v = v0 + wave; v < v1; v += 4, ++turn) {
             if (turn && (turn & 31) == 0) ids = ids_from(v);
-            wait_vmcnt<0>();
+            if (FP8 && v + 4 < v1) wait_vmcnt<PER_TILE>();
+            else                   wait_vmcnt<0>();
             __builtin_amdgcn_sched_barrier(0);
+            LDS_AS unsigned char* const tile = mine + (FP8 ? (turn & 1) * TILE_B : 0);
 
             // ---- scores
             f32x4 x[2][2];
             {
-                bf16x8 ka[2][NKS];
+                bf16x8 ka[2][NKS], kk[2][2];
+                u32x4 raw[2][NKS / 2];                      // (fp8) the codes of two k-steps
+                auto key_of = [&](int rb, int ks) -> bf16x8 {
+                    if constexpr (FP8) return widened(raw[rb][ks / 2][ks % 2 * 2], raw[rb][ks / 2][ks % 2 * 2 + 1]);
+                    else               return ka[rb][ks];
+                };
                 auto rk = [&](int ks) {
+                    if constexpr (FP8) {
+                        if (ks % 2 == 0) {
+#pragma unroll
+                            for (int rb = 0; rb < 2; ++rb) raw[rb][ks / 2] = *(LDS_AS u32x4*)(tile + a_base[0] + ks / 2 * 64 + rb * 4 * ROWB);
+                        }
+                        return;
+                    }
 #pragma unroll
                     for (int rb = 0; rb < 2; ++rb) ka[rb][ks] = *(LDS_AS bf16x8*)(tile + a_base[ks & 1] + (ks >> 1) * 128 + rb * 16 * ROWB);
                 };
@@ -181,24 +238,37 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                 for (int ks = 0; ks < NKS; ++ks) {
                     if (ks + AHEAD < NKS) rk(ks + AHEAD);
 #pragma unroll
+                    for (int rb = 0; rb < 2; ++rb) {
+                        kk[ks & 1][rb] = FP8 && ks ? kk[ks & 1][rb] : key_of(rb, ks);
+                        if (FP8 && ks + 1 < NKS) kk[~ks & 1][rb] = key_of(rb, ks + 1);      // (widened beside the matrix instructions before)
+                    }
+#pragma unroll
                     for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                         for (int hi = 0; hi < 2; ++hi)
-                            x[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[rb][ks], qreg[hi][ks], ks == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : x[rb][hi], 0, 0, 0);
+                            x[rb][hi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[ks & 1][rb], qreg[hi][ks], ks == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : x[rb][hi], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if constexpr (FP8) {
+#pragma unroll
+                for (int rb = 0; rb < 2; ++rb) {
+                    ksc[rb] = *(LDS_AS f32x4*)(my_scales + (turn & 1) * 64 + g * 8 + rb * 4);
+#pragma unroll
+                    for (int hi = 0; hi < 2; ++hi) x[rb][hi] *= ksc[rb];
                 }
             }
             if (__builtin_expect(!at.whole() || !whole.holds(v), 0)) {
                 bool odd = false;
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) {
-                    const uint32_t sees = (at.rows() & visible_rows(p, reach, reach.tile(v) * MK_TILE, token[hi], tree ? tree_smem[token[hi]] : 0)) >> (4 * g);
+                    const uint32_t sees = (at.rows() & visible_rows(p, reach, reach.tile(v) * MK_TILE, token[hi], tree ? tree_smem[token[hi]] : 0)) >> (LANE_KEYS * g);
 #pragma unroll
                     for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const bool bad = !(fabsf(x[rb][hi][i]) < INFINITY);
-                            if (sees >> (rb * 16 + i) & 1u) {
+                            if (sees >> (rb * BLOCK_KEYS + i) & 1u) {
                                 poisoned[hi] |= bad;
                             } else {
                                 odd |= bad;
@@ -206,14 +276,21 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                             }
                         }
                 }
-                if (__builtin_expect(__any(odd), 0))        // values that are not finite, of keys that somebody does not see
+                if (__builtin_expect(__any(odd), 0)) {      // values (fp8: or scales) that are not finite, of keys that somebody does not see
                     for (int i = lane; i < TILE_B / 16; i += 64) {
                         LDS_AS u32x4* unit = (LDS_AS u32x4*)(tile + i * 16);
                         u32x4 w = *unit;
 #pragma unroll
-                        for (int d = 0; d < 4; ++d) w[d] = finite_halves(w[d]);
+                        for (int d = 0; d < 4; ++d) w[d] = FP8 ? finite_codes(w[d]) : finite_halves(w[d]);
                         *unit = w;
                     }
+                    if constexpr (FP8) {
+#pragma unroll
+                        for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) ksc[rb][i] = fabsf(ksc[rb][i]) < INFINITY ? ksc[rb][i] : 0.f;
+                    }
+                }
             }
             // ---- weights
 #pragma unroll
@@ -237,8 +314,12 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                 uint32_t w[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float e0 = fast_exp2(fmaf(x[k >> 1][hi][2 * (k & 1)], sc, -m_use)), e1 = fast_exp2(fmaf(x[k >> 1][hi][2 * (k & 1) + 1], sc, -m_use));
+                    float e0 = fast_exp2(fmaf(x[k >> 1][hi][2 * (k & 1)], sc, -m_use)), e1 = fast_exp2(fmaf(x[k >> 1][hi][2 * (k & 1) + 1], sc, -m_use));
                     l_run[hi] += e0 + e1;
+                    if constexpr (FP8) {
+                        e0 *= ksc[k >> 1][2 * (k & 1)];
+                        e1 *= ksc[k >> 1][2 * (k & 1) + 1];
+                    }
                     w[k] = pack_bf16x2(e0, e1);
                 }
                 pb[hi] = __builtin_bit_cast(bf16x8, (u32x4){w[0], w[1], w[2], w[3]});
@@ -246,8 +327,13 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
             // ---- values
             {
                 s16x4 lo[NCT], up[NCT];
+                u32x2 column[NCT];
                 auto rt = [&](int ct) {
-                    LDS_AS unsigned char* from = tile + t_base[ct & 3] + (ct >> 2) * 128;
+                    LDS_AS unsigned char* from = tile + t_base[ct & 3] + (ct >> 2) * (FP8 ? 64 : 128);
+                    if constexpr (FP8) {
+                        column[ct] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_AS i32x2*)from));
+                        return;
+                    }
                     lo[ct] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)from);
                     up[ct] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(from + 16 * ROWB));
                 };
@@ -258,18 +344,27 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 #pragma unroll
                 for (int ct = 0; ct < NCT; ++ct) {
                     if (ct + AHEAD < NCT) rt(ct + AHEAD);
-                    const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo[ct], up[ct], 0, 1, 2, 3, 4, 5, 6, 7));
+                    const bf16x8 va = FP8 ? widened(column[ct][0], column[ct][1])
+                                          : __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo[ct], up[ct], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                     for (int hi = 0; hi < 2; ++hi) oacc[hi][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[hi], oacc[hi][ct], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
             // (every read of the tile has been waited for: its place is free)
-            if (v + 4 < v1) {
-                const int i = 2 * ((turn + 1) & 31);
-                at = Place{(int)__builtin_amdgcn_readlane(ids, i), (int)__builtin_amdgcn_readlane(ids, i + 1)};
-                if (i == 0) at = tile_place(p, (const CONST_AS int32_t*)ptab, per_page, reach.tile(v + 4));
-                request(at);
+            if constexpr (FP8) {
+                at = next;
+                if (v + 8 < v1) {
+                    const int i = (turn + 2) & 31;
+                    next = Place{(int)__builtin_amdgcn_readlane(ids, 2 * i), (int)__builtin_amdgcn_readlane(ids, 2 * i + 1)};
+                    if (i < 2) next = place_now(v + 8);     // (not looked up yet)
+                    request(next, turn & 1);
+                }
+            } else if (v + 4 < v1) {
+                const int i = (turn + 1) & 31;
+                at = Place{(int)__builtin_amdgcn_readlane(ids, 2 * i), (int)__builtin_amdgcn_readlane(ids, 2 * i + 1)};
+                if (i == 0) at = place_now(v + 4);
+                request(at, 0);
             }
         }
         if (pass == ACCUMULATE_AGAIN) break;
@@ -306,18 +401,18 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
     if (tid < 128) {
         const int w = tid >> 5, r = tid & 31;
         const float m = fmaxf(fmaxf(m_smem[0][r], m_smem[1][r]), fmaxf(m_smem[2][r], m_smem[3][r])), ref = m == -INFINITY ? 0.f : m;
-        float l = 0.f, mine = 0.f;
+        float l = 0.f, own = 0.f;
         for (int k = 0; k < 4; ++k) {
             const float lk = l_smem[k][r], mk = m_smem[k][r];
             const float e = lk == 0.f ? 0.f : mk == -INFINITY ? 1.f : fast_exp2(mk - ref);       // (-inf with a sum: a NaN)
             if (lk != 0.f) l += lk * e;
-            if (k == w) mine = e;
+            if (k == w) own = e;
         }
-        f_smem[r][w] = bad_smem[w][r] ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : mine / l;
+        f_smem[r][w] = bad_smem[w][r] ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : own / l;
         if (w == 0 && r < HL && p.lse_part) p.lse_part[part_of(r)] = l == 0.f ? -INFINITY : ref * LN2 + __builtin_amdgcn_logf(l) * LN2;
     }
     constexpr int RSO = D_C * 2 + 16;                   // bytes from row to row of half the columns in fp32 (padded)
-    static_assert(32 * RSO <= TILE_B, "exchange space must fit in a tile's place");
+    static_assert(32 * RSO <= PLACE_B, "exchange space must fit in a tile's place");
     constexpr int LPR = D_C / 8;                        // lanes of half a row, four columns each
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -325,7 +420,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi)
 #pragma unroll
-            for (int ct = 0; ct < NCT / 2; ++ct) *(LDS_AS f32x4*)(tile + (hi * 16 + n) * RSO + (ct * 16 + g * 4) * 4) = oacc[hi][half * (NCT / 2) + ct];
+            for (int ct = 0; ct < NCT / 2; ++ct) *(LDS_AS f32x4*)(mine + (hi * 16 + n) * RSO + (ct * 16 + g * 4) * 4) = oacc[hi][half * (NCT / 2) + ct];
         __syncthreads();
         constexpr int STEP = MF_THREADS / LPR, TURNS = 32 / STEP, BATCH = 4;      // rows at a time; (all reads of a batch on their way before any is used)
         const int c = tid % LPR;
@@ -338,7 +433,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int r = tid / LPR + (k0 + k) * STEP;
-                    part[k][w] = *(LDS_AS f32x4*)(lds + w * TILE_B + r * RSO + c * 16);
+                    part[k][w] = *(LDS_AS f32x4*)(lds + w * PLACE_B + r * RSO + c * 16);
                     f[k][w] = f_smem[r][w];
                 }
             __builtin_amdgcn_sched_barrier(0);
@@ -363,11 +458,14 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 
 }  // namespace
 
-hipError_t launch_masked_thin(const MaskedParams& p, hipStream_t s)
+hipError_t launch_masked_thin(const MaskedParams& p, mla_dtype cache, hipStream_t s)
 {
     const unsigned chunks = ((unsigned)p.B * p.num_splits + 7) / 8 * 8, Z = (unsigned)((p.H + MK_THIN_ROWS - 1) / MK_THIN_ROWS);
-    if (p.d_c == 512) masked_thin_kernel<512><<<dim3(chunks * Z), dim3(MF_THREADS), 0, s>>>(p);
-    else              masked_thin_kernel<256><<<dim3(chunks * Z), dim3(MF_THREADS), 0, s>>>(p);
+    const dim3 grid(chunks * Z), block(MF_THREADS);
+    if (cache == MLA_BF16 && p.d_c == 512)      masked_thin_kernel<512, false><<<grid, block, 0, s>>>(p);
+    else if (cache == MLA_BF16)                 masked_thin_kernel<256, false><<<grid, block, 0, s>>>(p);
+    else if (p.d_c == 512)                      masked_thin_kernel<512, true><<<grid, block, 0, s>>>(p);
+    else                                        masked_thin_kernel<256, true><<<grid, block, 0, s>>>(p);
     return hipGetLastError();
 }
 

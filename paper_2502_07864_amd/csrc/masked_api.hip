@@ -87,12 +87,12 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
     const bool matrix = !(flags & MLA_FLAG_PORTABLE_KERNEL) && masked_tall_supported(p, io, cache);
     const size_t need = workspace_bytes_for(p.B, p.q_len, p.heads, p.d_c, tiles);
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return MLA_ERR_WORKSPACE;
-    // Groups of 32 rows read the tiles again for each (from L2), 128 rows wait longer for theirs: few rows or short chunks of them are better
+    // (either cache type.)  Groups of 32 rows read the tiles again for each (from L2), 128 rows wait longer for theirs: few rows or short chunks of them are better
     // off as groups of 32 (256 rows on 1000 / 16000 / 64000 rows: 24.7, 42, 86 us by 128, 21.9, 34, 66 by 32), many are not
     // (16 x 560 rows on 4000: 116, 192; 2 x 256 on 64000: 101, 112).
     Plan plan = plan_of(p.B, H, p.d_c, tiles, matrix ? TALL : PORTABLE);
     bool thin = false;
-    if (matrix && cache == MLA_BF16) {
+    if (matrix) {
         const Plan few = plan_of(p.B, H, p.d_c, tiles, THIN);
         thin = few.cost < plan.cost;
         if (thin) plan = few;
@@ -106,7 +106,7 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
         p.lse_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.lse_off);
     }
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    hipError_t e = thin ? launch_masked_thin(p, stream) : matrix ? launch_masked_tall(p, cache, stream) : launch_masked_portable(p, io, cache, stream);
+    hipError_t e = thin ? launch_masked_thin(p, cache, stream) : matrix ? launch_masked_tall(p, cache, stream) : launch_masked_portable(p, io, cache, stream);
     if (e == hipSuccess && plan.S > 1) e = launch_masked_merge(p, o_lat, lse, io, stream);
     return e == hipSuccess ? MLA_OK : MLA_ERR_HIP;
 }

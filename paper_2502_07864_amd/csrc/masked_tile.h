@@ -1,6 +1,7 @@
 // What the matrix-core kernels of the masked attention share.
 #pragma once
 #include "masked_internal.h"
+#include <type_traits>
 #include "mfma_tile.h"
 
 namespace mla {
@@ -107,6 +108,22 @@ __device__ __forceinline__ uint32_t finite_halves(uint32_t w)
     if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
     if ((w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
     return w;
+}
+
+// the four e4m3 codes of a word, zero where they are NaN
+__device__ __forceinline__ uint32_t finite_codes(uint32_t w)
+{
+#pragma unroll
+    for (int s = 0; s < 32; s += 8)
+        if ((w >> s & 0x7Fu) == 0x7Fu) w &= ~(0xFFu << s);
+    return w;
+}
+
+// eight e4m3 codes in bf16, which holds them exactly
+__device__ __forceinline__ bf16x8 widened(uint32_t lo, uint32_t up)
+{
+    auto two = [](uint32_t v, auto high) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, decltype(high)::value)); };
+    return __builtin_bit_cast(bf16x8, (u32x4){two(lo, std::false_type{}), two(lo, std::true_type{}), two(up, std::false_type{}), two(up, std::true_type{})});
 }
 
 // maximum of three (a NaN loses, as in fmaxf; written out: fmaxf would quieten every operand first)
