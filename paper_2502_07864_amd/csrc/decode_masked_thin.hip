@@ -4,7 +4,7 @@
 //
 // Few rows are bound by the stream of the cache.  The four wavefronts of a workgroup have the same 32 query rows and take the chunk's
 // tiles of 32 keys in turn, each with a place of its own in the LDS and a softmax of its own: no barrier until the end, where the four
-// results are joined.  A wavefront waits for its tile, scores, weighs and accumulates it, and asks for its next one; while one waits the
+// results are joined.  A wavefront waits for its tile block by block, scores, weighs and accumulates it, and asks for its next one block by block beside the value products; while one waits the
 // others compute, so that two or three tiles of a CU are on their way at any time, and a chunk of up to four tiles is one round trip.  fp8 tiles are half as
 // wide: a wavefront has two places, and asks two tiles ahead; codes are widened to bf16 (exactly) where they are read, the row's scale goes to
 // scores and weights.
@@ -12,9 +12,9 @@
 // A small call is bound by round trips (length, page, tile, and one for whatever of the code comes first: what runs once is kept short,
 // loops instead of their copies).
 //
-// Measured: 64 sequences x 32 rows under a window of 4096 76 us in the kernel, 303 MB, 4.0 TB/s (one workgroup per CU: 147 KB of tiles, two or three of the four on
-// their way); a window of 4096 of one sequence 15 us, of which 4 are the join; 256 rows on 1000 cached ones 18, where the kernel for many rows takes 20.  fp8: 16 sequences of 64000 rows, 32
-// query rows, 130 us a call, 4.5 TB/s (on the kernel for many rows 292).
+// Measured: 64 sequences x 32 rows under a window of 4096 71 us a call, 307 MB, 4.8 TB/s in the kernel (past the caches; 82 with whole tiles asked for at the end of the
+// last one and through them); a window of 4096 of one sequence 16 us in the kernel, of which 4 are the join; 256 rows on 1000 cached ones 18, where the kernel for many rows takes 20.  fp8: 16 sequences of 64000 rows, 32
+// query rows, 116 us a call, 5.1 TB/s (on the kernel for many rows 292); bf16 193 us, 6.1 TB/s.
 //
 // References of the exponentials, masks and keys that are not finite: as in the kernel for many rows (decode_masked.hip), but that a
 // wavefront goes over its tiles again by itself where a score exceeds its reference by more than 2^64.
@@ -26,7 +26,9 @@ namespace {
 
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 
-template <int D_C, bool FP8>
+// ONCE: a tile is read by this workgroup alone, past the caches.  32 query rows: 64 sequences under a window of 4096 80 us without, 70 with; 16 x 64000 rows 218, 192,
+// in fp8 130, 116.  Where other groups of rows read it too it costs more than it gives (256 rows on 4 x 16000: 62, 68).
+template <int D_C, bool FP8, bool ONCE>
 __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams p)
 {
     constexpr int ROW = D_C + 64, ROWB = FP8 ? ROW : ROW * 2, CPR = ROWB / 16;
@@ -81,6 +83,22 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
     // (fp8) codes as they are, chunk c of row r at position c ^ (r >> 2 & 2), and the scales; always as many loads, so that they can be waited
     // for by count: a half that is not there is some other, which nobody sees
     constexpr int PER_TILE = FP8 ? TILE_B / 1024 + 1 : 0;
+    // (bf16) in blocks of 64 columns, row r of a block behind row r - 1, its chunk c at position c ^ (r >> 1 & 7): the 16 rows of a read meet 16 different
+    // units, and a block that is done with can be asked for again while the others are read
+    constexpr int BLOCKS = ROW / 64, BLOCK_B = MK_TILE * 128;
+    auto load16 = [&](uint32_t to, uint32_t off, const unsigned char* src) {
+        if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(to), "v"(off), "s"(src) : "memory");
+        else                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(to), "v"(off), "s"(src) : "memory");
+    };
+    auto request_block = [&](const Place& s, int c) {
+        const int l = lane_again();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                   // eight rows at a time
+            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)max(i < 2 ? s.lo : s.hi, 0) * (TILE_B / 2) + (i & 1) * (8 * ROWB) + c * 128;
+            const uint32_t off = (uint32_t)((l >> 3) * ROWB) + (uint32_t)(((l & 7) ^ ((l >> 4) + 4 * (i & 1))) << 4), to = dst + (uint32_t)(c * BLOCK_B + i * 1024);
+            load16(to, off, src);
+        }
+    };
     auto request = [&](const Place& s, int slot) {
         const int l = lane_again();
         if constexpr (FP8) {
@@ -91,7 +109,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 #pragma unroll
                 for (int k = 0; k < TILE_B / 2048; ++k) {
                     const uint32_t off = (uint32_t)(l * 16) ^ (k * 64 + l >= 8 * CPR ? 32u : 0u), at = to + (uint32_t)h * (TILE_B / 2) + (uint32_t)k * 1024u;
-                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(at), "v"(off), "s"(src + k * 1024) : "memory");
+                    load16(at, off, src + k * 1024);
                 }
             }
             const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)my_scales + (uint32_t)slot * 256u);
@@ -100,19 +118,8 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(at), "v"(from) : "memory");
             return;
         }
-        constexpr int EIGHT = FP8 ? 1 : CPR / 8;        // loads of eight rows, after which the swizzle repeats
 #pragma unroll 1
-        for (int i = 0; i < 4; ++i) {
-            const int half = i < 2 ? s.lo : s.hi;
-            if (half < 0) continue;                     // a page outside the pool is never dereferenced
-            const unsigned char* src = static_cast<const unsigned char*>(p.kv) + (size_t)half * (TILE_B / 2) + (i & 1) * (EIGHT * 1024);
-#pragma unroll
-            for (int k = 0; k < EIGHT; ++k) {
-                const uint32_t off = ((uint32_t)l * 16) ^ piece_key<CPR>(k, l);
-                const uint32_t to = dst + (uint32_t)(i * EIGHT + k) * 1024u;
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(to), "v"(off), "s"(src + k * 1024) : "memory");
-            }
-        }
+        for (int c = 0; c < BLOCKS; ++c) request_block(s, c);
     };
     Place at, next = Place{-1, -1};                     // of this tile, (fp8) and of the wavefront's next one
     int32_t ids;
@@ -181,11 +188,11 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
         for (int e = 0; e < 4; ++e) t_base[e] = (uint32_t)(from * ROWB) + (((uint32_t)e ^ (uint32_t)(from >> 2 & 2)) << 4) + (uint32_t)((n & 1) * 8);
     } else {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) a_base[e] = (uint32_t)(n * ROWB) + ((((uint32_t)(4 * e + g)) ^ (uint32_t)swz_key(n)) << 4);
+        for (int e = 0; e < 2; ++e) a_base[e] = (uint32_t)(n * 128) + (((uint32_t)(4 * e + g) ^ (uint32_t)(n >> 1)) << 4);
         const int r = g * 4 + (n >> 2);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            t_base[e] = (uint32_t)(r * ROWB) + ((((uint32_t)(2 * e) + (uint32_t)((n & 3) >> 1)) ^ (uint32_t)swz_key(r)) << 4) + (uint32_t)((n & 1) * 8);
+            t_base[e] = (uint32_t)(r * 128) + ((((uint32_t)(2 * e) + (uint32_t)((n & 3) >> 1)) ^ (uint32_t)(r >> 1 & 7)) << 4) + (uint32_t)((n & 1) * 8);
     }
     f32x4 ksc[2];                                       // (fp8) scales of this lane's keys
 
@@ -203,11 +210,14 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
             for (int ct = 0; ct < NCT; ++ct) oacc[hi][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
         int turn = 0;
+        if constexpr (!FP8) wait_vmcnt<0>();            // (the queries, too: else each of their registers would be waited for in the loop)
         for (int v = v0 + wave; v < v1; v += 4, ++turn) {
             if (turn && (turn & 31) == 0) ids = ids_from(v);
-            if (FP8 && v + 4 < v1) wait_vmcnt<PER_TILE>();
-            else                   wait_vmcnt<0>();
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (FP8) {
+                if (v + 4 < v1) wait_vmcnt<PER_TILE>();
+                else            wait_vmcnt<0>();
+                __builtin_amdgcn_sched_barrier(0);
+            }
             LDS_AS unsigned char* const tile = mine + (FP8 ? (turn & 1) * TILE_B : 0);
 
             // ---- scores
@@ -219,6 +229,21 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                     if constexpr (FP8) return widened(raw[rb][ks / 2][ks % 2 * 2], raw[rb][ks / 2][ks % 2 * 2 + 1]);
                     else               return ka[rb][ks];
                 };
+                // (bf16) blocks 0 .. c are there: those behind them, four loads each, may be on their way
+                auto landed = [&](int c) {
+                    switch (BLOCKS - 1 - c) {
+                    case 0: wait_vmcnt<0>(); break;
+                    case 1: wait_vmcnt<4>(); break;
+                    case 2: wait_vmcnt<8>(); break;
+                    case 3: wait_vmcnt<12>(); break;
+                    case 4: wait_vmcnt<16>(); break;
+                    case 5: wait_vmcnt<20>(); break;
+                    case 6: wait_vmcnt<24>(); break;
+                    case 7: wait_vmcnt<28>(); break;
+                    default: wait_vmcnt<32>();
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                };
                 auto rk = [&](int ks) {
                     if constexpr (FP8) {
                         if (ks % 2 == 0) {
@@ -227,10 +252,12 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                         }
                         return;
                     }
+                    if (ks % 2 == 0) landed(ks / 2);
 #pragma unroll
-                    for (int rb = 0; rb < 2; ++rb) ka[rb][ks] = *(LDS_AS bf16x8*)(tile + a_base[ks & 1] + (ks >> 1) * 128 + rb * 16 * ROWB);
+                    for (int rb = 0; rb < 2; ++rb) ka[rb][ks] = *(LDS_AS bf16x8*)(tile + a_base[ks & 1] + (ks >> 1) * BLOCK_B + rb * 16 * 128);
                 };
                 static constexpr int AHEAD = 4;
+                static_assert(BLOCKS == 9 || BLOCKS == 5);
 #pragma unroll
                 for (int ks = 0; ks < AHEAD; ++ks) rk(ks);
                 __builtin_amdgcn_sched_barrier(0);
@@ -324,18 +351,24 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                 }
                 pb[hi] = __builtin_bit_cast(bf16x8, (u32x4){w[0], w[1], w[2], w[3]});
             }
-            // ---- values
+            // ---- values.  (bf16) The wavefront's next tile is asked for beside them, a block as soon as it is done with, the rope part's at the end.
+            const bool more = !FP8 && v + 4 < v1;
+            if (more) {
+                const int i = (turn + 1) & 31;
+                at = Place{(int)__builtin_amdgcn_readlane(ids, 2 * i), (int)__builtin_amdgcn_readlane(ids, 2 * i + 1)};
+                if (i == 0) at = place_now(v + 4);
+            }
             {
                 s16x4 lo[NCT], up[NCT];
                 u32x2 column[NCT];
                 auto rt = [&](int ct) {
-                    LDS_AS unsigned char* from = tile + t_base[ct & 3] + (ct >> 2) * (FP8 ? 64 : 128);
+                    LDS_AS unsigned char* from = tile + t_base[ct & 3] + (ct >> 2) * (FP8 ? 64 : BLOCK_B);
                     if constexpr (FP8) {
                         column[ct] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_AS i32x2*)from));
                         return;
                     }
                     lo[ct] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)from);
-                    up[ct] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(from + 16 * ROWB));
+                    up[ct] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(from + 16 * 128));
                 };
                 static constexpr int AHEAD = 4;
 #pragma unroll
@@ -348,6 +381,11 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                                           : __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo[ct], up[ct], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                     for (int hi = 0; hi < 2; ++hi) oacc[hi][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[hi], oacc[hi][ct], 0, 0, 0);
+                    if (!FP8 && ct % 4 == 3 && more) {
+                        __builtin_amdgcn_sched_barrier(0);              // (behind the wait for the block's last read)
+                        request_block(at, ct / 4);
+                        if (ct == NCT - 1) request_block(at, BLOCKS - 1);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -360,11 +398,6 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                     if (i < 2) next = place_now(v + 8);     // (not looked up yet)
                     request(next, turn & 1);
                 }
-            } else if (v + 4 < v1) {
-                const int i = (turn + 1) & 31;
-                at = Place{(int)__builtin_amdgcn_readlane(ids, 2 * i), (int)__builtin_amdgcn_readlane(ids, 2 * i + 1)};
-                if (i == 0) at = place_now(v + 4);
-                request(at, 0);
             }
         }
         if (pass == ACCUMULATE_AGAIN) break;
@@ -458,14 +491,19 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 
 }  // namespace
 
+template <int D_C, bool FP8> static void launch(const MaskedParams& p, unsigned chunks, unsigned Z, hipStream_t s)
+{
+    if (Z == 1) masked_thin_kernel<D_C, FP8, true><<<dim3(chunks), dim3(MF_THREADS), 0, s>>>(p);
+    else        masked_thin_kernel<D_C, FP8, false><<<dim3(chunks * Z), dim3(MF_THREADS), 0, s>>>(p);
+}
+
 hipError_t launch_masked_thin(const MaskedParams& p, mla_dtype cache, hipStream_t s)
 {
     const unsigned chunks = ((unsigned)p.B * p.num_splits + 7) / 8 * 8, Z = (unsigned)((p.H + MK_THIN_ROWS - 1) / MK_THIN_ROWS);
-    const dim3 grid(chunks * Z), block(MF_THREADS);
-    if (cache == MLA_BF16 && p.d_c == 512)      masked_thin_kernel<512, false><<<grid, block, 0, s>>>(p);
-    else if (cache == MLA_BF16)                 masked_thin_kernel<256, false><<<grid, block, 0, s>>>(p);
-    else if (p.d_c == 512)                      masked_thin_kernel<512, true><<<grid, block, 0, s>>>(p);
-    else                                        masked_thin_kernel<256, true><<<grid, block, 0, s>>>(p);
+    if (cache == MLA_BF16 && p.d_c == 512)      launch<512, false>(p, chunks, Z, s);
+    else if (cache == MLA_BF16)                 launch<256, false>(p, chunks, Z, s);
+    else if (p.d_c == 512)                      launch<512, true>(p, chunks, Z, s);
+    else                                        launch<256, true>(p, chunks, Z, s);
     return hipGetLastError();
 }
 
