@@ -26,8 +26,9 @@ namespace {
 
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 
-// ONCE: a tile is read by this workgroup alone, past the caches.  32 query rows: 64 sequences under a window of 4096 80 us without, 70 with; 16 x 64000 rows 218, 192,
-// in fp8 130, 116.  Where other groups of rows read it too it costs more than it gives (256 rows on 4 x 16000: 62, 68).
+// ONCE: tiles that this workgroup alone reads, past the caches.  32 query rows: 64 sequences under a window of 4096 80 us without, 70 with; 16 x 64000 rows 218, 192,
+// in fp8 130, 116.  Where other groups of rows read them too it costs more than it gives (256 rows on 4 x 16000: 62, 68), and where a call's rows are few
+// enough to be found in a cache by the next call (16 x 4000 rows, 75 MB: 38 and 34 on six sets in turn, 33 and 34 on two; one sequence of 16000, 19 MB: 27, 29).
 template <int D_C, bool FP8, bool ONCE>
 __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams p)
 {
@@ -491,19 +492,20 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 
 }  // namespace
 
-template <int D_C, bool FP8> static void launch(const MaskedParams& p, unsigned chunks, unsigned Z, hipStream_t s)
+template <int D_C, bool FP8> static void launch(const MaskedParams& p, unsigned chunks, unsigned Z, int64_t tiles, hipStream_t s)
 {
-    if (Z == 1) masked_thin_kernel<D_C, FP8, true><<<dim3(chunks), dim3(MF_THREADS), 0, s>>>(p);
-    else        masked_thin_kernel<D_C, FP8, false><<<dim3(chunks * Z), dim3(MF_THREADS), 0, s>>>(p);
+    const int64_t bytes = p.B * tiles * (MK_TILE * (D_C + 64) * (FP8 ? 1 : 2));
+    if (Z == 1 && bytes >= 64 << 20) masked_thin_kernel<D_C, FP8, true><<<dim3(chunks), dim3(MF_THREADS), 0, s>>>(p);
+    else masked_thin_kernel<D_C, FP8, false><<<dim3(chunks * Z), dim3(MF_THREADS), 0, s>>>(p);
 }
 
-hipError_t launch_masked_thin(const MaskedParams& p, mla_dtype cache, hipStream_t s)
+hipError_t launch_masked_thin(const MaskedParams& p, mla_dtype cache, int64_t tiles, hipStream_t s)
 {
     const unsigned chunks = ((unsigned)p.B * p.num_splits + 7) / 8 * 8, Z = (unsigned)((p.H + MK_THIN_ROWS - 1) / MK_THIN_ROWS);
-    if (cache == MLA_BF16 && p.d_c == 512)      launch<512, false>(p, chunks, Z, s);
-    else if (cache == MLA_BF16)                 launch<256, false>(p, chunks, Z, s);
-    else if (p.d_c == 512)                      launch<512, true>(p, chunks, Z, s);
-    else                                        launch<256, true>(p, chunks, Z, s);
+    if (cache == MLA_BF16 && p.d_c == 512)      launch<512, false>(p, chunks, Z, tiles, s);
+    else if (cache == MLA_BF16)                 launch<256, false>(p, chunks, Z, tiles, s);
+    else if (p.d_c == 512)                      launch<512, true>(p, chunks, Z, tiles, s);
+    else                                        launch<256, true>(p, chunks, Z, tiles, s);
     return hipGetLastError();
 }
 

@@ -106,7 +106,7 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
         p.lse_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.lse_off);
     }
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    hipError_t e = thin ? launch_masked_thin(p, cache, stream) : matrix ? launch_masked_tall(p, cache, stream) : launch_masked_portable(p, io, cache, stream);
+    hipError_t e = thin ? launch_masked_thin(p, cache, tiles, stream) : matrix ? launch_masked_tall(p, cache, stream) : launch_masked_portable(p, io, cache, stream);
     if (e == hipSuccess && plan.S > 1) e = launch_masked_merge(p, o_lat, lse, io, stream);
     return e == hipSuccess ? MLA_OK : MLA_ERR_HIP;
 }

@@ -77,8 +77,8 @@ constexpr int MK_PORTABLE_ROWS = 4;       // query rows of a workgroup
 bool       masked_tall_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache);
 hipError_t launch_masked_tall(const MaskedParams& p, mla_dtype cache, hipStream_t s);
 constexpr int MK_TALL_ROWS = 128;
-// the same with 32 query rows per workgroup, whose wavefronts take the tiles in turn (bf16 caches)
-hipError_t launch_masked_thin(const MaskedParams& p, mla_dtype cache, hipStream_t s);
+// the same with 32 query rows per workgroup, whose wavefronts take the tiles in turn; of what the other one supports
+hipError_t launch_masked_thin(const MaskedParams& p, mla_dtype cache, int64_t tiles, hipStream_t s);
 constexpr int MK_THIN_ROWS = 32;
 // the chunks' results (S > 1) merged
 hipError_t launch_masked_merge(const MaskedParams& p, void* o_lat, float* lse, mla_dtype io, hipStream_t s);

@@ -40,6 +40,15 @@ def test_many_rows_in_chunks(kind, d_c):
     run_tree(kind, [16000, 9000], 20, 28, d_c)
 
 
+@pytest.mark.parametrize("kind, d_c, longest", [("bf16", 512, 14700), ("bf16", 256, 14700), ("fp8", 512, 14700), ("fp8", 256, 29500)])
+def test_few_rows_of_a_large_cache(kind, d_c, longest):
+    """64 MB of rows and more for 32 query rows go past the caches."""
+    (out, lse), c, (q, qr), mask, lens = run_tree(kind, [longest, 3, 9000, 0, 31, 700, 64, 2000], 2, 16, d_c)
+    for _ in range(3):
+        o, l = mla.decode_paged_tree(q, qr, c.kv, c.table, lens, mask, SCALE, kv_scale=c.scale, return_lse=True)
+        assert torch.equal(o, out) and torch.equal(l, lse)
+
+
 @pytest.mark.parametrize("page", [32, 96])
 def test_many_rows_pages(page):
     run_tree("bf16", crowd([95, 96, 97, 300]), 20, 28, page=page)
