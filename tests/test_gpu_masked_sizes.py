@@ -275,3 +275,36 @@ def test_results_off_sixteen_bytes(kind):
         a = mla.decode_paged_window(q, qr, c.kv, c.table, n, wide, wide, SCALE, kv_scale=c.scale)
         b = mla.decode_paged_window(q, qr, c.kv, c.table, n, 2 ** 31 - 1, 0, SCALE, kv_scale=c.scale)
         assert (a.double() - b.double()).abs().max() <= 0.02 * b.double().abs().max()
+
+
+def test_prompts_and_fp8_trees_in_graphs():
+    """Captured once, replayed on changing inputs and lengths beside eager calls: a prompt whose keys are cut into chunks, a tree over an fp8 cache."""
+    T, L = 5, 3000
+    _, c8, (q, qr), mask, lens = run_tree("fp8", [L, 40], T, 28)
+    ws = torch.empty(max(256, mla.decode_tree_workspace_bytes(2, T, 28, 512, c8.table.shape[1] * 64)), dtype=torch.uint8, device=DEV)
+    o8 = torch.empty_like(q)
+    _, _, (qn, pr, UK, UV), c, n = run_prefill([L], 70, 3, 2500, 4, 256)
+    wp = torch.empty(mla.prefill_window_workspace_bytes(1, 70, 3, 256, c.table.shape[1], 2500, 4), dtype=torch.uint8, device=DEV)
+    op, lp = torch.empty_like(qn), torch.empty((1, 70, 3), device=DEV)
+    tree = lambda o: mla.decode_paged_tree(q, qr, c8.kv, c8.table, lens, mask, SCALE, kv_scale=c8.scale, workspace=ws, out=o)
+    prompt = lambda o, l: mla.prefill_window(qn, pr, UK, UV, c.kv, c.table, n, 2500, 4, SCALE, workspace=wp, out=o, lse=l)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        tree(o8), prompt(op, lp)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tree(o8), prompt(op, lp)
+    for step in range(4):
+        q.copy_(queries(2, T, 28, 512, 64, BF, 70 + step)[0])
+        qn.copy_(torch.randn(qn.shape, generator=gen(step), device=DEV))
+        lens.copy_(torch.tensor([L - 131 * step, 40 - step], dtype=torch.int32))
+        n.fill_(L - 67 * step)
+        graph.replay()
+        a, b, l = tree(torch.empty_like(q)), torch.empty_like(qn), torch.empty_like(lp)
+        prompt(b, l)
+        torch.cuda.synchronize()
+        # (bits: lengths that shrink meet rows that were given back and hold NaN)
+        assert torch.equal(a.view(torch.int16), o8.view(torch.int16)), step
+        assert torch.equal(b.view(torch.int16), op.view(torch.int16)) and torch.equal(l.view(torch.int32), lp.view(torch.int32)), step
