@@ -442,7 +442,8 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
             if (lk != 0.f) l += lk * e;
             if (k == w) own = e;
         }
-        f_smem[r][w] = bad_smem[w][r] ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : own / l;
+        // (an infinite score makes the sum infinite where it is not its wavefront's reference: own / l would be 0 for every wavefront, and nothing is multiplied by that)
+        f_smem[r][w] = bad_smem[w][r] || !(l < INFINITY) ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : own / l;
         if (w == 0 && r < HL && p.lse_part) p.lse_part[part_of(r)] = l == 0.f ? -INFINITY : ref * LN2 + __builtin_amdgcn_logf(l) * LN2;
     }
     constexpr int RSO = D_C * 2 + 16;                   // bytes from row to row of half the columns in fp32 (padded)
