@@ -17,7 +17,10 @@
  *
  * A token that sees no row gets zeros and -inf.  A row that a token does not see has
  * no influence on it, whatever the row holds (infinities and NaN included); rows that
- * no token sees need not have a page.  A page id outside the pool where a row would be
+ * no token sees need not have a page.  A token and head whose score with a row that it
+ * sees is NaN or infinite, as with every row that is not finite, gets NaN in all of o_lat
+ * and for lse (the prompts of mla_prefill_window: where that score is -inf, the row counts
+ * for nothing).  A page id outside the pool where a row would be
  * read is not an error code: the rows of that page are seen by nobody.
  */
 #ifndef MLA_MASKED_GFX950_H

@@ -32,7 +32,8 @@
 //
 // Keys that a row does not see get the score -inf, in the tiles that need it.  A key that is not finite has scores that are not: where
 // a wavefront meets one that some row of its own does not see, it clears what is not finite from the transposed tile before
-// it multiplies (0 times infinity would be a NaN), and the rows that do see the key end as NaN.
+// it multiplies (0 times infinity would be a NaN).  The rows that do see the key end as NaN, whichever tile it lies in and whichever way its score
+// goes: their sums become one, and results, log-sum-exps and merged chunks follow from those.
 #include "masked_tile.h"
 #include <type_traits>
 
@@ -239,7 +240,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     }
     if (tree && tid < p.q_len) tree_smem[tid] = tree_word(p, b, tid);
     if (tid < MT_ROWS) token_smem[tid] = (hb + min(tid, HL - 1)) / p.heads;        // (both are read in few tiles)
-    const WholeTiles whole = whole_tiles(p, reach, hb / p.heads, (hb + HL - 1) / p.heads);
+    WholeTiles whole = whole_tiles(p, reach, hb / p.heads, (hb + HL - 1) / p.heads);
     auto seen_whole = [&](int v, uint32_t halves) { return halves == 3 && whole.holds(v); };      // (halves: the tile's bits)
 
     // ---- per-lane state: this lane's queries = column n of the D tiles of the two groups
@@ -274,7 +275,6 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 
     typedef f32x4 Scores[NRB][2];              // [block of 16 keys][query group]: the lane's keys of query n
     f32x4 ksc[NRB];                            // (fp8) scales of this lane's keys
-    bool poisoned[2] = {false, false};         // one of this lane's keys that its query sees was not finite
     bool dirty[NT] = {};                       // one that some query of the wavefront does not see was not, in tile t of the step
 
     // rows of tile v (bit: row) that the lane's query of group hi sees
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
                 for (int i = 0; i < 4; ++i) {
                     const bool bad = !(fabsf(x[2 * t + rb][hi][i]) < INFINITY);
                     if (sees >> (rb * BLOCK_KEYS + i) & 1u) {
-                        poisoned[hi] |= bad;
+                        if (bad) l_run[hi] = __uint_as_float(QUIET_NAN);
                     } else {
                         odd |= bad;
                         x[2 * t + rb][hi][i] = -INFINITY;
@@ -343,28 +343,42 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     };
     // scores of step u, just made: masked.  (fp8: scaled, and their maximum taken as if all were seen, beside the products with the values.
     // 4 sequences of 128k: 1127 us with both here, 1103; in the bf16 forms it costs the registers that keep the queries.)
-    float glanced[2];
+    float glanced[2];                          // (fp8)
+    // A row that is not finite has no score that is, whatever the query (zero times infinity is a NaN); so one query group of one wavefront, another one every
+    // step, meets it for everybody, and then the sweep is done again with every tile masked, which looks at all scores.  (Every wavefront on every step, as the
+    // kernel for few rows does it: 3 - 4 % of a call; so it is 0 at d_c = 512, 2 % at 256.)
+    float odd = 0.f;                           // not zero any more if a score of a step that everybody sees whole was not finite
+    bool some = false;                         // a step that everybody sees whole was there
     auto look_at = [&](Scores& x, int u, uint32_t bits) {
-        if constexpr (!FP8) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (__builtin_expect(!seen_whole(v0 + NT * u + t, bits >> 2 * t & 3), 0)) mask(x, t, v0 + NT * u + t, bits >> 2 * t & 3);
-            raise_top(x);
-            if (unset) set_reference(x);
-            return;
-        }
         bool whole_step = true;
 #pragma unroll
         for (int t = 0; t < NT; ++t) whole_step &= seen_whole(v0 + NT * u + t, bits >> 2 * t & 3);
         if (__builtin_expect(whole_step, 1)) {
+            some = true;
+            if constexpr (FP8) {
 #pragma unroll
-            for (int hi = 0; hi < 2; ++hi) top[hi] = fmaxf(top[hi], glanced[hi]);
+                for (int hi = 0; hi < 2; ++hi) top[hi] = fmaxf(top[hi], glanced[hi]);
+            }
+            if ((u & 3) == wave) {
+                float o[2] = {odd, 0.f};
+#pragma unroll
+                for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[rb & 1] = fmaf(x[rb][0][i], 0.f, o[rb & 1]);
+                odd = o[0] + o[1];
+            }
         } else {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                if (!seen_whole(v0 + NT * u + t, bits >> 2 * t & 3)) mask(x, t, v0 + NT * u + t, bits >> 2 * t & 3);
-            raise_top(x);
+            for (int t = 0; t < NT; ++t) {
+                if (!seen_whole(v0 + NT * u + t, bits >> 2 * t & 3)) {
+                    mask(x, t, v0 + NT * u + t, bits >> 2 * t & 3);
+                    continue;
+                }
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) l_run[hi] = with_least(l_run[hi], x[2 * t][hi], x[2 * t + 1][hi]);
+            }
         }
+        if (!FP8 || !whole_step) raise_top(x);
         if (unset) set_reference(x);
     };
 
@@ -508,7 +522,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
 
     // ---- sweeps over the tiles.  ACCUMULATE against the references (set on the way where they are not yet); if some score exceeded its
     // reference by more than FAST_GAP (rare), a sweep for the exact maxima (it accumulates too, which is not used) and the
-    // accumulation again against them.
+    // accumulation again against them; if one was not finite (rare), the accumulation again.
     enum { ACCUMULATE, MAXIMA, ACCUMULATE_AGAIN };
     auto slot = [&](int u) { return lds + (int)((unsigned)u % RING) * (NT * TILE_B); };
     auto scales_of = [&](int u) { return ks_lds + (FP8 ? (int)((unsigned)u % RING) * (NT * 64) : 0); };
@@ -519,7 +533,6 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
         for (int hi = 0; hi < 2; ++hi) {
             l_run[hi] = 0.f;
             top[hi] = -INFINITY;
-            poisoned[hi] = false;
 #pragma unroll
             for (int ct = 0; ct < NCT; ++ct) oacc[hi][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
@@ -560,8 +573,10 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
             // (an infinite score makes a NaN of its row either way, and no other row shall be the worse for it)
             const bool jumped = (top[0] * sc > m_ref[0] + FAST_GAP && top[0] < INFINITY) || (top[1] * sc > m_ref[1] + FAST_GAP && top[1] < INFINITY);
             wait_vmcnt<0>();     // (fp8: nothing is on its way to the places that are asked for again)
-            if (__builtin_expect(!__syncthreads_or(jumped), 1)) break;
-            pass = MAXIMA;
+            const bool strange = !(odd == 0.f);
+            if (__builtin_expect(!__syncthreads_or(jumped || strange), 1)) break;
+            if (__syncthreads_or(strange)) whole = WholeTiles{0, 0, 0};
+            pass = __syncthreads_or(jumped) ? MAXIMA : ACCUMULATE_AGAIN;      // (against the same references: no bit changes)
             unset = false;
         } else {
             wait_vmcnt<0>();
@@ -585,9 +600,9 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     for (int hi = 0; hi < 2; ++hi) {
         float l = l_run[hi] + __shfl_xor(l_run[hi], 16);
         lt[hi] = l + __shfl_xor(l, 32);
+        // (an infinite query whose scores are all -inf: a sum of zero, though there are rows that it sees)
+        if (!(lt[hi] < INFINITY) || (some && lt[hi] == 0.f)) lt[hi] = __uint_as_float(QUIET_NAN);
         inv[hi] = lt[hi] == 0.f ? 0.f : 1.f / lt[hi];
-        const uint64_t who = __ballot(poisoned[hi]);
-        if ((who | who >> 16 | who >> 32 | who >> 48) >> n & 1u) inv[hi] = __uint_as_float(0x7FC00000u);
     }
     constexpr int RSO = D_C * 2 + 32;           // row stride of the transposed block (padded)
     static_assert(4 * 32 * RSO <= sizeof(smem), "exchange space must fit");

@@ -42,7 +42,6 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
     __shared__ uint64_t tree_smem[64];
     __shared__ float m_smem[4][32], l_smem[4][32];      // reference and normaliser of every wavefront's rows
     __shared__ __attribute__((aligned(16))) float f_smem[32][4];         // and factor
-    __shared__ uint8_t bad_smem[4][32];
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -175,7 +174,6 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 
     // ---- per-lane state: this lane's queries = column n of the D tiles of the two groups
     float m_ref[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
-    bool poisoned[2] = {false, false};
     f32x4 oacc[2][NCT];
     const float sc = fmaxf(fabsf(p.scale) * LOG2E, 1.17549435e-38f);     // (never zero: a masked score is -inf and has to stay it)
 
@@ -206,7 +204,6 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
             l_run[hi] = 0.f;
-            poisoned[hi] = false;
 #pragma unroll
             for (int ct = 0; ct < NCT; ++ct) oacc[hi][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
@@ -297,7 +294,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                         for (int i = 0; i < 4; ++i) {
                             const bool bad = !(fabsf(x[rb][hi][i]) < INFINITY);
                             if (sees >> (rb * BLOCK_KEYS + i) & 1u) {
-                                poisoned[hi] |= bad;
+                                if (bad) l_run[hi] = __uint_as_float(QUIET_NAN);
                             } else {
                                 odd |= bad;
                                 x[rb][hi][i] = -INFINITY;
@@ -319,6 +316,9 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
                             for (int i = 0; i < 4; ++i) ksc[rb][i] = fabsf(ksc[rb][i]) < INFINITY ? ksc[rb][i] : 0.f;
                     }
                 }
+            } else {
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) l_run[hi] = with_least(l_run[hi], x[0][hi], x[1][hi]);
             }
             // ---- weights
 #pragma unroll
@@ -424,11 +424,9 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
     for (int hi = 0; hi < 2; ++hi) {
         float l = l_run[hi] + __shfl_xor(l_run[hi], 16);
         l += __shfl_xor(l, 32);
-        const uint64_t who = __ballot(poisoned[hi]);
         if (g == 0) {
             m_smem[wave][hi * 16 + n] = m_ref[hi];
             l_smem[wave][hi * 16 + n] = l;
-            bad_smem[wave][hi * 16 + n] = (who | who >> 16 | who >> 32 | who >> 48) >> n & 1u;
         }
     }
     __syncthreads();
@@ -443,7 +441,8 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_thin_kernel(MaskedParams
             if (k == w) own = e;
         }
         // (an infinite score makes the sum infinite where it is not its wavefront's reference: own / l would be 0 for every wavefront, and nothing is multiplied by that)
-        f_smem[r][w] = bad_smem[w][r] || !(l < INFINITY) ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : own / l;
+        if (!(l < INFINITY)) l = own = __uint_as_float(QUIET_NAN);
+        f_smem[r][w] = l == 0.f ? 0.f : own / l;
         if (w == 0 && r < HL && p.lse_part) p.lse_part[part_of(r)] = l == 0.f ? -INFINITY : ref * LN2 + __builtin_amdgcn_logf(l) * LN2;
     }
     constexpr int RSO = D_C * 2 + 16;                   // bytes from row to row of half the columns in fp32 (padded)

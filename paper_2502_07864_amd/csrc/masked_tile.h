@@ -133,6 +133,22 @@ __device__ __forceinline__ float max_of(float a, float b, float c)
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
+// minimum of three (likewise)
+__device__ __forceinline__ float min_of(float a, float b, float c)
+{
+    float r;
+    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+// A score of a row that a query row sees which is not finite makes a NaN of the query row's sum, and of its result with it.  NaN and +inf do that by themselves; -inf, whose
+// weight is zero, does it here: the sum plus zero times the least of a tile's scores.
+__device__ __forceinline__ float with_least(float sum, f32x4 a, f32x4 b)
+{
+    const float least = min_of(min_of(min_of(a[0], a[1], a[2]), a[3], b[0]), min_of(b[1], b[2], b[3]), b[3]);
+    return fmaf(least, 0.f, sum);
+}
+constexpr uint32_t QUIET_NAN = 0x7FC00000u;
+
 // maximum over the four lane groups, on every lane
 __device__ __forceinline__ float over_groups(float v)
 {

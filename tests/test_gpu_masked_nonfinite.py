@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2502_07864_amd import mla
-from test_gpu_masked import BF, DEV, SCALE, run_tree
+from test_gpu_masked import DEV, SCALE, run_tree, run_window, window_sees
 from test_gpu_masked_sizes import crowd
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +48,97 @@ def test_an_infinite_score_in_the_middle_of_a_prefix(kind, d_c, flags, which):
         rows[at] = kept
         got, l2 = call()
         assert torch.equal(got, out) and torch.equal(l2, lse)
+
+
+def all_nan(x):
+    return bool(torch.isnan(x.float()).all())
+
+
+# one infinite value: of the latent part, whose score is +inf for some heads and -inf for others, or of the rope part, where the
+# values themselves are finite
+@pytest.mark.parametrize("column", [3, -9])
+@pytest.mark.parametrize("which", CALLS)
+@pytest.mark.parametrize("flags", [0, mla.FLAG_PORTABLE_KERNEL])
+@pytest.mark.parametrize("kind, d_c", [("bf16", 512), ("bf16", 256), ("fp8", 512), ("f32", 512)])
+def test_whoever_sees_an_infinite_row_is_nan_in_any_tile(kind, d_c, flags, which, column):
+    call, out, lse, c, (q, qr), b, n = tree_call(kind, which, flags, d_c)
+    # the first rows, whole tiles, the tile in which the prefix ends
+    for j in (0, 5, n // 2, n - 70, n - 1):
+        at = c.places(b, [j])
+        rows = c.scale.view(-1) if kind == "fp8" else c.kv.view(-1, d_c + 64)[:, column]
+        for what in (math.inf, -math.inf):
+            kept = rows[at].clone()
+            rows[at] = what
+            got, l2 = call()
+            assert all_nan(got[b]) and all_nan(l2[b]), (j, what)
+            others = torch.arange(len(out), device=DEV) != b
+            assert torch.equal(got[others], out[others]) and torch.equal(l2[others], lse[others])
+            rows[at] = kept
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "f32"])
+def test_an_infinite_drafted_row_makes_its_tokens_nan_whole(kind):
+    T, H, prefix = 9, 28, [77, 640]
+    masks = [[(2 << i) - 1 for i in range(T)]] * 2
+    (out, lse), c, (q, qr), mask, lens = run_tree(kind, prefix, T, H, masks=masks)
+    for b in range(2):
+        for k in (0, 4, 8):
+            at = c.places(b, [prefix[b] + k])
+            rows = c.scale.view(-1) if kind == "fp8" else c.kv.view(-1, 576)[:, 3]
+            kept = rows[at].clone()
+            rows[at] = -math.inf
+            got, l2 = mla.decode_paged_tree(q, qr, c.kv, c.table, lens, mask, SCALE, kv_scale=c.scale, return_lse=True)
+            assert all_nan(got[b, k:]) and all_nan(l2[b, k:])
+            assert torch.equal(got[b, :k], out[b, :k]) and torch.equal(l2[b, :k], lse[b, :k]) and torch.equal(got[1 - b], out[1 - b])
+            rows[at] = kept
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "f32"])
+def test_an_infinite_row_in_a_chunk_without_weight(kind):
+    """A row that outweighs all others by more than fp32 holds lies in another chunk."""
+    call, out, lse, c, (q, qr), b, n = tree_call(kind, "few, in chunks")
+    c.put(0, [2900], torch.cat((q[0, 1, 5], qr[0, 1, 5])).float()[None] * 60.0)
+    rows = c.scale.view(-1) if kind == "fp8" else c.kv.view(-1, 576)[:, 3]
+    rows[c.places(0, [40])] = -math.inf
+    got, l2 = call()
+    assert all_nan(got) and all_nan(l2)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("lens, T, H", [([700], 3, 32), (crowd([700], 20), 20, 28)])
+def test_an_infinite_row_under_a_window(kind, lens, T, H):
+    window, sinks = 300, 40
+    (out, lse), c, (q, qr), n = run_window(kind, lens, T, H, window, sinks)
+    b = max(range(len(lens)), key=lambda i: lens[i])
+    rows = c.scale.view(-1) if kind == "fp8" else c.kv.view(-1, 576)[:, 3]
+    for j in (2, 39, 700 - T - window + 1, 700 - T - window + 2, 500, 700 - 2):
+        at = c.places(b, [j])
+        kept = rows[at].clone()
+        rows[at] = -math.inf
+        got, l2 = mla.decode_paged_window(q, qr, c.kv, c.table, n, window, sinks, SCALE, kv_scale=c.scale, return_lse=True)
+        sees = window_sees(lens, T, window, sinks, 700)[b][:, j]
+        assert sees.any() and all_nan(got[b][sees]) and all_nan(l2[b][sees]), j
+        assert torch.equal(got[b][~sees], out[b][~sees]) and torch.equal(l2[b][~sees], lse[b][~sees]), j
+        rows[at] = kept
+
+
+@pytest.mark.parametrize("which", CALLS)
+@pytest.mark.parametrize("flags", [0, mla.FLAG_PORTABLE_KERNEL])
+@pytest.mark.parametrize("kind, d_c", [("bf16", 512), ("bf16", 256), ("fp8", 512), ("fp8", 256), ("f32", 512)])
+def test_an_infinite_query_is_nan_and_nobody_else_is(kind, d_c, flags, which):
+    """Also where all of its scores are -inf: the rows' values at that place have one sign."""
+    call, out, lse, c, (q, qr), b, n = tree_call(kind, which, flags, d_c)
+    if kind == "fp8":
+        codes = c.kv.view(torch.uint8).view(-1, d_c + 64)
+        codes[:, 3] = torch.where((codes[:, 3] & 127) == 127, codes[:, 3], (codes[:, 3] & 127).clamp(min=1))
+    else:
+        c.kv.view(-1, d_c + 64)[:, 3].abs_()
+    ref, l0 = call()
+    kept = q.clone()
+    for t, h, what in ((0, 3, math.inf), (out.shape[1] - 1, out.shape[2] - 1, -math.inf)):
+        q[b, t, h, 3] = what
+        got, l2 = call()
+        assert all_nan(got[b, t, h]) and all_nan(l2[b, t, h])
+        got[b, t, h], l2[b, t, h] = ref[b, t, h], l0[b, t, h]
+        assert torch.equal(got, ref) and torch.equal(l2, l0)
+        q.copy_(kept)
