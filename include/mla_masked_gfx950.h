@@ -34,8 +34,9 @@ extern "C" {
 
 /*
  * Bytes of device workspace mla_decode_paged_tree needs (partial results where a
- * sequence's rows are shared out; 0 for many sizes).  max_rows: page_size *
- * max_pages_per_seq of the call.  Pure host function; 0 if an argument is invalid.
+ * sequence's rows are shared out; 0 for many sizes, at most 640 MB).  max_rows: page_size *
+ * max_pages_per_seq of the call.  Enough for every type and kernel; pure host function; 0 if
+ * an argument is invalid.
  */
 size_t mla_decode_tree_workspace_bytes(int B, int q_len, int heads, int d_c, int max_rows);
 

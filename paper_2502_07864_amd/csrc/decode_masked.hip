@@ -692,7 +692,7 @@ __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedParams p, void*
 bool masked_tall_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache)
 {
     auto on16 = [](const void* q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
-    return io == MLA_BF16 && (cache == MLA_BF16 || cache == MLA_FP8_E4M3) && p.d_rope == 64 && (p.d_c == 256 || p.d_c == 512) &&
+    return io == MLA_BF16 && (cache == MLA_BF16 || cache == MLA_FP8_E4M3) && p.d_rope == 64 && masked_tall_width(p.d_c) &&
            p.page_size % 16 == 0 && (int64_t)p.num_pages * (p.page_size / 16) <= 0x7FFFFFFF && on16(p.q_abs) && on16(p.q_rope) && on16(p.kv);
 }
 

@@ -24,7 +24,12 @@ struct Plan {
     int S;                      // chunks that a sequence's tiles are cut into: those that end first
     double cost;
     size_t lse_off, total;      // of the workspace (S > 1)
+    bool thin;
 };
+
+// Most bytes of partial results.  Where the query rows nearly fill the chip by themselves chunks only even out the last round of workgroups, and would take
+// gigabytes: on 131136 rows 17 sequences of 63 x 32 query rows 9.3 ms with 938 MB, 9.5 with 603; 33 of 64 x 64 34 ms with 1851 MB, 37 with 529, 41 without chunks.
+constexpr size_t MAX_PARTIALS = (size_t)640 << 20;
 
 Plan plan_of(int B, int64_t H, int d_c, int64_t tiles, const Kernel& k)
 {
@@ -34,8 +39,9 @@ Plan plan_of(int B, int64_t H, int d_c, int64_t tiles, const Kernel& k)
         const double rounds = (double)((((int64_t)B * s + 7) / 8 * Z + 31) / 32);
         return rounds * ((double)((tiles + s - 1) / s) * k.tile * wide + k.start) + (s > 1 ? 6.0 + 6e-4 * wide * (double)(B * H) * s : 0.0);
     };
-    Plan p = {1, cost(1), 0, 0};
-    for (int s = 2; s <= MK_MAX_CHUNKS && s <= tiles && B * Z < 4096; ++s)          // (4096: rounds enough; and what is left fits the merge's grid)
+    Plan p = {1, cost(1), 0, 0, false};
+    const int most = (int)std::min<int64_t>({(int64_t)MK_MAX_CHUNKS, tiles, (int64_t)(MAX_PARTIALS / ((size_t)B * H * (d_c + 1) * sizeof(float)))});
+    for (int s = 2; s <= most && B * Z < 4096; ++s)          // (4096: rounds enough; and what is left fits the merge's grid)
         if (const double c = cost(s); c < p.cost * 0.999) {
             p.S = s;
             p.cost = c;
@@ -45,13 +51,23 @@ Plan plan_of(int B, int64_t H, int d_c, int64_t tiles, const Kernel& k)
     return p;
 }
 
+// What a call takes, on the matrix cores or not.  Groups of 32 rows read the tiles again for each (from L2), 128 rows wait longer for theirs: few rows or short
+// chunks of them are better off as groups of 32 (256 rows on 1000 / 16000 / 64000 rows: 24.7, 42, 86 us by 128, 21.9, 34, 66 by 32), many are not
+// (16 x 560 rows on 4000: 116, 192; 2 x 256 on 64000: 101, 112).
+Plan choose(int B, int64_t H, int d_c, int64_t tiles, bool matrix)
+{
+    if (!matrix) return plan_of(B, H, d_c, tiles, PORTABLE);
+    const Plan many = plan_of(B, H, d_c, tiles, TALL);
+    Plan few = plan_of(B, H, d_c, tiles, THIN);
+    few.thin = few.cost < many.cost;
+    return few.thin ? few : many;
+}
+
 size_t workspace_bytes_for(int B, int q_len, int heads, int d_c, int64_t tiles)
 {
-    // (which kernel a call takes hangs on its types, which are not asked for here)
+    // (whether a call runs on the matrix cores hangs on its types, which are not asked for here)
     const int64_t H = (int64_t)q_len * heads;
-    size_t most = 0;
-    for (const Kernel& k : {PORTABLE, THIN, TALL}) most = std::max(most, plan_of(B, H, d_c, tiles, k).total);
-    return most;
+    return std::max(choose(B, H, d_c, tiles, false).total, masked_tall_width(d_c) ? choose(B, H, d_c, tiles, true).total : 0);
 }
 
 bool sizes_ok(int B, int q_len, int heads, int d_c, int max_rows)
@@ -85,18 +101,8 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
     p.H = (int)H;
     const int64_t tiles = most_tiles(p.q_len, (int64_t)p.max_pages * p.page_size, tree, p.window, p.sinks);
     const bool matrix = !(flags & MLA_FLAG_PORTABLE_KERNEL) && masked_tall_supported(p, io, cache);
-    const size_t need = workspace_bytes_for(p.B, p.q_len, p.heads, p.d_c, tiles);
-    if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return MLA_ERR_WORKSPACE;
-    // (either cache type.)  Groups of 32 rows read the tiles again for each (from L2), 128 rows wait longer for theirs: few rows or short chunks of them are better
-    // off as groups of 32 (256 rows on 1000 / 16000 / 64000 rows: 24.7, 42, 86 us by 128, 21.9, 34, 66 by 32), many are not
-    // (16 x 560 rows on 4000: 116, 192; 2 x 256 on 64000: 101, 112).
-    Plan plan = plan_of(p.B, H, p.d_c, tiles, matrix ? TALL : PORTABLE);
-    bool thin = false;
-    if (matrix) {
-        const Plan few = plan_of(p.B, H, p.d_c, tiles, THIN);
-        thin = few.cost < plan.cost;
-        if (thin) plan = few;
-    }
+    const Plan plan = choose(p.B, H, p.d_c, tiles, matrix);
+    if (plan.total && (!workspace || workspace_bytes < plan.total || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return MLA_ERR_WORKSPACE;
     p.num_splits = plan.S;
     if (plan.S == 1) {
         p.o_part = o_lat;
@@ -106,7 +112,7 @@ int masked_call(MaskedParams p, void* o_lat, float* lse, void* workspace, size_t
         p.lse_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.lse_off);
     }
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    hipError_t e = thin ? launch_masked_thin(p, cache, tiles, stream) : matrix ? launch_masked_tall(p, cache, stream) : launch_masked_portable(p, io, cache, stream);
+    hipError_t e = plan.thin ? launch_masked_thin(p, cache, tiles, stream) : matrix ? launch_masked_tall(p, cache, stream) : launch_masked_portable(p, io, cache, stream);
     if (e == hipSuccess && plan.S > 1) e = launch_masked_merge(p, o_lat, lse, io, stream);
     return e == hipSuccess ? MLA_OK : MLA_ERR_HIP;
 }

@@ -74,6 +74,7 @@ __host__ __device__ __forceinline__ int chunk_start(int tiles, int s, int S) { r
 hipError_t launch_masked_portable(const MaskedParams& p, mla_dtype io, mla_dtype cache, hipStream_t s);
 constexpr int MK_PORTABLE_ROWS = 4;       // query rows of a workgroup
 // matrix-core kernel
+inline bool masked_tall_width(int d_c) { return d_c == 256 || d_c == 512; }
 bool       masked_tall_supported(const MaskedParams& p, mla_dtype io, mla_dtype cache);
 hipError_t launch_masked_tall(const MaskedParams& p, mla_dtype cache, hipStream_t s);
 constexpr int MK_TALL_ROWS = 128;

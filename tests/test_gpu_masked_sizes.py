@@ -308,3 +308,12 @@ def test_prompts_and_fp8_trees_in_graphs():
         # (bits: lengths that shrink meet rows that were given back and hold NaN)
         assert torch.equal(a.view(torch.int16), o8.view(torch.int16)), step
         assert torch.equal(b.view(torch.int16), op.view(torch.int16)) and torch.equal(l.view(torch.int32), lp.view(torch.int32)), step
+
+
+def test_a_workspace_of_what_the_calls_own_kernel_needs():
+    """The size is asked for without the types: a call on the matrix cores in one chunk takes any workspace."""
+    q, ws, tree, window = prepared("bf16", 2, 28, (150,))
+    assert ws.numel() > 256               # (the portable kernel would cut the sequences)
+    for call in (tree, window):
+        ref, small = call(workspace=ws), torch.empty(256, dtype=torch.uint8, device=DEV)
+        assert torch.equal(call(workspace=small), ref) and torch.equal(call(workspace=small, out=torch.empty_like(q)), ref)

@@ -136,3 +136,12 @@ def test_windows_past_32_bits_are_wide_ones():
         assert mla.decode_window_workspace_bytes(4, 1, 32, 512, 8192, 64, big) == wide
         assert mla.prefill_window_workspace_bytes(1, 100, 8, 512, 1000, big, big) == mla.prefill_window_workspace_bytes(1, 100, 8, 512, 1000, 64000, 64000)
         assert mla.decode_window_workspace_bytes(4, 1, 32, 512, 8192, -big, 0) == 0
+
+
+def test_workspaces_are_those_of_the_kernels_that_are_used(L):
+    """64 sequences of 63 x 32 query rows fill the chip: no kernel that such a call takes has partial results.  No call's partial results take more than 640 MB."""
+    t, w = L.mla_decode_tree_workspace_bytes, L.mla_decode_window_workspace_bytes
+    assert t(64, 63, 32, 512, 131136) == 0 and w(64, 63, 32, 512, 131136, 1 << 30, 0) == 0
+    for B, T, H, d_c, rows in ((33, 64, 64, 512, 131136), (17, 63, 32, 512, 131136), (15, 64, 128, 512, 1 << 20), (100, 10, 100, 512, 70000), (40, 64, 64, 256, 1 << 18),
+                               (9, 64, 128, 504, 1 << 20), (3000, 1, 1, 512, 1 << 20), (2, 64, 128, 512, 1 << 30)):
+        assert max(t(B, T, H, d_c, rows), w(B, T, H, d_c, rows, 1 << 30, 4)) <= (640 << 20) + 512          # (two parts, each whole 256 bytes)
