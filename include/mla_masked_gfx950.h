@@ -19,8 +19,7 @@
  * no influence on it, whatever the row holds (infinities and NaN included); rows that
  * no token sees need not have a page.  A token and head whose score with a row that it
  * sees is NaN or infinite, as with every row that is not finite, gets NaN in all of o_lat
- * and for lse (the prompts of mla_prefill_window: where that score is -inf, the row counts
- * for nothing).  A page id outside the pool where a row would be
+ * and for lse.  A page id outside the pool where a row would be
  * read is not an error code: the rows of that page are seen by nobody.
  */
 #ifndef MLA_MASKED_GFX950_H
@@ -115,6 +114,9 @@ size_t mla_prefill_window_workspace_bytes(int B, int q_len, int heads, int d_c, 
  * mla_prefill_mha under the mask of mla_decode_paged_window: prompts, or chunks of them,
  * in the MHA paradigm (keys and values materialised per head, for the rows that some token
  * of the call sees and no others).
+ * A row is taken for one that is not finite if a value of its latent part is 2^100 or more
+ * in magnitude; one of which the rope part only is not finite, and whose score is -inf, counts
+ * for nothing.
  *   lse [B, q_len, heads] fp32 (output, may be NULL)
  *   workspace  mla_prefill_window_workspace_bytes bytes, 256-byte aligned; scratch
  * Everything else, the sizes supported included, as for mla_prefill_mha; q_len <= 2^29 and

@@ -385,7 +385,7 @@ int mla_prefill_mha(const void* q_nope, const void* q_rope, const void* W_UK, co
     void* pool2 = ws + wl.pool_off;
     int32_t* lens2 = reinterpret_cast<int32_t*>(ws + wl.lens_off);
     hipError_t e = launch_prefill_materialise(kv_cache, page_table, seq_lens, W_UK, W_UV, ws, pool2, lens2,
-                                              B, q_len, heads, d_c, num_pages, max_pages_per_seq, stream);
+                                              B, q_len, heads, d_c, num_pages, max_pages_per_seq, false, stream);
     if (e != hipSuccess) return MLA_ERR_HIP;
     // the attention: every (sequence, head) pair is a sequence of q_len query rows over its own rows
     PrefillParams p;

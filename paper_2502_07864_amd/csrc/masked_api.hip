@@ -223,7 +223,7 @@ int mla_prefill_window(const void* q_nope, const void* q_rope, const void* W_UK,
     int32_t* lens2 = reinterpret_cast<int32_t*>(ws + wl.lens_off);
     hipError_t e = launch_window_pages(page_table, seq_lens, pages, lens, B, q_len, max_pages_per_seq, width, window, sinks, stream);
     if (e != hipSuccess) return MLA_ERR_HIP;
-    e = launch_prefill_materialise(kv_cache, pages, lens, W_UK, W_UV, ws, ws + wl.pool_off, lens2, B, q_len, heads, d_c, num_pages, width, stream);
+    e = launch_prefill_materialise(kv_cache, pages, lens, W_UK, W_UV, ws, ws + wl.pool_off, lens2, B, q_len, heads, d_c, num_pages, width, true, stream);
     if (e != hipSuccess) return MLA_ERR_HIP;
     PrefillParams p;
     p.q_nope = q_nope; p.q_rope = q_rope; p.pool = ws + wl.pool_off; p.lens = lens2;

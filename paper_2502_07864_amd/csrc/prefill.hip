@@ -27,6 +27,45 @@ typedef __attribute__((ext_vector_type(8))) short s16x8;
 constexpr int PF_DH = 128;      // head dimension
 constexpr int PF_PAGE = 64 * 2 * PF_DH;           // values per materialised page: 64 keys, then the values transposed
 
+// (Under a window) A wavefront's 32 latent rows, 16 per tile nt: a bit for each that is not finite or so large, 2^100 and more, that its values might not be.  The values of such a
+// row are zeros and its keys NaN: whoever sees it is NaN, and whoever does not has no product of the weight zero with an infinity or a NaN in its sums, whatever the row holds.
+// (Weights below 2^17 then give finite values.  Two instructions for two numbers, once for 256 products with each: 4 x 8192 tokens, 32 heads, d_c = 512, 296 us without and
+// 299 with; 8 x 500 tokens, 28 heads, d_c = 256, 58.6, 58.0.  Values cleared by the attention where it met one instead were cleared under the eyes of other wavefronts.)
+struct WildRows {
+    uint32_t in[2];
+    __device__ __forceinline__ bool any() const { return (in[0] | in[1]) != 0; }
+    // all ones for the row of this lane's token in tile nt
+    __device__ __forceinline__ uint32_t mine(int nt, int n) const { return 0u - (in[nt] >> n & 1u); }
+};
+template <int NKS> __device__ __forceinline__ WildRows wild_rows(bf16x8 (&rows)[2][NKS], int n)
+{
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    constexpr uint32_t LARGE = 0x7180u;               // 2^100 in bf16
+    bool wild[2];
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+        u16x2 most = {0, 0};
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+                most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, __builtin_bit_cast(u32x4, rows[nt][ks])[d] & 0x7FFF7FFFu));
+        wild[nt] = most[0] >= LARGE || most[1] >= LARGE;
+    }
+    WildRows w = {{0u, 0u}};
+    if (__builtin_expect(__any(wild[0] || wild[1]), 0)) {
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            const uint64_t who = __ballot(wild[nt]);  // (a row lies in four lanes)
+            w.in[nt] = (uint32_t)(who | who >> 16 | who >> 32 | who >> 48) & 0xFFFFu;
+            const uint32_t keep = ~w.mine(nt, n);
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) rows[nt][ks] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, rows[nt][ks]) & (u32x4){keep, keep, keep, keep});
+        }
+    }
+    return w;
+}
+
 // Weights in LDS: row r (a dimension of the keys or of the values) of d_c values, its 16-byte piece c at position c ^ (r & 15):
 // the 16 lanes that share a cycle of an operand read meet 16 different units.  The values' weights are stored k-major by the caller
 // and are transposed once, at the start, by the transposing LDS read.
@@ -36,7 +75,7 @@ constexpr int PF_PAGE = 64 * 2 * PF_DH;           // values per materialised pag
 // Whole pages per wavefront (eight of them): 149; a wavefront's rows requested a unit ahead: 160 to 200 (registers).
 template <int D_C> constexpr int PM_WAVES = 4096 / D_C;            // wavefronts of a workgroup: 16 / 8
 
-template <int D_C>
+template <int D_C, bool WINDOW>
 __global__ __launch_bounds__(PM_WAVES<D_C> * 64, PM_WAVES<D_C> / 4) void prefill_materialise_kernel(const uint16_t* kv, const int32_t* page_table,
                                                                                const int32_t* seq_lens, const uint16_t* W_UK, const uint16_t* W_UV,
                                                                                uint16_t* pool2, int32_t* lens2,
@@ -178,6 +217,9 @@ __global__ __launch_bounds__(PM_WAVES<D_C> * 64, PM_WAVES<D_C> / 4) void prefill
             }
         }
 
+        WildRows wild = {{0u, 0u}};
+        if constexpr (WINDOW) wild = wild_rows(cb, n);
+
         // 32 dimensions (two row tiles of the weights) x the wavefront's tokens.  Keys: weights as the A operand (a lane ends with four
         // dimensions of a token); values: tokens as the A operand (four tokens of a dimension)
         f32x4 acc[2][NT];
@@ -213,8 +255,11 @@ __global__ __launch_bounds__(PM_WAVES<D_C> * 64, PM_WAVES<D_C> / 4) void prefill
                 product(std::true_type{}, w_keys + c * 32 * WROWB);
                 // 32 dimensions of the tokens: position 8g + 4 ml + i of the 32 is dimension 16 ml + 4g + i
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-                    *reinterpret_cast<u32x4*>(dst + (tok0 + nt * 16 + n) * PF_DH + c * 32 + g * 8) = pack8(acc[0][nt], acc[1][nt]);
+                for (int nt = 0; nt < NT; ++nt) {
+                    u32x4 k = pack8(acc[0][nt], acc[1][nt]);
+                    if (WINDOW && __builtin_expect(wild.any(), 0)) k |= wild.mine(nt, n);
+                    *reinterpret_cast<u32x4*>(dst + (tok0 + nt * 16 + n) * PF_DH + c * 32 + g * 8) = k;
+                }
             }
         }
         if (values) {
@@ -261,7 +306,7 @@ __global__ __launch_bounds__(256) void prefill_weights_kernel(const uint16_t* W_
 // A wavefront owns 32 tokens (two column tiles) and keeps their latent rows in registers.
 // The first weights are asked for before anything else, page and length by scalar loads: 4 x 8192 tokens, 32 heads, d_c = 512
 // 348 -> 333 us (and 11 for the weights' layout); the figures against the kernel above stand at the rule below.
-template <int D_C>
+template <int D_C, bool WINDOW>
 __global__ __launch_bounds__(256, 2) void prefill_stream_kernel(const uint16_t* kv, const int32_t* page_table,
                                                                      const int32_t* seq_lens, const uint16_t* Wcat,
                                                                      uint16_t* pool2, int32_t* lens2,
@@ -346,6 +391,8 @@ __global__ __launch_bounds__(256, 2) void prefill_stream_kernel(const uint16_t* 
             }
         }
     }
+    WildRows wild = {{0u, 0u}};
+    if (WINDOW && in_seq) wild = wild_rows(cb, n);
     for (int c = 0; c < NCHUNK; ++c) {
         // my part of this chunk (requested a chunk ago) is there; the two results stored since may be on their way ...
         if (c > 0 && in_seq) wait_vmcnt<2>();
@@ -390,8 +437,11 @@ __global__ __launch_bounds__(256, 2) void prefill_stream_kernel(const uint16_t* 
                 product(std::true_type{});
                 // 32 dimensions of 32 tokens: position 8g + 4 ml + i of the 32 is dimension 16 ml + 4g + i
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
-                    *reinterpret_cast<u32x4*>(dst + (tok0 + nt * 16 + n) * PF_DH + c * 32 + g * 8) = pack8(acc[0][nt], acc[1][nt]);
+                for (int nt = 0; nt < 2; ++nt) {
+                    u32x4 k = pack8(acc[0][nt], acc[1][nt]);
+                    if (WINDOW && __builtin_expect(wild.any(), 0)) k |= wild.mine(nt, n);
+                    *reinterpret_cast<u32x4*>(dst + (tok0 + nt * 16 + n) * PF_DH + c * 32 + g * 8) = k;
+                }
             } else {
                 product(std::false_type{});
                 // 32 tokens (this wavefront's half page) of 32 dimensions: key 4 nt + i of group g is token 16 nt + 4g + i
@@ -454,9 +504,9 @@ hipError_t launch_prefill_rope(const void* kv, const int32_t* page_table, const 
     return hipGetLastError();
 }
 
-hipError_t launch_prefill_materialise(const void* kv, const int32_t* page_table, const int32_t* seq_lens,
-                                      const void* W_UK, const void* W_UV, void* Wcat, void* pool2, int32_t* lens2, int B, int q_len, int heads, int d_c, int num_pages, int max_pages,
-                                      hipStream_t s)
+template <bool WINDOW>
+static hipError_t materialise(const void* kv, const int32_t* page_table, const int32_t* seq_lens, const void* W_UK, const void* W_UV, void* Wcat, void* pool2, int32_t* lens2,
+                              int B, int q_len, int heads, int d_c, int num_pages, int max_pages, hipStream_t s)
 {
     const uint16_t *rows = static_cast<const uint16_t*>(kv), *uk = static_cast<const uint16_t*>(W_UK), *uv = static_cast<const uint16_t*>(W_UV);
     uint16_t* pool = static_cast<uint16_t*>(pool2);
@@ -483,8 +533,8 @@ hipError_t launch_prefill_materialise(const void* kv, const int32_t* page_table,
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const dim3 grid((max_pages + 1) / 2, B * heads);
-        if (d_c == 512) prefill_stream_kernel<512><<<grid, 256, 0, s>>>(rows, page_table, seq_lens, cat, pool, lens2, heads, num_pages, max_pages);
-        else            prefill_stream_kernel<256><<<grid, 256, 0, s>>>(rows, page_table, seq_lens, cat, pool, lens2, heads, num_pages, max_pages);
+        if (d_c == 512) prefill_stream_kernel<512, WINDOW><<<grid, 256, 0, s>>>(rows, page_table, seq_lens, cat, pool, lens2, heads, num_pages, max_pages);
+        else            prefill_stream_kernel<256, WINDOW><<<grid, 256, 0, s>>>(rows, page_table, seq_lens, cat, pool, lens2, heads, num_pages, max_pages);
         return hipGetLastError();
     }
     // One workgroup per CU (its weights fill the LDS), the same number for every head: of one to eight rounds of them the number
@@ -508,9 +558,17 @@ hipError_t launch_prefill_materialise(const void* kv, const int32_t* page_table,
     // (752) 1002 / 1024.  Not multiples of eight: 28 heads by page 84 -> 91, 4000 x 4 200 -> 201.
     const bool by_page = d_c == 256 && heads % 8 == 0 && heads <= 32 && pages > std::max(160, 6 * heads);
     const dim3 grid = by_page ? dim3(per, kinds) : dim3(kinds, per);
-    if (d_c == 512) prefill_materialise_kernel<512><<<grid, PM_WAVES<512> * 64, 0, s>>>(rows, page_table, seq_lens, uk, uv, pool, lens2, B, heads, num_pages, max_pages, by_page);
-    else            prefill_materialise_kernel<256><<<grid, PM_WAVES<256> * 64, 0, s>>>(rows, page_table, seq_lens, uk, uv, pool, lens2, B, heads, num_pages, max_pages, by_page);
+    if (d_c == 512) prefill_materialise_kernel<512, WINDOW><<<grid, PM_WAVES<512> * 64, 0, s>>>(rows, page_table, seq_lens, uk, uv, pool, lens2, B, heads, num_pages, max_pages, by_page);
+    else            prefill_materialise_kernel<256, WINDOW><<<grid, PM_WAVES<256> * 64, 0, s>>>(rows, page_table, seq_lens, uk, uv, pool, lens2, B, heads, num_pages, max_pages, by_page);
     return hipGetLastError();
+}
+
+hipError_t launch_prefill_materialise(const void* kv, const int32_t* page_table, const int32_t* seq_lens,
+                                      const void* W_UK, const void* W_UV, void* Wcat, void* pool2, int32_t* lens2, int B, int q_len, int heads, int d_c, int num_pages, int max_pages,
+                                      bool window, hipStream_t s)
+{
+    return window ? materialise<true>(kv, page_table, seq_lens, W_UK, W_UV, Wcat, pool2, lens2, B, q_len, heads, d_c, num_pages, max_pages, s)
+                  : materialise<false>(kv, page_table, seq_lens, W_UK, W_UV, Wcat, pool2, lens2, B, q_len, heads, d_c, num_pages, max_pages, s);
 }
 
 }  // namespace mla

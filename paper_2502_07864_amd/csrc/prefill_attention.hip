@@ -50,7 +50,8 @@ constexpr int PA_ROWS = 128;                // query rows per workgroup
 // Roundings: as without a window, keys and values to bf16 when they are materialised and weights before their products.  Each is 1.2 to 1.4e-3 of a
 // result of random inputs, the result's own 1.7e-3, all together 2.8e-3; the bf16 instructions take no more, and halves of weights in two terms would be 2.5e-3 for 40 %
 // more products.  Keys are numbered as the pool has them; where
-// that leaves out pages that no query of the call sees, the windows lie behind the sinks' pages all the same.
+// that leaves out pages that no query of the call sees, the windows lie behind the sinks' pages all the same.  All values in the pool are finite (a row that is
+// not has NaN for its keys): a weight of zero makes zero of each.
 template <bool WINDOW>
 __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(PrefillParams p)
 {
@@ -330,23 +331,6 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
         v = fmaxf(v, __shfl_xor(v, 16));
         return fmaxf(v, __shfl_xor(v, 32));
     };
-    // (WINDOW) A key that a query does not see has the weight zero, but its values may be infinite or NaN (then its scores are, too):
-    // such values become zeros before they are multiplied.  Whoever sees the key has a NaN for its weight, or the weight zero where
-    // the score is -inf.  Every wavefront that met one does this for itself, and it does not matter who comes first.
-    bool dirty = false;
-    auto clean_values = [&](int at) {
-        for (int u = lane; u < V_B / 16; u += 64) {
-            LDS_AS u32x4* unit = (LDS_AS u32x4*)(lds + at + u * 16);
-            u32x4 v = *unit;
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                if ((v[d] & 0x7F80u) == 0x7F80u) v[d] &= 0xFFFF0000u;
-                if ((v[d] & 0x7F800000u) == 0x7F800000u) v[d] &= 0xFFFFu;
-            }
-            *unit = v;
-        }
-        dirty = false;
-    };
     // keys a query must not see (or that are not there) at -inf
     auto mask = [&](Scores& x, int t) {
         // (few tiles take this: what it compares with is worked out here and not kept in registers)
@@ -358,7 +342,6 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
             first = l >> 4 << 2;
             // keys of the tile that the query sees, a bit each; the lane's from bit 0 on
             auto low = [](int k) -> uint32_t { return k <= 0 ? 0u : k >= 32 ? ~0u : (1u << k) - 1u; };
-            float odd = 0.f;
             const int row = row_of(t);
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) {
@@ -368,12 +351,10 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
                 for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        odd = fmaf(x[rb][hi][i], 0.f, odd);                  // (not zero any more if it is infinite or NaN)
                         const uint32_t gone = (uint32_t)__builtin_amdgcn_sbfe((int)unseen, rb * 16 + i, 1), s = __float_as_uint(x[rb][hi][i]);
                         x[rb][hi][i] = __uint_as_float((s & ~gone) | (0xFF800000u & gone));
                     }
             }
-            dirty = __any(!(odd == 0.f));
             return;
         }
 #pragma unroll
@@ -535,11 +516,9 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
             rk(unit, false, 1);
             if (t + 2 < t1) fetch_unit((t >> 1) + 1);
             if (late_values && t + 2 >= t1) drop_late_values(t1 - 1);
-            if (WINDOW && __builtin_expect(dirty, 0)) clean_values((int)unit + V0);
             step(Yes{}, No{}, unit, x, y);
             if (t + 1 >= t1) break;
             look_at(y, t + 1);
-            if (WINDOW && __builtin_expect(dirty, 0)) clean_values((int)unit + V1);
             step(Yes{}, Yes{}, unit, y, x);
             if (t + 2 < t1) look_at(x, t + 2);
             unit = SLOT_B - unit;

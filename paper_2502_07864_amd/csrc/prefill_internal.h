@@ -42,11 +42,11 @@ inline PrefillWs prefill_ws(int B, int heads, int d_c, int max_pages)
 }
 
 bool       prefill_supported(int d_head, int d_c, int d_rope, int page_size, mla_dtype io, mla_dtype cache);
-// materialise [W_UK c | W_UV c] per pair into pool2, and the pairs' lengths
+// materialise [W_UK c | W_UV c] per pair into pool2, and the pairs' lengths.  window: with every value finite
 hipError_t launch_prefill_materialise(const void* kv, const int32_t* page_table, const int32_t* seq_lens,
                                       const void* W_UK, const void* W_UV, void* Wcat, void* pool2, int32_t* lens2,
                                       int B, int q_len, int heads, int d_c, int num_pages, int max_pages,
-                                      hipStream_t s);
+                                      bool window, hipStream_t s);
 // the rope parts of a cache that is not on 16 bytes: copied to dst, page by page of the sequences, [B * max_pages, 64, 64], and their
 // ids there, [B, max_pages] (-1: not in the cache)
 hipError_t launch_prefill_rope(const void* kv, const int32_t* page_table, const int32_t* seq_lens, void* dst, int32_t* ids,

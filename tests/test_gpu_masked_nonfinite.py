@@ -1,12 +1,13 @@
-"""Committed rows that are not finite, in tiles that every token of the call sees whole (tests/test_gpu_masked.py has them in drafted
-rows and at a window's edge): the tokens that see such a row are NaN, on every kernel and whichever tile it lies in."""
+"""Rows that are not finite, in tiles that every token of the call sees whole and in others (tests/test_gpu_masked.py has them in drafted
+rows and at a window's edge): the tokens that see such a row are NaN, on every kernel and whichever tile it lies in; the others keep
+their bits."""
 import math
 
 import pytest
 import torch
 
 from paper_2502_07864_amd import mla
-from test_gpu_masked import DEV, SCALE, run_tree, run_window, window_sees
+from test_gpu_masked import BF, Cache, DEV, SCALE, gen, run_tree, run_window, window_sees
 from test_gpu_masked_sizes import crowd
 
 pytestmark = pytest.mark.gpu
@@ -142,3 +143,68 @@ def test_an_infinite_query_is_nan_and_nobody_else_is(kind, d_c, flags, which):
         got[b, t, h], l2[b, t, h] = ref[b, t, h], l0[b, t, h]
         assert torch.equal(got, ref) and torch.equal(l2, l0)
         q.copy_(kept)
+
+
+# ------------------------------------------------------------------ prompts
+
+# (length, tokens, heads, window, sinks, d_c): keys and values by the kernel that keeps a head's weights and by the one that streams them, keys whole and in chunks
+PROMPTS = [(520, 300, 2, 90, 4, 256), (520, 300, 2, 90, 40, 512), (4500, 130, 2, 4200, 70, 512), (2760, 200, 64, 900, 33, 512), (2760, 200, 64, 900, 33, 256)]
+
+
+def prompt(L, T, H, window, sinks, d_c):
+    g, c = gen(L + d_c), Cache([L], d_c, 64, 64, BF, 3)
+    qn, qr = (torch.randn((1, T, H, d), generator=g, device=DEV).to(BF) for d in (128, 64))
+    UK, UV = ((torch.randn(s, generator=g, device=DEV) * d_c ** -0.5).to(BF) for s in ((H, 128, d_c), (H, d_c, 128)))
+    n = torch.tensor([L], dtype=torch.int32, device=DEV)
+    call = lambda: [x[0] for x in mla.prefill_window(qn, qr, UK, UV, c.kv, c.table, n, window, sinks, SCALE, return_lse=True)]
+    # a row of the first ones, one that only some of the tokens see for its age, one that everybody sees (if the window is wide enough), new ones
+    rows = [1, sinks - 1, L - T - window + T // 2, L - T - window + T - 1, L - window - 3, L - T - 1, L - T + 10, L - T // 2, L - 1]
+    return call, c, (UK, UV), [j for j in dict.fromkeys(rows) if j >= 0], lambda j: window_sees([L], T, window, sinks, L)[0][:, j]
+
+
+@pytest.mark.parametrize("size", PROMPTS)
+@pytest.mark.parametrize("what", [3e38, -2.0 ** 100])
+def test_a_row_whose_values_do_not_fit_reaches_nobody_who_does_not_see_it(size, what):
+    """Its keys are small, and so are the scores: W_UK has little to do with the one large latent.  Its values are past bf16's range."""
+    call, c, (UK, UV), rows, sees = prompt(*size)
+    UK[:, :, 9] = 2.0 ** -120
+    UV[:, 9] = 2.0 ** 40
+    c.kv[:, :, 9] = torch.where(torch.isnan(c.kv[:, :, 9]), c.kv[:, :, 9], torch.zeros_like(c.kv[:, :, 9]))
+    out, lse = call()
+    assert torch.isfinite(out.float()).all()
+    for j in rows:
+        at = c.places(0, [j])
+        c.kv.view(-1, c.kv.shape[2])[at, 9] = what
+        got, l2 = call()
+        s = sees(j)
+        assert torch.equal(got[~s], out[~s]) and torch.equal(l2[~s], lse[~s]), j
+        assert s.any() and all_nan(got[s]) and all_nan(l2[s]), j
+        c.kv.view(-1, c.kv.shape[2])[at, 9] = 0.0
+
+
+@pytest.mark.parametrize("size", PROMPTS)
+@pytest.mark.parametrize("what", [math.inf, -math.inf, math.nan])
+def test_a_latent_that_is_not_finite_reaches_whoever_sees_it(size, what):
+    """Where 32 query rows beside each other all see it and where some do, new rows and old ones."""
+    call, c, _, rows, sees = prompt(*size)
+    out, lse = call()
+    for j in rows:
+        at = c.places(0, [j])
+        kept = c.kv.view(-1, c.kv.shape[2])[at].clone()
+        c.kv.view(-1, c.kv.shape[2])[at, 9] = what
+        s = sees(j)
+        for _ in range(2):
+            got, l2 = call()
+            assert torch.equal(got[~s], out[~s]) and torch.equal(l2[~s], lse[~s]), j
+            assert s.any() and all_nan(got[s]) and all_nan(l2[s]), j
+        c.kv.view(-1, c.kv.shape[2])[at] = kept
+
+
+def test_a_large_latent_below_the_limit_is_a_number():
+    call, c, (UK, UV), rows, sees = prompt(520, 300, 2, 90, 4, 256)
+    UK[:, :, 9] = 2.0 ** -100
+    UV[:, 9] = 2.0 ** -100
+    for j in rows:
+        c.kv.view(-1, 320)[c.places(0, [j]), 9] = 2.0 ** 99
+    out, lse = call()
+    assert torch.isfinite(out.float()).all() and torch.isfinite(lse).all()
