@@ -526,7 +526,9 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
         __syncthreads();         // every wave is done with the units of this sweep
         if (pass == ACCUMULATE_AGAIN) break;
         if (pass == ACCUMULATE) {
-            const bool jumped = top[0] * sc > m_ref[0] + FAST_GAP || top[1] * sc > m_ref[1] + FAST_GAP;
+            // (WINDOW: an infinite score makes a NaN of its query either way, and no other query shall get other references for it)
+            auto jump_of = [&](int hi) { return top[hi] * sc > m_ref[hi] + FAST_GAP && !(WINDOW && top[hi] == INFINITY); };
+            const bool jumped = jump_of(0) || jump_of(1);
             // (a flag per wavefront, where start() puts nothing)
             LDS_AS int* const flags = (LDS_AS int*)(lds + SLOT_B);
             const bool mine = __any(jumped);
@@ -573,7 +575,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
             for (int hi = 0; hi < 2; ++hi)
                 if (hi * 16 + n < nrow)
                     p.lse_part[io_row(hb + my_row + hi * 16) * S + split] =
-                        lacc[hi][0] != 0.f ? (m_ref[hi] + __builtin_amdgcn_logf(lacc[hi][0])) * LN2 : -INFINITY;
+                        lacc[hi][0] != 0.f ? (m_ref[hi] + __builtin_amdgcn_logf(lacc[hi][0])) * LN2 : -INFINITY;      // (infinite: a NaN of the merge)
         }
         return;
     }
@@ -601,7 +603,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
         for (int hi = 0; hi < 2; ++hi)
             if (my_row + hi * 16 < HL)
                 p.lse[io_row(hb + my_row + hi * 16)] =
-                    (WINDOW ? lt[hi] != 0.f : lt[hi] > 0.f) ? (m_ref[hi] + __builtin_amdgcn_logf(lt[hi])) * LN2 : -INFINITY;
+                    WINDOW && !(lt[hi] < INFINITY) ? __uint_as_float(0x7FC00000u) : lt[hi] > 0.f ? (m_ref[hi] + __builtin_amdgcn_logf(lt[hi])) * LN2 : -INFINITY;
     }
 }
 
