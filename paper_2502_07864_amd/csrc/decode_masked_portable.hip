@@ -111,17 +111,14 @@ __global__ __launch_bounds__(64 * PM_WAVES) void masked_portable_kernel(MaskedPa
         for (int h = 0; h < PM_HG; ++h) {
             // scores of the four rows, on every lane
             float s[PM_ROWS], tm = -INFINITY;
-            bool seen[PM_ROWS], finite = true;
+            bool seen[PM_ROWS];
 #pragma unroll
             for (int r = 0; r < PM_ROWS; ++r) {
                 const float d = wave_sum(dot4(q[h][2], x[r][2], dot4(q[h][1], x[r][1], dot4(q[h][0], x[r][0], 0.f))));
                 seen[r] = ((there >> r) & 1u) && visible(h, jb + r);
-                const float unscaled = d * lane_value(scale, r);
-                if (seen[r]) finite &= fabsf(unscaled) < INFINITY;
-                s[r] = seen[r] ? unscaled * p.scale : -INFINITY;
+                s[r] = seen[r] ? d * lane_value(scale, r) * p.scale : -INFINITY;
                 tm = fmaxf(tm, s[r]);
             }
-            if (!finite) l[h] = __uint_as_float(0x7FC00000u);  // (and whatever is added to it; -inf alone would have the weight zero)
             const float top = fmaxf(m[h], tm);
             const float ref = top == -INFINITY ? 0.f : top;    // (scores of -inf have no weight, a NaN stays one)
             if (top != m[h]) {
@@ -135,7 +132,7 @@ __global__ __launch_bounds__(64 * PM_WAVES) void masked_portable_kernel(MaskedPa
             for (int r = 0; r < PM_ROWS; ++r) {
                 if (!seen[r]) continue;                        // (uniform)
                 const float e = expf(s[r] - ref), w = e * lane_value(scale, r);
-                l[h] += e;
+                l[h] = fmaf(s[r], 0.f, l[h] + e);              // (a NaN for good where the score is infinite: -inf alone would have the weight zero)
                 add4(acc[h][0], w, x[r][0]);
                 add4(acc[h][1], w, x[r][1]);
             }
