@@ -12,19 +12,19 @@
 // instructions; so it is 68 x 17 + 16 x 26 + 8 x 17 = 1708.
 //
 // A step scores tile i + 1 (and weighs tile i between its matrix instructions), then accumulates tile i (and transposes tile
-// i + 1), while tile i + 2 is on its way (direct-to-LDS loads).  Two slots for tiles and two for their transposes: 136 KB of LDS at
-// d_c = 512, one workgroup per CU; at d_c = 256 a step is two tiles.  A bf16 tile waits for all loads at once; an fp8 one is half as
-// wide, so that three slots fit and two are on their way, waited for by count.
+// i + 1), while tile i + 2 is on its way (direct-to-LDS loads).  Two slots for tiles and two for their transposes, and the queries' last k-steps, which the registers do
+// not hold: 153 KB (fp8: 152) of the CU's 160 KB of LDS at d_c = 512, one workgroup per CU; at d_c = 256 a step is two tiles, 145 and 127 KB.  A bf16 tile waits for all
+// loads at once; an fp8 one is half as wide, so that three slots fit and two are on their way, waited for by count.
 //
 // fp8 codes stay in LDS as they are and are widened to bf16, which is exact, where they are read: the keys beside the matrix instructions of the
 // 32 dimensions before, the values once, when their tile is transposed.  The row's scale goes to the scores and the weights.  (Widened on the way into LDS, through
 // registers, 31 tokens x 32 heads on 4 x 131072 rows took 1678 us.)
 //
-// Measured (whole calls): that case 1074 us, 1.05 PFLOP/s; 16 x 32 on 16 x 8192 bf16 rows 162 us, 0.90; 63 x 28 on 64 sequences of 512 .. 4096 rows at
-// d_c = 256 352 us, 0.74; a large library product reaches 1.35.  Bound by the one wavefront per SIMD that the registers leave: matrix pipes busy 31 to
-// 44 % of the cycles, the wavefronts issue 50 to 61 % of theirs, and wait for tiles, LDS and barriers 20 to 25 %.  What had most weight on the way: no
-// spilled register may be read back in the loop, since the wait for it is a wait for the tiles requested before it.  Not taken, for they were slower: two steps
-// unrolled (the sums move between register files), more keys read ahead, the scores' maximum beside the value products in the bf16 forms.
+// Measured (whole calls of a running server; the first dozen are some 10 % slower): that case 1068 us, 1.06 PFLOP/s; 16 x 32 on 16 x 8192 bf16 rows 162 us, 0.90; 63 x 28 on
+// 64 sequences of 512 .. 4096 rows at d_c = 256 361 us, 0.73; a large library product reaches 1.35.  Bound by the one wavefront per SIMD that the registers leave: matrix pipes busy 30 to
+// 44 % of the cycles, the wavefronts issue 50 to 61 % of theirs, and wait for tiles, LDS and barriers 21 to 25 %.  What had most weight on the way: no
+// spilled register may be read back in the loop, since the wait for it is a wait for the tiles requested before it.  Not
+// taken, for they were slower: two steps unrolled (the sums move between register files), more keys read ahead, the scores' maximum beside the value products in the bf16 forms.
 //
 // The reference of a query row's exponentials is the maximum of the first tile with a row it sees, and nothing is rescaled; where a
 // score exceeds it by more than 2^64 the chunk is done again against the exact maxima.  The normaliser sums the weights before
@@ -65,6 +65,7 @@ __global__ __launch_bounds__(MF_THREADS, 1) void masked_tall_kernel(MaskedParams
     __shared__ __attribute__((aligned(16))) float ks_smem[FP8 ? RING : 1][NT * 2][32];     // (fp8) scales of a step's rows, the 16 of a half tile twice
     __shared__ uint64_t tree_smem[64];
     __shared__ int token_smem[MT_ROWS];
+    static_assert(sizeof(smem) + sizeof(ks_smem) + sizeof(tree_smem) + sizeof(token_smem) <= 160 * 1024, "LDS of a CU");
     LDS_AS unsigned char* lds = (LDS_AS unsigned char*)smem;
     LDS_AS float* ks_lds = (LDS_AS float*)ks_smem;
 

@@ -8,8 +8,9 @@
 // further on and (the first lanes) four of the rope part: the same registers serve score and sum.  A running softmax per wavefront,
 // joined over the four at the end.  What a row that a token does not see holds is never multiplied, not even by zero.
 //
-// Bound by vector instructions: 38 for a row and a query row, of which 20 are products (the sum over the wavefront takes seven).  8 tokens x 32 heads on
-// 4 x 4096 rows in fp32: 558 us, 16 TFLOP/s; the same in bf16 and pages of 8 rows 849 (the matrix cores' kernels: 36).
+// Bound by vector instructions and, with two wavefronts per SIMD, by the waits for rows between them: 57 for a row and a query row, of which 20 are products (the sum over the wavefront
+// takes seven, exponentials and masks most of the rest).  8 tokens x 32 heads on 4 x 4096 rows in fp32: 561 us, 16 TFLOP/s, vector pipes busy 72 % of the time, wavefronts waiting for data
+// 37 % of theirs; the same in bf16 and pages of 8 rows 684, 50 % and 59 % (the matrix cores' kernels in pages of 16: 34).
 #include "masked_internal.h"
 #include <type_traits>
 

@@ -12,8 +12,9 @@
 // A small call is bound by round trips (length, page, tile, and one for whatever of the code comes first: what runs once is kept short,
 // loops instead of their copies).
 //
-// Measured: 64 sequences x 32 rows under a window of 4096 71 us a call, 307 MB, 4.8 TB/s in the kernel (past the caches; 82 with whole tiles asked for at the end of the
-// last one and through them); a window of 4096 of one sequence 16 us in the kernel, of which 4 are the join; 256 rows on 1000 cached ones 18, where the kernel for many rows takes 20.  fp8: 16 sequences of 64000 rows, 32
+// Measured: 64 sequences x 32 rows under a window of 4096 70 us a call, 307 MB, 4.5 to 4.7 TB/s in the kernel (past the caches; 82 with whole tiles asked for at the end of the
+// last one and through them); a window of 4096 of one sequence 16 us in the kernel, of which 4 are the join (the kernel for plain decode, whose wavefronts share every tile and
+// have nothing to join, takes 8 for as many rows); 256 rows on 1000 cached ones 18, where the kernel for many rows takes 20.  fp8: 16 sequences of 64000 rows, 32
 // query rows, 116 us a call, 5.1 TB/s (on the kernel for many rows 292); bf16 193 us, 6.1 TB/s.
 //
 // References of the exponentials, masks and keys that are not finite: as in the kernel for many rows (decode_masked.hip), but that a

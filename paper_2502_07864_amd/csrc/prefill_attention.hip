@@ -45,8 +45,9 @@ constexpr int PA_ROWS = 128;                // query rows per workgroup
 
 // WINDOW: a query sees the keys of its window and the first ones only (p.window, p.sinks), and a workgroup meets the pages that its
 // queries see: the sinks' and, behind a jump, those from the first query's window on, in p.splits chunks where whole ones leave CUs idle.  4 prompts of 8192
-// tokens, 32 heads, under 1024: 881 us for 36 to 38 tiles a workgroup, matrix pipes busy 43 %, vector instructions 44 % (ten of the tiles are masked for
-// some wavefront, and start and end weigh more than under the causal mask); 2 x 136 tokens on 10539 under 4096 58 us in four chunks, 113 in one.
+// tokens, 32 heads, under 1024: 862 us for 36 to 38 tiles a workgroup, matrix pipes busy 43 %, vector instructions 43 % (ten of the tiles are masked for
+// some wavefront, each with a spilled register read back behind the next page's loads, and start and end weigh more than under the causal mask); 2 x 136 tokens on 10539
+// under 4096 58 us in four chunks, 113 in one.
 // Roundings: as without a window, keys and values to bf16 when they are materialised and weights before their products.  Each is 1.2 to 1.4e-3 of a
 // result of random inputs, the result's own 1.7e-3, all together 2.8e-3; the bf16 instructions take no more, and halves of weights in two terms would be 2.5e-3 for 40 %
 // more products.  Keys are numbered as the pool has them; where
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(MF_THREADS, 2) void prefill_attention_kernel(Prefil
                      :: "s"(dst), "v"(off), "s"(base), "i"(decltype(at)::value) : "memory", "scc");
     };
     // (WINDOW: one register for the places of all pieces, their distances in the base; its masks want the others, and a reload of a spilled
-    // one waits for every load before it)
+    // one in every step would wait for every load before it)
     auto fetch_keys = [&](const unsigned char* src, uint32_t dst, auto at) {
         load16(src, koff[0], dst, at);
         load16(WINDOW ? src + 4096 : src, koff[WINDOW ? 0 : 1], dst, std::integral_constant<int, decltype(at)::value + 4096>{});
