@@ -36,8 +36,6 @@ __host__ __device__ __forceinline__ int visible_rows(const DecodeParams& p, int 
     return L - (p.q_len - 1 - h / p.heads);
 }
 
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
 struct MergeParams {
     const void* o_part;    // partial outputs in the io dtype (see DecodeParams)
     const float* lse_part;

@@ -25,6 +25,8 @@ struct PrefillParams {
     float* lse_part = nullptr;  // [B, q_len, heads, splits]
 };
 
+inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
 // The workspace.  (Sized for keys with their rope part and a page table for every pair, as callers have sized it: the keys and values
 // take four fifths of the pool's room, and rope parts that have to be copied, once for all heads, and their ids what they leave.)
 struct PrefillWs {
