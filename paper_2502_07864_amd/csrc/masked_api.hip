@@ -40,7 +40,8 @@ Plan plan_of(int B, int64_t H, int d_c, int64_t tiles, const Kernel& k)
         return rounds * ((double)((tiles + s - 1) / s) * k.tile * wide + k.start) + (s > 1 ? 6.0 + 6e-4 * wide * (double)(B * H) * s : 0.0);
     };
     Plan p = {1, cost(1), 0, 0, false};
-    const int most = (int)std::min<int64_t>({(int64_t)MK_MAX_CHUNKS, tiles, (int64_t)(MAX_PARTIALS / ((size_t)B * H * (d_c + 1) * sizeof(float)))});
+    // (in floating point: sizes may be asked for that no call has)
+    const int most = (int)std::min({(double)MK_MAX_CHUNKS, (double)tiles, (double)MAX_PARTIALS / ((double)B * (double)H * ((double)d_c + 1.0) * sizeof(float))});
     for (int s = 2; s <= most && B * Z < 4096; ++s)          // (4096: rounds enough; and what is left fits the merge's grid)
         if (const double c = cost(s); c < p.cost * 0.999) {
             p.S = s;

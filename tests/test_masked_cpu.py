@@ -145,3 +145,11 @@ def test_workspaces_are_those_of_the_kernels_that_are_used(L):
     for B, T, H, d_c, rows in ((33, 64, 64, 512, 131136), (17, 63, 32, 512, 131136), (15, 64, 128, 512, 1 << 20), (100, 10, 100, 512, 70000), (40, 64, 64, 256, 1 << 18),
                                (9, 64, 128, 504, 1 << 20), (3000, 1, 1, 512, 1 << 20), (2, 64, 128, 512, 1 << 30)):
         assert max(t(B, T, H, d_c, rows), w(B, T, H, d_c, rows, 1 << 30, 4)) <= (640 << 20) + 512          # (two parts, each whole 256 bytes)
+
+
+def test_workspaces_of_sizes_that_no_call_has(L):
+    """Products past 64 bits: a size, whatever it is, and no arithmetic exception."""
+    big = 2 ** 31 - 1
+    for B, T, H, d_c, rows in ((1 << 20, 1, 8192, big, big), (big, 1, 1, big, big), (big, 64, 128, big, 1), (1, 1, 1, big, big), (65536, 1, 8192, big, 1 << 30)):
+        assert L.mla_decode_tree_workspace_bytes(B, T, H, d_c, rows) <= (640 << 20) + 512
+        assert L.mla_decode_window_workspace_bytes(B, T, H, d_c, rows, big, big) <= (640 << 20) + 512
